@@ -85,6 +85,23 @@ typedef struct {
   int64_t kv_stride_tok, kv_stride_head;  /* K[g*kv_stride_head + j*kv_stride_tok + c], same for V */
 } focus_shape;
 
+/* ---- 8-bit K/V cache (no counterpart in the paper: a deployment variant of its bf16 cache) --------------------
+ * K and V are held as 8-bit codes with one float scale per token and KV head; a stored element stands for
+ * code * scale.  The scale of a row x is max|x| / Q, its codes are the numbers of the format nearest to x / scale
+ * (quotient rounded to float first; ties to even), so the largest element is always representable.
+ *   FOCUS_KV_INT8  Q = 127, codes -127 .. 127: steps of equal size, error at most scale / 2
+ *   FOCUS_KV_E4M3  Q = 448, 8-bit floats (4 exponent, 3 fraction bits): error at most 2^-4 of the element
+ * Codes lie as K/V do, [Hkv, L, d] by the shape's kv strides (an element is one byte; strides must be multiples of
+ * 16 bytes, base pointers 16-byte aligned); scales are float, token j of KV head g at [g * scale_stride_head + j].
+ * shape.dtype is the type on the other side: of the rows written, the rows read back, Q and O. */
+typedef enum { FOCUS_KV_INT8 = 0, FOCUS_KV_E4M3 = 1 } focus_kv_format;
+typedef struct {
+  int32_t format;                  /* focus_kv_format */
+  void* K; void* V;                /* codes, 8 bits each (device) */
+  float* K_scale; float* V_scale;  /* scales (device) */
+  int64_t scale_stride_head;       /* in floats, >= L; 0 => L */
+} focus_quant_cache;
+
 /* ---- context ------------------------------------------------------------------------------- */
 
 /* Creates a context on `device` and allocates its workspace (workspace_bytes == 0: 256 MiB) and a
@@ -275,6 +292,22 @@ focus_status focus_dense_attn(focus_ctx* ctx, const focus_shape* shape, const vo
                               const int32_t* q_rows, const int32_t* n_rows, int32_t max_rows,
                               const void* K, const void* V, void* O, float* lse, focus_stream stream);
 
+/* focus_sparse_attn and focus_dense_attn over an 8-bit cache: the same rows, key sets, outputs and layouts, with K and
+ * V taken from `cache`.  Codes enter the tensor cores as they are (fp16 holds every code of both formats); the scales
+ * are applied to the logits and to the softmax numerators in fp32, so nothing is rounded between the cache and the
+ * products.  A row with no key to attend (empty lists, no sinks, M == L) gives O = 0 and lse = -inf.  Errors as
+ * there; INVALID_ARG also for an unknown format or a misaligned cache.
+ * The codes of every attended token and the scales must be finite. */
+focus_status focus_sparse_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q, int32_t q_base,
+                                         int32_t n_q, const int32_t* q_rows, const int32_t* n_rows, int32_t max_rows,
+                                         const focus_quant_cache* cache, int32_t head_reduce,
+                                         const int32_t* block_idx, int32_t max_blocks, const int32_t* block_cnt,
+                                         const int32_t* sink_idx, const uint8_t* sink_keep, int32_t n_sink,
+                                         void* O, float* lse, focus_stream stream);
+focus_status focus_dense_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q, int32_t q_base,
+                                        int32_t n_q, const int32_t* q_rows, const int32_t* n_rows, int32_t max_rows,
+                                        const focus_quant_cache* cache, void* O, float* lse, focus_stream stream);
+
 /* ---- closing the decoding loop around the attention path ------------------------------------------ */
 
 /* Eq. 2: for each listed position, the predicted token argmax_v p(v) (lowest v on ties; NaN logits count as
@@ -290,6 +323,28 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
                               int32_t pos_base, int32_t n_pos, const int32_t* rows, const int32_t* n_rows,
                               int32_t max_rows, float* conf, int32_t* token, focus_stream stream);
 
+/* Eq. 2 with a drawn token in place of the argmax (the paper decodes greedily; its models' own samplers have these
+ * four knobs): for each listed position one token is drawn from its logits row x by a given uniform number.
+ *   weights   w_v = exp((x_v - max x) / temperature); NaN and -inf logits have no weight, +inf logits share it all
+ *   kept set  the tokens in descending order of x (ties: lower v), cut to the first top_k (0: no cut), to the
+ *             shortest prefix that holds at least top_p of the weight left by top_k (1: no cut), and to those with
+ *             w_v >= min_p (0: no cut); at least one token stays
+ *   token     the first kept v, in ascending v, whose running sum of kept weights exceeds u * their total; weights
+ *             and sums are held in 64 bits, so that the token is the one the definition names
+ *   conf      w_token / total: its probability in the distribution it was drawn from
+ *   prob      (may be NULL) softmax_v(x)[token] at temperature 1 over the whole vocabulary: Eq. 2's confidence
+ *   n_kept    (may be NULL) int32, size of the kept set
+ * logits, rows and output layout as for focus_confidence; u float[max_rows], u[r] in [0, 1) belongs to row r.  Rows
+ * beyond n_rows get token -1, conf 0, prob 0, n_kept 0; so does a row without a finite or +inf logit, and a row whose
+ * position or u is out of range, which is reported through the status word.
+ * Requires temperature > 0 (finite; for temperature 0 call focus_confidence), top_k >= 0, 0 < top_p <= 1,
+ * 0 <= min_p <= 1; vocab at most 800 000 (bf16) / 400 000 (f32), else UNSUPPORTED.  One launch, no workspace. */
+focus_status focus_sample(focus_ctx* ctx, const void* logits, int32_t dtype, int64_t row_stride, int32_t vocab,
+                          int32_t pos_base, int32_t n_pos, const int32_t* rows, const int32_t* n_rows,
+                          int32_t max_rows, float temperature, int32_t top_k, float top_p, float min_p,
+                          const float* u, float* conf, int32_t* token, float* prob, int32_t* n_kept,
+                          focus_stream stream);
+
 /* Eq. 3; Algorithm 1, the cache-update step of the non-block-entry branch: the key and value states computed this
  * step for the listed positions replace the cached rows; every other row keeps its cached state.
  *   K_cache, V_cache  [Hkv, L, d] by the shape's strides (updated in place)
@@ -300,6 +355,33 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
 focus_status focus_update_kv(focus_ctx* ctx, const focus_shape* shape, void* K_cache, void* V_cache,
                              const void* K_new, const void* V_new, const int32_t* rows, const int32_t* n_rows,
                              int32_t max_rows, focus_stream stream);
+
+/* Eq. 3 into an 8-bit cache: the key and value states computed this step are quantised as they are written; every
+ * other row keeps its codes and scale.
+ *   K_new, V_new  row r, KV head g at [r * new_stride_row + g * new_stride_head], dtype shape.dtype (the K and V parts
+ *                 of a fused projection's rows, for instance); strides in elements, multiples of 8.  Either may be
+ *                 NULL: that half of the cache is left alone
+ *   rows          int32[max_rows] positions, strictly ascending, with n_rows int32[1] (device), or both NULL:
+ *                 positions pos_base .. pos_base + max_rows - 1 (a prompt, a block entry)
+ * NaN elements count as 0, infinite ones take the largest code; neither enters the scale.  A row whose largest
+ * magnitude is below 2^-80 is stored as zeros with scale 0.  Rows listed outside [0, L) or out of order are skipped
+ * and reported through the status word. */
+focus_status focus_quantize_kv(focus_ctx* ctx, const focus_shape* shape, const void* K_new, const void* V_new,
+                               int64_t new_stride_row, int64_t new_stride_head, int32_t pos_base, const int32_t* rows,
+                               const int32_t* n_rows, int32_t max_rows, const focus_quant_cache* cache,
+                               focus_stream stream);
+
+/* Reads rows of an 8-bit cache back: out = code * scale, rounded once to shape.dtype.  With contiguous [Hkv, L, d]
+ * strides the result is what focus_pool_keys, focus_find_sinks and focus_score_blocks take as K.
+ *   K_out, V_out  row r, KV head g at [r * out_stride_row + g * out_stride_head] (strides in elements, multiples of
+ *                 8); either may be NULL
+ *   rows          int32[max_rows] positions in any order with n_rows int32[1] (device), or both NULL: positions
+ *                 pos_base .. pos_base + max_rows - 1.  Output rows beyond n_rows, and those of positions outside
+ *                 [0, L) (reported through the status word), are left as they were. */
+focus_status focus_dequantize_kv(focus_ctx* ctx, const focus_shape* shape, const focus_quant_cache* cache,
+                                 int32_t pos_base, const int32_t* rows, const int32_t* n_rows, int32_t max_rows,
+                                 void* K_out, void* V_out, int64_t out_stride_row, int64_t out_stride_head,
+                                 focus_stream stream);
 
 /* Incremental maintenance of the pooled keys after focus_update_kv (Eq. 3 applied to prompt rows, e.g. at a
  * block-entry refresh; K-bar_b of "Block-wise token pruning"): K-bar[g, b, :] is recomputed for exactly the prompt

@@ -24,6 +24,9 @@ Functions and the passages they follow
   update_kv        "Approximate KV cache in dLLMs", Eq. 3: refreshed rows replace the cached ones.
   commit_step      Algorithm 1, the state update that ends a step, with the unmasking rule stated right after Eq. 2:
                    the most confident masked positions receive their predicted tokens, the rest stay masked.
+Beside the paper (deployment variants of its cache and its decoding rule, stated in include/focus.h)
+  quantize_rows    rows as 8-bit codes with one scale each, and the numbers the codes stand for.
+  sample_token     one token of a logits row by temperature, top-k, top-p, min-p and a uniform number.
 
 Readings where the paper leaves a choice (parity unpinned by the paper for these):
   * Eq. 6 writes one softmax over an "aggregated query representation"; here every
@@ -273,3 +276,70 @@ def commit_step(conf: np.ndarray, masked: np.ndarray, x: np.ndarray, pos: Sequen
         x[p] = token_new[row_of[p]]
         masked[p] = 0
     return conf, masked, x, picks
+
+
+# ---- 8-bit cache, sampling (no counterpart in the paper) --------------------------------------------
+def quantize_rows(x: np.ndarray, fmt: str) -> Tuple[np.ndarray, np.ndarray]:
+    """x [..., d] -> (code values [..., d], scales [...]).  scale = max|x| / Q over the finite elements, 0 if that maximum
+    is below 2^-80; code = the format's number nearest to float32(x / scale), ties to even; NaN -> 0, infinities -> +-Q."""
+    x = np.asarray(x, dtype=np.float64)
+    top = {"int8": 127.0, "e4m3": 448.0}[fmt]
+    amax = np.where(np.isfinite(x), np.abs(x), 0.0).max(-1)
+    scale = np.where(amax < 2.0 ** -80, 0.0, (amax / top).astype(np.float32).astype(np.float64))
+    code = np.zeros_like(x)
+    # the numbers of the format, non-negative, ascending (e4m3: exponent field 0 is subnormal, 1111.111 is NaN)
+    if fmt == "int8":
+        grid = np.arange(0, 128, dtype=np.float64)
+    else:
+        grid = np.array([(m / 8.0) * 2.0 ** -6 if e == 0 else (1 + m / 8.0) * 2.0 ** (e - 7)
+                         for e in range(16) for m in range(8)][:-1])
+    for ix in np.ndindex(*x.shape[:-1]):
+        if scale[ix] == 0.0:
+            continue
+        row = np.where(np.isnan(x[ix]), 0.0, x[ix])
+        with np.errstate(over="ignore"):
+            q = (row / scale[ix]).astype(np.float32).astype(np.float64)
+        a = np.minimum(np.abs(q), top)
+        hi = np.minimum(np.searchsorted(grid, a), len(grid) - 1)
+        lo = np.maximum(hi - 1, 0)
+        up, down = grid[hi] - a, a - grid[lo]
+        pick = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)      # ties: even place in the grid
+        pick = np.where(grid[hi] == a, hi, pick)
+        code[ix] = np.sign(q) * grid[pick]
+    return code, scale
+
+
+def sample_token(x: np.ndarray, temperature: float, top_k: int, top_p: float, min_p: float, u: float):
+    """(token, its probability in the kept distribution, its probability in softmax(x), size of the kept set)."""
+    x = np.asarray(x, dtype=np.float64)
+    cand = [v for v in range(len(x)) if not np.isnan(x[v]) and x[v] != -np.inf]
+    if not cand:
+        return -1, 0.0, 0.0, 0
+    m = max(x[v] for v in cand)
+
+    def weight(v, t):
+        return 1.0 if x[v] == m else (0.0 if m == np.inf else math.exp((x[v] - m) / t))
+
+    order = sorted(cand, key=lambda v: (-x[v], v))
+    w = [weight(v, temperature) for v in order]
+    k = min(top_k, len(order)) if top_k > 0 else len(order)
+    n = k
+    if top_p < 1.0:
+        target = top_p * math.fsum(w[:k])
+        run, n = 0.0, 0
+        while n < k and run < target:
+            run = math.fsum(w[:n + 1]) if n < 64 else run + w[n]
+            n += 1
+        n = max(n, 1)
+    n = min(n, sum(1 for a in w if a >= min_p)) if min_p > 0.0 else n
+    kept = sorted(order[:n])
+    total = math.fsum(weight(v, temperature) for v in kept)
+    run, tok = 0.0, None
+    for v in kept:
+        run += weight(v, temperature)
+        if weight(v, temperature) > 0.0:
+            tok = v
+        if run > u * total:
+            break
+    z = math.fsum(weight(v, 1.0) for v in cand)
+    return tok, weight(tok, temperature) / total, weight(tok, 1.0) / z, n

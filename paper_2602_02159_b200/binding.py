@@ -16,6 +16,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_CUDA, ERR_TIM
 F32, BF16 = 0, 1
 HEADS_PER_KV_GROUP, HEADS_ALL = 0, 1
 SINK_TOKENS, SINK_BLOCKS = 0, 1
+KV_INT8, KV_E4M3 = 0, 1
 OPT_MERGE_MODE, OPT_NO_WIDE, OPT_NO_PDL = 0, 1, 2
 MERGE_AUTO, MERGE_COUNTERS, MERGE_KERNEL = 0, 1, 2
 
@@ -33,9 +34,15 @@ class focus_shape(C.Structure):
                 ("kv_stride_tok", C.c_int64), ("kv_stride_head", C.c_int64)]
 
 
+class focus_quant_cache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p),
+                ("V_scale", C.c_void_p), ("scale_stride_head", C.c_int64)]
+
+
 _lib = None
 _P, _I, _Z = C.c_void_p, C.c_int32, C.c_size_t
 _SH = C.POINTER(focus_shape)
+_QC, _F = C.POINTER(focus_quant_cache), C.c_float
 
 _SIGS = {
     "focus_create": (_I, [C.POINTER(_P), C.c_int, _Z]),
@@ -63,6 +70,11 @@ _SIGS = {
     "focus_update_kv": (_I, [_P, _SH, _P, _P, _P, _P, _P, _P, _I, _P]),
     "focus_update_pooled_keys": (_I, [_P, _SH, _P, _P, _P, _P, _I, _P]),
     "focus_commit_step": (_I, [_P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P]),
+    "focus_quantize_kv": (_I, [_P, _SH, _P, _P, C.c_int64, C.c_int64, _I, _P, _P, _I, _QC, _P]),
+    "focus_dequantize_kv": (_I, [_P, _SH, _QC, _I, _P, _P, _I, _P, _P, C.c_int64, C.c_int64, _P]),
+    "focus_sparse_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _I, _P, _I, _P, _P, _P, _I, _P, _P, _P]),
+    "focus_dense_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _P, _P, _P]),
+    "focus_sample": (_I, [_P, _P, _I, C.c_int64, _I, _I, _I, _P, _P, _I, _F, _I, _F, _F, _P, _P, _P, _P, _P, _P]),
     "focus_dense_attn": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P]),
 }
 
@@ -120,6 +132,13 @@ def make_shape(L, M, H, Hkv, d, B, dtype, q_stride_row=None, q_stride_head=None,
                        d if q_stride_head is None else q_stride_head,
                        d if kv_stride_tok is None else kv_stride_tok,
                        L * d if kv_stride_head is None else kv_stride_head)
+
+
+def make_quant_cache(format, K, V, K_scale, V_scale, scale_stride_head=0) -> focus_quant_cache:
+    """An 8-bit cache over the caller's tensors: codes K, V (8 bits each, laid out by the shape's kv strides) and float
+    scales [Hkv, >= L] with scale_stride_head floats per KV head (0: the shape's L).  The tensors stay the caller's to
+    keep alive."""
+    return focus_quant_cache(format, _ptr(K), _ptr(V), _ptr(K_scale), _ptr(V_scale), scale_stride_head)
 
 
 class Context:
@@ -277,3 +296,38 @@ def focus_commit_step(ctx, conf_new, token_new, pos_base, rows, n_rows, max_rows
     _check(ctx._lib.focus_commit_step(ctx.handle, _ptr(conf_new), _ptr(token_new), pos_base, _ptr(rows), _ptr(n_rows),
                                       max_rows, L, blk_lo, blk_hi, n_unmask, _ptr(conf), _ptr(masked), _ptr(x),
                                       _ptr(unmasked_idx), _ptr(n_unmasked), _stream(stream)), "focus_commit_step")
+
+
+def focus_quantize_kv(ctx, shape, K_new, V_new, new_stride_row, new_stride_head, pos_base, rows, n_rows, max_rows, cache,
+                      stream=None):
+    _check(ctx._lib.focus_quantize_kv(ctx.handle, C.byref(shape), _ptr(K_new), _ptr(V_new), new_stride_row,
+                                      new_stride_head, pos_base, _ptr(rows), _ptr(n_rows), max_rows, C.byref(cache),
+                                      _stream(stream)), "focus_quantize_kv")
+
+
+def focus_dequantize_kv(ctx, shape, cache, pos_base, rows, n_rows, max_rows, K_out, V_out, out_stride_row,
+                        out_stride_head, stream=None):
+    _check(ctx._lib.focus_dequantize_kv(ctx.handle, C.byref(shape), C.byref(cache), pos_base, _ptr(rows), _ptr(n_rows),
+                                        max_rows, _ptr(K_out), _ptr(V_out), out_stride_row, out_stride_head,
+                                        _stream(stream)), "focus_dequantize_kv")
+
+
+def focus_sparse_attn_quantized(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, cache, head_reduce, block_idx,
+                                max_blocks, block_cnt, sink_idx, sink_keep, n_sink, O, lse=None, stream=None):
+    _check(ctx._lib.focus_sparse_attn_quantized(ctx.handle, C.byref(shape), _ptr(Q), q_base, n_q, _ptr(q_rows),
+                                                _ptr(n_rows), max_rows, C.byref(cache), head_reduce, _ptr(block_idx),
+                                                max_blocks, _ptr(block_cnt), _ptr(sink_idx), _ptr(sink_keep), n_sink,
+                                                _ptr(O), _ptr(lse), _stream(stream)), "focus_sparse_attn_quantized")
+
+
+def focus_dense_attn_quantized(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, cache, O, lse=None, stream=None):
+    _check(ctx._lib.focus_dense_attn_quantized(ctx.handle, C.byref(shape), _ptr(Q), q_base, n_q, _ptr(q_rows),
+                                               _ptr(n_rows), max_rows, C.byref(cache), _ptr(O), _ptr(lse),
+                                               _stream(stream)), "focus_dense_attn_quantized")
+
+
+def focus_sample(ctx, logits, dtype, row_stride, vocab, pos_base, n_pos, rows, n_rows, max_rows, temperature, top_k,
+                 top_p, min_p, u, conf, token, prob=None, n_kept=None, stream=None):
+    _check(ctx._lib.focus_sample(ctx.handle, _ptr(logits), dtype, row_stride, vocab, pos_base, n_pos, _ptr(rows),
+                                 _ptr(n_rows), max_rows, temperature, top_k, top_p, min_p, _ptr(u), _ptr(conf),
+                                 _ptr(token), _ptr(prob), _ptr(n_kept), _stream(stream)), "focus_sample")

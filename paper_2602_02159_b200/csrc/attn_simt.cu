@@ -1,6 +1,6 @@
 // Generic SIMT attention (Eq. 9 and FullAttn of Algorithm 1) and the SIMT sink column-sum (Eq. 6).
-// Any dtype (f32, bf16), head_dim 64/128, any block size: this is the fp32 path of the library and the
-// fallback for shapes the tensor-core kernels do not take.  One CTA of eight or sixteen warps per (eight query rows, head); the
+// Any dtype (f32, bf16), head_dim 64/128, any block size, K/V in that dtype or as 8-bit codes with a scale per token
+// and KV head: this is the fp32 path of the library and the fallback for shapes the tensor-core kernels do not take.  One CTA of eight or sixteen warps per (eight query rows, head); the
 // lanes of a warp hold 32 different keys during the logit phase and 32 slices of the output during the value phase.
 #include "focus_common.cuh"
 
@@ -15,6 +15,12 @@ __device__ __forceinline__ void load_slice(const T* __restrict__ p, float (&out)
       const float2 v = __ldg(reinterpret_cast<const float2*>(p));
       out[0] = v.x; out[1] = v.y;
     }
+  } else if constexpr (sizeof(T) == 1) {
+    float f[4];
+    if constexpr (EPL == 4) codes_to_float(__ldg(reinterpret_cast<const uint32_t*>(p)), T(), f);
+    else codes_to_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)), T(), f);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) out[e] = f[e];
   } else {
     if constexpr (EPL == 4) {
       const uint2 raw = __ldg(reinterpret_cast<const uint2*>(p));
@@ -48,6 +54,8 @@ struct SimtParams {
   int q_base, n_q, rows_bound, L, M, H, hpg, B, nb, dense, group_stride, max_blocks, n_sink, lse_stride;
   float scale;
   int32_t* status;
+  const float* K_scale; const float* V_scale;        // 8-bit K/V: [Hkv] rows of scale_stride floats, else unused
+  long long scale_stride;
 };
 
 // warps per CTA: sixteen for head_dim 64, eight for 128 (the warps' partial outputs must fit in 48 KB)
@@ -61,11 +69,14 @@ constexpr int UNROLL_DOT = 2, UNROLL_V = 4;
 // take the 32-key chunks of the key set in turn, each with its own running (max, sum, output) per row; the
 // partials are merged through shared memory at the end.  Lane j of a warp owns key j of the chunk during the logit
 // phase and slice j of the output during the value phase.
-template <typename T, int D, int R>
+// T: type of Q and O; KT: type of K and V (T itself, or int8_t / __nv_fp8_e4m3 codes).  With codes the logit is
+// (q . code) * scale, one multiplication per key, and the value's scale goes into its softmax numerator.
+template <typename T, typename KT, int D, int R>
 __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const SimtParams p) {
   constexpr int NW = simt_warps(D), NTH = NW * 32;
   constexpr int EPL = D / 32;
-  constexpr int EPC = 16 / sizeof(T);                // elements per 16-byte load
+  constexpr int EPC = 16 / sizeof(KT);               // K elements per 16-byte load
+  constexpr bool CODES = sizeof(KT) == 1;
   __shared__ __align__(16) float qs[R][D];
   __shared__ float part_o[NW][R][D];
   __shared__ float part_ml[NW][R][2];
@@ -96,8 +107,8 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
   }
   __syncthreads();
   const int g = h / p.hpg;
-  const T* Kg = (const T*)p.K + (long long)g * p.kv_stride_head;
-  const T* Vg = (const T*)p.V + (long long)g * p.kv_stride_head;
+  const KT* Kg = (const KT*)p.K + (long long)g * p.kv_stride_head;
+  const KT* Vg = (const KT*)p.V + (long long)g * p.kv_stride_head;
   const bool want_o = p.O != nullptr;
   float m[R], l[R], o[R][EPL];
 #pragma unroll
@@ -119,7 +130,16 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
       for (int c = 0; c < D / EPC; ++c) {
         const uint4 raw = __ldg(kr + c);
         float kf[EPC];
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (CODES) {
+          const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float f[4];
+            codes_to_float(rw[w], KT(), f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kf[4 * w + e] = f[e];
+          }
+        } else if constexpr (sizeof(KT) == 2) {
           const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&raw);
 #pragma unroll
           for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(pb[e]); kf[2 * e] = f.x; kf[2 * e + 1] = f.y; }
@@ -140,6 +160,15 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
     }
     // row maxima and row sums of the R rows as interleaved butterflies (R independent shuffles per level)
     float si[R], mx[R], pj[R], corr[R];
+    float vscale = 1.f;
+    if constexpr (CODES) {
+      if (key >= 0) {
+        const float ks = __ldg(p.K_scale + (long long)g * p.scale_stride + key);
+        vscale = __ldg(p.V_scale + (long long)g * p.scale_stride + key);
+#pragma unroll
+        for (int i = 0; i < R; ++i) s[i] *= ks;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < R; ++i) { si[i] = key >= 0 ? s[i] * p.scale : -INFINITY; mx[i] = si[i]; }
 #pragma unroll
@@ -173,13 +202,17 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
 #pragma unroll
       for (int e = 0; e < EPL; ++e) o[i][e] *= corr[i];
     }
+    if constexpr (CODES) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) pj[i] *= vscale;     // the row sums above took the numerators themselves
+    }
     if (want_o && any) {
       // the 32 V rows of the chunk, sixteen loads in flight; an absent key reads row 0 and is discarded
 #pragma unroll UNROLL_V
       for (int jj = 0; jj < 32; ++jj) {
         const int kk = __shfl_sync(0xffffffffu, key, jj);
         float v[EPL];
-        load_slice<T, EPL>(Vg + (long long)max(kk, 0) * p.kv_stride_tok + lane * EPL, v);
+        load_slice<KT, EPL>(Vg + (long long)max(kk, 0) * p.kv_stride_tok + lane * EPL, v);
 #pragma unroll
         for (int e = 0; e < EPL; ++e) v[e] = kk >= 0 ? v[e] : 0.f;
 #pragma unroll
@@ -274,14 +307,22 @@ focus_status launch_attn_simt(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st
   if (a.max_rows == 0) return FOCUS_OK;
   constexpr int R = 8;                               // query rows per CTA
   const unsigned grid = (unsigned)(((long long)a.max_rows + R - 1) / R * a.sh.n_q_heads);
-  const bool bf = a.sh.dtype == FOCUS_BF16;
-  if (a.sh.head_dim == 128) {
-    if (bf) attn_simt_kernel<__nv_bfloat16, 128, R><<<grid, simt_warps(128) * 32, 0, st>>>(p);
-    else attn_simt_kernel<float, 128, R><<<grid, simt_warps(128) * 32, 0, st>>>(p);
+  p.K_scale = p.V_scale = nullptr; p.scale_stride = 0;
+  if (a.qc) { p.K_scale = a.qc->K_scale; p.V_scale = a.qc->V_scale; p.scale_stride = quant_scale_stride(a.qc, &a.sh); }
+  const bool bf = a.sh.dtype == FOCUS_BF16, d128 = a.sh.head_dim == 128;
+#define FOCUS_SIMT(T, KT)                                                                            \
+  do {                                                                                               \
+    if (d128) attn_simt_kernel<T, KT, 128, R><<<grid, simt_warps(128) * 32, 0, st>>>(p);             \
+    else attn_simt_kernel<T, KT, 64, R><<<grid, simt_warps(64) * 32, 0, st>>>(p);                    \
+  } while (0)
+  if (a.qc && a.qc->format == FOCUS_KV_INT8) {
+    if (bf) FOCUS_SIMT(__nv_bfloat16, int8_t); else FOCUS_SIMT(float, int8_t);
+  } else if (a.qc) {
+    if (bf) FOCUS_SIMT(__nv_bfloat16, __nv_fp8_e4m3); else FOCUS_SIMT(float, __nv_fp8_e4m3);
   } else {
-    if (bf) attn_simt_kernel<__nv_bfloat16, 64, R><<<grid, simt_warps(64) * 32, 0, st>>>(p);
-    else attn_simt_kernel<float, 64, R><<<grid, simt_warps(64) * 32, 0, st>>>(p);
+    if (bf) FOCUS_SIMT(__nv_bfloat16, __nv_bfloat16); else FOCUS_SIMT(float, float);
   }
+#undef FOCUS_SIMT
   FOCUS_CHECK_LAUNCH();
   return FOCUS_OK;
 }

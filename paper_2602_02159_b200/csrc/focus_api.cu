@@ -148,9 +148,22 @@ static focus_status attn_common(focus_ctx* ctx, const focus_shape* shape, const 
   return FOCUS_OK;
 }
 
+// the key set of a sparse call: block lists + sink tokens + response region
+static focus_status attn_sparse_keys(int head_reduce, const int32_t* block_idx, int max_blocks, const int32_t* block_cnt,
+                                     const int32_t* sink_idx, const uint8_t* sink_keep, int n_sink, AttnArgs& a) {
+  if (head_reduce != FOCUS_HEADS_PER_KV_GROUP && head_reduce != FOCUS_HEADS_ALL) return FOCUS_ERR_INVALID_ARG;
+  if (!block_idx || !block_cnt || max_blocks < 0 || n_sink < 0) return FOCUS_ERR_INVALID_ARG;
+  if (n_sink > 0 && (!sink_idx || !sink_keep)) return FOCUS_ERR_INVALID_ARG;
+  a.dense = 0;
+  a.group_stride = head_reduce == FOCUS_HEADS_ALL ? 0 : 1;
+  a.block_idx = block_idx; a.max_blocks = max_blocks; a.block_cnt = block_cnt;
+  a.sink_idx = sink_idx; a.sink_keep = sink_keep; a.n_sink = n_sink;
+  return FOCUS_OK;
+}
+
 static focus_status attn_dispatch(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   if (a.max_rows == 0) return FOCUS_OK;
-  if (!ctx->force_simt && attn_tc_supported(ctx, a)) return launch_attn_tc(ctx, a, st);
+  if (!ctx->force_simt && !a.qc && attn_tc_supported(ctx, a)) return launch_attn_tc(ctx, a, st);
   ctx->last_attn_variant = 1;
   return launch_attn_simt(ctx, a, st);
 }
@@ -176,13 +189,46 @@ extern "C" focus_status focus_sparse_attn(focus_ctx* ctx, const focus_shape* sha
   AttnArgs a{};
   focus_status s = attn_common(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, K, V, O, lse, a);
   if (s != FOCUS_OK) return s;
-  if (head_reduce != FOCUS_HEADS_PER_KV_GROUP && head_reduce != FOCUS_HEADS_ALL) return FOCUS_ERR_INVALID_ARG;
-  if (!block_idx || !block_cnt || max_blocks < 0 || n_sink < 0) return FOCUS_ERR_INVALID_ARG;
-  if (n_sink > 0 && (!sink_idx || !sink_keep)) return FOCUS_ERR_INVALID_ARG;
-  a.dense = 0;
-  a.group_stride = head_reduce == FOCUS_HEADS_ALL ? 0 : 1;
-  a.block_idx = block_idx; a.max_blocks = max_blocks; a.block_cnt = block_cnt;
-  a.sink_idx = sink_idx; a.sink_keep = sink_keep; a.n_sink = n_sink;
+  s = attn_sparse_keys(head_reduce, block_idx, max_blocks, block_cnt, sink_idx, sink_keep, n_sink, a);
+  if (s != FOCUS_OK) return s;
+  return attn_dispatch(ctx, a, stream);
+}
+
+// ---- attention over an 8-bit cache -----------------------------------------------------------------
+static focus_status attn_quant_common(focus_ctx* ctx, const focus_shape* shape, const void* Q, int q_base, int n_q,
+                                      const int32_t* q_rows, const int32_t* n_rows, int max_rows,
+                                      const focus_quant_cache* cache, void* O, float* lse, AttnArgs& a) {
+  if (!ctx || !quant_cache_ok(shape, cache, true, true)) return FOCUS_ERR_INVALID_ARG;
+  a.qc = cache;
+  return attn_common(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, cache->K, cache->V, O, lse, a);
+}
+
+extern "C" focus_status focus_dense_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q, int32_t q_base,
+                                                   int32_t n_q, const int32_t* q_rows, const int32_t* n_rows,
+                                                   int32_t max_rows, const focus_quant_cache* cache, void* O, float* lse,
+                                                   focus_stream stream) {
+  FOCUS_STAGE("focus_dense_attn_quantized");
+  AttnArgs a{};
+  focus_status s = attn_quant_common(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, cache, O, lse, a);
+  if (s != FOCUS_OK) return s;
+  a.dense = 1;
+  return attn_dispatch(ctx, a, stream);
+}
+
+extern "C" focus_status focus_sparse_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q,
+                                                    int32_t q_base, int32_t n_q, const int32_t* q_rows,
+                                                    const int32_t* n_rows, int32_t max_rows,
+                                                    const focus_quant_cache* cache, int32_t head_reduce,
+                                                    const int32_t* block_idx, int32_t max_blocks,
+                                                    const int32_t* block_cnt, const int32_t* sink_idx,
+                                                    const uint8_t* sink_keep, int32_t n_sink, void* O, float* lse,
+                                                    focus_stream stream) {
+  FOCUS_STAGE("focus_sparse_attn_quantized");
+  AttnArgs a{};
+  focus_status s = attn_quant_common(ctx, shape, Q, q_base, n_q, q_rows, n_rows, max_rows, cache, O, lse, a);
+  if (s != FOCUS_OK) return s;
+  s = attn_sparse_keys(head_reduce, block_idx, max_blocks, block_cnt, sink_idx, sink_keep, n_sink, a);
+  if (s != FOCUS_OK) return s;
   return attn_dispatch(ctx, a, stream);
 }
 

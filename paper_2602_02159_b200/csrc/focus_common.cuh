@@ -2,6 +2,8 @@
 #pragma once
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 #include <stdint.h>
@@ -25,7 +27,7 @@ struct focus_ctx {
   // launch state that belongs to the device (function attributes, occupancy answers): kept per context, since a
   // process may hold contexts on several devices.  Zero-initialised by focus_create.
   struct LaunchState {
-    bool attn_attr_set, select_attr_set, topn_attr_set;
+    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[2];
     int sink_attr_smem;
     int cluster_cap[9], cluster_cap_w[9], cluster_cap_k[9];   // co-resident clusters per cluster size, value + 1 (0 = not asked yet)
     int select_cluster;                        // 0 not tried, 1 works, 2 the cluster launch was refused once
@@ -92,6 +94,22 @@ static inline bool shape_supported(const focus_shape* s) {
 static inline float shape_scale(const focus_shape* s) {
   return s->softmax_scale != 0.f ? s->softmax_scale : 1.0f / sqrtf((float)s->head_dim);
 }
+// Row stride of a cache's scales: scale_stride_head, or contiguous [Hkv, L] where that is 0.
+static inline long long quant_scale_stride(const focus_quant_cache* c, const focus_shape* s) {
+  return c->scale_stride_head ? c->scale_stride_head : s->L;
+}
+// Host checks of an 8-bit cache against the shape whose kv strides describe its codes (one element = one byte there):
+// 16-byte aligned code rows, 4-byte aligned scales.
+static inline bool quant_cache_ok(const focus_shape* s, const focus_quant_cache* c, bool need_k, bool need_v) {
+  if (!shape_ok_basic(s) || !c) return false;
+  if (c->format != FOCUS_KV_INT8 && c->format != FOCUS_KV_E4M3) return false;
+  if (need_k && (!c->K || !c->K_scale)) return false;
+  if (need_v && (!c->V || !c->V_scale)) return false;
+  if (!all_aligned16(c->K, c->V)) return false;
+  if ((reinterpret_cast<uintptr_t>(c->K_scale) | reinterpret_cast<uintptr_t>(c->V_scale)) & 3u) return false;
+  if ((s->kv_stride_tok | s->kv_stride_head) & 15) return false;
+  return c->scale_stride_head == 0 || c->scale_stride_head >= s->L;
+}
 static inline int shape_nb(const focus_shape* s) { return (s->M + s->kv_block - 1) / s->kv_block; }
 
 #ifdef __CUDACC__
@@ -121,6 +139,21 @@ __device__ __forceinline__ float key_to_float(uint32_t k) {
 
 __device__ __forceinline__ float load_as_float(const float* p) { return *p; }
 __device__ __forceinline__ float load_as_float(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+
+// Four 8-bit codes (one 32-bit word, lowest byte first) as the numbers they stand for, before the scale: int8, or e4m3
+// (every e4m3 value is an fp16 value, so the way through half loses nothing).
+__device__ __forceinline__ void codes_to_float(uint32_t w, int8_t, float (&f)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = (float)(int8_t)(w >> (8 * e));
+}
+__device__ __forceinline__ void codes_to_float(uint32_t w, __nv_fp8_e4m3, float (&f)[4]) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * e)), __NV_E4M3);
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    f[2 * e] = v.x; f[2 * e + 1] = v.y;
+  }
+}
 
 // Exclusive prefix sum over the thread block of one int per thread; returns the exclusive prefix and the
 // block total through `total`.  `warp_tot` is shared scratch of at least 33 ints.  All threads must call.
@@ -237,6 +270,7 @@ struct AttnArgs {
   void* O;            // may be NULL (lse only)
   float* lse;         // may be NULL
   int lse_stride;
+  const focus_quant_cache* qc;   // non-NULL: K and V are the 8-bit codes of this cache (K == qc->K, V == qc->V)
 };
 
 struct SinkGather {          // sink rows of one layer gathered into compact per-KV-head tiles

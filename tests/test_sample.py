@@ -1,0 +1,248 @@
+"""focus_sample against the float64 oracle: temperature, top-k, top-p, min-p from given uniform numbers."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import focus_oracle as fo
+from paper_2602_02159_b200 import binding as fb
+from paper_2602_02159_b200 import build as fbuild
+from paper_2602_02159_b200 import step as fstep
+from paper_2602_02159_b200 import workloads as wl
+
+gpu = pytest.mark.gpu
+DT = {"bf16": fb.BF16, "f32": fb.F32}
+# conf and prob are rounded once to fp32 (2^-24) from sums in fp64; prob's denominator has fp32 terms: expf is within 2
+# units in the last place (2^-22) and every thread adds at most vocab / 512 of them in fp32 (2^-24 each)
+CONF_TOL = 2.0 ** -24 + 1e-12
+
+
+def prob_tol(vocab):
+    return 2.0 ** -24 + 2.0 ** -22 + (vocab / 512 + 1) * 2.0 ** -24 + 1e-12
+
+
+def single(x):
+    return float(np.float32(x))
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = fb.Context(0)
+    yield c
+    assert c.poll_status() == 0
+    c.close()
+
+
+def run(ctx, xs, dtype, vocab, pos_base, rows, max_rows, T, k, p, mp, u, outputs=True):
+    """xs: storage array [n_pos, stride]; rows: list of positions or None."""
+    dx = fstep.to_device(xs, dtype)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    dr = torch.tensor(list(rows) + [-1] * (max_rows - len(rows)), **i32) if rows is not None else None
+    dn = torch.tensor([len(rows)], **i32) if rows is not None else None
+    du = torch.from_numpy(np.asarray(u, dtype=np.float32)).cuda()
+    conf, prob = torch.full((max_rows + 2,), 7.0, device="cuda"), torch.full((max_rows + 2,), 7.0, device="cuda")
+    tok, kept = torch.full((max_rows + 2,), 7, **i32), torch.full((max_rows + 2,), 7, **i32)
+    fb.focus_sample(ctx, dx, DT[dtype], xs.shape[1], vocab, pos_base, xs.shape[0], dr, dn, max_rows, T, k, p, mp, du, conf, tok,
+                    prob if outputs else None, kept if outputs else None)
+    out = [t.cpu().numpy() for t in (tok, conf, prob, kept)]
+    assert all((o[max_rows:] == 7).all() for o in out)                       # nothing behind the rows is written
+    return out
+
+
+def check(out, x, rows_local, T, k, p, mp, u):
+    tok, conf, prob, kept = out
+    V = x.shape[1]
+    for r, pr in enumerate(rows_local):
+        et, ec, ep, en = fo.sample_token(x[pr], single(T), k, single(p), single(mp), single(u[r]))
+        assert (int(tok[r]), int(kept[r])) == (et, en), (r, int(tok[r]), et, int(kept[r]), en)
+        assert abs(float(conf[r]) - ec) <= CONF_TOL * ec + 1e-45 and abs(float(prob[r]) - ep) <= prob_tol(V) * ep + 1e-45
+
+
+KNOBS = [(1.0, 0, 1.0, 0.0), (0.7, 0, 0.95, 0.0), (1.3, 50, 1.0, 0.0), (0.5, 20, 0.9, 0.05), (1.0, 0, 1.0, 0.1),
+         (0.9, 1, 0.5, 0.0), (2.0, 700, 0.3, 0.01), (0.05, 0, 0.999, 0.0)]
+
+
+@gpu
+@pytest.mark.parametrize("knobs", KNOBS)
+@pytest.mark.parametrize("dtype,vocab,stride,spread", [("bf16", 5000, 5000, 2.0), ("f32", 4099, 4100, 2.5), ("bf16", 7, 8, 1.0),
+                                                       ("f32", 1, 4, 1.0), ("bf16", 32768, 32776, 0.5), ("f32", 12289, 12292, 4.0)])
+def test_tokens_are_the_oracles(ctx, dtype, vocab, stride, spread, knobs):
+    rng = np.random.default_rng(vocab + int(10 * knobs[0]))
+    n_pos, pos_base = 12, 300
+    xs = wl.to_storage((rng.standard_normal((n_pos, stride)) * spread).astype(np.float32), dtype)
+    rows = sorted(rng.choice(n_pos, size=9, replace=False).tolist())
+    u = rng.random(11)
+    u[:3] = [0.0, np.nextafter(np.float32(1.0), np.float32(0.0)), 0.5]
+    out = run(ctx, xs, dtype, vocab, pos_base, [pos_base + r for r in rows], 11, *knobs, u)
+    check(out, wl.storage_to_f64(xs, dtype)[:, :vocab], rows, *knobs, u)
+    assert (out[0][9:11] == -1).all() and (out[1][9:11] == 0).all() and (out[2][9:11] == 0).all() and (out[3][9:11] == 0).all()
+    # the same rows without a list, and without the optional outputs
+    again = run(ctx, xs, dtype, vocab, pos_base, None, 12, *knobs, np.concatenate([u, u[:1]])[:12], outputs=False)
+    check((again[0], again[1], out[2] * 0, out[3]), wl.storage_to_f64(xs, dtype)[:0, :vocab], [], *knobs, u)
+    one = run(ctx, xs, dtype, vocab, pos_base, None, 12, *knobs, np.concatenate([u, u[:1]])[:12])
+    assert np.array_equal(one[0], again[0]) and np.array_equal(one[1], again[1])
+    assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties_masks_and_infinities(ctx, dtype):
+    rng = np.random.default_rng(4)
+    V = 2000
+    x = (rng.standard_normal((12, V)) * 2).astype(np.float32)
+    x[0] = 1.5                                          # every token equal: ties cut by index
+    x[1] = np.round(x[1])                               # a handful of values, hundreds of tokens each
+    x[2, ::2] = -np.inf                                 # masked vocabulary
+    x[3, :] = -np.inf
+    x[3, 77] = -3.0                                     # one candidate
+    x[4, :] = -np.inf                                   # none
+    x[5, 10:30] = np.nan
+    x[6, [5, 900, 1999]] = np.inf                       # infinities share the weight
+    x[7, :] = np.nan
+    x[8, :] = wl.storage_to_f64(wl.to_storage(np.array([np.finfo(np.float32).min], np.float32), "f32"), "f32")[0] if dtype == "f32" else -3.3e38
+    x[8, 1234] = -1e38                                  # lowest values of the type, weight zero
+    x[9, :] = -0.0
+    x[9, 50:60] = 0.0                                   # the two zeros are equal
+    x[10, 3] = 500.0                                    # everything else underflows
+    xs = wl.to_storage(x, dtype)
+    xf = wl.storage_to_f64(xs, dtype)
+    for T, k, p, mp in ((1.0, 0, 1.0, 0.0), (0.8, 7, 1.0, 0.0), (1.0, 0, 0.5, 0.0), (1.2, 333, 0.75, 0.0), (0.6, 0, 0.9, 0.3),
+                        (1.0, 100, 1.0, 1.0), (1.0, 0, 0.25, 0.0)):
+        for u in (np.zeros(12), rng.random(12), np.full(12, 0.9999)):
+            out = run(ctx, xs, dtype, V, 0, None, 12, T, k, p, mp, u)
+            check(out, xf, range(12), T, k, p, mp, u)
+    assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,vocab,max_rows", [("bf16", 126464, 3), ("f32", 126464, 2), ("bf16", 151936, 40), ("f32", 300001, 2)])
+def test_long_rows(ctx, dtype, vocab, max_rows):
+    """Rows that span a whole cluster, flat and peaked, with and without cuts."""
+    rng = np.random.default_rng(vocab)
+    stride = (vocab + 7) // 8 * 8
+    x = rng.standard_normal((max_rows, stride)).astype(np.float32)
+    x *= np.where(np.arange(max_rows) % 2 == 0, 0.4, 3.0)[:, None].astype(np.float32)
+    xs = wl.to_storage(x, dtype)
+    xf = wl.storage_to_f64(xs, dtype)[:, :vocab]
+    for T, k, p, mp in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (0.8, 5000, 0.97, 0.0), (0.9, 50, 0.9, 0.02)):
+        u = rng.random(max_rows)
+        out = run(ctx, xs, dtype, vocab, 0, None, max_rows, T, k, p, mp, u)
+        few = list(range(min(2, max_rows)))
+        check(out, xf, few, T, k, p, mp, u)
+        assert ((out[0][:max_rows] >= 0) & (out[0][:max_rows] < vocab)).all()
+        # a row's answer does not depend on the rows beside it
+        alone = run(ctx, xs[max_rows - 1:], dtype, vocab, 0, None, 1, T, k, p, mp, u[max_rows - 1:])
+        assert alone[0][0] == out[0][max_rows - 1] and alone[3][0] == out[3][max_rows - 1]
+    assert ctx.poll_status() == 0
+
+
+@gpu
+def test_frequencies_follow_the_distribution(ctx):
+    """u = (i + 1/2) / n for i < n: every kept token is drawn as often as its probability says, off by at most one."""
+    rng = np.random.default_rng(12)
+    V, n = 40, 4000
+    x = (rng.standard_normal((1, V)) * 1.5).astype(np.float32)
+    xs = np.repeat(x, n, axis=0)
+    u = (np.arange(n) + 0.5) / n
+    tok = run(ctx, xs, "f32", V, 0, None, n, 0.9, 12, 1.0, 0.0, u)[0][:n]
+    order = np.argsort(-x[0], kind="stable")[:12]
+    w = np.exp(x[0].astype(np.float64) / single(0.9))
+    want = np.zeros(V)
+    want[order] = w[order] / w[order].sum() * n
+    assert (np.abs(np.bincount(tok, minlength=V) - want) <= 1.0).all()
+
+
+@gpu
+def test_top_k_of_one_is_the_confidence_call(ctx):
+    """top_k = 1 draws the argmax that focus_confidence reports, prob is its confidence, whatever u is."""
+    rng = np.random.default_rng(2)
+    V, n = 30000, 24
+    xs = wl.to_storage((rng.standard_normal((n, V)) * 3).astype(np.float32), "bf16")
+    out = run(ctx, xs, "bf16", V, 0, None, n, 1.0, 1, 1.0, 0.0, rng.random(n))
+    dx = fstep.to_device(xs, "bf16")
+    conf, tok = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    fb.focus_confidence(ctx, dx, fb.BF16, V, V, 0, n, None, None, n, conf, tok)
+    assert np.array_equal(tok.cpu().numpy(), out[0][:n]) and (out[1][:n] == 1).all() and (out[3][:n] == 1).all()
+    # focus_confidence sums fast-math exponentials of fp32 (2^-21 each)
+    assert np.max(np.abs(conf.cpu().numpy() / out[2][:n] - 1)) <= 2.0 ** -20 + prob_tol(V)
+
+
+@gpu
+def test_bad_rows_and_numbers_are_reported(ctx):
+    V = 64
+    xs = wl.to_storage(np.random.default_rng(0).standard_normal((4, V)).astype(np.float32), "f32")
+    good = run(ctx, xs, "f32", V, 10, [10, 11, 13], 3, 1.0, 0, 1.0, 0.0, [0.1, 0.2, 0.3])
+    assert ctx.poll_status() == 0
+    for rows, u, bad in (([10, 14, 13], [0.1, 0.2, 0.3], 1), ([9, 11, 13], [0.1, 0.2, 0.3], 0), ([10, 11, 13], [0.1, 1.0, 0.3], 1),
+                         ([10, 11, 13], [0.1, 0.2, -0.1], 2), ([10, 11, 13], [np.nan, 0.2, 0.3], 0)):
+        out = run(ctx, xs, "f32", V, 10, rows, 3, 1.0, 0, 1.0, 0.0, u)
+        assert ctx.poll_status() == fb.ERR_INVALID_ARG
+        assert out[0][bad] == -1 and out[1][bad] == 0 and out[2][bad] == 0 and out[3][bad] == 0
+        for r in range(3):
+            assert r == bad or (out[0][r] == good[0][r] and out[1][r] == good[1][r])
+
+
+def test_refusals_need_no_device():
+    fbuild.build()
+    lib = fb.load_library()
+    fake = ctypes.create_string_buffer(4096)
+    h, P = ctypes.cast(fake, ctypes.c_void_p), 1 << 20
+
+    def call(ctx=h, logits=P, dtype=fb.BF16, stride=1000, vocab=1000, base=0, n_pos=8, rows=None, n=None, max_rows=8, T=1.0, k=0,
+             p=1.0, mp=0.0, u=P, conf=P, tok=P):
+        return lib.focus_sample(ctx, logits, dtype, stride, vocab, base, n_pos, rows, n, max_rows, T, k, p, mp, u, conf, tok, None,
+                                None, None)
+    bad = [dict(ctx=None), dict(logits=None), dict(logits=P + 8), dict(dtype=2), dict(stride=999), dict(stride=1004), dict(vocab=0),
+           dict(base=-1), dict(n_pos=-1), dict(max_rows=-1), dict(max_rows=9), dict(rows=P), dict(n=P), dict(T=0.0), dict(T=-1.0),
+           dict(T=math.inf), dict(T=math.nan), dict(k=-1), dict(p=0.0), dict(p=1.5), dict(p=math.nan), dict(mp=-0.1), dict(mp=1.1),
+           dict(mp=math.nan), dict(u=None), dict(conf=None), dict(tok=None)]
+    for b in bad:
+        assert call(**b) == fb.ERR_INVALID_ARG, b
+    assert call(vocab=900_000, stride=900_000) == fb.ERR_UNSUPPORTED
+    assert call(max_rows=0) == fb.OK
+
+
+@gpu
+def test_a_sampled_step_captured_and_replayed(ctx):
+    """Logits -> drawn tokens -> state update (focus_commit_step), as one graph; new numbers and logits on replay."""
+    rng = np.random.default_rng(6)
+    L, M, V, n = 200, 120, 3000, 30
+    pos = np.sort(rng.choice(np.arange(M, L), size=n, replace=False))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    rows, n_rows = torch.from_numpy(pos.astype(np.int32)).cuda(), torch.tensor([n], **i32)
+    logits, u = torch.zeros(L - M, V, device="cuda").bfloat16(), torch.zeros(n, device="cuda")
+    conf, masked, x = torch.zeros(L, device="cuda"), torch.zeros(L, dtype=torch.uint8, device="cuda"), torch.zeros(L, **i32)
+    cn, tn, pr = torch.zeros(n, device="cuda"), torch.zeros(n, **i32), torch.zeros(n, device="cuda")
+    out, n_out = torch.zeros(4, **i32), torch.zeros(1, **i32)
+
+    def fill():
+        logits.copy_(torch.from_numpy(rng.standard_normal((L - M, V)).astype(np.float32) * 2))
+        u.copy_(torch.from_numpy(rng.random(n).astype(np.float32)))
+        masked.zero_(), x.zero_(), conf.zero_()
+        masked[M:] = 1
+
+    def step():
+        fb.focus_sample(ctx, logits, fb.BF16, V, V, M, L - M, rows, n_rows, n, 0.8, 40, 0.9, 0.01, u, cn, tn, pr)
+        fb.focus_commit_step(ctx, pr, tn, M, rows, n_rows, n, L, M, L, 4, conf, masked, x, out, n_out)
+
+    def check_state():
+        torch.cuda.synchronize()
+        xf = logits.double().cpu().numpy()
+        want = [fo.sample_token(xf[p - M], single(0.8), 40, single(0.9), single(0.01), float(u[r])) for r, p in enumerate(pos)]
+        assert tn.cpu().numpy().tolist() == [w[0] for w in want]
+        _, em, ex, picks = fo.commit_step(np.zeros(L, np.float32), np.r_[np.zeros(M, np.uint8), np.ones(L - M, np.uint8)],
+                                          np.zeros(L, np.int32), pos.tolist(), pr.cpu().numpy(), [w[0] for w in want], M, L, 4)
+        assert out.cpu().numpy().tolist() == picks and np.array_equal(x.cpu().numpy(), ex) and np.array_equal(masked.cpu().numpy(), em)
+
+    fill(), step(), check_state()
+    fill()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(2):
+        fill(), graph.replay(), check_state()
+    assert ctx.poll_status() == 0
