@@ -1,0 +1,887 @@
+// Attention over an 8-bit K/V cache on the 5th-generation tensor cores (focus_dense_attn_quantized,
+// focus_sparse_attn_quantized).  bf16 queries and outputs, head_dim 128 or 64, fp32 accumulation in TMEM.
+//
+// Mathematics.  With codes ck_j, cv_j and scales sk_j, sv_j of token j, a query row r has the logits (base 2)
+//   s_rj = (q_r . ck_j) * sk_j * scale * log2(e)           and   o_r = sum_j 2^(s_rj) sv_j cv_j / sum_j 2^(s_rj).
+// The kernel works on the transposed products, S^T = K Q^T and O^T = V^T P^T: a thread then owns one KEY for the softmax,
+// so both scales of that key are scalars in its registers.  sk_j joins the logit's scale factor and sv_j the exponent
+// (a_rj = s_rj + log2 sv_j, P_rj = 2^(a_rj - ref_r)): one fused multiply-add per logit either way, and the row sum
+// takes P_rj / sv_j.  ref_r follows the running maximum of a_rj lazily, so P fits fp16 (below).
+// Codes enter the products as they are: every int8 and every e4m3 value is an fp16 value.  q enters as fp16 too, scaled
+// by a power of two that puts the tile's largest |q| at 2^14..2^15: bf16 has fewer fraction bits, so only elements
+// 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-12, absolute 2^-31 of the row's
+// largest), which is the one rounding between the cache and the output; sums are fp32.
+//
+// Work split.  CTA = up to 128 stacked query rows of one KV head (the rows of a group's query heads share its K/V) x one
+// contiguous range ("split") of that head's key tiles of 128 tokens.  The transposed form costs in proportion to the
+// rows there are (N = rows rounded to 16), not to a tile of 128: with the 35 to 72 rows of a denoising step the launch
+// is meant to be bound by the bytes of the cache.
+//
+// Warp roles (640 threads):
+//   warp 0        producer: K and V tiles as raw codes into two rings (TMA; sink tokens one by one with cp.async)
+//   warp 1        tcgen05.mma issuer
+//   warp 2        TMEM allocation
+//   warps 4..7    K codes -> fp16 in TMEM (lane = key): the A operand of S^T
+//   warps 8..11   V codes -> fp16 in TMEM (lane = channel; ldmatrix transposes the bytes): the A operand of O^T
+//   warps 12..19  softmax, two warpgroups with half of the query rows each; P^T to shared memory (the B operand of O^T)
+// Expanding the codes into TMEM instead of shared memory halves the shared-memory traffic of a tile: one byte in, one
+// byte out per code, no fp16 copy there.
+#include "attn_tiles.cuh"
+#include "tc_common.cuh"
+
+using namespace tc;
+
+namespace {
+
+constexpr int QN = 128;                        // most query rows per CTA
+constexpr int NTH = 640;
+constexpr int RING = 3;                        // raw slots per ring (K, V)
+constexpr int SLOT = TN * 128;                 // bytes of a raw tile (head dim 64 fills half)
+constexpr int Q_BYTES = QN * 128 * 2;
+constexpr int P_BYTES = TN * QN * 2;           // P^T of one tile: [key][row], two 64-row halves
+constexpr int MAXT = 256;                      // key tiles of a split whose descriptors are staged
+constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
+constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
+constexpr float THRESH = 8.f;                  // the reference follows the maximum once it is this far (log2) above ...
+constexpr float OFFSET = 6.f;                  // ... and is put this far below it: P <= 2^14, normal fp16 down to 2^-20
+constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
+constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
+                                                    // rows hold zeros, the writer flushes them)
+
+struct QParams {
+  const __nv_bfloat16* Q;
+  __nv_bfloat16* O;
+  float* lse;
+  const int32_t* q_rows;
+  const int32_t* n_rows;
+  const int32_t* block_idx;
+  const int32_t* block_cnt;
+  const int32_t* sink_idx;
+  const uint8_t* sink_keep;
+  const uint8_t* K;
+  const uint8_t* V;
+  const float* K_scale;
+  const float* V_scale;
+  float* part_O;               // [cta][row][d] unnormalised partial outputs (n_splits > 1)
+  float* part_ml;              // [cta][row][2] reference and sum
+  int32_t* counters;           // one arrival counter per (KV head, row tile)
+  long long q_stride_row, q_stride_head, kv_stride_tok, kv_stride_head, scale_stride;
+  int q_base, n_q, rows_bound, L, M, H, hpg, B, nb, dense, group_stride, max_blocks, n_sink, ns_pad;
+  int n_mtiles, n_splits, lse_stride, pair, pdl, evict_first;
+  float scale_log2;
+  int32_t* status;
+};
+
+struct Misc {                                  // behind the tiles in shared memory
+  unsigned long long bars[4 * RING + 16];
+  float ref[QN];                               // reference exponent per row
+  float fac[QN];                               // rescale factor / normaliser per row
+  unsigned colmax[QN];
+  int orow[QN];                                // output row (position slot * H + head), -1: none
+  float lsum[8][64];                           // row sums per softmax warp
+  int2 tlist[MAXT];
+  uint32_t tmem;
+  int abort_flag, last;
+  unsigned qmax;
+};
+constexpr int SMEM = 1024 + OFF_MISC + (int)sizeof(Misc);
+static_assert(SMEM <= 227 * 1024, "shared memory");
+
+// ---- instructions this kernel adds to tc_common.cuh ----
+// kind::f16 with fp16 operands, fp32 accumulation
+__device__ __forceinline__ uint32_t idesc_f16(int N, int b_mn) {
+  return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
+}
+#define TC_LD8(taddr, r)                                                                             \
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"              \
+               : "=r"((r)[0]), "=r"((r)[1]), "=r"((r)[2]), "=r"((r)[3]), "=r"((r)[4]), "=r"((r)[5]), \
+                 "=r"((r)[6]), "=r"((r)[7])                                                          \
+               : "r"(taddr) : "memory")
+#define TC_ST8(taddr, r)                                                                             \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"              \
+               ::"r"(taddr), "r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]),        \
+                 "r"((r)[5]), "r"((r)[6]), "r"((r)[7])                                               \
+               : "memory")
+// sixteen lanes x 32 columns in the fragment layout of four 16x8 accumulator tiles
+#define TC_ST_FRAG16(taddr, r)                                                                                     \
+  asm volatile(                                                                                                    \
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"     \
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),        \
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])               \
+      : "memory")
+// two 16x16 byte matrices, transposed: register i of a pair holds row lane/4 + 8 i, columns 4 (lane % 4) .. + 3
+__device__ __forceinline__ void ldsm_t8(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ bool named_any(int id, int n, bool v) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(id), "r"(n), "r"(v ? 1u : 0u) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Four codes of one word -> two fp16 pairs.  int8: code + 128 as the low byte of the half 0x64xx = 1024 + (code + 128),
+// then 1152 off -- exact, and cheaper than integer conversions (5 operations for four codes).
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi, int8_t) {
+  w ^= 0x80808080u;
+  const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+  const __half2 k = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), k), y = __hsub2(*reinterpret_cast<const __half2*>(&b), k);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi, __nv_fp8_e4m3) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(w));
+}
+
+// 16-byte chunk c of raw row `row`: rows of 128 bytes with the 128-byte swizzle, rows of 64 bytes with the 64-byte one
+template <int D>
+__device__ __forceinline__ uint32_t raw_off(int row, int c) {
+  return D == 128 ? (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)) : (uint32_t)(row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
+}
+
+// Token of column k of a tile, or -1 if the column is masked out (padding, a sink that is dropped or out of range).
+__device__ __forceinline__ int key_token(const QParams& p, const TileInfo& ti, int g, int k) {
+  if (k >= ti.nvalid) return -1;
+  if (ti.kind == 0) return (k < 64 ? ti.start : ti.start2 - 64) + k;
+  const int s = ti.start + k;
+  const int j = __ldg(p.sink_idx + s);
+  const bool keep = __ldg(p.sink_keep + (size_t)g * p.group_stride * p.n_sink + s) != 0;
+  return (keep && j >= 0 && j < p.M) ? j : -1;             // response tokens are attended through their own tiles
+}
+
+template <typename F, int D>
+__global__ void __launch_bounds__(NTH, 1)
+attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const QParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
+  const int g = blockIdx.x / p.n_mtiles, mt = blockIdx.x % p.n_mtiles, split = blockIdx.y;
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* sptr = smem_raw + (sbase - smem_u32(smem_raw));
+  Misc& ms = *reinterpret_cast<Misc*>(sptr + OFF_MISC);
+  const uint32_t sQ = sbase, sP = sbase + Q_BYTES, sRawK = sbase + OFF_RAW, sRawV = sRawK + RING * SLOT;
+  const uint32_t sBar = smem_u32(ms.bars);
+  auto k_full = [&](int s) { return sBar + 8u * s; };
+  auto k_empty = [&](int s) { return sBar + 8u * (RING + s); };
+  auto v_full = [&](int s) { return sBar + 8u * (2 * RING + s); };
+  auto v_empty = [&](int s) { return sBar + 8u * (3 * RING + s); };
+  auto kop_full = [&](int b) { return sBar + 8u * (4 * RING + b); };
+  auto kop_empty = [&](int b) { return sBar + 8u * (4 * RING + 2 + b); };
+  auto vop_full = [&](int b) { return sBar + 8u * (4 * RING + 4 + b); };
+  auto vop_empty = [&](int b) { return sBar + 8u * (4 * RING + 6 + b); };
+  auto s_full = [&](int b) { return sBar + 8u * (4 * RING + 8 + b); };
+  auto s_empty = [&](int b) { return sBar + 8u * (4 * RING + 10 + b); };
+  auto p_full = [&](int b) { return sBar + 8u * (4 * RING + 12 + b); };
+  auto p_empty = [&](int b) { return sBar + 8u * (4 * RING + 14 + b); };
+  volatile int* abort_flag = &ms.abort_flag;
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&tmK); prefetch_tmap(&tmV);
+    for (int s = 0; s < RING; ++s) {
+      mbar_init(k_full(s), 32); mbar_init(v_full(s), 32);            // the producer warp's lanes
+      mbar_init(k_empty(s), 4); mbar_init(v_empty(s), 4);            // four expanding warps
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(kop_full(b), 4); mbar_init(vop_full(b), 4);
+      mbar_init(kop_empty(b), 1); mbar_init(vop_empty(b), 1); mbar_init(s_full(b), 1); mbar_init(p_empty(b), 1);
+      mbar_init(s_empty(b), 8); mbar_init(p_full(b), 8);             // eight softmax warps
+    }
+    ms.abort_flag = 0; ms.qmax = 0u;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 2) { tmem_alloc(smem_u32(&ms.tmem), 512); tmem_relinquish(); }
+  if (threadIdx.x < QN) { ms.ref[threadIdx.x] = REF_NONE; ms.colmax[threadIdx.x] = 0u; }
+  if (p.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing in global memory is touched before this
+  __syncthreads();
+
+  // ---- rows, tiles ----
+  const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
+  const int total_fr = nrows * p.hpg;                                // stacked (row, head of the group) rows
+  const int rows = min(QN, total_fr - mt * QN);                      // of this CTA
+  const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
+  const TileEnum te = make_enum(p, g, cnt_raw);
+  const int t0 = split_lo(te.total, split, p.n_splits), nt = split_lo(te.total, split + 1, p.n_splits) - t0;
+  const int cta = blockIdx.x * p.n_splits + split;
+  const bool use_list = nt <= MAXT;
+  auto make_tile = [&](int idx) -> TileInfo {
+    TileInfo ti = tile_info(p, te, t0 + idx);
+    if (ti.nvalid == 0) { ti.start = ti.start2 = (p.L + 63) & ~63; } // bad block index: wholly outside, arrives as zeros
+    return ti;
+  };
+  auto get_tile = [&](int idx) -> TileInfo { return use_list ? unpack_tile(ms.tlist[idx]) : make_tile(idx); };
+  const int N = rows > 0 ? (rows + 15) & ~15 : 16;                   // columns of S^T and O^T
+  const int NS = (N + 31) & ~31;
+  const int n_op = (512 - 3 * NS) / 64;                              // 64-column operand slots in TMEM (2 to 6)
+  const int nK = n_op >= 3 ? 2 : 1, nV = n_op >= 4 ? 2 : 1;
+
+  const bool work = rows > 0 && nt > 0;
+  // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
+  const int qrow = (int)threadIdx.x >> 1, half = (int)threadIdx.x & 1;   // threads 0..255: half a row each
+  uint4 qv[8];
+  if (warp < 8) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) qv[c] = make_uint4(0, 0, 0, 0);
+    unsigned m = 0u;
+    if (half == 0) ms.orow[qrow] = -1;
+    if (qrow < rows) {
+      const int fr = mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
+      const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
+      if (pos >= p.q_base && pos < p.q_base + p.n_q) {
+        if (half == 0) ms.orow[qrow] = qr * p.H + g * p.hpg + hh;
+        if (work && half * 64 < D) {
+          const uint4* src = reinterpret_cast<const uint4*>(p.Q + (long long)(pos - p.q_base) * p.q_stride_row +
+                                                            (long long)(g * p.hpg + hh) * p.q_stride_head + half * 64);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) qv[c] = ld_ordered(src + c);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned u = w[e] & 0x7FFFu, v = (w[e] >> 16) & 0x7FFFu;  // magnitudes of bf16 order as integers
+              if (u < 0x7F80u) m = max(m, u);                                 // finite ones
+              if (v < 0x7F80u) m = max(m, v);
+            }
+          }
+        }
+      } else if (half == 0) {
+        set_status(p.status, FOCUS_ERR_INVALID_ARG);
+      }
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (lane == 0) atomicMax(&ms.qmax, m);
+  } else if (warp == 12 && use_list) {                                 // meanwhile: tile descriptors
+    for (int t = lane; t < nt; t += 32) {
+      const TileInfo ti = make_tile(t);
+      if (t0 + t < te.n_blk && ti.nvalid == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);
+      ms.tlist[t] = pack_tile(ti);
+    }
+  }
+  __syncthreads();
+  // the power of two: the tile's largest |q| to 2^14 .. 2^15
+  const int q_shift = ms.qmax ? min(14 - ((int)(ms.qmax >> 7) - 127), 126) : 0;
+  if (warp < 8 && work && half * 64 < D && qrow < NS) {
+    const float f = exp2f((float)q_shift);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+      uint32_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        o[i] = pack_f16(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xFFFF0000u) * f);
+      sts128(sQ + half * (QN * 128) + qrow * 128 + ((c ^ (qrow & 7)) << 4), o[0], o[1], o[2], o[3]);
+    }
+  }
+  const uint32_t tmem = ms.tmem;
+  const uint32_t tS = tmem, tO = tmem + 2 * NS, tOp = tmem + 3 * NS;
+  if (D == 64 && work && (warp == 10 || warp == 11)) {   // channels 64..127 do not exist: zeros, once
+    uint32_t z[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = 0u;
+    for (int b = 0; b < nV; ++b) {
+      const uint32_t a = tOp + (uint32_t)((nK + b) * 64) + ((uint32_t)((warp & 3) * 32) << 16);
+      TC_ST32(a, z);
+      TC_ST32(a + 32, z);
+    }
+    tc_wait_st();
+  }
+  fence_proxy_async();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+
+  if (wg == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 0 && work) {
+      // ================================ producer ==================================================
+      const uint64_t pol = l2_policy_evict_first();
+      bool ok = true;
+      int slot = 0, issued = 0;
+      uint32_t round = 0;
+      for (int j = 0; j < nt && ok; ++j) {
+        const TileInfo ti = get_tile(j);
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint32_t full = kv ? v_full(slot) : k_full(slot), empty = kv ? v_empty(slot) : k_empty(slot);
+          const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
+          ok = mbar_wait(empty, (round & 1u) ^ 1u, abort_flag, p.status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ++issued;
+          if (ti.kind == 0) {
+            fence_proxy_async();                                       // the slot may have been filled with plain copies before
+            if (lane == 0) {
+              const CUtensorMap* map = kv ? &tmV : &tmK;
+              mbar_expect_tx(full, TN * D);
+              if (p.pair) {
+                if (p.evict_first) {
+                  tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
+                  tma_load_3d_hint(dst + 64 * D, map, full, 0, ti.start2, g, pol);
+                } else {
+                  tma_load_3d(dst, map, full, 0, ti.start, g);
+                  tma_load_3d(dst + 64 * D, map, full, 0, ti.start2, g);
+                }
+              } else if (p.evict_first) {
+                tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
+              } else {
+                tma_load_3d(dst, map, full, 0, ti.start, g);
+              }
+            } else {
+              mbar_arrive(full);
+            }
+          } else {
+            // sink tokens lie anywhere: 16-byte copies, dropped ones as zeros
+            constexpr int CPR = D / 16;
+            const uint8_t* base = (kv ? p.V : p.K) + (long long)g * p.kv_stride_head;
+            int tok[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tok[i] = key_token(p, ti, g, i * 32 + lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+              for (int it = 0; it < CPR; ++it) {
+                const int q = it * 32 + lane, rr = q / CPR, c = q % CPR;      // row within this group of 32, chunk
+                const int t = __shfl_sync(0xffffffffu, tok[i], rr);
+                const uint32_t n = t >= 0 ? 16u : 0u;
+                const uint8_t* src = base + (long long)max(t, 0) * p.kv_stride_tok + c * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"(dst + raw_off<D>(i * 32 + rr, c)), "l"(src), "r"(n) : "memory");
+              }
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+            if (kv == 0) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {                            // a listed sink outside [0, L) is reported
+                const int k = i * 32 + lane;
+                if (k < ti.nvalid) {
+                  const int s = __ldg(p.sink_idx + ti.start + k);
+                  if (s < 0 || s >= p.L) set_status(p.status, FOCUS_ERR_INVALID_ARG);
+                }
+              }
+            }
+          }
+        }
+        if (++slot == RING) { slot = 0; ++round; }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (!ok) {
+        // unwinding: let the copies already issued land before the CTA's shared memory is released
+        for (int q = max(0, issued - 2 * RING); q < issued; ++q) {
+          const int i = q >> 1, sl = i % RING;
+          const uint64_t t_start = global_ns();
+          while (!mbar_try_wait(q & 1 ? v_full(sl) : k_full(sl), (uint32_t)(i / RING) & 1u)) {
+            if (global_ns() - t_start > WAIT_LIMIT_NS) break;
+          }
+        }
+      }
+    } else if (warp == 1 && lane == 0 && work) {
+      // ================================ MMA issuer ================================================
+      const uint32_t ID_QK = idesc_f16(N, 0), ID_PV = idesc_f16(N, 1);
+      const uint64_t qdesc = make_sdesc(sQ, 16, 1024);
+      bool ok = true;
+      int kb = 0, vb = 0;
+      uint32_t kr = 0, vr = 0;
+      auto do_pv = [&](int j) -> bool {
+        const int b = j & 1;
+        if (!mbar_wait(vop_full(vb), vr & 1u, abort_flag, p.status)) return false;
+        if (!mbar_wait(p_full(b), (uint32_t)(j >> 1) & 1u, abort_flag, p.status)) return false;
+        tc_fence_after();
+        const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
+        const uint32_t a = tOp + (uint32_t)((nK + vb) * 64);
+#pragma unroll
+        for (int ks = 0; ks < TN / 16; ++ks)
+          mma_ts(tO, a + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (j | ks) ? 1u : 0u);
+        tc_commit(vop_empty(vb));
+        tc_commit(p_empty(b));
+        if (++vb == nV) { vb = 0; ++vr; }
+        return true;
+      };
+      for (int j = 0; j < nt && ok; ++j) {
+        const int b = j & 1;
+        if (!mbar_wait(kop_full(kb), kr & 1u, abort_flag, p.status)) { ok = false; break; }
+        if (!mbar_wait(s_empty(b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t a = tOp + (uint32_t)(kb * 64);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_ts(tS + b * NS, a + ks * 8, qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), ID_QK, ks ? 1u : 0u);
+        tc_commit(kop_empty(kb));
+        tc_commit(s_full(b));
+        if (++kb == nK) { kb = 0; ++kr; }
+        if (j > 0) ok = do_pv(j - 1);
+      }
+      if (ok) do_pv(nt - 1);
+    }
+    __syncwarp();
+    tc_fence_before();
+    asm volatile("bar.sync 0;" ::: "memory");
+    tc_fence_after();
+    if (warp == 2) { __syncwarp(); tmem_dealloc(tmem, 512); }
+  } else if (wg == 1) {
+    // ================================ K codes -> A operand of S^T =====================================
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (work) {
+      const int key = (warp & 3) * 32 + lane;
+      const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+      int slot = 0, ob = 0;
+      uint32_t round = 0, orr = 0;
+      for (int j = 0; j < nt; ++j) {
+        bool ok = mbar_wait(k_full(slot), round & 1u, abort_flag, p.status) &&
+                  mbar_wait(kop_empty(ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        tc_fence_after();
+        const uint32_t src = sRawK + slot * SLOT, dst = tOp + (uint32_t)(ob * 64) + lane_off;
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) {
+          uint32_t o[32];
+          uint4 raw[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) raw[c] = lds128(src + raw_off<D>(key, h * 4 + c));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            expand(raw[c].x, o[8 * c + 0], o[8 * c + 1], F());
+            expand(raw[c].y, o[8 * c + 2], o[8 * c + 3], F());
+            expand(raw[c].z, o[8 * c + 4], o[8 * c + 5], F());
+            expand(raw[c].w, o[8 * c + 6], o[8 * c + 7], F());
+          }
+          TC_ST32(dst + h * 32, o);
+        }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(k_empty(slot)); mbar_arrive(kop_full(ob)); }
+        if (++slot == RING) { slot = 0; ++round; }
+        if (++ob == nK) { ob = 0; ++orr; }
+      }
+    }
+    tc_fence_before();
+    asm volatile("bar.sync 0;" ::: "memory");
+  } else if (wg == 2) {
+    // ================================ V codes, transposed -> A operand of O^T ===========================
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (work) {
+      const int cw = warp & 3;                                         // channels 32 cw .. 32 cw + 31
+      int slot = 0, ob = 0;
+      uint32_t round = 0, orr = 0;
+      for (int j = 0; j < nt; ++j) {
+        bool ok = mbar_wait(v_full(slot), round & 1u, abort_flag, p.status) &&
+                  mbar_wait(vop_empty(ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        tc_fence_after();
+        const uint32_t src = sRawV + slot * SLOT, dst = tOp + (uint32_t)((nK + ob) * 64) + ((uint32_t)(cw * 32) << 16);
+        if (cw * 32 < D) {
+#pragma unroll
+          for (int hc = 0; hc < 2; ++hc) {                             // sixteen channels
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {                              // 64 keys = four 16-key matrices
+              uint32_t o[16];
+#pragma unroll
+              for (int pr = 0; pr < 2; ++pr) {
+                uint32_t m[4];
+                ldsm_t8(src + raw_off<D>(q * 64 + pr * 32 + lane, cw * 2 + hc), m);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  expand(m[2 * i], o[(2 * pr + i) * 4 + 0], o[(2 * pr + i) * 4 + 1], F());
+                  expand(m[2 * i + 1], o[(2 * pr + i) * 4 + 2], o[(2 * pr + i) * 4 + 3], F());
+                }
+              }
+              TC_ST_FRAG16(dst + ((uint32_t)(hc * 16) << 16) + q * 32, o);
+            }
+          }
+        }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(v_empty(slot)); mbar_arrive(vop_full(ob)); }
+        if (++slot == RING) { slot = 0; ++round; }
+        if (++ob == nV) { ob = 0; ++orr; }
+      }
+    }
+    tc_fence_before();
+    asm volatile("bar.sync 0;" ::: "memory");
+  } else {
+    // ================================ softmax =========================================================
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+    const int NC = N >> 1, np = NC >> 3;                               // this warpgroup's rows, in pieces of 8
+    const int c0 = x * NC;
+    float l[64];
+#pragma unroll
+    for (int c = 0; c < 64; ++c) l[c] = 0.f;
+    if (work) {
+      bool ok = true;
+      const float cs = p.scale_log2 * exp2f((float)-q_shift);
+      const float* Ks = p.K_scale + (long long)g * p.scale_stride;
+      const float* Vs = p.V_scale + (long long)g * p.scale_stride;
+      auto scales = [&](int idx, float& sk, float& sv) {               // sv == -1: masked
+        sk = 0.f; sv = -1.f;
+        if (idx >= nt) return;
+        const int t = key_token(p, get_tile(idx), g, key);
+        if (t >= 0) { sk = __ldg(Ks + t); sv = __ldg(Vs + t); }
+      };
+      float sk0, sv0, sk1, sv1, sk2, sv2;                              // two tiles ahead: their latency is out of the way
+      scales(0, sk0, sv0);
+      scales(1, sk1, sv1);
+      for (int j = 0; j < nt; ++j) {
+        const int b = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+        scales(j + 2, sk2, sv2);
+        const bool masked = sv0 == -1.f;
+        const float svc = fmaxf(sv0, SV_MIN);
+        const float ck = sk0 * cs, lv = masked ? -INFINITY : __log2f(svc), iv = masked ? 0.f : __fdividef(1.f, svc);
+        sk0 = sk1; sv0 = sv1; sk1 = sk2; sv1 = sv2;
+        ok = __all_sync(0xffffffffu, mbar_wait(s_full(b), ph, abort_flag, p.status)) && ok;
+        tc_fence_after();
+        const uint32_t ts = tS + (uint32_t)(b * NS + c0) + lane_off;
+        float a[32];
+        // exponents of row group grp (32 rows): a = s ck + lv, minus the reference where `minus` is set
+        auto load_group = [&](int grp, bool minus) {
+          uint32_t* ar = reinterpret_cast<uint32_t*>(a);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (grp * 4 + i < np) TC_LD8(ts + (grp * 4 + i) * 8, ar + i * 8);
+          tc_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (grp * 4 + i < np) {
+              const float4* rf = reinterpret_cast<const float4*>(ms.ref + c0 + (grp * 4 + i) * 8);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float* v = a + i * 8 + h * 4;
+                ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
+                ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
+                if (minus) {
+                  const float4 rv = rf[h];
+                  fadd2(v[0], v[1], v[0], v[1], -rv.x, -rv.y);
+                  fadd2(v[2], v[3], v[2], v[3], -rv.z, -rv.w);
+                }
+              }
+            }
+        };
+        float mx = -INFINITY;
+        auto group_max = [&](int grp) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (grp * 4 + i < np) {
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) mx = fmax3(mx, a[i * 8 + e], a[i * 8 + e + 1]);
+            }
+        };
+        // the upper rows first: rows 0..31 stay in registers for the second pass
+        if (np > 4) { load_group(1, true); group_max(1); }
+        load_group(0, true);
+        group_max(0);
+        bool fresh = true;
+        if (named_any(1 + x, 128, mx > THRESH || !ok)) {
+          // ---- some row's maximum outgrew its reference (always so at the first key): new references ----
+          if (named_any(1 + x, 128, !ok)) break;
+          fresh = false;
+#pragma unroll 1
+          for (int grp = 0; grp * 4 < np; ++grp) {
+            load_group(grp, false);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (grp * 4 + i < np) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const unsigned k = __reduce_max_sync(0xffffffffu, float_key(a[i * 8 + e]));
+                  if (lane == 0) atomicMax(&ms.colmax[c0 + (grp * 4 + i) * 8 + e], k);
+                }
+              }
+          }
+          named_sync(1 + x, 128);
+          if (key < NC) {
+            const float old = ms.ref[c0 + key], now = key_to_float(ms.colmax[c0 + key]) - OFFSET;
+            const bool up = now > old;
+            ms.fac[c0 + key] = up ? ex2(old - now) : 1.f;
+            if (up) ms.ref[c0 + key] = now;
+            ms.colmax[c0 + key] = 0u;
+          }
+          named_sync(1 + x, 128);
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < NC) l[c] *= ms.fac[c0 + c];
+          if (j > 0) {
+            // the sums so far are in TMEM once P V of the last tile is done; P V of this one waits for its P
+            ok = __all_sync(0xffffffffu, mbar_wait(p_empty(b ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, p.status));
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < np; ++i) {
+              const uint32_t at = tO + (uint32_t)(c0 + i * 8) + lane_off;
+              uint32_t o[8];
+              TC_LD8(at, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ms.fac[c0 + i * 8 + e]);
+              TC_ST8(at, o);
+            }
+            tc_wait_st();
+          }
+        }
+        // ---- P = 2^(a - ref): row sums in fp32, fp16 to shared memory ----
+        ok = __all_sync(0xffffffffu, mbar_wait(p_empty(b), ph ^ 1u, abort_flag, p.status)) && ok;   // P V of tile j - 2
+        const uint32_t prow = sP + (uint32_t)(b * P_BYTES + key * 128);
+#pragma unroll
+        for (int grp = 0; grp < 2; ++grp) {
+          if (grp * 4 >= np) continue;
+          if (grp == 1 || !fresh) load_group(grp, true);
+          if (grp == 1 || np <= 4) {                                   // S_b is in registers: the next product may overwrite it
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(s_empty(b));
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (grp * 4 + i < np) {
+              float* v = a + i * 8;
+              float* lc = l + grp * 32 + i * 8;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = ex2(v[e]);
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) ffma2(lc[e], lc[e + 1], v[e], v[e + 1], iv, iv, lc[e], lc[e + 1]);
+              const int col = c0 + (grp * 4 + i) * 8;
+              sts128(prow + (uint32_t)((col >> 6) * (TN * 128)) + (uint32_t)((((col & 63) >> 3) ^ (key & 7)) << 4),
+                     pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+            }
+        }
+        fence_proxy_async();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(b));
+      }
+      // all products done?
+      mbar_wait(p_empty((nt - 1) & 1), (uint32_t)((nt - 1) >> 1) & 1u, abort_flag, p.status);
+      tc_fence_after();
+    }
+    // ---- row sums over the 128 keys: lane i of every warp ends with row i of a group, warps in order ----
+#pragma unroll
+    for (int grp = 0; grp < 2; ++grp) {
+      if (grp * 32 >= NC) continue;
+      float* v = l + grp * 32;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const bool hi = (lane & o) != 0;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+          const float send = hi ? v[i] : v[i + o], keep = hi ? v[i + o] : v[i];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+      }
+      ms.lsum[x * 4 + wq][grp * 32 + lane] = v[0];
+    }
+    named_sync(1 + x, 128);
+    if (key < NC) {
+      const int r = c0 + key;
+      const float tot = ((ms.lsum[x * 4][key] + ms.lsum[x * 4 + 1][key]) + ms.lsum[x * 4 + 2][key]) + ms.lsum[x * 4 + 3][key];
+      const float ref = ms.ref[r];
+      if (p.n_splits > 1) {
+        if (r < rows) reinterpret_cast<float2*>(p.part_ml)[(size_t)cta * QN + r] = make_float2(ref, tot);
+      } else {
+        ms.fac[r] = tot > 0.f ? 1.f / tot : (tot == 0.f ? 0.f : tot);   // NaN stays NaN
+        const int orow = ms.orow[r];
+        if (r < rows && orow >= 0 && p.lse)
+          p.lse[(size_t)(orow % p.H) * p.lse_stride + orow / p.H] = tot == 0.f ? -INFINITY : (ref + log2f(tot)) * 0.6931471805599453f;
+      }
+    }
+    named_sync(1 + x, 128);
+    // ---- O^T: this thread's channel of every row of its half ----
+    const int ch = key;
+#pragma unroll 1
+    for (int i = 0; i < np; ++i) {
+      uint32_t o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = 0u;
+      if (work) {
+        TC_LD8(tO + (uint32_t)(c0 + i * 8) + lane_off, o);
+        tc_wait_ld();
+      }
+      if (ch < D) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int r = c0 + i * 8 + e;
+          if (r < rows) {
+            if (p.n_splits > 1) {
+              p.part_O[((size_t)cta * QN + r) * D + ch] = __uint_as_float(o[e]);
+            } else if (ms.orow[r] >= 0) {
+              p.O[(size_t)ms.orow[r] * D + ch] = __float2bfloat16_rn(__uint_as_float(o[e]) * ms.fac[r]);
+            }
+          }
+        }
+      }
+    }
+    tc_fence_before();
+    asm volatile("bar.sync 0;" ::: "memory");
+    // ---- merge of the splits by the CTA that arrives last, splits in order ----
+    if (p.n_splits > 1 && rows > 0) {
+      const int tid = (int)threadIdx.x - 384, S = p.n_splits;
+      __threadfence();
+      named_sync(3, 256);
+      if (tid == 0) {
+        const int prev = atomicAdd(&p.counters[blockIdx.x], 1);
+        ms.last = prev == S - 1;
+        if (ms.last) p.counters[blockIdx.x] = 0;                       // armed for the next launch
+        __threadfence();
+      }
+      named_sync(3, 256);
+      if (ms.last) {
+        float* wts = reinterpret_cast<float*>(sptr + Q_BYTES);         // [row][split], over the P tiles
+        const size_t c_first = (size_t)blockIdx.x * S;
+        if (tid < rows) {
+          const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + c_first * QN + tid;
+          float m = -INFINITY, tot = 0.f;
+          for (int s = 0; s < S; ++s) {
+            const float2 v = __ldcg(ml + (size_t)s * QN);
+            if (v.y != 0.f) m = fmaxf(m, v.x);
+          }
+          for (int s = 0; s < S; ++s) {
+            const float2 v = __ldcg(ml + (size_t)s * QN);
+            const float w = v.y != 0.f ? ex2(v.x - m) : 0.f;
+            tot += w * v.y;
+            wts[tid * S + s] = w;
+          }
+          const int orow = ms.orow[tid];
+          ms.fac[tid] = tot != 0.f ? 1.f / tot : 0.f;
+          if (orow >= 0 && p.lse)
+            p.lse[(size_t)(orow % p.H) * p.lse_stride + orow / p.H] = tot == 0.f ? -INFINITY : (m + log2f(tot)) * 0.6931471805599453f;
+        }
+        named_sync(3, 256);
+        for (int it = tid; it < rows * (D / 4); it += 256) {
+          const int r = it / (D / 4), c4 = it % (D / 4), orow = ms.orow[r];
+          if (orow < 0) continue;
+          const float4* po = reinterpret_cast<const float4*>(p.part_O) + (c_first * QN + r) * (D / 4) + c4;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int s = 0; s < S; ++s) {
+            const float w = wts[r * S + s];
+            const float4 o = __ldcg(po + (size_t)s * QN * (D / 4));
+            if (w != 0.f) { acc.x += w * o.x; acc.y += w * o.y; acc.z += w * o.z; acc.w += w * o.w; }
+          }
+          const float f = ms.fac[r];
+          uint2 v;
+          v.x = pack_bf16(acc.x * f, acc.y * f);
+          v.y = pack_bf16(acc.z * f, acc.w * f);
+          *reinterpret_cast<uint2*>(p.O + (size_t)orow * D + c4 * 4) = v;
+        }
+      }
+    }
+  }
+}
+
+bool encode_code_map(void* fn, CUtensorMap* map, const void* base, const focus_shape& s, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)s.head_dim, (cuuint64_t)s.L, (cuuint64_t)s.n_kv_heads};
+  const cuuint64_t strides[2] = {(cuuint64_t)s.kv_stride_tok, (cuuint64_t)s.kv_stride_head};
+  const cuuint32_t box[3] = {(cuuint32_t)s.head_dim, (cuuint32_t)box_rows, 1};
+  const cuuint32_t one[3] = {1, 1, 1};
+  return ((EncodeTiledFn)fn)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, one,
+                             CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             s.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename F, int D>
+focus_status launch(focus_ctx* ctx, bool& attr_set, const CUtensorMap& tmK, const CUtensorMap& tmV, const QParams& p,
+                    dim3 grid, cudaStream_t st) {
+  if (!attr_set) {
+    if (cudaFuncSetAttribute(attn_quant_tc_kernel<F, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess)
+      return FOCUS_ERR_CUDA;
+    attr_set = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(NTH, 1, 1); cfg.dynamicSmemBytes = SMEM; cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = p.pdl ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, attn_quant_tc_kernel<F, D>, tmK, tmV, p) != cudaSuccess) {
+    cudaGetLastError();
+    return FOCUS_ERR_CUDA;
+  }
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
+
+constexpr int MAX_SPLITS = 64;
+
+}  // namespace
+
+bool attn_quant_tc_supported(const focus_ctx* ctx, const AttnArgs& a) {
+  return ctx->encode_tiled != nullptr && a.sh.dtype == FOCUS_BF16 && (a.sh.head_dim == 128 || a.sh.head_dim == 64) &&
+         (a.sh.n_q_heads / a.sh.n_kv_heads) <= QN && (long long)a.max_rows * a.sh.n_q_heads < (1ll << 31);
+}
+
+focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
+  const focus_shape& sh = a.sh;
+  const int Hkv = sh.n_kv_heads, hpg = sh.n_q_heads / Hkv;
+  const long long stacked = (long long)a.max_rows * hpg;              // stacked query rows per KV head (host bound)
+  QParams p;
+  p.pair = !a.dense && sh.kv_block == 64;
+  p.ns_pad = a.dense ? 0 : (a.n_sink + TN - 1) / TN * TN;
+  const int n_resp = a.dense ? (sh.L + TN - 1) / TN : (sh.L - sh.M + TN - 1) / TN;
+  const int max_tiles = a.dense ? n_resp : (p.pair ? (a.max_blocks + 1) / 2 : a.max_blocks) + p.ns_pad / TN + n_resp;
+  p.n_mtiles = (int)((stacked + QN - 1) / QN);
+  const long long base = (long long)p.n_mtiles * Hkv;
+  if (base > 0x7FFFFFFF) return FOCUS_ERR_UNSUPPORTED;
+  // key splits: as many CTAs as SMs, at least two tiles each
+  int splits = (int)(ctx->sm_count / base);
+  if (splits > max_tiles / 2) splits = max_tiles / 2;
+  if (splits > MAX_SPLITS) splits = MAX_SPLITS;
+  if (splits < 1) splits = 1;
+  p.n_splits = splits;
+  p.part_O = p.part_ml = nullptr;
+  if (splits > 1) {
+    WsAlloc ws(ctx);
+    p.part_O = ws.get<float>((size_t)base * splits * QN * sh.head_dim);
+    p.part_ml = ws.get<float>((size_t)base * splits * QN * 2);
+    if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
+  }
+  p.counters = ctx->d_counters;
+  p.Q = (const __nv_bfloat16*)a.Q; p.O = (__nv_bfloat16*)a.O; p.lse = a.lse;
+  p.q_rows = a.q_rows; p.n_rows = a.n_rows; p.block_idx = a.block_idx; p.block_cnt = a.block_cnt;
+  p.sink_idx = a.sink_idx; p.sink_keep = a.sink_keep;
+  p.K = (const uint8_t*)a.qc->K; p.V = (const uint8_t*)a.qc->V; p.K_scale = a.qc->K_scale; p.V_scale = a.qc->V_scale;
+  p.q_stride_row = sh.q_stride_row; p.q_stride_head = sh.q_stride_head;
+  p.kv_stride_tok = sh.kv_stride_tok; p.kv_stride_head = sh.kv_stride_head; p.scale_stride = quant_scale_stride(a.qc, &sh);
+  p.q_base = a.q_base; p.n_q = a.n_q; p.rows_bound = a.max_rows; p.L = sh.L; p.M = sh.M; p.H = sh.n_q_heads; p.hpg = hpg;
+  p.B = sh.kv_block; p.nb = shape_nb(&sh); p.dense = a.dense; p.group_stride = a.group_stride;
+  p.max_blocks = a.max_blocks; p.n_sink = a.n_sink; p.lse_stride = a.lse_stride;
+  p.pdl = ctx->no_pdl ? 0 : 1;
+  p.evict_first = p.n_mtiles == 1;                                     // otherwise the row tiles of a head share its K/V in L2
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.status = ctx->d_status;
+  CUtensorMap tmK, tmV;
+  const int box_rows = p.pair ? 64 : TN;
+  if (!encode_code_map(ctx->encode_tiled, &tmK, p.K, sh, box_rows) || !encode_code_map(ctx->encode_tiled, &tmV, p.V, sh, box_rows))
+    return FOCUS_ERR_INVALID_ARG;
+  ctx->last_attn_variant = 5;
+  const dim3 grid((unsigned)base, splits, 1);
+  const bool i8 = a.qc->format == FOCUS_KV_INT8;
+  bool* set = ctx->ls.quant_attr_set;
+  if (sh.head_dim == 128)
+    return i8 ? launch<int8_t, 128>(ctx, set[0], tmK, tmV, p, grid, st) : launch<__nv_fp8_e4m3, 128>(ctx, set[1], tmK, tmV, p, grid, st);
+  return i8 ? launch<int8_t, 64>(ctx, set[2], tmK, tmV, p, grid, st) : launch<__nv_fp8_e4m3, 64>(ctx, set[3], tmK, tmV, p, grid, st);
+}
+
+size_t attn_quant_tc_workspace(const focus_shape* s, int n_q) {
+  // partial outputs of every split: no more CTAs than SMs take part in a split launch (160 bounds the part at hand)
+  (void)n_q;
+  return (size_t)160 * QN * ((size_t)s->head_dim + 2) * 4 + 1024;
+}

@@ -124,6 +124,8 @@ extern "C" focus_status focus_workspace_bytes(const focus_shape* shape, int32_t 
   size_t sink = H * L * 4 + L * 4 + H * (size_t)n_q * 4 + (size_t)n_q * H * shape->head_dim * 2 + 4096;
   size_t score = (size_t)shape->n_kv_heads * (shape->head_dim + shape_nb(shape)) * 4 + 1024;
   size_t attn = attn_tc_workspace(shape, n_q, max_blocks, n_sink);
+  const size_t quant = attn_quant_tc_workspace(shape, n_q);
+  if (quant > attn) attn = quant;
   // focus_find_sinks without a log-sum-exp runs an attention pass on top of its own buffers: the two add up
   size_t m = sink + attn;
   *out_bytes = (m > score ? m : score) + 4096;
@@ -163,7 +165,11 @@ static focus_status attn_sparse_keys(int head_reduce, const int32_t* block_idx, 
 
 static focus_status attn_dispatch(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
   if (a.max_rows == 0) return FOCUS_OK;
-  if (!ctx->force_simt && !a.qc && attn_tc_supported(ctx, a)) return launch_attn_tc(ctx, a, st);
+  if (a.qc) {
+    if (!ctx->force_simt && attn_quant_tc_supported(ctx, a)) return launch_attn_quant_tc(ctx, a, st);
+  } else if (!ctx->force_simt && attn_tc_supported(ctx, a)) {
+    return launch_attn_tc(ctx, a, st);
+  }
   ctx->last_attn_variant = 1;
   return launch_attn_simt(ctx, a, st);
 }

@@ -27,7 +27,7 @@ struct focus_ctx {
   // launch state that belongs to the device (function attributes, occupancy answers): kept per context, since a
   // process may hold contexts on several devices.  Zero-initialised by focus_create.
   struct LaunchState {
-    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[2];
+    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[2], quant_attr_set[4];
     int sink_attr_smem;
     int cluster_cap[9], cluster_cap_w[9], cluster_cap_k[9];   // co-resident clusters per cluster size, value + 1 (0 = not asked yet)
     int select_cluster;                        // 0 not tried, 1 works, 2 the cluster launch was refused once
@@ -284,3 +284,7 @@ focus_status launch_attn_tc_ws(focus_ctx* ctx, const AttnArgs& a, WsAlloc& ws, c
 focus_status launch_attn_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st);
 bool attn_tc_supported(const focus_ctx* ctx, const AttnArgs& a);
 size_t attn_tc_workspace(const focus_shape* s, int n_q, int max_blocks, int n_sink);
+// the same over an 8-bit cache (a.qc non-NULL)
+focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st);
+bool attn_quant_tc_supported(const focus_ctx* ctx, const AttnArgs& a);
+size_t attn_quant_tc_workspace(const focus_shape* s, int n_q);

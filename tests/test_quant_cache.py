@@ -239,13 +239,18 @@ def _attention_case(rng, dtype, fmt, H, Hkv, d, L, N, spread=1.0):
     return Q, out[0], out[1]
 
 
-def _bounds(Q, K, V, O, scale, hpg, dtype, keys=None):
+def _bounds(Q, K, V, vs, O, scale, hpg, dtype, keys=None):
     """Elementwise bounds of O and lse, from the roundings on the way.
 
     Logits: d products summed in fp32 are off by at most E = (d + 4) 2^-24 sum|q k| scale (one step per addition); the
     tensor-core path also carries q in fp16 relative to its row's largest element, subnormal below 2^-14 of it, which
     adds 2^-24 max|q| sum|k|.  Every numerator is then off by a factor 1 + E + 2^-21 (exp2), the ones that meet V by
-    another 2^-11 (fp16), sums over the n keys by n 2^-24, and the output is rounded once (bf16: 2^-8)."""
+    another 2^-11 (fp16), sums over the n keys by n 2^-24, and the output is rounded once (bf16: 2^-8).
+
+    fp16 also has a smallest step.  A numerator that meets V is p_j sv_j in units that put the row's largest at 2^6 or
+    more, and fp16 numbers below 2^-14 are 2^-24 apart: off by at most 2^-25, i.e. 2^-31 of the row's largest p_j sv_j.
+    The codes weigh those errors, so a channel is off by at most 2^-31 max_j(p_j sv_j) sum_j |cv_j| more (it shows where
+    the token that holds nearly all the weight has code 0 in that channel)."""
     n, H, d = Q.shape
     tolO, tolL = np.zeros_like(O), np.zeros((H, n))
     for h in range(H):
@@ -261,7 +266,10 @@ def _bounds(Q, K, V, O, scale, hpg, dtype, keys=None):
         A = p @ np.abs(Vg)
         num = E + 2.0 ** -21 + len(Kg) * 2.0 ** -24
         per = num * 2 + (2.0 ** -11 if dtype == "bf16" else 0.0)
-        tolO[:, h] = per[:, None] * A + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * np.abs(O[:, h]) + 1e-30
+        sv = vs[g] if keys is None else vs[g][keys[g]]
+        codes = np.abs(np.divide(Vg, sv[:, None], out=np.zeros_like(Vg), where=sv[:, None] > 0)).sum(0)
+        step = 2.0 ** -31 * (p * sv).max(1)[:, None] * codes if dtype == "bf16" else 0.0
+        tolO[:, h] = step + per[:, None] * A + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * np.abs(O[:, h]) + 1e-30
         tolL[h] = num + 2.0 ** -22 * (1 + np.abs(np.log(np.exp(s - s.max(1, keepdims=True)).sum(1)) + s.max(1)))
     return tolO, tolL
 
@@ -304,7 +312,7 @@ def test_dense_attention_over_an_8bit_cache(ctx, simt, fmt, dtype, H, Hkv, d, L,
         ctx.set_force_simt(False)
     Qf = wl.storage_to_f64(Q, dtype)[pos - q_base]
     eO, eL = fo.dense_attn(Qf, K, V, 1.0 / math.sqrt(d))
-    tO, tL = _bounds(Qf, K, V, eO, 1.0 / math.sqrt(d), H // Hkv, dtype)
+    tO, tL = _bounds(Qf, K, V, vs, eO, 1.0 / math.sqrt(d), H // Hkv, dtype)
     assert (np.abs(fstep.from_device(O)[:n] - eO) <= tO).all()
     assert (np.abs(fstep.from_device(lse)[:, :n] - eL) <= tL).all()
     assert (O[n:] == 9).all() and (lse[:, n:] == 9).all()
@@ -366,7 +374,7 @@ def test_sparse_attention_over_an_8bit_cache(ctx, simt, fmt, case):
     K, V = r["kc"] * r["ks"][..., None], r["vc"] * r["vs"][..., None]
     eO, eL = fo.sparse_attn(r["Q"], K, V, M, B, r["blocks"], r["sink"], scale)
     keys = [fo.key_set(M, L, B, r["blocks"][0 if all_heads else g], r["sink"]) for g in range(Hkv)]
-    tO, tL = _bounds(r["Q"], K, V, eO, scale, H // Hkv, dtype, keys)
+    tO, tL = _bounds(r["Q"], K, V, r["vs"], eO, scale, H // Hkv, dtype, keys)
     assert (np.abs(fstep.from_device(r["O"])[:n] - eO) <= tO).all()
     assert (np.abs(fstep.from_device(r["lse"])[:, :n] - eL) <= tL).all()
     assert (r["O"][n:] == 9).all() and (r["lse"][:, n:] == 9).all()
@@ -416,7 +424,7 @@ def test_unattended_rows_may_hold_anything(ctx, simt):
         keys = fo.key_set(M, L, B, r["blocks"][g], r["sink"][seen["keep"][g] != 0])
         K, V = (c[g][keys] * s[g][keys][:, None] for c, s in ((r["kc"], r["ks"]), (r["vc"], r["vs"])))
         eO, eL = fo.dense_attn(r["Q"][:, g:g + 1], K[None], V[None], 1.0 / math.sqrt(d))
-        tO, tL = _bounds(r["Q"][:, g:g + 1], K[None], V[None], eO, 1.0 / math.sqrt(d), 1, "bf16")
+        tO, tL = _bounds(r["Q"][:, g:g + 1], K[None], V[None], r["vs"][g:g + 1, keys], eO, 1.0 / math.sqrt(d), 1, "bf16")
         assert (np.abs(fstep.from_device(r["O"])[:, g:g + 1] - eO) <= tO).all()
         assert (np.abs(fstep.from_device(r["lse"])[g:g + 1] - eL) <= tL).all()
     assert ctx.poll_status() == 0
@@ -455,7 +463,7 @@ def test_scales_and_logits_of_unequal_size(ctx, simt, kind):
         ctx.set_force_simt(False)
     Qf = wl.storage_to_f64(Q, "bf16")
     eO, eL = fo.dense_attn(Qf, K, V, 1.0 / math.sqrt(d))
-    tO, tL = _bounds(Qf, K, V, eO, 1.0 / math.sqrt(d), 1, "bf16")
+    tO, tL = _bounds(Qf, K, V, vs, eO, 1.0 / math.sqrt(d), 1, "bf16")
     assert (np.abs(fstep.from_device(O) - eO) <= tO).all()
     assert (np.abs(fstep.from_device(lse) - eL) <= tL).all()
     assert ctx.poll_status() == 0
@@ -539,13 +547,13 @@ def test_a_sparse_layer_over_an_8bit_cache(ctx, fmt):
         q = Q.double().cpu().numpy()[rows.cpu().numpy() - M]
         scale = 1.0 / math.sqrt(d)
         eO, eL = fo.dense_attn(q, Kd, Vd, scale)
-        tO, tL = _bounds(q, Kd, Vd, eO, scale, H // Hkv, "bf16")
+        tO, tL = _bounds(q, Kd, Vd, want[1][1], eO, scale, H // Hkv, "bf16")
         assert (np.abs(fstep.from_device(O) - eO) <= tO).all() and (np.abs(fstep.from_device(lse) - eL) <= tL).all()
         bl, sk = [b for b in blocks.cpu().numpy()], sinks.cpu().numpy()
         assert all((b >= 0).all() for b in bl) and (sk >= 0).all()
         eO, eL = fo.sparse_attn(q, Kd, Vd, M, B, bl, sk, scale)
         keys = [fo.key_set(M, L, B, bl[g], sk) for g in range(Hkv)]
-        tO, tL = _bounds(q, Kd, Vd, eO, scale, H // Hkv, "bf16", keys)
+        tO, tL = _bounds(q, Kd, Vd, want[1][1], eO, scale, H // Hkv, "bf16", keys)
         assert (np.abs(fstep.from_device(O2) - eO) <= tO).all() and (np.abs(fstep.from_device(lse2) - eL) <= tL).all()
 
     layer()
