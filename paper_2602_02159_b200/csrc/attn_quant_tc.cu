@@ -33,6 +33,7 @@ using namespace tc;
 
 namespace {
 
+// registers per thread after the roles split: 32 + 64 + 64 + 160 + 160 = 480 = 5 x the 96 of the launch
 constexpr int QN = 128;                        // most query rows per CTA
 constexpr int NTH = 640;
 constexpr int RING = 3;                        // raw slots per ring (K, V)
@@ -42,8 +43,8 @@ constexpr int P_BYTES = TN * QN * 2;           // P^T of one tile: [key][row], t
 constexpr int MAXT = 256;                      // key tiles of a split whose descriptors are staged
 constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
-constexpr float THRESH = 8.f;                  // the reference follows the maximum once it is this far (log2) above ...
-constexpr float OFFSET = 6.f;                  // ... and is put this far below it: P <= 2^14, normal fp16 down to 2^-20
+constexpr float THRESH = 15.5f;               // the reference follows the maximum once that is this far (log2) above ...
+constexpr float OFFSET = 6.f;                  // ... and is put this far below it: P <= 2^15.5, normal fp16 down to 2^-20
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
 constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
                                                     // rows hold zeros, the writer flushes them)
@@ -72,14 +73,16 @@ struct QParams {
   int32_t* status;
 };
 
+constexpr int MAX_STOK = 8;                    // sink tiles of a split whose tokens are staged
+
 struct Misc {                                  // behind the tiles in shared memory
   unsigned long long bars[4 * RING + 16];
-  float ref[QN];                               // reference exponent per row
-  float fac[QN];                               // rescale factor / normaliser per row
-  unsigned colmax[QN];
+  float nref[2][QN];                           // minus the reference exponent per row (set 1: second warpgroup's own)
+  float fac[2][QN];                            // rescale factor / weight per row
+  float red[8][64];                            // per softmax warp: column maxima, then row sums
   int orow[QN];                                // output row (position slot * H + head), -1: none
-  float lsum[8][64];                           // row sums per softmax warp
   int2 tlist[MAXT];
+  int stok[MAX_STOK * TN];                     // tokens of the sink tiles, -1: dropped
   uint32_t tmem;
   int abort_flag, last;
   unsigned qmax;
@@ -157,13 +160,250 @@ __device__ __forceinline__ uint32_t raw_off(int row, int c) {
 }
 
 // Token of column k of a tile, or -1 if the column is masked out (padding, a sink that is dropped or out of range).
-__device__ __forceinline__ int key_token(const QParams& p, const TileInfo& ti, int g, int k) {
-  if (k >= ti.nvalid) return -1;
-  if (ti.kind == 0) return (k < 64 ? ti.start : ti.start2 - 64) + k;
-  const int s = ti.start + k;
+__device__ __forceinline__ int sink_token(const QParams& p, int g, int s) {
   const int j = __ldg(p.sink_idx + s);
   const bool keep = __ldg(p.sink_keep + (size_t)g * p.group_stride * p.n_sink + s) != 0;
   return (keep && j >= 0 && j < p.M) ? j : -1;             // response tokens are attended through their own tiles
+}
+
+struct Geo {                                   // what the roles share about their CTA
+  int g, t0, nt, N, NS, nK, nV;
+  TileEnum te;
+  int stok_first;                              // first sink (list position) in Misc::stok, and how many are there
+  int stok_n;
+  uint32_t sP, sBar, tmem;
+  float cs;                                    // logit scale: softmax scale * log2(e) / query scale
+};
+// tile idx of this split: by arithmetic (dense), from the staged list, or from the block list (splits longer than that)
+__device__ __forceinline__ TileInfo make_tile(const QParams& p, const Geo& gm, int idx) {
+  TileInfo ti = tile_info(p, gm.te, gm.t0 + idx);
+  if (ti.nvalid == 0) ti.start = ti.start2 = (p.L + 63) & ~63;         // bad block index: wholly outside, arrives as zeros
+  return ti;
+}
+__device__ __forceinline__ TileInfo get_tile(const QParams& p, const Misc& ms, const Geo& gm, int idx) {
+  if (!p.dense && gm.nt <= MAXT) return unpack_tile(ms.tlist[idx]);
+  return make_tile(p, gm, idx);
+}
+__device__ __forceinline__ int key_token(const QParams& p, const Misc& ms, const Geo& gm, const TileInfo& ti, int k) {
+  if (k >= ti.nvalid) return -1;
+  if (ti.kind == 0) return (k < 64 ? ti.start : ti.start2 - 64) + k;
+  const int s = ti.start + k, i = s - gm.stok_first;
+  return i >= 0 && i < gm.stok_n ? ms.stok[i] : sink_token(p, gm.g, s);
+}
+
+__device__ __forceinline__ uint32_t bar_k_full(uint32_t b, int s) { return b + 8u * s; }
+__device__ __forceinline__ uint32_t bar_k_empty(uint32_t b, int s) { return b + 8u * (RING + s); }
+__device__ __forceinline__ uint32_t bar_v_full(uint32_t b, int s) { return b + 8u * (2 * RING + s); }
+__device__ __forceinline__ uint32_t bar_v_empty(uint32_t b, int s) { return b + 8u * (3 * RING + s); }
+__device__ __forceinline__ uint32_t bar_kop_full(uint32_t b, int i) { return b + 8u * (4 * RING + i); }
+__device__ __forceinline__ uint32_t bar_kop_empty(uint32_t b, int i) { return b + 8u * (4 * RING + 2 + i); }
+__device__ __forceinline__ uint32_t bar_vop_full(uint32_t b, int i) { return b + 8u * (4 * RING + 4 + i); }
+__device__ __forceinline__ uint32_t bar_vop_empty(uint32_t b, int i) { return b + 8u * (4 * RING + 6 + i); }
+__device__ __forceinline__ uint32_t bar_s_full(uint32_t b, int i) { return b + 8u * (4 * RING + 8 + i); }
+__device__ __forceinline__ uint32_t bar_s_empty(uint32_t b, int i) { return b + 8u * (4 * RING + 10 + i); }
+__device__ __forceinline__ uint32_t bar_p_full(uint32_t b, int i) { return b + 8u * (4 * RING + 12 + i); }
+__device__ __forceinline__ uint32_t bar_p_empty(uint32_t b, int i) { return b + 8u * (4 * RING + 14 + i); }
+
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+
+// Reduces 32 values per lane over the 32 lanes by halving: 31 shuffles, lane i ends with the result of value i.
+template <typename Op>
+__device__ __forceinline__ float lane_reduce32(float* v, int lane, Op op) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool hi = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float send = hi ? v[i] : v[i + o], keep = hi ? v[i + o] : v[i];
+      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, o));
+    }
+  }
+  return v[0];
+}
+
+// Softmax of one warpgroup (x = 0, 1), NP pieces of 8 rows; straight-line code per tile, since its length in cycles is
+// what a tile costs.
+//   ALT   (N <= 64)  the two warpgroups take the key tiles in turn, all N rows each, with references, sums and O of
+//                    their own (joined at the end): a tile's chain of latencies has two tile periods of time
+//   !ALT  (N > 64)   every tile, half of the rows each
+// Leaves the row sums over this warpgroup's keys in ms.red.
+template <int NP, bool ALT>
+__device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const Geo& gm, int x, int wq, int lane) {
+  constexpr int NC = NP * 8;
+  constexpr int NG = NP <= 6 ? 1 : 2;                                  // more rows do not fit the registers twice (a and l)
+  constexpr int GP = NP / NG;                                          // pieces per group
+  const int key = wq * 32 + lane, nt = gm.nt, set = ALT ? x : 0;
+  const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+  const int c0 = ALT ? 0 : x * NC;                                     // first row (column of S^T)
+  const uint32_t tO = gm.tmem + (uint32_t)((2 + set) * gm.NS + c0) + lane_off;
+  volatile int* abort_flag = &ms.abort_flag;
+  float* nref = ms.nref[set] + c0;
+  float* fac = ms.fac[set] + c0;
+  float* red = ms.red[x * 4 + wq];
+  const float* Ks = p.K_scale + (long long)gm.g * p.scale_stride;
+  const float* Vs = p.V_scale + (long long)gm.g * p.scale_stride;
+  float l[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) l[c] = 0.f;
+  constexpr int STEP = ALT ? 2 : 1;
+  auto scales = [&](int idx, float& sk, float& sv) {                   // sv == -1: masked
+    sk = 0.f; sv = -1.f;
+    if (idx >= nt) return;
+    const int t = key_token(p, ms, gm, get_tile(p, ms, gm, idx), key);
+    if (t >= 0) { sk = __ldg(Ks + t); sv = __ldg(Vs + t); }
+  };
+  float sk, sv;
+  scales(ALT ? x : 0, sk, sv);
+  bool ok = true;
+  for (int j = ALT ? x : 0; j < nt; j += STEP) {
+    const int b = j & 1;
+    const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+    const bool masked = sv == -1.f;
+    const float svc = fmaxf(sv, SV_MIN);
+    const float ck = sk * gm.cs, lv = masked ? -INFINITY : __log2f(svc), iv = masked ? 0.f : __fdividef(1.f, svc);
+    scales(j + STEP, sk, sv);                                          // the next tile's, out of the way of their latency
+    ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(gm.sBar, b), ph, abort_flag, p.status)) && ok;
+    tc_fence_after();
+    const uint32_t ts = gm.tmem + (uint32_t)(b * gm.NS + c0) + lane_off;
+    float a[GP * 8];
+    uint32_t* ar = reinterpret_cast<uint32_t*>(a);
+    // exponents a = s ck + lv - ref of group grp
+    auto load_group = [&](int grp) {
+#pragma unroll
+      for (int i = 0; i < GP; ++i) TC_LD8(ts + (grp * GP + i) * 8, ar + i * 8);
+      tc_wait_ld();
+      const float4* rf = reinterpret_cast<const float4*>(nref + grp * GP * 8);
+#pragma unroll
+      for (int q = 0; q < GP * 2; ++q) {
+        const float4 rv = rf[q];
+        float* v = a + q * 4;
+        ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
+        ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
+        fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
+        fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
+      }
+    };
+    float mx = -INFINITY;
+#pragma unroll
+    for (int grp = NG - 1; grp >= 0; --grp) {                          // group 0 last: it stays in registers
+      load_group(grp);
+      float m1 = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < GP * 8; e += 4) {
+        mx = fmax3(mx, a[e], a[e + 1]);
+        m1 = fmax3(m1, a[e + 2], a[e + 3]);
+      }
+      mx = fmaxf(mx, m1);
+    }
+    if (named_any(1 + x, 128, mx > THRESH || !ok)) {
+      // ---- some row's maximum outgrew its reference (always so at the first key): new references ----
+      if (named_any(1 + x, 128, !ok)) break;
+#pragma unroll 1
+      for (int h = 0; h * 4 < NP; ++h) {                               // 32 rows at a time
+        float v[32];
+        uint32_t* vr = reinterpret_cast<uint32_t*>(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (h * 4 + i < NP) {
+            TC_LD8(ts + (h * 4 + i) * 8, vr + i * 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i * 8 + e] = -INFINITY;
+          }
+        }
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = (h * 4 + (e >> 3) < NP) ? fmaf(v[e], ck, lv) : -INFINITY;
+        red[h * 32 + lane] = lane_reduce32(v, lane, [](float u, float w) { return fmaxf(u, w); });
+      }
+      named_sync(1 + x, 128);
+      if (key < NC) {
+        const float(*r)[64] = &ms.red[x * 4];
+        const float top = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
+        const float old = nref[key], now = OFFSET - top;
+        const bool up = now < old;
+        fac[key] = up ? ex2(now - old) : 1.f;
+        if (up) nref[key] = now;
+      }
+      named_sync(1 + x, 128);
+#pragma unroll
+      for (int q = 0; q < NP * 2; ++q) {
+        const float4 f = reinterpret_cast<const float4*>(fac)[q];
+        l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w;
+      }
+      // what these rows have summed is in TMEM once the last P V is done; P V of this tile waits for its P
+      const int prev = ALT ? j - 2 : j - 1;
+      if (prev >= 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, prev & 1), (uint32_t)(prev >> 1) & 1u, abort_flag, p.status));
+        tc_fence_after();
+#pragma unroll 1
+        for (int h = 0; h * 2 < NP; ++h) {
+          uint32_t o[16];
+          TC_LD8(tO + h * 16, o);
+          TC_LD8(tO + h * 16 + 8, o + 8);
+          tc_wait_ld();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 f = reinterpret_cast<const float4*>(fac)[h * 4 + q];
+            o[4 * q] = __float_as_uint(__uint_as_float(o[4 * q]) * f.x);
+            o[4 * q + 1] = __float_as_uint(__uint_as_float(o[4 * q + 1]) * f.y);
+            o[4 * q + 2] = __float_as_uint(__uint_as_float(o[4 * q + 2]) * f.z);
+            o[4 * q + 3] = __float_as_uint(__uint_as_float(o[4 * q + 3]) * f.w);
+          }
+          TC_ST8(tO + h * 16, o);
+          TC_ST8(tO + h * 16 + 8, o + 8);
+        }
+        tc_wait_st();
+      }
+      load_group(0);
+    }
+    // ---- P = 2^a: row sums in fp32, fp16 to shared memory ----
+    const uint32_t prow = gm.sP + (uint32_t)(b * P_BYTES + key * 128);
+    bool waited = false;
+#pragma unroll
+    for (int grp = 0; grp < NG; ++grp) {
+      if (grp > 0) load_group(grp);
+      if (grp == NG - 1) {                                             // S_b is in registers: the next product may overwrite it
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_n(bar_s_empty(gm.sBar, b), STEP);
+      }
+#pragma unroll
+      for (int e = 0; e < GP * 8; ++e) a[e] = ex2(a[e]);
+      if (!waited) {                                                   // P V of tile j - 2 has read this buffer
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, b), ph ^ 1u, abort_flag, p.status)) && ok;
+        waited = true;
+      }
+#pragma unroll
+      for (int i = 0; i < GP; ++i) {
+        const float* v = a + i * 8;
+        const int col = c0 + (grp * GP + i) * 8;
+        sts128(prow + (uint32_t)((col >> 6) * (TN * 128)) + (uint32_t)((((col & 63) >> 3) ^ (key & 7)) << 4),
+               pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+      }
+      fence_proxy_async();
+      float* lc = l + grp * GP * 8;
+#pragma unroll
+      for (int e = 0; e < GP * 8; e += 2) ffma2(lc[e], lc[e + 1], a[e], a[e + 1], iv, iv, lc[e], lc[e + 1]);
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_n(bar_p_full(gm.sBar, b), STEP);
+  }
+  // all products done (each warpgroup waits for both buffers: their last two tiles)
+  for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) mbar_wait(bar_p_empty(gm.sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag, p.status);
+  tc_fence_after();
+  // ---- row sums over this warp's 32 keys: lane i of a warp ends with row i of a group ----
+  named_sync(1 + x, 128);                                              // the column maxima in ms.red have been read
+#pragma unroll
+  for (int h = 0; h * 4 < NP; ++h) {
+    float v[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = h * 32 + e < NC ? l[h * 32 + e < NC ? h * 32 + e : 0] : 0.f;
+    red[h * 32 + lane] = lane_reduce32(v, lane, [](float u, float w) { return u + w; });
+  }
 }
 
 template <typename F, int D>
@@ -177,38 +417,26 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   Misc& ms = *reinterpret_cast<Misc*>(sptr + OFF_MISC);
   const uint32_t sQ = sbase, sP = sbase + Q_BYTES, sRawK = sbase + OFF_RAW, sRawV = sRawK + RING * SLOT;
   const uint32_t sBar = smem_u32(ms.bars);
-  auto k_full = [&](int s) { return sBar + 8u * s; };
-  auto k_empty = [&](int s) { return sBar + 8u * (RING + s); };
-  auto v_full = [&](int s) { return sBar + 8u * (2 * RING + s); };
-  auto v_empty = [&](int s) { return sBar + 8u * (3 * RING + s); };
-  auto kop_full = [&](int b) { return sBar + 8u * (4 * RING + b); };
-  auto kop_empty = [&](int b) { return sBar + 8u * (4 * RING + 2 + b); };
-  auto vop_full = [&](int b) { return sBar + 8u * (4 * RING + 4 + b); };
-  auto vop_empty = [&](int b) { return sBar + 8u * (4 * RING + 6 + b); };
-  auto s_full = [&](int b) { return sBar + 8u * (4 * RING + 8 + b); };
-  auto s_empty = [&](int b) { return sBar + 8u * (4 * RING + 10 + b); };
-  auto p_full = [&](int b) { return sBar + 8u * (4 * RING + 12 + b); };
-  auto p_empty = [&](int b) { return sBar + 8u * (4 * RING + 14 + b); };
   volatile int* abort_flag = &ms.abort_flag;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     prefetch_tmap(&tmK); prefetch_tmap(&tmV);
     for (int s = 0; s < RING; ++s) {
-      mbar_init(k_full(s), 32); mbar_init(v_full(s), 32);            // the producer warp's lanes
-      mbar_init(k_empty(s), 4); mbar_init(v_empty(s), 4);            // four expanding warps
+      mbar_init(bar_k_full(sBar, s), 32); mbar_init(bar_v_full(sBar, s), 32);            // the producer warp's lanes
+      mbar_init(bar_k_empty(sBar, s), 4); mbar_init(bar_v_empty(sBar, s), 4);            // four expanding warps
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(kop_full(b), 4); mbar_init(vop_full(b), 4);
-      mbar_init(kop_empty(b), 1); mbar_init(vop_empty(b), 1); mbar_init(s_full(b), 1); mbar_init(p_empty(b), 1);
-      mbar_init(s_empty(b), 8); mbar_init(p_full(b), 8);             // eight softmax warps
+      mbar_init(bar_kop_full(sBar, b), 4); mbar_init(bar_vop_full(sBar, b), 4);
+      mbar_init(bar_kop_empty(sBar, b), 1); mbar_init(bar_vop_empty(sBar, b), 1); mbar_init(bar_s_full(sBar, b), 1); mbar_init(bar_p_empty(sBar, b), 1);
+      mbar_init(bar_s_empty(sBar, b), 8); mbar_init(bar_p_full(sBar, b), 8);             // eight softmax warps
     }
     ms.abort_flag = 0; ms.qmax = 0u;
     fence_barrier_init();
     fence_proxy_async();
   }
   if (warp == 2) { tmem_alloc(smem_u32(&ms.tmem), 512); tmem_relinquish(); }
-  if (threadIdx.x < QN) { ms.ref[threadIdx.x] = REF_NONE; ms.colmax[threadIdx.x] = 0u; }
+  if (threadIdx.x < 2 * QN) ms.nref[0][threadIdx.x] = -REF_NONE;
   if (p.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing in global memory is touched before this
   __syncthreads();
 
@@ -220,17 +448,17 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   const TileEnum te = make_enum(p, g, cnt_raw);
   const int t0 = split_lo(te.total, split, p.n_splits), nt = split_lo(te.total, split + 1, p.n_splits) - t0;
   const int cta = blockIdx.x * p.n_splits + split;
-  const bool use_list = nt <= MAXT;
-  auto make_tile = [&](int idx) -> TileInfo {
-    TileInfo ti = tile_info(p, te, t0 + idx);
-    if (ti.nvalid == 0) { ti.start = ti.start2 = (p.L + 63) & ~63; } // bad block index: wholly outside, arrives as zeros
-    return ti;
-  };
-  auto get_tile = [&](int idx) -> TileInfo { return use_list ? unpack_tile(ms.tlist[idx]) : make_tile(idx); };
-  const int N = rows > 0 ? (rows + 15) & ~15 : 16;                   // columns of S^T and O^T
+  // columns of S^T and O^T.  TMEM: S_0 | S_1 | O_0 (| O_1) | K operands | V operands, 64 columns per operand
+  const bool alt = rows <= 64;
+  const int N = alt ? (rows > 0 ? (rows + 15) & ~15 : 16) : (rows + 31) & ~31;
   const int NS = (N + 31) & ~31;
-  const int n_op = (512 - 3 * NS) / 64;                              // 64-column operand slots in TMEM (2 to 6)
+  const int n_op = (512 - (alt ? 4 : 3) * NS) / 64;                  // operand slots: 4 or more (N <= 64), 3, 2
   const int nK = n_op >= 3 ? 2 : 1, nV = n_op >= 4 ? 2 : 1;
+  Geo gm;
+  gm.g = g; gm.t0 = t0; gm.te = te; gm.nt = nt; gm.N = N; gm.NS = NS; gm.nK = nK; gm.nV = nV; gm.sP = sP; gm.sBar = sBar;
+  const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);   // sink tiles of this split
+  gm.stok_first = (st_lo - te.n_blk) * TN;
+  gm.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
 
   const bool work = rows > 0 && nt > 0;
   // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
@@ -268,11 +496,14 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
     m = __reduce_max_sync(0xffffffffu, m);
     if (lane == 0) atomicMax(&ms.qmax, m);
-  } else if (warp == 12 && use_list) {                                 // meanwhile: tile descriptors
+  } else if (warp == 12 && !p.dense && nt <= MAXT) {                                 // meanwhile: tile descriptors
     for (int t = lane; t < nt; t += 32) {
-      const TileInfo ti = make_tile(t);
-      if (t0 + t < te.n_blk && ti.nvalid == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);
-      ms.tlist[t] = pack_tile(ti);
+      ms.tlist[t] = pack_tile(make_tile(p, gm, t));
+    }
+  } else if (warp > 12) {                                              // and the sink tokens
+    for (int i = (int)threadIdx.x - 13 * 32; i < gm.stok_n; i += NTH - 13 * 32) {
+      const int s = gm.stok_first + i;
+      ms.stok[i] = s < p.n_sink ? sink_token(p, g, s) : -1;
     }
   }
   __syncthreads();
@@ -291,7 +522,9 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     }
   }
   const uint32_t tmem = ms.tmem;
-  const uint32_t tS = tmem, tO = tmem + 2 * NS, tOp = tmem + 3 * NS;
+  const uint32_t tS = tmem, tO = tmem + 2 * NS, tOp = tmem + (alt ? 4 : 3) * NS;
+  gm.tmem = tmem;
+  gm.cs = p.scale_log2 * exp2f((float)-q_shift);
   if (D == 64 && work && (warp == 10 || warp == 11)) {   // channels 64..127 do not exist: zeros, once
     uint32_t z[32];
 #pragma unroll
@@ -309,7 +542,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   tc_fence_after();
 
   if (wg == 0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     if (warp == 0 && work) {
       // ================================ producer ==================================================
       const uint64_t pol = l2_policy_evict_first();
@@ -317,15 +550,16 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       int slot = 0, issued = 0;
       uint32_t round = 0;
       for (int j = 0; j < nt && ok; ++j) {
-        const TileInfo ti = get_tile(j);
+        const TileInfo ti = get_tile(p, ms, gm, j);
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t full = kv ? v_full(slot) : k_full(slot), empty = kv ? v_empty(slot) : k_empty(slot);
+          const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot), empty = kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot);
           const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
           ok = mbar_wait(empty, (round & 1u) ^ 1u, abort_flag, p.status);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           ++issued;
+          if (ti.nvalid == 0 && lane == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
           if (ti.kind == 0) {
             fence_proxy_async();                                       // the slot may have been filled with plain copies before
             if (lane == 0) {
@@ -353,7 +587,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             const uint8_t* base = (kv ? p.V : p.K) + (long long)g * p.kv_stride_head;
             int tok[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tok[i] = key_token(p, ti, g, i * 32 + lane);
+            for (int i = 0; i < 4; ++i) tok[i] = key_token(p, ms, gm, ti, i * 32 + lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -387,7 +621,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int q = max(0, issued - 2 * RING); q < issued; ++q) {
           const int i = q >> 1, sl = i % RING;
           const uint64_t t_start = global_ns();
-          while (!mbar_try_wait(q & 1 ? v_full(sl) : k_full(sl), (uint32_t)(i / RING) & 1u)) {
+          while (!mbar_try_wait(q & 1 ? bar_v_full(sBar, sl) : bar_k_full(sBar, sl), (uint32_t)(i / RING) & 1u)) {
             if (global_ns() - t_start > WAIT_LIMIT_NS) break;
           }
         }
@@ -401,30 +635,30 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       uint32_t kr = 0, vr = 0;
       auto do_pv = [&](int j) -> bool {
         const int b = j & 1;
-        if (!mbar_wait(vop_full(vb), vr & 1u, abort_flag, p.status)) return false;
-        if (!mbar_wait(p_full(b), (uint32_t)(j >> 1) & 1u, abort_flag, p.status)) return false;
+        if (!mbar_wait(bar_vop_full(sBar, vb), vr & 1u, abort_flag, p.status)) return false;
+        if (!mbar_wait(bar_p_full(sBar, b), (uint32_t)(j >> 1) & 1u, abort_flag, p.status)) return false;
         tc_fence_after();
         const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
         const uint32_t a = tOp + (uint32_t)((nK + vb) * 64);
 #pragma unroll
         for (int ks = 0; ks < TN / 16; ++ks)
-          mma_ts(tO, a + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (j | ks) ? 1u : 0u);
-        tc_commit(vop_empty(vb));
-        tc_commit(p_empty(b));
+          mma_ts(tO + (alt ? b * NS : 0), a + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (ks || j > (alt ? 1 : 0)) ? 1u : 0u);
+        tc_commit(bar_vop_empty(sBar, vb));
+        tc_commit(bar_p_empty(sBar, b));
         if (++vb == nV) { vb = 0; ++vr; }
         return true;
       };
       for (int j = 0; j < nt && ok; ++j) {
         const int b = j & 1;
-        if (!mbar_wait(kop_full(kb), kr & 1u, abort_flag, p.status)) { ok = false; break; }
-        if (!mbar_wait(s_empty(b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status)) { ok = false; break; }
+        if (!mbar_wait(bar_kop_full(sBar, kb), kr & 1u, abort_flag, p.status)) { ok = false; break; }
+        if (!mbar_wait(bar_s_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status)) { ok = false; break; }
         tc_fence_after();
         const uint32_t a = tOp + (uint32_t)(kb * 64);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
           mma_ts(tS + b * NS, a + ks * 8, qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), ID_QK, ks ? 1u : 0u);
-        tc_commit(kop_empty(kb));
-        tc_commit(s_full(b));
+        tc_commit(bar_kop_empty(sBar, kb));
+        tc_commit(bar_s_full(sBar, b));
         if (++kb == nK) { kb = 0; ++kr; }
         if (j > 0) ok = do_pv(j - 1);
       }
@@ -437,15 +671,15 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (warp == 2) { __syncwarp(); tmem_dealloc(tmem, 512); }
   } else if (wg == 1) {
     // ================================ K codes -> A operand of S^T =====================================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (work) {
       const int key = (warp & 3) * 32 + lane;
       const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
       int slot = 0, ob = 0;
       uint32_t round = 0, orr = 0;
       for (int j = 0; j < nt; ++j) {
-        bool ok = mbar_wait(k_full(slot), round & 1u, abort_flag, p.status) &&
-                  mbar_wait(kop_empty(ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        bool ok = mbar_wait(bar_k_full(sBar, slot), round & 1u, abort_flag, p.status) &&
+                  mbar_wait(bar_kop_empty(sBar, ob), (orr & 1u) ^ 1u, abort_flag, p.status);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawK + slot * SLOT, dst = tOp + (uint32_t)(ob * 64) + lane_off;
@@ -467,7 +701,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(k_empty(slot)); mbar_arrive(kop_full(ob)); }
+        if (lane == 0) { mbar_arrive(bar_k_empty(sBar, slot)); mbar_arrive(bar_kop_full(sBar, ob)); }
         if (++slot == RING) { slot = 0; ++round; }
         if (++ob == nK) { ob = 0; ++orr; }
       }
@@ -476,14 +710,14 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     asm volatile("bar.sync 0;" ::: "memory");
   } else if (wg == 2) {
     // ================================ V codes, transposed -> A operand of O^T ===========================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (work) {
       const int cw = warp & 3;                                         // channels 32 cw .. 32 cw + 31
       int slot = 0, ob = 0;
       uint32_t round = 0, orr = 0;
       for (int j = 0; j < nt; ++j) {
-        bool ok = mbar_wait(v_full(slot), round & 1u, abort_flag, p.status) &&
-                  mbar_wait(vop_empty(ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        bool ok = mbar_wait(bar_v_full(sBar, slot), round & 1u, abort_flag, p.status) &&
+                  mbar_wait(bar_vop_empty(sBar, ob), (orr & 1u) ^ 1u, abort_flag, p.status);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawV + slot * SLOT, dst = tOp + (uint32_t)((nK + ob) * 64) + ((uint32_t)(cw * 32) << 16);
@@ -510,7 +744,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(v_empty(slot)); mbar_arrive(vop_full(ob)); }
+        if (lane == 0) { mbar_arrive(bar_v_empty(sBar, slot)); mbar_arrive(bar_vop_full(sBar, ob)); }
         if (++slot == RING) { slot = 0; ++round; }
         if (++ob == nV) { ob = 0; ++orr; }
       }
@@ -519,199 +753,57 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     asm volatile("bar.sync 0;" ::: "memory");
   } else {
     // ================================ softmax =========================================================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane;
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-    const int NC = N >> 1, np = NC >> 3;                               // this warpgroup's rows, in pieces of 8
-    const int c0 = x * NC;
-    float l[64];
-#pragma unroll
-    for (int c = 0; c < 64; ++c) l[c] = 0.f;
     if (work) {
-      bool ok = true;
-      const float cs = p.scale_log2 * exp2f((float)-q_shift);
-      const float* Ks = p.K_scale + (long long)g * p.scale_stride;
-      const float* Vs = p.V_scale + (long long)g * p.scale_stride;
-      auto scales = [&](int idx, float& sk, float& sv) {               // sv == -1: masked
-        sk = 0.f; sv = -1.f;
-        if (idx >= nt) return;
-        const int t = key_token(p, get_tile(idx), g, key);
-        if (t >= 0) { sk = __ldg(Ks + t); sv = __ldg(Vs + t); }
-      };
-      float sk0, sv0, sk1, sv1, sk2, sv2;                              // two tiles ahead: their latency is out of the way
-      scales(0, sk0, sv0);
-      scales(1, sk1, sv1);
-      for (int j = 0; j < nt; ++j) {
-        const int b = j & 1;
-        const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-        scales(j + 2, sk2, sv2);
-        const bool masked = sv0 == -1.f;
-        const float svc = fmaxf(sv0, SV_MIN);
-        const float ck = sk0 * cs, lv = masked ? -INFINITY : __log2f(svc), iv = masked ? 0.f : __fdividef(1.f, svc);
-        sk0 = sk1; sv0 = sv1; sk1 = sk2; sv1 = sv2;
-        ok = __all_sync(0xffffffffu, mbar_wait(s_full(b), ph, abort_flag, p.status)) && ok;
-        tc_fence_after();
-        const uint32_t ts = tS + (uint32_t)(b * NS + c0) + lane_off;
-        float a[32];
-        // exponents of row group grp (32 rows): a = s ck + lv, minus the reference where `minus` is set
-        auto load_group = [&](int grp, bool minus) {
-          uint32_t* ar = reinterpret_cast<uint32_t*>(a);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (grp * 4 + i < np) TC_LD8(ts + (grp * 4 + i) * 8, ar + i * 8);
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (grp * 4 + i < np) {
-              const float4* rf = reinterpret_cast<const float4*>(ms.ref + c0 + (grp * 4 + i) * 8);
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float* v = a + i * 8 + h * 4;
-                ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
-                ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
-                if (minus) {
-                  const float4 rv = rf[h];
-                  fadd2(v[0], v[1], v[0], v[1], -rv.x, -rv.y);
-                  fadd2(v[2], v[3], v[2], v[3], -rv.z, -rv.w);
-                }
-              }
-            }
-        };
-        float mx = -INFINITY;
-        auto group_max = [&](int grp) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (grp * 4 + i < np) {
-#pragma unroll
-              for (int e = 0; e < 8; e += 2) mx = fmax3(mx, a[i * 8 + e], a[i * 8 + e + 1]);
-            }
-        };
-        // the upper rows first: rows 0..31 stay in registers for the second pass
-        if (np > 4) { load_group(1, true); group_max(1); }
-        load_group(0, true);
-        group_max(0);
-        bool fresh = true;
-        if (named_any(1 + x, 128, mx > THRESH || !ok)) {
-          // ---- some row's maximum outgrew its reference (always so at the first key): new references ----
-          if (named_any(1 + x, 128, !ok)) break;
-          fresh = false;
-#pragma unroll 1
-          for (int grp = 0; grp * 4 < np; ++grp) {
-            load_group(grp, false);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (grp * 4 + i < np) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const unsigned k = __reduce_max_sync(0xffffffffu, float_key(a[i * 8 + e]));
-                  if (lane == 0) atomicMax(&ms.colmax[c0 + (grp * 4 + i) * 8 + e], k);
-                }
-              }
-          }
-          named_sync(1 + x, 128);
-          if (key < NC) {
-            const float old = ms.ref[c0 + key], now = key_to_float(ms.colmax[c0 + key]) - OFFSET;
-            const bool up = now > old;
-            ms.fac[c0 + key] = up ? ex2(old - now) : 1.f;
-            if (up) ms.ref[c0 + key] = now;
-            ms.colmax[c0 + key] = 0u;
-          }
-          named_sync(1 + x, 128);
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c < NC) l[c] *= ms.fac[c0 + c];
-          if (j > 0) {
-            // the sums so far are in TMEM once P V of the last tile is done; P V of this one waits for its P
-            ok = __all_sync(0xffffffffu, mbar_wait(p_empty(b ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, p.status));
-            tc_fence_after();
-#pragma unroll 1
-            for (int i = 0; i < np; ++i) {
-              const uint32_t at = tO + (uint32_t)(c0 + i * 8) + lane_off;
-              uint32_t o[8];
-              TC_LD8(at, o);
-              tc_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ms.fac[c0 + i * 8 + e]);
-              TC_ST8(at, o);
-            }
-            tc_wait_st();
-          }
-        }
-        // ---- P = 2^(a - ref): row sums in fp32, fp16 to shared memory ----
-        ok = __all_sync(0xffffffffu, mbar_wait(p_empty(b), ph ^ 1u, abort_flag, p.status)) && ok;   // P V of tile j - 2
-        const uint32_t prow = sP + (uint32_t)(b * P_BYTES + key * 128);
-#pragma unroll
-        for (int grp = 0; grp < 2; ++grp) {
-          if (grp * 4 >= np) continue;
-          if (grp == 1 || !fresh) load_group(grp, true);
-          if (grp == 1 || np <= 4) {                                   // S_b is in registers: the next product may overwrite it
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(s_empty(b));
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (grp * 4 + i < np) {
-              float* v = a + i * 8;
-              float* lc = l + grp * 32 + i * 8;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = ex2(v[e]);
-#pragma unroll
-              for (int e = 0; e < 8; e += 2) ffma2(lc[e], lc[e + 1], v[e], v[e + 1], iv, iv, lc[e], lc[e + 1]);
-              const int col = c0 + (grp * 4 + i) * 8;
-              sts128(prow + (uint32_t)((col >> 6) * (TN * 128)) + (uint32_t)((((col & 63) >> 3) ^ (key & 7)) << 4),
-                     pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
-            }
-        }
-        fence_proxy_async();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(b));
-      }
-      // all products done?
-      mbar_wait(p_empty((nt - 1) & 1), (uint32_t)((nt - 1) >> 1) & 1u, abort_flag, p.status);
-      tc_fence_after();
-    }
-    // ---- row sums over the 128 keys: lane i of every warp ends with row i of a group, warps in order ----
-#pragma unroll
-    for (int grp = 0; grp < 2; ++grp) {
-      if (grp * 32 >= NC) continue;
-      float* v = l + grp * 32;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const bool hi = (lane & o) != 0;
-#pragma unroll
-        for (int i = 0; i < o; ++i) {
-          const float send = hi ? v[i] : v[i + o], keep = hi ? v[i + o] : v[i];
-          v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-        }
-      }
-      ms.lsum[x * 4 + wq][grp * 32 + lane] = v[0];
-    }
-    named_sync(1 + x, 128);
-    if (key < NC) {
-      const int r = c0 + key;
-      const float tot = ((ms.lsum[x * 4][key] + ms.lsum[x * 4 + 1][key]) + ms.lsum[x * 4 + 2][key]) + ms.lsum[x * 4 + 3][key];
-      const float ref = ms.ref[r];
-      if (p.n_splits > 1) {
-        if (r < rows) reinterpret_cast<float2*>(p.part_ml)[(size_t)cta * QN + r] = make_float2(ref, tot);
+      if (alt) {
+        if (N == 16) softmax_loop<2, true>(p, ms, gm, x, wq, lane);
+        else if (N == 32) softmax_loop<4, true>(p, ms, gm, x, wq, lane);
+        else if (N == 48) softmax_loop<6, true>(p, ms, gm, x, wq, lane);
+        else softmax_loop<8, true>(p, ms, gm, x, wq, lane);
       } else {
-        ms.fac[r] = tot > 0.f ? 1.f / tot : (tot == 0.f ? 0.f : tot);   // NaN stays NaN
+        if (N == 96) softmax_loop<6, false>(p, ms, gm, x, wq, lane);
+        else softmax_loop<8, false>(p, ms, gm, x, wq, lane);
+      }
+    }
+    named_sync(3, 256);
+    // ---- row statistics: sums of the warps in order; the two warpgroups' shares of a row joined (ALT) ----
+    if ((int)threadIdx.x - 384 < rows) {
+      const int r = (int)threadIdx.x - 384;
+      float ref = REF_NONE, tot = 0.f, w0 = 0.f, w1 = 0.f;
+      if (work) {
+        const int xr = alt ? 0 : r / (N / 2), cr = alt ? r : r - xr * (N / 2);
+        auto warps = [&](int q) { return ((ms.red[q * 4][cr] + ms.red[q * 4 + 1][cr]) + ms.red[q * 4 + 2][cr]) + ms.red[q * 4 + 3][cr]; };
+        const float l0 = warps(xr), r0 = -ms.nref[0][r];
+        const float l1 = alt && nt > 1 ? warps(1) : 0.f, r1 = alt ? -ms.nref[1][r] : REF_NONE;
+        ref = fmaxf(r0, r1);
+        w0 = l0 != 0.f ? ex2(r0 - ref) : 0.f;
+        w1 = l1 != 0.f ? ex2(r1 - ref) : 0.f;
+        tot = w0 * l0 + w1 * l1;
+      }
+      if (p.n_splits > 1) {
+        reinterpret_cast<float2*>(p.part_ml)[(size_t)cta * QN + r] = make_float2(ref, tot);
+      } else {
+        const float inv = tot != 0.f ? 1.f / tot : 0.f;
+        w0 *= inv; w1 *= inv;
         const int orow = ms.orow[r];
-        if (r < rows && orow >= 0 && p.lse)
+        if (orow >= 0 && p.lse)
           p.lse[(size_t)(orow % p.H) * p.lse_stride + orow / p.H] = tot == 0.f ? -INFINITY : (ref + log2f(tot)) * 0.6931471805599453f;
       }
+      ms.fac[0][r] = w0; ms.fac[1][r] = w1;
     }
-    named_sync(1 + x, 128);
+    named_sync(3, 256);
     // ---- O^T: this thread's channel of every row of its half ----
-    const int ch = key;
+    const int ch = key, c0 = x * (N >> 1);
 #pragma unroll 1
-    for (int i = 0; i < np; ++i) {
-      uint32_t o[8];
+    for (int i = 0; i < N >> 4; ++i) {
+      uint32_t o[8], o1[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = 0u;
+      for (int e = 0; e < 8; ++e) o[e] = o1[e] = 0u;
       if (work) {
         TC_LD8(tO + (uint32_t)(c0 + i * 8) + lane_off, o);
+        if (alt && nt > 1) TC_LD8(tO + (uint32_t)(NS + c0 + i * 8) + lane_off, o1);
         tc_wait_ld();
       }
       if (ch < D) {
@@ -719,11 +811,12 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int e = 0; e < 8; ++e) {
           const int r = c0 + i * 8 + e;
           if (r < rows) {
-            if (p.n_splits > 1) {
-              p.part_O[((size_t)cta * QN + r) * D + ch] = __uint_as_float(o[e]);
-            } else if (ms.orow[r] >= 0) {
-              p.O[(size_t)ms.orow[r] * D + ch] = __float2bfloat16_rn(__uint_as_float(o[e]) * ms.fac[r]);
-            }
+            // a row's share without a key holds nothing that may be read
+            const float f0 = ms.fac[0][r], f1 = ms.fac[1][r];
+            float v = f0 != 0.f ? __uint_as_float(o[e]) * f0 : 0.f;
+            if (f1 != 0.f) v = fmaf(__uint_as_float(o1[e]), f1, v);
+            if (p.n_splits > 1) p.part_O[((size_t)cta * QN + r) * D + ch] = v;
+            else if (ms.orow[r] >= 0) p.O[(size_t)ms.orow[r] * D + ch] = __float2bfloat16_rn(v);
           }
         }
       }
@@ -759,7 +852,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             wts[tid * S + s] = w;
           }
           const int orow = ms.orow[tid];
-          ms.fac[tid] = tot != 0.f ? 1.f / tot : 0.f;
+          ms.fac[0][tid] = tot != 0.f ? 1.f / tot : 0.f;
           if (orow >= 0 && p.lse)
             p.lse[(size_t)(orow % p.H) * p.lse_stride + orow / p.H] = tot == 0.f ? -INFINITY : (m + log2f(tot)) * 0.6931471805599453f;
         }
@@ -775,7 +868,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             const float4 o = __ldcg(po + (size_t)s * QN * (D / 4));
             if (w != 0.f) { acc.x += w * o.x; acc.y += w * o.y; acc.z += w * o.z; acc.w += w * o.w; }
           }
-          const float f = ms.fac[r];
+          const float f = ms.fac[0][r];
           uint2 v;
           v.x = pack_bf16(acc.x * f, acc.y * f);
           v.y = pack_bf16(acc.z * f, acc.w * f);
