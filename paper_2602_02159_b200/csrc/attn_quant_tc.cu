@@ -12,10 +12,10 @@
 // 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-12, absolute 2^-31 of the row's
 // largest), which is the one rounding between the cache and the output; sums are fp32.
 //
-// Work split.  CTA = up to 128 stacked query rows of one KV head (the rows of a group's query heads share its K/V) x one
+// Work split.  CTA = up to 64 stacked query rows of one KV head (the rows of a group's query heads share its K/V) x one
 // contiguous range ("split") of that head's key tiles of 128 tokens.  The transposed form costs in proportion to the
 // rows there are (N = rows rounded to 16), not to a tile of 128: with the 35 to 72 rows of a denoising step the launch
-// is meant to be bound by the bytes of the cache.
+// is meant to be bound by the bytes of the cache.  The splits of a row tile are joined by the CTA that finishes last.
 //
 // Warp roles (640 threads):
 //   warp 0        producer: K and V tiles as raw codes into two rings (TMA; sink tokens one by one with cp.async)
@@ -23,9 +23,13 @@
 //   warp 2        TMEM allocation
 //   warps 4..7    K codes -> fp16 in TMEM (lane = key): the A operand of S^T
 //   warps 8..11   V codes -> fp16 in TMEM (lane = channel; ldmatrix transposes the bytes): the A operand of O^T
-//   warps 12..19  softmax, two warpgroups with half of the query rows each; P^T to shared memory (the B operand of O^T)
+//   warps 12..19  softmax: two warpgroups that take the key tiles in turn, with references, row sums and an O^T of their
+//                 own (a tile's chain of latencies, S ready -> P ready, then has two tile periods of time); P^T goes to
+//                 shared memory (the B operand of O^T)
 // Expanding the codes into TMEM instead of shared memory halves the shared-memory traffic of a tile: one byte in, one
 // byte out per code, no fp16 copy there.
+#include <stddef.h>
+
 #include "attn_tiles.cuh"
 #include "tc_common.cuh"
 
@@ -33,13 +37,15 @@ using namespace tc;
 
 namespace {
 
-// registers per thread after the roles split: 32 + 64 + 64 + 160 + 160 = 480 = 5 x the 96 of the launch
-constexpr int QN = 128;                        // most query rows per CTA
+// registers per thread after the roles split: 64 + 48 + 48 + 160 + 160 = 480 = 5 x the 96 of the launch
+constexpr int QN = 64;                         // most query rows per CTA
 constexpr int NTH = 640;
-constexpr int RING = 3;                        // raw slots per ring (K, V)
+constexpr int RING = 5;                        // raw slots per ring (K, V)
 constexpr int SLOT = TN * 128;                 // bytes of a raw tile (head dim 64 fills half)
 constexpr int Q_BYTES = QN * 128 * 2;
-constexpr int P_BYTES = TN * QN * 2;           // P^T of one tile: [key][row], two 64-row halves
+constexpr int P_BYTES = TN * QN * 2;           // P^T of one tile: [key][row]
+// TMEM columns: S of even / odd tiles, O of the two warpgroups, expanded K and V (two tiles each)
+constexpr int T_S = 0, T_O = 128, T_K = 256, T_V = 384;
 constexpr int MAXT = 256;                      // key tiles of a split whose descriptors are staged
 constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
@@ -76,9 +82,9 @@ struct QParams {
 constexpr int MAX_STOK = 8;                    // sink tiles of a split whose tokens are staged
 
 struct Misc {                                  // behind the tiles in shared memory
-  unsigned long long bars[4 * RING + 16];
-  float nref[2][QN];                           // minus the reference exponent per row (set 1: second warpgroup's own)
-  float fac[2][QN];                            // rescale factor / weight per row
+  unsigned long long bars[4 * RING + 17];
+  alignas(16) float nref[2][QN];               // minus the reference exponent per row (set 1: second warpgroup's own)
+  alignas(16) float fac[2][QN];                // rescale factor / weight per row
   float red[8][64];                            // per softmax warp: column maxima, then row sums
   int orow[QN];                                // output row (position slot * H + head), -1: none
   int2 tlist[MAXT];
@@ -89,6 +95,8 @@ struct Misc {                                  // behind the tiles in shared mem
 };
 constexpr int SMEM = 1024 + OFF_MISC + (int)sizeof(Misc);
 static_assert(SMEM <= 227 * 1024, "shared memory");
+static_assert(offsetof(Misc, nref) % 16 == 0 && offsetof(Misc, fac) % 16 == 0 && OFF_MISC % 16 == 0, "read as float4");
+static_assert(offsetof(Misc, bars) % 8 == 0 && OFF_RAW % 1024 == 0 && SLOT % 1024 == 0 && P_BYTES % 1024 == 0, "operand tiles");
 
 // ---- instructions this kernel adds to tc_common.cuh ----
 // kind::f16 with fp16 operands, fp32 accumulation
@@ -124,6 +132,12 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// a load that stays where it is written (a plain one may be moved down to its first use, an iteration later)
+__device__ __forceinline__ float ld_pinned(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+  return v;
 }
 __device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ bool named_any(int id, int n, bool v) {
@@ -167,12 +181,12 @@ __device__ __forceinline__ int sink_token(const QParams& p, int g, int s) {
 }
 
 struct Geo {                                   // what the roles share about their CTA
-  int g, t0, nt, N, NS, nK, nV;
+  int g, t0, nt, N;
   TileEnum te;
   int stok_first;                              // first sink (list position) in Misc::stok, and how many are there
   int stok_n;
   uint32_t sP, sBar, tmem;
-  float cs;                                    // logit scale: softmax scale * log2(e) / query scale
+  float cs;                                    // logit scale: softmax scale * log2(e) / query scale (softmax warps only)
 };
 // tile idx of this split: by arithmetic (dense), from the staged list, or from the block list (splits longer than that)
 __device__ __forceinline__ TileInfo make_tile(const QParams& p, const Geo& gm, int idx) {
@@ -204,9 +218,7 @@ __device__ __forceinline__ uint32_t bar_s_empty(uint32_t b, int i) { return b + 
 __device__ __forceinline__ uint32_t bar_p_full(uint32_t b, int i) { return b + 8u * (4 * RING + 12 + i); }
 __device__ __forceinline__ uint32_t bar_p_empty(uint32_t b, int i) { return b + 8u * (4 * RING + 14 + i); }
 
-__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
-}
+__device__ __forceinline__ uint32_t bar_q_full(uint32_t b) { return b + 8u * (4 * RING + 16); }
 
 // Reduces 32 values per lane over the 32 lanes by halving: 31 shuffles, lane i ends with the result of value i.
 template <typename Op>
@@ -223,61 +235,60 @@ __device__ __forceinline__ float lane_reduce32(float* v, int lane, Op op) {
   return v[0];
 }
 
-// Softmax of one warpgroup (x = 0, 1), NP pieces of 8 rows; straight-line code per tile, since its length in cycles is
-// what a tile costs.
-//   ALT   (N <= 64)  the two warpgroups take the key tiles in turn, all N rows each, with references, sums and O of
-//                    their own (joined at the end): a tile's chain of latencies has two tile periods of time
-//   !ALT  (N > 64)   every tile, half of the rows each
-// Leaves the row sums over this warpgroup's keys in ms.red.
-template <int NP, bool ALT>
+// Softmax of one warpgroup (x = 0, 1: even, odd tiles), NP pieces of 8 rows; straight-line code per tile, since its length
+// in cycles is what a tile costs.  Leaves the row sums over this warpgroup's keys in ms.red.
+template <int NP>
 __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const Geo& gm, int x, int wq, int lane) {
   constexpr int NC = NP * 8;
-  constexpr int NG = NP <= 6 ? 1 : 2;                                  // more rows do not fit the registers twice (a and l)
-  constexpr int GP = NP / NG;                                          // pieces per group
-  const int key = wq * 32 + lane, nt = gm.nt, set = ALT ? x : 0;
+  const int key = wq * 32 + lane, nt = gm.nt;
   const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-  const int c0 = ALT ? 0 : x * NC;                                     // first row (column of S^T)
-  const uint32_t tO = gm.tmem + (uint32_t)((2 + set) * gm.NS + c0) + lane_off;
+  const uint32_t tO = gm.tmem + (uint32_t)(T_O + x * QN) + lane_off, ts = gm.tmem + (uint32_t)(T_S + x * QN) + lane_off;
+  const uint32_t prow = gm.sP + (uint32_t)(x * P_BYTES + key * 128);
   volatile int* abort_flag = &ms.abort_flag;
-  float* nref = ms.nref[set] + c0;
-  float* fac = ms.fac[set] + c0;
+  float* nref = ms.nref[x];
+  float* fac = ms.fac[x];
   float* red = ms.red[x * 4 + wq];
   const float* Ks = p.K_scale + (long long)gm.g * p.scale_stride;
   const float* Vs = p.V_scale + (long long)gm.g * p.scale_stride;
   float l[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) l[c] = 0.f;
-  constexpr int STEP = ALT ? 2 : 1;
   auto scales = [&](int idx, float& sk, float& sv) {                   // sv == -1: masked
     sk = 0.f; sv = -1.f;
     if (idx >= nt) return;
-    const int t = key_token(p, ms, gm, get_tile(p, ms, gm, idx), key);
-    if (t >= 0) { sk = __ldg(Ks + t); sv = __ldg(Vs + t); }
+    int t;
+    if (p.dense) {
+      t = (gm.t0 + idx) * TN + key;
+      if (t >= p.L) return;
+    } else {
+      t = key_token(p, ms, gm, get_tile(p, ms, gm, idx), key);
+      if (t < 0) return;
+    }
+    sk = ld_pinned(Ks + t);
+    sv = ld_pinned(Vs + t);
   };
   float sk, sv;
-  scales(ALT ? x : 0, sk, sv);
+  scales(x, sk, sv);
   bool ok = true;
-  for (int j = ALT ? x : 0; j < nt; j += STEP) {
-    const int b = j & 1;
+  for (int j = x; j < nt; j += 2) {
     const uint32_t ph = (uint32_t)(j >> 1) & 1u;
     const bool masked = sv == -1.f;
     const float svc = fmaxf(sv, SV_MIN);
     const float ck = sk * gm.cs, lv = masked ? -INFINITY : __log2f(svc), iv = masked ? 0.f : __fdividef(1.f, svc);
-    scales(j + STEP, sk, sv);                                          // the next tile's, out of the way of their latency
-    ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(gm.sBar, b), ph, abort_flag, p.status)) && ok;
+    scales(j + 2, sk, sv);                                             // the next tile's, out of the way of their latency
+    ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(gm.sBar, x), ph, abort_flag, p.status)) && ok;
     tc_fence_after();
-    const uint32_t ts = gm.tmem + (uint32_t)(b * gm.NS + c0) + lane_off;
-    float a[GP * 8];
+    float a[NC];
     uint32_t* ar = reinterpret_cast<uint32_t*>(a);
-    // exponents a = s ck + lv - ref of group grp
-    auto load_group = [&](int grp) {
+    auto load_logits = [&]() {
 #pragma unroll
-      for (int i = 0; i < GP; ++i) TC_LD8(ts + (grp * GP + i) * 8, ar + i * 8);
+      for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
       tc_wait_ld();
-      const float4* rf = reinterpret_cast<const float4*>(nref + grp * GP * 8);
+    };
+    auto exponents = [&]() {                                           // a = s ck + lv - ref
 #pragma unroll
-      for (int q = 0; q < GP * 2; ++q) {
-        const float4 rv = rf[q];
+      for (int q = 0; q < NP * 2; ++q) {
+        const float4 rv = reinterpret_cast<const float4*>(nref)[q];
         float* v = a + q * 4;
         ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
         ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
@@ -285,42 +296,28 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const G
         fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
       }
     };
-    float mx = -INFINITY;
+    load_logits();
+    exponents();
+    float mx = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-    for (int grp = NG - 1; grp >= 0; --grp) {                          // group 0 last: it stays in registers
-      load_group(grp);
-      float m1 = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < GP * 8; e += 4) {
-        mx = fmax3(mx, a[e], a[e + 1]);
-        m1 = fmax3(m1, a[e + 2], a[e + 3]);
-      }
-      mx = fmaxf(mx, m1);
+    for (int e = 0; e < NC; e += 4) {
+      mx = fmax3(mx, a[e], a[e + 1]);
+      m1 = fmax3(m1, a[e + 2], a[e + 3]);
     }
-    if (named_any(1 + x, 128, mx > THRESH || !ok)) {
+    if (named_any(1 + x, 128, fmaxf(mx, m1) > THRESH || !ok)) {
       // ---- some row's maximum outgrew its reference (always so at the first key): new references ----
       if (named_any(1 + x, 128, !ok)) break;
-#pragma unroll 1
+      load_logits();
+#pragma unroll
       for (int h = 0; h * 4 < NP; ++h) {                               // 32 rows at a time
         float v[32];
-        uint32_t* vr = reinterpret_cast<uint32_t*>(v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (h * 4 + i < NP) {
-            TC_LD8(ts + (h * 4 + i) * 8, vr + i * 8);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i * 8 + e] = -INFINITY;
-          }
-        }
-        tc_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = (h * 4 + (e >> 3) < NP) ? fmaf(v[e], ck, lv) : -INFINITY;
+        for (int e = 0; e < 32; ++e) v[e] = h * 32 + e < NC ? fmaf(a[h * 32 + e < NC ? h * 32 + e : 0], ck, lv) : -INFINITY;
         red[h * 32 + lane] = lane_reduce32(v, lane, [](float u, float w) { return fmaxf(u, w); });
       }
       named_sync(1 + x, 128);
       if (key < NC) {
-        const float(*r)[64] = &ms.red[x * 4];
+        const float(*r)[QN] = &ms.red[x * 4];
         const float top = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
         const float old = nref[key], now = OFFSET - top;
         const bool up = now < old;
@@ -328,71 +325,49 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const G
         if (up) nref[key] = now;
       }
       named_sync(1 + x, 128);
-#pragma unroll
-      for (int q = 0; q < NP * 2; ++q) {
-        const float4 f = reinterpret_cast<const float4*>(fac)[q];
-        l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w;
-      }
-      // what these rows have summed is in TMEM once the last P V is done; P V of this tile waits for its P
-      const int prev = ALT ? j - 2 : j - 1;
-      if (prev >= 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, prev & 1), (uint32_t)(prev >> 1) & 1u, abort_flag, p.status));
+      if (j >= 2) {
+        // what these rows have summed is in TMEM once P V of this warpgroup's last tile is done
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, x), ph ^ 1u, abort_flag, p.status));
         tc_fence_after();
-#pragma unroll 1
-        for (int h = 0; h * 2 < NP; ++h) {
-          uint32_t o[16];
-          TC_LD8(tO + h * 16, o);
-          TC_LD8(tO + h * 16 + 8, o + 8);
-          tc_wait_ld();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float4 f = reinterpret_cast<const float4*>(fac)[h * 4 + q];
-            o[4 * q] = __float_as_uint(__uint_as_float(o[4 * q]) * f.x);
-            o[4 * q + 1] = __float_as_uint(__uint_as_float(o[4 * q + 1]) * f.y);
-            o[4 * q + 2] = __float_as_uint(__uint_as_float(o[4 * q + 2]) * f.z);
-            o[4 * q + 3] = __float_as_uint(__uint_as_float(o[4 * q + 3]) * f.w);
-          }
-          TC_ST8(tO + h * 16, o);
-          TC_ST8(tO + h * 16 + 8, o + 8);
+        for (int i = 0; i < NP; ++i) TC_LD8(tO + i * 8, ar + i * 8);
+        tc_wait_ld();
+#pragma unroll
+        for (int q = 0; q < NP * 2; ++q) {
+          const float4 f = reinterpret_cast<const float4*>(fac)[q];
+          float* v = a + q * 4;
+          l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w;
+          v[0] *= f.x; v[1] *= f.y; v[2] *= f.z; v[3] *= f.w;
         }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) TC_ST8(tO + i * 8, ar + i * 8);
         tc_wait_st();
       }
-      load_group(0);
+      load_logits();
+      exponents();
     }
     // ---- P = 2^a: row sums in fp32, fp16 to shared memory ----
-    const uint32_t prow = gm.sP + (uint32_t)(b * P_BYTES + key * 128);
-    bool waited = false;
-#pragma unroll
-    for (int grp = 0; grp < NG; ++grp) {
-      if (grp > 0) load_group(grp);
-      if (grp == NG - 1) {                                             // S_b is in registers: the next product may overwrite it
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_n(bar_s_empty(gm.sBar, b), STEP);
-      }
-#pragma unroll
-      for (int e = 0; e < GP * 8; ++e) a[e] = ex2(a[e]);
-      if (!waited) {                                                   // P V of tile j - 2 has read this buffer
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, b), ph ^ 1u, abort_flag, p.status)) && ok;
-        waited = true;
-      }
-#pragma unroll
-      for (int i = 0; i < GP; ++i) {
-        const float* v = a + i * 8;
-        const int col = c0 + (grp * GP + i) * 8;
-        sts128(prow + (uint32_t)((col >> 6) * (TN * 128)) + (uint32_t)((((col & 63) >> 3) ^ (key & 7)) << 4),
-               pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
-      }
-      fence_proxy_async();
-      float* lc = l + grp * GP * 8;
-#pragma unroll
-      for (int e = 0; e < GP * 8; e += 2) ffma2(lc[e], lc[e + 1], a[e], a[e + 1], iv, iv, lc[e], lc[e + 1]);
-    }
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive_n(bar_p_full(gm.sBar, b), STEP);
+    if (lane == 0) mbar_arrive(bar_s_empty(gm.sBar, x));               // S is in registers: the next product may overwrite it
+#pragma unroll
+    for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
+    // P V of this warpgroup's last tile has read the buffer
+    ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, x), ph ^ 1u, abort_flag, p.status)) && ok;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const float* v = a + i * 8;
+      sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
+             pack_f16(v[6], v[7]));
+    }
+    fence_proxy_async();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_p_full(gm.sBar, x));
+#pragma unroll
+    for (int e = 0; e < NC; e += 2) ffma2(l[e], l[e + 1], a[e], a[e + 1], iv, iv, l[e], l[e + 1]);
   }
-  // all products done (each warpgroup waits for both buffers: their last two tiles)
+  // all products done (each warpgroup waits for both buffers: the last two tiles)
   for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) mbar_wait(bar_p_empty(gm.sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag, p.status);
   tc_fence_after();
   // ---- row sums over this warp's 32 keys: lane i of a warp ends with row i of a group ----
@@ -423,14 +398,16 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (threadIdx.x == 0) {
     prefetch_tmap(&tmK); prefetch_tmap(&tmV);
     for (int s = 0; s < RING; ++s) {
-      mbar_init(bar_k_full(sBar, s), 32); mbar_init(bar_v_full(sBar, s), 32);            // the producer warp's lanes
-      mbar_init(bar_k_empty(sBar, s), 4); mbar_init(bar_v_empty(sBar, s), 4);            // four expanding warps
+      mbar_init(bar_k_full(sBar, s), 32); mbar_init(bar_v_full(sBar, s), 32);      // the producer warp's lanes
+      mbar_init(bar_k_empty(sBar, s), 4); mbar_init(bar_v_empty(sBar, s), 4);      // four expanding warps
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(bar_kop_full(sBar, b), 4); mbar_init(bar_vop_full(sBar, b), 4);
-      mbar_init(bar_kop_empty(sBar, b), 1); mbar_init(bar_vop_empty(sBar, b), 1); mbar_init(bar_s_full(sBar, b), 1); mbar_init(bar_p_empty(sBar, b), 1);
-      mbar_init(bar_s_empty(sBar, b), 8); mbar_init(bar_p_full(sBar, b), 8);             // eight softmax warps
+      mbar_init(bar_kop_empty(sBar, b), 1); mbar_init(bar_vop_empty(sBar, b), 1);
+      mbar_init(bar_s_full(sBar, b), 1); mbar_init(bar_p_empty(sBar, b), 1);
+      mbar_init(bar_s_empty(sBar, b), 4); mbar_init(bar_p_full(sBar, b), 4);       // one softmax warpgroup's warps
     }
+    mbar_init(bar_q_full(sBar), 8);                                    // eight softmax warps
     ms.abort_flag = 0; ms.qmax = 0u;
     fence_barrier_init();
     fence_proxy_async();
@@ -438,177 +415,102 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (warp == 2) { tmem_alloc(smem_u32(&ms.tmem), 512); tmem_relinquish(); }
   if (threadIdx.x < 2 * QN) ms.nref[0][threadIdx.x] = -REF_NONE;
   if (p.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing in global memory is touched before this
-  __syncthreads();
 
   // ---- rows, tiles ----
   const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
-  const int total_fr = nrows * p.hpg;                                // stacked (row, head of the group) rows
-  const int rows = min(QN, total_fr - mt * QN);                      // of this CTA
   const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
   const TileEnum te = make_enum(p, g, cnt_raw);
   const int t0 = split_lo(te.total, split, p.n_splits), nt = split_lo(te.total, split + 1, p.n_splits) - t0;
+  const int rows = min(QN, nrows * p.hpg - mt * QN);                 // stacked (row, head of the group) rows of this CTA
+  const bool work = rows > 0 && nt > 0;
   const int cta = blockIdx.x * p.n_splits + split;
-  // columns of S^T and O^T.  TMEM: S_0 | S_1 | O_0 (| O_1) | K operands | V operands, 64 columns per operand
-  const bool alt = rows <= 64;
-  const int N = alt ? (rows > 0 ? (rows + 15) & ~15 : 16) : (rows + 31) & ~31;
-  const int NS = (N + 31) & ~31;
-  const int n_op = (512 - (alt ? 4 : 3) * NS) / 64;                  // operand slots: 4 or more (N <= 64), 3, 2
-  const int nK = n_op >= 3 ? 2 : 1, nV = n_op >= 4 ? 2 : 1;
+  const int N = rows > 0 ? (rows + 15) & ~15 : 16;                   // columns of S^T and O^T
   Geo gm;
-  gm.g = g; gm.t0 = t0; gm.te = te; gm.nt = nt; gm.N = N; gm.NS = NS; gm.nK = nK; gm.nV = nV; gm.sP = sP; gm.sBar = sBar;
+  gm.g = g; gm.t0 = t0; gm.te = te; gm.nt = nt; gm.N = N; gm.sP = sP; gm.sBar = sBar; gm.cs = 0.f;
   const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);   // sink tiles of this split
   gm.stok_first = (st_lo - te.n_blk) * TN;
   gm.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
 
-  const bool work = rows > 0 && nt > 0;
-  // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
-  const int qrow = (int)threadIdx.x >> 1, half = (int)threadIdx.x & 1;   // threads 0..255: half a row each
-  uint4 qv[8];
-  if (warp < 8) {
-#pragma unroll
-    for (int c = 0; c < 8; ++c) qv[c] = make_uint4(0, 0, 0, 0);
-    unsigned m = 0u;
-    if (half == 0) ms.orow[qrow] = -1;
-    if (qrow < rows) {
-      const int fr = mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
-      const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
-      if (pos >= p.q_base && pos < p.q_base + p.n_q) {
-        if (half == 0) ms.orow[qrow] = qr * p.H + g * p.hpg + hh;
-        if (work && half * 64 < D) {
-          const uint4* src = reinterpret_cast<const uint4*>(p.Q + (long long)(pos - p.q_base) * p.q_stride_row +
-                                                            (long long)(g * p.hpg + hh) * p.q_stride_head + half * 64);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) qv[c] = ld_ordered(src + c);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const unsigned u = w[e] & 0x7FFFu, v = (w[e] >> 16) & 0x7FFFu;  // magnitudes of bf16 order as integers
-              if (u < 0x7F80u) m = max(m, u);                                 // finite ones
-              if (v < 0x7F80u) m = max(m, v);
-            }
-          }
-        }
-      } else if (half == 0) {
-        set_status(p.status, FOCUS_ERR_INVALID_ARG);
-      }
+  // one K or V tile of the cache into its ring slot (all lanes of the producer warp)
+  auto issue_tma = [&](const TileInfo& ti, int kv, int slot, uint64_t pol) {
+    const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot);
+    const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
+    if (lane == 0) {
+      const CUtensorMap* map = kv ? &tmV : &tmK;
+      mbar_expect_tx(full, TN * D);
+      tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
+      if (p.pair) tma_load_3d_hint(dst + 64 * D, map, full, 0, ti.start2, g, pol);
+    } else {
+      mbar_arrive(full);
     }
-    m = __reduce_max_sync(0xffffffffu, m);
-    if (lane == 0) atomicMax(&ms.qmax, m);
-  } else if (warp == 12 && !p.dense && nt <= MAXT) {                                 // meanwhile: tile descriptors
-    for (int t = lane; t < nt; t += 32) {
-      ms.tlist[t] = pack_tile(make_tile(p, gm, t));
-    }
-  } else if (warp > 12) {                                              // and the sink tokens
-    for (int i = (int)threadIdx.x - 13 * 32; i < gm.stok_n; i += NTH - 13 * 32) {
+  };
+  // K/V tiles are read once (several row tiles of a head: once each, through L2)
+  const uint64_t pol = p.evict_first ? l2_policy_evict_first() : l2_policy_evict_normal();
+  // a dense key set is known without reading anything: its first copies start here, ahead of everything else
+  const int n_early = p.dense && work ? min(nt, RING) : 0;
+  if (warp == 0) {
+    __syncwarp();
+    for (int j = 0; j < n_early; ++j)
+      for (int kv = 0; kv < 2; ++kv) issue_tma(make_tile(p, gm, j), kv, j, pol);
+  }
+  if (!p.dense && warp == 4 && nt <= MAXT) {                         // tile descriptors
+    for (int t = lane; t < nt; t += 32) ms.tlist[t] = pack_tile(make_tile(p, gm, t));
+  }
+  if (warp >= 12) {                                                  // sink tokens
+    for (int i = (int)threadIdx.x - 384; i < gm.stok_n; i += 256) {
       const int s = gm.stok_first + i;
       ms.stok[i] = s < p.n_sink ? sink_token(p, g, s) : -1;
     }
   }
-  __syncthreads();
-  // the power of two: the tile's largest |q| to 2^14 .. 2^15
-  const int q_shift = ms.qmax ? min(14 - ((int)(ms.qmax >> 7) - 127), 126) : 0;
-  if (warp < 8 && work && half * 64 < D && qrow < NS) {
-    const float f = exp2f((float)q_shift);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
-      uint32_t o[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        o[i] = pack_f16(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xFFFF0000u) * f);
-      sts128(sQ + half * (QN * 128) + qrow * 128 + ((c ^ (qrow & 7)) << 4), o[0], o[1], o[2], o[3]);
-    }
-  }
-  const uint32_t tmem = ms.tmem;
-  const uint32_t tS = tmem, tO = tmem + 2 * NS, tOp = tmem + (alt ? 4 : 3) * NS;
-  gm.tmem = tmem;
-  gm.cs = p.scale_log2 * exp2f((float)-q_shift);
-  if (D == 64 && work && (warp == 10 || warp == 11)) {   // channels 64..127 do not exist: zeros, once
-    uint32_t z[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) z[i] = 0u;
-    for (int b = 0; b < nV; ++b) {
-      const uint32_t a = tOp + (uint32_t)((nK + b) * 64) + ((uint32_t)((warp & 3) * 32) << 16);
-      TC_ST32(a, z);
-      TC_ST32(a + 32, z);
-    }
-    tc_wait_st();
-  }
-  fence_proxy_async();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  const uint32_t tmem = ms.tmem;
+  gm.tmem = tmem;
 
   if (wg == 0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 && work) {
       // ================================ producer ==================================================
-      const uint64_t pol = l2_policy_evict_first();
       bool ok = true;
-      int slot = 0, issued = 0;
-      uint32_t round = 0;
-      for (int j = 0; j < nt && ok; ++j) {
+      int slot = n_early == RING ? 0 : n_early, issued = 2 * n_early;
+      uint32_t round = n_early == RING ? 1u : 0u;
+      for (int j = n_early; j < nt && ok; ++j) {
         const TileInfo ti = get_tile(p, ms, gm, j);
+        if (ti.nvalid == 0 && lane == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot), empty = kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot);
+          const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot);
           const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
-          ok = mbar_wait(empty, (round & 1u) ^ 1u, abort_flag, p.status);
+          ok = mbar_wait(kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot), (round & 1u) ^ 1u, abort_flag, p.status);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           ++issued;
-          if (ti.nvalid == 0 && lane == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
           if (ti.kind == 0) {
             fence_proxy_async();                                       // the slot may have been filled with plain copies before
-            if (lane == 0) {
-              const CUtensorMap* map = kv ? &tmV : &tmK;
-              mbar_expect_tx(full, TN * D);
-              if (p.pair) {
-                if (p.evict_first) {
-                  tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
-                  tma_load_3d_hint(dst + 64 * D, map, full, 0, ti.start2, g, pol);
-                } else {
-                  tma_load_3d(dst, map, full, 0, ti.start, g);
-                  tma_load_3d(dst + 64 * D, map, full, 0, ti.start2, g);
-                }
-              } else if (p.evict_first) {
-                tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
-              } else {
-                tma_load_3d(dst, map, full, 0, ti.start, g);
-              }
-            } else {
-              mbar_arrive(full);
-            }
+            issue_tma(ti, kv, slot, pol);
           } else {
             // sink tokens lie anywhere: 16-byte copies, dropped ones as zeros
             constexpr int CPR = D / 16;
             const uint8_t* base = (kv ? p.V : p.K) + (long long)g * p.kv_stride_head;
-            int tok[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tok[i] = key_token(p, ms, gm, ti, i * 32 + lane);
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < 4; ++i) {
+              const int tok = key_token(p, ms, gm, ti, i * 32 + lane);
 #pragma unroll
               for (int it = 0; it < CPR; ++it) {
                 const int q = it * 32 + lane, rr = q / CPR, c = q % CPR;      // row within this group of 32, chunk
-                const int t = __shfl_sync(0xffffffffu, tok[i], rr);
-                const uint32_t n = t >= 0 ? 16u : 0u;
+                const int t = __shfl_sync(0xffffffffu, tok, rr);
                 const uint8_t* src = base + (long long)max(t, 0) * p.kv_stride_tok + c * 16;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                             ::"r"(dst + raw_off<D>(i * 32 + rr, c)), "l"(src), "r"(n) : "memory");
+                             ::"r"(dst + raw_off<D>(i * 32 + rr, c)), "l"(src), "r"(t >= 0 ? 16u : 0u) : "memory");
               }
             }
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
             if (kv == 0) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {                            // a listed sink outside [0, L) is reported
-                const int k = i * 32 + lane;
-                if (k < ti.nvalid) {
-                  const int s = __ldg(p.sink_idx + ti.start + k);
-                  if (s < 0 || s >= p.L) set_status(p.status, FOCUS_ERR_INVALID_ARG);
-                }
+#pragma unroll 1
+              for (int k = lane; k < ti.nvalid; k += 32) {             // a listed sink outside [0, L) is reported
+                const int s = __ldg(p.sink_idx + ti.start + k);
+                if (s < 0 || s >= p.L) set_status(p.status, FOCUS_ERR_INVALID_ARG);
               }
             }
           }
@@ -628,41 +530,41 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
     } else if (warp == 1 && lane == 0 && work) {
       // ================================ MMA issuer ================================================
+      // S of tile j + 2 goes ahead of P V of tile j: its buffer is free as soon as the softmax has tile j's logits in
+      // registers, long before P of that tile is written
       const uint32_t ID_QK = idesc_f16(N, 0), ID_PV = idesc_f16(N, 1);
       const uint64_t qdesc = make_sdesc(sQ, 16, 1024);
-      bool ok = true;
-      int kb = 0, vb = 0;
-      uint32_t kr = 0, vr = 0;
-      auto do_pv = [&](int j) -> bool {
+      auto do_qk = [&](int j) -> bool {
         const int b = j & 1;
-        if (!mbar_wait(bar_vop_full(sBar, vb), vr & 1u, abort_flag, p.status)) return false;
-        if (!mbar_wait(bar_p_full(sBar, b), (uint32_t)(j >> 1) & 1u, abort_flag, p.status)) return false;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+        if (!mbar_wait(bar_kop_full(sBar, b), ph, abort_flag, p.status)) return false;
+        if (!mbar_wait(bar_s_empty(sBar, b), ph ^ 1u, abort_flag, p.status)) return false;
         tc_fence_after();
-        const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
-        const uint32_t a = tOp + (uint32_t)((nK + vb) * 64);
-#pragma unroll
-        for (int ks = 0; ks < TN / 16; ++ks)
-          mma_ts(tO + (alt ? b * NS : 0), a + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (ks || j > (alt ? 1 : 0)) ? 1u : 0u);
-        tc_commit(bar_vop_empty(sBar, vb));
-        tc_commit(bar_p_empty(sBar, b));
-        if (++vb == nV) { vb = 0; ++vr; }
-        return true;
-      };
-      for (int j = 0; j < nt && ok; ++j) {
-        const int b = j & 1;
-        if (!mbar_wait(bar_kop_full(sBar, kb), kr & 1u, abort_flag, p.status)) { ok = false; break; }
-        if (!mbar_wait(bar_s_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t a = tOp + (uint32_t)(kb * 64);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-          mma_ts(tS + b * NS, a + ks * 8, qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), ID_QK, ks ? 1u : 0u);
-        tc_commit(bar_kop_empty(sBar, kb));
+          mma_ts(tmem + T_S + b * QN, tmem + T_K + b * 64 + ks * 8,
+                 qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), ID_QK, ks ? 1u : 0u);
+        tc_commit(bar_kop_empty(sBar, b));
         tc_commit(bar_s_full(sBar, b));
-        if (++kb == nK) { kb = 0; ++kr; }
-        if (j > 0) ok = do_pv(j - 1);
+        return true;
+      };
+      bool ok = mbar_wait(bar_q_full(sBar), 0u, abort_flag, p.status);
+      if (ok) ok = do_qk(0);
+      if (ok && nt > 1) ok = do_qk(1);
+      for (int j = 0; j < nt && ok; ++j) {
+        if (j + 2 < nt && !do_qk(j + 2)) break;
+        const int b = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+        if (!mbar_wait(bar_vop_full(sBar, b), ph, abort_flag, p.status)) break;
+        if (!mbar_wait(bar_p_full(sBar, b), ph, abort_flag, p.status)) break;
+        tc_fence_after();
+        const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
+#pragma unroll
+        for (int ks = 0; ks < TN / 16; ++ks)
+          mma_ts(tmem + T_O + b * QN, tmem + T_V + b * 64 + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (ks || j > 1) ? 1u : 0u);
+        tc_commit(bar_vop_empty(sBar, b));
+        tc_commit(bar_p_empty(sBar, b));
       }
-      if (ok) do_pv(nt - 1);
     }
     __syncwarp();
     tc_fence_before();
@@ -671,18 +573,19 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     if (warp == 2) { __syncwarp(); tmem_dealloc(tmem, 512); }
   } else if (wg == 1) {
     // ================================ K codes -> A operand of S^T =====================================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (work) {
       const int key = (warp & 3) * 32 + lane;
       const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-      int slot = 0, ob = 0;
-      uint32_t round = 0, orr = 0;
+      int slot = 0;
+      uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
-        bool ok = mbar_wait(bar_k_full(sBar, slot), round & 1u, abort_flag, p.status) &&
-                  mbar_wait(bar_kop_empty(sBar, ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        const int b = j & 1;
+        const bool ok = mbar_wait(bar_k_full(sBar, slot), round & 1u, abort_flag, p.status) &&
+                        mbar_wait(bar_kop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
-        const uint32_t src = sRawK + slot * SLOT, dst = tOp + (uint32_t)(ob * 64) + lane_off;
+        const uint32_t src = sRawK + slot * SLOT, dst = tmem + (uint32_t)(T_K + b * 64) + lane_off;
 #pragma unroll
         for (int h = 0; h < D / 64; ++h) {
           uint32_t o[32];
@@ -701,26 +604,34 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(bar_k_empty(sBar, slot)); mbar_arrive(bar_kop_full(sBar, ob)); }
+        if (lane == 0) { mbar_arrive(bar_k_empty(sBar, slot)); mbar_arrive(bar_kop_full(sBar, b)); }
         if (++slot == RING) { slot = 0; ++round; }
-        if (++ob == nK) { ob = 0; ++orr; }
       }
     }
     tc_fence_before();
     asm volatile("bar.sync 0;" ::: "memory");
   } else if (wg == 2) {
     // ================================ V codes, transposed -> A operand of O^T ===========================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (work) {
       const int cw = warp & 3;                                         // channels 32 cw .. 32 cw + 31
-      int slot = 0, ob = 0;
-      uint32_t round = 0, orr = 0;
+      if (cw * 32 >= D) {                                              // head dim 64: the upper lanes stay zero
+        uint32_t z[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] = 0u;
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) TC_ST32(tmem + (uint32_t)(T_V + i * 32) + ((uint32_t)(cw * 32) << 16), z);
+        tc_wait_st();
+      }
+      int slot = 0;
+      uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
-        bool ok = mbar_wait(bar_v_full(sBar, slot), round & 1u, abort_flag, p.status) &&
-                  mbar_wait(bar_vop_empty(sBar, ob), (orr & 1u) ^ 1u, abort_flag, p.status);
+        const int b = j & 1;
+        const bool ok = mbar_wait(bar_v_full(sBar, slot), round & 1u, abort_flag, p.status) &&
+                        mbar_wait(bar_vop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
-        const uint32_t src = sRawV + slot * SLOT, dst = tOp + (uint32_t)((nK + ob) * 64) + ((uint32_t)(cw * 32) << 16);
+        const uint32_t src = sRawV + slot * SLOT, dst = tmem + (uint32_t)(T_V + b * 64) + ((uint32_t)(cw * 32) << 16);
         if (cw * 32 < D) {
 #pragma unroll
           for (int hc = 0; hc < 2; ++hc) {                             // sixteen channels
@@ -744,9 +655,8 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(bar_v_empty(sBar, slot)); mbar_arrive(bar_vop_full(sBar, ob)); }
+        if (lane == 0) { mbar_arrive(bar_v_empty(sBar, slot)); mbar_arrive(bar_vop_full(sBar, b)); }
         if (++slot == RING) { slot = 0; ++round; }
-        if (++ob == nV) { ob = 0; ++orr; }
       }
     }
     tc_fence_before();
@@ -754,29 +664,79 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   } else {
     // ================================ softmax =========================================================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
-    const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane;
+    const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane, tid = (int)threadIdx.x - 384;
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-    if (work) {
-      if (alt) {
-        if (N == 16) softmax_loop<2, true>(p, ms, gm, x, wq, lane);
-        else if (N == 32) softmax_loop<4, true>(p, ms, gm, x, wq, lane);
-        else if (N == 48) softmax_loop<6, true>(p, ms, gm, x, wq, lane);
-        else softmax_loop<8, true>(p, ms, gm, x, wq, lane);
-      } else {
-        if (N == 96) softmax_loop<6, false>(p, ms, gm, x, wq, lane);
-        else softmax_loop<8, false>(p, ms, gm, x, wq, lane);
+    if (rows > 0) {
+      // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
+      const int qrow = tid >> 2, quarter = tid & 3;                    // a quarter (32 elements) of a row per thread
+      uint4 qv[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) qv[c] = make_uint4(0, 0, 0, 0);
+      unsigned m = 0u;
+      int orow = -1;
+      if (qrow < rows) {
+        const int fr = mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
+        const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
+        if (pos >= p.q_base && pos < p.q_base + p.n_q) {
+          orow = qr * p.H + g * p.hpg + hh;
+          if (quarter * 32 < D) {
+            const uint4* src = reinterpret_cast<const uint4*>(p.Q + (long long)(pos - p.q_base) * p.q_stride_row +
+                                                              (long long)(g * p.hpg + hh) * p.q_stride_head + quarter * 32);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) qv[c] = ld_ordered(src + c);
+          }
+        } else if (quarter == 0) {
+          set_status(p.status, FOCUS_ERR_INVALID_ARG);
+        }
       }
+      if (quarter == 0) ms.orow[qrow] = orow;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned u = w[e] & 0x7FFFu, v = (w[e] >> 16) & 0x7FFFu;      // magnitudes of bf16 order as integers
+          if (u < 0x7F80u) m = max(m, u);                                     // finite ones
+          if (v < 0x7F80u) m = max(m, v);
+        }
+      }
+      m = __reduce_max_sync(0xffffffffu, m);
+      if (lane == 0) atomicMax(&ms.qmax, m);
+      named_sync(3, 256);
+      // the power of two: the tile's largest |q| to 2^14 .. 2^15
+      const int sh = ms.qmax ? min(14 - ((int)(ms.qmax >> 7) - 127), 126) : 0;
+      const float f = exp2f((float)sh);
+      gm.cs = p.scale_log2 * exp2f((float)-sh);
+      if (quarter * 32 < D) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t w[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            o[i] = pack_f16(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xFFFF0000u) * f);
+          const int cc = (quarter & 1) * 4 + c;                        // chunk within the row's 64-element half
+          sts128(sQ + (quarter >> 1) * (QN * 128) + qrow * 128 + ((cc ^ (qrow & 7)) << 4), o[0], o[1], o[2], o[3]);
+        }
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_q_full(sBar));
+    }
+    if (work) {
+      if (N == 16) softmax_loop<2>(p, ms, gm, x, wq, lane);
+      else if (N == 32) softmax_loop<4>(p, ms, gm, x, wq, lane);
+      else if (N == 48) softmax_loop<6>(p, ms, gm, x, wq, lane);
+      else softmax_loop<8>(p, ms, gm, x, wq, lane);
     }
     named_sync(3, 256);
-    // ---- row statistics: sums of the warps in order; the two warpgroups' shares of a row joined (ALT) ----
-    if ((int)threadIdx.x - 384 < rows) {
-      const int r = (int)threadIdx.x - 384;
+    // ---- row statistics: sums of the warps in order, the two warpgroups' shares of a row joined ----
+    if (tid < rows) {
+      const int r = tid;
       float ref = REF_NONE, tot = 0.f, w0 = 0.f, w1 = 0.f;
       if (work) {
-        const int xr = alt ? 0 : r / (N / 2), cr = alt ? r : r - xr * (N / 2);
-        auto warps = [&](int q) { return ((ms.red[q * 4][cr] + ms.red[q * 4 + 1][cr]) + ms.red[q * 4 + 2][cr]) + ms.red[q * 4 + 3][cr]; };
-        const float l0 = warps(xr), r0 = -ms.nref[0][r];
-        const float l1 = alt && nt > 1 ? warps(1) : 0.f, r1 = alt ? -ms.nref[1][r] : REF_NONE;
+        auto warps = [&](int q) { return ((ms.red[q * 4][r] + ms.red[q * 4 + 1][r]) + ms.red[q * 4 + 2][r]) + ms.red[q * 4 + 3][r]; };
+        const float l0 = warps(0), l1 = warps(1), r0 = -ms.nref[0][r], r1 = -ms.nref[1][r];
         ref = fmaxf(r0, r1);
         w0 = l0 != 0.f ? ex2(r0 - ref) : 0.f;
         w1 = l1 != 0.f ? ex2(r1 - ref) : 0.f;
@@ -794,29 +754,36 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       ms.fac[0][r] = w0; ms.fac[1][r] = w1;
     }
     named_sync(3, 256);
-    // ---- O^T: this thread's channel of every row of its half ----
+    // ---- O^T: this thread's channel of the rows of its half (a warpgroup's share without a key is never read) ----
     const int ch = key, c0 = x * (N >> 1);
 #pragma unroll 1
     for (int i = 0; i < N >> 4; ++i) {
-      uint32_t o[8], o1[8];
+      uint32_t o0[8], o1[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = o1[e] = 0u;
+      for (int e = 0; e < 8; ++e) o0[e] = o1[e] = 0u;
       if (work) {
-        TC_LD8(tO + (uint32_t)(c0 + i * 8) + lane_off, o);
-        if (alt && nt > 1) TC_LD8(tO + (uint32_t)(NS + c0 + i * 8) + lane_off, o1);
+        TC_LD8(tmem + (uint32_t)(T_O + c0 + i * 8) + lane_off, o0);
+        TC_LD8(tmem + (uint32_t)(T_O + QN + c0 + i * 8) + lane_off, o1);
         tc_wait_ld();
       }
-      if (ch < D) {
+      const int r0 = c0 + i * 8;
+      float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int r = c0 + i * 8 + e;
-          if (r < rows) {
-            // a row's share without a key holds nothing that may be read
-            const float f0 = ms.fac[0][r], f1 = ms.fac[1][r];
-            float v = f0 != 0.f ? __uint_as_float(o[e]) * f0 : 0.f;
-            if (f1 != 0.f) v = fmaf(__uint_as_float(o1[e]), f1, v);
-            if (p.n_splits > 1) p.part_O[((size_t)cta * QN + r) * D + ch] = v;
-            else if (ms.orow[r] >= 0) p.O[(size_t)ms.orow[r] * D + ch] = __float2bfloat16_rn(v);
+      for (int e = 0; e < 8; ++e) {
+        const float f0 = ms.fac[0][r0 + e], f1 = ms.fac[1][r0 + e];
+        v[e] = (f0 != 0.f ? __uint_as_float(o0[e]) * f0 : 0.f) + (f1 != 0.f ? __uint_as_float(o1[e]) * f1 : 0.f);
+      }
+      if (ch < D) {
+        if (p.n_splits > 1) {
+          float* dst = p.part_O + ((size_t)cta * QN + r0) * D + ch;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (r0 + e < rows) dst[e * D] = v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int orow = ms.orow[r0 + e];
+            if (r0 + e < rows && orow >= 0) p.O[(size_t)orow * D + ch] = __float2bfloat16_rn(v[e]);
           }
         }
       }
@@ -825,7 +792,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     asm volatile("bar.sync 0;" ::: "memory");
     // ---- merge of the splits by the CTA that arrives last, splits in order ----
     if (p.n_splits > 1 && rows > 0) {
-      const int tid = (int)threadIdx.x - 384, S = p.n_splits;
+      const int S = p.n_splits;
       __threadfence();
       named_sync(3, 256);
       if (tid == 0) {
@@ -918,7 +885,7 @@ constexpr int MAX_SPLITS = 64;
 
 bool attn_quant_tc_supported(const focus_ctx* ctx, const AttnArgs& a) {
   return ctx->encode_tiled != nullptr && a.sh.dtype == FOCUS_BF16 && (a.sh.head_dim == 128 || a.sh.head_dim == 64) &&
-         (a.sh.n_q_heads / a.sh.n_kv_heads) <= QN && (long long)a.max_rows * a.sh.n_q_heads < (1ll << 31);
+         (long long)a.max_rows * a.sh.n_q_heads < (1ll << 31);
 }
 
 focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
