@@ -19,7 +19,7 @@
 //
 // Warp roles (640 threads):
 //   warp 0        producer: K and V tiles as raw codes into two rings (TMA; sink tokens one by one with cp.async)
-//   warp 1        tcgen05.mma issuer
+//   warps 1, 3    tcgen05.mma issuers, one per product: neither has to wait for what only the other needs
 //   warp 2        TMEM allocation
 //   warps 4..7    K codes -> fp16 in TMEM (lane = key): the A operand of S^T
 //   warps 8..11   V codes -> fp16 in TMEM (lane = channel; ldmatrix transposes the bytes): the A operand of O^T
@@ -49,6 +49,7 @@ constexpr int T_S = 0, T_O = 128, T_K = 256, T_V = 384;
 constexpr int MAXT = 256;                      // key tiles of a split whose descriptors are staged
 constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
+constexpr int MAX_SPLITS = 64;
 constexpr float THRESH = 15.5f;               // the reference follows the maximum once that is this far (log2) above ...
 constexpr float OFFSET = 6.f;                  // ... and is put this far below it: P <= 2^15.5, normal fp16 down to 2^-20
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
@@ -74,7 +75,7 @@ struct QParams {
   int32_t* counters;           // one arrival counter per (KV head, row tile)
   long long q_stride_row, q_stride_head, kv_stride_tok, kv_stride_head, scale_stride;
   int q_base, n_q, rows_bound, L, M, H, hpg, B, nb, dense, group_stride, max_blocks, n_sink, ns_pad;
-  int n_mtiles, n_splits, lse_stride, pair, pdl, evict_first;
+  int Hkv, max_tiles, sms, lse_stride, pair, pdl;
   float scale_log2;
   int32_t* status;
 };
@@ -386,7 +387,6 @@ __global__ void __launch_bounds__(NTH, 1)
 attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const QParams p) {
   extern __shared__ uint8_t smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
-  const int g = blockIdx.x / p.n_mtiles, mt = blockIdx.x % p.n_mtiles, split = blockIdx.y;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* sptr = smem_raw + (sbase - smem_u32(smem_raw));
   Misc& ms = *reinterpret_cast<Misc*>(sptr + OFF_MISC);
@@ -416,14 +416,19 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (threadIdx.x < 2 * QN) ms.nref[0][threadIdx.x] = -REF_NONE;
   if (p.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing in global memory is touched before this
 
-  // ---- rows, tiles ----
+  // ---- which row tile and which key tiles.  How many rows there are is known on the device only, so the split of the
+  // grid is chosen here: the row tiles that hold rows share all CTAs, at least two key tiles per split ----
   const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
+  const int n_mt = (nrows * p.hpg + QN - 1) / QN, base = n_mt * p.Hkv;
+  const int n_splits = max(1, min(min(p.sms / max(base, 1), p.max_tiles >> 1), MAX_SPLITS));   // > 1: at most sms CTAs in all
+  const int tile = (int)blockIdx.x / n_splits, split = (int)blockIdx.x - tile * n_splits;
+  const int g = min(tile / max(n_mt, 1), p.Hkv - 1), mt = tile - g * n_mt;
+  const int cta = (int)blockIdx.x;
+  const int rows = tile < base ? min(QN, nrows * p.hpg - mt * QN) : 0;   // stacked (row, head of the group) rows of this CTA
   const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
   const TileEnum te = make_enum(p, g, cnt_raw);
-  const int t0 = split_lo(te.total, split, p.n_splits), nt = split_lo(te.total, split + 1, p.n_splits) - t0;
-  const int rows = min(QN, nrows * p.hpg - mt * QN);                 // stacked (row, head of the group) rows of this CTA
+  const int t0 = split_lo(te.total, split, n_splits), nt = split_lo(te.total, split + 1, n_splits) - t0;
   const bool work = rows > 0 && nt > 0;
-  const int cta = blockIdx.x * p.n_splits + split;
   const int N = rows > 0 ? (rows + 15) & ~15 : 16;                   // columns of S^T and O^T
   Geo gm;
   gm.g = g; gm.t0 = t0; gm.te = te; gm.nt = nt; gm.N = N; gm.sP = sP; gm.sBar = sBar; gm.cs = 0.f;
@@ -444,8 +449,8 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       mbar_arrive(full);
     }
   };
-  // K/V tiles are read once (several row tiles of a head: once each, through L2)
-  const uint64_t pol = p.evict_first ? l2_policy_evict_first() : l2_policy_evict_normal();
+  // K/V tiles are read once, or once per row tile of their head (through L2)
+  const uint64_t pol = n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
   // a dense key set is known without reading anything: its first copies start here, ahead of everything else
   const int n_early = p.dense && work ? min(nt, RING) : 0;
   if (warp == 0) {
@@ -529,30 +534,27 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         }
       }
     } else if (warp == 1 && lane == 0 && work) {
-      // ================================ MMA issuer ================================================
-      // S of tile j + 2 goes ahead of P V of tile j: its buffer is free as soon as the softmax has tile j's logits in
-      // registers, long before P of that tile is written
-      const uint32_t ID_QK = idesc_f16(N, 0), ID_PV = idesc_f16(N, 1);
+      // ================================ S^T = K Q^T ===============================================
+      const uint32_t id = idesc_f16(N, 0);
       const uint64_t qdesc = make_sdesc(sQ, 16, 1024);
-      auto do_qk = [&](int j) -> bool {
-        const int b = j & 1;
-        const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-        if (!mbar_wait(bar_kop_full(sBar, b), ph, abort_flag, p.status)) return false;
-        if (!mbar_wait(bar_s_empty(sBar, b), ph ^ 1u, abort_flag, p.status)) return false;
-        tc_fence_after();
+      if (mbar_wait(bar_q_full(sBar), 0u, abort_flag, p.status))
+        for (int j = 0; j < nt; ++j) {
+          const int b = j & 1;
+          const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+          if (!mbar_wait(bar_kop_full(sBar, b), ph, abort_flag, p.status)) break;
+          if (!mbar_wait(bar_s_empty(sBar, b), ph ^ 1u, abort_flag, p.status)) break;
+          tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          mma_ts(tmem + T_S + b * QN, tmem + T_K + b * 64 + ks * 8,
-                 qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), ID_QK, ks ? 1u : 0u);
-        tc_commit(bar_kop_empty(sBar, b));
-        tc_commit(bar_s_full(sBar, b));
-        return true;
-      };
-      bool ok = mbar_wait(bar_q_full(sBar), 0u, abort_flag, p.status);
-      if (ok) ok = do_qk(0);
-      if (ok && nt > 1) ok = do_qk(1);
-      for (int j = 0; j < nt && ok; ++j) {
-        if (j + 2 < nt && !do_qk(j + 2)) break;
+          for (int ks = 0; ks < D / 16; ++ks)
+            mma_ts(tmem + T_S + b * QN, tmem + T_K + b * 64 + ks * 8,
+                   qdesc + (uint64_t)(((ks >> 2) * (QN * 128) + (ks & 3) * 32) >> 4), id, ks ? 1u : 0u);
+          tc_commit(bar_kop_empty(sBar, b));
+          tc_commit(bar_s_full(sBar, b));
+        }
+    } else if (warp == 3 && lane == 0 && work) {
+      // ================================ O^T += V^T P^T ============================================
+      const uint32_t id = idesc_f16(N, 1);
+      for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1u;
         if (!mbar_wait(bar_vop_full(sBar, b), ph, abort_flag, p.status)) break;
@@ -561,7 +563,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
 #pragma unroll
         for (int ks = 0; ks < TN / 16; ++ks)
-          mma_ts(tmem + T_O + b * QN, tmem + T_V + b * 64 + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), ID_PV, (ks || j > 1) ? 1u : 0u);
+          mma_ts(tmem + T_O + b * QN, tmem + T_V + b * 64 + ks * 8, pdesc + (uint64_t)(ks * (2048 >> 4)), id, (ks || j > 1) ? 1u : 0u);
         tc_commit(bar_vop_empty(sBar, b));
         tc_commit(bar_p_empty(sBar, b));
       }
@@ -742,7 +744,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         w1 = l1 != 0.f ? ex2(r1 - ref) : 0.f;
         tot = w0 * l0 + w1 * l1;
       }
-      if (p.n_splits > 1) {
+      if (n_splits > 1) {
         reinterpret_cast<float2*>(p.part_ml)[(size_t)cta * QN + r] = make_float2(ref, tot);
       } else {
         const float inv = tot != 0.f ? 1.f / tot : 0.f;
@@ -774,7 +776,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         v[e] = (f0 != 0.f ? __uint_as_float(o0[e]) * f0 : 0.f) + (f1 != 0.f ? __uint_as_float(o1[e]) * f1 : 0.f);
       }
       if (ch < D) {
-        if (p.n_splits > 1) {
+        if (n_splits > 1) {
           float* dst = p.part_O + ((size_t)cta * QN + r0) * D + ch;
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -791,20 +793,20 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     tc_fence_before();
     asm volatile("bar.sync 0;" ::: "memory");
     // ---- merge of the splits by the CTA that arrives last, splits in order ----
-    if (p.n_splits > 1 && rows > 0) {
-      const int S = p.n_splits;
+    if (n_splits > 1 && rows > 0) {
+      const int S = n_splits;
       __threadfence();
       named_sync(3, 256);
       if (tid == 0) {
-        const int prev = atomicAdd(&p.counters[blockIdx.x], 1);
+        const int prev = atomicAdd(&p.counters[tile], 1);
         ms.last = prev == S - 1;
-        if (ms.last) p.counters[blockIdx.x] = 0;                       // armed for the next launch
+        if (ms.last) p.counters[tile] = 0;                       // armed for the next launch
         __threadfence();
       }
       named_sync(3, 256);
       if (ms.last) {
         float* wts = reinterpret_cast<float*>(sptr + Q_BYTES);         // [row][split], over the P tiles
-        const size_t c_first = (size_t)blockIdx.x * S;
+        const size_t c_first = (size_t)tile * S;
         if (tid < rows) {
           const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + c_first * QN + tid;
           float m = -INFINITY, tot = 0.f;
@@ -879,8 +881,6 @@ focus_status launch(focus_ctx* ctx, bool& attr_set, const CUtensorMap& tmK, cons
   return FOCUS_OK;
 }
 
-constexpr int MAX_SPLITS = 64;
-
 }  // namespace
 
 bool attn_quant_tc_supported(const focus_ctx* ctx, const AttnArgs& a) {
@@ -897,22 +897,16 @@ focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_
   p.ns_pad = a.dense ? 0 : (a.n_sink + TN - 1) / TN * TN;
   const int n_resp = a.dense ? (sh.L + TN - 1) / TN : (sh.L - sh.M + TN - 1) / TN;
   const int max_tiles = a.dense ? n_resp : (p.pair ? (a.max_blocks + 1) / 2 : a.max_blocks) + p.ns_pad / TN + n_resp;
-  p.n_mtiles = (int)((stacked + QN - 1) / QN);
-  const long long base = (long long)p.n_mtiles * Hkv;
+  p.max_tiles = max_tiles; p.sms = ctx->sm_count;
+  p.Hkv = Hkv;
+  const long long base = (stacked + QN - 1) / QN * Hkv;               // row tiles, if every listed row is there
   if (base > 0x7FFFFFFF) return FOCUS_ERR_UNSUPPORTED;
-  // key splits: as many CTAs as SMs, at least two tiles each
-  int splits = (int)(ctx->sm_count / base);
-  if (splits > max_tiles / 2) splits = max_tiles / 2;
-  if (splits > MAX_SPLITS) splits = MAX_SPLITS;
-  if (splits < 1) splits = 1;
-  p.n_splits = splits;
-  p.part_O = p.part_ml = nullptr;
-  if (splits > 1) {
-    WsAlloc ws(ctx);
-    p.part_O = ws.get<float>((size_t)base * splits * QN * sh.head_dim);
-    p.part_ml = ws.get<float>((size_t)base * splits * QN * 2);
-    if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
-  }
+  // one CTA per SM, or per row tile where there are more; splits (chosen in the kernel) occur only in the first case
+  const int ctas = base > ctx->sm_count ? (int)base : ctx->sm_count;
+  WsAlloc ws(ctx);
+  p.part_O = ws.get<float>((size_t)ctx->sm_count * QN * sh.head_dim);
+  p.part_ml = ws.get<float>((size_t)ctx->sm_count * QN * 2);
+  if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
   p.counters = ctx->d_counters;
   p.Q = (const __nv_bfloat16*)a.Q; p.O = (__nv_bfloat16*)a.O; p.lse = a.lse;
   p.q_rows = a.q_rows; p.n_rows = a.n_rows; p.block_idx = a.block_idx; p.block_cnt = a.block_cnt;
@@ -924,7 +918,6 @@ focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_
   p.B = sh.kv_block; p.nb = shape_nb(&sh); p.dense = a.dense; p.group_stride = a.group_stride;
   p.max_blocks = a.max_blocks; p.n_sink = a.n_sink; p.lse_stride = a.lse_stride;
   p.pdl = ctx->no_pdl ? 0 : 1;
-  p.evict_first = p.n_mtiles == 1;                                     // otherwise the row tiles of a head share its K/V in L2
   p.scale_log2 = a.scale * 1.4426950408889634f;
   p.status = ctx->d_status;
   CUtensorMap tmK, tmV;
@@ -932,7 +925,7 @@ focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_
   if (!encode_code_map(ctx->encode_tiled, &tmK, p.K, sh, box_rows) || !encode_code_map(ctx->encode_tiled, &tmV, p.V, sh, box_rows))
     return FOCUS_ERR_INVALID_ARG;
   ctx->last_attn_variant = 5;
-  const dim3 grid((unsigned)base, splits, 1);
+  const dim3 grid((unsigned)ctas, 1, 1);
   const bool i8 = a.qc->format == FOCUS_KV_INT8;
   bool* set = ctx->ls.quant_attr_set;
   if (sh.head_dim == 128)
