@@ -26,6 +26,8 @@
 //   warps 12..19  softmax: two warpgroups that take the key tiles in turn, with references, row sums and an O^T of their
 //                 own (a tile's chain of latencies, S ready -> P ready, then has two tile periods of time); P^T goes to
 //                 shared memory (the B operand of O^T)
+// Five kinds of code run side by side, so their loops are kept short (rolled where that costs little): with 24 KB of loop
+// bodies the softmax warps waited four to ten cycles for each instruction.
 // Expanding the codes into TMEM instead of shared memory halves the shared-memory traffic of a tile: one byte in, one
 // byte out per code, no fp16 copy there.
 #include <stddef.h>
@@ -50,8 +52,8 @@ constexpr int MAXT = 256;                      // key tiles of a split whose des
 constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
 constexpr int MAX_SPLITS = 64;
-constexpr float THRESH = 15.5f;               // the reference follows the maximum once that is this far (log2) above ...
-constexpr float OFFSET = 6.f;                  // ... and is put this far below it: P <= 2^15.5, normal fp16 down to 2^-20
+constexpr float P_MAX = 46340.f;               // the reference follows the maximum once a numerator exceeds 2^15.5 (fp16 ends at 65504) ...
+constexpr float OFFSET = 6.f;                  // ... and is put 6 (log2) below it: P is normal fp16 down to 2^-20 of the row's largest
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
 constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
                                                     // rows hold zeros, the writer flushes them)
@@ -80,6 +82,12 @@ struct QParams {
   int32_t* status;
 };
 
+struct Geo {                                   // a CTA's share of the work; lives in shared memory, each role takes what it needs
+  int g, t0, nt, rows, N;                      // KV head, first key tile, key tiles, query rows, rows rounded to 16
+  int mt, tile, n_splits, n_mt;                // row tile of the head, of the launch; splits it is cut into; row tiles per head
+  int stok_first, stok_n;                      // first sink (list position) in Misc::stok, and how many are there
+  TileEnum te;
+};
 constexpr int MAX_STOK = 8;                    // sink tiles of a split whose tokens are staged
 
 struct Misc {                                  // behind the tiles in shared memory
@@ -93,6 +101,7 @@ struct Misc {                                  // behind the tiles in shared mem
   uint32_t tmem;
   int abort_flag, last;
   unsigned qmax;
+  Geo geo;
 };
 constexpr int SMEM = 1024 + OFF_MISC + (int)sizeof(Misc);
 static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -133,6 +142,12 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// maximum over the warp of one float per lane (NaN is passed over)
+__device__ __forceinline__ float warp_max_f32(float x) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+  return m;
 }
 // a load that stays where it is written (a plain one may be moved down to its first use, an iteration later)
 __device__ __forceinline__ float ld_pinned(const float* p) {
@@ -181,14 +196,6 @@ __device__ __forceinline__ int sink_token(const QParams& p, int g, int s) {
   return (keep && j >= 0 && j < p.M) ? j : -1;             // response tokens are attended through their own tiles
 }
 
-struct Geo {                                   // what the roles share about their CTA
-  int g, t0, nt, N;
-  TileEnum te;
-  int stok_first;                              // first sink (list position) in Misc::stok, and how many are there
-  int stok_n;
-  uint32_t sP, sBar, tmem;
-  float cs;                                    // logit scale: softmax scale * log2(e) / query scale (softmax warps only)
-};
 // tile idx of this split: by arithmetic (dense), from the staged list, or from the block list (splits longer than that)
 __device__ __forceinline__ TileInfo make_tile(const QParams& p, const Geo& gm, int idx) {
   TileInfo ti = tile_info(p, gm.te, gm.t0 + idx);
@@ -221,6 +228,20 @@ __device__ __forceinline__ uint32_t bar_p_empty(uint32_t b, int i) { return b + 
 
 __device__ __forceinline__ uint32_t bar_q_full(uint32_t b) { return b + 8u * (4 * RING + 16); }
 
+// Bounded wait of few instructions (the roles' loops have to stay in the instruction cache; see the file comment): gives up
+// after about a second of polling, or when another thread of the CTA did, and leaves the report to the CTA's last lines.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (int n = 0; !mbar_try_wait(bar, parity); ++n) {
+    if (*abort_flag || n > (1 << 23)) { *abort_flag = 1; return false; }
+  }
+  return true;
+}
+
+// the arrivals of n threads at once: the same barrier from 31 lanes would be 31 shared-memory atomics in a row
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+
 // Reduces 32 values per lane over the 32 lanes by halving: 31 shuffles, lane i ends with the result of value i.
 template <typename Op>
 __device__ __forceinline__ float lane_reduce32(float* v, int lane, Op op) {
@@ -239,12 +260,15 @@ __device__ __forceinline__ float lane_reduce32(float* v, int lane, Op op) {
 // Softmax of one warpgroup (x = 0, 1: even, odd tiles), NP pieces of 8 rows; straight-line code per tile, since its length
 // in cycles is what a tile costs.  Leaves the row sums over this warpgroup's keys in ms.red.
 template <int NP>
-__device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const Geo& gm, int x, int wq, int lane) {
+__device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_t sP, uint32_t sBar, float cs, int x, int wq,
+                                             int lane) {
   constexpr int NC = NP * 8;
-  const int key = wq * 32 + lane, nt = gm.nt;
+  const Geo& gm = ms.geo;
+  const int key = wq * 32 + lane, nt = gm.nt, tok0 = gm.t0 * TN + key;
+  const uint32_t tmem = ms.tmem;
   const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-  const uint32_t tO = gm.tmem + (uint32_t)(T_O + x * QN) + lane_off, ts = gm.tmem + (uint32_t)(T_S + x * QN) + lane_off;
-  const uint32_t prow = gm.sP + (uint32_t)(x * P_BYTES + key * 128);
+  const uint32_t tO = tmem + (uint32_t)(T_O + x * QN) + lane_off, ts = tmem + (uint32_t)(T_S + x * QN) + lane_off;
+  const uint32_t prow = sP + (uint32_t)(x * P_BYTES + key * 128);
   volatile int* abort_flag = &ms.abort_flag;
   float* nref = ms.nref[x];
   float* fac = ms.fac[x];
@@ -259,7 +283,7 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const G
     if (idx >= nt) return;
     int t;
     if (p.dense) {
-      t = (gm.t0 + idx) * TN + key;
+      t = tok0 + idx * TN;
       if (t >= p.L) return;
     } else {
       t = key_token(p, ms, gm, get_tile(p, ms, gm, idx), key);
@@ -268,25 +292,35 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const G
     sk = ld_pinned(Ks + t);
     sv = ld_pinned(Vs + t);
   };
-  float sk, sv;
+  // of a tile's key: logit factor, log2 of the value scale (-inf: masked), one over the value scale
+  float ck, lv, iv;
+  auto factors = [&](float sk, float sv) {
+    const bool masked = sv == -1.f;
+    const float svc = fmaxf(sv, SV_MIN);
+    ck = sk * cs;
+    lv = masked ? -INFINITY : __log2f(svc);
+    iv = masked ? 0.f : __fdividef(1.f, svc);
+  };
+  float sk, sv;                                                        // the next tile's scales, on their way
   scales(x, sk, sv);
+  factors(sk, sv);
+  scales(x + 2, sk, sv);
   bool ok = true;
   for (int j = x; j < nt; j += 2) {
     const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-    const bool masked = sv == -1.f;
-    const float svc = fmaxf(sv, SV_MIN);
-    const float ck = sk * gm.cs, lv = masked ? -INFINITY : __log2f(svc), iv = masked ? 0.f : __fdividef(1.f, svc);
-    scales(j + 2, sk, sv);                                             // the next tile's, out of the way of their latency
-    ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full(gm.sBar, x), ph, abort_flag, p.status)) && ok;
+    ok = wait_bar(bar_s_full(sBar, x), ph, abort_flag);
+    // P V of this warpgroup's last tile has read the buffer (long ago, as a rule)
+    ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
     tc_fence_after();
     float a[NC];
     uint32_t* ar = reinterpret_cast<uint32_t*>(a);
-    auto load_logits = [&]() {
+    bool again = false;
+#pragma unroll 1
+    for (;;) {
+      // ---- P = 2^(s ck + lv - ref), to shared memory as fp16 ----
 #pragma unroll
       for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
       tc_wait_ld();
-    };
-    auto exponents = [&]() {                                           // a = s ck + lv - ref
 #pragma unroll
       for (int q = 0; q < NP * 2; ++q) {
         const float4 rv = reinterpret_cast<const float4*>(nref)[q];
@@ -296,80 +330,80 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, const G
         fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
         fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
       }
-    };
-    load_logits();
-    exponents();
-    float mx = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < NC; e += 4) {
-      mx = fmax3(mx, a[e], a[e + 1]);
-      m1 = fmax3(m1, a[e + 2], a[e + 3]);
-    }
-    if (named_any(1 + x, 128, fmaxf(mx, m1) > THRESH || !ok)) {
-      // ---- some row's maximum outgrew its reference (always so at the first key): new references ----
-      if (named_any(1 + x, 128, !ok)) break;
-      load_logits();
+      for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
+      float m0 = 0.f, m1 = 0.f;
 #pragma unroll
-      for (int h = 0; h * 4 < NP; ++h) {                               // 32 rows at a time
-        float v[32];
+      for (int e = 0; e < NC; e += 4) {
+        m0 = fmax3(m0, a[e], a[e + 1]);
+        m1 = fmax3(m1, a[e + 2], a[e + 3]);
+      }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = h * 32 + e < NC ? fmaf(a[h * 32 + e < NC ? h * 32 + e : 0], ck, lv) : -INFINITY;
-        red[h * 32 + lane] = lane_reduce32(v, lane, [](float u, float w) { return fmaxf(u, w); });
+      for (int i = 0; i < NP; ++i) {
+        const float* v = a + i * 8;
+        sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
+               pack_f16(v[6], v[7]));
+      }
+      fence_proxy_async();
+      // The numerators are formed before anyone has looked whether they fit: the look costs a barrier of the four warps,
+      // and here it is the one that hands the tile over anyway.
+      if (!named_any(1 + x, 128, (fmaxf(m0, m1) > P_MAX && !again) || !ok)) break;
+      if (named_any(1 + x, 128, !ok)) { again = true; ok = false; break; }
+      // ---- some row's maximum outgrew its reference (always so at the first key): new references, once more.  Rolled
+      // loops: code that runs this seldom is fetched from L2 each time ----
+#pragma unroll 1
+      for (int i = 0; i < NP; ++i) {
+        uint32_t v[8];
+        TC_LD8(ts + i * 8, v);
+        tc_wait_ld();
+        float mine = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float w = warp_max_f32(fmaf(__uint_as_float(v[e]), ck, lv));
+          if (lane == e) mine = w;
+        }
+        if (lane < 8) red[i * 8 + lane] = mine;
       }
       named_sync(1 + x, 128);
       if (key < NC) {
         const float(*r)[QN] = &ms.red[x * 4];
-        const float top = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
-        const float old = nref[key], now = OFFSET - top;
+        const float rowmax = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
+        const float old = nref[key], now = OFFSET - rowmax;
         const bool up = now < old;
         fac[key] = up ? ex2(now - old) : 1.f;
         if (up) nref[key] = now;
       }
       named_sync(1 + x, 128);
-      if (j >= 2) {
-        // what these rows have summed is in TMEM once P V of this warpgroup's last tile is done
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, x), ph ^ 1u, abort_flag, p.status));
-        tc_fence_after();
+      if (j >= 2) {                                                    // what these rows have summed: P V of tile j - 2 is done
+#pragma unroll 1
+        for (int i = 0; i < NP; ++i) {
+          uint32_t v[8];
+          TC_LD8(tO + i * 8, v);
+          tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < NP; ++i) TC_LD8(tO + i * 8, ar + i * 8);
-        tc_wait_ld();
+          for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fac[i * 8 + e]);
+          TC_ST8(tO + i * 8, v);
+        }
+        tc_wait_st();
 #pragma unroll
         for (int q = 0; q < NP * 2; ++q) {
           const float4 f = reinterpret_cast<const float4*>(fac)[q];
-          float* v = a + q * 4;
           l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w;
-          v[0] *= f.x; v[1] *= f.y; v[2] *= f.z; v[3] *= f.w;
         }
-#pragma unroll
-        for (int i = 0; i < NP; ++i) TC_ST8(tO + i * 8, ar + i * 8);
-        tc_wait_st();
       }
-      load_logits();
-      exponents();
+      again = true;
     }
-    // ---- P = 2^a: row sums in fp32, fp16 to shared memory ----
+    if (!ok) break;
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive(bar_s_empty(gm.sBar, x));               // S is in registers: the next product may overwrite it
-#pragma unroll
-    for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
-    // P V of this warpgroup's last tile has read the buffer
-    ok = __all_sync(0xffffffffu, mbar_wait(bar_p_empty(gm.sBar, x), ph ^ 1u, abort_flag, p.status)) && ok;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const float* v = a + i * 8;
-      sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
-             pack_f16(v[6], v[7]));
-    }
-    fence_proxy_async();
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar_p_full(gm.sBar, x));
+    if (lane == 0) { mbar_arrive(bar_p_full(sBar, x)); mbar_arrive(bar_s_empty(sBar, x)); }
 #pragma unroll
     for (int e = 0; e < NC; e += 2) ffma2(l[e], l[e + 1], a[e], a[e + 1], iv, iv, l[e], l[e + 1]);
+    factors(sk, sv);
+    scales(j + 4, sk, sv);
   }
   // all products done (each warpgroup waits for both buffers: the last two tiles)
-  for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) mbar_wait(bar_p_empty(gm.sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag, p.status);
+  for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) wait_bar(bar_p_empty(sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag);
   tc_fence_after();
   // ---- row sums over this warp's 32 keys: lane i of a warp ends with row i of a group ----
   named_sync(1 + x, 128);                                              // the column maxima in ms.red have been read
@@ -418,65 +452,69 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 
   // ---- which row tile and which key tiles.  How many rows there are is known on the device only, so the split of the
   // grid is chosen here: the row tiles that hold rows share all CTAs, at least two key tiles per split ----
-  const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
-  const int n_mt = (nrows * p.hpg + QN - 1) / QN, base = n_mt * p.Hkv;
-  const int n_splits = max(1, min(min(p.sms / max(base, 1), p.max_tiles >> 1), MAX_SPLITS));   // > 1: at most sms CTAs in all
-  const int tile = (int)blockIdx.x / n_splits, split = (int)blockIdx.x - tile * n_splits;
-  const int g = min(tile / max(n_mt, 1), p.Hkv - 1), mt = tile - g * n_mt;
-  const int cta = (int)blockIdx.x;
-  const int rows = tile < base ? min(QN, nrows * p.hpg - mt * QN) : 0;   // stacked (row, head of the group) rows of this CTA
-  const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
-  const TileEnum te = make_enum(p, g, cnt_raw);
-  const int t0 = split_lo(te.total, split, n_splits), nt = split_lo(te.total, split + 1, n_splits) - t0;
-  const bool work = rows > 0 && nt > 0;
-  const int N = rows > 0 ? (rows + 15) & ~15 : 16;                   // columns of S^T and O^T
-  Geo gm;
-  gm.g = g; gm.t0 = t0; gm.te = te; gm.nt = nt; gm.N = N; gm.sP = sP; gm.sBar = sBar; gm.cs = 0.f;
-  const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);   // sink tiles of this split
-  gm.stok_first = (st_lo - te.n_blk) * TN;
-  gm.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
-
-  // one K or V tile of the cache into its ring slot (all lanes of the producer warp)
-  auto issue_tma = [&](const TileInfo& ti, int kv, int slot, uint64_t pol) {
+  const Geo& gm = ms.geo;
+  if (warp == 0) {
+    const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
+    const int n_mt = (nrows * p.hpg + QN - 1) / QN, base = n_mt * p.Hkv;
+    const int n_splits = max(1, min(min(p.sms / max(base, 1), p.max_tiles >> 1), MAX_SPLITS));   // > 1: at most sms CTAs in all
+    const int tile = (int)blockIdx.x / n_splits, split = (int)blockIdx.x - tile * n_splits;
+    const int g = min(tile / max(n_mt, 1), p.Hkv - 1), mt = tile - g * n_mt;
+    const int rows = tile < base ? max(min(QN, nrows * p.hpg - mt * QN), 0) : 0;   // stacked (row, head of the group) rows
+    const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
+    const TileEnum te = make_enum(p, g, cnt_raw);
+    const int t0 = split_lo(te.total, split, n_splits), nt = split_lo(te.total, split + 1, n_splits) - t0;
+    const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);            // sink tiles of this split
+    if (lane == 0) {
+      Geo q;
+      q.g = g; q.t0 = t0; q.nt = nt; q.rows = rows; q.N = rows > 0 ? (rows + 15) & ~15 : 16;
+      q.mt = mt; q.tile = tile; q.n_splits = n_splits; q.n_mt = n_mt;
+      q.stok_first = (st_lo - te.n_blk) * TN;
+      q.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
+      q.te = te;
+      ms.geo = q;
+    }
+    __syncwarp();
+  }
+  // one K or V tile of the cache into its ring slot (lane 0 of the producer warp)
+  auto issue_tma = [&](const TileInfo& ti, int g, int kv, int slot, uint64_t pol) {
     const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot);
     const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
-    if (lane == 0) {
-      const CUtensorMap* map = kv ? &tmV : &tmK;
-      mbar_expect_tx(full, TN * D);
-      tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
-      if (p.pair) tma_load_3d_hint(dst + 64 * D, map, full, 0, ti.start2, g, pol);
-    } else {
-      mbar_arrive(full);
-    }
+    const CUtensorMap* map = kv ? &tmV : &tmK;
+    mbar_expect_tx(full, TN * D);
+    tma_load_3d_hint(dst, map, full, 0, ti.start, g, pol);
+    if (p.pair) tma_load_3d_hint(dst + 64 * D, map, full, 0, ti.start2, g, pol);
+    mbar_arrive_n(full, 31);                                           // the barrier counts 32 lanes (sink tiles need them)
   };
-  // K/V tiles are read once, or once per row tile of their head (through L2)
-  const uint64_t pol = n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
   // a dense key set is known without reading anything: its first copies start here, ahead of everything else
-  const int n_early = p.dense && work ? min(nt, RING) : 0;
-  if (warp == 0) {
-    __syncwarp();
-    for (int j = 0; j < n_early; ++j)
-      for (int kv = 0; kv < 2; ++kv) issue_tma(make_tile(p, gm, j), kv, j, pol);
-  }
-  if (!p.dense && warp == 4 && nt <= MAXT) {                         // tile descriptors
-    for (int t = lane; t < nt; t += 32) ms.tlist[t] = pack_tile(make_tile(p, gm, t));
-  }
-  if (warp >= 12) {                                                  // sink tokens
-    for (int i = (int)threadIdx.x - 384; i < gm.stok_n; i += 256) {
-      const int s = gm.stok_first + i;
-      ms.stok[i] = s < p.n_sink ? sink_token(p, g, s) : -1;
-    }
+  if (warp == 0 && lane == 0 && p.dense && gm.rows > 0) {
+    // K/V tiles are read once, or once per row tile of their head (through L2)
+    const uint64_t pol = gm.n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+    const int n = min(gm.nt, RING), g = gm.g;
+    for (int j = 0; j < n; ++j)
+      for (int kv = 0; kv < 2; ++kv) issue_tma(make_tile(p, gm, j), g, kv, j, pol);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = ms.tmem;
-  gm.tmem = tmem;
+  if (!p.dense) {                                                      // tile descriptors and sink tokens
+    if (warp == 4 && gm.nt <= MAXT)
+      for (int t = lane; t < gm.nt; t += 32) ms.tlist[t] = pack_tile(make_tile(p, gm, t));
+    if (warp >= 12)
+      for (int i = (int)threadIdx.x - 384; i < gm.stok_n; i += 256) {
+        const int s = gm.stok_first + i;
+        ms.stok[i] = s < p.n_sink ? sink_token(p, gm.g, s) : -1;
+      }
+    __syncthreads();
+  }
 
   if (wg == 0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp == 0 && work) {
+    const int nt = gm.rows > 0 ? gm.nt : 0;
+    const uint32_t tmem = ms.tmem;
+    if (warp == 0) {
       // ================================ producer ==================================================
+      const int g = gm.g, n_early = p.dense ? min(nt, RING) : 0;
+      const uint64_t pol = gm.n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
       bool ok = true;
       int slot = n_early == RING ? 0 : n_early, issued = 2 * n_early;
       uint32_t round = n_early == RING ? 1u : 0u;
@@ -487,13 +525,13 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         for (int kv = 0; kv < 2; ++kv) {
           const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot);
           const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
-          ok = mbar_wait(kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot), (round & 1u) ^ 1u, abort_flag, p.status);
+          ok = wait_bar(kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot), (round & 1u) ^ 1u, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           ++issued;
           if (ti.kind == 0) {
             fence_proxy_async();                                       // the slot may have been filled with plain copies before
-            issue_tma(ti, kv, slot, pol);
+            if (lane == 0) issue_tma(ti, g, kv, slot, pol);
           } else {
             // sink tokens lie anywhere: 16-byte copies, dropped ones as zeros
             constexpr int CPR = D / 16;
@@ -533,16 +571,16 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           }
         }
       }
-    } else if (warp == 1 && lane == 0 && work) {
+    } else if (warp == 1 && lane == 0 && nt > 0) {
       // ================================ S^T = K Q^T ===============================================
-      const uint32_t id = idesc_f16(N, 0);
+      const uint32_t id = idesc_f16(gm.N, 0);
       const uint64_t qdesc = make_sdesc(sQ, 16, 1024);
-      if (mbar_wait(bar_q_full(sBar), 0u, abort_flag, p.status))
+      if (wait_bar(bar_q_full(sBar), 0u, abort_flag))
         for (int j = 0; j < nt; ++j) {
           const int b = j & 1;
           const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-          if (!mbar_wait(bar_kop_full(sBar, b), ph, abort_flag, p.status)) break;
-          if (!mbar_wait(bar_s_empty(sBar, b), ph ^ 1u, abort_flag, p.status)) break;
+          if (!wait_bar(bar_kop_full(sBar, b), ph, abort_flag)) break;
+          if (!wait_bar(bar_s_empty(sBar, b), ph ^ 1u, abort_flag)) break;
           tc_fence_after();
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
@@ -551,14 +589,14 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           tc_commit(bar_kop_empty(sBar, b));
           tc_commit(bar_s_full(sBar, b));
         }
-    } else if (warp == 3 && lane == 0 && work) {
+    } else if (warp == 3 && lane == 0 && nt > 0) {
       // ================================ O^T += V^T P^T ============================================
-      const uint32_t id = idesc_f16(N, 1);
+      const uint32_t id = idesc_f16(gm.N, 1);
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-        if (!mbar_wait(bar_vop_full(sBar, b), ph, abort_flag, p.status)) break;
-        if (!mbar_wait(bar_p_full(sBar, b), ph, abort_flag, p.status)) break;
+        if (!wait_bar(bar_vop_full(sBar, b), ph, abort_flag)) break;
+        if (!wait_bar(bar_p_full(sBar, b), ph, abort_flag)) break;
         tc_fence_after();
         const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
 #pragma unroll
@@ -573,22 +611,25 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     asm volatile("bar.sync 0;" ::: "memory");
     tc_fence_after();
     if (warp == 2) { __syncwarp(); tmem_dealloc(tmem, 512); }
+    if (threadIdx.x == 96 && ms.abort_flag) set_status(p.status, FOCUS_ERR_TIMEOUT);
   } else if (wg == 1) {
     // ================================ K codes -> A operand of S^T =====================================
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (work) {
+    const int nt = gm.rows > 0 ? gm.nt : 0;
+    const uint32_t tmem = ms.tmem;
+    if (nt > 0) {
       const int key = (warp & 3) * 32 + lane;
       const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
       int slot = 0;
       uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
-        const bool ok = mbar_wait(bar_k_full(sBar, slot), round & 1u, abort_flag, p.status) &&
-                        mbar_wait(bar_kop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status);
+        const bool ok = wait_bar(bar_k_full(sBar, slot), round & 1u, abort_flag) &&
+                        wait_bar(bar_kop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawK + slot * SLOT, dst = tmem + (uint32_t)(T_K + b * 64) + lane_off;
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < D / 64; ++h) {
           uint32_t o[32];
           uint4 raw[4];
@@ -615,7 +656,9 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   } else if (wg == 2) {
     // ================================ V codes, transposed -> A operand of O^T ===========================
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (work) {
+    const int nt = gm.rows > 0 ? gm.nt : 0;
+    const uint32_t tmem = ms.tmem;
+    if (nt > 0) {
       const int cw = warp & 3;                                         // channels 32 cw .. 32 cw + 31
       if (cw * 32 >= D) {                                              // head dim 64: the upper lanes stay zero
         uint32_t z[32];
@@ -629,29 +672,27 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
-        const bool ok = mbar_wait(bar_v_full(sBar, slot), round & 1u, abort_flag, p.status) &&
-                        mbar_wait(bar_vop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag, p.status);
+        const bool ok = wait_bar(bar_v_full(sBar, slot), round & 1u, abort_flag) &&
+                        wait_bar(bar_vop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawV + slot * SLOT, dst = tmem + (uint32_t)(T_V + b * 64) + ((uint32_t)(cw * 32) << 16);
         if (cw * 32 < D) {
+#pragma unroll 1
+          for (int it = 0; it < 4; ++it) {                             // sixteen channels x 64 keys: four 16-key matrices
+            const int hc = it >> 1, q = it & 1;
+            uint32_t o[16];
 #pragma unroll
-          for (int hc = 0; hc < 2; ++hc) {                             // sixteen channels
+            for (int pr = 0; pr < 2; ++pr) {
+              uint32_t m[4];
+              ldsm_t8(src + raw_off<D>(q * 64 + pr * 32 + lane, cw * 2 + hc), m);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {                              // 64 keys = four 16-key matrices
-              uint32_t o[16];
-#pragma unroll
-              for (int pr = 0; pr < 2; ++pr) {
-                uint32_t m[4];
-                ldsm_t8(src + raw_off<D>(q * 64 + pr * 32 + lane, cw * 2 + hc), m);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  expand(m[2 * i], o[(2 * pr + i) * 4 + 0], o[(2 * pr + i) * 4 + 1], F());
-                  expand(m[2 * i + 1], o[(2 * pr + i) * 4 + 2], o[(2 * pr + i) * 4 + 3], F());
-                }
+              for (int i = 0; i < 2; ++i) {
+                expand(m[2 * i], o[(2 * pr + i) * 4 + 0], o[(2 * pr + i) * 4 + 1], F());
+                expand(m[2 * i + 1], o[(2 * pr + i) * 4 + 2], o[(2 * pr + i) * 4 + 3], F());
               }
-              TC_ST_FRAG16(dst + ((uint32_t)(hc * 16) << 16) + q * 32, o);
             }
+            TC_ST_FRAG16(dst + ((uint32_t)(hc * 16) << 16) + q * 32, o);
           }
         }
         tc_wait_st();
@@ -667,6 +708,10 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // ================================ softmax =========================================================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane, tid = (int)threadIdx.x - 384;
+    const int rows = gm.rows, N = gm.N, n_splits = gm.n_splits, g = gm.g;
+    const bool work = rows > 0 && gm.nt > 0;
+    const uint32_t tmem = ms.tmem;
+    float cs = 0.f;
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
     if (rows > 0) {
       // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
@@ -677,7 +722,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       unsigned m = 0u;
       int orow = -1;
       if (qrow < rows) {
-        const int fr = mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
+        const int fr = gm.mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
         const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
         if (pos >= p.q_base && pos < p.q_base + p.n_q) {
           orow = qr * p.H + g * p.hpg + hh;
@@ -708,7 +753,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       // the power of two: the tile's largest |q| to 2^14 .. 2^15
       const int sh = ms.qmax ? min(14 - ((int)(ms.qmax >> 7) - 127), 126) : 0;
       const float f = exp2f((float)sh);
-      gm.cs = p.scale_log2 * exp2f((float)-sh);
+      cs = p.scale_log2 * exp2f((float)-sh);
       if (quarter * 32 < D) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -726,10 +771,10 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       if (lane == 0) mbar_arrive(bar_q_full(sBar));
     }
     if (work) {
-      if (N == 16) softmax_loop<2>(p, ms, gm, x, wq, lane);
-      else if (N == 32) softmax_loop<4>(p, ms, gm, x, wq, lane);
-      else if (N == 48) softmax_loop<6>(p, ms, gm, x, wq, lane);
-      else softmax_loop<8>(p, ms, gm, x, wq, lane);
+      if (N == 16) softmax_loop<2>(p, ms, sP, sBar, cs, x, wq, lane);
+      else if (N == 32) softmax_loop<4>(p, ms, sP, sBar, cs, x, wq, lane);
+      else if (N == 48) softmax_loop<6>(p, ms, sP, sBar, cs, x, wq, lane);
+      else softmax_loop<8>(p, ms, sP, sBar, cs, x, wq, lane);
     }
     named_sync(3, 256);
     // ---- row statistics: sums of the warps in order, the two warpgroups' shares of a row joined ----
@@ -745,7 +790,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tot = w0 * l0 + w1 * l1;
       }
       if (n_splits > 1) {
-        reinterpret_cast<float2*>(p.part_ml)[(size_t)cta * QN + r] = make_float2(ref, tot);
+        reinterpret_cast<float2*>(p.part_ml)[(size_t)blockIdx.x * QN + r] = make_float2(ref, tot);
       } else {
         const float inv = tot != 0.f ? 1.f / tot : 0.f;
         w0 *= inv; w1 *= inv;
@@ -777,7 +822,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       }
       if (ch < D) {
         if (n_splits > 1) {
-          float* dst = p.part_O + ((size_t)cta * QN + r0) * D + ch;
+          float* dst = p.part_O + ((size_t)blockIdx.x * QN + r0) * D + ch;
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (r0 + e < rows) dst[e * D] = v[e];
@@ -798,15 +843,15 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       __threadfence();
       named_sync(3, 256);
       if (tid == 0) {
-        const int prev = atomicAdd(&p.counters[tile], 1);
+        const int prev = atomicAdd(&p.counters[gm.tile], 1);
         ms.last = prev == S - 1;
-        if (ms.last) p.counters[tile] = 0;                       // armed for the next launch
+        if (ms.last) p.counters[gm.tile] = 0;                       // armed for the next launch
         __threadfence();
       }
       named_sync(3, 256);
       if (ms.last) {
         float* wts = reinterpret_cast<float*>(sptr + Q_BYTES);         // [row][split], over the P tiles
-        const size_t c_first = (size_t)tile * S;
+        const size_t c_first = (size_t)gm.tile * S;
         if (tid < rows) {
           const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + c_first * QN + tid;
           float m = -INFINITY, tot = 0.f;
