@@ -9,7 +9,7 @@
 // takes P_rj / sv_j.  ref_r follows the running maximum of a_rj lazily, so P fits fp16 (below).
 // Codes enter the products as they are: every int8 and every e4m3 value is an fp16 value.  q enters as fp16 too, scaled
 // by a power of two that puts the tile's largest |q| at 2^14..2^15: bf16 has fewer fraction bits, so only elements
-// 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-12, absolute 2^-31 of the row's
+// 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-12, absolute 2^-27 of the row's
 // largest), which is the one rounding between the cache and the output; sums are fp32.
 //
 // Work split.  CTA = up to 64 stacked query rows of one KV head (the rows of a group's query heads share its K/V) x one
@@ -43,6 +43,7 @@ namespace {
 constexpr int QN = 64;                         // most query rows per CTA
 constexpr int NTH = 640;
 constexpr int RING = 5;                        // raw slots per ring (K, V)
+constexpr int EARLY = 2;                       // tiles of a dense key set requested ahead of everything else (< RING)
 constexpr int SLOT = TN * 128;                 // bytes of a raw tile (head dim 64 fills half)
 constexpr int Q_BYTES = QN * 128 * 2;
 constexpr int P_BYTES = TN * QN * 2;           // P^T of one tile: [key][row]
@@ -53,7 +54,7 @@ constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
 constexpr int MAX_SPLITS = 64;
 constexpr float P_MAX = 46340.f;               // the reference follows the maximum once a numerator exceeds 2^15.5 (fp16 ends at 65504) ...
-constexpr float OFFSET = 6.f;                  // ... and is put 6 (log2) below it: P is normal fp16 down to 2^-20 of the row's largest
+constexpr float OFFSET = 2.f;                  // ... and is put 2 (log2) below it: P is normal fp16 down to 2^-16 of the row's largest
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
 constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
                                                     // rows hold zeros, the writer flushes them)
@@ -100,7 +101,7 @@ struct Misc {                                  // behind the tiles in shared mem
   int stok[MAX_STOK * TN];                     // tokens of the sink tiles, -1: dropped
   uint32_t tmem;
   int abort_flag, last;
-  unsigned qmax;
+  unsigned qmax, pieces[2];                    // largest |q| (bf16 bits); row pieces a warpgroup has to re-reference
   Geo geo;
 };
 constexpr int SMEM = 1024 + OFF_MISC + (int)sizeof(Misc);
@@ -143,6 +144,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+// normal numbers only
+__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 // maximum over the warp of one float per lane (NaN is passed over)
 __device__ __forceinline__ float warp_max_f32(float x) {
   float m;
@@ -298,8 +302,8 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
     const bool masked = sv == -1.f;
     const float svc = fmaxf(sv, SV_MIN);
     ck = sk * cs;
-    lv = masked ? -INFINITY : __log2f(svc);
-    iv = masked ? 0.f : __fdividef(1.f, svc);
+    lv = masked ? -INFINITY : lg2(svc);
+    iv = masked ? 0.f : rcp(svc);
   };
   float sk, sv;                                                        // the next tile's scales, on their way
   scales(x, sk, sv);
@@ -308,9 +312,7 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
   bool ok = true;
   for (int j = x; j < nt; j += 2) {
     const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-    ok = wait_bar(bar_s_full(sBar, x), ph, abort_flag);
-    // P V of this warpgroup's last tile has read the buffer (long ago, as a rule)
-    ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
+    ok = __all_sync(0xffffffffu, wait_bar(bar_s_full(sBar, x), ph, abort_flag));
     tc_fence_after();
     float a[NC];
     uint32_t* ar = reinterpret_cast<uint32_t*>(a);
@@ -332,6 +334,8 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
       }
 #pragma unroll
       for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
+      // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
+      ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
       float m0 = 0.f, m1 = 0.f;
 #pragma unroll
       for (int e = 0; e < NC; e += 4) {
@@ -349,10 +353,21 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
       // and here it is the one that hands the tile over anyway.
       if (!named_any(1 + x, 128, (fmaxf(m0, m1) > P_MAX && !again) || !ok)) break;
       if (named_any(1 + x, 128, !ok)) { again = true; ok = false; break; }
-      // ---- some row's maximum outgrew its reference (always so at the first key): new references, once more.  Rolled
-      // loops: code that runs this seldom is fetched from L2 each time ----
+      // ---- some row's maximum outgrew its reference (always so at the first key): new references for the pieces it is
+      // in, and the tile once more.  Rolled loops: code that runs this seldom is fetched from L2 each time ----
+      unsigned pieces = 0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const float* v = a + i * 8;
+        if (fmaxf(fmax3(fmax3(v[0], v[1], v[2]), v[3], v[4]), fmax3(v[5], v[6], v[7])) > P_MAX) pieces |= 1u << i;
+      }
+      pieces = __reduce_or_sync(0xffffffffu, pieces);
+      if (lane == 0 && pieces) atomicOr(&ms.pieces[x], pieces);
+      named_sync(1 + x, 128);
+      pieces = ms.pieces[x];
 #pragma unroll 1
       for (int i = 0; i < NP; ++i) {
+        if (!(pieces >> i & 1u)) continue;
         uint32_t v[8];
         TC_LD8(ts + i * 8, v);
         tc_wait_ld();
@@ -366,17 +381,22 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
       }
       named_sync(1 + x, 128);
       if (key < NC) {
-        const float(*r)[QN] = &ms.red[x * 4];
-        const float rowmax = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
-        const float old = nref[key], now = OFFSET - rowmax;
-        const bool up = now < old;
-        fac[key] = up ? ex2(now - old) : 1.f;
-        if (up) nref[key] = now;
+        float f = 1.f;
+        if (pieces >> (key >> 3) & 1u) {
+          const float(*r)[QN] = &ms.red[x * 4];
+          const float rowmax = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
+          const float old = nref[key], now = OFFSET - rowmax;
+          if (now < old) { f = ex2(now - old); nref[key] = now; }
+        }
+        fac[key] = f;
+        if (key == 0) ms.pieces[x] = 0u;
       }
       named_sync(1 + x, 128);
       if (j >= 2) {                                                    // what these rows have summed: P V of tile j - 2 is done
+        tc_fence_after();
 #pragma unroll 1
         for (int i = 0; i < NP; ++i) {
+          if (!(pieces >> i & 1u)) continue;
           uint32_t v[8];
           TC_LD8(tO + i * 8, v);
           tc_wait_ld();
@@ -442,7 +462,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       mbar_init(bar_s_empty(sBar, b), 4); mbar_init(bar_p_full(sBar, b), 4);       // one softmax warpgroup's warps
     }
     mbar_init(bar_q_full(sBar), 8);                                    // eight softmax warps
-    ms.abort_flag = 0; ms.qmax = 0u;
+    ms.abort_flag = 0; ms.qmax = 0u; ms.pieces[0] = ms.pieces[1] = 0u;
     fence_barrier_init();
     fence_proxy_async();
   }
@@ -489,7 +509,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (warp == 0 && lane == 0 && p.dense && gm.rows > 0) {
     // K/V tiles are read once, or once per row tile of their head (through L2)
     const uint64_t pol = gm.n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-    const int n = min(gm.nt, RING), g = gm.g;
+    const int n = min(gm.nt, EARLY), g = gm.g;
     for (int j = 0; j < n; ++j)
       for (int kv = 0; kv < 2; ++kv) issue_tma(make_tile(p, gm, j), g, kv, j, pol);
   }
@@ -513,11 +533,14 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const uint32_t tmem = ms.tmem;
     if (warp == 0) {
       // ================================ producer ==================================================
-      const int g = gm.g, n_early = p.dense ? min(nt, RING) : 0;
+      const int g = gm.g, n_early = p.dense ? min(nt, EARLY) : 0;
       const uint64_t pol = gm.n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
       bool ok = true;
-      int slot = n_early == RING ? 0 : n_early, issued = 2 * n_early;
-      uint32_t round = n_early == RING ? 1u : 0u;
+      int slot = n_early, issued = 2 * n_early;
+      uint32_t round = 0;
+      // All CTAs start together: with whole rings requested at once the first tile -- and the queries -- would wait behind
+      // everybody's fifth.  The rest follows once the first tile's keys have landed.
+      if (n_early > 0 && nt > n_early) ok = wait_bar(bar_k_full(sBar, 0), 0u, abort_flag);
       for (int j = n_early; j < nt && ok; ++j) {
         const TileInfo ti = get_tile(p, ms, gm, j);
         if (ti.nvalid == 0 && lane == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
@@ -678,7 +701,7 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         tc_fence_after();
         const uint32_t src = sRawV + slot * SLOT, dst = tmem + (uint32_t)(T_V + b * 64) + ((uint32_t)(cw * 32) << 16);
         if (cw * 32 < D) {
-#pragma unroll 1
+#pragma unroll 2
           for (int it = 0; it < 4; ++it) {                             // sixteen channels x 64 keys: four 16-key matrices
             const int hc = it >> 1, q = it & 1;
             uint32_t o[16];

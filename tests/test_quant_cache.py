@@ -247,9 +247,9 @@ def _bounds(Q, K, V, vs, O, scale, hpg, dtype, keys=None):
     adds 2^-24 max|q| sum|k|.  Every numerator is then off by a factor 1 + E + 2^-21 (exp2), the ones that meet V by
     another 2^-11 (fp16), sums over the n keys by n 2^-24, and the output is rounded once (bf16: 2^-8).
 
-    fp16 also has a smallest step.  A numerator that meets V is p_j sv_j in units that put the row's largest at 2^6 or
-    more, and fp16 numbers below 2^-14 are 2^-24 apart: off by at most 2^-25, i.e. 2^-31 of the row's largest p_j sv_j.
-    The codes weigh those errors, so a channel is off by at most 2^-31 max_j(p_j sv_j) sum_j |cv_j| more (it shows where
+    fp16 also has a smallest step.  A numerator that meets V is p_j sv_j in units that put the row's largest at 2^2 or
+    more, and fp16 numbers below 2^-14 are 2^-24 apart: off by at most 2^-25, i.e. 2^-27 of the row's largest p_j sv_j.
+    The codes weigh those errors, so a channel is off by at most 2^-27 max_j(p_j sv_j) sum_j |cv_j| more (it shows where
     the token that holds nearly all the weight has code 0 in that channel)."""
     n, H, d = Q.shape
     tolO, tolL = np.zeros_like(O), np.zeros((H, n))
@@ -268,7 +268,7 @@ def _bounds(Q, K, V, vs, O, scale, hpg, dtype, keys=None):
         per = num * 2 + (2.0 ** -11 if dtype == "bf16" else 0.0)
         sv = vs[g] if keys is None else vs[g][keys[g]]
         codes = np.abs(np.divide(Vg, sv[:, None], out=np.zeros_like(Vg), where=sv[:, None] > 0)).sum(0)
-        step = 2.0 ** -31 * (p * sv).max(1)[:, None] * codes if dtype == "bf16" else 0.0
+        step = 2.0 ** -27 * (p * sv).max(1)[:, None] * codes if dtype == "bf16" else 0.0
         tolO[:, h] = step + per[:, None] * A + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * np.abs(O[:, h]) + 1e-30
         tolL[h] = num + 2.0 ** -22 * (1 + np.abs(np.log(np.exp(s - s.max(1, keepdims=True)).sum(1)) + s.max(1)))
     return tolO, tolL
