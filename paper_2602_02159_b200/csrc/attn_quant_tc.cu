@@ -18,9 +18,8 @@
 // is meant to be bound by the bytes of the cache.  The splits of a row tile are joined by the CTA that finishes last.
 //
 // Warp roles (640 threads):
-//   warp 0        producer: K and V tiles as raw codes into two rings (TMA; sink tokens one by one with cp.async)
+//   warps 0, 2    producers: K and V tiles as raw codes into two rings (TMA; sink tokens one by one with cp.async)
 //   warps 1, 3    tcgen05.mma issuers, one per product: neither has to wait for what only the other needs
-//   warp 2        TMEM allocation
 //   warps 4..7    K codes -> fp16 in TMEM (lane = key): the A operand of S^T
 //   warps 8..11   V codes -> fp16 in TMEM (lane = channel; ldmatrix transposes the bytes): the A operand of O^T
 //   warps 12..19  softmax: two warpgroups that take the key tiles in turn, with references, row sums and an O^T of their
@@ -531,53 +530,53 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int nt = gm.rows > 0 ? gm.nt : 0;
     const uint32_t tmem = ms.tmem;
-    if (warp == 0) {
-      // ================================ producer ==================================================
-      const int g = gm.g, n_early = p.dense ? min(nt, EARLY) : 0;
+    if ((warp & 1) == 0) {
+      // ================================ producers: warp 0 K, warp 2 V ==============================
+      const int kv = warp >> 1, g = gm.g, n_early = p.dense ? min(nt, EARLY) : 0;
       const uint64_t pol = gm.n_mt == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-      bool ok = true;
-      int slot = n_early, issued = 2 * n_early;
+      const uint32_t full0 = kv ? bar_v_full(sBar, 0) : bar_k_full(sBar, 0), empty0 = kv ? bar_v_empty(sBar, 0) : bar_k_empty(sBar, 0);
+      bool ok = true, plain = false;                                   // plain: a slot may hold copies of the other kind
+      int slot = n_early, issued = n_early;
       uint32_t round = 0;
       // All CTAs start together: with whole rings requested at once the first tile -- and the queries -- would wait behind
       // everybody's fifth.  The rest follows once the first tile's keys have landed.
-      if (n_early > 0 && nt > n_early) ok = wait_bar(bar_k_full(sBar, 0), 0u, abort_flag);
+      if (n_early > 0 && nt > n_early) ok = __all_sync(0xffffffffu, wait_bar(bar_k_full(sBar, 0), 0u, abort_flag));
       for (int j = n_early; j < nt && ok; ++j) {
         const TileInfo ti = get_tile(p, ms, gm, j);
-        if (ti.nvalid == 0 && lane == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
-#pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t full = kv ? bar_v_full(sBar, slot) : bar_k_full(sBar, slot);
+        ok = __all_sync(0xffffffffu, wait_bar(empty0 + 8u * slot, (round & 1u) ^ 1u, abort_flag));
+        if (!ok) break;
+        ++issued;
+        if (ti.kind == 0) {
+          if (lane == 0) {
+            if (ti.nvalid == 0) set_status(p.status, FOCUS_ERR_INVALID_ARG);   // bad block index
+            if (plain) fence_proxy_async();
+            issue_tma(ti, g, kv, slot, pol);
+          }
+          __syncwarp();
+        } else {
+          // sink tokens lie anywhere: 16-byte copies, dropped ones as zeros
+          constexpr int CPR = D / 16;
           const uint32_t dst = (kv ? sRawV : sRawK) + slot * SLOT;
-          ok = wait_bar(kv ? bar_v_empty(sBar, slot) : bar_k_empty(sBar, slot), (round & 1u) ^ 1u, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          ++issued;
-          if (ti.kind == 0) {
-            fence_proxy_async();                                       // the slot may have been filled with plain copies before
-            if (lane == 0) issue_tma(ti, g, kv, slot, pol);
-          } else {
-            // sink tokens lie anywhere: 16-byte copies, dropped ones as zeros
-            constexpr int CPR = D / 16;
-            const uint8_t* base = (kv ? p.V : p.K) + (long long)g * p.kv_stride_head;
+          const uint8_t* base = (kv ? p.V : p.K) + (long long)g * p.kv_stride_head;
+          plain = true;
 #pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-              const int tok = key_token(p, ms, gm, ti, i * 32 + lane);
+          for (int i = 0; i < 4; ++i) {
+            const int tok = key_token(p, ms, gm, ti, i * 32 + lane);
 #pragma unroll
-              for (int it = 0; it < CPR; ++it) {
-                const int q = it * 32 + lane, rr = q / CPR, c = q % CPR;      // row within this group of 32, chunk
-                const int t = __shfl_sync(0xffffffffu, tok, rr);
-                const uint8_t* src = base + (long long)max(t, 0) * p.kv_stride_tok + c * 16;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                             ::"r"(dst + raw_off<D>(i * 32 + rr, c)), "l"(src), "r"(t >= 0 ? 16u : 0u) : "memory");
-              }
+            for (int it = 0; it < CPR; ++it) {
+              const int q = it * 32 + lane, rr = q / CPR, c = q % CPR;        // row within this group of 32, chunk
+              const int t = __shfl_sync(0xffffffffu, tok, rr);
+              const uint8_t* src = base + (long long)max(t, 0) * p.kv_stride_tok + c * 16;
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                           ::"r"(dst + raw_off<D>(i * 32 + rr, c)), "l"(src), "r"(t >= 0 ? 16u : 0u) : "memory");
             }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
-            if (kv == 0) {
+          }
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full0 + 8u * slot) : "memory");
+          if (kv == 0) {
 #pragma unroll 1
-              for (int k = lane; k < ti.nvalid; k += 32) {             // a listed sink outside [0, L) is reported
-                const int s = __ldg(p.sink_idx + ti.start + k);
-                if (s < 0 || s >= p.L) set_status(p.status, FOCUS_ERR_INVALID_ARG);
-              }
+            for (int k = lane; k < ti.nvalid; k += 32) {               // a listed sink outside [0, L) is reported
+              const int s = __ldg(p.sink_idx + ti.start + k);
+              if (s < 0 || s >= p.L) set_status(p.status, FOCUS_ERR_INVALID_ARG);
             }
           }
         }
@@ -586,10 +585,9 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       asm volatile("cp.async.wait_all;" ::: "memory");
       if (!ok) {
         // unwinding: let the copies already issued land before the CTA's shared memory is released
-        for (int q = max(0, issued - 2 * RING); q < issued; ++q) {
-          const int i = q >> 1, sl = i % RING;
+        for (int i = max(0, issued - RING); i < issued; ++i) {
           const uint64_t t_start = global_ns();
-          while (!mbar_try_wait(q & 1 ? bar_v_full(sBar, sl) : bar_k_full(sBar, sl), (uint32_t)(i / RING) & 1u)) {
+          while (!mbar_try_wait(full0 + 8u * (i % RING), (uint32_t)(i / RING) & 1u)) {
             if (global_ns() - t_start > WAIT_LIMIT_NS) break;
           }
         }
