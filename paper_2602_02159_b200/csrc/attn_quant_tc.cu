@@ -51,7 +51,7 @@ constexpr int T_S = 0, T_O = 128, T_K = 256, T_V = 384;
 constexpr int MAXT = 256;                      // key tiles of a split whose descriptors are staged
 constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
-constexpr int MAX_SPLITS = 64;
+constexpr int MAX_SPLITS = 32;
 constexpr float P_MAX = 46340.f;               // the reference follows the maximum once a numerator exceeds 2^15.5 (fp16 ends at 65504) ...
 constexpr float OFFSET = 2.f;                  // ... and is put 2 (log2) below it: P is normal fp16 down to 2^-16 of the row's largest
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
@@ -316,54 +316,57 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
     float a[NC];
     uint32_t* ar = reinterpret_cast<uint32_t*>(a);
     bool again = false;
+    unsigned pieces = (1u << NP) - 1u;
 #pragma unroll 1
     for (;;) {
-      // ---- P = 2^(s ck + lv - ref), to shared memory as fp16 ----
+      if (j >= 2 || again) {
+        // ---- P = 2^(s ck + lv - ref), to shared memory as fp16 ----
 #pragma unroll
-      for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
-      tc_wait_ld();
+        for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
+        tc_wait_ld();
 #pragma unroll
-      for (int q = 0; q < NP * 2; ++q) {
-        const float4 rv = reinterpret_cast<const float4*>(nref)[q];
-        float* v = a + q * 4;
-        ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
-        ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
-        fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
-        fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
+        for (int q = 0; q < NP * 2; ++q) {
+          const float4 rv = reinterpret_cast<const float4*>(nref)[q];
+          float* v = a + q * 4;
+          ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
+          ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
+          fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
+          fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
+        }
+#pragma unroll
+        for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
+        // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
+        ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
+        float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < NC; e += 4) {
+          m0 = fmax3(m0, a[e], a[e + 1]);
+          m1 = fmax3(m1, a[e + 2], a[e + 3]);
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const float* v = a + i * 8;
+          sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
+                 pack_f16(v[6], v[7]));
+        }
+        fence_proxy_async();
+        // The numerators are formed before anyone has looked whether they fit: the look costs a barrier of the four warps,
+        // and here it is the one that hands the tile over anyway.
+        if (!named_any(1 + x, 128, (fmaxf(m0, m1) > P_MAX && !again) || !ok)) break;
+        if (named_any(1 + x, 128, !ok)) { ok = false; break; }
+        // ---- some row's maximum outgrew its reference: new references for the pieces it is in, and the tile once more
+        // (the first tile starts here, for all of them).  Rolled loops: code that runs this seldom is fetched from L2 each time ----
+        pieces = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const float* v = a + i * 8;
+          if (fmaxf(fmax3(fmax3(v[0], v[1], v[2]), v[3], v[4]), fmax3(v[5], v[6], v[7])) > P_MAX) pieces |= 1u << i;
+        }
+        pieces = __reduce_or_sync(0xffffffffu, pieces);
+        if (lane == 0 && pieces) atomicOr(&ms.pieces[x], pieces);
+        named_sync(1 + x, 128);
+        pieces = ms.pieces[x];
       }
-#pragma unroll
-      for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
-      // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
-      ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
-      float m0 = 0.f, m1 = 0.f;
-#pragma unroll
-      for (int e = 0; e < NC; e += 4) {
-        m0 = fmax3(m0, a[e], a[e + 1]);
-        m1 = fmax3(m1, a[e + 2], a[e + 3]);
-      }
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const float* v = a + i * 8;
-        sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
-               pack_f16(v[6], v[7]));
-      }
-      fence_proxy_async();
-      // The numerators are formed before anyone has looked whether they fit: the look costs a barrier of the four warps,
-      // and here it is the one that hands the tile over anyway.
-      if (!named_any(1 + x, 128, (fmaxf(m0, m1) > P_MAX && !again) || !ok)) break;
-      if (named_any(1 + x, 128, !ok)) { again = true; ok = false; break; }
-      // ---- some row's maximum outgrew its reference (always so at the first key): new references for the pieces it is
-      // in, and the tile once more.  Rolled loops: code that runs this seldom is fetched from L2 each time ----
-      unsigned pieces = 0;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const float* v = a + i * 8;
-        if (fmaxf(fmax3(fmax3(v[0], v[1], v[2]), v[3], v[4]), fmax3(v[5], v[6], v[7])) > P_MAX) pieces |= 1u << i;
-      }
-      pieces = __reduce_or_sync(0xffffffffu, pieces);
-      if (lane == 0 && pieces) atomicOr(&ms.pieces[x], pieces);
-      named_sync(1 + x, 128);
-      pieces = ms.pieces[x];
 #pragma unroll 1
       for (int i = 0; i < NP; ++i) {
         if (!(pieces >> i & 1u)) continue;
@@ -472,27 +475,50 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   // ---- which row tile and which key tiles.  How many rows there are is known on the device only, so the split of the
   // grid is chosen here: the row tiles that hold rows share all CTAs, at least two key tiles per split ----
   const Geo& gm = ms.geo;
-  if (warp == 0) {
+  uint4 qv[4];                                                         // softmax warps: a quarter (32 elements) of a query row
+  int orow = -1;
+  const int qrow = ((int)threadIdx.x - 384) >> 2, quarter = (int)threadIdx.x & 3;
+  if (warp == 0 || wg >= 3) {                                          // both from the same numbers, neither waiting for the other
     const int nrows = p.q_rows ? min(max(ld_ordered(p.n_rows), 0), p.rows_bound) : p.n_q;
     const int n_mt = (nrows * p.hpg + QN - 1) / QN, base = n_mt * p.Hkv;
     const int n_splits = max(1, min(min(p.sms / max(base, 1), p.max_tiles >> 1), MAX_SPLITS));   // > 1: at most sms CTAs in all
     const int tile = (int)blockIdx.x / n_splits, split = (int)blockIdx.x - tile * n_splits;
     const int g = min(tile / max(n_mt, 1), p.Hkv - 1), mt = tile - g * n_mt;
     const int rows = tile < base ? max(min(QN, nrows * p.hpg - mt * QN), 0) : 0;   // stacked (row, head of the group) rows
-    const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
-    const TileEnum te = make_enum(p, g, cnt_raw);
-    const int t0 = split_lo(te.total, split, n_splits), nt = split_lo(te.total, split + 1, n_splits) - t0;
-    const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);            // sink tiles of this split
-    if (lane == 0) {
-      Geo q;
-      q.g = g; q.t0 = t0; q.nt = nt; q.rows = rows; q.N = rows > 0 ? (rows + 15) & ~15 : 16;
-      q.mt = mt; q.tile = tile; q.n_splits = n_splits; q.n_mt = n_mt;
-      q.stok_first = (st_lo - te.n_blk) * TN;
-      q.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
-      q.te = te;
-      ms.geo = q;
+    if (wg >= 3) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) qv[c] = make_uint4(0, 0, 0, 0);
+      if (qrow < rows) {
+        const int fr = mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
+        const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
+        if (pos >= p.q_base && pos < p.q_base + p.n_q) {
+          orow = qr * p.H + g * p.hpg + hh;
+          if (quarter * 32 < D) {
+            const uint4* src = reinterpret_cast<const uint4*>(p.Q + (long long)(pos - p.q_base) * p.q_stride_row +
+                                                              (long long)(g * p.hpg + hh) * p.q_stride_head + quarter * 32);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) qv[c] = ld_ordered(src + c);
+          }
+        } else if (quarter == 0) {
+          set_status(p.status, FOCUS_ERR_INVALID_ARG);
+        }
+      }
+    } else {
+      const int cnt_raw = p.dense ? 0 : ld_ordered(p.block_cnt + g * p.group_stride);
+      const TileEnum te = make_enum(p, g, cnt_raw);
+      const int t0 = split_lo(te.total, split, n_splits), nt = split_lo(te.total, split + 1, n_splits) - t0;
+      const int st_lo = max(t0, te.n_blk), st_hi = min(t0 + nt, te.n_blk + te.n_sinkt);            // sink tiles of this split
+      if (lane == 0) {
+        Geo q;
+        q.g = g; q.t0 = t0; q.nt = nt; q.rows = rows; q.N = rows > 0 ? (rows + 15) & ~15 : 16;
+        q.mt = mt; q.tile = tile; q.n_splits = n_splits; q.n_mt = n_mt;
+        q.stok_first = (st_lo - te.n_blk) * TN;
+        q.stok_n = p.dense ? 0 : min(max(st_hi - st_lo, 0), MAX_STOK) * TN;
+        q.te = te;
+        ms.geo = q;
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
   // one K or V tile of the cache into its ring slot (lane 0 of the producer warp)
   auto issue_tma = [&](const TileInfo& ti, int g, int kv, int slot, uint64_t pol) {
@@ -729,34 +755,14 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     // ================================ softmax =========================================================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int x = wg - 3, wq = warp & 3, key = wq * 32 + lane, tid = (int)threadIdx.x - 384;
-    const int rows = gm.rows, N = gm.N, n_splits = gm.n_splits, g = gm.g;
+    const int rows = gm.rows, N = gm.N, n_splits = gm.n_splits;
     const bool work = rows > 0 && gm.nt > 0;
     const uint32_t tmem = ms.tmem;
     float cs = 0.f;
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
     if (rows > 0) {
       // ---- queries -> fp16, 128-byte-swizzled K-major tile; one power of two for the whole tile ----
-      const int qrow = tid >> 2, quarter = tid & 3;                    // a quarter (32 elements) of a row per thread
-      uint4 qv[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) qv[c] = make_uint4(0, 0, 0, 0);
       unsigned m = 0u;
-      int orow = -1;
-      if (qrow < rows) {
-        const int fr = gm.mt * QN + qrow, qr = fr / p.hpg, hh = fr - qr * p.hpg;
-        const int pos = p.q_rows ? ld_ordered(p.q_rows + qr) : p.q_base + qr;
-        if (pos >= p.q_base && pos < p.q_base + p.n_q) {
-          orow = qr * p.H + g * p.hpg + hh;
-          if (quarter * 32 < D) {
-            const uint4* src = reinterpret_cast<const uint4*>(p.Q + (long long)(pos - p.q_base) * p.q_stride_row +
-                                                              (long long)(g * p.hpg + hh) * p.q_stride_head + quarter * 32);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) qv[c] = ld_ordered(src + c);
-          }
-        } else if (quarter == 0) {
-          set_status(p.status, FOCUS_ERR_INVALID_ARG);
-        }
-      }
       if (quarter == 0) ms.orow[qrow] = orow;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -876,10 +882,12 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         if (tid < rows) {
           const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + c_first * QN + tid;
           float m = -INFINITY, tot = 0.f;
+#pragma unroll 4
           for (int s = 0; s < S; ++s) {
             const float2 v = __ldcg(ml + (size_t)s * QN);
             if (v.y != 0.f) m = fmaxf(m, v.x);
           }
+#pragma unroll 4
           for (int s = 0; s < S; ++s) {
             const float2 v = __ldcg(ml + (size_t)s * QN);
             const float w = v.y != 0.f ? ex2(v.x - m) : 0.f;
@@ -892,12 +900,13 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
             p.lse[(size_t)(orow % p.H) * p.lse_stride + orow / p.H] = tot == 0.f ? -INFINITY : (m + log2f(tot)) * 0.6931471805599453f;
         }
         named_sync(3, 256);
+#pragma unroll 2
         for (int it = tid; it < rows * (D / 4); it += 256) {
           const int r = it / (D / 4), c4 = it % (D / 4), orow = ms.orow[r];
           if (orow < 0) continue;
           const float4* po = reinterpret_cast<const float4*>(p.part_O) + (c_first * QN + r) * (D / 4) + c4;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
           for (int s = 0; s < S; ++s) {
             const float w = wts[r * S + s];
             const float4 o = __ldcg(po + (size_t)s * QN * (D / 4));
