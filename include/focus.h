@@ -338,7 +338,7 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
  * beyond n_rows get token -1, conf 0, prob 0, n_kept 0; so does a row without a finite or +inf logit, and a row whose
  * position or u is out of range, which is reported through the status word.
  * Requires temperature > 0 (finite; for temperature 0 call focus_confidence), top_k >= 0, 0 < top_p <= 1,
- * 0 <= min_p <= 1; vocab at most 800 000 (bf16) / 400 000 (f32), else UNSUPPORTED.  One launch, no workspace. */
+ * 0 <= min_p <= 1; vocab at most 700 000 (bf16) / 350 000 (f32), else UNSUPPORTED.  One launch, no workspace. */
 focus_status focus_sample(focus_ctx* ctx, const void* logits, int32_t dtype, int64_t row_stride, int32_t vocab,
                           int32_t pos_base, int32_t n_pos, const int32_t* rows, const int32_t* n_rows,
                           int32_t max_rows, float temperature, int32_t top_k, float top_p, float min_p,

@@ -8,15 +8,16 @@
 // the answer does not depend on timing or on the number of rows.
 //
 // The kept set is a prefix of the descending order.  Two ways to it:
-//   short list  (top-k up to 512, or a nucleus that lies within the 512 largest logits): the 512 k maxima of the threads'
-//               shares give a lower bound of the k-th largest logit -- that many logits reach it, and few more do --, the
-//               logits from there up are collected, sorted and cut by one CTA.  One pass for the maximum, one for the
-//               list (with the sums over the vocabulary that prob and top-p need).
+//   short list  (up to 2048 tokens: top-k to 1024, most nuclei): the k-th largest of the maxima of the threads' shares is a
+//               lower bound of the k-th largest logit -- that many logits reach it, and few more do.  The logits from there
+//               up are collected in index order and cut by one CTA, which has them in registers.  One pass for the maxima,
+//               one for the list (with the sums over the vocabulary that prob and top-p need).
 //   any length  (no cut, min-p alone, long top-k, flat nuclei): the key T of the last kept logit, by counts (top-k: 8-bit
-//               digits of a radix descent) and by weight (top-p: one bit of the key per pass); (T, how many of the tokens
+//               digits of a radix descent) and by weight (top-p: two bits of the key per pass); (T, how many of the tokens
 //               at T) says all about the set.  Then the kept weight per warp segment in index order, the segment that
 //               holds u * total, and its walk.
 #include <cooperative_groups.h>
+#include <float.h>
 
 #include "focus_common.cuh"
 
@@ -27,14 +28,15 @@ namespace {
 constexpr int SP_THREADS = 512;
 constexpr int SP_WARPS = SP_THREADS / 32;
 constexpr int SP_MAX_CLUSTER = 8;
-constexpr int SP_SLICE_BYTES = 196 * 1024;               // largest slice of a row per CTA
-constexpr int SP_LIST = 1024;                            // most tokens of a short list
-constexpr int SP_LIST_K = 512;                           // largest top-k that goes through it; tokens tried for a nucleus
-constexpr int SP_SCRATCH = 16 * 1024;                    // thread maxima of a cluster, or two lists
+constexpr int SP_SLICE_BYTES = 180 * 1024;               // largest slice of a row per CTA
+constexpr int SP_LIST = 2048;                            // most tokens of a short list
+constexpr int SP_LIST_K = 1024;                          // largest top-k that goes through it; tokens tried for a nucleus
+constexpr int SP_PER = SP_LIST / SP_THREADS;             // tokens of the list per thread
+// scratch behind the slice: list (before it: the cluster's thread maxima) | one byte per 16-byte vector | thread maxima
+constexpr int SP_OFF_MASK = SP_LIST * 8, SP_OFF_MAX = SP_OFF_MASK + 14 * 1024, SP_SCRATCH = SP_OFF_MAX + SP_THREADS * 4;
 constexpr int SP_TAB = 1024;                             // entries of the table of powers
-static_assert(SP_SLICE_BYTES + SP_SCRATCH + 14 * 1024 <= 227 * 1024, "shared memory");
-static_assert(SP_MAX_CLUSTER * SP_THREADS * 4 <= SP_SCRATCH && 2 * SP_LIST * 8 <= SP_SCRATCH, "scratch");
 constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN is below it
+static_assert(SP_MAX_CLUSTER * SP_THREADS * 4 <= SP_OFF_MASK && SP_SLICE_BYTES / 16 + 4 <= SP_OFF_MAX - SP_OFF_MASK, "scratch");
 
 struct SegSum {            // one warp's contiguous segment of the row
   double w;                // kept weight above the threshold key
@@ -43,25 +45,23 @@ struct SegSum {            // one warp's contiguous segment of the row
 
 struct SampleShared {
   double tab[SP_TAB];      // 2^(i / SP_TAB)
-  double dsum[2][SP_WARPS];
+  double dsum[2][SP_WARPS][3];
   int isum[2][SP_WARPS];
-  double cta_d[2];
+  double cta_d[2][3];
   int cta_i[2];
   SegSum seg[SP_WARPS];
   SegSum all[SP_MAX_CLUSTER * SP_WARPS];
   float wmax[SP_WARPS];
-  double raw, z;           // this CTA's sums over the vocabulary (temperature 1 / given temperature)
   int list_n, list_ok;
   int hist[2][256];
-  int digit, above;
-  double scan[SP_WARPS + 1];
-  int found, n_kept;
+  int scan_i[33];
+  double scan[SP_WARPS];
+  int digit, above, found;
   // the segment that holds u * total
   int hit, hit_eq, kept;
   double before, total;
 };
-
-static_assert(sizeof(SampleShared) <= 14 * 1024, "shared memory");
+static_assert(sizeof(SampleShared) <= 15 * 1024 && SP_SLICE_BYTES + SP_SCRATCH + 15 * 1024 <= 227 * 1024, "shared memory");
 
 struct SampleParams {
   const void* logits;
@@ -79,39 +79,56 @@ struct SampleParams {
   int32_t* status;
 };
 
-// Sum over the cluster, the same in every thread.  Two slots in turn: one cluster barrier per call is enough, since a
-// CTA writes a slot again only after a barrier that its slowest reader has passed.
-__device__ __forceinline__ double cluster_sum(cg::cluster_group& cl, SampleShared& sh, int& turn, double v, int& cnt) {
+// Sums over the cluster, the same in every thread.  Two slots in turn: one cluster barrier per call is enough, since a
+// CTA writes a slot again only after a barrier that its slowest reader has passed.  CTA = true: of this CTA alone.
+template <int N, bool CTA = false>
+__device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh, int& turn, double (&v)[N], int& cnt) {
   const int t = turn & 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ++turn;
-  int n = cnt;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    v += __shfl_xor_sync(0xffffffffu, v, o);
-    n += __shfl_xor_sync(0xffffffffu, n, o);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   }
-  if (lane == 0) { sh.dsum[t][warp] = v; sh.isum[t][warp] = n; }
+  cnt = __reduce_add_sync(0xffffffffu, cnt);
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sh.dsum[t][warp][i] = v[i];
+    sh.isum[t][warp] = cnt;
+  }
   __syncthreads();
+  if (CTA || warp == 0) {                                // the warps' sums in a fixed tree
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lane < SP_WARPS ? sh.dsum[t][lane][i] : 0.0;
+    cnt = lane < SP_WARPS ? sh.isum[t][lane] : 0;
+#pragma unroll
+    for (int o = SP_WARPS / 2; o > 0; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      cnt += __shfl_xor_sync(0xffffffffu, cnt, o);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+    cnt = __shfl_sync(0xffffffffu, cnt, 0);
+  }
+  if (CTA) return;
   if (threadIdx.x == 0) {
-    double s = 0.0;
-    int c = 0;
-    for (int w = 0; w < SP_WARPS; ++w) { s += sh.dsum[t][w]; c += sh.isum[t][w]; }
-    sh.cta_d[t] = s; sh.cta_i[t] = c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sh.cta_d[t][i] = v[i];
+    sh.cta_i[t] = cnt;
   }
   cl.sync();
-  double s = 0.0;
-  int c = 0;
-  for (unsigned r = 0; r < cl.num_blocks(); ++r) {
-    const SampleShared* p = cl.map_shared_rank(&sh, r);
-    s += p->cta_d[t]; c += p->cta_i[t];
+  const int nc = (int)cl.num_blocks();
+  const SampleShared* far = cl.map_shared_rank(&sh, min(lane, nc - 1));   // lane q fetches rank q's sums
+  double f[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) { f[i] = lane < nc ? far->cta_d[t][i] : 0.0; v[i] = 0.0; }
+  cnt = __reduce_add_sync(0xffffffffu, lane < nc ? far->cta_i[t] : 0);
+  for (int r = 0; r < nc; ++r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_sync(0xffffffffu, f[i], r);
   }
-  cnt = c;
-  return s;
 }
-
-template <typename T> __device__ __forceinline__ T nan_logit();
-template <> __device__ __forceinline__ float nan_logit<float>() { return __uint_as_float(0x7FC00000u); }
-template <> __device__ __forceinline__ __nv_bfloat16 nan_logit<__nv_bfloat16>() { return __ushort_as_bfloat16(0x7FC0u); }
 
 template <typename T>
 __device__ __forceinline__ void unpack_logits(const uint4& raw, float (&x)[16 / sizeof(T)]) {
@@ -126,84 +143,69 @@ __device__ __forceinline__ void unpack_logits(const uint4& raw, float (&x)[16 / 
     }
   }
 }
+// NaN -> -inf, and the largest and smallest of a vector
+__device__ __forceinline__ uint32_t max_bf2(uint32_t a, uint32_t b) { uint32_t d; asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+__device__ __forceinline__ uint32_t min_bf2(uint32_t a, uint32_t b) { uint32_t d; asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+template <typename T>
+__device__ __forceinline__ void clean_logits(uint4& raw, float& hi, float& lo) {
+  if constexpr (sizeof(T) == 2) {
+    raw.x = max_bf2(raw.x, 0xFF80FF80u); raw.y = max_bf2(raw.y, 0xFF80FF80u);
+    raw.z = max_bf2(raw.z, 0xFF80FF80u); raw.w = max_bf2(raw.w, 0xFF80FF80u);
+    const uint32_t a = max_bf2(max_bf2(raw.x, raw.y), max_bf2(raw.z, raw.w)), b = min_bf2(min_bf2(raw.x, raw.y), min_bf2(raw.z, raw.w));
+    hi = fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+    lo = fminf(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+  } else {
+    float x[4];
+    unpack_logits<float>(raw, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fmaxf(x[i], -INFINITY);
+    raw = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+  }
+}
+template <typename T>
+__device__ __forceinline__ float largest_of(const uint4& raw) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t a = max_bf2(max_bf2(raw.x, raw.y), max_bf2(raw.z, raw.w));
+    return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+  } else {
+    return fmaxf(fmaxf(__uint_as_float(raw.x), __uint_as_float(raw.y)), fmaxf(__uint_as_float(raw.z), __uint_as_float(raw.w)));
+  }
+}
 
-// 2^t for t <= 0 in fp64: t = n / 1024 + r, 2^t = 2^(n >> 10) * tab[n & 1023] * 2^r, the last factor by its Taylor
-// polynomial (Tang's table-driven scheme, 1989).  |r| <= 2^-11, so the cubic leaves 6e-16; below 2^-1000 it is zero.
-__device__ __forceinline__ double pow2_neg(double t, const double* tab) {
-  if (t < -1000.0) return 0.0;
+// Powers of two in fp64: t = n / 1024 + r, 2^t = 2^(n >> 10) * tab[n & 1023] * 2^r, the last factor by its Taylor
+// polynomial (Tang's table-driven scheme, 1989).  |r| <= 2^-11, so the square leaves 7e-12 of a weight, of either sign.
+// -1000 <= t <= 0; no branch, so that several run side by side.
+__device__ __forceinline__ double pow2_near(double t, const double* tab) {
   const double magic = 6755399441055744.0;               // 1.5 * 2^52: adding it leaves the rounded integer in the low bits
   const double tm = fma(t, (double)SP_TAB, magic);
   const int n = __double2loint(tm);
   const double r = fma(tm - magic, -1.0 / SP_TAB, t);
-  const double c1 = 0.69314718055994531, c2 = 0.24022650695910071, c3 = 0.055504108664821580;   // ln2^k / k!
-  const double q = r * fma(r, fma(r, c3, c2), c1);
   const double b = tab[n & (SP_TAB - 1)];
-  const double w = fma(b, q, b);
+  const double w = fma(b, r * fma(r, 0.24022650695910071, 0.69314718055994531), b);   // ln2^2 / 2, ln2
   return __hiloint2double(__double2hiint(w) + ((n >> 10) << 20), __double2loint(w));
 }
 
-// Sorts n2 (a power of two) 64-bit numbers in shared memory, descending; every thread of the block calls it.
-__device__ __forceinline__ void block_sort_desc(unsigned long long* v, int n2) {
-  for (int k = 2; k <= n2; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < n2 / 2; i += SP_THREADS) {
-        const int lo = ((i & ~(j - 1)) << 1) | (i & (j - 1)), hi = lo | j;
-        const unsigned long long a = v[lo], b = v[hi];
-        if ((a < b) == ((lo & k) == 0)) { v[lo] = b; v[hi] = a; }
-      }
-    }
-  __syncthreads();
-}
-
-// Inclusive prefix sums of the n <= SP_LIST numbers get(0), get(1), ... into out, in fixed order; every thread calls it.
-template <typename Get>
-__device__ __forceinline__ void block_scan_list(SampleShared& sh, double* out, int n, Get get) {
-  constexpr int PER = SP_LIST / SP_THREADS;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  double v[PER], run = 0.0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = threadIdx.x * PER + i;
-    run += at < n ? get(at) : 0.0;
-    v[i] = run;
-  }
-  double inc = run;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const double y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += y;
-  }
-  __syncthreads();
-  if (lane == 31) sh.scan[warp] = inc;
-  __syncthreads();
-  double before = inc - run;
-  for (int w = 0; w < warp; ++w) before += sh.scan[w];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = threadIdx.x * PER + i;
-    if (at < n) out[at] = before + v[i];
-  }
-  __syncthreads();
-}
-
-// Key of the k-th largest of n keys in shared memory (1 <= k <= n), 8-bit digits from the top; BITS of the key in use.
-template <int BITS>
-__device__ __forceinline__ uint32_t block_kth(SampleShared& sh, const uint32_t* key, int n, int k) {
+// The k-th largest (1 <= k <= n) of the keys get(0), get(1), ..., 8-bit digits from the top, BITS of the key in use;
+// k becomes its place among the keys equal to it.  Every thread of the block calls it.
+template <int BITS, typename Get>
+__device__ __forceinline__ uint32_t block_kth(SampleShared& sh, int n, int& k, Get get) {
   uint32_t prefix = 0;
   for (int shift = BITS - 8; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += SP_THREADS) sh.hist[0][i] = 0;
+    int* hist = sh.hist[(shift >> 3) & 1];
+    for (int i = threadIdx.x; i < 256; i += SP_THREADS) hist[i] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += SP_THREADS) {
-      const uint32_t q = key[i];
-      if (shift + 8 >= BITS || (q >> (shift + 8)) == prefix) atomicAdd(&sh.hist[0][(q >> shift) & 255u], 1);
+      const uint32_t q = get(i);
+      if (shift + 8 >= BITS || (q >> (shift + 8)) == prefix) atomicAdd(&hist[(q >> shift) & 255u], 1);
     }
     __syncthreads();
     if (threadIdx.x < 32) {                              // digits from the largest down, eight per lane
       const int lane = threadIdx.x;
       int c[8], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { c[i] = sh.hist[0][255 - (lane * 8 + i)]; sum += c[i]; }
+      for (int i = 0; i < 8; ++i) { c[i] = hist[255 - (lane * 8 + i)]; sum += c[i]; }
       int inc = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -222,7 +224,6 @@ __device__ __forceinline__ uint32_t block_kth(SampleShared& sh, const uint32_t* 
     __syncthreads();
     prefix = (prefix << 8) | (uint32_t)sh.digit;
     k -= sh.above;
-    __syncthreads();
   }
   return prefix;
 }
@@ -257,19 +258,24 @@ sample_kernel(const SampleParams p) {
     return;
   }
   int turn = 0;
-  // ---- the slice, the maxima of the threads' shares ----
-  const int lo = min(rank * p.slice, p.vocab), cnt = min(p.slice, p.vocab - lo);
+  // ---- the slice (NaN as -inf, padded to whole vectors with -inf), the maxima of the threads' shares ----
+  const int lo = min(rank * p.slice, p.vocab), cnt = min(p.slice, p.vocab - lo), n_vec = (cnt + EPC - 1) / EPC;
   const T* row = (const T*)p.logits + (long long)(pos - p.pos_base) * p.row_stride + lo;
-  uint8_t* scratch = smem_raw + (((size_t)p.slice * sizeof(T) + 15) & ~size_t(15));
-  float m = -INFINITY;
+  uint8_t* scratch = smem_raw + (size_t)p.slice * sizeof(T);
+  float share = -INFINITY;
   int n_cand = 0;
-  auto look = [&](const uint4& raw) {
-    float x[EPC];
-    unpack_logits<T>(raw, x);
+  auto take = [&](uint4 raw, int i) {
+    float hi, low;
+    clean_logits<T>(raw, hi, low);
+    *reinterpret_cast<uint4*>(xs + i) = raw;
+    share = fmaxf(share, hi);
+    if (low > -INFINITY) {
+      n_cand += EPC;
+    } else {
+      float x[EPC];
+      unpack_logits<T>(raw, x);
 #pragma unroll
-    for (int e = 0; e < EPC; ++e) {
-      n_cand += x[e] > -INFINITY ? 1 : 0;                // false for NaN
-      m = fmaxf(m, x[e]);                                // a NaN is passed over
+      for (int e = 0; e < EPC; ++e) n_cand += x[e] > -INFINITY ? 1 : 0;
     }
   };
   {
@@ -280,34 +286,43 @@ sample_kernel(const SampleParams p) {
 #pragma unroll
       for (int q = 0; q < U; ++q) raw[q] = __ldg(reinterpret_cast<const uint4*>(row + i + q * STEP));
 #pragma unroll
-      for (int q = 0; q < U; ++q) { *reinterpret_cast<uint4*>(xs + i + q * STEP) = raw[q]; look(raw[q]); }
+      for (int q = 0; q < U; ++q) take(raw[q], i + q * STEP);
     }
-    for (; i + EPC <= cnt; i += STEP) {
-      const uint4 raw = __ldg(reinterpret_cast<const uint4*>(row + i));
-      *reinterpret_cast<uint4*>(xs + i) = raw;
-      look(raw);
-    }
-    // the slice is padded to whole vectors with NaN: later passes need no other bound
-    const int tail = cnt / EPC * EPC, end = (cnt + EPC - 1) / EPC * EPC;
-    if (tail + tid < end) {
-      const T v = tail + tid < cnt ? row[tail + tid] : nan_logit<T>();
-      xs[tail + tid] = v;
-      const float x = load_as_float(&v);
-      if (x > -INFINITY) { m = fmaxf(m, x); ++n_cand; }
+    for (; i + EPC <= cnt; i += STEP) take(__ldg(reinterpret_cast<const uint4*>(row + i)), i);
+    if (i < cnt) {                                       // the one vector that the row ends in
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (sizeof(T) == 2) {
+          const uint32_t a = i + 2 * q < cnt ? __bfloat16_as_ushort(row[i + 2 * q]) : 0xFF80u;
+          const uint32_t b = i + 2 * q + 1 < cnt ? __bfloat16_as_ushort(row[i + 2 * q + 1]) : 0xFF80u;
+          w[q] = a | (b << 16);
+        } else {
+          w[q] = i + q < cnt ? __float_as_uint(row[i + q]) : 0xFF800000u;
+        }
+      }
+      take(make_uint4(w[0], w[1], w[2], w[3]), i);
     }
   }
-  for (int i = tid; i < SP_TAB; i += SP_THREADS) sh.tab[i] = exp2((double)i / SP_TAB);
-  const float share = m;                                 // largest logit of this thread's share
-  reinterpret_cast<uint32_t*>(scratch)[tid] = float_key(share) >> (32 - KEY_BITS);
+  for (int i = tid; i < SP_TAB; i += SP_THREADS) {       // 2^(i / 1024) as the product of its binary digits' powers
+    const double f[10] = {1.0006771306930664, 1.0013547198921082, 1.0027112750502025, 1.0054299011128027, 1.0108892860517005,
+                          1.0218971486541166, 1.0442737824274138, 1.0905077326652577, 1.189207115002721, 1.4142135623730951};
+    double v = 1.0;
+#pragma unroll
+    for (int q = 0; q < 10; ++q) v *= (i >> q & 1) ? f[q] : 1.0;
+    sh.tab[i] = v;
+  }
+  uint32_t* share_key = reinterpret_cast<uint32_t*>(scratch + SP_OFF_MAX);
+  share_key[tid] = float_key(share) >> (32 - KEY_BITS);
+  float m = share;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (lane == 0) sh.wmax[warp] = m;
-  if (tid == 0) sh.list_n = 0;
-  (void)cluster_sum(cl, sh, turn, 0.0, n_cand);          // its barriers publish the maxima as well
-  if (lane < nc * SP_WARPS) {
-    m = -INFINITY;
-    for (int q = lane; q < nc * SP_WARPS; q += 32) m = fmaxf(m, cl.map_shared_rank(&sh, q / SP_WARPS)->wmax[q % SP_WARPS]);
+  {
+    double none[1] = {0.0};
+    sum_all<1>(cl, sh, turn, none, n_cand);              // its barriers publish the maxima as well
   }
+  for (int q = lane; q < nc * SP_WARPS; q += 32) m = fmaxf(m, cl.map_shared_rank(&sh, q / SP_WARPS)->wmax[q % SP_WARPS]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (n_cand == 0) {
@@ -315,9 +330,19 @@ sample_kernel(const SampleParams p) {
     cl.sync();
     return;
   }
+  // ---- weights: 2^((x - m) log2(e) / temperature) ----
   const double scale = 1.4426950408889634 / (double)p.temperature, md = (double)m;
-  // the maximum itself has weight 1, also where it is +inf (everything else then has none)
-  auto weight = [&](float x) -> double { return x == m ? 1.0 : pow2_neg(((double)x - md) * scale, sh.tab); };
+  const float floor_x = (float)fmax(md - 1000.0 / scale, -(double)FLT_MAX);      // lighter ones may count as 2^-1000
+  // weights without a branch, where that floor is a logit well below the maximum (not so for an infinite maximum, one whose
+  // neighbouring floats are further apart, or a temperature that flattens the type's whole range)
+  const double floor_t = ((double)floor_x - md) * scale;
+  const bool plain = m < INFINITY && floor_t < -900.0 && floor_t > -1020.0;
+  auto weight = [&](float x) -> double {
+    if (m == INFINITY) return x == m ? 1.0 : 0.0;
+    const double t = ((double)x - md) * scale;
+    return t >= -1000.0 ? pow2_near(t, sh.tab) : 0.0;
+  };
+  auto weight_plain = [&](float x) -> double { return pow2_near(((double)fmaxf(x, floor_x) - md) * scale, sh.tab); };
   // keys of bf16 logits in 16 bits, so that both types descend through their own bits only
   auto key_of = [&](float x) -> uint32_t { return float_key(x) >> (32 - KEY_BITS); };
   constexpr uint32_t BOTTOM = KEY_NEG_INF >> (32 - KEY_BITS);
@@ -327,131 +352,223 @@ sample_kernel(const SampleParams p) {
     if (KEY_BITS < 32 && !(full & 0x80000000u)) full |= 0xFFFFu;
     return key_to_float(full);
   };
-  const int n_vec = (cnt + EPC - 1) / EPC;               // vectors of the slice
-  auto every = [&](auto f) {                             // f(x, element) over this thread's share
+  const uint4* vecs = reinterpret_cast<const uint4*>(xs);
+  // f(x of one vector): the sum of f over this thread's share, four running sums
+  auto sum_over = [&](auto f) -> double {
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
     for (int i = tid; i < n_vec; i += SP_THREADS) {
       float x[EPC];
-      unpack_logits<T>(*reinterpret_cast<const uint4*>(xs + i * EPC), x);
+      unpack_logits<T>(vecs[i], x);
 #pragma unroll
-      for (int e = 0; e < EPC; ++e) f(x[e], i * EPC + e);
+      for (int e = 0; e < EPC; ++e) s[e & 3] += f(x[e]);
     }
+    return (s[0] + s[1]) + (s[2] + s[3]);
   };
-  const bool cut_k = p.top_k > 0 && p.top_k < n_cand, cut_p = p.top_p < 1.f;
-  const int k_max = cut_k ? p.top_k : n_cand;
-  // ---- short list ----
+  const float l2e = 1.4426950408889634f;
+  // softmax denominator at temperature 1 over the vocabulary, an output value: fp32 terms
+  auto raw_sum = [&]() -> double {
+    if (m == INFINITY) return sum_over([&](float x) { return x == m ? 1.0 : 0.0; });
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = tid; i < n_vec; i += SP_THREADS) {
+      float x[EPC];
+      unpack_logits<T>(vecs[i], x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        float y;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x[e] - m) * l2e));
+        s[e & 3] += y;
+      }
+    }
+    return (double)((s[0] + s[1]) + (s[2] + s[3]));
+  };
+  const bool cut_k = p.top_k > 0 && p.top_k < n_cand, cut_p = p.top_p < 1.f, need_z = cut_p && !cut_k;
+  const int groups = nc * SP_THREADS, want = cut_k ? p.top_k : min(SP_LIST_K, groups / 2);
   bool have_raw = false;
   double raw_all = 0.0;
-  if ((cut_k && p.top_k <= SP_LIST_K) || (cut_p && !cut_k) || n_cand <= SP_LIST) {
-    const int groups = nc * SP_THREADS, want = cut_k ? p.top_k : SP_LIST_K;
-    float from = -INFINITY;                              // collect the logits from here up
+  // ---- short list (the bound is tight while the k wanted are at most half of the shares) ----
+  if (((cut_k || cut_p) && want <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
+    float from = -FLT_MAX;                               // collect the logits from here up
     if (n_cand > SP_LIST) {
-      // a lower bound of the want-th largest logit: the want-th largest of the shares' maxima (groups >= want)
       uint32_t* keys = reinterpret_cast<uint32_t*>(scratch);
-      uint32_t mine[SP_MAX_CLUSTER];
 #pragma unroll
       for (int q = 0; q < SP_MAX_CLUSTER; ++q)
-        if (q < nc) mine[q] = reinterpret_cast<const uint32_t*>(cl.map_shared_rank(scratch, q))[tid];
-      cl.sync();                                         // everybody has read: the copies may go over the originals
-#pragma unroll
-      for (int q = 0; q < SP_MAX_CLUSTER; ++q)
-        if (q < nc) keys[q * SP_THREADS + tid] = mine[q];
-      __syncthreads();
-      const uint32_t kth = block_kth<KEY_BITS>(sh, keys, groups, want);
-      from = kth > BOTTOM ? key_value(kth) : -INFINITY;
+        if (q < nc) keys[q * SP_THREADS + tid] = cl.map_shared_rank(share_key, q)[tid];
+      int k = want;
+      const uint32_t kth = block_kth<KEY_BITS>(sh, groups, k, [&](int i) { return keys[i]; });
+      if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
-    unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch);
-    const bool need_z = cut_p && !cut_k;
-    double z = 0.0;
-    float part = 0.f;
-    every([&](float x, int i) {
-      if (x >= from && x > -INFINITY) {
-        const int at = atomicAdd(&sh.list_n, 1);
-        if (at < SP_LIST) list[at] = ((unsigned long long)float_key(x) << 32) | (uint32_t)~(lo + i);
+    double v[2] = {0.0, 0.0};
+    if (p.prob) v[0] = raw_sum();
+    if (need_z) v[1] = plain ? sum_over(weight_plain) : sum_over([&](float x) { return x > -INFINITY ? weight(x) : 0.0; });
+    // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order
+    uint8_t* mask = scratch + SP_OFF_MASK;
+    const int n_words = (n_vec + 3) >> 2;
+    for (int i = tid; i < n_words * 4; i += SP_THREADS) {
+      uint32_t bits = 0;
+      if (i < n_vec) {
+        const uint4 raw = vecs[i];
+        if (largest_of<T>(raw) >= from) {
+          float x[EPC];
+          unpack_logits<T>(raw, x);
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) bits |= x[e] >= from ? 1u << e : 0u;
+        }
       }
-      if (p.prob) part += x == m ? 1.f : (x > -INFINITY ? expf(x - m) : 0.f);
-      if (need_z && x > -INFINITY) z += weight(x);
-    });
-    // sums of the CTA, then of the cluster (both in the order of the ranks)
-    int dummy = 0;
-    raw_all = cluster_sum(cl, sh, turn, (double)part, dummy);     // its barriers publish the lists as well
+      mask[i] = (uint8_t)bits;
+    }
+    __syncthreads();                                     // also: nobody reads the keys any more
+    unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch);
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(mask);
+    const int per_w = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per_w, n_words), w1 = min(w0 + per_w, n_words);
+    int mine = 0;
+    for (int i = w0; i < w1; ++i) mine += __popc(words[i]);
+    int tot;
+    int at = block_excl_scan(mine, sh.scan_i, tot);
+    if (mine && tot <= SP_LIST)
+      for (int i = w0; i < w1; ++i)
+        for (uint32_t b = words[i]; b; b &= b - 1u) {
+          const int bit = __ffs(b) - 1, e = (i * 4 + (bit >> 3)) * EPC + (bit & 7);
+          list[at++] = ((unsigned long long)float_key(load_as_float(xs + e)) << 32) | (uint32_t)(lo + e);
+        }
+    if (tid == 0) sh.list_n = tot;
+    int n_list = tot;
+    sum_all<2>(cl, sh, turn, v, n_list);                 // publishes the lists as well
+    n_list = 0;
+#pragma unroll
+    for (int q = 0; q < SP_MAX_CLUSTER; ++q)
+      if (q < nc) n_list += cl.map_shared_rank(&sh, q)->list_n;
+    raw_all = v[0];
     have_raw = true;
-    double z_all = 0.0;
-    if (need_z) { dummy = 0; z_all = cluster_sum(cl, sh, turn, z, dummy); }
-    int n = 0;
-    for (int q = 0; q < nc; ++q) n += cl.map_shared_rank(&sh, q)->list_n;
-    const bool fits = n <= SP_LIST;                                 // more: ties at the bound (uniform over the cluster)
-    if (fits) {
-      unsigned long long* sorted = list + SP_LIST;
-      double* cum = reinterpret_cast<double*>(scratch);  // over the first list, once it has been gathered
+    if (n_list <= SP_LIST) {                             // more: ties at the bound (uniform over the cluster)
       if (rank == 0) {
-        int at = 0;
-        for (int q = 0; q < nc; ++q) {
+        int have = tot;
+        for (int q = 1; q < nc; ++q) {                   // the other slices follow this one: the list stays in index order
           const int c = cl.map_shared_rank(&sh, q)->list_n;
           const unsigned long long* src = reinterpret_cast<const unsigned long long*>(cl.map_shared_rank(scratch, q));
-          for (int i = tid; i < c; i += SP_THREADS) sorted[at + i] = src[i];
-          at += c;
-        }
-        int n2 = 32;
-        while (n2 < n) n2 <<= 1;
-        for (int i = n + tid; i < n2; i += SP_THREADS) sorted[i] = 0ull;
-        block_sort_desc(sorted, n2);
-        auto listed = [&](int i) -> float { return key_to_float((uint32_t)(sorted[i] >> 32)); };
-        if (tid == 0) { sh.found = n; sh.n_kept = 0; }
-        block_scan_list(sh, cum, n, [&](int i) { return weight(listed(i)); });
-        // n_p: the first prefix that holds top_p of the weight left by top-k; n_m: those of at least min_p
-        const int k = min(k_max, n);
-        const double target = (double)p.top_p * (need_z ? z_all : cum[k - 1]);
-        int below = 0, light = 0;
-        for (int i = tid; i < k; i += SP_THREADS) {
-          below += cum[i] < target ? 1 : 0;
-          light += weight(listed(i)) < (double)p.min_p ? 1 : 0;
+          for (int i = tid; i < c; i += SP_THREADS) list[have + i] = src[i];
+          have += c;
         }
         __syncthreads();
-        if (below) atomicAdd(&sh.n_kept, below);
-        if (light) atomicSub(&sh.found, light);
-        __syncthreads();
-        const int n_below = sh.n_kept, n_heavy = sh.found - (n - k);
-        int kept = cut_p ? min(k, n_below + 1) : k;
-        if (p.min_p > 0.f) kept = min(kept, n_heavy);
-        kept = max(kept, 1);
-        // a nucleus that the list does not reach the end of is found the long way -- unless min-p ends it earlier
-        const bool whole = !need_z || n_below < k || n == n_cand || (p.min_p > 0.f && n_heavy < k);
-        __syncthreads();
-        if (tid == 0) sh.list_ok = whole ? 1 : 0;
+        // this thread's tokens: neighbours in index order
+        uint32_t key[SP_PER];
+        double w[SP_PER];
+        bool in[SP_PER];
+#pragma unroll
+        for (int q = 0; q < SP_PER; ++q) {
+          const int i = tid * SP_PER + q;
+          in[q] = i < n_list;
+          const uint32_t full = in[q] ? (uint32_t)(list[i] >> 32) : 0u;
+          key[q] = full >> (32 - KEY_BITS);
+          w[q] = in[q] ? weight(key_to_float(full)) : 0.0;
+        }
+        // keeps of the tokens at key t the first `quota` in index order, drops those below t
+        auto cut_at = [&](uint32_t t, int quota) {
+          int eq = 0, all;
+#pragma unroll
+          for (int q = 0; q < SP_PER; ++q) eq += in[q] && key[q] == t ? 1 : 0;
+          int before = block_excl_scan(eq, sh.scan_i, all);
+#pragma unroll
+          for (int q = 0; q < SP_PER; ++q) {
+            const bool at_t = in[q] && key[q] == t;
+            in[q] = in[q] && (key[q] > t || (at_t && before < quota));
+            before += at_t ? 1 : 0;
+          }
+        };
+        if (cut_k) {
+          int k = p.top_k;
+          const uint32_t t = block_kth<KEY_BITS>(sh, n_list, k, [&](int i) { return (uint32_t)(list[i] >> 32) >> (32 - KEY_BITS); });
+          cut_at(t, k);
+        }
+        bool whole = true;
+        int dummy = 0, own_turn = 0;                     // sums of this CTA: not in step with the cluster's
+        if (cut_p) {
+          double a[1] = {0.0};
+#pragma unroll
+          for (int q = 0; q < SP_PER; ++q) a[0] += in[q] ? w[q] : 0.0;
+          sum_all<1, true>(cl, sh, own_turn, a, dummy);
+          const double target = (double)p.top_p * (need_z ? v[1] : a[0]);
+          // a nucleus that reaches beyond the list is found the long way
+          whole = a[0] >= target || n_list == n_cand;
+          if (whole && a[0] >= target) {
+            // the largest key whose tokens, with all above, hold the target: two bits per step below the bits all share
+            const uint32_t k_hi = key_of(m), k_lo = from == -FLT_MAX ? BOTTOM : key_of(from);
+            const int vary = (33 - __clz(k_hi ^ k_lo)) & ~1;      // bits that differ, made even: k_lo <= every key <= k_hi
+            uint32_t best = vary >= 32 ? 0u : k_hi >> vary << vary;
+            double above = 0.0;                          // weight of the keys from best + 2^sft up
+            for (int sft = vary; sft > 0;) {
+              sft -= 2;
+              const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
+              double s3[3] = {0.0, 0.0, 0.0};
+#pragma unroll
+              for (int q = 0; q < SP_PER; ++q) {
+                const double wq = in[q] ? w[q] : 0.0;
+                s3[0] += key[q] >= t1 ? wq : 0.0;
+                s3[1] += key[q] >= t2 ? wq : 0.0;
+                s3[2] += key[q] >= t3 ? wq : 0.0;
+              }
+              sum_all<3, true>(cl, sh, own_turn, s3, dummy);
+              if (s3[2] >= target) best = t3;
+              else if (s3[1] >= target) { best = t2; above = s3[2]; }
+              else if (s3[0] >= target) { best = t1; above = s3[1]; }
+              else above = s3[0];
+            }
+            const double need = ceil((target - above) / weight(key_value(best)));
+            cut_at(best, (int)fmin(fmax(need, 1.0), (double)SP_LIST));
+          }
+        }
+        if (whole && p.min_p > 0.f) {
+#pragma unroll
+          for (int q = 0; q < SP_PER; ++q) in[q] = in[q] && w[q] >= (double)p.min_p;
+        }
+        if (tid == 0) { sh.list_ok = whole ? 1 : 0; sh.found = SP_LIST; }
         if (whole) {
-          // in index order: sort the kept ones by ~index (descending = ascending index), sum again, take the first sum
-          // above u * total
-          unsigned long long v[SP_LIST / SP_THREADS];
+          // running sums of the kept weights in index order; the first one above u * total
+          double mine_w = 0.0, cum[SP_PER];
+          int kept = 0;
 #pragma unroll
-          for (int q = 0; q < SP_LIST / SP_THREADS; ++q) {
-            const int i = tid + q * SP_THREADS;
-            v[q] = i < kept ? (sorted[i] << 32) | (sorted[i] >> 32) : 0ull;
+          for (int q = 0; q < SP_PER; ++q) {
+            mine_w += in[q] ? w[q] : 0.0;
+            cum[q] = mine_w;
+            kept += in[q] ? 1 : 0;
           }
-          __syncthreads();
-          int k2 = 32;
-          while (k2 < kept) k2 <<= 1;
+          double inc = mine_w;
 #pragma unroll
-          for (int q = 0; q < SP_LIST / SP_THREADS; ++q) {
-            const int i = tid + q * SP_THREADS;
-            if (i < k2) sorted[i] = v[q];
+          for (int o = 1; o < 32; o <<= 1) {
+            const double y = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += y;
           }
-          block_sort_desc(sorted, k2);
-          block_scan_list(sh, cum, kept, [&](int i) { return weight(key_to_float((uint32_t)sorted[i])); });
-          const double total = cum[kept - 1], t_u = (double)u * total;
-          if (tid == 0) sh.found = kept;
+          if (lane == 31) sh.scan[warp] = inc;
+          kept = __reduce_add_sync(0xffffffffu, kept);
+          if (lane == 0) sh.isum[0][warp] = kept;
           __syncthreads();
-          for (int i = tid; i < kept; i += SP_THREADS)
-            if (cum[i] > t_u) atomicMin(&sh.found, i);
+          double base = 0.0, total = 0.0;
+          kept = 0;
+#pragma unroll
+          for (int q = 0; q < SP_WARPS; ++q) {
+            if (q == warp) base = total;
+            total += sh.scan[q];
+            kept += sh.isum[0][q];
+          }
+          base += inc - mine_w;
+          const double target = (double)u * total;
+          int first = SP_LIST, last = -1;                // last kept token with a weight: where rounding leaves none above
+#pragma unroll
+          for (int q = SP_PER - 1; q >= 0; --q)
+            if (in[q] && w[q] > 0.0) {
+              if (base + cum[q] > target) first = tid * SP_PER + q;
+              if (last < 0) last = tid * SP_PER + q;
+            }
+          first = (int)__reduce_min_sync(0xffffffffu, (unsigned)first);
+          last = __reduce_max_sync(0xffffffffu, last);
+          if (lane == 0) { sh.isum[1][warp] = last; if (first < SP_LIST) atomicMin(&sh.found, first); }
           __syncthreads();
           if (tid == 0) {
             int f = sh.found;
-            if (f >= kept) {                             // rounding at the far end: the last token with a weight
-              f = kept - 1;
-              while (f > 0 && weight(key_to_float((uint32_t)sorted[f])) == 0.0) --f;
-            }
-            const float x = key_to_float((uint32_t)sorted[f]);
-            finish((int)~(uint32_t)(sorted[f] >> 32), (float)(weight(x) / total),
-                   (float)((x == m ? 1.0 : exp((double)x - (double)m)) / raw_all), kept);
+            if (f >= SP_LIST)
+              for (int q = 0; q < SP_WARPS; ++q) f = f >= SP_LIST ? sh.isum[1][q] : max(f, sh.isum[1][q]);
+            const float x = key_to_float((uint32_t)(list[f] >> 32));
+            finish((int)(uint32_t)list[f], (float)(weight(x) / total),
+                   (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
           }
         }
       }
@@ -473,15 +590,20 @@ sample_kernel(const SampleParams p) {
       cl.sync();                                         // last round's readers of this histogram are done
       for (int i = tid; i < 256; i += SP_THREADS) sh.hist[b][i] = 0;
       __syncthreads();
-      every([&](float x, int) {
-        const uint32_t k = key_of(x);
-        if (k > BOTTOM && (shift + 8 >= KEY_BITS || (k >> (shift + 8)) == prefix)) atomicAdd(&sh.hist[b][(k >> shift) & 255u], 1);
-      });
+      for (int i = tid; i < n_vec; i += SP_THREADS) {
+        float x[EPC];
+        unpack_logits<T>(vecs[i], x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          const uint32_t k = key_of(x[e]);
+          if (k > BOTTOM && (shift + 8 >= KEY_BITS || (k >> (shift + 8)) == prefix)) atomicAdd(&sh.hist[b][(k >> shift) & 255u], 1);
+        }
+      }
       cl.sync();
       if (tid < 256) {
-        int s = 0;
-        for (int q = 0; q < nc; ++q) s += cl.map_shared_rank(&sh, q)->hist[b][tid];
-        sh.hist[b ^ 1][tid] = s;                         // combined counts: private to this CTA until the next round
+        int c = 0;
+        for (int q = 0; q < nc; ++q) c += cl.map_shared_rank(&sh, q)->hist[b][tid];
+        sh.hist[b ^ 1][tid] = c;                         // combined counts: private to this CTA until the next round
       }
       __syncthreads();
       if (tid == 0) {
@@ -499,122 +621,177 @@ sample_kernel(const SampleParams p) {
     T_key = prefix; quota = need;
     cl.sync();
   }
-  // ---- top-p: weight of the tokens above a key, within the top-k set ----
-  auto weight_from = [&](uint32_t k0, int& c) -> double {
-    double s = 0.0;
-    int n_in = 0;
-    every([&](float x, int) {
-      const uint32_t k = key_of(x);
-      if (k >= k0 && k > BOTTOM) { s += weight(x); ++n_in; }
-    });
-    c = n_in;
-    return cluster_sum(cl, sh, turn, s, c);
+  // ---- top-p: weight of the tokens from a key up ----
+  auto weights_from = [&](uint32_t k1, uint32_t k2, uint32_t k3, double (&s)[3]) {
+    const float t1 = key_value(k1), t2 = key_value(k2), t3 = key_value(k3);      // no logit reaches a NaN
+    s[0] = s[1] = s[2] = 0.0;
+    for (int i = tid; i < n_vec; i += SP_THREADS) {
+      const uint4 raw = vecs[i];
+      if (!(largest_of<T>(raw) >= t1)) continue;
+      float x[EPC];
+      unpack_logits<T>(raw, x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e)
+        if (x[e] >= t1) {
+          const double w = weight(x[e]);
+          s[0] += w;
+          s[1] += x[e] >= t2 ? w : 0.0;
+          s[2] += x[e] >= t3 ? w : 0.0;
+        }
+    }
+    int none = 0;
+    sum_all<3>(cl, sh, turn, s, none);
   };
-  auto key_weight = [&](uint32_t k) -> double { return weight(key_value(k)); };
   if (cut_p) {
-    int c;
-    const double all = weight_from(T_key + 1, c) + (quota ? (double)quota * key_weight(T_key) : 0.0);
-    const double target = (double)p.top_p * all;
+    double s3[3];
+    const double w_at = quota ? weight(key_value(T_key)) : 0.0;
+    weights_from(T_key + 1, T_key + 1, T_key + 1, s3);
+    const double target = (double)p.top_p * (s3[0] + (double)quota * w_at);
+    double above = 0.0;                                  // weight of the keys from best + 2^sft up
     uint32_t best = 0;
-    for (int bit = KEY_BITS - 1; bit >= 0; --bit) {
-      const uint32_t k = best | (1u << bit);
-      if (k <= T_key) { best = k; continue; }            // everything from T_key down is in: enough by definition
-      if (weight_from(k, c) >= target) best = k;
+    for (int sft = KEY_BITS; sft > 0;) {
+      sft -= 2;
+      const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
+      // thresholds down to T_key hold everything that is left, which is enough by definition
+      if (t3 <= T_key) { best = t3; continue; }
+      weights_from(max(t1, T_key + 1), max(t2, T_key + 1), t3, s3);
+      if (s3[2] >= target) best = t3;
+      else if (t2 <= T_key || s3[1] >= target) { best = t2; above = s3[2]; }
+      else if (t1 <= T_key || s3[0] >= target) { best = t1; above = s3[1]; }
+      else above = s3[0];
     }
-    if (best > T_key) {
-      // tokens above `best` do not reach the target, those at it do
-      int c_gt, c_ge;
-      const double w_gt = weight_from(best + 1, c_gt);
-      (void)weight_from(best, c_ge);
-      const double q = ceil((target - w_gt) / key_weight(best));
-      T_key = best;
-      quota = (int)fmin(fmax(q, 1.0), (double)(c_ge - c_gt));
-    } else if (quota) {
-      const double w_gt = weight_from(T_key + 1, c);
-      const double q = ceil((target - w_gt) / key_weight(T_key));
-      quota = (int)fmin(fmax(q, 1.0), (double)quota);
-    }
+    const uint32_t t = max(best, T_key);
+    const double need = ceil((target - above) / weight(key_value(t)));
+    const int most = t == T_key ? quota : INT_MAX;
+    if (t > T_key || quota) { T_key = t; quota = (int)fmin(fmax(need, 1.0), (double)most); }
   }
   // ---- kept weight of every warp's segment, in index order ----
   const double min_w = (double)p.min_p;
-  const double w_T = quota ? key_weight(T_key) : 0.0;
+  const double w_T = quota ? weight(key_value(T_key)) : 0.0;
   const bool tie_in = quota > 0 && w_T >= min_w;
-  const int seg = ((p.slice + SP_WARPS - 1) / SP_WARPS + 31) / 32 * 32;
-  const int s0 = min(warp * seg, cnt), s1 = min(s0 + seg, cnt);
+  constexpr int SEG_UNIT = 32 * EPC;
+  const int seg = (p.slice + SP_WARPS * SEG_UNIT - 1) / (SP_WARPS * SEG_UNIT) * SEG_UNIT;
+  const int s0 = min(warp * seg, n_vec * EPC), s1 = min(s0 + seg, n_vec * EPC);   // whole vectors; the padding is -inf
   {
-    double s = 0.0;
+    double s[2] = {0.0, 0.0};
     int ngt = 0, neq = 0;
-    for (int i = s0 + lane; i < s1; i += 32) {
-      const float x = load_as_float(xs + i);
-      const uint32_t k = key_of(x);
-      if (k > T_key) {
-        const double w = weight(x);
-        if (w >= min_w) { s += w; ++ngt; }
-      } else if (k == T_key && k > BOTTOM) {
-        ++neq;
+    if (T_key == BOTTOM && min_w == 0.0 && plain) {      // no cut at all: every candidate, without a branch
+      for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
+        float x[EPC];
+        unpack_logits<T>(vecs[i], x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          s[e & 1] += weight_plain(x[e]);
+          ngt += x[e] > -INFINITY ? 1 : 0;
+        }
+      }
+    } else {
+      const float t = key_value(T_key), t_all = T_key == BOTTOM ? -INFINITY : t;
+      for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
+        const uint4 raw = vecs[i];
+        if (!(largest_of<T>(raw) >= t_all)) continue;
+        float x[EPC];
+        unpack_logits<T>(raw, x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          if (x[e] > t_all) {
+            const double w = weight(x[e]);
+            if (w >= min_w) { s[0] += w; ++ngt; }
+          } else if (T_key > BOTTOM && x[e] == t) {
+            ++neq;
+          }
+        }
       }
     }
+    s[0] += s[1];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      ngt += __shfl_xor_sync(0xffffffffu, ngt, o);
-      neq += __shfl_xor_sync(0xffffffffu, neq, o);
-    }
-    if (lane == 0) { sh.seg[warp].w = s; sh.seg[warp].n_gt = ngt; sh.seg[warp].n_eq = neq; }
+    for (int o = 16; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+    ngt = __reduce_add_sync(0xffffffffu, ngt);
+    neq = __reduce_add_sync(0xffffffffu, neq);
+    if (lane == 0) { sh.seg[warp].w = s[0]; sh.seg[warp].n_gt = ngt; sh.seg[warp].n_eq = neq; }
   }
-  // sum at temperature 1 over the whole vocabulary (an output value, fp32 terms)
-  double raw = 0.0;
-  if (p.prob && !have_raw) {
-    float part = 0.f;
-    every([&](float x, int) { part += x == m ? 1.f : (x > -INFINITY ? expf(x - m) : 0.f); });
-    raw = part;
+  {
+    double raw[1] = {p.prob && !have_raw ? raw_sum() : 0.0};
+    int none = 0;
+    sum_all<1>(cl, sh, turn, raw, none);                 // its barrier publishes seg[] as well
+    if (!have_raw) raw_all = raw[0];
   }
-  int dummy = 0;
-  raw = cluster_sum(cl, sh, turn, raw, dummy);           // its barrier publishes seg[] as well
-  if (have_raw) raw = raw_all;
-  // ---- the segment that holds u * total ----
-  if (tid < nc * SP_WARPS) sh.all[tid] = cl.map_shared_rank(&sh, tid / SP_WARPS)->seg[tid % SP_WARPS];
-  __syncthreads();
-  if (tid == 0) {
-    double total = 0.0;
-    int eq_left = tie_in ? quota : 0, kept = 0;
-    for (int q = 0; q < nc * SP_WARPS; ++q) {
-      const int e = min(sh.all[q].n_eq, eq_left);
-      eq_left -= e;
-      total += sh.all[q].w + e * w_T;
-      kept += sh.all[q].n_gt + e;
-    }
-    const double target = (double)u * total;
-    double run = 0.0, before = 0.0;
-    int hit = -1, hit_eq = 0;
-    eq_left = tie_in ? quota : 0;
-    for (int q = 0; q < nc * SP_WARPS; ++q) {
-      const int e = min(sh.all[q].n_eq, eq_left);
-      const double sw = sh.all[q].w + e * w_T;
-      if (sw > 0.0) { hit = q; hit_eq = eq_left; before = run; }       // so far the last segment with a weight
-      if (run + sw > target) break;
-      run += sw;
-      eq_left -= e;
-    }
-    sh.hit = hit; sh.hit_eq = hit_eq; sh.before = before; sh.total = total; sh.kept = kept;
+  // ---- the segment that holds u * total: four segments per lane of one warp ----
+  if (tid < SP_MAX_CLUSTER * SP_WARPS) {
+    SegSum q; q.w = 0.0; q.n_gt = 0; q.n_eq = 0;
+    if (tid < nc * SP_WARPS) q = cl.map_shared_rank(&sh, tid / SP_WARPS)->seg[tid % SP_WARPS];
+    sh.all[tid] = q;
   }
   __syncthreads();
-  const int hit = sh.hit, hit_eq = sh.hit_eq, kept = sh.kept;
-  const double mine_before = sh.before, total = sh.total, target = (double)u * total;
-  if (hit == rank * SP_WARPS + warp) {
+  if (warp == 0) {
+    constexpr int PER = SP_MAX_CLUSTER * SP_WARPS / 32;
+    int eq = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) eq += sh.all[lane * PER + q].n_eq;
+    int eq_inc = eq;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, eq_inc, o);
+      if (lane >= o) eq_inc += y;
+    }
+    int left = max((tie_in ? quota : 0) - (eq_inc - eq), 0), kept = 0, left_at[PER];
+    double sw[PER], run = 0.0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const SegSum& a = sh.all[lane * PER + q];
+      const int e = min(a.n_eq, left);
+      left_at[q] = left;
+      left -= e;
+      sw[q] = a.w + e * w_T;
+      run += sw[q];
+      kept += a.n_gt + e;
+    }
+    double inc = run;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    const double total = __shfl_sync(0xffffffffu, inc, 31), target = (double)u * total;
+    kept = __reduce_add_sync(0xffffffffu, kept);
+    double before = inc - run;
+    int first = INT_MAX, last = -1;
+    double first_before = 0.0, last_before = 0.0;
+    int first_left = 0, last_left = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      if (sw[q] > 0.0) {
+        last = lane * PER + q; last_before = before; last_left = left_at[q];
+        if (first == INT_MAX && before + sw[q] > target) { first = last; first_before = before; first_left = left_at[q]; }
+      }
+      before += sw[q];
+    }
+    const int hit = (int)__reduce_min_sync(0xffffffffu, (unsigned)first), end = __reduce_max_sync(0xffffffffu, last);
+    // rounding at the far end: the last segment with a weight
+    const bool own = hit != INT_MAX ? first == hit : last == end;
+    if (own && (hit != INT_MAX || last >= 0)) {
+      sh.hit = hit != INT_MAX ? first : last;
+      sh.before = hit != INT_MAX ? first_before : last_before;
+      sh.hit_eq = hit != INT_MAX ? first_left : last_left;
+    }
+    if (lane == 0) { sh.total = total; sh.kept = kept; }
+  }
+  __syncthreads();
+  const int hit_eq = sh.hit_eq, kept = sh.kept;
+  const double total = sh.total, target = (double)u * total;
+  if (sh.hit == rank * SP_WARPS + warp) {
     // walk of the segment, 32 consecutive tokens at a time
-    double before = mine_before;
-    int eq = hit_eq, tok = -1, fallback = -1;
+    double before = sh.before;
+    int eq = tie_in ? hit_eq : 0, tok = -1, fallback = -1;
     for (int i0 = s0; i0 < s1 && tok < 0; i0 += 32) {
       const int i = i0 + lane;
-      float x = -INFINITY;
-      if (i < s1) x = load_as_float(xs + i);
-      const uint32_t k = i < s1 ? key_of(x) : 0u;
-      const bool is_eq = i < s1 && k == T_key && k > BOTTOM;
+      const float x = i < s1 ? load_as_float(xs + i) : -INFINITY;
+      const uint32_t k = key_of(x);
+      const bool is_eq = k == T_key && k > BOTTOM;
       const uint32_t eq_mask = __ballot_sync(0xffffffffu, is_eq);
       double w = 0.0;
       bool in = false;
-      if (i < s1 && k > T_key) { w = weight(x); in = w >= min_w; }
+      if (k > T_key && x > -INFINITY) { w = weight(x); in = w >= min_w; }
       else if (is_eq) { in = __popc(eq_mask & ((1u << lane) - 1u)) < eq; w = w_T; }
       if (!in) w = 0.0;
       eq -= min(eq, __popc(eq_mask));
@@ -631,9 +808,9 @@ sample_kernel(const SampleParams p) {
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
     if (tok < 0) tok = fallback;
-    if (lane == 0) {
+    if (lane == 0 && tok >= 0) {
       const float x = load_as_float(xs + tok);
-      finish(lo + tok, (float)(weight(x) / total), (float)((x == m ? 1.0 : exp((double)x - (double)m)) / raw), kept);
+      finish(lo + tok, (float)(weight(x) / total), (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
     }
   }
   cl.sync();                                             // nobody leaves while its shared memory may still be read
@@ -650,7 +827,7 @@ focus_status launch_sample(focus_ctx* ctx, SampleParams& p, cudaStream_t st) {
     nc *= 2;
   p.slice = ((p.vocab + nc - 1) / nc + EPC - 1) / EPC * EPC;
   if ((size_t)p.slice * sizeof(T) > SP_SLICE_BYTES) return FOCUS_ERR_UNSUPPORTED;
-  const size_t smem = (((size_t)p.slice * sizeof(T) + 15) & ~size_t(15)) + SP_SCRATCH;
+  const size_t smem = (size_t)p.slice * sizeof(T) + SP_SCRATCH;
   bool& attr_set = ctx->ls.sample_attr_set[sizeof(T) == 2];
   if (!attr_set) {
     if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SP_SLICE_BYTES + SP_SCRATCH) != cudaSuccess)
