@@ -27,7 +27,7 @@ struct focus_ctx {
   // launch state that belongs to the device (function attributes, occupancy answers): kept per context, since a
   // process may hold contexts on several devices.  Zero-initialised by focus_create.
   struct LaunchState {
-    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[2], quant_attr_set[4];
+    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[4], quant_attr_set[4];
     int sink_attr_smem;
     int cluster_cap[9], cluster_cap_w[9], cluster_cap_k[9];   // co-resident clusters per cluster size, value + 1 (0 = not asked yet)
     int select_cluster;                        // 0 not tried, 1 works, 2 the cluster launch was refused once

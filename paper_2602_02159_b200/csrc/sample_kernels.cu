@@ -32,11 +32,11 @@ constexpr int SP_SLICE_BYTES = 180 * 1024;               // largest slice of a r
 constexpr int SP_LIST = 2048;                            // most tokens of a short list
 constexpr int SP_LIST_K = 1024;                          // largest top-k that goes through it; tokens tried for a nucleus
 constexpr int SP_PER = SP_LIST / SP_THREADS;             // tokens of the list per thread
-// scratch behind the slice: list (before it: the cluster's thread maxima) | one byte per 16-byte vector | thread maxima
-constexpr int SP_OFF_MASK = SP_LIST * 8, SP_OFF_MAX = SP_OFF_MASK + 14 * 1024, SP_SCRATCH = SP_OFF_MAX + SP_THREADS * 4;
+// scratch behind the slice: thread maxima | list | one byte per 16-byte vector of the slice
+constexpr int SP_OFF_LIST = SP_THREADS * 4, SP_OFF_MASK = SP_OFF_LIST + SP_LIST * 8, SP_SMEM = 212 * 1024;   // largest, all told
 constexpr int SP_TAB = 1024;                             // entries of the table of powers
 constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN is below it
-static_assert(SP_MAX_CLUSTER * SP_THREADS * 4 <= SP_OFF_MASK && SP_SLICE_BYTES / 16 + 4 <= SP_OFF_MAX - SP_OFF_MASK, "scratch");
+static_assert(SP_SLICE_BYTES + SP_OFF_MASK + SP_SLICE_BYTES / 16 + 16 <= SP_SMEM, "scratch");
 
 struct SegSum {            // one warp's contiguous segment of the row
   double w;                // kept weight above the threshold key
@@ -55,13 +55,14 @@ struct SampleShared {
   int list_n, list_ok;
   int hist[2][256];
   int scan_i[33];
-  double scan[SP_WARPS];
+  unsigned long long fx[2][SP_WARPS][3];
+  int last[SP_WARPS];
   int digit, above, found;
   // the segment that holds u * total
   int hit, hit_eq, kept;
   double before, total;
 };
-static_assert(sizeof(SampleShared) <= 15 * 1024 && SP_SLICE_BYTES + SP_SCRATCH + 15 * 1024 <= 227 * 1024, "shared memory");
+static_assert(sizeof(SampleShared) <= 15 * 1024 && SP_SMEM + 15 * 1024 <= 227 * 1024, "shared memory");
 
 struct SampleParams {
   const void* logits;
@@ -80,8 +81,8 @@ struct SampleParams {
 };
 
 // Sums over the cluster, the same in every thread.  Two slots in turn: one cluster barrier per call is enough, since a
-// CTA writes a slot again only after a barrier that its slowest reader has passed.  CTA = true: of this CTA alone.
-template <int N, bool CTA = false>
+// CTA writes a slot again only after a barrier that its slowest reader has passed.
+template <int N>
 __device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh, int& turn, double (&v)[N], int& cnt) {
   const int t = turn & 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ++turn;
@@ -97,7 +98,7 @@ __device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh,
     sh.isum[t][warp] = cnt;
   }
   __syncthreads();
-  if (CTA || warp == 0) {                                // the warps' sums in a fixed tree
+  if (warp == 0) {                                       // the warps' sums in a fixed tree
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = lane < SP_WARPS ? sh.dsum[t][lane][i] : 0.0;
     cnt = lane < SP_WARPS ? sh.isum[t][lane] : 0;
@@ -111,7 +112,6 @@ __device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh,
     for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
     cnt = __shfl_sync(0xffffffffu, cnt, 0);
   }
-  if (CTA) return;
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) sh.cta_d[t][i] = v[i];
@@ -187,49 +187,202 @@ __device__ __forceinline__ double pow2_near(double t, const double* tab) {
   return __hiloint2double(__double2hiint(w) + ((n >> 10) << 20), __double2loint(w));
 }
 
-// The k-th largest (1 <= k <= n) of the keys get(0), get(1), ..., 8-bit digits from the top, BITS of the key in use;
-// k becomes its place among the keys equal to it.  Every thread of the block calls it.
-template <int BITS, typename Get>
-__device__ __forceinline__ uint32_t block_kth(SampleShared& sh, int n, int& k, Get get) {
-  uint32_t prefix = 0;
-  for (int shift = BITS - 8; shift >= 0; shift -= 8) {
-    int* hist = sh.hist[(shift >> 3) & 1];
-    for (int i = threadIdx.x; i < 256; i += SP_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += SP_THREADS) {
-      const uint32_t q = get(i);
-      if (shift + 8 >= BITS || (q >> (shift + 8)) == prefix) atomicAdd(&hist[(q >> shift) & 255u], 1);
+// Sums over the first NW warps of a block (all of them call it) of numbers below 2^53: integer weights, so that a
+// warp's sum is two hardware reductions of 27-bit halves instead of five rounds of shuffles.  Two slots in turn: one
+// barrier per call.
+__device__ __forceinline__ unsigned long long warp_sum_fx(unsigned long long v) {
+  const unsigned lo = __reduce_add_sync(0xffffffffu, (unsigned)(v & 0x7FFFFFFu)), hi = __reduce_add_sync(0xffffffffu, (unsigned)(v >> 27));
+  return ((unsigned long long)hi << 27) + lo;
+}
+template <int NW, int N>
+__device__ __forceinline__ void sum_fx(SampleShared& sh, int& turn, unsigned long long (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = warp_sum_fx(v[i]);
+  if constexpr (NW > 1) {
+    const int t = turn & 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    ++turn;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sh.fx[t][warp][i] = v[i];
     }
     __syncthreads();
-    if (threadIdx.x < 32) {                              // digits from the largest down, eight per lane
-      const int lane = threadIdx.x;
-      int c[8], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { c[i] = hist[255 - (lane * 8 + i)]; sum += c[i]; }
-      int inc = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-      }
-      int run = inc - sum;
-      if (run < k && inc >= k) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (run < k && run + c[i] >= k) { sh.digit = 255 - (lane * 8 + i); sh.above = run; }
-          run += c[i];
-        }
-      }
+    for (int i = 0; i < N; ++i) {
+      // the halves of a warp's sum: below 2^32 and 2^31, so they are summed in 16-bit steps too
+      const unsigned long long w = lane < NW ? sh.fx[t][lane][i] : 0ull;
+      v[i] = warp_sum_fx(w & 0x3FFFFFFFFFFFFFull) + ((unsigned long long)__reduce_add_sync(0xffffffffu, (unsigned)(w >> 54)) << 54);
     }
-    __syncthreads();
-    prefix = (prefix << 8) | (uint32_t)sh.digit;
-    k -= sh.above;
   }
-  return prefix;
+}
+// Exclusive prefix over those warps' threads; `total` over all of them.
+template <int NW>
+__device__ __forceinline__ unsigned long long excl_fx(SampleShared& sh, int& turn, unsigned long long v, unsigned long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned long long inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  unsigned long long before = inc - v;
+  total = __shfl_sync(0xffffffffu, inc, 31);
+  if constexpr (NW > 1) {
+    const int t = turn & 1;
+    ++turn;
+    if (lane == 0) sh.fx[t][warp][0] = total;
+    __syncthreads();
+    unsigned long long sum = 0;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      if (q == warp) before += sum;
+      sum += sh.fx[t][q][0];
+    }
+    total = sum;
+  }
+  return before;
+}
+// The largest t such that what(t) = the sum over the threads of f(t) reaches `goal`, searched two bits per step among the
+// keys that share the bits of `hi` above `vary` (even); what(lowest of them) reaches it by assumption.  `above`: what(t + 1).
+template <int NW, typename F>
+__device__ __forceinline__ uint32_t largest_reaching(SampleShared& sh, int& turn, uint32_t hi, int vary, unsigned long long goal,
+                                                     unsigned long long& above, F f) {
+  uint32_t best = vary >= 32 ? 0u : hi >> vary << vary;
+  above = 0ull;
+  for (int sft = vary; sft > 0;) {
+    sft -= 2;
+    const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
+    unsigned long long s[3];
+    f(t1, t2, t3, s);
+    sum_fx<NW, 3>(sh, turn, s);
+    if (s[2] >= goal) best = t3;
+    else if (s[1] >= goal) { best = t2; above = s[2]; }
+    else if (s[0] >= goal) { best = t1; above = s[1]; }
+    else above = s[0];
+  }
+  return best;
+}
+__device__ __forceinline__ int even_bits(uint32_t differ) { return (33 - __clz(differ)) & ~1; }
+
+constexpr double FX_ONE = 1125899906842624.0;            // 2^50: a weight of 1 (a thread holds at most four)
+
+struct Draw {                                            // what a list is cut by
+  int top_k;                                             // 0: no cut
+  double top_p, z, min_p, u;                             // top_p 1: no cut; z: weight of the whole vocabulary, or < 0: the list's
+  uint32_t key_lo;                                       // no key of the list is below
+  bool complete;                                         // the list holds every candidate
+};
+// Cuts the list of n <= NW * 32 * SP_PER tokens (descending priority: key, then place) and draws.  Returns the place of the
+// token drawn in `at` (on the thread that holds it; -1 elsewhere), or false where the nucleus reaches beyond the list.
+// Called by the first NW warps; a thread's tokens are neighbours.
+template <int NW, int KEY_BITS, typename W>
+__device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned long long* list, int n, uint32_t key_hi, const Draw& d,
+                                               W weight, int& at, double& w_at, double& total_w, int& kept) {
+  const int tid = threadIdx.x;
+  int turn = 0;
+  uint32_t key[SP_PER];
+  unsigned long long fx[SP_PER];
+  unsigned in = 0;                                       // bit q: token q is in
+#pragma unroll
+  for (int q = 0; q < SP_PER; ++q) {
+    const int i = tid * SP_PER + q;
+    const uint32_t full = i < n ? (uint32_t)(list[i] >> 32) : 0u;
+    key[q] = full >> (32 - KEY_BITS);
+    fx[q] = 0ull;
+    if (i < n) {
+      const double w = weight(key_to_float(full));
+      fx[q] = (unsigned long long)__double2ll_rn(w * FX_ONE);
+      if (w > 0.0 && fx[q] == 0ull) fx[q] = 1ull;        // u = 0 draws the first token that has a weight, however small
+      in |= 1u << q;
+    }
+  }
+  const int vary = even_bits(key_hi ^ d.key_lo);
+  // keeps of the tokens at key t the first `quota`, drops those below t
+  auto cut_at = [&](uint32_t t, unsigned long long quota) {
+    unsigned long long eq = 0, all;
+#pragma unroll
+    for (int q = 0; q < SP_PER; ++q) eq += (in >> q & 1u) && key[q] == t ? 1 : 0;
+    unsigned long long before = excl_fx<NW>(sh, turn, eq, all);
+#pragma unroll
+    for (int q = 0; q < SP_PER; ++q) {
+      const bool tie = (in >> q & 1u) && key[q] == t;
+      if (key[q] < t || (tie && before >= quota)) in &= ~(1u << q);
+      before += tie ? 1 : 0;
+    }
+  };
+  if (d.top_k > 0 && d.top_k < n) {
+    unsigned long long above;
+    const uint32_t t = largest_reaching<NW>(sh, turn, key_hi, vary, (unsigned long long)d.top_k, above,
+                                            [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
+      s[0] = s[1] = s[2] = 0ull;
+#pragma unroll
+      for (int q = 0; q < SP_PER; ++q)
+        if (in >> q & 1u) { s[0] += key[q] >= t1; s[1] += key[q] >= t2; s[2] += key[q] >= t3; }
+    });
+    cut_at(t, (unsigned long long)d.top_k - above);
+  }
+  if (d.top_p < 1.0) {
+    unsigned long long a[1] = {0ull};
+#pragma unroll
+    for (int q = 0; q < SP_PER; ++q) a[0] += in >> q & 1u ? fx[q] : 0ull;
+    sum_fx<NW, 1>(sh, turn, a);
+    const double goal_w = d.top_p * (d.z >= 0.0 ? d.z * FX_ONE : (double)a[0]);
+    const unsigned long long goal = (unsigned long long)ceil(goal_w);
+    if (a[0] < goal && !d.complete) return false;
+    if (a[0] >= goal) {
+      unsigned long long above;
+      const uint32_t t = largest_reaching<NW>(sh, turn, key_hi, vary, goal, above,
+                                              [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
+        s[0] = s[1] = s[2] = 0ull;
+#pragma unroll
+        for (int q = 0; q < SP_PER; ++q) {
+          const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
+          s[0] += key[q] >= t1 ? v : 0ull;
+          s[1] += key[q] >= t2 ? v : 0ull;
+          s[2] += key[q] >= t3 ? v : 0ull;
+        }
+      });
+      // how many of the tokens at t it takes (their weight is one number)
+      const double each = rint(weight(key_to_float(KEY_BITS == 32 ? t : t << 16 | (t & 0x8000u ? 0u : 0xFFFFu))) * FX_ONE);
+      const double need = ceil((double)(goal - above) / each);
+      cut_at(t, (unsigned long long)fmin(fmax(need, 1.0), (double)SP_LIST));
+    }
+  }
+  if (d.min_p > 0.0) {
+#pragma unroll
+    for (int q = 0; q < SP_PER; ++q)
+      if (in >> q & 1u)
+        if (!(weight(key_to_float((uint32_t)(list[tid * SP_PER + q] >> 32))) >= d.min_p)) in &= ~(1u << q);
+  }
+  // running sums of the kept weights in index order; the first one above u * total
+  unsigned long long mine = 0ull, total, count;
+#pragma unroll
+  for (int q = 0; q < SP_PER; ++q) mine += in >> q & 1u ? fx[q] : 0ull;
+  unsigned long long run = excl_fx<NW>(sh, turn, mine, total);
+  unsigned long long c1[1] = {(unsigned long long)__popc(in)};
+  sum_fx<NW, 1>(sh, turn, c1);
+  count = c1[0];
+  kept = (int)count;
+  total_w = (double)total / FX_ONE;
+  const unsigned long long target = (unsigned long long)(d.u * (double)total);      // a sum above u * total is one above its floor
+  const bool has = mine > 0ull && run <= target && run + mine > target;             // one thread, as u < 1
+  at = -1;
+  w_at = 0.0;
+  if (has) {
+#pragma unroll
+    for (int q = 0; q < SP_PER; ++q) {
+      const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
+      if (at < 0 && run + v > target) at = tid * SP_PER + q;
+      run += v;
+    }
+  }
+  if (at >= 0) w_at = weight(key_to_float((uint32_t)(list[at] >> 32)));
+  return true;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(SP_THREADS)
+// STREAM: one CTA per row, every pass reads the logits from global memory (the second and later ones from L2) instead of
+// from a copy in shared memory, and there is no cluster to wait for.
+template <typename T, bool STREAM>
+__global__ void __launch_bounds__(SP_THREADS, 2)
 sample_kernel(const SampleParams p) {
   constexpr int EPC = 16 / sizeof(T);
   constexpr int KEY_BITS = 8 * sizeof(T);                // bf16: the upper half of the float key tells all keys apart
@@ -261,13 +414,28 @@ sample_kernel(const SampleParams p) {
   // ---- the slice (NaN as -inf, padded to whole vectors with -inf), the maxima of the threads' shares ----
   const int lo = min(rank * p.slice, p.vocab), cnt = min(p.slice, p.vocab - lo), n_vec = (cnt + EPC - 1) / EPC;
   const T* row = (const T*)p.logits + (long long)(pos - p.pos_base) * p.row_stride + lo;
-  uint8_t* scratch = smem_raw + (size_t)p.slice * sizeof(T);
+  uint8_t* scratch = smem_raw + (STREAM ? 0 : (size_t)p.slice * sizeof(T));
+  // the one vector that the row ends in, beyond its end -inf
+  auto tail_vector = [&](int i) -> uint4 {
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t a = i + 2 * q < cnt ? __bfloat16_as_ushort(row[i + 2 * q]) : 0xFF80u;
+        const uint32_t b = i + 2 * q + 1 < cnt ? __bfloat16_as_ushort(row[i + 2 * q + 1]) : 0xFF80u;
+        w[q] = a | (b << 16);
+      } else {
+        w[q] = i + q < cnt ? __float_as_uint(row[i + q]) : 0xFF800000u;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  };
   float share = -INFINITY;
   int n_cand = 0;
   auto take = [&](uint4 raw, int i) {
     float hi, low;
     clean_logits<T>(raw, hi, low);
-    *reinterpret_cast<uint4*>(xs + i) = raw;
+    if constexpr (!STREAM) *reinterpret_cast<uint4*>(xs + i) = raw;
     share = fmaxf(share, hi);
     if (low > -INFINITY) {
       n_cand += EPC;
@@ -289,20 +457,7 @@ sample_kernel(const SampleParams p) {
       for (int q = 0; q < U; ++q) take(raw[q], i + q * STEP);
     }
     for (; i + EPC <= cnt; i += STEP) take(__ldg(reinterpret_cast<const uint4*>(row + i)), i);
-    if (i < cnt) {                                       // the one vector that the row ends in
-      uint32_t w[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if constexpr (sizeof(T) == 2) {
-          const uint32_t a = i + 2 * q < cnt ? __bfloat16_as_ushort(row[i + 2 * q]) : 0xFF80u;
-          const uint32_t b = i + 2 * q + 1 < cnt ? __bfloat16_as_ushort(row[i + 2 * q + 1]) : 0xFF80u;
-          w[q] = a | (b << 16);
-        } else {
-          w[q] = i + q < cnt ? __float_as_uint(row[i + q]) : 0xFF800000u;
-        }
-      }
-      take(make_uint4(w[0], w[1], w[2], w[3]), i);
-    }
+    if (i < cnt) take(tail_vector(i), i);
   }
   for (int i = tid; i < SP_TAB; i += SP_THREADS) {       // 2^(i / 1024) as the product of its binary digits' powers
     const double f[10] = {1.0006771306930664, 1.0013547198921082, 1.0027112750502025, 1.0054299011128027, 1.0108892860517005,
@@ -312,7 +467,7 @@ sample_kernel(const SampleParams p) {
     for (int q = 0; q < 10; ++q) v *= (i >> q & 1) ? f[q] : 1.0;
     sh.tab[i] = v;
   }
-  uint32_t* share_key = reinterpret_cast<uint32_t*>(scratch + SP_OFF_MAX);
+  uint32_t* share_key = reinterpret_cast<uint32_t*>(scratch);
   share_key[tid] = float_key(share) >> (32 - KEY_BITS);
   float m = share;
 #pragma unroll
@@ -352,13 +507,26 @@ sample_kernel(const SampleParams p) {
     if (KEY_BITS < 32 && !(full & 0x80000000u)) full |= 0xFFFFu;
     return key_to_float(full);
   };
-  const uint4* vecs = reinterpret_cast<const uint4*>(xs);
+  auto vec = [&](int i) -> uint4 {                       // vector i, NaN as -inf
+    if constexpr (STREAM) {
+      uint4 raw = (i + 1) * EPC <= cnt ? __ldg(reinterpret_cast<const uint4*>(row + i * EPC)) : tail_vector(i * EPC);
+      float a, b;
+      clean_logits<T>(raw, a, b);
+      return raw;
+    } else {
+      return reinterpret_cast<const uint4*>(xs)[i];
+    }
+  };
+  auto logit = [&](int i) -> float {                     // element i < cnt
+    if constexpr (STREAM) return fmaxf(load_as_float(row + i), -INFINITY);
+    else return load_as_float(xs + i);
+  };
   // f(x of one vector): the sum of f over this thread's share, four running sums
   auto sum_over = [&](auto f) -> double {
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     for (int i = tid; i < n_vec; i += SP_THREADS) {
       float x[EPC];
-      unpack_logits<T>(vecs[i], x);
+      unpack_logits<T>(vec(i), x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) s[e & 3] += f(x[e]);
     }
@@ -371,7 +539,7 @@ sample_kernel(const SampleParams p) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     for (int i = tid; i < n_vec; i += SP_THREADS) {
       float x[EPC];
-      unpack_logits<T>(vecs[i], x);
+      unpack_logits<T>(vec(i), x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
         float y;
@@ -389,12 +557,27 @@ sample_kernel(const SampleParams p) {
   if (((cut_k || cut_p) && want <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
     float from = -FLT_MAX;                               // collect the logits from here up
     if (n_cand > SP_LIST) {
-      uint32_t* keys = reinterpret_cast<uint32_t*>(scratch);
+      uint32_t key[SP_MAX_CLUSTER], least = 0xFFFFFFFFu;
 #pragma unroll
-      for (int q = 0; q < SP_MAX_CLUSTER; ++q)
-        if (q < nc) keys[q * SP_THREADS + tid] = cl.map_shared_rank(share_key, q)[tid];
-      int k = want;
-      const uint32_t kth = block_kth<KEY_BITS>(sh, groups, k, [&](int i) { return keys[i]; });
+      for (int q = 0; q < SP_MAX_CLUSTER; ++q) {
+        key[q] = 0u;
+        if (q < nc) { key[q] = cl.map_shared_rank(share_key, q)[tid]; least = min(least, key[q]); }
+      }
+      least = __reduce_min_sync(0xffffffffu, least);
+      if (tid == 0) sh.digit = -1;
+      __syncthreads();
+      if (lane == 0) atomicMin(reinterpret_cast<unsigned*>(&sh.digit), least);
+      __syncthreads();
+      least = (uint32_t)sh.digit;
+      int own_turn = 0;
+      unsigned long long above;
+      const uint32_t kth = largest_reaching<SP_WARPS>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)want, above,
+                                                      [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&c)[3]) {
+        c[0] = c[1] = c[2] = 0ull;
+#pragma unroll
+        for (int q = 0; q < SP_MAX_CLUSTER; ++q)
+          if (q < nc) { c[0] += key[q] >= t1; c[1] += key[q] >= t2; c[2] += key[q] >= t3; }
+      });
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
     double v[2] = {0.0, 0.0};
@@ -406,7 +589,7 @@ sample_kernel(const SampleParams p) {
     for (int i = tid; i < n_words * 4; i += SP_THREADS) {
       uint32_t bits = 0;
       if (i < n_vec) {
-        const uint4 raw = vecs[i];
+        const uint4 raw = vec(i);
         if (largest_of<T>(raw) >= from) {
           float x[EPC];
           unpack_logits<T>(raw, x);
@@ -416,8 +599,8 @@ sample_kernel(const SampleParams p) {
       }
       mask[i] = (uint8_t)bits;
     }
-    __syncthreads();                                     // also: nobody reads the keys any more
-    unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch);
+    __syncthreads();
+    unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch + SP_OFF_LIST);
     const uint32_t* words = reinterpret_cast<const uint32_t*>(mask);
     const int per_w = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per_w, n_words), w1 = min(w0 + per_w, n_words);
     int mine = 0;
@@ -428,7 +611,7 @@ sample_kernel(const SampleParams p) {
       for (int i = w0; i < w1; ++i)
         for (uint32_t b = words[i]; b; b &= b - 1u) {
           const int bit = __ffs(b) - 1, e = (i * 4 + (bit >> 3)) * EPC + (bit & 7);
-          list[at++] = ((unsigned long long)float_key(load_as_float(xs + e)) << 32) | (uint32_t)(lo + e);
+          list[at++] = ((unsigned long long)float_key(logit(e)) << 32) | (uint32_t)(lo + e);
         }
     if (tid == 0) sh.list_n = tot;
     int n_list = tot;
@@ -441,135 +624,35 @@ sample_kernel(const SampleParams p) {
     have_raw = true;
     if (n_list <= SP_LIST) {                             // more: ties at the bound (uniform over the cluster)
       if (rank == 0) {
-        int have = tot;
-        for (int q = 1; q < nc; ++q) {                   // the other slices follow this one: the list stays in index order
-          const int c = cl.map_shared_rank(&sh, q)->list_n;
-          const unsigned long long* src = reinterpret_cast<const unsigned long long*>(cl.map_shared_rank(scratch, q));
-          for (int i = tid; i < c; i += SP_THREADS) list[have + i] = src[i];
-          have += c;
+        // the other slices follow this one: the list stays in index order
+        int c[SP_MAX_CLUSTER], have = tot;
+#pragma unroll
+        for (int q = 1; q < SP_MAX_CLUSTER; ++q) c[q] = q < nc ? cl.map_shared_rank(&sh, q)->list_n : 0;
+#pragma unroll
+        for (int q = 1; q < SP_MAX_CLUSTER; ++q) {
+          if (q < nc) {
+            const unsigned long long* src = cl.map_shared_rank(list, q);
+            for (int i = tid; i < c[q]; i += SP_THREADS) list[have + i] = src[i];
+          }
+          have += c[q];
         }
         __syncthreads();
-        // this thread's tokens: neighbours in index order
-        uint32_t key[SP_PER];
-        double w[SP_PER];
-        bool in[SP_PER];
-#pragma unroll
-        for (int q = 0; q < SP_PER; ++q) {
-          const int i = tid * SP_PER + q;
-          in[q] = i < n_list;
-          const uint32_t full = in[q] ? (uint32_t)(list[i] >> 32) : 0u;
-          key[q] = full >> (32 - KEY_BITS);
-          w[q] = in[q] ? weight(key_to_float(full)) : 0.0;
-        }
-        // keeps of the tokens at key t the first `quota` in index order, drops those below t
-        auto cut_at = [&](uint32_t t, int quota) {
-          int eq = 0, all;
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) eq += in[q] && key[q] == t ? 1 : 0;
-          int before = block_excl_scan(eq, sh.scan_i, all);
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) {
-            const bool at_t = in[q] && key[q] == t;
-            in[q] = in[q] && (key[q] > t || (at_t && before < quota));
-            before += at_t ? 1 : 0;
-          }
-        };
-        if (cut_k) {
-          int k = p.top_k;
-          const uint32_t t = block_kth<KEY_BITS>(sh, n_list, k, [&](int i) { return (uint32_t)(list[i] >> 32) >> (32 - KEY_BITS); });
-          cut_at(t, k);
-        }
+        Draw d;
+        d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = need_z ? v[1] : -1.0; d.min_p = (double)p.min_p; d.u = (double)u;
+        d.key_lo = from == -FLT_MAX ? BOTTOM : key_of(from); d.complete = n_list == n_cand;
+        int at_tok = -1, kept = 0;
+        double w_tok = 0.0, total = 1.0;
         bool whole = true;
-        int dummy = 0, own_turn = 0;                     // sums of this CTA: not in step with the cluster's
-        if (cut_p) {
-          double a[1] = {0.0};
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) a[0] += in[q] ? w[q] : 0.0;
-          sum_all<1, true>(cl, sh, own_turn, a, dummy);
-          const double target = (double)p.top_p * (need_z ? v[1] : a[0]);
-          // a nucleus that reaches beyond the list is found the long way
-          whole = a[0] >= target || n_list == n_cand;
-          if (whole && a[0] >= target) {
-            // the largest key whose tokens, with all above, hold the target: two bits per step below the bits all share
-            const uint32_t k_hi = key_of(m), k_lo = from == -FLT_MAX ? BOTTOM : key_of(from);
-            const int vary = (33 - __clz(k_hi ^ k_lo)) & ~1;      // bits that differ, made even: k_lo <= every key <= k_hi
-            uint32_t best = vary >= 32 ? 0u : k_hi >> vary << vary;
-            double above = 0.0;                          // weight of the keys from best + 2^sft up
-            for (int sft = vary; sft > 0;) {
-              sft -= 2;
-              const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
-              double s3[3] = {0.0, 0.0, 0.0};
-#pragma unroll
-              for (int q = 0; q < SP_PER; ++q) {
-                const double wq = in[q] ? w[q] : 0.0;
-                s3[0] += key[q] >= t1 ? wq : 0.0;
-                s3[1] += key[q] >= t2 ? wq : 0.0;
-                s3[2] += key[q] >= t3 ? wq : 0.0;
-              }
-              sum_all<3, true>(cl, sh, own_turn, s3, dummy);
-              if (s3[2] >= target) best = t3;
-              else if (s3[1] >= target) { best = t2; above = s3[2]; }
-              else if (s3[0] >= target) { best = t1; above = s3[1]; }
-              else above = s3[0];
-            }
-            const double need = ceil((target - above) / weight(key_value(best)));
-            cut_at(best, (int)fmin(fmax(need, 1.0), (double)SP_LIST));
-          }
+        // a short one is cut by one warp, without a barrier
+        if (n_list <= 32 * SP_PER) {
+          if (warp == 0) whole = draw_from_list<1, KEY_BITS>(sh, list, n_list, key_of(m), d, weight, at_tok, w_tok, total, kept);
+        } else {
+          whole = draw_from_list<SP_WARPS, KEY_BITS>(sh, list, n_list, key_of(m), d, weight, at_tok, w_tok, total, kept);
         }
-        if (whole && p.min_p > 0.f) {
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) in[q] = in[q] && w[q] >= (double)p.min_p;
-        }
-        if (tid == 0) { sh.list_ok = whole ? 1 : 0; sh.found = SP_LIST; }
-        if (whole) {
-          // running sums of the kept weights in index order; the first one above u * total
-          double mine_w = 0.0, cum[SP_PER];
-          int kept = 0;
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) {
-            mine_w += in[q] ? w[q] : 0.0;
-            cum[q] = mine_w;
-            kept += in[q] ? 1 : 0;
-          }
-          double inc = mine_w;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
-          }
-          if (lane == 31) sh.scan[warp] = inc;
-          kept = __reduce_add_sync(0xffffffffu, kept);
-          if (lane == 0) sh.isum[0][warp] = kept;
-          __syncthreads();
-          double base = 0.0, total = 0.0;
-          kept = 0;
-#pragma unroll
-          for (int q = 0; q < SP_WARPS; ++q) {
-            if (q == warp) base = total;
-            total += sh.scan[q];
-            kept += sh.isum[0][q];
-          }
-          base += inc - mine_w;
-          const double target = (double)u * total;
-          int first = SP_LIST, last = -1;                // last kept token with a weight: where rounding leaves none above
-#pragma unroll
-          for (int q = SP_PER - 1; q >= 0; --q)
-            if (in[q] && w[q] > 0.0) {
-              if (base + cum[q] > target) first = tid * SP_PER + q;
-              if (last < 0) last = tid * SP_PER + q;
-            }
-          first = (int)__reduce_min_sync(0xffffffffu, (unsigned)first);
-          last = __reduce_max_sync(0xffffffffu, last);
-          if (lane == 0) { sh.isum[1][warp] = last; if (first < SP_LIST) atomicMin(&sh.found, first); }
-          __syncthreads();
-          if (tid == 0) {
-            int f = sh.found;
-            if (f >= SP_LIST)
-              for (int q = 0; q < SP_WARPS; ++q) f = f >= SP_LIST ? sh.isum[1][q] : max(f, sh.isum[1][q]);
-            const float x = key_to_float((uint32_t)(list[f] >> 32));
-            finish((int)(uint32_t)list[f], (float)(weight(x) / total),
-                   (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
-          }
+        if (tid == 0) sh.list_ok = whole ? 1 : 0;
+        if (whole && at_tok >= 0) {
+          const float x = key_to_float((uint32_t)(list[at_tok] >> 32));
+          finish((int)(uint32_t)list[at_tok], (float)(w_tok / total), (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
         }
       }
       cl.sync();                                         // the lists have been read, the outcome is known
@@ -592,7 +675,7 @@ sample_kernel(const SampleParams p) {
       __syncthreads();
       for (int i = tid; i < n_vec; i += SP_THREADS) {
         float x[EPC];
-        unpack_logits<T>(vecs[i], x);
+        unpack_logits<T>(vec(i), x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
           const uint32_t k = key_of(x[e]);
@@ -626,7 +709,7 @@ sample_kernel(const SampleParams p) {
     const float t1 = key_value(k1), t2 = key_value(k2), t3 = key_value(k3);      // no logit reaches a NaN
     s[0] = s[1] = s[2] = 0.0;
     for (int i = tid; i < n_vec; i += SP_THREADS) {
-      const uint4 raw = vecs[i];
+      const uint4 raw = vec(i);
       if (!(largest_of<T>(raw) >= t1)) continue;
       float x[EPC];
       unpack_logits<T>(raw, x);
@@ -678,17 +761,17 @@ sample_kernel(const SampleParams p) {
     if (T_key == BOTTOM && min_w == 0.0 && plain) {      // no cut at all: every candidate, without a branch
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
         float x[EPC];
-        unpack_logits<T>(vecs[i], x);
+        unpack_logits<T>(vec(i), x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          s[e & 1] += weight_plain(x[e]);
+          s[e & 1] += x[e] > floor_x ? weight_plain(x[e]) : 0.0;
           ngt += x[e] > -INFINITY ? 1 : 0;
         }
       }
     } else {
       const float t = key_value(T_key), t_all = T_key == BOTTOM ? -INFINITY : t;
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
-        const uint4 raw = vecs[i];
+        const uint4 raw = vec(i);
         if (!(largest_of<T>(raw) >= t_all)) continue;
         float x[EPC];
         unpack_logits<T>(raw, x);
@@ -785,7 +868,7 @@ sample_kernel(const SampleParams p) {
     int eq = tie_in ? hit_eq : 0, tok = -1, fallback = -1;
     for (int i0 = s0; i0 < s1 && tok < 0; i0 += 32) {
       const int i = i0 + lane;
-      const float x = i < s1 ? load_as_float(xs + i) : -INFINITY;
+      const float x = i < min(s1, cnt) ? logit(i) : -INFINITY;
       const uint32_t k = key_of(x);
       const bool is_eq = k == T_key && k > BOTTOM;
       const uint32_t eq_mask = __ballot_sync(0xffffffffu, is_eq);
@@ -802,35 +885,27 @@ sample_kernel(const SampleParams p) {
         if (lane >= o) inc += y;
       }
       const uint32_t got = __ballot_sync(0xffffffffu, in && before + inc > target);
-      const uint32_t any = __ballot_sync(0xffffffffu, in && w > 0.0);
+      const uint32_t any = __ballot_sync(0xffffffffu, in);
       if (any) fallback = i0 + 31 - __clz(any);
       if (got) tok = i0 + __ffs(got) - 1;
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
     if (tok < 0) tok = fallback;
     if (lane == 0 && tok >= 0) {
-      const float x = load_as_float(xs + tok);
+      const float x = logit(tok);
       finish(lo + tok, (float)(weight(x) / total), (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
     }
   }
   cl.sync();                                             // nobody leaves while its shared memory may still be read
 }
 
-template <typename T>
-focus_status launch_sample(focus_ctx* ctx, SampleParams& p, cudaStream_t st) {
-  constexpr int EPC = 16 / sizeof(T);
-  // cluster size: a slice has to fit in shared memory, and small calls spread a row over more SMs while there are idle
-  // ones and a slice still feeds every thread
-  int nc = 1;
-  while (nc < SP_MAX_CLUSTER && ((long long)p.vocab * sizeof(T) > (long long)nc * SP_SLICE_BYTES / 2 ||
-                                 (p.max_rows * nc * 2 <= ctx->sm_count && p.vocab > nc * SP_THREADS * EPC)))
-    nc *= 2;
-  p.slice = ((p.vocab + nc - 1) / nc + EPC - 1) / EPC * EPC;
-  if ((size_t)p.slice * sizeof(T) > SP_SLICE_BYTES) return FOCUS_ERR_UNSUPPORTED;
-  const size_t smem = (size_t)p.slice * sizeof(T) + SP_SCRATCH;
-  bool& attr_set = ctx->ls.sample_attr_set[sizeof(T) == 2];
+template <typename T, bool STREAM>
+focus_status launch_sample_as(focus_ctx* ctx, const SampleParams& p, int nc, cudaStream_t st) {
+  const size_t n_vec = ((size_t)p.slice * sizeof(T) + 15) / 16;
+  const size_t smem = (STREAM ? 0 : n_vec * 16) + SP_OFF_MASK + ((n_vec + 15) & ~size_t(15));
+  bool& attr_set = ctx->ls.sample_attr_set[(sizeof(T) == 2) * 2 + STREAM];
   if (!attr_set) {
-    if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SP_SLICE_BYTES + SP_SCRATCH) != cudaSuccess)
+    if (cudaFuncSetAttribute(sample_kernel<T, STREAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, SP_SMEM) != cudaSuccess)
       return FOCUS_ERR_CUDA;
     attr_set = true;
   }
@@ -841,9 +916,27 @@ focus_status launch_sample(focus_ctx* ctx, SampleParams& p, cudaStream_t st) {
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = nc; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, sample_kernel<T>, p) != cudaSuccess) { cudaGetLastError(); return FOCUS_ERR_CUDA; }
+  if (cudaLaunchKernelEx(&cfg, sample_kernel<T, STREAM>, p) != cudaSuccess) { cudaGetLastError(); return FOCUS_ERR_CUDA; }
   FOCUS_CHECK_LAUNCH();
   return FOCUS_OK;
+}
+
+template <typename T>
+focus_status launch_sample(focus_ctx* ctx, SampleParams& p, cudaStream_t st) {
+  constexpr int EPC = 16 / sizeof(T);
+  if ((size_t)p.vocab * sizeof(T) > (size_t)SP_MAX_CLUSTER * SP_SLICE_BYTES) return FOCUS_ERR_UNSUPPORTED;
+  // cluster size: a slice has to fit in shared memory, and small calls spread a row over more SMs while there are idle
+  // ones and a slice still feeds every thread
+  int nc = 1;
+  while (nc < SP_MAX_CLUSTER && ((long long)p.vocab * sizeof(T) > (long long)nc * SP_SLICE_BYTES / 2 ||
+                                 (p.max_rows * nc * 2 <= ctx->sm_count && p.vocab > nc * SP_THREADS * EPC)))
+    nc *= 2;
+  if (nc > 1 && p.max_rows >= ctx->sm_count) {           // rows enough for every SM: no slices
+    p.slice = (p.vocab + EPC - 1) / EPC * EPC;
+    return launch_sample_as<T, true>(ctx, p, 1, st);
+  }
+  p.slice = ((p.vocab + nc - 1) / nc + EPC - 1) / EPC * EPC;
+  return launch_sample_as<T, false>(ctx, p, nc, st);
 }
 
 }  // namespace

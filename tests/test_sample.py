@@ -139,6 +139,27 @@ def test_long_rows(ctx, dtype, vocab, max_rows):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 50003), ("f32", 30001)])
+def test_many_rows(ctx, dtype, vocab):
+    """More rows than SMs; every row is the one that a call of a few rows gives, three of them are the oracle's."""
+    rng = np.random.default_rng(vocab)
+    n, stride = 170, (vocab + 7) // 8 * 8
+    x = rng.standard_normal((n, stride)).astype(np.float32) * np.array([0.3, 2.0, 3.5], np.float32)[np.arange(n) % 3, None]
+    x[5, :100], x[6, 11:] = np.nan, -np.inf
+    xs = wl.to_storage(x, dtype)
+    xf = wl.storage_to_f64(xs, dtype)[:, :vocab]
+    u = rng.random(n)
+    for T, k, p, mp in ((0.8, 40, 0.9, 0.02), (0.7, 0, 0.95, 0.0), (1.0, 0, 1.0, 0.0), (1.0, 3000, 1.0, 0.001)):
+        many = run(ctx, xs, dtype, vocab, 0, None, n, T, k, p, mp, u)
+        for lo in range(0, n, 34):
+            few = run(ctx, xs[lo:lo + 34], dtype, vocab, 0, None, 34, T, k, p, mp, u[lo:lo + 34])
+            assert np.array_equal(few[0][:34], many[0][lo:lo + 34]) and np.array_equal(few[3][:34], many[3][lo:lo + 34])
+            assert np.allclose(few[1][:34], many[1][lo:lo + 34], rtol=2 * CONF_TOL, atol=0)
+        check([o[4:7] for o in many], xf[4:7], range(3), T, k, p, mp, u[4:7])
+    assert ctx.poll_status() == 0
+
+
+@gpu
 def test_frequencies_follow_the_distribution(ctx):
     """u = (i + 1/2) / n for i < n: every kept token is drawn as often as its probability says, off by at most one."""
     rng = np.random.default_rng(12)
