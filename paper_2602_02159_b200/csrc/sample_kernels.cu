@@ -8,14 +8,14 @@
 // the answer does not depend on timing or on the number of rows.
 //
 // The kept set is a prefix of the descending order.  Two ways to it:
-//   short list  (up to 2048 tokens: top-k to 1024, most nuclei): the k-th largest of the maxima of the threads' shares is a
-//               lower bound of the k-th largest logit -- that many logits reach it, and few more do.  The logits from there
-//               up are collected in index order and cut by one CTA, which has them in registers.  One pass for the maxima,
-//               one for the list (with the sums over the vocabulary that prob and top-p need).
-//   any length  (no cut, min-p alone, long top-k, flat nuclei): the key T of the last kept logit, by counts (top-k: 8-bit
-//               digits of a radix descent) and by weight (top-p: two bits of the key per pass); (T, how many of the tokens
-//               at T) says all about the set.  Then the kept weight per warp segment in index order, the segment that
-//               holds u * total, and its walk.
+//   short list  (up to 2048 tokens).  Which logits to collect: for top-k up to 1024, those from the k-th largest of the
+//               maxima of the threads' shares up -- a lower bound of the k-th largest logit that few more reach; for a
+//               nucleus, those up to the histogram bin in which it must end.  They are collected in index order and cut by
+//               one CTA (by one warp, if they are at most 128), which has them in registers.
+//   any length  (no cut, min-p alone, longer top-k and nuclei): the key T of the last kept logit, by counts (top-k: 8-bit
+//               digits of a radix descent) and by weight (top-p: two bits of the key per pass, of those that the
+//               histogram leaves open); (T, how many of the tokens at T) says all about the set.  Then the kept weight per
+//               warp segment in index order, the segment that holds u * total, and its walk.
 #include <cooperative_groups.h>
 #include <float.h>
 
@@ -35,7 +35,9 @@ constexpr int SP_PER = SP_LIST / SP_THREADS;             // tokens of the list p
 // scratch behind the slice: thread maxima | list | one byte per 16-byte vector of the slice
 constexpr int SP_OFF_LIST = SP_THREADS * 4, SP_OFF_MASK = SP_OFF_LIST + SP_LIST * 8, SP_SMEM = 212 * 1024;   // largest, all told
 constexpr int SP_TAB = 1024;                             // entries of the table of powers
+constexpr int SP_BINS = 2048, SP_BINS_PER_E = 64;        // histogram of a nucleus: bins, and how many to a factor of e
 constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN is below it
+static_assert(SP_BINS * 4 <= SP_LIST * 8 && SP_BINS == 4 * SP_THREADS, "a histogram lies where a list does");
 static_assert(SP_SLICE_BYTES + SP_OFF_MASK + SP_SLICE_BYTES / 16 + 16 <= SP_SMEM, "scratch");
 
 struct SegSum {            // one warp's contiguous segment of the row
@@ -58,6 +60,7 @@ struct SampleShared {
   unsigned long long fx[2][SP_WARPS][3];
   int last[SP_WARPS];
   int digit, above, found;
+  uint32_t key_hi[SP_WARPS], key_lo[SP_WARPS];
   // the segment that holds u * total
   int hit, hit_eq, kept;
   double before, total;
@@ -550,13 +553,83 @@ sample_kernel(const SampleParams p) {
     return (double)((s[0] + s[1]) + (s[2] + s[3]));
   };
   const bool cut_k = p.top_k > 0 && p.top_k < n_cand, cut_p = p.top_p < 1.f, need_z = cut_p && !cut_k;
-  const int groups = nc * SP_THREADS, want = cut_k ? p.top_k : min(SP_LIST_K, groups / 2);
+  const int groups = nc * SP_THREADS;
   bool have_raw = false;
-  double raw_all = 0.0;
-  // ---- short list (the bound is tight while the k wanted are at most half of the shares) ----
-  if (((cut_k || cut_p) && want <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
+  double raw_all = 0.0, z_all = -1.0;                    // z_all: weight of the vocabulary, where top-p needs it
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch + SP_OFF_LIST);
+  // ---- a nucleus: where does it end, to within a few histogram bins? ----
+  // Bins of 1/64 in the exponent (nearest, the last one open), counted; the weight of a bin lies between those of its
+  // edges, so the running weight is known to +-0.8 %.  Bins before bin_lo are in the nucleus, those after bin_hi are not.
+  const float per_bin = (float)SP_BINS_PER_E / p.temperature;
+  auto bin_of = [&](float x) -> float {                  // as the float 2^23 + bin
+    return fminf((m - x) * per_bin, (float)(SP_BINS - 1)) + 8388608.f;
+  };
+  float reach_bin = 8388608.f + SP_BINS, bin_lo = 0.f, bin_hi = 0.f;      // as 2^23 + bin; tokens to collect: up to reach_bin
+  bool narrowed = false;
+  if (need_z && plain && n_cand > SP_LIST) {
+    int* hist = reinterpret_cast<int*>(list);
+    for (int i = tid; i < SP_BINS; i += SP_THREADS) hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n_vec; i += SP_THREADS) {
+      float x[EPC];
+      unpack_logits<T>(vec(i), x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        const int bin = __float_as_int(bin_of(x[e])) & (SP_BINS - 1);
+        if (bin < SP_BINS - 1) atomicAdd(&hist[bin], 1);             // the last bin is what the others leave
+      }
+    }
+    double v[2] = {p.prob ? raw_sum() : 0.0, sum_over([&](float x) { return x > floor_x ? weight_plain(x) : 0.0; })};
+    int none = 0;
+    sum_all<2>(cl, sh, turn, v, none);                   // publishes the counts as well
+    raw_all = v[0]; z_all = v[1];
+    have_raw = true;
+    constexpr int PER = SP_BINS / SP_THREADS;
+    constexpr float FX = 17179869184.f;                  // 2^34
+    int count[PER] = {};
+    for (int q = 0; q < nc; ++q) {
+      const int4 c = *reinterpret_cast<const int4*>(cl.map_shared_rank(hist, q) + tid * PER);
+      count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
+    }
+    int fx_turn = 0;
+    unsigned long long counted[1] = {(unsigned long long)(count[0] + count[1] + count[2] + count[3])};
+    sum_fx<SP_WARPS, 1>(sh, fx_turn, counted);
+    if (tid == SP_THREADS - 1) count[PER - 1] = n_cand - (int)counted[0];
+    unsigned long long light[PER], heavy[PER], light_sum = 0, heavy_sum = 0, tot;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      // edges half a bin to either side, and a little for the bins' own rounding
+      const float b = (float)(tid * PER + q);
+      const float hi = exp2f(-fmaxf(b - 0.501f, 0.f) * (l2e / SP_BINS_PER_E)) * 1.00002f;
+      const float low = tid * PER + q == SP_BINS - 1 ? 0.f : exp2f(-(b + 0.501f) * (l2e / SP_BINS_PER_E)) * 0.99998f;
+      light[q] = (unsigned long long)count[q] * (unsigned long long)(low * FX);
+      heavy[q] = (unsigned long long)count[q] * ((unsigned long long)(hi * FX) + 1ull);
+      light_sum += light[q]; heavy_sum += heavy[q];
+    }
+    unsigned long long light_at = excl_fx<SP_WARPS>(sh, fx_turn, light_sum, tot), heavy_at = excl_fx<SP_WARPS>(sh, fx_turn, heavy_sum, tot);
+    unsigned long long count_at = excl_fx<SP_WARPS>(sh, fx_turn, (unsigned long long)(count[0] + count[1] + count[2] + count[3]), tot);
+    const double goal = (double)p.top_p * z_all * (double)FX;
+    if (tid == 0) { sh.digit = 0; sh.above = SP_BINS - 1; sh.found = n_cand; }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      // one bin each: the first whose upper sum reaches the goal, and the first whose lower sum does
+      if ((double)heavy_at * 1.0 < goal && (double)(heavy_at + heavy[q]) >= goal) sh.digit = tid * PER + q;
+      count_at += count[q];
+      if ((double)light_at < goal && (double)(light_at + light[q]) >= goal) { sh.above = tid * PER + q; sh.found = (int)count_at; }
+      heavy_at += heavy[q]; light_at += light[q];
+    }
+    __syncthreads();
+    bin_lo = 8388608.f + (float)sh.digit; bin_hi = 8388608.f + (float)sh.above;
+    narrowed = true;
+    if (sh.found <= SP_LIST) reach_bin = bin_hi;         // short enough: its tokens, and a few too many, as a list
+    cl.sync();                                           // everybody has read the counts: the list may go over them
+  }
+  const bool short_nucleus = narrowed && reach_bin == bin_hi;
+  // ---- short list (top-k: the bound is tight while the k wanted are at most half of the shares) ----
+  if (short_nucleus || (cut_k && p.top_k <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
     float from = -FLT_MAX;                               // collect the logits from here up
-    if (n_cand > SP_LIST) {
+    if (n_cand > SP_LIST && cut_k) {
       uint32_t key[SP_MAX_CLUSTER], least = 0xFFFFFFFFu;
 #pragma unroll
       for (int q = 0; q < SP_MAX_CLUSTER; ++q) {
@@ -571,7 +644,7 @@ sample_kernel(const SampleParams p) {
       least = (uint32_t)sh.digit;
       int own_turn = 0;
       unsigned long long above;
-      const uint32_t kth = largest_reaching<SP_WARPS>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)want, above,
+      const uint32_t kth = largest_reaching<SP_WARPS>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k, above,
                                                       [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&c)[3]) {
         c[0] = c[1] = c[2] = 0ull;
 #pragma unroll
@@ -580,9 +653,8 @@ sample_kernel(const SampleParams p) {
       });
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
-    double v[2] = {0.0, 0.0};
-    if (p.prob) v[0] = raw_sum();
-    if (need_z) v[1] = plain ? sum_over(weight_plain) : sum_over([&](float x) { return x > -INFINITY ? weight(x) : 0.0; });
+    auto reaches = [&](float x) -> bool { return x >= from && !(bin_of(x) > reach_bin); };
+    double raw[1] = {p.prob && !have_raw ? raw_sum() : 0.0};
     // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order
     uint8_t* mask = scratch + SP_OFF_MASK;
     const int n_words = (n_vec + 3) >> 2;
@@ -590,17 +662,16 @@ sample_kernel(const SampleParams p) {
       uint32_t bits = 0;
       if (i < n_vec) {
         const uint4 raw = vec(i);
-        if (largest_of<T>(raw) >= from) {
+        if (reaches(largest_of<T>(raw))) {
           float x[EPC];
           unpack_logits<T>(raw, x);
 #pragma unroll
-          for (int e = 0; e < EPC; ++e) bits |= x[e] >= from ? 1u << e : 0u;
+          for (int e = 0; e < EPC; ++e) bits |= reaches(x[e]) ? 1u << e : 0u;
         }
       }
       mask[i] = (uint8_t)bits;
     }
     __syncthreads();
-    unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch + SP_OFF_LIST);
     const uint32_t* words = reinterpret_cast<const uint32_t*>(mask);
     const int per_w = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per_w, n_words), w1 = min(w0 + per_w, n_words);
     int mine = 0;
@@ -615,12 +686,12 @@ sample_kernel(const SampleParams p) {
         }
     if (tid == 0) sh.list_n = tot;
     int n_list = tot;
-    sum_all<2>(cl, sh, turn, v, n_list);                 // publishes the lists as well
+    sum_all<1>(cl, sh, turn, raw, n_list);               // publishes the lists as well
     n_list = 0;
 #pragma unroll
     for (int q = 0; q < SP_MAX_CLUSTER; ++q)
       if (q < nc) n_list += cl.map_shared_rank(&sh, q)->list_n;
-    raw_all = v[0];
+    if (!have_raw) raw_all = raw[0];
     have_raw = true;
     if (n_list <= SP_LIST) {                             // more: ties at the bound (uniform over the cluster)
       if (rank == 0) {
@@ -638,8 +709,10 @@ sample_kernel(const SampleParams p) {
         }
         __syncthreads();
         Draw d;
-        d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = need_z ? v[1] : -1.0; d.min_p = (double)p.min_p; d.u = (double)u;
-        d.key_lo = from == -FLT_MAX ? BOTTOM : key_of(from); d.complete = n_list == n_cand;
+        d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = z_all; d.min_p = (double)p.min_p; d.u = (double)u;
+        // (a logit of the last bin is at most half a bin, and the rounding, below its middle)
+        d.key_lo = short_nucleus ? max(key_of(m - (bin_hi - 8388607.f) / per_bin), BOTTOM) : from == -FLT_MAX ? BOTTOM : key_of(from);
+        d.complete = n_list == n_cand;
         int at_tok = -1, kept = 0;
         double w_tok = 0.0, total = 1.0;
         bool whole = true;
@@ -725,7 +798,67 @@ sample_kernel(const SampleParams p) {
     int none = 0;
     sum_all<3>(cl, sh, turn, s, none);
   };
-  if (cut_p) {
+  if (narrowed) {
+    // the weight before the open bins, and the keys in them; then their bits
+    double base[1];
+    uint32_t k_hi = 0u, k_lo = 0xFFFFFFFFu;
+    double s4[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int i = tid; i < n_vec; i += SP_THREADS) {
+      const uint4 raw = vec(i);
+      if (bin_of(largest_of<T>(raw)) > bin_hi) continue;
+      float x[EPC];
+      unpack_logits<T>(raw, x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        const float b = bin_of(x[e]);
+        s4[e & 3] += b < bin_lo ? weight_plain(x[e]) : 0.0;
+        if (b >= bin_lo && b <= bin_hi && x[e] > -INFINITY) { k_hi = max(k_hi, key_of(x[e])); k_lo = min(k_lo, key_of(x[e])); }
+      }
+    }
+    base[0] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    k_hi = __reduce_max_sync(0xffffffffu, k_hi); k_lo = __reduce_min_sync(0xffffffffu, k_lo);
+    if (lane == 0) { sh.key_hi[warp] = k_hi; sh.key_lo[warp] = k_lo; }
+    int none = 0;
+    sum_all<1>(cl, sh, turn, base, none);                // publishes the keys as well
+    for (int q = lane; q < nc * SP_WARPS; q += 32) {
+      const SampleShared* o = cl.map_shared_rank(&sh, q / SP_WARPS);
+      k_hi = max(k_hi, o->key_hi[q % SP_WARPS]); k_lo = min(k_lo, o->key_lo[q % SP_WARPS]);
+    }
+    k_hi = __reduce_max_sync(0xffffffffu, k_hi); k_lo = __reduce_min_sync(0xffffffffu, k_lo);
+    const double target = (double)p.top_p * z_all;
+    const int vary = even_bits(k_hi ^ k_lo);
+    uint32_t best = vary >= 32 ? 0u : k_hi >> vary << vary;
+    double above = base[0];                              // weight before the bins, and in them from best + 2^sft up
+    for (int sft = vary; sft > 0;) {
+      sft -= 2;
+      const uint32_t t[3] = {best | (1u << sft), best | (2u << sft), best | (3u << sft)};
+      double s3[3] = {0.0, 0.0, 0.0};
+      for (int i = tid; i < n_vec; i += SP_THREADS) {
+        const uint4 raw = vec(i);
+        if (bin_of(largest_of<T>(raw)) > bin_hi) continue;
+        float x[EPC];
+        unpack_logits<T>(raw, x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          const float b = bin_of(x[e]);
+          if (b >= bin_lo && b <= bin_hi) {
+            const uint32_t k = key_of(x[e]);
+            const double w = weight_plain(x[e]);
+            s3[0] += k >= t[0] ? w : 0.0;
+            s3[1] += k >= t[1] ? w : 0.0;
+            s3[2] += k >= t[2] ? w : 0.0;
+          }
+        }
+      }
+      sum_all<3>(cl, sh, turn, s3, none);
+      if (base[0] + s3[2] >= target) best = t[2];
+      else if (base[0] + s3[1] >= target) { best = t[1]; above = base[0] + s3[2]; }
+      else if (base[0] + s3[0] >= target) { best = t[0]; above = base[0] + s3[1]; }
+      else above = base[0] + s3[0];
+    }
+    T_key = best;
+    quota = (int)fmin(fmax(ceil((target - above) / weight(key_value(best))), 1.0), (double)INT_MAX);
+  } else if (cut_p) {
     double s3[3];
     const double w_at = quota ? weight(key_value(T_key)) : 0.0;
     weights_from(T_key + 1, T_key + 1, T_key + 1, s3);
