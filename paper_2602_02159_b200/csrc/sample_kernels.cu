@@ -61,6 +61,7 @@ struct SampleShared {
   int last[SP_WARPS];
   int digit, above, found;
   uint32_t key_hi[SP_WARPS], key_lo[SP_WARPS];
+  float2 edge[SP_WARPS];
   // the segment that holds u * total
   int hit, hit_eq, kept;
   double before, total;
@@ -177,6 +178,12 @@ __device__ __forceinline__ float largest_of(const uint4& raw) {
   }
 }
 
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Powers of two in fp64: t = n / 1024 + r, 2^t = 2^(n >> 10) * tab[n & 1023] * 2^r, the last factor by its Taylor
 // polynomial (Tang's table-driven scheme, 1989).  |r| <= 2^-11, so the square leaves 7e-12 of a weight, of either sign.
 // -1000 <= t <= 0; no branch, so that several run side by side.
@@ -217,6 +224,22 @@ __device__ __forceinline__ void sum_fx(SampleShared& sh, int& turn, unsigned lon
     }
   }
 }
+// The same for three small counts (at most 31 per thread), packed into one word.
+template <int NW>
+__device__ __forceinline__ void sum_counts(SampleShared& sh, int& turn, const unsigned (&c)[3], unsigned long long (&v)[3]) {
+  const unsigned w = __reduce_add_sync(0xffffffffu, c[0] | (c[1] << 10) | (c[2] << 20));
+  if constexpr (NW == 1) {
+    v[0] = w & 1023u; v[1] = (w >> 10) & 1023u; v[2] = w >> 20;
+  } else {
+    const int t = turn & 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    ++turn;
+    if (lane == 0) sh.fx[t][warp][0] = w;
+    __syncthreads();
+    const unsigned x = lane < NW ? (unsigned)sh.fx[t][lane][0] : 0u;
+    const unsigned a = __reduce_add_sync(0xffffffffu, (x & 1023u) | ((x >> 10 & 1023u) << 16));
+    v[0] = a & 0xFFFFu; v[1] = a >> 16; v[2] = __reduce_add_sync(0xffffffffu, x >> 20);
+  }
+}
 // Exclusive prefix over those warps' threads; `total` over all of them.
 template <int NW>
 __device__ __forceinline__ unsigned long long excl_fx(SampleShared& sh, int& turn, unsigned long long v, unsigned long long& total) {
@@ -246,7 +269,7 @@ __device__ __forceinline__ unsigned long long excl_fx(SampleShared& sh, int& tur
 }
 // The largest t such that what(t) = the sum over the threads of f(t) reaches `goal`, searched two bits per step among the
 // keys that share the bits of `hi` above `vary` (even); what(lowest of them) reaches it by assumption.  `above`: what(t + 1).
-template <int NW, typename F>
+template <int NW, bool COUNTS, typename F>
 __device__ __forceinline__ uint32_t largest_reaching(SampleShared& sh, int& turn, uint32_t hi, int vary, unsigned long long goal,
                                                      unsigned long long& above, F f) {
   uint32_t best = vary >= 32 ? 0u : hi >> vary << vary;
@@ -255,8 +278,14 @@ __device__ __forceinline__ uint32_t largest_reaching(SampleShared& sh, int& turn
     sft -= 2;
     const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
     unsigned long long s[3];
-    f(t1, t2, t3, s);
-    sum_fx<NW, 3>(sh, turn, s);
+    if constexpr (COUNTS) {
+      unsigned c[3];
+      f(t1, t2, t3, c);
+      sum_counts<NW>(sh, turn, c, s);
+    } else {
+      f(t1, t2, t3, s);
+      sum_fx<NW, 3>(sh, turn, s);
+    }
     if (s[2] >= goal) best = t3;
     else if (s[1] >= goal) { best = t2; above = s[2]; }
     else if (s[0] >= goal) { best = t1; above = s[1]; }
@@ -314,9 +343,9 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
   };
   if (d.top_k > 0 && d.top_k < n) {
     unsigned long long above;
-    const uint32_t t = largest_reaching<NW>(sh, turn, key_hi, vary, (unsigned long long)d.top_k, above,
-                                            [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
-      s[0] = s[1] = s[2] = 0ull;
+    const uint32_t t = largest_reaching<NW, true>(sh, turn, key_hi, vary, (unsigned long long)d.top_k, above,
+                                                  [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&s)[3]) {
+      s[0] = s[1] = s[2] = 0u;
 #pragma unroll
       for (int q = 0; q < SP_PER; ++q)
         if (in >> q & 1u) { s[0] += key[q] >= t1; s[1] += key[q] >= t2; s[2] += key[q] >= t3; }
@@ -333,7 +362,7 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
     if (a[0] < goal && !d.complete) return false;
     if (a[0] >= goal) {
       unsigned long long above;
-      const uint32_t t = largest_reaching<NW>(sh, turn, key_hi, vary, goal, above,
+      const uint32_t t = largest_reaching<NW, false>(sh, turn, key_hi, vary, goal, above,
                                               [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
         s[0] = s[1] = s[2] = 0ull;
 #pragma unroll
@@ -433,20 +462,30 @@ sample_kernel(const SampleParams p) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   };
-  float share = -INFINITY;
+  const float l2e = 1.4426950408889634f;
+  float share = -INFINITY;                               // largest logit of this thread's share
+  float raw_part = 0.f;                                  // sum of exp(x - share) over it: prob's denominator at temperature 1
   int n_cand = 0;
   auto take = [&](uint4 raw, int i) {
-    float hi, low;
+    float hi, low, x[EPC];
     clean_logits<T>(raw, hi, low);
     if constexpr (!STREAM) *reinterpret_cast<uint4*>(xs + i) = raw;
-    share = fmaxf(share, hi);
+    unpack_logits<T>(raw, x);
     if (low > -INFINITY) {
       n_cand += EPC;
     } else {
-      float x[EPC];
-      unpack_logits<T>(raw, x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) n_cand += x[e] > -INFINITY ? 1 : 0;
+    }
+    if (hi > share) {
+      raw_part *= ex2_approx((share - hi) * l2e);
+      share = hi;
+    }
+    if (p.prob && share > -INFINITY) {
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < EPC; e += 2) { s0 += ex2_approx((x[e] - share) * l2e); s1 += ex2_approx((x[e + 1] - share) * l2e); }
+      raw_part += s0 + s1;
     }
   };
   {
@@ -535,23 +574,10 @@ sample_kernel(const SampleParams p) {
     }
     return (s[0] + s[1]) + (s[2] + s[3]);
   };
-  const float l2e = 1.4426950408889634f;
-  // softmax denominator at temperature 1 over the vocabulary, an output value: fp32 terms
-  auto raw_sum = [&]() -> double {
-    if (m == INFINITY) return sum_over([&](float x) { return x == m ? 1.0 : 0.0; });
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = tid; i < n_vec; i += SP_THREADS) {
-      float x[EPC];
-      unpack_logits<T>(vec(i), x);
-#pragma unroll
-      for (int e = 0; e < EPC; ++e) {
-        float y;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x[e] - m) * l2e));
-        s[e & 3] += y;
-      }
-    }
-    return (double)((s[0] + s[1]) + (s[2] + s[3]));
-  };
+  // softmax denominator at temperature 1 over the vocabulary, an output value: this thread's share of it, in fp32
+  const double raw_mine = !p.prob ? 0.0
+                          : m == INFINITY ? sum_over([&](float x) { return x == m ? 1.0 : 0.0; })
+                          : share > -INFINITY ? (double)(raw_part * expf(share - m)) : 0.0;
   const bool cut_k = p.top_k > 0 && p.top_k < n_cand, cut_p = p.top_p < 1.f, need_z = cut_p && !cut_k;
   const int groups = nc * SP_THREADS;
   bool have_raw = false;
@@ -579,50 +605,61 @@ sample_kernel(const SampleParams p) {
         if (bin < SP_BINS - 1) atomicAdd(&hist[bin], 1);             // the last bin is what the others leave
       }
     }
-    double v[2] = {p.prob ? raw_sum() : 0.0, sum_over([&](float x) { return x > floor_x ? weight_plain(x) : 0.0; })};
+    double v[2] = {raw_mine, sum_over(weight_plain)};
     int none = 0;
     sum_all<2>(cl, sh, turn, v, none);                   // publishes the counts as well
     raw_all = v[0]; z_all = v[1];
     have_raw = true;
     constexpr int PER = SP_BINS / SP_THREADS;
-    constexpr float FX = 17179869184.f;                  // 2^34
     int count[PER] = {};
-    for (int q = 0; q < nc; ++q) {
-      const int4 c = *reinterpret_cast<const int4*>(cl.map_shared_rank(hist, q) + tid * PER);
-      count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
-    }
-    int fx_turn = 0;
-    unsigned long long counted[1] = {(unsigned long long)(count[0] + count[1] + count[2] + count[3])};
-    sum_fx<SP_WARPS, 1>(sh, fx_turn, counted);
-    if (tid == SP_THREADS - 1) count[PER - 1] = n_cand - (int)counted[0];
-    unsigned long long light[PER], heavy[PER], light_sum = 0, heavy_sum = 0, tot;
+#pragma unroll
+    for (int q = 0; q < SP_MAX_CLUSTER; ++q)
+      if (q < nc) {
+        const int4 c = *reinterpret_cast<const int4*>(cl.map_shared_rank(hist, q) + tid * PER);
+        count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
+      }
+    // running weights from the bins' edges, half a bin to either side of its middle; 2e-5 for the bins' own rounding and
+    // for these sums'.  The open last bin (its count is what the others leave) weighs from nothing to its upper edge.
+    float light[PER], heavy[PER], light_at = 0.f, heavy_at = 0.f;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-      // edges half a bin to either side, and a little for the bins' own rounding
-      const float b = (float)(tid * PER + q);
-      const float hi = exp2f(-fmaxf(b - 0.501f, 0.f) * (l2e / SP_BINS_PER_E)) * 1.00002f;
-      const float low = tid * PER + q == SP_BINS - 1 ? 0.f : exp2f(-(b + 0.501f) * (l2e / SP_BINS_PER_E)) * 0.99998f;
-      light[q] = (unsigned long long)count[q] * (unsigned long long)(low * FX);
-      heavy[q] = (unsigned long long)count[q] * ((unsigned long long)(hi * FX) + 1ull);
-      light_sum += light[q]; heavy_sum += heavy[q];
+      const float b = (float)(tid * PER + q), c = (float)count[q];
+      light_at += c * ex2_approx(-(b + 0.501f) * (l2e / SP_BINS_PER_E)) * 0.99998f;
+      heavy_at += c * ex2_approx(-fmaxf(b - 0.501f, 0.f) * (l2e / SP_BINS_PER_E)) * 1.00002f;
+      light[q] = light_at; heavy[q] = heavy_at;
     }
-    unsigned long long light_at = excl_fx<SP_WARPS>(sh, fx_turn, light_sum, tot), heavy_at = excl_fx<SP_WARPS>(sh, fx_turn, heavy_sum, tot);
-    unsigned long long count_at = excl_fx<SP_WARPS>(sh, fx_turn, (unsigned long long)(count[0] + count[1] + count[2] + count[3]), tot);
-    const double goal = (double)p.top_p * z_all * (double)FX;
-    if (tid == 0) { sh.digit = 0; sh.above = SP_BINS - 1; sh.found = n_cand; }
+    float light_in = light_at, heavy_in = heavy_at;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float a = __shfl_up_sync(0xffffffffu, light_in, o), b = __shfl_up_sync(0xffffffffu, heavy_in, o);
+      if (lane >= o) { light_in += a; heavy_in += b; }
+    }
+    if (lane == 31) sh.edge[warp] = make_float2(light_in, heavy_in);
+    if (tid == 0) { sh.digit = SP_BINS - 1; sh.above = SP_BINS - 1; sh.found = 0; }
     __syncthreads();
+    float light_0 = light_in - light_at, heavy_0 = heavy_in - heavy_at;
+    for (int q = 0; q < warp; ++q) { light_0 += sh.edge[q].x; heavy_0 += sh.edge[q].y; }
+    const float goal = (float)((double)p.top_p * z_all);
+    // the first bin whose upper sum reaches the goal, and the first whose lower sum does
+    int first_hi = SP_BINS - 1, first_lo = SP_BINS - 1;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) {
-      // one bin each: the first whose upper sum reaches the goal, and the first whose lower sum does
-      if ((double)heavy_at * 1.0 < goal && (double)(heavy_at + heavy[q]) >= goal) sh.digit = tid * PER + q;
-      count_at += count[q];
-      if ((double)light_at < goal && (double)(light_at + light[q]) >= goal) { sh.above = tid * PER + q; sh.found = (int)count_at; }
-      heavy_at += heavy[q]; light_at += light[q];
+    for (int q = PER - 1; q >= 0; --q) {
+      if (heavy_0 + heavy[q] >= goal * 0.999999f) first_hi = tid * PER + q;
+      if (light_0 + light[q] >= goal * 1.000001f) first_lo = tid * PER + q;
     }
+    first_hi = (int)__reduce_min_sync(0xffffffffu, (unsigned)first_hi);
+    first_lo = (int)__reduce_min_sync(0xffffffffu, (unsigned)first_lo);
+    if (lane == 0) { atomicMin(&sh.digit, first_hi); atomicMin(&sh.above, first_lo); }
+    __syncthreads();
+    int upto = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) upto += tid * PER + q <= sh.above ? count[q] : 0;
+    upto = __reduce_add_sync(0xffffffffu, upto);
+    if (lane == 0) atomicAdd(&sh.found, upto);
     __syncthreads();
     bin_lo = 8388608.f + (float)sh.digit; bin_hi = 8388608.f + (float)sh.above;
     narrowed = true;
-    if (sh.found <= SP_LIST) reach_bin = bin_hi;         // short enough: its tokens, and a few too many, as a list
+    if (sh.found <= SP_LIST && sh.above < SP_BINS - 1) reach_bin = bin_hi;   // short enough: its tokens, and a few too many, as a list
     cl.sync();                                           // everybody has read the counts: the list may go over them
   }
   const bool short_nucleus = narrowed && reach_bin == bin_hi;
@@ -644,9 +681,9 @@ sample_kernel(const SampleParams p) {
       least = (uint32_t)sh.digit;
       int own_turn = 0;
       unsigned long long above;
-      const uint32_t kth = largest_reaching<SP_WARPS>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k, above,
-                                                      [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&c)[3]) {
-        c[0] = c[1] = c[2] = 0ull;
+      const uint32_t kth = largest_reaching<SP_WARPS, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k,
+                                                            above, [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
+        c[0] = c[1] = c[2] = 0u;
 #pragma unroll
         for (int q = 0; q < SP_MAX_CLUSTER; ++q)
           if (q < nc) { c[0] += key[q] >= t1; c[1] += key[q] >= t2; c[2] += key[q] >= t3; }
@@ -654,23 +691,23 @@ sample_kernel(const SampleParams p) {
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
     auto reaches = [&](float x) -> bool { return x >= from && !(bin_of(x) > reach_bin); };
-    double raw[1] = {p.prob && !have_raw ? raw_sum() : 0.0};
+    double raw_sum[1] = {raw_mine};
     // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order
     uint8_t* mask = scratch + SP_OFF_MASK;
     const int n_words = (n_vec + 3) >> 2;
-    for (int i = tid; i < n_words * 4; i += SP_THREADS) {
-      uint32_t bits = 0;
-      if (i < n_vec) {
+    for (int i = tid; i < n_words; i += SP_THREADS) reinterpret_cast<uint32_t*>(mask)[i] = 0u;
+    __syncthreads();
+    if (reaches(share))                                  // most threads have nothing to look for
+      for (int i = tid; i < n_vec; i += SP_THREADS) {
         const uint4 raw = vec(i);
-        if (reaches(largest_of<T>(raw))) {
-          float x[EPC];
-          unpack_logits<T>(raw, x);
+        if (!reaches(largest_of<T>(raw))) continue;
+        float x[EPC];
+        unpack_logits<T>(raw, x);
+        uint32_t bits = 0;
 #pragma unroll
-          for (int e = 0; e < EPC; ++e) bits |= reaches(x[e]) ? 1u << e : 0u;
-        }
+        for (int e = 0; e < EPC; ++e) bits |= reaches(x[e]) ? 1u << e : 0u;
+        mask[i] = (uint8_t)bits;
       }
-      mask[i] = (uint8_t)bits;
-    }
     __syncthreads();
     const uint32_t* words = reinterpret_cast<const uint32_t*>(mask);
     const int per_w = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per_w, n_words), w1 = min(w0 + per_w, n_words);
@@ -686,12 +723,12 @@ sample_kernel(const SampleParams p) {
         }
     if (tid == 0) sh.list_n = tot;
     int n_list = tot;
-    sum_all<1>(cl, sh, turn, raw, n_list);               // publishes the lists as well
+    sum_all<1>(cl, sh, turn, raw_sum, n_list);           // publishes the lists as well
     n_list = 0;
 #pragma unroll
     for (int q = 0; q < SP_MAX_CLUSTER; ++q)
       if (q < nc) n_list += cl.map_shared_rank(&sh, q)->list_n;
-    if (!have_raw) raw_all = raw[0];
+    if (!have_raw) raw_all = raw_sum[0];
     have_raw = true;
     if (n_list <= SP_LIST) {                             // more: ties at the bound (uniform over the cluster)
       if (rank == 0) {
@@ -927,7 +964,7 @@ sample_kernel(const SampleParams p) {
     if (lane == 0) { sh.seg[warp].w = s[0]; sh.seg[warp].n_gt = ngt; sh.seg[warp].n_eq = neq; }
   }
   {
-    double raw[1] = {p.prob && !have_raw ? raw_sum() : 0.0};
+    double raw[1] = {raw_mine};
     int none = 0;
     sum_all<1>(cl, sh, turn, raw, none);                 // its barrier publishes seg[] as well
     if (!have_raw) raw_all = raw[0];
