@@ -147,6 +147,46 @@ def test_written_rows_are_the_oracles_bit_for_bit(ctx, fmt, dtype, d, Hkv, L, n,
 
 
 @gpu
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_a_long_cache_bit_for_bit_both_ways(ctx, fmt, dtype, d):
+    """Many rows (several in flight per thread), magnitudes over the whole range of fp32, quotients on and beside the
+    ties: IEEE division on the host is the reference."""
+    Hkv, L = 8, 10007                                     # an odd length: the last group of rows is ragged
+    rng = np.random.default_rng(d)
+    top = {"int8": 127.0, "e4m3": 448.0}[fmt]
+    x = rng.standard_normal((L, Hkv, d)).astype(np.float32)
+    x *= np.exp2(rng.integers(-96, 125, (L, Hkv, 1))).astype(np.float32)
+    m = np.abs(x[:L // 2]).max(-1, keepdims=True)
+    ties = (rng.integers(-2 * top, 2 * top + 1, (L // 2, Hkv, d)) / np.float32(2.0 * top)).astype(np.float32) * m
+    x[:L // 2] = np.where(rng.random(ties.shape) < 0.5, ties, x[:L // 2])
+    x[5, 0, :] = np.float32(3.3e38)                       # the largest scale
+    x[6, 0, 1], x[7, 1, 2], x[L - 1, 7, d - 1] = np.inf, np.nan, -np.inf
+    src = storage(x, dtype)
+    x = wl.storage_to_f64(src, dtype).astype(np.float32)
+    fin = np.where(np.isfinite(x), np.abs(x), np.float32(0)).max(-1)
+    scale = np.where(fin < np.float32(2.0 ** -80), np.float32(0), fin / np.float32(top)).astype(np.float32)
+    with np.errstate(all="ignore"):
+        q = np.where(np.isnan(x) | (scale[..., None] == 0), np.float32(0), x / scale[..., None])
+    q = torch.from_numpy(np.clip(q, -top, top))
+    want = q.round().to(torch.int8) if fmt == "int8" else q.to(torch.float8_e4m3fn)          # both: ties to even
+    dx = fstep.to_device(src, dtype)
+    sh = fb.make_shape(L, 0, Hkv, Hkv, d, 64, DT[dtype])
+    codes = torch.zeros(2, Hkv, L, d, dtype=want.dtype, device="cuda")
+    scales = torch.full((2, Hkv, L), -1.0, device="cuda")
+    cache = fb.make_quant_cache(FMT[fmt], codes[0], codes[1], scales[0], scales[1])
+    for i in (0, 1):
+        fb.focus_quantize_kv(ctx, sh, None if i else dx, dx if i else None, Hkv * d, d, 0, None, None, L, cache)
+        assert np.array_equal(scales[i].cpu().numpy(), scale.T)
+        assert torch.equal(codes[i].float().cpu(), want.float().transpose(0, 1))
+    out = torch.zeros(2, Hkv, L, d, dtype=dx.dtype, device="cuda")
+    fb.focus_dequantize_kv(ctx, sh, cache, 0, None, None, L, out[0], out[1], d, L * d)
+    ref = (want.float() * torch.from_numpy(scale)[..., None]).transpose(0, 1).to(dx.dtype)   # one rounding (+ bf16's)
+    assert torch.equal(out[0].cpu(), ref) and torch.equal(out[1].cpu(), ref)
+    assert ctx.poll_status() == 0
+
+
+@gpu
 def test_one_half_of_the_cache_at_a_time_and_no_rows(ctx):
     L, Hkv, d, n = 40, 2, 64, 6
     sh = fb.make_shape(L, 0, 2, Hkv, d, 64, fb.BF16)
