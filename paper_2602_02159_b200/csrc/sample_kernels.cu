@@ -32,9 +32,10 @@ constexpr int SP_SLICE_BYTES = 180 * 1024;               // largest slice of a r
 constexpr int SP_LIST = 2048;                            // most tokens of a short list
 constexpr int SP_LIST_K = 1024;                          // largest top-k that goes through it; tokens tried for a nucleus
 constexpr int SP_PER = SP_LIST / SP_THREADS;             // tokens of the list per thread
+constexpr int SP_PAIRS = SP_THREADS / 4;                 // most tokens of a list that is cut by comparing all pairs
 // scratch behind the slice: thread maxima | list | one byte per 16-byte vector of the slice
 constexpr int SP_OFF_LIST = SP_THREADS * 4, SP_OFF_MASK = SP_OFF_LIST + SP_LIST * 8, SP_SMEM = 212 * 1024;   // largest, all told
-constexpr int SP_TAB = 1024;                             // entries of the table of powers
+constexpr int SP_TAB = 64, SP_TAB_COPIES = 16;           // table of powers: entries, and copies (one per pair of banks)
 constexpr int SP_BINS = 2048, SP_BINS_PER_E = 64;        // histogram of a nucleus: bins, and how many to a factor of e
 constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN is below it
 static_assert(SP_BINS * 4 <= SP_LIST * 8 && SP_BINS == 4 * SP_THREADS, "a histogram lies where a list does");
@@ -46,16 +47,16 @@ struct SegSum {            // one warp's contiguous segment of the row
 };
 
 struct SampleShared {
-  double tab[SP_TAB];      // 2^(i / SP_TAB)
+  double tab[SP_TAB * SP_TAB_COPIES];        // [i][copy]: 2^(i / SP_TAB)
   double dsum[2][SP_WARPS][3];
   int isum[2][SP_WARPS];
   double cta_d[2][3];
   int cta_i[2];
   SegSum seg[SP_WARPS];
   SegSum all[SP_MAX_CLUSTER * SP_WARPS];
-  float wmax[SP_WARPS];
+  uint2 first[SP_WARPS], cta_first;
   int list_n, list_ok;
-  int hist[2][256];
+  alignas(16) int hist[2][256];
   int scan_i[33];
   unsigned long long fx[2][SP_WARPS][3];
   int last[SP_WARPS];
@@ -134,6 +135,25 @@ __device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh,
   }
 }
 
+// The largest logit and the number of candidates, over the cluster and in every thread; its barriers publish what was
+// written before it.
+__device__ __forceinline__ void first_all(cg::cluster_group& cl, SampleShared& sh, float& m, int& cnt) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t k = __reduce_max_sync(0xffffffffu, float_key(m)), c = __reduce_add_sync(0xffffffffu, (unsigned)cnt);
+  if (lane == 0) sh.first[warp] = make_uint2(k, c);
+  __syncthreads();
+  uint2 v = lane < SP_WARPS ? sh.first[lane] : make_uint2(0u, 0u);
+  v.x = __reduce_max_sync(0xffffffffu, v.x); v.y = __reduce_add_sync(0xffffffffu, v.y);
+  const int nc = (int)cl.num_blocks();
+  if (nc > 1) {
+    if (threadIdx.x == 0) sh.cta_first = v;
+    cl.sync();
+    v = lane < nc ? cl.map_shared_rank(&sh, lane)->cta_first : make_uint2(0u, 0u);
+    v.x = __reduce_max_sync(0xffffffffu, v.x); v.y = __reduce_add_sync(0xffffffffu, v.y);
+  }
+  m = key_to_float(v.x); cnt = (int)v.y;
+}
+
 template <typename T>
 __device__ __forceinline__ void unpack_logits(const uint4& raw, float (&x)[16 / sizeof(T)]) {
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -177,6 +197,22 @@ __device__ __forceinline__ float largest_of(const uint4& raw) {
     return fmaxf(fmaxf(__uint_as_float(raw.x), __uint_as_float(raw.y)), fmaxf(__uint_as_float(raw.z), __uint_as_float(raw.w)));
   }
 }
+// bit e: element e of a vector is at least `from`
+template <typename T>
+__device__ __forceinline__ uint32_t reaching_bits(const uint4& raw, float from) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint32_t bits = 0u;
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162 f = __bfloat162bfloat162(__float2bfloat16_ru(from));         // the least bf16 that is
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bits |= __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), f) & (0x00020001u << (2 * i));
+    return (bits | bits >> 16) & 0xFFu;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bits |= __uint_as_float(w[i]) >= from ? 1u << i : 0u;
+    return bits;
+  }
+}
 
 __device__ __forceinline__ float ex2_approx(float x) {
   float y;
@@ -184,17 +220,22 @@ __device__ __forceinline__ float ex2_approx(float x) {
   return y;
 }
 
-// Powers of two in fp64: t = n / 1024 + r, 2^t = 2^(n >> 10) * tab[n & 1023] * 2^r, the last factor by its Taylor
-// polynomial (Tang's table-driven scheme, 1989).  |r| <= 2^-11, so the square leaves 7e-12 of a weight, of either sign.
+// Powers of two in fp64: t = n / 64 + r, 2^t = 2^(n >> 6) * tab[n & 63] * 2^r (Tang's table-driven scheme, 1989).  Every
+// lane reads its own copy of the table, so that no two lanes of a half warp meet in a bank: with one table of 1024
+// entries, and one multiplication less, the lookups took most of the time.  2^r is a cubic with |r| <= h = 1/128: the
+// Taylor terms, and the fourth power replaced by h^2 r^2 - h^4 / 8 (Chebyshev), without that constant, since only ratios
+// of weights matter.  It leaves ln2^4 / 24 * h^4 / 4 = 9e-12 of a weight between any two of them.
 // -1000 <= t <= 0; no branch, so that several run side by side.
 __device__ __forceinline__ double pow2_near(double t, const double* tab) {
   const double magic = 6755399441055744.0;               // 1.5 * 2^52: adding it leaves the rounded integer in the low bits
+  constexpr double ln2 = 0.69314718055994531, h = 0.5 / SP_TAB;
   const double tm = fma(t, (double)SP_TAB, magic);
   const int n = __double2loint(tm);
   const double r = fma(tm - magic, -1.0 / SP_TAB, t);
-  const double b = tab[n & (SP_TAB - 1)];
-  const double w = fma(b, r * fma(r, 0.24022650695910071, 0.69314718055994531), b);   // ln2^2 / 2, ln2
-  return __hiloint2double(__double2hiint(w) + ((n >> 10) << 20), __double2loint(w));
+  const double b = tab[(n & (SP_TAB - 1)) * SP_TAB_COPIES];
+  const double f = fma(r, fma(r, ln2 * ln2 * ln2 / 6.0, ln2 * ln2 / 2.0 + h * h * (ln2 * ln2 * ln2 * ln2 / 24.0)), ln2);
+  const double w = fma(b, r * f, b);
+  return __hiloint2double(__double2hiint(w) + ((n >> 6) << 20), __double2loint(w));
 }
 
 // Sums over the first NW warps of a block (all of them call it) of numbers below 2^53: integer weights, so that a
@@ -301,14 +342,16 @@ struct Draw {                                            // what a list is cut b
   int top_k;                                             // 0: no cut
   double top_p, z, min_p, u;                             // top_p 1: no cut; z: weight of the whole vocabulary, or < 0: the list's
   uint32_t key_lo;                                       // no key of the list is below
+  uint32_t key_top;                                      // the nucleus does not end above
   bool complete;                                         // the list holds every candidate
 };
-// Cuts the list of n <= NW * 32 * SP_PER tokens (descending priority: key, then place) and draws.  Returns the place of the
+// Cuts the list of n <= SP_LIST tokens (descending priority: key, then place) and draws.  Returns the place of the
 // token drawn in `at` (on the thread that holds it; -1 elsewhere), or false where the nucleus reaches beyond the list.
-// Called by the first NW warps; a thread's tokens are neighbours.
-template <int NW, int KEY_BITS, typename W>
+// Called by all threads; a thread's tokens are neighbours.
+template <int KEY_BITS, typename W>
 __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned long long* list, int n, uint32_t key_hi, const Draw& d,
                                                W weight, int& at, double& w_at, double& total_w, int& kept) {
+  constexpr int NW = SP_WARPS;
   const int tid = threadIdx.x;
   int turn = 0;
   uint32_t key[SP_PER];
@@ -327,7 +370,6 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
       in |= 1u << q;
     }
   }
-  const int vary = even_bits(key_hi ^ d.key_lo);
   // keeps of the tokens at key t the first `quota`, drops those below t
   auto cut_at = [&](uint32_t t, unsigned long long quota) {
     unsigned long long eq = 0, all;
@@ -341,9 +383,10 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
       before += tie ? 1 : 0;
     }
   };
+  uint32_t key_end = d.key_lo;                           // nor below this
   if (d.top_k > 0 && d.top_k < n) {
     unsigned long long above;
-    const uint32_t t = largest_reaching<NW, true>(sh, turn, key_hi, vary, (unsigned long long)d.top_k, above,
+    const uint32_t t = largest_reaching<NW, true>(sh, turn, key_hi, even_bits(key_hi ^ d.key_lo), (unsigned long long)d.top_k, above,
                                                   [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&s)[3]) {
       s[0] = s[1] = s[2] = 0u;
 #pragma unroll
@@ -351,6 +394,7 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
         if (in >> q & 1u) { s[0] += key[q] >= t1; s[1] += key[q] >= t2; s[2] += key[q] >= t3; }
     });
     cut_at(t, (unsigned long long)d.top_k - above);
+    key_end = t;
   }
   if (d.top_p < 1.0) {
     unsigned long long a[1] = {0ull};
@@ -361,22 +405,61 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
     const unsigned long long goal = (unsigned long long)ceil(goal_w);
     if (a[0] < goal && !d.complete) return false;
     if (a[0] >= goal) {
-      unsigned long long above;
-      const uint32_t t = largest_reaching<NW, false>(sh, turn, key_hi, vary, goal, above,
-                                              [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
-        s[0] = s[1] = s[2] = 0ull;
+      // the tokens above key_top are in; the few from there down, if they are few, by comparing all pairs of them
+      int slot[SP_PER];
+      unsigned long long* b_fx = reinterpret_cast<unsigned long long*>(sh.hist[1]);
+      uint2* b_key = reinterpret_cast<uint2*>(sh.hist[0]);               // key, place; later .x: whether it is in
+      unsigned long long sure[1] = {0ull};
+      if (tid == 0) sh.found = 0;
+      __syncthreads();
 #pragma unroll
-        for (int q = 0; q < SP_PER; ++q) {
-          const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
-          s[0] += key[q] >= t1 ? v : 0ull;
-          s[1] += key[q] >= t2 ? v : 0ull;
-          s[2] += key[q] >= t3 ? v : 0ull;
+      for (int q = 0; q < SP_PER; ++q) {
+        slot[q] = -1;
+        if (in >> q & 1u) {
+          if (key[q] > d.key_top) sure[0] += fx[q];
+          else slot[q] = atomicAdd(&sh.found, 1);
+          if (slot[q] >= 0 && slot[q] < SP_PAIRS) {
+            b_fx[slot[q]] = fx[q];
+            b_key[slot[q]] = make_uint2(key[q], (uint32_t)(tid * SP_PER + q));
+          }
         }
-      });
-      // how many of the tokens at t it takes (their weight is one number)
-      const double each = rint(weight(key_to_float(KEY_BITS == 32 ? t : t << 16 | (t & 0x8000u ? 0u : 0xFFFFu))) * FX_ONE);
-      const double need = ceil((double)(goal - above) / each);
-      cut_at(t, (unsigned long long)fmin(fmax(need, 1.0), (double)SP_LIST));
+      }
+      sum_fx<NW, 1>(sh, turn, sure);
+      const int n_b = sh.found;
+      if (n_b <= SP_PAIRS) {
+        const int i = tid >> 2;
+        const uint2 me = b_key[min(i, max(n_b - 1, 0))];
+        unsigned long long above = 0ull;
+        for (int j = tid & 3; j < n_b; j += 4) {
+          const uint2 o = b_key[j];
+          if (o.x > me.x || (o.x == me.x && o.y < me.y)) above += b_fx[j];
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+        __syncthreads();
+        if (i < n_b && (tid & 3) == 0) b_key[i].x = sure[0] + above < goal ? 1u : 0u;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < SP_PER; ++q)
+          if (slot[q] >= 0 && b_key[slot[q]].x == 0u) in &= ~(1u << q);
+      } else {
+        unsigned long long above;
+        const uint32_t t = largest_reaching<NW, false>(sh, turn, d.key_top, even_bits(d.key_top ^ key_end), goal, above,
+                                                [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
+          s[0] = s[1] = s[2] = 0ull;
+#pragma unroll
+          for (int q = 0; q < SP_PER; ++q) {
+            const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
+            s[0] += key[q] >= t1 ? v : 0ull;
+            s[1] += key[q] >= t2 ? v : 0ull;
+            s[2] += key[q] >= t3 ? v : 0ull;
+          }
+        });
+        // how many of the tokens at t it takes (their weight is one number)
+        const double each = rint(weight(key_to_float(KEY_BITS == 32 ? t : t << 16 | (t & 0x8000u ? 0u : 0xFFFFu))) * FX_ONE);
+        const double need = ceil((double)(goal - above) / each);
+        cut_at(t, (unsigned long long)fmin(fmax(need, 1.0), (double)SP_LIST));
+      }
     }
   }
   if (d.min_p > 0.0) {
@@ -408,6 +491,76 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
     }
   }
   if (at >= 0) w_at = weight(key_to_float((uint32_t)(list[at] >> 32)));
+  return true;
+}
+
+// The same for at most SP_PAIRS tokens, by all threads: four per token, which sum what precedes it in descending order.
+// That answers every cut at once, without a search: about 1000 cycles, where the steps of the search above take 4000 to
+// 9000.  The outcome is with the first warp.
+template <typename W>
+__device__ __forceinline__ bool draw_from_pairs(SampleShared& sh, const unsigned long long* list, int n, const Draw& d, W weight, int& at,
+                                                double& w_at, double& total_w, int& kept) {
+  unsigned long long* fx = reinterpret_cast<unsigned long long*>(sh.hist[1]);
+  const int tid = threadIdx.x, lane = tid & 31, i = tid >> 2, part = tid & 3;
+  const uint32_t key = i < n ? (uint32_t)(list[i] >> 32) : 0u;
+  double w = 0.0;
+  unsigned long long mine = 0ull;
+  if (i < n) {
+    w = weight(key_to_float(key));
+    mine = (unsigned long long)__double2ll_rn(w * FX_ONE);
+    if (w > 0.0 && mine == 0ull) mine = 1ull;            // u = 0 draws the first token that has a weight, however small
+  }
+  if (part == 0) fx[i] = mine;
+  __syncthreads();
+  unsigned long long above = 0ull;
+  int rank = 0;
+  for (int j = part; j < n; j += 4) {
+    const uint32_t k = (uint32_t)(list[j] >> 32);
+    if (k > key || (k == key && j < i)) { above += fx[j]; ++rank; }
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    above += __shfl_xor_sync(0xffffffffu, above, o);
+    rank += __shfl_xor_sync(0xffffffffu, rank, o);
+  }
+  const int k = d.top_k > 0 ? min(d.top_k, n) : n;
+  if (i < n && rank == k - 1 && part == 0) sh.fx[0][0][0] = above + mine;        // the weight of the k largest
+  __syncthreads();
+  const unsigned long long all = sh.fx[0][0][0];
+  bool in = i < n && rank < k;
+  if (d.top_p < 1.0) {
+    const unsigned long long goal = (unsigned long long)ceil(d.top_p * (d.z >= 0.0 ? d.z * FX_ONE : (double)all));
+    if (all < goal && !d.complete) return false;
+    in = in && above < goal;
+  }
+  in = in && w >= d.min_p;
+  if (part == 0) fx[i] = in ? mine | 1ull << 63 : 0ull;
+  __syncthreads();
+  at = -1;
+  if (tid >= 32) return true;
+  int turn = 0;
+  constexpr int PER = SP_PAIRS / 32;
+  unsigned long long v[PER], sum = 0ull, total;
+  int count = 0;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    v[q] = fx[lane * PER + q];
+    count += (int)(v[q] >> 63);
+    v[q] &= ~(1ull << 63);
+    sum += v[q];
+  }
+  unsigned long long run = excl_fx<1>(sh, turn, sum, total);
+  kept = __reduce_add_sync(0xffffffffu, count);
+  total_w = (double)total / FX_ONE;
+  const unsigned long long target = (unsigned long long)(d.u * (double)total);
+  if (run <= target && run + sum > target) {             // one lane, as u < 1
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      if (at < 0 && run + v[q] > target) at = lane * PER + q;
+      run += v[q];
+    }
+    w_at = weight(key_to_float((uint32_t)(list[at] >> 32)));
+  }
   return true;
 }
 
@@ -501,27 +654,19 @@ sample_kernel(const SampleParams p) {
     for (; i + EPC <= cnt; i += STEP) take(__ldg(reinterpret_cast<const uint4*>(row + i)), i);
     if (i < cnt) take(tail_vector(i), i);
   }
-  for (int i = tid; i < SP_TAB; i += SP_THREADS) {       // 2^(i / 1024) as the product of its binary digits' powers
-    const double f[10] = {1.0006771306930664, 1.0013547198921082, 1.0027112750502025, 1.0054299011128027, 1.0108892860517005,
-                          1.0218971486541166, 1.0442737824274138, 1.0905077326652577, 1.189207115002721, 1.4142135623730951};
+  for (int i = tid; i < SP_TAB * SP_TAB_COPIES; i += SP_THREADS) {         // as the product of its binary digits' powers
+    const double f[6] = {1.0108892860517005, 1.0218971486541166, 1.0442737824274138, 1.0905077326652577, 1.189207115002721,
+                         1.4142135623730951};
     double v = 1.0;
 #pragma unroll
-    for (int q = 0; q < 10; ++q) v *= (i >> q & 1) ? f[q] : 1.0;
+    for (int q = 0; q < 6; ++q) v *= (i / SP_TAB_COPIES >> q & 1) ? f[q] : 1.0;
     sh.tab[i] = v;
   }
+  const double* tab = sh.tab + (lane & (SP_TAB_COPIES - 1));
   uint32_t* share_key = reinterpret_cast<uint32_t*>(scratch);
   share_key[tid] = float_key(share) >> (32 - KEY_BITS);
   float m = share;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) sh.wmax[warp] = m;
-  {
-    double none[1] = {0.0};
-    sum_all<1>(cl, sh, turn, none, n_cand);              // its barriers publish the maxima as well
-  }
-  for (int q = lane; q < nc * SP_WARPS; q += 32) m = fmaxf(m, cl.map_shared_rank(&sh, q / SP_WARPS)->wmax[q % SP_WARPS]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  first_all(cl, sh, m, n_cand);
   if (n_cand == 0) {
     if (lead) finish(-1, 0.f, 0.f, 0);
     cl.sync();
@@ -537,9 +682,9 @@ sample_kernel(const SampleParams p) {
   auto weight = [&](float x) -> double {
     if (m == INFINITY) return x == m ? 1.0 : 0.0;
     const double t = ((double)x - md) * scale;
-    return t >= -1000.0 ? pow2_near(t, sh.tab) : 0.0;
+    return t >= -1000.0 ? pow2_near(t, tab) : 0.0;
   };
-  auto weight_plain = [&](float x) -> double { return pow2_near(((double)fmaxf(x, floor_x) - md) * scale, sh.tab); };
+  auto weight_plain = [&](float x) -> double { return pow2_near(((double)fmaxf(x, floor_x) - md) * scale, tab); };
   // keys of bf16 logits in 16 bits, so that both types descend through their own bits only
   auto key_of = [&](float x) -> uint32_t { return float_key(x) >> (32 - KEY_BITS); };
   constexpr uint32_t BOTTOM = KEY_NEG_INF >> (32 - KEY_BITS);
@@ -584,28 +729,32 @@ sample_kernel(const SampleParams p) {
   double raw_all = 0.0, z_all = -1.0;                    // z_all: weight of the vocabulary, where top-p needs it
   unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch + SP_OFF_LIST);
   // ---- a nucleus: where does it end, to within a few histogram bins? ----
-  // Bins of 1/64 in the exponent (nearest, the last one open), counted; the weight of a bin lies between those of its
+  // Bins of 1/64 in the exponent (nearest, the last one open), counted; the last one is where all that is lighter weighs
+  // less than half of what a nucleus may leave out: n_cand e^-(b / 64) <= (1 - top_p) / 2.  The weight of a bin lies between those of its
   // edges, so the running weight is known to +-0.8 %.  Bins before bin_lo are in the nucleus, those after bin_hi are not.
   const float per_bin = (float)SP_BINS_PER_E / p.temperature;
+  const int last_bin = (int)fminf((float)(SP_BINS - 1), (float)SP_BINS_PER_E * logf(2.f * (float)n_cand / fmaxf(1.f - p.top_p, FLT_MIN)) + 2.f);
   auto bin_of = [&](float x) -> float {                  // as the float 2^23 + bin
-    return fminf((m - x) * per_bin, (float)(SP_BINS - 1)) + 8388608.f;
+    return fminf((m - x) * per_bin, (float)last_bin) + 8388608.f;
   };
-  float reach_bin = 8388608.f + SP_BINS, bin_lo = 0.f, bin_hi = 0.f;      // as 2^23 + bin; tokens to collect: up to reach_bin
-  bool narrowed = false;
+  float bin_lo = 0.f, bin_hi = 0.f;                      // as 2^23 + bin
+  bool narrowed = false, short_nucleus = false;
   if (need_z && plain && n_cand > SP_LIST) {
     int* hist = reinterpret_cast<int*>(list);
     for (int i = tid; i < SP_BINS; i += SP_THREADS) hist[i] = 0;
     __syncthreads();
+    double w[4] = {0.0, 0.0, 0.0, 0.0};
     for (int i = tid; i < n_vec; i += SP_THREADS) {
       float x[EPC];
       unpack_logits<T>(vec(i), x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
         const int bin = __float_as_int(bin_of(x[e])) & (SP_BINS - 1);
-        if (bin < SP_BINS - 1) atomicAdd(&hist[bin], 1);             // the last bin is what the others leave
+        if (bin < last_bin) atomicAdd(&hist[bin], 1);
+        w[e & 3] += weight_plain(x[e]);
       }
     }
-    double v[2] = {raw_mine, sum_over(weight_plain)};
+    double v[2] = {raw_mine, (w[0] + w[1]) + (w[2] + w[3])};
     int none = 0;
     sum_all<2>(cl, sh, turn, v, none);                   // publishes the counts as well
     raw_all = v[0]; z_all = v[1];
@@ -635,13 +784,13 @@ sample_kernel(const SampleParams p) {
       if (lane >= o) { light_in += a; heavy_in += b; }
     }
     if (lane == 31) sh.edge[warp] = make_float2(light_in, heavy_in);
-    if (tid == 0) { sh.digit = SP_BINS - 1; sh.above = SP_BINS - 1; sh.found = 0; }
+    if (tid == 0) { sh.digit = last_bin; sh.above = last_bin; sh.found = 0; }
     __syncthreads();
     float light_0 = light_in - light_at, heavy_0 = heavy_in - heavy_at;
     for (int q = 0; q < warp; ++q) { light_0 += sh.edge[q].x; heavy_0 += sh.edge[q].y; }
     const float goal = (float)((double)p.top_p * z_all);
     // the first bin whose upper sum reaches the goal, and the first whose lower sum does
-    int first_hi = SP_BINS - 1, first_lo = SP_BINS - 1;
+    int first_hi = last_bin, first_lo = last_bin;
 #pragma unroll
     for (int q = PER - 1; q >= 0; --q) {
       if (heavy_0 + heavy[q] >= goal * 0.999999f) first_hi = tid * PER + q;
@@ -659,55 +808,77 @@ sample_kernel(const SampleParams p) {
     __syncthreads();
     bin_lo = 8388608.f + (float)sh.digit; bin_hi = 8388608.f + (float)sh.above;
     narrowed = true;
-    if (sh.found <= SP_LIST && sh.above < SP_BINS - 1) reach_bin = bin_hi;   // short enough: its tokens, and a few too many, as a list
+    short_nucleus = sh.found <= SP_LIST && sh.above < last_bin;    // its tokens, and a few too many, as a list
     cl.sync();                                           // everybody has read the counts: the list may go over them
   }
-  const bool short_nucleus = narrowed && reach_bin == bin_hi;
   // ---- short list (top-k: the bound is tight while the k wanted are at most half of the shares) ----
   if (short_nucleus || (cut_k && p.top_k <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
     float from = -FLT_MAX;                               // collect the logits from here up
     if (n_cand > SP_LIST && cut_k) {
-      uint32_t key[SP_MAX_CLUSTER], least = 0xFFFFFFFFu;
-#pragma unroll
-      for (int q = 0; q < SP_MAX_CLUSTER; ++q) {
-        key[q] = 0u;
-        if (q < nc) { key[q] = cl.map_shared_rank(share_key, q)[tid]; least = min(least, key[q]); }
-      }
-      least = __reduce_min_sync(0xffffffffu, least);
-      if (tid == 0) sh.digit = -1;
-      __syncthreads();
-      if (lane == 0) atomicMin(reinterpret_cast<unsigned*>(&sh.digit), least);
-      __syncthreads();
-      least = (uint32_t)sh.digit;
-      int own_turn = 0;
+      uint32_t least = 0xFFFFFFFFu, kth;
       unsigned long long above;
-      const uint32_t kth = largest_reaching<SP_WARPS, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k,
-                                                            above, [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
-        c[0] = c[1] = c[2] = 0u;
+      int own_turn = 0;
+      if (nc == 1) {                                     // 512 keys: one warp, without barriers
+        if (warp == 0) {
+          uint32_t key[SP_WARPS];
 #pragma unroll
-        for (int q = 0; q < SP_MAX_CLUSTER; ++q)
-          if (q < nc) { c[0] += key[q] >= t1; c[1] += key[q] >= t2; c[2] += key[q] >= t3; }
-      });
+          for (int q = 0; q < SP_WARPS; ++q) { key[q] = share_key[lane + 32 * q]; least = min(least, key[q]); }
+          least = __reduce_min_sync(0xffffffffu, least);
+          kth = largest_reaching<1, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k, above,
+                                          [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
+            c[0] = c[1] = c[2] = 0u;
+#pragma unroll
+            for (int q = 0; q < SP_WARPS; ++q) { c[0] += key[q] >= t1; c[1] += key[q] >= t2; c[2] += key[q] >= t3; }
+          });
+          if (lane == 0) sh.digit = (int)kth;
+        }
+        __syncthreads();
+        kth = (uint32_t)sh.digit;
+      } else {
+        uint32_t key[SP_MAX_CLUSTER];
+#pragma unroll
+        for (int q = 0; q < SP_MAX_CLUSTER; ++q) {
+          key[q] = 0u;
+          if (q < nc) { key[q] = cl.map_shared_rank(share_key, q)[tid]; least = min(least, key[q]); }
+        }
+        least = __reduce_min_sync(0xffffffffu, least);
+        if (tid == 0) sh.digit = -1;
+        __syncthreads();
+        if (lane == 0) atomicMin(reinterpret_cast<unsigned*>(&sh.digit), least);
+        __syncthreads();
+        least = (uint32_t)sh.digit;
+        kth = largest_reaching<SP_WARPS, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k,
+                                               above, [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
+          c[0] = c[1] = c[2] = 0u;
+#pragma unroll
+          for (int q = 0; q < SP_MAX_CLUSTER; ++q)
+            if (q < nc) { c[0] += key[q] >= t1; c[1] += key[q] >= t2; c[2] += key[q] >= t3; }
+        });
+      }
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
-    auto reaches = [&](float x) -> bool { return x >= from && !(bin_of(x) > reach_bin); };
+    if (short_nucleus) from = fmaxf(m - (bin_hi - 8388607.f) / per_bin, -FLT_MAX);   // half a bin and the rounding below its middle
     double raw_sum[1] = {raw_mine};
-    // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order
+    // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order.
+    // Only the shares whose maximum reaches it are looked at, and those by all threads.
     uint8_t* mask = scratch + SP_OFF_MASK;
+    uint16_t* shares = reinterpret_cast<uint16_t*>(sh.hist[0]);
     const int n_words = (n_vec + 3) >> 2;
     for (int i = tid; i < n_words; i += SP_THREADS) reinterpret_cast<uint32_t*>(mask)[i] = 0u;
+    const bool wanted = share >= from;
+    int n_shares;
+    const int my_place = block_excl_scan(wanted ? 1 : 0, sh.scan_i, n_shares);
+    if (wanted) shares[my_place] = (uint16_t)tid;
     __syncthreads();
-    if (reaches(share))                                  // most threads have nothing to look for
-      for (int i = tid; i < n_vec; i += SP_THREADS) {
-        const uint4 raw = vec(i);
-        if (!reaches(largest_of<T>(raw))) continue;
-        float x[EPC];
-        unpack_logits<T>(raw, x);
-        uint32_t bits = 0;
-#pragma unroll
-        for (int e = 0; e < EPC; ++e) bits |= reaches(x[e]) ? 1u << e : 0u;
-        mask[i] = (uint8_t)bits;
+    const int deep = (n_vec + SP_THREADS - 1) / SP_THREADS;          // vectors per share
+#pragma unroll 4
+    for (int q = tid; q < n_shares * deep; q += SP_THREADS) {
+      const int i = shares[q / deep] + q % deep * SP_THREADS;
+      if (i < n_vec) {
+        const uint32_t bits = reaching_bits<T>(vec(i), from);
+        if (bits) mask[i] = (uint8_t)bits;
       }
+    }
     __syncthreads();
     const uint32_t* words = reinterpret_cast<const uint32_t*>(mask);
     const int per_w = (n_words + SP_THREADS - 1) / SP_THREADS, w0 = min(tid * per_w, n_words), w1 = min(w0 + per_w, n_words);
@@ -718,12 +889,19 @@ sample_kernel(const SampleParams p) {
     if (mine && tot <= SP_LIST)
       for (int i = w0; i < w1; ++i)
         for (uint32_t b = words[i]; b; b &= b - 1u) {
-          const int bit = __ffs(b) - 1, e = (i * 4 + (bit >> 3)) * EPC + (bit & 7);
-          list[at++] = ((unsigned long long)float_key(logit(e)) << 32) | (uint32_t)(lo + e);
+          const int bit = __ffs(b) - 1;
+          list[at++] = (unsigned long long)((i * 4 + (bit >> 3)) * EPC + (bit & 7));
         }
+    __syncthreads();
+    if (tot <= SP_LIST)                                  // the logits: all at once, not one after the other by their finders
+      for (int i = tid; i < tot; i += SP_THREADS) {
+        const int e = (int)list[i];
+        list[i] = (unsigned long long)float_key(logit(e)) << 32 | (uint32_t)(lo + e);
+      }
     if (tid == 0) sh.list_n = tot;
     int n_list = tot;
-    sum_all<1>(cl, sh, turn, raw_sum, n_list);           // publishes the lists as well
+    if (have_raw) cl.sync();                             // publishes the lists
+    else sum_all<1>(cl, sh, turn, raw_sum, n_list);      // so do its barriers
     n_list = 0;
 #pragma unroll
     for (int q = 0; q < SP_MAX_CLUSTER; ++q)
@@ -747,17 +925,17 @@ sample_kernel(const SampleParams p) {
         __syncthreads();
         Draw d;
         d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = z_all; d.min_p = (double)p.min_p; d.u = (double)u;
-        // (a logit of the last bin is at most half a bin, and the rounding, below its middle)
-        d.key_lo = short_nucleus ? max(key_of(m - (bin_hi - 8388607.f) / per_bin), BOTTOM) : from == -FLT_MAX ? BOTTOM : key_of(from);
+        d.key_lo = from == -FLT_MAX ? BOTTOM : key_of(from);
+        d.key_top = key_of(m);
+        if (short_nucleus) d.key_top = min(key_of(fmaxf(m - (bin_lo - 8388609.f) / per_bin, -FLT_MAX)), d.key_top);
         d.complete = n_list == n_cand;
         int at_tok = -1, kept = 0;
         double w_tok = 0.0, total = 1.0;
         bool whole = true;
-        // a short one is cut by one warp, without a barrier
-        if (n_list <= 32 * SP_PER) {
-          if (warp == 0) whole = draw_from_list<1, KEY_BITS>(sh, list, n_list, key_of(m), d, weight, at_tok, w_tok, total, kept);
+        if (n_list <= SP_PAIRS) {
+          whole = draw_from_pairs(sh, list, n_list, d, weight, at_tok, w_tok, total, kept);
         } else {
-          whole = draw_from_list<SP_WARPS, KEY_BITS>(sh, list, n_list, key_of(m), d, weight, at_tok, w_tok, total, kept);
+          whole = draw_from_list<KEY_BITS>(sh, list, n_list, key_of(m), d, weight, at_tok, w_tok, total, kept);
         }
         if (tid == 0) sh.list_ok = whole ? 1 : 0;
         if (whole && at_tok >= 0) {
