@@ -36,7 +36,7 @@ constexpr int SP_PAIRS = SP_THREADS / 4;                 // most tokens of a lis
 // scratch behind the slice: thread maxima | list | one byte per 16-byte vector of the slice
 constexpr int SP_OFF_LIST = SP_THREADS * 4, SP_OFF_MASK = SP_OFF_LIST + SP_LIST * 8, SP_SMEM = 212 * 1024;   // largest, all told
 constexpr int SP_TAB = 64, SP_TAB_COPIES = 16;           // table of powers: entries, and copies (one per pair of banks)
-constexpr int SP_BINS = 2048, SP_BINS_PER_E = 64;        // histogram of a nucleus: bins, and how many to a factor of e
+constexpr int SP_BINS = 2048;                            // of a nucleus's histogram
 constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN is below it
 static_assert(SP_BINS * 4 <= SP_LIST * 8 && SP_BINS == 4 * SP_THREADS, "a histogram lies where a list does");
 static_assert(SP_SLICE_BYTES + SP_OFF_MASK + SP_SLICE_BYTES / 16 + 16 <= SP_SMEM, "scratch");
@@ -237,6 +237,29 @@ __device__ __forceinline__ double pow2_near(double t, const double* tab) {
   const double w = fma(b, r * f, b);
   return __hiloint2double(__double2hiint(w) + ((n >> 6) << 20), __double2loint(w));
 }
+
+// The same for sums over the vocabulary, in 18 instructions of which two are fp64 (more than sixty, ten of them fp64, with
+// pow2_near and a separate histogram): x s for s = s_hi + s_lo is reduced in fp32.  With zero = 1.5 * 2^17 - R / 64 the sum
+// x s_hi + zero is rounded to multiples of 1/64, R being 64 m s_hi rounded, so its bits count 64ths of the exponent from
+// the maximum's down (the bins of a histogram as well) and x s_hi less that multiple is a single fused operation: r.
+// Weights come relative to 2^(R / 64).  r is rounded to 2^-33, so a weight is off by ln2 2^-32 = 1.7e-10 of itself, and
+// 2^r - 1 < 0.0055 by 2.5 roundings of 2^-24: together less than 1e-9, of either sign.
+struct Reduced {
+  int bits;
+  float r;
+};
+__device__ __forceinline__ Reduced reduce_exponent(float x, float s_hi, float s_lo, float zero) {
+  const float tm = fmaf(x, s_hi, zero);
+  return {__float_as_int(tm), fmaf(x, s_lo, fmaf(x, s_hi, -(tm - zero)))};
+}
+__device__ __forceinline__ double pow2_reduced(const Reduced& a, const double* tab) {
+  const float ln2 = 0.69314718f, h = 0.5f / SP_TAB;
+  const float q = a.r * fmaf(a.r, fmaf(a.r, ln2 * ln2 * ln2 / 6.f, ln2 * ln2 / 2.f + h * h * (ln2 * ln2 * ln2 * ln2 / 24.f)), ln2);
+  const double b = tab[(a.bits & (SP_TAB - 1)) * SP_TAB_COPIES];
+  const double w = fma(b, (double)q, b);
+  return __hiloint2double(__double2hiint(w) + ((a.bits & -SP_TAB) << 14), __double2loint(w));
+}
+static_assert(SP_TAB == 64, "the bits above a table's index start at an exponent's");
 
 // Sums over the first NW warps of a block (all of them call it) of numbers below 2^53: integer weights, so that a
 // warp's sum is two hardware reductions of 27-bit halves instead of five rounds of shuffles.  Two slots in turn: one
@@ -676,15 +699,23 @@ sample_kernel(const SampleParams p) {
   const double scale = 1.4426950408889634 / (double)p.temperature, md = (double)m;
   const float floor_x = (float)fmax(md - 1000.0 / scale, -(double)FLT_MAX);      // lighter ones may count as 2^-1000
   // weights without a branch, where that floor is a logit well below the maximum (not so for an infinite maximum, one whose
-  // neighbouring floats are further apart, or a temperature that flattens the type's whole range)
+  // neighbouring floats are further apart, or a temperature that flattens the type's whole range) and nothing overflows
   const double floor_t = ((double)floor_x - md) * scale;
-  const bool plain = m < INFINITY && floor_t < -900.0 && floor_t > -1020.0;
+  const float s_hi = (float)scale, s_lo = (float)(scale - (double)s_hi);
+  const bool plain = m < INFINITY && floor_t < -900.0 && floor_t > -1020.0 && s_hi > 1e-30f && s_hi < 1e30f;
+  // they are 2^(x s) for |m s| up to 4096, above that 2^((x - m) s): x is within a factor of two of m then, which makes the
+  // difference exact
+  const float shift = fabs(md * scale) < 4096.0 ? 0.f : m;
+  const float top64 = plain ? (float)(rint((double)(m - shift) * (double)s_hi * SP_TAB) / SP_TAB) : 0.f, zero = 196608.f - top64;
+  auto reduced = [&](float x) -> Reduced { return reduce_exponent(fmaxf(x, floor_x) - shift, s_hi, s_lo, zero); };
+  const int top_bits = reduced(m).bits;                  // (a tie may put them one off top64's)
   auto weight = [&](float x) -> double {
     if (m == INFINITY) return x == m ? 1.0 : 0.0;
     const double t = ((double)x - md) * scale;
     return t >= -1000.0 ? pow2_near(t, tab) : 0.0;
   };
-  auto weight_plain = [&](float x) -> double { return pow2_near(((double)fmaxf(x, floor_x) - md) * scale, tab); };
+  auto weight_plain = [&](float x) -> double { return pow2_reduced(reduced(x), tab); };
+  const double unit = pow2_near((double)top64 - (double)(m - shift) * scale, tab);                   // weight_plain's, in weight's
   // keys of bf16 logits in 16 bits, so that both types descend through their own bits only
   auto key_of = [&](float x) -> uint32_t { return float_key(x) >> (32 - KEY_BITS); };
   constexpr uint32_t BOTTOM = KEY_NEG_INF >> (32 - KEY_BITS);
@@ -729,15 +760,16 @@ sample_kernel(const SampleParams p) {
   double raw_all = 0.0, z_all = -1.0;                    // z_all: weight of the vocabulary, where top-p needs it
   unsigned long long* list = reinterpret_cast<unsigned long long*>(scratch + SP_OFF_LIST);
   // ---- a nucleus: where does it end, to within a few histogram bins? ----
-  // Bins of 1/64 in the exponent (nearest, the last one open), counted; the last one is where all that is lighter weighs
-  // less than half of what a nucleus may leave out: n_cand e^-(b / 64) <= (1 - top_p) / 2.  The weight of a bin lies between those of its
-  // edges, so the running weight is known to +-0.8 %.  Bins before bin_lo are in the nucleus, those after bin_hi are not.
-  const float per_bin = (float)SP_BINS_PER_E / p.temperature;
-  const int last_bin = (int)fminf((float)(SP_BINS - 1), (float)SP_BINS_PER_E * logf(2.f * (float)n_cand / fmaxf(1.f - p.top_p, FLT_MIN)) + 2.f);
-  auto bin_of = [&](float x) -> float {                  // as the float 2^23 + bin
-    return fminf((m - x) * per_bin, (float)last_bin) + 8388608.f;
+  // Bins of 1/64 in the binary exponent (nearest), counted from the maximum's down to 2^-32 of it: what lies below is
+  // rarely of interest (n_cand e^-22 is what it weighs at most).  The weight of a bin lies between those of its edges, so
+  // the running weight is known to half a bin, +-0.6 %.  Bins before bin_lo are in the nucleus, those after bin_hi are not.
+  auto bin_of = [&](float x) -> int { return top_bits - reduced(x).bits; };
+  // the logit `bins` below the maximum's bin, as a float: no smaller one is nearer to it
+  auto bin_edge = [&](double bins) -> float {
+    const double top = (double)top64 + (double)(top_bits - __float_as_int(196608.f)) / SP_TAB;
+    return (float)fmax((double)shift + (top - bins / SP_TAB) / (double)s_hi, -(double)FLT_MAX);
   };
-  float bin_lo = 0.f, bin_hi = 0.f;                      // as 2^23 + bin
+  int bin_lo = 0, bin_hi = 0;
   bool narrowed = false, short_nucleus = false;
   if (need_z && plain && n_cand > SP_LIST) {
     int* hist = reinterpret_cast<int*>(list);
@@ -749,15 +781,16 @@ sample_kernel(const SampleParams p) {
       unpack_logits<T>(vec(i), x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
-        const int bin = __float_as_int(bin_of(x[e])) & (SP_BINS - 1);
-        if (bin < last_bin) atomicAdd(&hist[bin], 1);
-        w[e & 3] += weight_plain(x[e]);
+        const Reduced a = reduced(x[e]);
+        const unsigned bin = (unsigned)(top_bits - a.bits);
+        if (bin < SP_BINS - 1) atomicAdd(&hist[bin], 1);             // the last bin is what the others leave
+        w[e & 3] += pow2_reduced(a, tab);
       }
     }
     double v[2] = {raw_mine, (w[0] + w[1]) + (w[2] + w[3])};
     int none = 0;
     sum_all<2>(cl, sh, turn, v, none);                   // publishes the counts as well
-    raw_all = v[0]; z_all = v[1];
+    raw_all = v[0]; z_all = v[1] * unit;
     have_raw = true;
     constexpr int PER = SP_BINS / SP_THREADS;
     int count[PER] = {};
@@ -767,14 +800,15 @@ sample_kernel(const SampleParams p) {
         const int4 c = *reinterpret_cast<const int4*>(cl.map_shared_rank(hist, q) + tid * PER);
         count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
       }
-    // running weights from the bins' edges, half a bin to either side of its middle; 2e-5 for the bins' own rounding and
-    // for these sums'.  The open last bin (its count is what the others leave) weighs from nothing to its upper edge.
+    // running weights from the bins' edges, half a bin to either side of its middle (a hundredth more for s_lo, of which the
+    // bins know nothing); 2e-5 for these sums' rounding.  The last bin weighs from nothing to its upper edge.
+    const float off = (float)(top_bits - __float_as_int(196608.f));
     float light[PER], heavy[PER], light_at = 0.f, heavy_at = 0.f;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       const float b = (float)(tid * PER + q), c = (float)count[q];
-      light_at += c * ex2_approx(-(b + 0.501f) * (l2e / SP_BINS_PER_E)) * 0.99998f;
-      heavy_at += c * ex2_approx(-fmaxf(b - 0.501f, 0.f) * (l2e / SP_BINS_PER_E)) * 1.00002f;
+      light_at += c * ex2_approx((off - b - 0.51f) * (1.f / SP_TAB)) * 0.99998f;
+      heavy_at += c * ex2_approx((off - b + 0.51f) * (1.f / SP_TAB)) * 1.00002f;
       light[q] = light_at; heavy[q] = heavy_at;
     }
     float light_in = light_at, heavy_in = heavy_at;
@@ -784,13 +818,13 @@ sample_kernel(const SampleParams p) {
       if (lane >= o) { light_in += a; heavy_in += b; }
     }
     if (lane == 31) sh.edge[warp] = make_float2(light_in, heavy_in);
-    if (tid == 0) { sh.digit = last_bin; sh.above = last_bin; sh.found = 0; }
+    if (tid == 0) { sh.digit = sh.above = SP_BINS - 1; sh.found = 0; }
     __syncthreads();
     float light_0 = light_in - light_at, heavy_0 = heavy_in - heavy_at;
     for (int q = 0; q < warp; ++q) { light_0 += sh.edge[q].x; heavy_0 += sh.edge[q].y; }
-    const float goal = (float)((double)p.top_p * z_all);
+    const float goal = (float)((double)p.top_p * v[1]);
     // the first bin whose upper sum reaches the goal, and the first whose lower sum does
-    int first_hi = last_bin, first_lo = last_bin;
+    int first_hi = SP_BINS - 1, first_lo = SP_BINS - 1;
 #pragma unroll
     for (int q = PER - 1; q >= 0; --q) {
       if (heavy_0 + heavy[q] >= goal * 0.999999f) first_hi = tid * PER + q;
@@ -806,9 +840,9 @@ sample_kernel(const SampleParams p) {
     upto = __reduce_add_sync(0xffffffffu, upto);
     if (lane == 0) atomicAdd(&sh.found, upto);
     __syncthreads();
-    bin_lo = 8388608.f + (float)sh.digit; bin_hi = 8388608.f + (float)sh.above;
+    bin_lo = sh.digit; bin_hi = sh.above < SP_BINS - 1 ? sh.above : INT_MAX;
     narrowed = true;
-    short_nucleus = sh.found <= SP_LIST && sh.above < last_bin;    // its tokens, and a few too many, as a list
+    short_nucleus = sh.found <= SP_LIST && sh.above < SP_BINS - 1;    // its tokens, and a few too many, as a list
     cl.sync();                                           // everybody has read the counts: the list may go over them
   }
   // ---- short list (top-k: the bound is tight while the k wanted are at most half of the shares) ----
@@ -857,7 +891,7 @@ sample_kernel(const SampleParams p) {
       }
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
-    if (short_nucleus) from = fmaxf(m - (bin_hi - 8388607.f) / per_bin, -FLT_MAX);   // half a bin and the rounding below its middle
+    if (short_nucleus) from = bin_edge((double)bin_hi + 1.0);            // its lower edge, and half a bin
     double raw_sum[1] = {raw_mine};
     // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order.
     // Only the shares whose maximum reaches it are looked at, and those by all threads.
@@ -927,7 +961,7 @@ sample_kernel(const SampleParams p) {
         d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = z_all; d.min_p = (double)p.min_p; d.u = (double)u;
         d.key_lo = from == -FLT_MAX ? BOTTOM : key_of(from);
         d.key_top = key_of(m);
-        if (short_nucleus) d.key_top = min(key_of(fmaxf(m - (bin_lo - 8388609.f) / per_bin, -FLT_MAX)), d.key_top);
+        if (short_nucleus) d.key_top = min(key_of(bin_edge((double)bin_lo - 1.0)), d.key_top);
         d.complete = n_list == n_cand;
         int at_tok = -1, kept = 0;
         double w_tok = 0.0, total = 1.0;
@@ -1025,12 +1059,13 @@ sample_kernel(const SampleParams p) {
       unpack_logits<T>(raw, x);
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
-        const float b = bin_of(x[e]);
-        s4[e & 3] += b < bin_lo ? weight_plain(x[e]) : 0.0;
+        const Reduced a = reduced(x[e]);
+        const int b = top_bits - a.bits;
+        s4[e & 3] += b < bin_lo ? pow2_reduced(a, tab) : 0.0;
         if (b >= bin_lo && b <= bin_hi && x[e] > -INFINITY) { k_hi = max(k_hi, key_of(x[e])); k_lo = min(k_lo, key_of(x[e])); }
       }
     }
-    base[0] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    base[0] = ((s4[0] + s4[1]) + (s4[2] + s4[3])) * unit;
     k_hi = __reduce_max_sync(0xffffffffu, k_hi); k_lo = __reduce_min_sync(0xffffffffu, k_lo);
     if (lane == 0) { sh.key_hi[warp] = k_hi; sh.key_lo[warp] = k_lo; }
     int none = 0;
@@ -1055,10 +1090,10 @@ sample_kernel(const SampleParams p) {
         unpack_logits<T>(raw, x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          const float b = bin_of(x[e]);
+          const int b = bin_of(x[e]);
           if (b >= bin_lo && b <= bin_hi) {
             const uint32_t k = key_of(x[e]);
-            const double w = weight_plain(x[e]);
+            const double w = weight_plain(x[e]) * unit;
             s3[0] += k >= t[0] ? w : 0.0;
             s3[1] += k >= t[1] ? w : 0.0;
             s3[2] += k >= t[2] ? w : 0.0;
@@ -1104,7 +1139,7 @@ sample_kernel(const SampleParams p) {
   const int seg = (p.slice + SP_WARPS * SEG_UNIT - 1) / (SP_WARPS * SEG_UNIT) * SEG_UNIT;
   const int s0 = min(warp * seg, n_vec * EPC), s1 = min(s0 + seg, n_vec * EPC);   // whole vectors; the padding is -inf
   {
-    double s[2] = {0.0, 0.0};
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
     int ngt = 0, neq = 0;
     if (T_key == BOTTOM && min_w == 0.0 && plain) {      // no cut at all: every candidate, without a branch
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
@@ -1112,10 +1147,11 @@ sample_kernel(const SampleParams p) {
         unpack_logits<T>(vec(i), x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          s[e & 1] += x[e] > floor_x ? weight_plain(x[e]) : 0.0;
+          s[e & 3] += x[e] > floor_x ? weight_plain(x[e]) : 0.0;
           ngt += x[e] > -INFINITY ? 1 : 0;
         }
       }
+      s[0] = ((s[0] + s[1]) + (s[2] + s[3])) * unit;
     } else {
       const float t = key_value(T_key), t_all = T_key == BOTTOM ? -INFINITY : t;
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
@@ -1134,7 +1170,6 @@ sample_kernel(const SampleParams p) {
         }
       }
     }
-    s[0] += s[1];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
     ngt = __reduce_add_sync(0xffffffffu, ngt);
@@ -1211,20 +1246,54 @@ sample_kernel(const SampleParams p) {
   const int hit_eq = sh.hit_eq, kept = sh.kept;
   const double total = sh.total, target = (double)u * total;
   if (sh.hit == rank * SP_WARPS + warp) {
-    // walk of the segment, 32 consecutive tokens at a time
-    double before = sh.before;
-    int eq = tie_in ? hit_eq : 0, tok = -1, fallback = -1;
-    for (int i0 = s0; i0 < s1 && tok < 0; i0 += 32) {
-      const int i = i0 + lane;
-      const float x = i < min(s1, cnt) ? logit(i) : -INFINITY;
+    // a run of it per lane, then the run that holds the target, 32 consecutive tokens at a time
+    auto kept_weight = [&](float x, bool& eq) -> double {  // of a token that is not at T_key; ties are counted
       const uint32_t k = key_of(x);
-      const bool is_eq = k == T_key && k > BOTTOM;
+      eq = k == T_key && k > BOTTOM;
+      if (!(k > T_key && x > -INFINITY)) return 0.0;
+      const double w = weight(x);
+      return w >= min_w ? w : 0.0;
+    };
+    const int run_len = (s1 - s0 + 32 * EPC - 1) / (32 * EPC) * EPC, r0 = min(s0 + lane * run_len, s1), r1 = min(r0 + run_len, s1);
+    double run_w = 0.0;
+    int run_eq = 0;
+    for (int i = r0 / EPC; i < r1 / EPC; ++i) {
+      float x[EPC];
+      unpack_logits<T>(vec(i), x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        bool eq;
+        run_w += kept_weight(x[e], eq);
+        run_eq += eq ? 1 : 0;
+      }
+    }
+    int eq_inc = run_eq;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, eq_inc, o);
+      if (lane >= o) eq_inc += y;
+    }
+    int eq = max((tie_in ? hit_eq : 0) - (eq_inc - run_eq), 0);
+    run_w += min(run_eq, eq) * w_T;
+    double inc = run_w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    const uint32_t some = __ballot_sync(0xffffffffu, run_w > 0.0);
+    const uint32_t past = __ballot_sync(0xffffffffu, run_w > 0.0 && sh.before + inc > target);
+    const int at = past ? __ffs(past) - 1 : some ? 31 - __clz(some) : 31;    // rounding at the far end: the last with a weight
+    double before = __shfl_sync(0xffffffffu, sh.before + (inc - run_w), at);
+    eq = __shfl_sync(0xffffffffu, eq, at);
+    const int w0 = __shfl_sync(0xffffffffu, r0, at), w1 = __shfl_sync(0xffffffffu, r1, at);
+    int tok = -1, fallback = -1;
+    for (int i0 = w0; i0 < w1 && tok < 0; i0 += 32) {
+      const int i = i0 + lane;
+      bool is_eq;
+      double w = kept_weight(i < min(w1, cnt) ? logit(i) : -INFINITY, is_eq);
       const uint32_t eq_mask = __ballot_sync(0xffffffffu, is_eq);
-      double w = 0.0;
-      bool in = false;
-      if (k > T_key && x > -INFINITY) { w = weight(x); in = w >= min_w; }
-      else if (is_eq) { in = __popc(eq_mask & ((1u << lane) - 1u)) < eq; w = w_T; }
-      if (!in) w = 0.0;
+      if (is_eq && __popc(eq_mask & ((1u << lane) - 1u)) < eq) w = w_T;
       eq -= min(eq, __popc(eq_mask));
       double inc = w;
 #pragma unroll
@@ -1232,8 +1301,8 @@ sample_kernel(const SampleParams p) {
         const double y = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += y;
       }
-      const uint32_t got = __ballot_sync(0xffffffffu, in && before + inc > target);
-      const uint32_t any = __ballot_sync(0xffffffffu, in);
+      const uint32_t got = __ballot_sync(0xffffffffu, w > 0.0 && before + inc > target);
+      const uint32_t any = __ballot_sync(0xffffffffu, w > 0.0);
       if (any) fallback = i0 + 31 - __clz(any);
       if (got) tok = i0 + __ffs(got) - 1;
       before += __shfl_sync(0xffffffffu, inc, 31);
@@ -1274,9 +1343,10 @@ focus_status launch_sample(focus_ctx* ctx, SampleParams& p, cudaStream_t st) {
   constexpr int EPC = 16 / sizeof(T);
   if ((size_t)p.vocab * sizeof(T) > (size_t)SP_MAX_CLUSTER * SP_SLICE_BYTES) return FOCUS_ERR_UNSUPPORTED;
   // cluster size: a slice has to fit in shared memory, and small calls spread a row over more SMs while there are idle
-  // ones and a slice still feeds every thread
+  // ones and a slice still feeds every thread.  No finer than that: two CTAs of different rows on one SM cost more than
+  // their halves save (72 rows of 126464 bf16 logits, nucleus: 40 us with two CTAs per row, 56 with four).
   int nc = 1;
-  while (nc < SP_MAX_CLUSTER && ((long long)p.vocab * sizeof(T) > (long long)nc * SP_SLICE_BYTES / 2 ||
+  while (nc < SP_MAX_CLUSTER && ((long long)p.vocab * sizeof(T) > (long long)nc * SP_SLICE_BYTES ||
                                  (p.max_rows * nc * 2 <= ctx->sm_count && p.vocab > nc * SP_THREADS * EPC)))
     nc *= 2;
   if (nc > 1 && p.max_rows >= ctx->sm_count) {           // rows enough for every SM: no slices
