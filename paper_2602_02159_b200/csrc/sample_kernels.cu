@@ -5,17 +5,22 @@
 // (the logits cross HBM once) and every later pass runs there; the CTAs exchange a few numbers per pass through
 // distributed shared memory.  Weights and sums are fp64: a token is decided by comparing two sums over the vocabulary,
 // and in fp32 those sums are off by as much as a rare token weighs.  Sums run in a fixed order (lanes, warps, CTAs), so
-// the answer does not depend on timing or on the number of rows.
+// the answer does not depend on timing.
 //
 // The kept set is a prefix of the descending order.  Two ways to it:
 //   short list  (up to 2048 tokens).  Which logits to collect: for top-k up to 1024, those from the k-th largest of the
 //               maxima of the threads' shares up -- a lower bound of the k-th largest logit that few more reach; for a
 //               nucleus, those up to the histogram bin in which it must end.  They are collected in index order and cut by
-//               one CTA (by one warp, if they are at most 128), which has them in registers.
+//               one CTA with integer weights in registers: up to 128 tokens by comparing all pairs, else by searching the
+//               last kept key.
 //   any length  (no cut, min-p alone, longer top-k and nuclei): the key T of the last kept logit, by counts (top-k: 8-bit
-//               digits of a radix descent) and by weight (top-p: two bits of the key per pass, of those that the
-//               histogram leaves open); (T, how many of the tokens at T) says all about the set.  Then the kept weight per
-//               warp segment in index order, the segment that holds u * total, and its walk.
+//               digits of a radix descent) and by weight (top-p: quarters of the keys that the histogram leaves open);
+//               (T, how many of the tokens at T) says all about the set.  Then the kept weight per warp segment in index
+//               order, the segment that holds u * total, a run of it per lane, and its walk.
+// What bounds it: HBM for many rows of top-k (512 rows of 126464 bf16 logits, top-k 50, top-p 0.9: 66 us, of which the
+// loads are 20), instruction issue in the pass over the vocabulary's weights for a nucleus (35 rows, top-p 0.95: 35 us;
+// 11 us are that pass, 24 instructions per logit), and the latency of a dozen barriers and exchanges for one row (50257
+// fp32 logits: 14 us).
 #include <cooperative_groups.h>
 #include <float.h>
 
@@ -41,6 +46,10 @@ constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;            // float_key(-inf); NaN
 static_assert(SP_BINS * 4 <= SP_LIST * 8 && SP_BINS == 4 * SP_THREADS, "a histogram lies where a list does");
 static_assert(SP_SLICE_BYTES + SP_OFF_MASK + SP_SLICE_BYTES / 16 + 16 <= SP_SMEM, "scratch");
 
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
 struct SegSum {            // one warp's contiguous segment of the row
   double w;                // kept weight above the threshold key
   int n_gt, n_eq;          // tokens above it / at it
@@ -61,6 +70,7 @@ struct SampleShared {
   unsigned long long fx[2][SP_WARPS][3];
   int last[SP_WARPS];
   int digit, above, found;
+  uint4 tail;              // the vector that the row ends in
   uint32_t key_hi[SP_WARPS], key_lo[SP_WARPS];
   float2 edge[SP_WARPS];
   // the segment that holds u * total
@@ -122,7 +132,7 @@ __device__ __forceinline__ void sum_all(cg::cluster_group& cl, SampleShared& sh,
     for (int i = 0; i < N; ++i) sh.cta_d[t][i] = v[i];
     sh.cta_i[t] = cnt;
   }
-  cl.sync();
+  cluster_sync();
   const int nc = (int)cl.num_blocks();
   const SampleShared* far = cl.map_shared_rank(&sh, min(lane, nc - 1));   // lane q fetches rank q's sums
   double f[N];
@@ -147,7 +157,7 @@ __device__ __forceinline__ void first_all(cg::cluster_group& cl, SampleShared& s
   const int nc = (int)cl.num_blocks();
   if (nc > 1) {
     if (threadIdx.x == 0) sh.cta_first = v;
-    cl.sync();
+    cluster_sync();
     v = lane < nc ? cl.map_shared_rank(&sh, lane)->cta_first : make_uint2(0u, 0u);
     v.x = __reduce_max_sync(0xffffffffu, v.x); v.y = __reduce_add_sync(0xffffffffu, v.y);
   }
@@ -331,33 +341,42 @@ __device__ __forceinline__ unsigned long long excl_fx(SampleShared& sh, int& tur
   }
   return before;
 }
-// The largest t such that what(t) = the sum over the threads of f(t) reaches `goal`, searched two bits per step among the
-// keys that share the bits of `hi` above `vary` (even); what(lowest of them) reaches it by assumption.  `above`: what(t + 1).
+// Three keys that cut lo + 1 .. hi into quarters, and which part a search among lo .. hi goes on with: `reached` says
+// whether what(t[i]) reaches the goal.
+__device__ __forceinline__ void quarter(uint32_t lo, uint32_t hi, uint32_t (&t)[3]) {
+  const uint32_t n = hi - lo, r = n & 3u;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) t[i] = lo + (i + 1) * (n >> 2) + (((i + 1) * r + 3u) >> 2);
+}
+template <typename V>
+__device__ __forceinline__ void go_on(uint32_t& lo, uint32_t& hi, V& above, const uint32_t (&t)[3], const bool (&reached)[3], const V (&what)[3]) {
+  if (reached[2]) lo = t[2];
+  else if (reached[1]) { lo = t[1]; hi = t[2] - 1; above = what[2]; }
+  else if (reached[0]) { lo = t[0]; hi = t[1] - 1; above = what[1]; }
+  else { hi = t[0] - 1; above = what[0]; }
+}
+// The largest t of lo .. hi such that what(t) = the sum over the threads of f(t) reaches `goal`, a quarter of the keys left
+// per step; what(lo) reaches it by assumption.  `above`: what(hi + 1), then what(t + 1).
 template <int NW, bool COUNTS, typename F>
-__device__ __forceinline__ uint32_t largest_reaching(SampleShared& sh, int& turn, uint32_t hi, int vary, unsigned long long goal,
+__device__ __forceinline__ uint32_t largest_reaching(SampleShared& sh, int& turn, uint32_t lo, uint32_t hi, unsigned long long goal,
                                                      unsigned long long& above, F f) {
-  uint32_t best = vary >= 32 ? 0u : hi >> vary << vary;
-  above = 0ull;
-  for (int sft = vary; sft > 0;) {
-    sft -= 2;
-    const uint32_t t1 = best | (1u << sft), t2 = best | (2u << sft), t3 = best | (3u << sft);
+  while (lo < hi) {
+    uint32_t t[3];
+    quarter(lo, hi, t);
     unsigned long long s[3];
     if constexpr (COUNTS) {
       unsigned c[3];
-      f(t1, t2, t3, c);
+      f(t[0], t[1], t[2], c);
       sum_counts<NW>(sh, turn, c, s);
     } else {
-      f(t1, t2, t3, s);
+      f(t[0], t[1], t[2], s);
       sum_fx<NW, 3>(sh, turn, s);
     }
-    if (s[2] >= goal) best = t3;
-    else if (s[1] >= goal) { best = t2; above = s[2]; }
-    else if (s[0] >= goal) { best = t1; above = s[1]; }
-    else above = s[0];
+    const bool reached[3] = {s[0] >= goal, s[1] >= goal, s[2] >= goal};
+    go_on(lo, hi, above, t, reached, s);
   }
-  return best;
+  return lo;
 }
-__device__ __forceinline__ int even_bits(uint32_t differ) { return (33 - __clz(differ)) & ~1; }
 
 constexpr double FX_ONE = 1125899906842624.0;            // 2^50: a weight of 1 (a thread holds at most four)
 
@@ -408,8 +427,8 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
   };
   uint32_t key_end = d.key_lo;                           // nor below this
   if (d.top_k > 0 && d.top_k < n) {
-    unsigned long long above;
-    const uint32_t t = largest_reaching<NW, true>(sh, turn, key_hi, even_bits(key_hi ^ d.key_lo), (unsigned long long)d.top_k, above,
+    unsigned long long above = 0ull;
+    const uint32_t t = largest_reaching<NW, true>(sh, turn, d.key_lo, key_hi, (unsigned long long)d.top_k, above,
                                                   [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&s)[3]) {
       s[0] = s[1] = s[2] = 0u;
 #pragma unroll
@@ -428,61 +447,27 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
     const unsigned long long goal = (unsigned long long)ceil(goal_w);
     if (a[0] < goal && !d.complete) return false;
     if (a[0] >= goal) {
-      // the tokens above key_top are in; the few from there down, if they are few, by comparing all pairs of them
-      int slot[SP_PER];
-      unsigned long long* b_fx = reinterpret_cast<unsigned long long*>(sh.hist[1]);
-      uint2* b_key = reinterpret_cast<uint2*>(sh.hist[0]);               // key, place; later .x: whether it is in
-      unsigned long long sure[1] = {0ull};
-      if (tid == 0) sh.found = 0;
-      __syncthreads();
+      unsigned long long above[1] = {0ull};
 #pragma unroll
-      for (int q = 0; q < SP_PER; ++q) {
-        slot[q] = -1;
-        if (in >> q & 1u) {
-          if (key[q] > d.key_top) sure[0] += fx[q];
-          else slot[q] = atomicAdd(&sh.found, 1);
-          if (slot[q] >= 0 && slot[q] < SP_PAIRS) {
-            b_fx[slot[q]] = fx[q];
-            b_key[slot[q]] = make_uint2(key[q], (uint32_t)(tid * SP_PER + q));
-          }
+      for (int q = 0; q < SP_PER; ++q) above[0] += (in >> q & 1u) && key[q] > d.key_top ? fx[q] : 0ull;
+      sum_fx<NW, 1>(sh, turn, above);
+      uint32_t lo = min(key_end, d.key_top), hi = d.key_top;
+      if (above[0] >= goal) { lo = hi + 1; hi = key_hi; above[0] = 0ull; }         // (should key_top not hold)
+      const uint32_t t = largest_reaching<NW, false>(sh, turn, lo, hi, goal, above[0],
+                                              [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
+        s[0] = s[1] = s[2] = 0ull;
+#pragma unroll
+        for (int q = 0; q < SP_PER; ++q) {
+          const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
+          s[0] += key[q] >= t1 ? v : 0ull;
+          s[1] += key[q] >= t2 ? v : 0ull;
+          s[2] += key[q] >= t3 ? v : 0ull;
         }
-      }
-      sum_fx<NW, 1>(sh, turn, sure);
-      const int n_b = sh.found;
-      if (n_b <= SP_PAIRS) {
-        const int i = tid >> 2;
-        const uint2 me = b_key[min(i, max(n_b - 1, 0))];
-        unsigned long long above = 0ull;
-        for (int j = tid & 3; j < n_b; j += 4) {
-          const uint2 o = b_key[j];
-          if (o.x > me.x || (o.x == me.x && o.y < me.y)) above += b_fx[j];
-        }
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-        __syncthreads();
-        if (i < n_b && (tid & 3) == 0) b_key[i].x = sure[0] + above < goal ? 1u : 0u;
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < SP_PER; ++q)
-          if (slot[q] >= 0 && b_key[slot[q]].x == 0u) in &= ~(1u << q);
-      } else {
-        unsigned long long above;
-        const uint32_t t = largest_reaching<NW, false>(sh, turn, d.key_top, even_bits(d.key_top ^ key_end), goal, above,
-                                                [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned long long (&s)[3]) {
-          s[0] = s[1] = s[2] = 0ull;
-#pragma unroll
-          for (int q = 0; q < SP_PER; ++q) {
-            const unsigned long long v = in >> q & 1u ? fx[q] : 0ull;
-            s[0] += key[q] >= t1 ? v : 0ull;
-            s[1] += key[q] >= t2 ? v : 0ull;
-            s[2] += key[q] >= t3 ? v : 0ull;
-          }
-        });
-        // how many of the tokens at t it takes (their weight is one number)
-        const double each = rint(weight(key_to_float(KEY_BITS == 32 ? t : t << 16 | (t & 0x8000u ? 0u : 0xFFFFu))) * FX_ONE);
-        const double need = ceil((double)(goal - above) / each);
-        cut_at(t, (unsigned long long)fmin(fmax(need, 1.0), (double)SP_LIST));
-      }
+      });
+      // how many of the tokens at t it takes (their weight is one number)
+      const double each = rint(weight(key_to_float(KEY_BITS == 32 ? t : t << 16 | (t & 0x8000u ? 0u : 0xFFFFu))) * FX_ONE);
+      const double need = ceil((double)(goal - above[0]) / each);
+      cut_at(t, (unsigned long long)fmin(fmax(need, 1.0), (double)SP_LIST));
     }
   }
   if (d.min_p > 0.0) {
@@ -675,7 +660,11 @@ sample_kernel(const SampleParams p) {
       for (int q = 0; q < U; ++q) take(raw[q], i + q * STEP);
     }
     for (; i + EPC <= cnt; i += STEP) take(__ldg(reinterpret_cast<const uint4*>(row + i)), i);
-    if (i < cnt) take(tail_vector(i), i);
+    if (i < cnt) {
+      const uint4 raw = tail_vector(i);
+      sh.tail = raw;
+      take(raw, i);
+    }
   }
   for (int i = tid; i < SP_TAB * SP_TAB_COPIES; i += SP_THREADS) {         // as the product of its binary digits' powers
     const double f[6] = {1.0108892860517005, 1.0218971486541166, 1.0442737824274138, 1.0905077326652577, 1.189207115002721,
@@ -692,7 +681,7 @@ sample_kernel(const SampleParams p) {
   first_all(cl, sh, m, n_cand);
   if (n_cand == 0) {
     if (lead) finish(-1, 0.f, 0.f, 0);
-    cl.sync();
+    cluster_sync();
     return;
   }
   // ---- weights: 2^((x - m) log2(e) / temperature) ----
@@ -727,7 +716,7 @@ sample_kernel(const SampleParams p) {
   };
   auto vec = [&](int i) -> uint4 {                       // vector i, NaN as -inf
     if constexpr (STREAM) {
-      uint4 raw = (i + 1) * EPC <= cnt ? __ldg(reinterpret_cast<const uint4*>(row + i * EPC)) : tail_vector(i * EPC);
+      uint4 raw = (i + 1) * EPC <= cnt ? __ldg(reinterpret_cast<const uint4*>(row + i * EPC)) : sh.tail;
       float a, b;
       clean_logits<T>(raw, a, b);
       return raw;
@@ -843,14 +832,14 @@ sample_kernel(const SampleParams p) {
     bin_lo = sh.digit; bin_hi = sh.above < SP_BINS - 1 ? sh.above : INT_MAX;
     narrowed = true;
     short_nucleus = sh.found <= SP_LIST && sh.above < SP_BINS - 1;    // its tokens, and a few too many, as a list
-    cl.sync();                                           // everybody has read the counts: the list may go over them
+    cluster_sync();                                           // everybody has read the counts: the list may go over them
   }
   // ---- short list (top-k: the bound is tight while the k wanted are at most half of the shares) ----
   if (short_nucleus || (cut_k && p.top_k <= min(SP_LIST_K, groups / 2)) || n_cand <= SP_LIST) {
     float from = -FLT_MAX;                               // collect the logits from here up
     if (n_cand > SP_LIST && cut_k) {
       uint32_t least = 0xFFFFFFFFu, kth;
-      unsigned long long above;
+      unsigned long long above = 0ull;
       int own_turn = 0;
       if (nc == 1) {                                     // 512 keys: one warp, without barriers
         if (warp == 0) {
@@ -858,7 +847,7 @@ sample_kernel(const SampleParams p) {
 #pragma unroll
           for (int q = 0; q < SP_WARPS; ++q) { key[q] = share_key[lane + 32 * q]; least = min(least, key[q]); }
           least = __reduce_min_sync(0xffffffffu, least);
-          kth = largest_reaching<1, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k, above,
+          kth = largest_reaching<1, true>(sh, own_turn, least, key_of(m), (unsigned long long)p.top_k, above,
                                           [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
             c[0] = c[1] = c[2] = 0u;
 #pragma unroll
@@ -881,7 +870,7 @@ sample_kernel(const SampleParams p) {
         if (lane == 0) atomicMin(reinterpret_cast<unsigned*>(&sh.digit), least);
         __syncthreads();
         least = (uint32_t)sh.digit;
-        kth = largest_reaching<SP_WARPS, true>(sh, own_turn, key_of(m), even_bits(key_of(m) ^ least), (unsigned long long)p.top_k,
+        kth = largest_reaching<SP_WARPS, true>(sh, own_turn, least, key_of(m), (unsigned long long)p.top_k,
                                                above, [&](uint32_t t1, uint32_t t2, uint32_t t3, unsigned (&c)[3]) {
           c[0] = c[1] = c[2] = 0u;
 #pragma unroll
@@ -904,13 +893,19 @@ sample_kernel(const SampleParams p) {
     const int my_place = block_excl_scan(wanted ? 1 : 0, sh.scan_i, n_shares);
     if (wanted) shares[my_place] = (uint16_t)tid;
     __syncthreads();
+    auto look_at = [&](int i) {
+      const uint32_t bits = reaching_bits<T>(vec(i), from);
+      if (bits) mask[i] = (uint8_t)bits;
+    };
     const int deep = (n_vec + SP_THREADS - 1) / SP_THREADS;          // vectors per share
+    if (n_shares * 4 > SP_THREADS) {                     // most of the work: no lookup then
 #pragma unroll 4
-    for (int q = tid; q < n_shares * deep; q += SP_THREADS) {
-      const int i = shares[q / deep] + q % deep * SP_THREADS;
-      if (i < n_vec) {
-        const uint32_t bits = reaching_bits<T>(vec(i), from);
-        if (bits) mask[i] = (uint8_t)bits;
+      for (int i = tid; i < n_vec; i += SP_THREADS) look_at(i);
+    } else {
+#pragma unroll 4
+      for (int q = tid; q < n_shares * deep; q += SP_THREADS) {
+        const int i = shares[q / deep] + q % deep * SP_THREADS;
+        if (i < n_vec) look_at(i);
       }
     }
     __syncthreads();
@@ -934,7 +929,7 @@ sample_kernel(const SampleParams p) {
       }
     if (tid == 0) sh.list_n = tot;
     int n_list = tot;
-    if (have_raw) cl.sync();                             // publishes the lists
+    if (have_raw) cluster_sync();                             // publishes the lists
     else sum_all<1>(cl, sh, turn, raw_sum, n_list);      // so do its barriers
     n_list = 0;
 #pragma unroll
@@ -945,16 +940,15 @@ sample_kernel(const SampleParams p) {
     if (n_list <= SP_LIST) {                             // more: ties at the bound (uniform over the cluster)
       if (rank == 0) {
         // the other slices follow this one: the list stays in index order
-        int c[SP_MAX_CLUSTER], have = tot;
-#pragma unroll
-        for (int q = 1; q < SP_MAX_CLUSTER; ++q) c[q] = q < nc ? cl.map_shared_rank(&sh, q)->list_n : 0;
-#pragma unroll
-        for (int q = 1; q < SP_MAX_CLUSTER; ++q) {
-          if (q < nc) {
-            const unsigned long long* src = cl.map_shared_rank(list, q);
-            for (int i = tid; i < c[q]; i += SP_THREADS) list[have + i] = src[i];
+        if (nc > 1) {
+          if (tid < nc) sh.scan_i[tid] = cl.map_shared_rank(&sh, tid)->list_n;
+          __syncthreads();
+#pragma unroll 1
+          for (int i = tot + tid; i < n_list; i += SP_THREADS) {
+            int q = 1, at = i - tot;
+            while (at >= sh.scan_i[q]) at -= sh.scan_i[q++];
+            list[i] = cl.map_shared_rank(list, q)[at];
           }
-          have += c[q];
         }
         __syncthreads();
         Draw d;
@@ -977,9 +971,9 @@ sample_kernel(const SampleParams p) {
           finish((int)(uint32_t)list[at_tok], (float)(w_tok / total), (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
         }
       }
-      cl.sync();                                         // the lists have been read, the outcome is known
+      cluster_sync();                                         // the lists have been read, the outcome is known
       if (cl.map_shared_rank(&sh, 0)->list_ok) {
-        cl.sync();
+        cluster_sync();
         return;
       }
     }
@@ -992,7 +986,7 @@ sample_kernel(const SampleParams p) {
     int need = p.top_k;
     for (int shift = KEY_BITS - 8; shift >= 0; shift -= 8) {
       const int b = (shift >> 3) & 1;
-      cl.sync();                                         // last round's readers of this histogram are done
+      cluster_sync();                                         // last round's readers of this histogram are done
       for (int i = tid; i < 256; i += SP_THREADS) sh.hist[b][i] = 0;
       __syncthreads();
       for (int i = tid; i < n_vec; i += SP_THREADS) {
@@ -1004,7 +998,7 @@ sample_kernel(const SampleParams p) {
           if (k > BOTTOM && (shift + 8 >= KEY_BITS || (k >> (shift + 8)) == prefix)) atomicAdd(&sh.hist[b][(k >> shift) & 255u], 1);
         }
       }
-      cl.sync();
+      cluster_sync();
       if (tid < 256) {
         int c = 0;
         for (int q = 0; q < nc; ++q) c += cl.map_shared_rank(&sh, q)->hist[b][tid];
@@ -1024,7 +1018,7 @@ sample_kernel(const SampleParams p) {
       need -= sh.above;
     }
     T_key = prefix; quota = need;
-    cl.sync();
+    cluster_sync();
   }
   // ---- top-p: weight of the tokens from a key up ----
   auto weights_from = [&](uint32_t k1, uint32_t k2, uint32_t k3, double (&s)[3]) {
@@ -1076,22 +1070,20 @@ sample_kernel(const SampleParams p) {
     }
     k_hi = __reduce_max_sync(0xffffffffu, k_hi); k_lo = __reduce_min_sync(0xffffffffu, k_lo);
     const double target = (double)p.top_p * z_all;
-    const int vary = even_bits(k_hi ^ k_lo);
-    uint32_t best = vary >= 32 ? 0u : k_hi >> vary << vary;
-    double above = base[0];                              // weight before the bins, and in them from best + 2^sft up
-    for (int sft = vary; sft > 0;) {
-      sft -= 2;
-      const uint32_t t[3] = {best | (1u << sft), best | (2u << sft), best | (3u << sft)};
+    const float x_lo = key_value(k_lo), x_hi = key_value(k_hi);        // these keys are all there is in the open bins
+    double above = base[0];                              // weight from k_hi + 1 up
+    while (k_lo < k_hi) {
+      uint32_t t[3];
+      quarter(k_lo, k_hi, t);
       double s3[3] = {0.0, 0.0, 0.0};
       for (int i = tid; i < n_vec; i += SP_THREADS) {
         const uint4 raw = vec(i);
-        if (bin_of(largest_of<T>(raw)) > bin_hi) continue;
+        if (!(largest_of<T>(raw) >= x_lo)) continue;
         float x[EPC];
         unpack_logits<T>(raw, x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          const int b = bin_of(x[e]);
-          if (b >= bin_lo && b <= bin_hi) {
+          if (x[e] >= x_lo && x[e] <= x_hi) {
             const uint32_t k = key_of(x[e]);
             const double w = weight_plain(x[e]) * unit;
             s3[0] += k >= t[0] ? w : 0.0;
@@ -1101,11 +1093,12 @@ sample_kernel(const SampleParams p) {
         }
       }
       sum_all<3>(cl, sh, turn, s3, none);
-      if (base[0] + s3[2] >= target) best = t[2];
-      else if (base[0] + s3[1] >= target) { best = t[1]; above = base[0] + s3[2]; }
-      else if (base[0] + s3[0] >= target) { best = t[0]; above = base[0] + s3[1]; }
-      else above = base[0] + s3[0];
+#pragma unroll
+      for (int q = 0; q < 3; ++q) s3[q] += base[0];
+      const bool reached[3] = {s3[0] >= target, s3[1] >= target, s3[2] >= target};
+      go_on(k_lo, k_hi, above, t, reached, s3);
     }
+    const uint32_t best = k_lo;
     T_key = best;
     quota = (int)fmin(fmax(ceil((target - above) / weight(key_value(best))), 1.0), (double)INT_MAX);
   } else if (cut_p) {
@@ -1151,7 +1144,8 @@ sample_kernel(const SampleParams p) {
           ngt += x[e] > -INFINITY ? 1 : 0;
         }
       }
-      s[0] = ((s[0] + s[1]) + (s[2] + s[3])) * unit;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] *= unit;
     } else {
       const float t = key_value(T_key), t_all = T_key == BOTTOM ? -INFINITY : t;
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
@@ -1162,14 +1156,23 @@ sample_kernel(const SampleParams p) {
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
           if (x[e] > t_all) {
-            const double w = weight(x[e]);
-            if (w >= min_w) { s[0] += w; ++ngt; }
+            double w;
+            bool in;
+            if (plain) {                                 // the exact weight only where min-p depends on its last bits
+              w = weight_plain(x[e]) * unit;
+              in = w >= min_w * (1.0 + 1e-8) || (w >= min_w * (1.0 - 1e-8) && weight(x[e]) >= min_w);
+            } else {
+              w = weight(x[e]);
+              in = w >= min_w;
+            }
+            if (in) { s[e & 3] += w; ++ngt; }
           } else if (T_key > BOTTOM && x[e] == t) {
             ++neq;
           }
         }
       }
     }
+    s[0] = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
     ngt = __reduce_add_sync(0xffffffffu, ngt);
@@ -1313,7 +1316,7 @@ sample_kernel(const SampleParams p) {
       finish(lo + tok, (float)(weight(x) / total), (float)((x == m ? 1.0 : exp((double)x - md)) / raw_all), kept);
     }
   }
-  cl.sync();                                             // nobody leaves while its shared memory may still be read
+  cluster_sync();                                             // nobody leaves while its shared memory may still be read
 }
 
 template <typename T, bool STREAM>
