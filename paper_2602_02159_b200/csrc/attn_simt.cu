@@ -15,12 +15,6 @@ __device__ __forceinline__ void load_slice(const T* __restrict__ p, float (&out)
       const float2 v = __ldg(reinterpret_cast<const float2*>(p));
       out[0] = v.x; out[1] = v.y;
     }
-  } else if constexpr (sizeof(T) == 1) {
-    float f[4];
-    if constexpr (EPL == 4) codes_to_float(__ldg(reinterpret_cast<const uint32_t*>(p)), T(), f);
-    else codes_to_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p)), T(), f);
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) out[e] = f[e];
   } else {
     if constexpr (EPL == 4) {
       const uint2 raw = __ldg(reinterpret_cast<const uint2*>(p));
@@ -78,7 +72,7 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
   constexpr int EPC = 16 / sizeof(KT);               // K elements per 16-byte load
   constexpr bool CODES = sizeof(KT) == 1;
   __shared__ __align__(16) float qs[R][D];
-  __shared__ float part_o[NW][R][D];
+  __shared__ __align__(16) float part_o[NW][R][D];
   __shared__ float part_ml[NW][R][2];
   __shared__ int row_ok[R];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -124,9 +118,33 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
     float s[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) s[i] = 0.f;
+    // Codes are few bytes: the chunk's V rows are requested at once, before the logits.  Keys and numerators go to the other
+    // lanes through the warp's part of part_o (idle until the end) rather than by shuffles, of which an SM does one per
+    // cycle: 83 rows, 8 heads of 64, 1024 keys took 24.6 us with them, ... without.
+    uint32_t vr[CODES ? 32 : 1];
+    float* p_sh = &part_o[warp][0][0];                 // [R][32]
+    int* key_sh = reinterpret_cast<int*>(p_sh + R * 32);
+    if constexpr (CODES) {
+      if (want_o) {
+        __syncwarp();
+        key_sh[lane] = key;
+        __syncwarp();
+#pragma unroll
+        for (int j4 = 0; j4 < 32; j4 += 4) {
+          const int4 kk = *reinterpret_cast<const int4*>(key_sh + j4);
+          const int ks[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const KT* src = Vg + (long long)max(ks[j], 0) * p.kv_stride_tok + lane * EPL;
+            if constexpr (EPL == 4) vr[j4 + j] = __ldg(reinterpret_cast<const uint32_t*>(src));
+            else vr[j4 + j] = __ldg(reinterpret_cast<const uint16_t*>(src));
+          }
+        }
+      }
+    }
     if (key >= 0) {
       const uint4* kr = reinterpret_cast<const uint4*>(Kg + (long long)key * p.kv_stride_tok);
-#pragma unroll UNROLL_DOT
+#pragma unroll (CODES ? 4 : UNROLL_DOT)
       for (int c = 0; c < D / EPC; ++c) {
         const uint4 raw = __ldg(kr + c);
         float kf[EPC];
@@ -171,10 +189,15 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) { si[i] = key >= 0 ? s[i] * p.scale : -INFINITY; mx[i] = si[i]; }
+    if constexpr (CODES) {
 #pragma unroll
-    for (int ofs = 16; ofs > 0; ofs >>= 1) {
+      for (int i = 0; i < R; ++i) asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(mx[i]) : "f"(mx[i]));
+    } else {
 #pragma unroll
-      for (int i = 0; i < R; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], ofs));
+      for (int ofs = 16; ofs > 0; ofs >>= 1) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], ofs));
+      }
     }
     bool any = false;
 #pragma unroll
@@ -191,10 +214,12 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
     float ps[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) ps[i] = pj[i];
+    if constexpr (!CODES) {                            // with codes every lane keeps its own part of the sum until the end
 #pragma unroll
-    for (int ofs = 16; ofs > 0; ofs >>= 1) {
+      for (int ofs = 16; ofs > 0; ofs >>= 1) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) ps[i] += __shfl_xor_sync(0xffffffffu, ps[i], ofs);
+        for (int i = 0; i < R; ++i) ps[i] += __shfl_xor_sync(0xffffffffu, ps[i], ofs);
+      }
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -207,19 +232,42 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
       for (int i = 0; i < R; ++i) pj[i] *= vscale;     // the row sums above took the numerators themselves
     }
     if (want_o && any) {
-      // the 32 V rows of the chunk, sixteen loads in flight; an absent key reads row 0 and is discarded
+      if constexpr (CODES) {
+        const uint32_t here = __ballot_sync(0xffffffffu, key >= 0);    // an absent key has read row 0, which is discarded
+#pragma unroll
+        for (int i = 0; i < R; ++i) p_sh[i * 32 + lane] = pj[i];
+        __syncwarp();
+#pragma unroll
+        for (int j4 = 0; j4 < 32; j4 += 4) {
+          float4 pk[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) pk[i] = *reinterpret_cast<const float4*>(p_sh + i * 32 + j4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float v[4];
+            codes_to_float(here >> (j4 + j) & 1u ? vr[j4 + j] : 0u, KT(), v);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const float w = j == 0 ? pk[i].x : j == 1 ? pk[i].y : j == 2 ? pk[i].z : pk[i].w;
+#pragma unroll
+              for (int e = 0; e < EPL; ++e) o[i][e] = fmaf(w, v[e], o[i][e]);
+            }
+          }
+        }
+      } else {
 #pragma unroll UNROLL_V
-      for (int jj = 0; jj < 32; ++jj) {
-        const int kk = __shfl_sync(0xffffffffu, key, jj);
-        float v[EPL];
-        load_slice<KT, EPL>(Vg + (long long)max(kk, 0) * p.kv_stride_tok + lane * EPL, v);
+        for (int jj = 0; jj < 32; ++jj) {
+          const int kk = __shfl_sync(0xffffffffu, key, jj);
+          float v[EPL];
+          load_slice<KT, EPL>(Vg + (long long)max(kk, 0) * p.kv_stride_tok + lane * EPL, v);
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) v[e] = kk >= 0 ? v[e] : 0.f;
+          for (int e = 0; e < EPL; ++e) v[e] = kk >= 0 ? v[e] : 0.f;
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          const float pk = __shfl_sync(0xffffffffu, pj[i], jj);
+          for (int i = 0; i < R; ++i) {
+            const float pk = __shfl_sync(0xffffffffu, pj[i], jj);
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) o[i][e] = fmaf(pk, v[e], o[i][e]);
+            for (int e = 0; e < EPL; ++e) o[i][e] = fmaf(pk, v[e], o[i][e]);
+          }
         }
       }
     }
@@ -258,6 +306,11 @@ __global__ void __launch_bounds__(simt_warps(D) * 32) attn_simt_kernel(const Sim
       step(key);
     }
     span(p.M, p.L);
+  }
+  if constexpr (CODES) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) l[i] = warp_sum(l[i]);
+    __syncwarp();                                      // the last numerators have been read from part_o
   }
   // merge of the warps' partials, warps in index order
 #pragma unroll
