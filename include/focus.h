@@ -25,7 +25,8 @@
  *     these kernels may have written (outputs, lists, workspace).  A kernel of another library placed after a call
  *     sees complete results.  Ahead of that wait these kernels read only inputs that none of them writes:
  *     focus_sparse_layer reads Q, the focus and sink index lists, the pooled keys and the sinks' K/V rows there,
- *     its attention kernel the row list and Q; focus_dense_attn and focus_sparse_attn read nothing ahead of it.
+ *     its attention kernel the row list and Q; focus_dense_attn, focus_sparse_attn and their _quantized forms read
+ *     nothing ahead of it.
  *     Such an input is complete if its producer finished before the call's predecessor in the stream started, or if
  *     the producer is a kernel of this library (those make their outputs visible before they exit).  An input
  *     written by a foreign kernel that runs immediately before a focus_sparse_layer call, with nothing in between
@@ -127,7 +128,8 @@ uint64_t focus_launch_count(void);
  * used: 1 = generic SIMT, 2 = tensor-core kernel with one 128-row query tile per CTA, 3 = tensor-core kernel with
  * two query tiles per CTA (taken for >= 256 stacked rows per KV head and >= 24 key tiles per CTA), 4 = tensor-core
  * kernel with one query tile and two softmax warpgroups on alternating key tiles (>= 128 stacked rows per KV head
- * and >= 4 key tiles per CTA, where 3 does not apply); 0 = none yet. */
+ * and >= 4 key tiles per CTA, where 3 does not apply), 5 = the tensor-core kernel for 8-bit caches (the two
+ * _quantized calls on bf16 queries); 0 = none yet. */
 int32_t focus_last_attn_variant(focus_ctx* ctx);
 
 /* Selects the attention implementation for bf16 inputs (head_dim 128 or 64): 0 = automatic (tensor-core
@@ -297,7 +299,8 @@ focus_status focus_dense_attn(focus_ctx* ctx, const focus_shape* shape, const vo
  * are applied to the logits and to the softmax numerators in fp32, so nothing is rounded between the cache and the
  * products.  A row with no key to attend (empty lists, no sinks, M == L) gives O = 0 and lse = -inf.  Errors as
  * there; INVALID_ARG also for an unknown format or a misaligned cache.
- * The codes of every attended token and the scales must be finite. */
+ * The codes of every attended token must be finite, its scales finite and non-negative; a V scale below 2^-87, where
+ * focus_quantize_kv writes none but 0, may count as 2^-87.  fp32 shapes run on the SIMT kernel. */
 focus_status focus_sparse_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q, int32_t q_base,
                                          int32_t n_q, const int32_t* q_rows, const int32_t* n_rows, int32_t max_rows,
                                          const focus_quant_cache* cache, int32_t head_reduce,
@@ -329,8 +332,9 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
  *   kept set  the tokens in descending order of x (ties: lower v), cut to the first top_k (0: no cut), to the
  *             shortest prefix that holds at least top_p of the weight left by top_k (1: no cut), and to those with
  *             w_v >= min_p (0: no cut); at least one token stays
- *   token     the first kept v, in ascending v, whose running sum of kept weights exceeds u * their total; weights
- *             and sums are held in 64 bits, so that the token is the one the definition names
+ *   token     the first kept v, in ascending v, whose running sum of kept weights exceeds u * their total.  Sums are
+ *             held in 64 bits and a weight is off by less than 1e-9 of itself, so the token (and the kept set) is
+ *             the one the definition names unless two sums that it compares are that close
  *   conf      w_token / total: its probability in the distribution it was drawn from
  *   prob      (may be NULL) softmax_v(x)[token] at temperature 1 over the whole vocabulary: Eq. 2's confidence
  *   n_kept    (may be NULL) int32, size of the kept set

@@ -610,3 +610,163 @@ def test_a_sparse_layer_over_an_8bit_cache(ctx, fmt):
     Kn.copy_(bf(n, Hkv, d)), Vn.copy_(bf(n, Hkv, d)), Q.copy_(bf(L - M, H, d))
     graph.replay()
     check()
+
+
+# ---- limits ---------------------------------------------------------------------------------------------------------
+def _random_cache(rng, fmt, Hkv, L, d):
+    """Codes and scales straight from the generator: (code values, scales, device codes, device scales)."""
+    if fmt == "int8":
+        vals = rng.integers(-127, 128, size=(Hkv, L, d)).astype(np.float64)
+    else:
+        bits = rng.integers(0, 256, size=(Hkv, L, d)).astype(np.uint8)
+        bits[(bits & 0x7f) >= 0x78] = 0x31                                  # no NaN, none above 240
+        vals = torch.from_numpy(bits).view(torch.float8_e4m3fn).float().double().numpy()
+    top = 127.0 if fmt == "int8" else 240.0
+    sc = (np.exp(0.5 * rng.standard_normal((Hkv, L))) / top * 1.7).astype(np.float32)
+    return vals, sc.astype(np.float64), codes_to_device(vals, fmt), torch.from_numpy(sc).cuda()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("L,M,keep,sinks", [(41001, 0, 0, 0), (36000, 35900, 300, 1500), (9000, 8800, 0, 2000)])
+def test_long_key_sets(ctx, fmt, L, M, keep, sinks):
+    """One KV head: more than 256 key tiles (those of a split that are staged at once), as many splits as there can be, more
+    than eight tiles of sinks.  M == 0: dense."""
+    rng = np.random.default_rng(L + sinks)
+    H, Hkv, d, B, N, n = 2, 1, 64, 64, 40, 33
+    Q = storage(rng.standard_normal((N, H, d)), "bf16")
+    kv, ks, dk, dks = _random_cache(rng, fmt, Hkv, L, d)
+    vv, vs, dv, dvs = _random_cache(rng, fmt, Hkv, L, d)
+    K, V = kv * ks[..., None], vv * vs[..., None]
+    pos = np.sort(rng.choice(N, size=n, replace=False)) + L - N
+    pos[3] = pos[2]                                                          # a position may be listed twice
+    rows, n_rows = torch.from_numpy(pos.astype(np.int32)).cuda(), torch.tensor([n], dtype=torch.int32, device="cuda")
+    dQ, O = fstep.to_device(Q, "bf16"), torch.full((n, H, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((H, n), 9.0, device="cuda")
+    cache = fb.make_quant_cache(FMT[fmt], dk, dv, dks, dvs)
+    Qf, scale = wl.storage_to_f64(Q, "bf16")[pos - (L - N)], 1.0 / math.sqrt(d)
+    if M == 0:
+        fb.focus_dense_attn_quantized(ctx, fb.make_shape(L, L, H, Hkv, d, B, fb.BF16), dQ, L - N, N, rows, n_rows, n, cache, O, lse)
+        eO, eL = fo.dense_attn(Qf, K, V, scale)
+        keys = None
+    else:
+        blocks = [np.sort(rng.choice((M + B - 1) // B, size=keep, replace=False))]
+        sink = np.sort(rng.choice(M, size=sinks, replace=False))
+        sk = np.array([[0 if (s // B) in set(blocks[0]) else 1 for s in sink]], dtype=np.uint8)
+        dev = [torch.from_numpy(a).cuda() for a in (np.concatenate([blocks[0], [-1]]).astype(np.int32)[None],
+                                                    np.array([keep], dtype=np.int32), sink.astype(np.int32), sk)]
+        fb.focus_sparse_attn_quantized(ctx, fb.make_shape(L, M, H, Hkv, d, B, fb.BF16), dQ, L - N, N, rows, n_rows, n, cache,
+                                       fb.HEADS_PER_KV_GROUP, dev[0], keep + 1, dev[1], dev[2], dev[3], sinks, O, lse)
+        eO, eL = fo.sparse_attn(Qf, K, V, M, B, blocks, sink, scale)
+        keys = [fo.key_set(M, L, B, blocks[0], sink)]
+    assert ctx.last_attn_variant() == 5
+    tO, tL = _bounds(Qf, K, V, vs, eO, scale, H // Hkv, "bf16", keys)
+    assert (np.abs(fstep.from_device(O) - eO) <= tO).all() and (np.abs(fstep.from_device(lse) - eL) <= tL).all()
+    assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("simt", [False, True])
+def test_offsets_beyond_32_bits(ctx, simt):
+    """Tokens a MiB apart, K and V interleaved in one buffer of more than 2^32 bytes: written, read back, attended."""
+    L, H, d, step = 4200, 2, 64, 1 << 20
+    buf = torch.empty(L * step, dtype=torch.int8, device="cuda")
+    K, V = (buf[o:].as_strided((H, L, d), (256, step, 1)) for o in (0, 128))
+    sc = torch.zeros(2, H, L, device="cuda")
+    cache = fb.make_quant_cache(fb.KV_INT8, buf, buf[128:], sc[0], sc[1])
+    sh = fb.make_shape(L, L, H, H, d, 64, fb.BF16, kv_stride_tok=step, kv_stride_head=256)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(2, L, H, d, generator=g, device="cuda").bfloat16()
+    fb.focus_quantize_kv(ctx, sh, x[0], x[1], H * d, d, 0, None, None, L, cache)
+    top = x.float().abs().amax(-1).cpu().numpy() / np.float32(127)            # IEEE division (the device's by a constant is not)
+    assert np.array_equal(sc.cpu().numpy(), top.swapaxes(1, 2)) and bool((K.abs().amax(-1) == 127).all())
+    out = torch.empty(2, H, L, d, dtype=torch.bfloat16, device="cuda")
+    fb.focus_dequantize_kv(ctx, sh, cache, 0, None, None, L, out[0], out[1], d, L * d)
+    for got, codes, s in ((out[0], K, sc[0]), (out[1], V, sc[1])):
+        assert torch.equal(got, (codes.float() * s[..., None]).bfloat16())
+    Q = torch.randn(9, H, d, generator=g, device="cuda").bfloat16()
+    O = torch.empty(9, H, d, dtype=torch.bfloat16, device="cuda")
+    ctx.set_force_simt(simt)
+    try:
+        fb.focus_dense_attn_quantized(ctx, sh, Q, L - 9, 9, None, None, 0, cache, O, None)
+    finally:
+        ctx.set_force_simt(False)
+    Kd, Vd = ((c.double() * s[..., None].double()).cpu().numpy() for c, s in ((K, sc[0]), (V, sc[1])))
+    Qf = Q.double().cpu().numpy()
+    eO, _ = fo.dense_attn(Qf, Kd, Vd, 1.0 / math.sqrt(d))
+    tO, _ = _bounds(Qf, Kd, Vd, sc[1].double().cpu().numpy(), eO, 1.0 / math.sqrt(d), 1, "bf16")
+    assert (np.abs(fstep.from_device(O) - eO) <= tO).all()
+    assert ctx.poll_status() == 0
+
+
+@gpu
+def test_two_graphs_on_one_context_and_another_stream(ctx):
+    """Two captured sequences (write, dense, sparse) that share the context's workspace, replayed in turn on a stream other
+    than the current one, against the eager calls."""
+    L, M, H, Hkv, d, N, rows = 6000, 5900, 8, 4, 128, 100, 40
+    g = torch.Generator(device="cuda").manual_seed(11)
+    sets = []
+    for fmt in (fb.KV_INT8, fb.KV_E4M3):
+        s = dict(x=torch.randn(2, L, Hkv, d, generator=g, device="cuda").bfloat16(),
+                 Q=torch.randn(N, H, d, generator=g, device="cuda").bfloat16(),
+                 pos=torch.arange(L - N, L - N + rows, dtype=torch.int32, device="cuda"),
+                 n=torch.tensor([rows], dtype=torch.int32, device="cuda"), codes=torch.zeros(2, Hkv, L, d, dtype=torch.int8, device="cuda"),
+                 sc=torch.zeros(2, Hkv, L, device="cuda"), idx=torch.tensor([[0, 3, 17, 40, -1]] * Hkv, dtype=torch.int32, device="cuda"),
+                 cnt=torch.full((Hkv,), 4, dtype=torch.int32, device="cuda"),
+                 sink=torch.tensor([130, 700, 5899], dtype=torch.int32, device="cuda"),
+                 keep=torch.ones(Hkv, 3, dtype=torch.uint8, device="cuda"),
+                 O=torch.zeros(2, rows, H, d, dtype=torch.bfloat16, device="cuda"), lse=torch.zeros(2, H, rows, device="cuda"))
+        s["cache"] = fb.make_quant_cache(fmt, s["codes"][0], s["codes"][1], s["sc"][0], s["sc"][1])
+        sets.append(s)
+    sh = fb.make_shape(L, M, H, Hkv, d, 128, fb.BF16)
+
+    def run(s, stream):
+        fb.focus_quantize_kv(ctx, sh, s["x"][0], s["x"][1], Hkv * d, d, 0, None, None, L, s["cache"], stream=stream)
+        fb.focus_dense_attn_quantized(ctx, sh, s["Q"], L - N, N, s["pos"], s["n"], rows, s["cache"], s["O"][0], s["lse"][0], stream=stream)
+        fb.focus_sparse_attn_quantized(ctx, sh, s["Q"], L - N, N, s["pos"], s["n"], rows, s["cache"], fb.HEADS_PER_KV_GROUP, s["idx"], 5,
+                                       s["cnt"], s["sink"], s["keep"], 3, s["O"][1], s["lse"][1], stream=stream)
+
+    want = []
+    for s in sets:
+        run(s, None)
+        want.append([s[k].clone() for k in ("codes", "sc", "O", "lse")])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graphs = []
+    for s in sets:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=side):
+            run(s, side)
+        graphs.append(gr)
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            for s, gr in zip(sets, graphs):
+                for k in ("codes", "sc", "O", "lse"):
+                    s[k].zero_()
+                gr.replay()
+            side.synchronize()
+            for s, w in zip(sets, want):
+                assert all(torch.equal(s[k], t) for k, t in zip(("codes", "sc", "O", "lse"), w))
+    run(sets[0], side)                                                       # a stream that is not the current one
+    side.synchronize()
+    assert torch.equal(sets[0]["O"], want[0][2])
+    assert ctx.poll_status() == 0
+
+
+@gpu
+def test_workspace_of_quantized_attention():
+    """A workspace that is too small is reported; one of the advertised size carries the calls."""
+    L, M, H, d, N = 20000, 19900, 4, 128, 64
+    sh = fb.make_shape(L, M, H, H, d, 128, fb.BF16)
+    codes, sc = torch.ones(H, L, d, dtype=torch.int8, device="cuda"), torch.ones(H, L, device="cuda")
+    cache = fb.make_quant_cache(fb.KV_INT8, codes, codes, sc, sc)
+    Q, O = torch.randn(N, H, d, device="cuda").bfloat16(), torch.zeros(N, H, d, dtype=torch.bfloat16, device="cuda")
+    tiny = fb.Context(0, workspace_bytes=4096)
+    with pytest.raises(fb.FocusError) as e:
+        fb.focus_dense_attn_quantized(tiny, sh, Q, L - N, N, None, None, 0, cache, O, None)
+    assert e.value.code == fb.ERR_WORKSPACE_TOO_SMALL and bool((O == 0).all())
+    tiny.close()
+    c = fb.Context(0, workspace_bytes=fb.focus_workspace_bytes(sh, N, 8, 4))
+    fb.focus_dense_attn_quantized(c, sh, Q, L - N, N, None, None, 0, cache, O, None)
+    assert bool((O == 1).all()) and c.poll_status() == 0                     # every value is 1
+    c.close()

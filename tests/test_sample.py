@@ -270,3 +270,42 @@ def test_a_sampled_step_captured_and_replayed(ctx):
     for _ in range(2):
         fill(), graph.replay(), check_state()
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("n", [3, 160])
+def test_rows_beyond_32_bits(ctx, n):
+    """Logits rows more than 2^32 bytes apart in all (in slices and in place)."""
+    V, stride = 40000, (1 << 32) // 2 // 150 // 8 * 8
+    buf = torch.empty(n * stride if n > 3 else 160 * stride, dtype=torch.bfloat16, device="cuda")
+    pos = list(range(n)) if n > 3 else [0, 100, 159]
+    n_pos = 160
+    rows = buf.as_strided((n_pos, V), (stride, 1))
+    rows.copy_(torch.randn(n_pos, V, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") * 3)
+    dr, dn = torch.tensor(pos, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    u = torch.linspace(0.01, 0.99, n, device="cuda")
+    conf, tok = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    for k, p in ((40, 0.9), (0, 0.95), (0, 1.0)):
+        fb.focus_sample(ctx, buf, fb.BF16, stride, V, 0, n_pos, dr, dn, n, 0.8, k, p, 0.0, u, conf, tok, None, None)
+        for r in (0, n // 2, n - 1):
+            et, ec, _, _ = fo.sample_token(rows[pos[r]].double().cpu().numpy(), single(0.8), k, single(p), 0.0, float(u[r]))
+            assert int(tok[r]) == et and abs(float(conf[r]) - ec) <= CONF_TOL * ec
+    assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("scale,T", [(1e4, 1.0), (1e-3, 1e-4), (3e5, 40.0), (1.0, 1e-3), (1e-30, 1e-30)])
+def test_logits_of_any_size(ctx, scale, T):
+    """Exponents x / T far beyond 4096 (where the difference to the maximum is taken first), and tiny or huge temperatures;
+    the logits spread over a few T, so that the cuts have work to do."""
+    rng = np.random.default_rng(3)
+    V = 6001
+    x = (scale + rng.standard_normal((8, 6004)) * T * 2.0).astype(np.float32)
+    u = rng.random(8)
+    for k, p, mp in ((0, 1.0, 0.0), (0, 0.9, 0.0), (30, 0.8, 0.0), (0, 1.0, 0.01)):
+        out = run(ctx, x, "f32", V, 0, None, 8, T, k, p, mp, u)
+        tok, conf, _, kept = out
+        for r in range(8):
+            et, ec, _, en = fo.sample_token(x[r, :V].astype(np.float64), single(T), k, single(p), single(mp), single(u[r]))
+            assert (int(tok[r]), int(kept[r])) == (et, en) and abs(float(conf[r]) - ec) <= CONF_TOL * ec
+    assert ctx.poll_status() == 0
