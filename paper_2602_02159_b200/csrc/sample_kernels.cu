@@ -1041,7 +1041,98 @@ sample_kernel(const SampleParams p) {
     int none = 0;
     sum_all<3>(cl, sh, turn, s, none);
   };
-  if (narrowed) {
+  // every warp's segment of the slice
+  constexpr int SEG_UNIT = 32 * EPC;
+  const int seg = (p.slice + SP_WARPS * SEG_UNIT - 1) / (SP_WARPS * SEG_UNIT) * SEG_UNIT;
+  const int s0 = min(warp * seg, n_vec * EPC), s1 = min(s0 + seg, n_vec * EPC);   // whole vectors; the padding is -inf
+  bool summed = false;                                   // the segments' kept weights are known
+  if (narrowed && p.min_p == 0.f) {
+    // One pass: per segment the weight before the open bins, and their tokens as a list of the warp's own (in a fixed order).
+    // They are a few percent of the nucleus; where they fit, the rest is done on them.
+    const int cap = (SP_LIST * 8 + p.slice / EPC) / (SP_WARPS * 4);    // over the list and the bytes per vector behind it
+    float* open_list = reinterpret_cast<float*>(list) + warp * cap;
+    double s4[4] = {0.0, 0.0, 0.0, 0.0}, base[1];
+    int ngt = 0, n_open = 0;
+#pragma unroll 1
+    for (int i0 = s0 / EPC; i0 < s1 / EPC; i0 += 32) {
+      const int i = i0 + lane;
+      uint32_t open = 0;
+      if (i < s1 / EPC) {
+        float x[EPC];
+        unpack_logits<T>(vec(i), x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          const Reduced a = reduced(x[e]);
+          const int b = top_bits - a.bits;
+          s4[e & 3] += b < bin_lo ? pow2_reduced(a, tab) : 0.0;
+          ngt += b < bin_lo ? 1 : 0;
+          open |= b >= bin_lo && b <= bin_hi && x[e] > -INFINITY ? 1u << e : 0u;
+        }
+      }
+      if (__any_sync(0xffffffffu, open != 0u)) {
+        int at = __popc(open);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, at, o);
+          if (lane >= o) at += y;
+        }
+        const int more = __shfl_sync(0xffffffffu, at, 31);
+        at += n_open - __popc(open);
+        for (; open; open &= open - 1u, ++at) {
+          if (at < cap) open_list[at] = logit(i * EPC + __ffs(open) - 1);
+        }
+        n_open += more;
+      }
+    }
+    __syncwarp();
+    const double mine = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    base[0] = mine;
+    int too_many = lane == 0 && n_open > cap ? 1 : 0;
+    sum_all<1>(cl, sh, turn, base, too_many);
+    if (too_many == 0) {
+      const double target = (double)p.top_p * z_all;
+      uint32_t k_hi = min(key_of(bin_edge((double)bin_lo - 1.0)), key_of(m));
+      uint32_t k_lo = bin_hi == INT_MAX ? BOTTOM : max(key_of(bin_edge((double)bin_hi + 1.0)), BOTTOM);
+      base[0] *= unit;
+      double above = base[0];
+      int none = 0;
+      while (k_lo < k_hi) {
+        uint32_t t[3];
+        quarter(k_lo, k_hi, t);
+        double s3[3] = {0.0, 0.0, 0.0};
+#pragma unroll 1
+        for (int i = lane; i < n_open; i += 32) {
+          const uint32_t k = key_of(open_list[i]);
+          const double w = weight_plain(open_list[i]) * unit;
+          s3[0] += k >= t[0] ? w : 0.0;
+          s3[1] += k >= t[1] ? w : 0.0;
+          s3[2] += k >= t[2] ? w : 0.0;
+        }
+        sum_all<3>(cl, sh, turn, s3, none);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) s3[q] += base[0];
+        const bool reached[3] = {s3[0] >= target, s3[1] >= target, s3[2] >= target};
+        go_on(k_lo, k_hi, above, t, reached, s3);
+      }
+      T_key = k_lo;
+      quota = (int)fmin(fmax(ceil((target - above) / weight(key_value(T_key))), 1.0), (double)INT_MAX);
+      double w_seg = mine * unit;
+      int neq = 0;
+#pragma unroll 1
+      for (int i = lane; i < n_open; i += 32) {
+        const uint32_t k = key_of(open_list[i]);
+        if (k > T_key) { w_seg += weight_plain(open_list[i]) * unit; ++ngt; }
+        neq += k == T_key ? 1 : 0;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) w_seg += __shfl_xor_sync(0xffffffffu, w_seg, o);
+      ngt = __reduce_add_sync(0xffffffffu, ngt);
+      neq = __reduce_add_sync(0xffffffffu, neq);
+      if (lane == 0) { sh.seg[warp].w = w_seg; sh.seg[warp].n_gt = ngt; sh.seg[warp].n_eq = neq; }
+      summed = true;
+    }
+  }
+  if (narrowed && !summed) {
     // the weight before the open bins, and the keys in them; then their bits
     double base[1];
     uint32_t k_hi = 0u, k_lo = 0xFFFFFFFFu;
@@ -1101,7 +1192,7 @@ sample_kernel(const SampleParams p) {
     const uint32_t best = k_lo;
     T_key = best;
     quota = (int)fmin(fmax(ceil((target - above) / weight(key_value(best))), 1.0), (double)INT_MAX);
-  } else if (cut_p) {
+  } else if (cut_p && !summed) {
     double s3[3];
     const double w_at = quota ? weight(key_value(T_key)) : 0.0;
     weights_from(T_key + 1, T_key + 1, T_key + 1, s3);
@@ -1128,10 +1219,7 @@ sample_kernel(const SampleParams p) {
   const double min_w = (double)p.min_p;
   const double w_T = quota ? weight(key_value(T_key)) : 0.0;
   const bool tie_in = quota > 0 && w_T >= min_w;
-  constexpr int SEG_UNIT = 32 * EPC;
-  const int seg = (p.slice + SP_WARPS * SEG_UNIT - 1) / (SP_WARPS * SEG_UNIT) * SEG_UNIT;
-  const int s0 = min(warp * seg, n_vec * EPC), s1 = min(s0 + seg, n_vec * EPC);   // whole vectors; the padding is -inf
-  {
+  if (!summed) {
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     int ngt = 0, neq = 0;
     if (T_key == BOTTOM && min_w == 0.0 && plain) {      // no cut at all: every candidate, without a branch
