@@ -770,3 +770,37 @@ def test_workspace_of_quantized_attention():
     fb.focus_dense_attn_quantized(c, sh, Q, L - N, N, None, None, 0, cache, O, None)
     assert bool((O == 1).all()) and c.poll_status() == 0                     # every value is 1
     c.close()
+
+
+@gpu
+def test_the_readmes_second_example_runs_as_printed(ctx):
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = re.findall(r"```python\n(.*?)```", text, flags=re.S)[1]
+    L, M, H, Hkv, d, B, k, C, n_sink, vocab = 2000, 1700, 8, 4, 128, 128, 4, 3, 5, 1000
+    g = torch.Generator(device="cuda").manual_seed(2)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").bfloat16()
+
+    i32 = dict(dtype=torch.int32, device="cuda")
+    env = dict(fb=fb, ctx=ctx, L=L, M=M, H=H, Hkv=Hkv, d=d, k=k, C=C, n_sink=n_sink, vocab=vocab,
+               shape=fb.make_shape(L, M, H, Hkv, d, B, fb.BF16), codes=torch.zeros(2, Hkv, L, d, dtype=torch.uint8, device="cuda"),
+               scales=torch.zeros(2, Hkv, L, device="cuda"), K_rows=randn(L, Hkv, d), V_rows=randn(L, Hkv, d), K_new=randn(k * 9, Hkv, d),
+               V_new=randn(k * 9, Hkv, d), active=torch.arange(M + 3, M + 3 + k * 9, **i32), n_active=torch.tensor([30], **i32),
+               Q=randn(L - M, H, d), O=randn(k * 9, H, d), lse=torch.zeros(H, k * 9, device="cuda"),
+               blocks=torch.tensor([0, 4, 9] * Hkv, **i32), cnt=torch.full((Hkv,), C, **i32), sinks=torch.tensor([1, 2, 3, 600, 1699], **i32),
+               keep=torch.ones(Hkv * n_sink, dtype=torch.uint8, device="cuda"), logits=randn(L - M, vocab), u=torch.rand(k * 9, device="cuda"),
+               conf=torch.zeros(k * 9, device="cuda"), token=torch.zeros(k * 9, **i32), prob=torch.zeros(k * 9, device="cuda"),
+               K=torch.zeros(Hkv, L, d, dtype=torch.bfloat16, device="cuda"))
+    exec(code, env)
+    assert ctx.poll_status() == 0
+    rows = env["K_rows"].clone()
+    rows[M + 3:M + 33] = env["K_new"][:30]
+    err = (env["K"].transpose(0, 1).float() - rows.float()).abs()
+    # e4m3: half a step of 2^-3 (2^-4 of the element), or half of the smallest step, 2^-9 scales (scale = max / 448); bf16
+    # adds 2^-8 and the scale's own rounding 2^-23
+    top = rows.float().abs().amax(-1, keepdim=True)
+    assert bool((err <= (2.0 ** -4 + 2.0 ** -7) * rows.float().abs() + 2.0 ** -10 * top / 448).all())
+    assert torch.isfinite(env["O"][:30].float()).all() and bool((env["token"][:30] >= 0).all()) and bool((env["token"][30:] == -1).all())
