@@ -1045,8 +1045,13 @@ sample_kernel(const SampleParams p) {
   constexpr int SEG_UNIT = 32 * EPC;
   const int seg = (p.slice + SP_WARPS * SEG_UNIT - 1) / (SP_WARPS * SEG_UNIT) * SEG_UNIT;
   const int s0 = min(warp * seg, n_vec * EPC), s1 = min(s0 + seg, n_vec * EPC);   // whole vectors; the padding is -inf
+  // A token of bin b weighs 2^-((b -+ 1) / 64).  min_below: min-p ends the set before the nucleus can end, which is then of
+  // no interest; min_above: it has no say among the tokens up to bin_hi.
+  const float margin = 1e-4f * p.min_p;
+  const bool min_below = narrowed && exp2f((1.f - (float)bin_lo) * (1.f / SP_TAB)) <= p.min_p - margin;
+  const bool min_above = p.min_p == 0.f || (bin_hi != INT_MAX && exp2f(-((float)bin_hi + 1.f) * (1.f / SP_TAB)) >= p.min_p + margin);
   bool summed = false;                                   // the segments' kept weights are known
-  if (narrowed && p.min_p == 0.f) {
+  if (narrowed && min_above) {
     // One pass: per segment the weight before the open bins, and their tokens as a list of the warp's own (in a fixed order).
     // They are a few percent of the nucleus; where they fit, the rest is done on them.
     const int cap = (SP_LIST * 8 + p.slice / EPC) / (SP_WARPS * 4);    // over the list and the bytes per vector behind it
@@ -1132,7 +1137,9 @@ sample_kernel(const SampleParams p) {
       summed = true;
     }
   }
-  if (narrowed && !summed) {
+  if (summed || min_below) {
+    // no search left
+  } else if (narrowed) {
     // the weight before the open bins, and the keys in them; then their bits
     double base[1];
     uint32_t k_hi = 0u, k_lo = 0xFFFFFFFFu;
@@ -1192,7 +1199,7 @@ sample_kernel(const SampleParams p) {
     const uint32_t best = k_lo;
     T_key = best;
     quota = (int)fmin(fmax(ceil((target - above) / weight(key_value(best))), 1.0), (double)INT_MAX);
-  } else if (cut_p && !summed) {
+  } else if (cut_p) {
     double s3[3];
     const double w_at = quota ? weight(key_value(T_key)) : 0.0;
     weights_from(T_key + 1, T_key + 1, T_key + 1, s3);
@@ -1236,14 +1243,16 @@ sample_kernel(const SampleParams p) {
       for (int e = 0; e < 4; ++e) s[e] *= unit;
     } else {
       const float t = key_value(T_key), t_all = T_key == BOTTOM ? -INFINITY : t;
+      // no lighter logit passes min-p (the millionth is for the logarithm's own rounding)
+      const float x_min = plain && min_w > 0.0 ? (float)(md + (log2(min_w) - 1e-6) / scale) : -INFINITY, x_look = fmaxf(t_all, x_min);
       for (int i = s0 / EPC + lane; i < s1 / EPC; i += 32) {
         const uint4 raw = vec(i);
-        if (!(largest_of<T>(raw) >= t_all)) continue;
+        if (!(largest_of<T>(raw) >= x_look)) continue;
         float x[EPC];
         unpack_logits<T>(raw, x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          if (x[e] > t_all) {
+          if (x[e] > t_all && x[e] >= x_min) {
             double w;
             bool in;
             if (plain) {                                 // the exact weight only where min-p depends on its last bits

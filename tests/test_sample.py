@@ -309,3 +309,17 @@ def test_logits_of_any_size(ctx, scale, T):
             et, ec, _, en = fo.sample_token(x[r, :V].astype(np.float64), single(T), k, single(p), single(mp), single(u[r]))
             assert (int(tok[r]), int(kept[r])) == (et, en) and abs(float(conf[r]) - ec) <= CONF_TOL * ec
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("min_p", [0.002, 0.02, 0.2, 0.55, 1.0])
+@pytest.mark.parametrize("dtype,spread,top_p", [("bf16", 0.5, 0.7), ("f32", 0.5, 0.3), ("f32", 0.5, 0.999), ("bf16", 3.0, 0.95)])
+def test_min_p_before_within_and_behind_a_long_nucleus(ctx, dtype, spread, top_p, min_p):
+    """min-p that ends the set before a nucleus of thousands of tokens, that cuts near its end, and that has no say."""
+    rng = np.random.default_rng(int(1000 * min_p))
+    V = 32003
+    xs = wl.to_storage((rng.standard_normal((6, 32008)) * spread).astype(np.float32), dtype)
+    u = rng.random(6)
+    out = run(ctx, xs, dtype, V, 0, None, 6, 0.9, 0, top_p, min_p, u)
+    check(out, wl.storage_to_f64(xs, dtype)[:, :V], range(6), 0.9, 0, top_p, min_p, u)
+    assert ctx.poll_status() == 0
