@@ -880,7 +880,7 @@ sample_kernel(const SampleParams p) {
       }
       if (kth > BOTTOM) from = fmaxf(key_value(kth), -FLT_MAX);
     }
-    if (short_nucleus) from = bin_edge((double)bin_hi + 1.0);            // its lower edge, and half a bin
+    if (short_nucleus) from = bin_edge((double)bin_hi + 0.501);            // its lower edge
     double raw_sum[1] = {raw_mine};
     // which logits reach the bound: a byte of bits per vector, then their places by a scan: the list is in index order.
     // Only the shares whose maximum reaches it are looked at, and those by all threads.
@@ -955,7 +955,7 @@ sample_kernel(const SampleParams p) {
         d.top_k = cut_k ? p.top_k : 0; d.top_p = (double)p.top_p; d.z = z_all; d.min_p = (double)p.min_p; d.u = (double)u;
         d.key_lo = from == -FLT_MAX ? BOTTOM : key_of(from);
         d.key_top = key_of(m);
-        if (short_nucleus) d.key_top = min(key_of(bin_edge((double)bin_lo - 1.0)), d.key_top);
+        if (short_nucleus) d.key_top = min(key_of(bin_edge((double)bin_lo - 0.501)), d.key_top);
         d.complete = n_list == n_cand;
         int at_tok = -1, kept = 0;
         double w_tok = 0.0, total = 1.0;
@@ -1096,8 +1096,8 @@ sample_kernel(const SampleParams p) {
     sum_all<1>(cl, sh, turn, base, too_many);
     if (too_many == 0) {
       const double target = (double)p.top_p * z_all;
-      uint32_t k_hi = min(key_of(bin_edge((double)bin_lo - 1.0)), key_of(m));
-      uint32_t k_lo = bin_hi == INT_MAX ? BOTTOM : max(key_of(bin_edge((double)bin_hi + 1.0)), BOTTOM);
+      uint32_t k_hi = min(key_of(bin_edge((double)bin_lo - 0.501)), key_of(m));
+      uint32_t k_lo = bin_hi == INT_MAX ? BOTTOM : max(key_of(bin_edge((double)bin_hi + 0.501)), BOTTOM);
       base[0] *= unit;
       double above = base[0];
       int none = 0;
