@@ -1015,8 +1015,7 @@ focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_
   return i8 ? launch<int8_t, 64>(ctx, set[2], tmK, tmV, p, grid, st) : launch<__nv_fp8_e4m3, 64>(ctx, set[3], tmK, tmV, p, grid, st);
 }
 
-size_t attn_quant_tc_workspace(const focus_shape* s, int n_q) {
+size_t attn_quant_tc_workspace(const focus_shape* s) {
   // partial outputs of every split: no more CTAs than SMs take part in a split launch (160 bounds the part at hand)
-  (void)n_q;
   return (size_t)160 * QN * ((size_t)s->head_dim + 2) * 4 + 1024;
 }

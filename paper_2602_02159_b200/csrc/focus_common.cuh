@@ -287,4 +287,4 @@ size_t attn_tc_workspace(const focus_shape* s, int n_q, int max_blocks, int n_si
 // the same over an 8-bit cache (a.qc non-NULL)
 focus_status launch_attn_quant_tc(focus_ctx* ctx, const AttnArgs& a, cudaStream_t st);
 bool attn_quant_tc_supported(const focus_ctx* ctx, const AttnArgs& a);
-size_t attn_quant_tc_workspace(const focus_shape* s, int n_q);
+size_t attn_quant_tc_workspace(const focus_shape* s);

@@ -68,7 +68,6 @@ struct SampleShared {
   alignas(16) int hist[2][256];
   int scan_i[33];
   unsigned long long fx[2][SP_WARPS][3];
-  int last[SP_WARPS];
   int digit, above, found;
   uint4 tail;              // the vector that the row ends in
   uint32_t key_hi[SP_WARPS], key_lo[SP_WARPS];
