@@ -7,17 +7,17 @@
 // row's two divisions are shared by more elements), so every access covers full sectors and the maximum is a butterfly
 // over those lanes.  Rows of one KV head are neighbours in the grid: their codes and scales are neighbours in the cache.
 // A thread has one row in flight where there are few (latency counts), else two (writing) or four (reading back):
-// 32768 keys of 32 heads of 128 read back into bf16 in 67 us with four (6.1 TB/s), 139 us with one.  Writing is held by
+// 32768 keys of 32 heads of 128 read back into bf16 in 66 us with four (6.2 TB/s), 139 us with one.  Writing is held by
 // its instructions before HBM: 16384 positions of 4 heads of 128, keys and values from bf16 to e4m3, take 14.4 us
 // (3.5 TB/s; the fixed cost of a launch is about 3), against 25 to 33 us with a library division and conversion per
-// element.
+// element; blocks of 128 threads, because the fence at a block's end then holds up fewer of them (int8 16.2 -> 14.7 us).
 #include <float.h>
 
 #include "focus_common.cuh"
 
 namespace {
 
-constexpr int QK_THREADS = 256;
+constexpr int QK_THREADS = 128;
 constexpr int QK_VECS = 2;                              // sixteen-byte vectors per lane when writing
 constexpr float FLUSH_BELOW = 8.271806125530277e-25f;   // 2^-80: rows smaller than this are stored as zeros
 
