@@ -397,7 +397,7 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
   int turn = 0;
   uint32_t key[SP_PER];
   unsigned long long fx[SP_PER];
-  unsigned in = 0;                                       // bit q: token q is in
+  unsigned in = 0, light = 0;                            // bit q: token q is in / has a weight, but less than half of 2^-50
 #pragma unroll
   for (int q = 0; q < SP_PER; ++q) {
     const int i = tid * SP_PER + q;
@@ -407,7 +407,7 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
     if (i < n) {
       const double w = weight(key_to_float(full));
       fx[q] = (unsigned long long)__double2ll_rn(w * FX_ONE);
-      if (w > 0.0 && fx[q] == 0ull) fx[q] = 1ull;        // u = 0 draws the first token that has a weight, however small
+      light |= w > 0.0 && fx[q] == 0ull ? 1u << q : 0u;
       in |= 1u << q;
     }
   }
@@ -475,7 +475,10 @@ __device__ __forceinline__ bool draw_from_list(SampleShared& sh, const unsigned 
       if (in >> q & 1u)
         if (!(weight(key_to_float((uint32_t)(list[tid * SP_PER + q] >> 32))) >= d.min_p)) in &= ~(1u << q);
   }
-  // running sums of the kept weights in index order; the first one above u * total
+  // running sums of the kept weights in index order; the first one above u * total (u = 0 draws the first token that has a
+  // weight, however small)
+#pragma unroll
+  for (int q = 0; q < SP_PER; ++q) fx[q] += light >> q & 1u;
   unsigned long long mine = 0ull, total, count;
 #pragma unroll
   for (int q = 0; q < SP_PER; ++q) mine += in >> q & 1u ? fx[q] : 0ull;
@@ -515,7 +518,6 @@ __device__ __forceinline__ bool draw_from_pairs(SampleShared& sh, const unsigned
   if (i < n) {
     w = weight(key_to_float(key));
     mine = (unsigned long long)__double2ll_rn(w * FX_ONE);
-    if (w > 0.0 && mine == 0ull) mine = 1ull;            // u = 0 draws the first token that has a weight, however small
   }
   if (part == 0) fx[i] = mine;
   __syncthreads();
@@ -541,6 +543,7 @@ __device__ __forceinline__ bool draw_from_pairs(SampleShared& sh, const unsigned
     in = in && above < goal;
   }
   in = in && w >= d.min_p;
+  if (w > 0.0 && mine == 0ull) mine = 1ull;              // u = 0 draws the first token that has a weight, however small
   if (part == 0) fx[i] = in ? mine | 1ull << 63 : 0ull;
   __syncthreads();
   at = -1;

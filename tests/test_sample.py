@@ -323,3 +323,17 @@ def test_min_p_before_within_and_behind_a_long_nucleus(ctx, dtype, spread, top_p
     out = run(ctx, xs, dtype, V, 0, None, 6, 0.9, 0, top_p, min_p, u)
     check(out, wl.storage_to_f64(xs, dtype)[:, :V], range(6), 0.9, 0, top_p, min_p, u)
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("V", [40, 700])
+def test_a_nucleus_of_half_between_two_equal_maxima(ctx, V):
+    """Two tokens share all the weight that fp64 sees beside them: the first is half of it, and u = 0 draws the first of them."""
+    x = np.full((2, (V + 3) // 4 * 4), -50.0, dtype=np.float32)
+    x[:, 7] = x[:, 30] = 4.0
+    for k, p, want in ((0, 0.5, 1), (20, 0.5, 1), (0, 0.75, 2), (2, 1.0, 2)):
+        tok, _, _, kept = run(ctx, x, "f32", V, 0, None, 2, 0.1, k, p, 0.0, [0.0, 0.999])
+        assert kept[:2].tolist() == [want, want] and tok[:2].tolist() == [7, 7 if want == 1 else 30]
+    tok, _, _, kept = run(ctx, x, "f32", V, 0, None, 2, 1.0, 0, 1.0, 0.0, [0.0, 0.999])
+    assert kept[:2].tolist() == [V, V] and tok[:2].tolist() == [0, 30]       # e^-54 is a weight, if a small one
+    assert ctx.poll_status() == 0
