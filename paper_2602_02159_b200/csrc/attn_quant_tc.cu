@@ -7,6 +7,12 @@
 // so both scales of that key are scalars in its registers.  sk_j joins the logit's scale factor and sv_j the exponent
 // (a_rj = s_rj + log2 sv_j, P_rj = 2^(a_rj - ref_r)): one fused multiply-add per logit either way, and the row sum
 // takes P_rj / sv_j.  ref_r follows the running maximum of a_rj lazily, so P fits fp16 (below).
+// The row sum does not depend on the value scales, but a numerator that P has lost (below 2^-126, where exponentials
+// flush to zero) is lost to it too: of two tokens of equal logits the one with sv 2^-87 beside one with 2^45.  ref_r is at
+// least 2 below the largest a_rj, so with all value scales within 2^64 of one another that takes a token 2^64 lighter than
+// the row's heaviest, which no sum sees.  From the first other scale on a warpgroup's exponentials are the numerators' square
+// roots: 2^-252 instead of 2^-126, the whole range of a float's exponents, for three multiplications more per logit (dense,
+// 32768 keys, 35 rows, every 50th V row zero: 84 us instead of 75).  Partial sums are joined with two factors each as well.
 // Codes enter the products as they are: every int8 and every e4m3 value is an fp16 value.  q enters as fp16 too, scaled
 // by a power of two that puts the tile's largest |q| at 2^14..2^15: bf16 has fewer fraction bits, so only elements
 // 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-11, absolute 2^-27 of the row's
@@ -60,10 +66,12 @@ constexpr int OFF_RAW = Q_BYTES + 2 * P_BYTES;
 constexpr int OFF_MISC = OFF_RAW + 2 * RING * SLOT;
 constexpr int MAX_SPLITS = 32;
 constexpr float P_MAX = 46340.f;               // the reference follows the maximum once a numerator exceeds 2^15.5 (fp16 ends at 65504) ...
+constexpr float ROOT_P_MAX = 215.2f;           // (where numerators are kept as their square roots)
 constexpr float OFFSET = 2.f;                  // ... and is put 2 (log2) below it: P is normal fp16 down to 2^-16 of the row's largest
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
 constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
                                                     // rows hold zeros, the writer flushes them)
+constexpr float SV_LOW = 0x1p-40f, SV_HIGH = 0x1p24f;   // 2^64 apart, around what values of ordinary size have
 
 struct QParams {
   const __nv_bfloat16* Q;
@@ -95,19 +103,20 @@ struct Geo {                                   // a CTA's share of the work; liv
   int stok_first, stok_n;                      // first sink (list position) in Misc::stok, and how many are there
   TileEnum te;
 };
+constexpr unsigned FAR = 1u << 31;             // in Misc::pieces: a value scale outside SV_LOW .. SV_HIGH
 constexpr int MAX_STOK = 8;                    // sink tiles of a split whose tokens are staged
 
 struct Misc {                                  // behind the tiles in shared memory
   unsigned long long bars[4 * RING + 17];
   alignas(16) float nref[2][QN];               // minus the reference exponent per row (set 1: second warpgroup's own)
-  alignas(16) float fac[2][QN];                // rescale factor / weight per row
+  alignas(16) float fac[2][QN];                // rescale factor (its root, see the softmax) / weight per row
   float red[8][64];                            // per softmax warp: column maxima, then row sums
   int orow[QN];                                // output row (position slot * H + head), -1: none
   int2 tlist[MAXT];
   int stok[MAX_STOK * TN];                     // tokens of the sink tiles, -1: dropped
   uint32_t tmem;
   int abort_flag, last;
-  unsigned qmax, pieces[2];                    // largest |q| (bf16 bits); row pieces a warpgroup has to re-reference
+  unsigned qmax, pieces[2];                    // largest |q| (bf16 bits); row pieces a warpgroup has to re-reference (and FAR)
   Geo geo;
 };
 constexpr int SMEM = 1024 + OFF_MISC + (int)sizeof(Misc);
@@ -152,7 +161,8 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 }
 // normal numbers only
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// from 2^-124 up; by way of a quarter, since the largest numbers' inverses are subnormal
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(0.25f * x)); return 0.25f * y; }
 // maximum over the warp of one float per lane (NaN is passed over)
 __device__ __forceinline__ float warp_max_f32(float x) {
   float m;
@@ -267,6 +277,9 @@ __device__ __forceinline__ float lane_reduce32(float* v, int lane, Op op) {
   return v[0];
 }
 
+struct Ordinary { static constexpr bool value = false; };
+struct Wide { static constexpr bool value = true; };
+
 // Softmax of one warpgroup (x = 0, 1: even, odd tiles), NP pieces of 8 rows; straight-line code per tile, since its length
 // in cycles is what a tile costs.  Leaves the row sums over this warpgroup's keys in ms.red.
 template <int NP>
@@ -304,9 +317,11 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
   };
   // of a tile's key: logit factor, log2 of the value scale (-inf: masked), one over the value scale
   float ck, lv, iv;
+  bool far = false;                                                    // its value scale is out of the ordinary
   auto factors = [&](float sk, float sv) {
     const bool masked = sv == -1.f;
     const float svc = fmaxf(sv, SV_MIN);
+    far = !masked && !(svc >= SV_LOW && svc <= SV_HIGH);
     ck = sk * cs;
     lv = masked ? -INFINITY : lg2(svc);
     iv = masked ? 0.f : rcp(svc);
@@ -315,122 +330,147 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
   scales(x, sk, sv);
   factors(sk, sv);
   scales(x + 2, sk, sv);
+  // Tiles j0, j0 + 2, ... .  With WIDE false it returns at the first tile that holds a value scale out of the ordinary, nothing of
+  // it done; with WIDE true the exponentials are square roots of the numerators and reach down to 2^-252 of the reference, and
+  // so are the factors of a changed reference, used twice.
   bool ok = true;
-  for (int j = x; j < nt; j += 2) {
-    const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-    ok = __all_sync(0xffffffffu, wait_bar(bar_s_full(sBar, x), ph, abort_flag));
-    tc_fence_after();
-    float a[NC];
-    uint32_t* ar = reinterpret_cast<uint32_t*>(a);
-    bool again = false;
-    unsigned pieces = (1u << NP) - 1u;
+  auto tiles = [&](auto wide, int j0) -> int {
+    constexpr bool WIDE = decltype(wide)::value;
+    constexpr float A_MAX = WIDE ? ROOT_P_MAX : P_MAX;
+    for (int j = j0; j < nt; j += 2) {
+      const uint32_t ph = (uint32_t)(j >> 1) & 1u;
+      ok = __all_sync(0xffffffffu, wait_bar(bar_s_full(sBar, x), ph, abort_flag));
+      tc_fence_after();
+      float a[NC];
+      uint32_t* ar = reinterpret_cast<uint32_t*>(a);
+      bool again = false;
+      unsigned pieces = (1u << NP) - 1u;
 #pragma unroll 1
-    for (;;) {
-      if (j >= 2 || again) {
-        // ---- P = 2^(s ck + lv - ref), to shared memory as fp16 ----
+      for (;;) {
+        if (j >= 2 || again) {
+          // ---- P = 2^(s ck + lv - ref), to shared memory as fp16 ----
 #pragma unroll
-        for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
-        tc_wait_ld();
+          for (int i = 0; i < NP; ++i) TC_LD8(ts + i * 8, ar + i * 8);
+          tc_wait_ld();
 #pragma unroll
-        for (int q = 0; q < NP * 2; ++q) {
-          const float4 rv = reinterpret_cast<const float4*>(nref)[q];
-          float* v = a + q * 4;
-          ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
-          ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
-          fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
-          fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
+          for (int q = 0; q < NP * 2; ++q) {
+            const float4 rv = reinterpret_cast<const float4*>(nref)[q];
+            float* v = a + q * 4;
+            ffma2(v[0], v[1], v[0], v[1], ck, ck, lv, lv);
+            ffma2(v[2], v[3], v[2], v[3], ck, ck, lv, lv);
+            fadd2(v[0], v[1], v[0], v[1], rv.x, rv.y);
+            fadd2(v[2], v[3], v[2], v[3], rv.z, rv.w);
+          }
+#pragma unroll
+          for (int e = 0; e < NC; ++e) a[e] = ex2(WIDE ? 0.5f * a[e] : a[e]);
+          // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
+          ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
+          float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+          for (int e = 0; e < NC; e += 4) {
+            m0 = fmax3(m0, a[e], a[e + 1]);
+            m1 = fmax3(m1, a[e + 2], a[e + 3]);
+          }
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = WIDE ? a[i * 8 + e] * a[i * 8 + e] : a[i * 8 + e];
+            sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
+                   pack_f16(v[6], v[7]));
+          }
+          fence_proxy_async();
+          // The numerators are formed before anyone has looked whether they fit: the look costs a barrier of the four warps,
+          // and here it is the one that hands the tile over anyway.
+          if (!named_any(1 + x, 128, (fmaxf(m0, m1) > A_MAX && !again) || (!WIDE && far) || !ok)) break;
+          if (named_any(1 + x, 128, !ok)) { ok = false; break; }
+          // ---- some row's maximum outgrew its reference: new references for the pieces it is in, and the tile once more
+          // (the first tile starts here, for all of them).  Rolled loops: code that runs this seldom is fetched from L2 each time ----
+          pieces = 0;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float* v = a + i * 8;
+            if (fmaxf(fmax3(fmax3(v[0], v[1], v[2]), v[3], v[4]), fmax3(v[5], v[6], v[7])) > A_MAX) pieces |= 1u << i;
+          }
+          pieces = __reduce_or_sync(0xffffffffu, pieces | (!WIDE && far ? FAR : 0u));
+          if (lane == 0 && pieces) atomicOr(&ms.pieces[x], pieces);
+          named_sync(1 + x, 128);
+          pieces = ms.pieces[x];
+          if (!WIDE && (pieces & FAR)) {                                 // the same in all threads
+            named_sync(1 + x, 128);
+            if (key == 0) ms.pieces[x] = 0u;
+            named_sync(1 + x, 128);
+            return j;
+          }
         }
-#pragma unroll
-        for (int e = 0; e < NC; ++e) a[e] = ex2(a[e]);
-        // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
-        ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
-        float m0 = 0.f, m1 = 0.f;
-#pragma unroll
-        for (int e = 0; e < NC; e += 4) {
-          m0 = fmax3(m0, a[e], a[e + 1]);
-          m1 = fmax3(m1, a[e + 2], a[e + 3]);
-        }
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const float* v = a + i * 8;
-          sts128(prow + (uint32_t)((i ^ (key & 7)) << 4), pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]),
-                 pack_f16(v[6], v[7]));
-        }
-        fence_proxy_async();
-        // The numerators are formed before anyone has looked whether they fit: the look costs a barrier of the four warps,
-        // and here it is the one that hands the tile over anyway.
-        if (!named_any(1 + x, 128, (fmaxf(m0, m1) > P_MAX && !again) || !ok)) break;
-        if (named_any(1 + x, 128, !ok)) { ok = false; break; }
-        // ---- some row's maximum outgrew its reference: new references for the pieces it is in, and the tile once more
-        // (the first tile starts here, for all of them).  Rolled loops: code that runs this seldom is fetched from L2 each time ----
-        pieces = 0;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const float* v = a + i * 8;
-          if (fmaxf(fmax3(fmax3(v[0], v[1], v[2]), v[3], v[4]), fmax3(v[5], v[6], v[7])) > P_MAX) pieces |= 1u << i;
-        }
-        pieces = __reduce_or_sync(0xffffffffu, pieces);
-        if (lane == 0 && pieces) atomicOr(&ms.pieces[x], pieces);
-        named_sync(1 + x, 128);
-        pieces = ms.pieces[x];
-      }
-#pragma unroll 1
-      for (int i = 0; i < NP; ++i) {
-        if (!(pieces >> i & 1u)) continue;
-        uint32_t v[8];
-        TC_LD8(ts + i * 8, v);
-        tc_wait_ld();
-        float mine = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float w = warp_max_f32(fmaf(__uint_as_float(v[e]), ck, lv));
-          if (lane == e) mine = w;
-        }
-        if (lane < 8) red[i * 8 + lane] = mine;
-      }
-      named_sync(1 + x, 128);
-      if (key < NC) {
-        float f = 1.f;
-        if (pieces >> (key >> 3) & 1u) {
-          const float(*r)[QN] = &ms.red[x * 4];
-          const float rowmax = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
-          const float old = nref[key], now = OFFSET - rowmax;
-          if (now < old) { f = ex2(now - old); nref[key] = now; }
-        }
-        fac[key] = f;
-        if (key == 0) ms.pieces[x] = 0u;
-      }
-      named_sync(1 + x, 128);
-      if (j >= 2) {                                                    // what these rows have summed: P V of tile j - 2 is done
-        tc_fence_after();
 #pragma unroll 1
         for (int i = 0; i < NP; ++i) {
           if (!(pieces >> i & 1u)) continue;
           uint32_t v[8];
-          TC_LD8(tO + i * 8, v);
+          TC_LD8(ts + i * 8, v);
           tc_wait_ld();
+          float mine = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fac[i * 8 + e]);
-          TC_ST8(tO + i * 8, v);
+          for (int e = 0; e < 8; ++e) {
+            const float w = warp_max_f32(fmaf(__uint_as_float(v[e]), ck, lv));
+            if (lane == e) mine = w;
+          }
+          if (lane < 8) red[i * 8 + lane] = mine;
         }
-        tc_wait_st();
+        named_sync(1 + x, 128);
+        if (key < NC) {
+          float f = 1.f;
+          if (pieces >> (key >> 3) & 1u) {
+            const float(*r)[QN] = &ms.red[x * 4];
+            const float rowmax = fmaxf(fmaxf(r[0][key], r[1][key]), fmaxf(r[2][key], r[3][key]));
+            const float old = nref[key], now = OFFSET - rowmax;
+            if (now < old) { f = ex2(WIDE ? 0.5f * (now - old) : now - old); nref[key] = now; }
+          }
+          fac[key] = f;
+          if (key == 0) ms.pieces[x] = 0u;
+        }
+        named_sync(1 + x, 128);
+        if (j >= 2) {                                                    // what these rows have summed: P V of tile j - 2 is done
+          tc_fence_after();
+#pragma unroll 1
+          for (int i = 0; i < NP; ++i) {
+            if (!(pieces >> i & 1u)) continue;
+            uint32_t v[8];
+            TC_LD8(tO + i * 8, v);
+            tc_wait_ld();
 #pragma unroll
-        for (int q = 0; q < NP * 2; ++q) {
-          const float4 f = reinterpret_cast<const float4*>(fac)[q];
-          l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w;
+            for (int e = 0; e < 8; ++e) {
+              const float f = fac[i * 8 + e];
+              v[e] = __float_as_uint(WIDE ? __uint_as_float(v[e]) * f * f : __uint_as_float(v[e]) * f);
+            }
+            TC_ST8(tO + i * 8, v);
+          }
+          tc_wait_st();
+#pragma unroll
+          for (int q = 0; q < NP * 2; ++q) {
+            const float4 f = reinterpret_cast<const float4*>(fac)[q];
+#pragma unroll
+            for (int t = 0; t < (WIDE ? 2 : 1); ++t) { l[4 * q] *= f.x; l[4 * q + 1] *= f.y; l[4 * q + 2] *= f.z; l[4 * q + 3] *= f.w; }
+          }
         }
+        again = true;
       }
-      again = true;
-    }
-    if (!ok) break;
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) { mbar_arrive(bar_p_full(sBar, x)); mbar_arrive(bar_s_empty(sBar, x)); }
+      if (!ok) return nt;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(bar_p_full(sBar, x)); mbar_arrive(bar_s_empty(sBar, x)); }
 #pragma unroll
-    for (int e = 0; e < NC; e += 2) ffma2(l[e], l[e + 1], a[e], a[e + 1], iv, iv, l[e], l[e + 1]);
-    factors(sk, sv);
-    scales(j + 4, sk, sv);
-  }
+      for (int e = 0; e < NC; e += 2) {
+        if constexpr (WIDE) { l[e] = fmaf(a[e] * iv, a[e], l[e]); l[e + 1] = fmaf(a[e + 1] * iv, a[e + 1], l[e + 1]); }
+        else ffma2(l[e], l[e + 1], a[e], a[e + 1], iv, iv, l[e], l[e + 1]);
+      }
+      factors(sk, sv);
+      scales(j + 4, sk, sv);
+    }
+    return nt;
+  };
+  const int rest = tiles(Ordinary(), x);
+  if (rest < nt) tiles(Wide(), rest);
   // all products done (each warpgroup waits for both buffers: the last two tiles)
   for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) wait_bar(bar_p_empty(sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag);
   tc_fence_after();
@@ -819,9 +859,10 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
         auto warps = [&](int q) { return ((ms.red[q * 4][r] + ms.red[q * 4 + 1][r]) + ms.red[q * 4 + 2][r]) + ms.red[q * 4 + 3][r]; };
         const float l0 = warps(0), l1 = warps(1), r0 = -ms.nref[0][r], r1 = -ms.nref[1][r];
         ref = fmaxf(r0, r1);
-        w0 = l0 != 0.f ? ex2(r0 - ref) : 0.f;
-        w1 = l1 != 0.f ? ex2(r1 - ref) : 0.f;
-        tot = w0 * l0 + w1 * l1;
+        const float h0 = l0 != 0.f ? ex2(0.5f * (r0 - ref)) : 0.f, h1 = l1 != 0.f ? ex2(0.5f * (r1 - ref)) : 0.f;
+        w0 = h0 * h0;
+        w1 = h1 * h1;
+        tot = h0 * l0 * h0 + h1 * l1 * h1;
       }
       if (n_splits > 1) {
         reinterpret_cast<float2*>(p.part_ml)[(size_t)blockIdx.x * QN + r] = make_float2(ref, tot);
@@ -897,9 +938,9 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll 4
           for (int s = 0; s < S; ++s) {
             const float2 v = __ldcg(ml + (size_t)s * QN);
-            const float w = v.y != 0.f ? ex2(v.x - m) : 0.f;
-            tot += w * v.y;
-            wts[tid * S + s] = w;
+            const float h = v.y != 0.f ? ex2(0.5f * (v.x - m)) : 0.f;
+            tot += h * v.y * h;
+            wts[tid * S + s] = h * h;
           }
           const int orow = ms.orow[tid];
           ms.fac[0][tid] = tot != 0.f ? 1.f / tot : 0.f;

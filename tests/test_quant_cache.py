@@ -804,3 +804,91 @@ def test_the_readmes_second_example_runs_as_printed(ctx):
     top = rows.float().abs().amax(-1, keepdim=True)
     assert bool((err <= (2.0 ** -4 + 2.0 ** -7) * rows.float().abs() + 2.0 ** -10 * top / 448).all())
     assert torch.isfinite(env["O"][:30].float()).all() and bool((env["token"][:30] >= 0).all()) and bool((env["token"][30:] == -1).all())
+
+
+# ---- value scales far apart: a row's sum and log-sum-exp do not depend on them -------------------------------------
+FAR = 2.0 ** -17 * math.log(2.0)
+# exponents (log2 of a value scale, a logit with it, the same less its reference) are below 2^8 in magnitude here: each is
+# rounded by at most 2^-17, which is a factor of 1 + FAR; three of them meet a numerator, two more its row's log-sum-exp
+
+
+def _far_scales(rng, kind, Hkv, L, d):
+    """Value codes and scales: a V row is all zeros, tiny or large."""
+    vc = rng.integers(-127, 128, size=(Hkv, L, d)).astype(np.float64)
+    vc[..., 0] = 127.0
+    e = rng.integers(45, 100, size=(Hkv, L))
+    first, odd = np.arange(L) < L // 2, np.arange(L) // 128 % 2 == 1
+    if kind == "zeros_beside_large":
+        e = np.where(rng.random((Hkv, L)) < 0.5, e, -1000)
+    elif kind == "tiny_beside_large":
+        e = np.where(rng.random((Hkv, L)) < 0.5, e, -e + 20)
+    elif kind == "large_last":                       # the splits of a key set, and the tiles of a split, differ
+        e = np.where(first, -80, 95) + 0 * e
+    elif kind == "large_first":
+        e = np.where(first, 95, -80) + 0 * e
+    elif kind == "tiles_in_turn":
+        e = np.where(odd, 95, -80) + 0 * e
+    else:                                            # all of them large, or all of them tiny
+        e = np.where(np.arange(Hkv)[:, None] % 2 == 0, 100, -80) + 0 * e
+    vs = np.where(e == -1000, 0.0, np.exp2(np.maximum(e, -80).astype(np.float64)) * rng.integers(2 ** 19, 2 ** 20, (Hkv, L)) / 2.0 ** 20)
+    vc[vs == 0.0] = 0.0
+    return vc, vs
+
+
+@gpu
+@pytest.mark.parametrize("simt", [False, True])
+@pytest.mark.parametrize("kind", ["zeros_beside_large", "tiny_beside_large", "large_last", "large_first", "tiles_in_turn", "one_size"])
+@pytest.mark.parametrize("H,Hkv,d,L,N", [(2, 2, 128, 900, 40), (80, 80, 64, 1100, 3), (4, 2, 128, 200, 30), (1, 1, 64, 6000, 5)])
+def test_value_scales_far_apart(ctx, simt, kind, H, Hkv, d, L, N):
+    """Every size that the writer makes (2^-87 .. 2^120, and 0) in one key set: O and lse of rows whose tokens all count."""
+    rng = np.random.default_rng(L + N)
+    Q = storage(rng.standard_normal((N, H, d)), "bf16")
+    kc, ks = fo.quantize_rows(rng.standard_normal((Hkv, L, d)) * 0.3, "int8")
+    vc, vs = _far_scales(rng, kind, Hkv, L, d)
+    K, V = kc * ks[..., None], vc * vs[..., None]
+    O, lse = torch.zeros(N, H, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(H, N, device="cuda")
+    dev = [codes_to_device(c, "int8") for c in (kc, vc)] + [torch.from_numpy(s).float().cuda().contiguous() for s in (ks, vs)]
+    ctx.set_force_simt(simt)
+    try:
+        fb.focus_dense_attn_quantized(ctx, fb.make_shape(L, L, H, Hkv, d, 64, fb.BF16), fstep.to_device(Q, "bf16"), L - N, N, None, None, 0,
+                                      fb.make_quant_cache(fb.KV_INT8, *dev), O, lse)
+    finally:
+        ctx.set_force_simt(False)
+    Qf, scale = wl.storage_to_f64(Q, "bf16"), 1.0 / math.sqrt(d)
+    eO, eL = fo.dense_attn(Qf, K, V, scale)
+    tO, tL = _bounds(Qf, K, V, vs, eO, scale, H // Hkv, "bf16")
+    for h in range(H):
+        s = Qf[:, h] @ K[h // (H // Hkv)].T * scale
+        p = np.exp(s - s.max(1, keepdims=True))
+        tO[:, h] += 2 * 3 * FAR * (p / p.sum(1, keepdims=True)) @ np.abs(V[h // (H // Hkv)])
+    assert (np.abs(fstep.from_device(lse) - eL) <= tL + 5 * FAR).all()
+    assert (np.abs(fstep.from_device(O) - eO) <= tO).all()
+    assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("simt", [False, True])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_a_token_without_a_value_takes_its_share(ctx, simt, fmt):
+    """Two tokens of equal logits, a V row of zeros beside one of any size: O is half of it and lse is log 2 more than a logit."""
+    d = 64
+    sh = fb.make_shape(2, 2, 1, 1, d, 64, fb.BF16)
+    Q = torch.zeros(1, 1, d, device="cuda").bfloat16()
+    for e in (0, 30, 40, 41, 45, 60, 90, 120):
+        x = torch.zeros(2, 1, d, device="cuda")
+        x[0] = 2.0 ** e
+        codes, sc = torch.zeros(2, 1, 2, d, dtype=torch.int8, device="cuda"), torch.zeros(2, 1, 2, device="cuda")
+        cache = fb.make_quant_cache(FMT[fmt], codes[0], codes[1], sc[0], sc[1])
+        rows = x.bfloat16().contiguous()
+        fb.focus_quantize_kv(ctx, sh, torch.zeros_like(rows), rows, d, d, 0, None, None, 2, cache)
+        O, lse = torch.zeros(1, 1, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 1, device="cuda")
+        ctx.set_force_simt(simt)
+        try:
+            fb.focus_dense_attn_quantized(ctx, sh, Q, 0, 1, None, None, 0, cache, O, lse)
+        finally:
+            ctx.set_force_simt(False)
+        # the stored value 2^e up to its scale's rounding (2^-24), fp16 numerators 2^-11, bf16 2^-8, exponents as above
+        want = 2.0 ** (e - 1)
+        assert bool(((O.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -11 + 6 * FAR + 2.0 ** -20)).all()), e
+        assert abs(float(lse) - math.log(2.0)) <= 5 * FAR + 2.0 ** -21, e
+    assert ctx.poll_status() == 0
