@@ -791,15 +791,17 @@ sample_kernel(const SampleParams p) {
         const int4 c = *reinterpret_cast<const int4*>(cl.map_shared_rank(hist, q) + tid * PER);
         count[0] += c.x; count[1] += c.y; count[2] += c.z; count[3] += c.w;
       }
-    // running weights from the bins' edges, half a bin to either side of its middle (a hundredth more for s_lo, of which the
-    // bins know nothing); 2e-5 for these sums' rounding.  The last bin weighs from nothing to its upper edge.
+    // running weights from the bins' edges, half a bin to either side of its middle, and 0.016 for x s_lo, of which the bins know
+    // nothing (|x s| <= 4096 + 32 above the last bin, |s_lo| <= 2^-24 s: 0.0158 of a bin); 2e-5 for these sums' rounding.  The last
+    // bin weighs from nothing to its upper edge.
+    constexpr float HALF = 0.516f;
     const float off = (float)(top_bits - __float_as_int(196608.f));
     float light[PER], heavy[PER], light_at = 0.f, heavy_at = 0.f;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       const float b = (float)(tid * PER + q), c = (float)count[q];
-      light_at += c * ex2_approx((off - b - 0.51f) * (1.f / SP_TAB)) * 0.99998f;
-      heavy_at += c * ex2_approx((off - b + 0.51f) * (1.f / SP_TAB)) * 1.00002f;
+      light_at += c * ex2_approx((off - b - HALF) * (1.f / SP_TAB)) * 0.99998f;
+      heavy_at += c * ex2_approx((off - b + HALF) * (1.f / SP_TAB)) * 1.00002f;
       light[q] = light_at; heavy[q] = heavy_at;
     }
     float light_in = light_at, heavy_in = heavy_at;

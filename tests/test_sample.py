@@ -337,3 +337,52 @@ def test_a_nucleus_of_half_between_two_equal_maxima(ctx, V):
     tok, _, _, kept = run(ctx, x, "f32", V, 0, None, 2, 1.0, 0, 1.0, 0.0, [0.0, 0.999])
     assert kept[:2].tolist() == [V, V] and tok[:2].tolist() == [0, 30]       # e^-54 is a weight, if a small one
     assert ctx.poll_status() == 0
+
+
+def _edge_logits(sign, n_values, apart):
+    """A temperature and descending fp32 logits for the far end of a histogram's precision.  log2(e) / T = s_hi + s_lo with
+    |s_lo| near half a step of s_hi, and x s_hi near 4096 for all of them, each x s_hi close to the upper (sign 1) or lower
+    edge (sign -1) between two multiples of 1/64, which x s_lo then oversteps by a 64th of a 64th."""
+    T = np.float32(1.44)
+    while True:
+        s = 1.4426950408889634 / float(T)
+        s_hi = float(np.float32(s))
+        if s > 1.0 and sign * (s - s_hi) > 0.49 * 2.0 ** -23:
+            break
+        T = np.nextafter(T, np.float32(0))
+    x, out, last = np.float32(4095.0 / s), [], None
+    while len(out) < n_values:
+        e = float(x) * s_hi * 64
+        b = round(e)
+        if sign * (e - b) > 0.4975 and (last is None or last - b >= apart):
+            out.append(x)
+            last = b
+        x = np.nextafter(x, np.float32(0))
+    return float(T), np.array(out, dtype=np.float32)
+
+
+@gpu
+@pytest.mark.parametrize("min_p", [0.0, 0.02, 0.2])
+@pytest.mark.parametrize("shuffled", [True, False])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_nucleus_that_ends_beside_the_edges_of_its_histogram(ctx, sign, shuffled, min_p):
+    """Equal logits 150 at a time, all of them on an edge; top-p 1e-5 on either side of a group's running weight."""
+    per = 150
+    T, values = _edge_logits(sign, 40, 8)
+    x = np.repeat(values, per)
+    if shuffled:
+        np.random.default_rng(1).shuffle(x)
+    xs = np.stack([x, x])
+    w = np.exp((values.astype(np.float64) - float(values[0])) / single(T))
+    share = np.cumsum(w) / w.sum()
+    wrong = []
+    for j in (4, 11, 19, 26, 33):
+        for side in (1 - 1e-5, 1 + 1e-5):
+            top_p, u = single(share[j] * side), [0.3, 0.999]
+            out = run(ctx, xs, "f32", len(x), 0, None, 2, T, 0, top_p, min_p, u)
+            for r in range(2):
+                want = fo.sample_token(x.astype(np.float64), single(T), 0, top_p, single(min_p), single(u[r]))
+                if (int(out[0][r]), int(out[3][r])) != (want[0], want[3]):
+                    wrong.append((j, side, r, int(out[0][r]), int(out[3][r]), want[0], want[3]))
+    assert not wrong, wrong
+    assert ctx.poll_status() == 0
