@@ -149,9 +149,9 @@ int32_t focus_set_option(focus_ctx* ctx, int32_t option, int32_t value);
 
 /* Self-test of the bounded waits (no counterpart in the paper).  Every wait on a barrier inside the tensor-core
  * kernels gives up after a time limit, records FOCUS_ERR_TIMEOUT in the status word and lets the kernel unwind
- * instead of spinning for ever.  This call launches one small CTA that waits, with a limit of limit_us microseconds
- * (1 .. 100 000), on a barrier nobody ever arrives at: afterwards focus_poll_status must report
- * FOCUS_ERR_TIMEOUT and the context must still be usable.  Nothing else is touched.  Errors: INVALID_ARG. */
+ * instead of spinning for ever.  This call launches one small CTA that waits on a barrier nobody ever arrives at, in both
+ * forms of a wait that the kernels have, one after the other, with a limit of limit_us microseconds (1 .. 100 000) each:
+ * afterwards focus_poll_status must report FOCUS_ERR_TIMEOUT and the context must still be usable.  Nothing else is touched.  Errors: INVALID_ARG. */
 focus_status focus_selftest_bounded_wait(focus_ctx* ctx, int32_t limit_us, focus_stream stream);
 
 /* Measurement aid (no counterpart in the paper): streams the `bytes` bytes at device pointer `ptr` once, read only,

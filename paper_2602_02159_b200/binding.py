@@ -187,8 +187,8 @@ class Context:
         return prev
 
     def selftest_bounded_wait(self, limit_us: int, stream=None) -> None:
-        """One small CTA waits limit_us microseconds on a barrier nobody arrives at, then gives up: poll_status()
-        reports ERR_TIMEOUT afterwards."""
+        """One small CTA waits limit_us microseconds on a barrier nobody arrives at and gives up, in either form of wait:
+        poll_status() reports ERR_TIMEOUT afterwards."""
         _check(self._lib.focus_selftest_bounded_wait(self.handle, int(limit_us), _stream(stream)),
                "focus_selftest_bounded_wait")
 

@@ -12,7 +12,7 @@
 // least 2 below the largest a_rj, so with all value scales within 2^64 of one another that takes a token 2^64 lighter than
 // the row's heaviest, which no sum sees.  From the first other scale on a warpgroup's exponentials are the numerators' square
 // roots: 2^-252 instead of 2^-126, the whole range of a float's exponents, for three multiplications more per logit (dense,
-// 32768 keys, 35 rows, every 50th V row zero: 84 us instead of 75).  Partial sums are joined with two factors each as well.
+// 32768 keys, 35 rows, every 50th V row zero: 83 us instead of 74).  Partial sums are joined with two factors each as well.
 // Codes enter the products as they are: every int8 and every e4m3 value is an fp16 value.  q enters as fp16 too, scaled
 // by a power of two that puts the tile's largest |q| at 2^14..2^15: bf16 has fewer fraction bits, so only elements
 // 2^28 times smaller than the largest lose any.  P is rounded to fp16 (relative 2^-11, absolute 2^-27 of the row's
@@ -248,15 +248,6 @@ __device__ __forceinline__ uint32_t bar_p_empty(uint32_t b, int i) { return b + 
 
 __device__ __forceinline__ uint32_t bar_q_full(uint32_t b) { return b + 8u * (4 * RING + 16); }
 
-// Bounded wait of few instructions (the roles' loops have to stay in the instruction cache; see the file comment): gives up
-// after about a second of polling, or when another thread of the CTA did, and leaves the report to the CTA's last lines.
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  for (int n = 0; !mbar_try_wait(bar, parity); ++n) {
-    if (*abort_flag || n > (1 << 23)) { *abort_flag = 1; return false; }
-  }
-  return true;
-}
-
 // the arrivals of n threads at once: the same barrier from 31 lanes would be 31 shared-memory atomics in a row
 __device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
@@ -339,7 +330,7 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
     constexpr float A_MAX = WIDE ? ROOT_P_MAX : P_MAX;
     for (int j = j0; j < nt; j += 2) {
       const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-      ok = __all_sync(0xffffffffu, wait_bar(bar_s_full(sBar, x), ph, abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_wait_quiet(bar_s_full(sBar, x), ph, abort_flag));
       tc_fence_after();
       float a[NC];
       uint32_t* ar = reinterpret_cast<uint32_t*>(a);
@@ -364,7 +355,7 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
 #pragma unroll
           for (int e = 0; e < NC; ++e) a[e] = ex2(WIDE ? 0.5f * a[e] : a[e]);
           // P V of this warpgroup's last tile has read the buffer (long ago, as a rule; the exponentials are on their way)
-          ok = __all_sync(0xffffffffu, wait_bar(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
+          ok = __all_sync(0xffffffffu, mbar_wait_quiet(bar_p_empty(sBar, x), ph ^ 1u, abort_flag) && ok);
           float m0 = 0.f, m1 = 0.f;
 #pragma unroll
           for (int e = 0; e < NC; e += 4) {
@@ -472,7 +463,7 @@ __device__ __forceinline__ void softmax_loop(const QParams& p, Misc& ms, uint32_
   const int rest = tiles(Ordinary(), x);
   if (rest < nt) tiles(Wide(), rest);
   // all products done (each warpgroup waits for both buffers: the last two tiles)
-  for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) wait_bar(bar_p_empty(sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag);
+  for (int j = nt > 1 ? nt - 2 : 0; j < nt; ++j) mbar_wait_quiet(bar_p_empty(sBar, j & 1), (uint32_t)(j >> 1) & 1u, abort_flag);
   tc_fence_after();
   // ---- row sums over this warp's 32 keys: lane i of a warp ends with row i of a group ----
   named_sync(1 + x, 128);                                              // the column maxima in ms.red have been read
@@ -613,10 +604,10 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       uint32_t round = 0;
       // All CTAs start together: with whole rings requested at once the first tile -- and the queries -- would wait behind
       // everybody's fifth.  The rest follows once the first tile's keys have landed.
-      if (n_early > 0 && nt > n_early) ok = __all_sync(0xffffffffu, wait_bar(bar_k_full(sBar, 0), 0u, abort_flag));
+      if (n_early > 0 && nt > n_early) ok = __all_sync(0xffffffffu, mbar_wait_quiet(bar_k_full(sBar, 0), 0u, abort_flag));
       for (int j = n_early; j < nt && ok; ++j) {
         const TileInfo ti = get_tile(p, ms, gm, j);
-        ok = __all_sync(0xffffffffu, wait_bar(empty0 + 8u * slot, (round & 1u) ^ 1u, abort_flag));
+        ok = __all_sync(0xffffffffu, mbar_wait_quiet(empty0 + 8u * slot, (round & 1u) ^ 1u, abort_flag));
         if (!ok) break;
         ++issued;
         if (ti.kind == 0) {
@@ -669,12 +660,12 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       // ================================ S^T = K Q^T ===============================================
       const uint32_t id = idesc_f16(gm.N, 0);
       const uint64_t qdesc = make_sdesc(sQ, 16, 1024);
-      if (wait_bar(bar_q_full(sBar), 0u, abort_flag))
+      if (mbar_wait_quiet(bar_q_full(sBar), 0u, abort_flag))
         for (int j = 0; j < nt; ++j) {
           const int b = j & 1;
           const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-          if (!wait_bar(bar_kop_full(sBar, b), ph, abort_flag)) break;
-          if (!wait_bar(bar_s_empty(sBar, b), ph ^ 1u, abort_flag)) break;
+          if (!mbar_wait_quiet(bar_kop_full(sBar, b), ph, abort_flag)) break;
+          if (!mbar_wait_quiet(bar_s_empty(sBar, b), ph ^ 1u, abort_flag)) break;
           tc_fence_after();
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
@@ -689,8 +680,8 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1u;
-        if (!wait_bar(bar_vop_full(sBar, b), ph, abort_flag)) break;
-        if (!wait_bar(bar_p_full(sBar, b), ph, abort_flag)) break;
+        if (!mbar_wait_quiet(bar_vop_full(sBar, b), ph, abort_flag)) break;
+        if (!mbar_wait_quiet(bar_p_full(sBar, b), ph, abort_flag)) break;
         tc_fence_after();
         const uint64_t pdesc = make_sdesc(sP + b * P_BYTES, TN * 128, 1024);
 #pragma unroll
@@ -718,8 +709,8 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
-        const bool ok = wait_bar(bar_k_full(sBar, slot), round & 1u, abort_flag) &&
-                        wait_bar(bar_kop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
+        const bool ok = mbar_wait_quiet(bar_k_full(sBar, slot), round & 1u, abort_flag) &&
+                        mbar_wait_quiet(bar_kop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawK + slot * SLOT, dst = tmem + (uint32_t)(T_K + b * 64) + lane_off;
@@ -766,8 +757,8 @@ attn_quant_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       uint32_t round = 0;
       for (int j = 0; j < nt; ++j) {
         const int b = j & 1;
-        const bool ok = wait_bar(bar_v_full(sBar, slot), round & 1u, abort_flag) &&
-                        wait_bar(bar_vop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
+        const bool ok = mbar_wait_quiet(bar_v_full(sBar, slot), round & 1u, abort_flag) &&
+                        mbar_wait_quiet(bar_vop_empty(sBar, b), ((uint32_t)(j >> 1) & 1u) ^ 1u, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
         const uint32_t src = sRawV + slot * SLOT, dst = tmem + (uint32_t)(T_V + b * 64) + ((uint32_t)(cw * 32) << 16);

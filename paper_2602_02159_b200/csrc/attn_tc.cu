@@ -1640,8 +1640,13 @@ __global__ void __launch_bounds__(32) bounded_wait_selftest_kernel(unsigned long
     fence_barrier_init();
   }
   __syncwarp();
-  // nobody arrives: the wait must give up after limit_ns, raise the flag and the status word, and return false
-  mbar_wait(b, 0u, &abort_flag, status, limit_ns);
+  // nobody arrives: the quiet wait must give up after limit_ns, raise the flag and return false; the other one then must do the
+  // same and raise the status word
+  const bool gave_up = !mbar_wait_quiet(b, 0u, &abort_flag, (uint32_t)limit_ns);
+  __syncwarp();
+  if (threadIdx.x == 0) abort_flag = 0;
+  __syncwarp();
+  if (gave_up) mbar_wait(b, 0u, &abort_flag, status, limit_ns);
 }
 }  // namespace
 

@@ -57,6 +57,21 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   set_status(status, FOCUS_ERR_TIMEOUT);
   return false;
 }
+// The same in few instructions, for loops that share the instruction cache with other roles': raises the flag alone and leaves
+// the report to the CTA's last lines.  The clock is read after every unsuccessful poll, since the hardware chooses how long a
+// poll stays suspended; its lower half (it wraps after 4.3 s) is enough for a second.
+__device__ __forceinline__ bool mbar_wait_quiet(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                                uint32_t limit_ns = (uint32_t)WAIT_LIMIT_NS) {
+  if (!mbar_try_wait(bar, parity)) {
+    uint32_t t0, now;
+    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t0));
+    do {
+      asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(now));
+      if (*abort_flag || now - t0 > limit_ns) { *abort_flag = 1; return false; }
+    } while (!mbar_try_wait(bar, parity));
+  }
+  return true;
+}
 __device__ __forceinline__ void fence_barrier_init() {
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }

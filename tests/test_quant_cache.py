@@ -892,3 +892,17 @@ def test_a_token_without_a_value_takes_its_share(ctx, simt, fmt):
         assert bool(((O.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -11 + 6 * FAR + 2.0 ** -20)).all()), e
         assert abs(float(lse) - math.log(2.0)) <= 5 * FAR + 2.0 ** -21, e
     assert ctx.poll_status() == 0
+
+
+@gpu
+def test_both_forms_of_a_wait_keep_to_their_limit(ctx):
+    """The self-test waits in the form of this file's kernel first, then in the other kernels': each for as long as it was told,
+    by the clock (a poll may stay suspended for as long as the hardware likes, so their number says nothing)."""
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    for limit_ms in (30, 90):
+        start.record()
+        ctx.selftest_bounded_wait(1000 * limit_ms)
+        end.record()
+        assert ctx.poll_status() == fb.ERR_TIMEOUT
+        assert 2 * limit_ms <= start.elapsed_time(end) < 2 * limit_ms + 100
+    assert ctx.poll_status() == 0
