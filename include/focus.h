@@ -375,8 +375,11 @@ focus_status focus_quantize_kv(focus_ctx* ctx, const focus_shape* shape, const v
                                const int32_t* n_rows, int32_t max_rows, const focus_quant_cache* cache,
                                focus_stream stream);
 
-/* Reads rows of an 8-bit cache back: out = code * scale, rounded once to shape.dtype.  With contiguous [Hkv, L, d]
- * strides the result is what focus_pool_keys, focus_find_sinks and focus_score_blocks take as K.
+/* Reads rows of an 8-bit cache back: out = code * scale, rounded to float and, for a bf16 shape, from there to bf16.  (A
+ * product may have 32 bits: where its float lies half way between two bf16 numbers, which about one in 100 000 does by
+ * rounding, the result can be the other neighbour of code * scale than the nearer one; it is within 2^-8 + 2^-24 of it.)
+ * With contiguous [Hkv, L, d] strides the result is what focus_pool_keys, focus_find_sinks and focus_score_blocks take
+ * as K.
  *   K_out, V_out  row r, KV head g at [r * out_stride_row + g * out_stride_head] (strides in elements, multiples of
  *                 8); either may be NULL
  *   rows          int32[max_rows] positions in any order with n_rows int32[1] (device), or both NULL: positions

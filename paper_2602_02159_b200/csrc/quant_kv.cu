@@ -1,7 +1,8 @@
 // Writing rows into an 8-bit K/V cache and reading them back:
 //   focus_quantize_kv    scale = max|x| / Q over the head_dim elements of one token and KV head, code = the format's
 //                        number nearest to x / scale;
-//   focus_dequantize_kv  x = code * scale.
+//   focus_dequantize_kv  x = code * scale, the product in fp32, which bf16 outputs round once more (one product instead of
+//                        an exact one of 32 bits: 2^-24 of the element beside the 2^-8 that bf16 costs anyway).
 // Both are bound by HBM: per element size(T) + 1 bytes move.  A row (64 or 128 elements) belongs to neighbouring lanes,
 // sixteen bytes of the wide side at a time (one such vector per lane when reading back, two when writing, so that the
 // row's two divisions are shared by more elements), so every access covers full sectors and the maximum is a butterfly

@@ -906,3 +906,34 @@ def test_both_forms_of_a_wait_keep_to_their_limit(ctx):
         assert ctx.poll_status() == fb.ERR_TIMEOUT
         assert 2 * limit_ms <= start.elapsed_time(end) < 2 * limit_ms + 100
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_rows_read_back_as_bf16_are_rounded_by_way_of_fp32(ctx, fmt):
+    """The two roundings that the header states, against products in 64 bits: every output is the fp32 product's nearest bf16,
+    and differs from the exact product's nearest only where that fp32 product is half way between two."""
+    Hkv, L, d = 2, 2048, 128
+    rng = np.random.default_rng(9)
+    if fmt == "int8":
+        vals = rng.integers(-127, 128, size=(Hkv, L, d)).astype(np.float64)
+    else:
+        bits = rng.integers(0, 256, size=(Hkv, L, d)).astype(np.uint8)
+        bits[(bits & 0x7f) == 0x7f] = 0x40
+        vals = torch.from_numpy(bits).view(torch.float8_e4m3fn).float().double().numpy()
+    sc = np.exp2(rng.integers(-40, 40, size=(Hkv, L))) * rng.integers(2 ** 23, 2 ** 24, size=(Hkv, L)) / 2.0 ** 24
+    vals[0, 0], sc[0, 0] = 6.0, float.fromhex("0x1.895554p-7")             # 6 x it is just below a tie, in fp32 the tie itself
+    out = torch.zeros(Hkv, L, d, dtype=torch.bfloat16, device="cuda")
+    codes, scales = codes_to_device(vals, fmt), torch.from_numpy(sc).float().cuda()
+    fb.focus_dequantize_kv(ctx, fb.make_shape(L, 0, 2, Hkv, d, 64, fb.BF16), fb.make_quant_cache(FMT[fmt], codes, None, scales, None), 0,
+                           None, None, L, out, None, d, L * d)
+    exact = vals * sc[..., None]                                            # 8 + 24 bits: exact in 64
+    got = out.double().cpu().numpy()
+    single = exact.astype(np.float32)
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(exact), 2.0 ** -120))) - 7)       # of bf16 there (8 bits)
+    assert (np.abs(got - exact) <= step / 2 + np.abs(exact) * 2.0 ** -24).all()
+    assert (np.abs(got - single.astype(np.float64)) <= step / 2).all()
+    tie = (single.view(np.uint32) & 0xFFFF) == 0x8000
+    assert (np.abs(got - exact)[~tie] <= step[~tie] / 2).all()
+    assert tie[0, 0].all() and (got[0, 0] == 0.072265625).all() and np.abs(exact[0, 0, 0] - 0.07177734375) < np.abs(exact[0, 0, 0] - 0.072265625)
+    assert ctx.poll_status() == 0
