@@ -119,8 +119,10 @@ def _stream(stream) -> Optional[int]:
         if _torch is None:
             import torch
             _torch = torch
-        # the handle of torch.cuda.current_stream() without building the stream object (a microsecond per call)
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+        # the handle of torch.cuda.current_stream() without building the stream object (a microsecond per call), by an internal
+        # function of PyTorch's where it is there
+        raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+        return raw(_torch.cuda.current_device()) if raw else _torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -89,3 +89,14 @@ def test_layer_schedule_matches_the_paper():
     d = layer_schedule(28, 5, final_dense=4)                 # paper: l_dense = 6 (1-indexed) -> probe layer 5
     assert d[:5] == ["dense"] * 5 and d[5] == "probe" and d[6:24] == ["sparse"] * 18 and d[24:] == ["dense"] * 4
     assert layer_schedule(4, 3, final_dense=4) == ["dense", "dense", "dense", "probe"]
+
+
+def test_the_current_stream_with_and_without_pytorchs_internal_lookup(monkeypatch):
+    """A call without a stream goes to PyTorch's current one, also where PyTorch lacks the internal function that tells its handle."""
+    from types import SimpleNamespace as NS
+    cuda = NS(current_device=lambda: 3, current_stream=lambda: NS(cuda_stream=77))
+    monkeypatch.setattr(fb, "_torch", NS(_C=NS(_cuda_getCurrentRawStream=lambda device: 1000 + device), cuda=cuda))
+    assert fb._stream(None) == 1003
+    monkeypatch.setattr(fb, "_torch", NS(_C=NS(), cuda=cuda))
+    assert fb._stream(None) == 77
+    assert fb._stream(5) == 5 and fb._stream(NS(cuda_stream=6)) == 6
