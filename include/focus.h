@@ -333,8 +333,10 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
  *             shortest prefix that holds at least top_p of the weight left by top_k (1: no cut), and to those with
  *             w_v >= min_p (0: no cut); at least one token stays
  *   token     the first kept v, in ascending v, whose running sum of kept weights exceeds u * their total.  Sums are
- *             held in 64 bits and a weight is off by less than 1e-9 of itself, so the token (and the kept set) is
- *             the one the definition names unless two sums that it compares are that close
+ *             held in 64 bits.  A weight is off by less than 1e-9 of itself or, where the kept tokens are few enough
+ *             to be listed (up to 2048), by 2^-51 of the largest; a listed token lighter than that counts as 2^-50 in
+ *             the draw, and weights below 2^-1000 of the largest may count as 2^-1000 or as 0.  So the token (and the
+ *             kept set) is the one the definition names unless two sums that it compares are that close
  *   conf      w_token / total: its probability in the distribution it was drawn from
  *   prob      (may be NULL) softmax_v(x)[token] at temperature 1 over the whole vocabulary: Eq. 2's confidence
  *   n_kept    (may be NULL) int32, size of the kept set

@@ -7,7 +7,8 @@
 // and in fp32 those sums are off by as much as a rare token weighs.  Sums run in a fixed order (lanes, warps, CTAs), so
 // the answer does not depend on timing.
 //
-// The kept set is a prefix of the descending order.  Two ways to it:
+// The kept set is a prefix of the descending order.  Two ways to it (a list's weights are integers in units of 2^-50 of the
+// largest weight, off by half of that; a lighter token counts as one unit in the draw, so that it has a share):
 //   short list  (up to 2048 tokens).  Which logits to collect: for top-k up to 1024, those from the k-th largest of the
 //               maxima of the threads' shares up -- a lower bound of the k-th largest logit that few more reach; for a
 //               nucleus, those up to the histogram bin in which it must end.  They are collected in index order and cut by
@@ -18,9 +19,9 @@
 //               (T, how many of the tokens at T) says all about the set.  Then the kept weight per warp segment in index
 //               order, the segment that holds u * total, a run of it per lane, and its walk.
 // What bounds it: HBM for many rows of top-k (512 rows of 126464 bf16 logits, top-k 50, top-p 0.9: 66 us, of which the
-// loads are 20), instruction issue in the pass over the vocabulary's weights for a nucleus (35 rows, top-p 0.95: 35 us;
-// 11 us are that pass, 24 instructions per logit), and the latency of a dozen barriers and exchanges for one row (50257
-// fp32 logits: 14 us).
+// loads are 20), instruction issue in the pass over the vocabulary's weights for a nucleus (35 rows, top-p 0.95: 35 us,
+// 41 on other boxes; 11 us are that pass, 24 instructions per logit), and the latency of a dozen barriers and exchanges for
+// one row (50257 fp32 logits: 14 us).
 #include <cooperative_groups.h>
 #include <float.h>
 
@@ -251,8 +252,10 @@ __device__ __forceinline__ double pow2_near(double t, const double* tab) {
 // pow2_near and a separate histogram): x s for s = s_hi + s_lo is reduced in fp32.  With zero = 1.5 * 2^17 - R / 64 the sum
 // x s_hi + zero is rounded to multiples of 1/64, R being 64 m s_hi rounded, so its bits count 64ths of the exponent from
 // the maximum's down (the bins of a histogram as well) and x s_hi less that multiple is a single fused operation: r.
-// Weights come relative to 2^(R / 64).  r is rounded to 2^-33, so a weight is off by ln2 2^-32 = 1.7e-10 of itself, and
-// 2^r - 1 < 0.0055 by 2.5 roundings of 2^-24: together less than 1e-9, of either sign.
+// Weights come relative to 2^(R / 64).  r, up to 2^-7, is rounded twice by up to 2^-32: ln2 2^-31 = 3.2e-10 of a weight.
+// 2^r - 1 < 0.0055 is r times a factor near 0.7 that its last addition rounds by 2^-25 and fp32's ln2 shifts by 1.9e-9
+// (2.5e-10 after r), and their product is rounded by 2^-32 (2.3e-10).  Together, with 1e-11 of the cubic and 2e-11 that
+// s_hi + s_lo lacks of s, 8.4e-10: less than 1e-9, of either sign.
 struct Reduced {
   int bits;
   float r;
