@@ -386,3 +386,19 @@ def test_a_nucleus_that_ends_beside_the_edges_of_its_histogram(ctx, sign, shuffl
                     wrong.append((j, side, r, int(out[0][r]), int(out[3][r]), want[0], want[3]))
     assert not wrong, wrong
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("knobs", KNOBS)
+@pytest.mark.parametrize("dtype,vocab,stride,spread", [("bf16", 5000, 5000, 2.0), ("f32", 4099, 4100, 2.5), ("bf16", 32768, 32776, 0.5)])
+def test_rows_without_a_list_start_at_the_base(ctx, dtype, vocab, stride, spread, knobs):
+    """No list: row r is position pos_base + r, whose logits are the r-th row; every row is the oracle's, with and without the
+    optional outputs."""
+    rng = np.random.default_rng(vocab + int(10 * knobs[0]))
+    xs = wl.to_storage((rng.standard_normal((12, stride)) * spread).astype(np.float32), dtype)
+    u = rng.random(12)
+    out = run(ctx, xs, dtype, vocab, 300, None, 12, *knobs, u)
+    check(out, wl.storage_to_f64(xs, dtype)[:, :vocab], range(12), *knobs, u)
+    bare = run(ctx, xs, dtype, vocab, 300, None, 12, *knobs, u, outputs=False)
+    assert np.array_equal(bare[0], out[0]) and np.array_equal(bare[1], out[1])
+    assert ctx.poll_status() == 0
