@@ -36,7 +36,7 @@ struct TileEnum {
   const int32_t* blocks;
 };
 
-// First key tile of split s of n: floor(total * s / n).  total < 2^23 tiles (2^30 tokens) and s <= 8, so the product
+// First key tile of split s of n: floor(total * s / n).  total < 2^23 tiles (2^30 tokens) and s <= 32, so the product
 // fits 32 bits (a 64-bit division is a subroutine of a few hundred cycles on the set-up path of every CTA).
 __device__ __forceinline__ int split_lo(int total, int s, int n) {
   return (int)((unsigned)total * (unsigned)s / (unsigned)n);
