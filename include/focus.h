@@ -370,8 +370,9 @@ focus_status focus_update_kv(focus_ctx* ctx, const focus_shape* shape, void* K_c
  *   rows          int32[max_rows] positions, strictly ascending, with n_rows int32[1] (device), or both NULL:
  *                 positions pos_base .. pos_base + max_rows - 1 (a prompt, a block entry)
  * NaN elements count as 0, infinite ones take the largest code; neither enters the scale.  A row whose largest
- * magnitude is below 2^-80 is stored as zeros with scale 0.  Rows listed outside [0, L) or out of order are skipped
- * and reported through the status word. */
+ * magnitude is below 2^-80 is stored as zeros with scale 0.  Rows listed outside [0, L), or not above the row listed
+ * before them, are skipped and reported through the status word (what such a list leaves at a position that it names
+ * twice further apart is not defined). */
 focus_status focus_quantize_kv(focus_ctx* ctx, const focus_shape* shape, const void* K_new, const void* V_new,
                                int64_t new_stride_row, int64_t new_stride_head, int32_t pos_base, const int32_t* rows,
                                const int32_t* n_rows, int32_t max_rows, const focus_quant_cache* cache,
