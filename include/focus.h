@@ -297,7 +297,10 @@ focus_status focus_dense_attn(focus_ctx* ctx, const focus_shape* shape, const vo
 /* focus_sparse_attn and focus_dense_attn over an 8-bit cache: the same rows, key sets, outputs and layouts, with K and
  * V taken from `cache`.  Codes enter the tensor cores as they are (fp16 holds every code of both formats); the scales
  * are applied to the logits and to the softmax numerators in fp32, so nothing is rounded between the cache and the
- * products.  A row with no key to attend (empty lists, no sinks, M == L) gives O = 0 and lse = -inf.  Errors as
+ * products.  What meets the codes there is fp16 too: the queries, up to 64 stacked rows of a KV head under one power of
+ * two (nothing is lost down to 2^-28 of their largest element), and the numerators (relative 2^-11, and 2^-27 of the
+ * row's largest numerator with its value scale).  Row sums and lse are fp32 and do not depend on how far the value
+ * scales are apart.  A row with no key to attend (empty lists, no sinks, M == L) gives O = 0 and lse = -inf.  Errors as
  * there; INVALID_ARG also for an unknown format or a misaligned cache.
  * The codes of every attended token must be finite, its scales finite and non-negative; a V scale below 2^-87, where
  * focus_quantize_kv writes none but 0, may count as 2^-87.  fp32 shapes run on the SIMT kernel. */

@@ -38,10 +38,11 @@
 //
 // What bounds it, and what it takes (32 heads of 128, int8 unless stated): a key tile's softmax, about 950 ns of a CTA per tile
 // of 128 keys and 35 rows, in which the two warpgroups have the SM's exponentials, conversions and shared-memory writes between
-// them, and about 14 us around the loop (prologue, first tile, merge of the splits).  Dense, 32768 keys, 35 rows: 76 us,
-// 3.5 TB/s of cache (its bytes alone would take 42).  Dense, 28 query heads on 4 KV heads, e4m3, 16384 keys, 61 rows: 47 us.
-// Sparse, 15 blocks of 128, 322 sinks and 512 response tokens, 35 rows: 22.5 us.  Dense, 16384 keys, 256 rows: 147 us
-// (467 TFLOP/s; every row tile of 64 expands the codes again).
+// them, and about 14 us around the loop (prologue, first tile, merge of the splits).  Dense, 32768 keys, 35 rows: 74 to
+// 77 us, 3.6 TB/s of cache (its bytes alone would take 42).  Dense, 28 query heads on 4 KV heads, e4m3, 16384 keys, 61 rows: 51 us
+// (47 to 52, from box to box).  Sparse, 15 blocks of 128, 322 sinks and 512 response tokens, 35 rows: 25.5 us (22.5 to 26).
+// Dense, 16384 keys, 256 rows: 147 us (467 TFLOP/s; every row tile of 64 expands the codes again).  attn_tc.cu, from a bf16
+// cache of the same shapes on the same box: 89, 37.5, 22 and 80 us.
 #include <stddef.h>
 
 #include "attn_tiles.cuh"
