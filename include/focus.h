@@ -302,8 +302,8 @@ focus_status focus_dense_attn(focus_ctx* ctx, const focus_shape* shape, const vo
  * row's largest numerator with its value scale).  Row sums and lse are fp32 and do not depend on how far the value
  * scales are apart.  A row with no key to attend (empty lists, no sinks, M == L) gives O = 0 and lse = -inf.  Errors as
  * there; INVALID_ARG also for an unknown format or a misaligned cache.
- * The codes of every attended token must be finite, its scales finite and non-negative; a V scale below 2^-87, where
- * focus_quantize_kv writes none but 0, may count as 2^-87.  fp32 shapes run on the SIMT kernel. */
+ * The codes of every attended token must be finite, its scales finite and non-negative; a V scale below 2^-89, where
+ * focus_quantize_kv writes none but 0, may count as 2^-89.  fp32 shapes run on the SIMT kernel. */
 focus_status focus_sparse_attn_quantized(focus_ctx* ctx, const focus_shape* shape, const void* Q, int32_t q_base,
                                          int32_t n_q, const int32_t* q_rows, const int32_t* n_rows, int32_t max_rows,
                                          const focus_quant_cache* cache, int32_t head_reduce,

@@ -8,7 +8,7 @@
 // (a_rj = s_rj + log2 sv_j, P_rj = 2^(a_rj - ref_r)): one fused multiply-add per logit either way, and the row sum
 // takes P_rj / sv_j.  ref_r follows the running maximum of a_rj lazily, so P fits fp16 (below).
 // The row sum does not depend on the value scales, but a numerator that P has lost (below 2^-126, where exponentials
-// flush to zero) is lost to it too: of two tokens of equal logits the one with sv 2^-87 beside one with 2^45.  ref_r is at
+// flush to zero) is lost to it too: of two tokens of equal logits the one with sv 2^-89 beside one with 2^45.  ref_r is at
 // least 2 below the largest a_rj, so with all value scales within 2^64 of one another that takes a token 2^64 lighter than
 // the row's heaviest, which no sum sees.  From the first other scale on a warpgroup's exponentials are the numerators' square
 // roots: 2^-252 instead of 2^-126, the whole range of a float's exponents, for three multiplications more per logit (dense,
@@ -70,8 +70,8 @@ constexpr float P_MAX = 46340.f;               // the reference follows the maxi
 constexpr float ROOT_P_MAX = 215.2f;           // (where numerators are kept as their square roots)
 constexpr float OFFSET = 2.f;                  // ... and is put 2 (log2) below it: P is normal fp16 down to 2^-16 of the row's largest
 constexpr float REF_NONE = -1e30f;             // reference of a row that has seen no key
-constexpr float SV_MIN = 6.4623485355705288e-27f;   // 2^-87: smaller value scales count as this (no product is lost: their
-                                                    // rows hold zeros, the writer flushes them)
+constexpr float SV_MIN = 0x1p-89f;             // smaller value scales count as this (no product is lost: their rows hold zeros, the
+                                               // writer's smallest other scale is 2^-80 / 448)
 constexpr float SV_LOW = 0x1p-40f, SV_HIGH = 0x1p24f;   // 2^64 apart, around what values of ordinary size have
 
 struct QParams {

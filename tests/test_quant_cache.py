@@ -937,3 +937,41 @@ def test_rows_read_back_as_bf16_are_rounded_by_way_of_fp32(ctx, fmt):
     assert (np.abs(got - exact)[~tie] <= step[~tie] / 2).all()
     assert tie[0, 0].all() and (got[0, 0] == 0.072265625).all() and np.abs(exact[0, 0, 0] - 0.07177734375) < np.abs(exact[0, 0, 0] - 0.072265625)
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("simt", [False, True])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_the_smallest_values_that_are_kept_are_attended(ctx, simt, fmt):
+    """V rows whose largest magnitude is 2^-80 and a little more, the smallest that are not stored as zeros: their scales are the
+    smallest there are (2^-80 / Q)."""
+    rng = np.random.default_rng(4)
+    H, d, L, N = 2, 64, 300, 20
+    x = rng.uniform(-1.0, 1.0, size=(L, H, d))
+    x[..., 0] = 1.0
+    x *= 2.0 ** -80 * rng.choice([1.0, 1.25, 2.0, 3.0], size=(L, H, 1))
+    V, K = storage(x, "bf16"), storage(rng.standard_normal((L, H, d)), "bf16")
+    codes, sc = torch.zeros(2, H, L, d, dtype=torch.int8, device="cuda"), torch.zeros(2, H, L, device="cuda")
+    cache = fb.make_quant_cache(FMT[fmt], codes[0], codes[1], sc[0], sc[1])
+    sh = fb.make_shape(L, L, H, H, d, 64, fb.BF16)
+    fb.focus_quantize_kv(ctx, sh, fstep.to_device(K, "bf16"), fstep.to_device(V, "bf16"), H * d, d, 0, None, None, L, cache)
+    assert bool((sc[1] > 0).all())
+    Q = storage(rng.standard_normal((N, H, d)), "bf16")
+    O, lse = torch.zeros(N, H, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(H, N, device="cuda")
+    ctx.set_force_simt(simt)
+    try:
+        fb.focus_dense_attn_quantized(ctx, sh, fstep.to_device(Q, "bf16"), L - N, N, None, None, 0, cache, O, lse)
+    finally:
+        ctx.set_force_simt(False)
+    kc, vc = (fo.quantize_rows(wl.storage_to_f64(a, "bf16").transpose(1, 0, 2), fmt) for a in (K, V))
+    Kd, Vd = (c * s[..., None] for c, s in (kc, vc))
+    Qf, scale = wl.storage_to_f64(Q, "bf16"), 1.0 / math.sqrt(d)
+    eO, eL = fo.dense_attn(Qf, Kd, Vd, scale)
+    tO, tL = _bounds(Qf, Kd, Vd, vc[1], eO, scale, 1, "bf16")
+    for h in range(H):                                                      # exponents near 2^-87, rounded as FAR says
+        s = Qf[:, h] @ Kd[h].T * scale
+        p = np.exp(s - s.max(1, keepdims=True))
+        tO[:, h] += 2 * 3 * FAR * (p / p.sum(1, keepdims=True)) @ np.abs(Vd[h])
+    assert (np.abs(fstep.from_device(O) - eO) <= tO).all()
+    assert (np.abs(fstep.from_device(lse) - eL) <= tL + 5 * FAR).all()
+    assert ctx.poll_status() == 0
