@@ -338,7 +338,7 @@ focus_status focus_confidence(focus_ctx* ctx, const void* logits, int32_t dtype,
  *   token     the first kept v, in ascending v, whose running sum of kept weights exceeds u * their total.  Sums are
  *             held in 64 bits.  A weight is off by less than 1e-9 of itself or, where the kept tokens are few enough
  *             to be listed (up to 2048), by 2^-51 of the largest; a listed token lighter than that counts as 2^-50 in
- *             the draw, and weights below 2^-1000 of the largest may count as 2^-1000 or as 0.  So the token (and the
+ *             the draw, and weights below 2^-900 of the largest may count as 2^-1000 or as 0.  So the token (and the
  *             kept set) is the one the definition names unless two sums that it compares are that close
  *   conf      w_token / total: its probability in the distribution it was drawn from
  *   prob      (may be NULL) softmax_v(x)[token] at temperature 1 over the whole vocabulary: Eq. 2's confidence

@@ -235,7 +235,7 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // entries, and one multiplication less, the lookups took most of the time.  2^r is a cubic with |r| <= h = 1/128: the
 // Taylor terms, and the fourth power replaced by h^2 r^2 - h^4 / 8 (Chebyshev), without that constant, since only ratios
 // of weights matter.  It leaves ln2^4 / 24 * h^4 / 4 = 9e-12 of a weight between any two of them.
-// -1000 <= t <= 0; no branch, so that several run side by side.
+// -1020 <= t <= 0; no branch, so that several run side by side.
 __device__ __forceinline__ double pow2_near(double t, const double* tab) {
   const double magic = 6755399441055744.0;               // 1.5 * 2^52: adding it leaves the rounded integer in the low bits
   constexpr double ln2 = 0.69314718055994531, h = 0.5 / SP_TAB;
@@ -703,10 +703,12 @@ sample_kernel(const SampleParams p) {
   const float top64 = plain ? (float)(rint((double)(m - shift) * (double)s_hi * SP_TAB) / SP_TAB) : 0.f, zero = 196608.f - top64;
   auto reduced = [&](float x) -> Reduced { return reduce_exponent(fmaxf(x, floor_x) - shift, s_hi, s_lo, zero); };
   const int top_bits = reduced(m).bits;                  // (a tie may put them one off top64's)
+  // Which tokens have a weight at all must be one rule wherever a draw can end on them: with u = 0 the first segment, run and
+  // token with a weight have to be each other's.  Where weight_plain may be used it is the comparison with floor_x.
   auto weight = [&](float x) -> double {
     if (m == INFINITY) return x == m ? 1.0 : 0.0;
     const double t = ((double)x - md) * scale;
-    return t >= -1000.0 ? pow2_near(t, tab) : 0.0;
+    return (plain ? x > floor_x : t >= -1000.0) ? pow2_near(t, tab) : 0.0;
   };
   auto weight_plain = [&](float x) -> double { return pow2_reduced(reduced(x), tab); };
   const double unit = pow2_near((double)top64 - (double)(m - shift) * scale, tab);                   // weight_plain's, in weight's
@@ -1277,7 +1279,7 @@ sample_kernel(const SampleParams p) {
             double w;
             bool in;
             if (plain) {                                 // the exact weight only where min-p depends on its last bits
-              w = weight_plain(x[e]) * unit;
+              w = x[e] > floor_x ? weight_plain(x[e]) * unit : 0.0;
               in = w >= min_w * (1.0 + 1e-8) || (w >= min_w * (1.0 - 1e-8) && weight(x[e]) >= min_w);
             } else {
               w = weight(x[e]);

@@ -402,3 +402,23 @@ def test_rows_without_a_list_start_at_the_base(ctx, dtype, vocab, stride, spread
     bare = run(ctx, xs, dtype, vocab, 300, None, 12, *knobs, u, outputs=False)
     assert np.array_equal(bare[0], out[0]) and np.array_equal(bare[1], out[1])
     assert ctx.poll_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("knobs", [(0.1, 3000, 1.0, 0.0), (0.1, 20000, 1.0, 0.0), (0.1, 0, 1.0, 0.0), (0.1, 0, 0.99, 0.0), (0.1, 40, 1.0, 0.0),
+                                   (0.1, 3000, 0.9, 0.0), (0.1, 3000, 1.0, 0.5)])
+def test_a_number_of_zero_beside_weights_that_vanish(ctx, dtype, knobs):
+    """One logit a thousand temperatures above the rest, whose weights no 64-bit float holds: u = 0 draws that one, wherever it lies
+    and however many others the cuts keep."""
+    rng = np.random.default_rng(7)
+    V = 40001
+    x = rng.standard_normal((4, 40008)).astype(np.float32)
+    for r, at in enumerate((0, 17000, 31111, V - 1)):
+        x[r, at] = 120.0
+    xs = wl.to_storage(x, dtype)
+    for u in (np.zeros(4), np.full(4, 1e-44), np.full(4, 0.5)):
+        out = run(ctx, xs, dtype, V, 0, None, 4, *knobs, u)
+        check(out, wl.storage_to_f64(xs, dtype)[:, :V], range(4), *knobs, u)
+        assert out[0][:4].tolist() == [0, 17000, 31111, V - 1] and (out[1][:4] == 1).all()
+    assert ctx.poll_status() == 0
