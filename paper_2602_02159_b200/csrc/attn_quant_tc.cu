@@ -40,9 +40,9 @@
 // of 128 keys and 35 rows, in which the two warpgroups have the SM's exponentials, conversions and shared-memory writes between
 // them, and about 14 us around the loop (prologue, first tile, merge of the splits).  Dense, 32768 keys, 35 rows: 74 to
 // 77 us, 3.6 TB/s of cache (its bytes alone would take 42).  Dense, 28 query heads on 4 KV heads, e4m3, 16384 keys, 61 rows: 51 us
-// (47 to 52, from box to box).  Sparse, 15 blocks of 128, 322 sinks and 512 response tokens, 35 rows: 25.5 us (22.5 to 26).
+// (47 to 52, from device to device).  Sparse, 15 blocks of 128, 322 sinks and 512 response tokens, 35 rows: 25.5 us (22.5 to 26).
 // Dense, 16384 keys, 256 rows: 147 us (467 TFLOP/s; every row tile of 64 expands the codes again).  attn_tc.cu, from a bf16
-// cache of the same shapes on the same box: 89, 37.5, 22 and 80 us.
+// cache of the same shapes on the same device: 89, 37.5, 22 and 80 us.
 #include <stddef.h>
 
 #include "attn_tiles.cuh"

@@ -20,7 +20,7 @@
 //               order, the segment that holds u * total, a run of it per lane, and its walk.
 // What bounds it: HBM for many rows of top-k (512 rows of 126464 bf16 logits, top-k 50, top-p 0.9: 66 us, of which the
 // loads are 20), instruction issue in the pass over the vocabulary's weights for a nucleus (35 rows, top-p 0.95: 35 us,
-// 41 on other boxes; 11 us are that pass, 24 instructions per logit), and the latency of a dozen barriers and exchanges for
+// 41 on other devices; 11 us are that pass, 24 instructions per logit), and the latency of a dozen barriers and exchanges for
 // one row (50257 fp32 logits: 14 us).
 #include <cooperative_groups.h>
 #include <float.h>
