@@ -103,6 +103,50 @@ typedef struct {
   int64_t scale_stride_head;       /* in floats, >= L; 0 => L */
 } focus_quant_cache;
 
+/* ---- rotary positions (the paper leaves them to the model: Q and K arrive turned) -----------------------------
+ * The first rot_dim elements of a head are pairs; pair i of a row at position p turns by the angle p * f_i:
+ *     y1 = m (x1 cos - x2 sin),   y2 = m (x2 cos + x1 sin)
+ *   FOCUS_ROPE_HALVES  pair i = elements i and i + rot_dim / 2
+ *   FOCUS_ROPE_PAIRS   pair i = elements 2 i and 2 i + 1
+ * Frequencies f_i in radians per position, from `base`:
+ *   FOCUS_ROPE_PLAIN   f_i = base^(-2 i / rot_dim)
+ *   FOCUS_ROPE_LINEAR  f_i / factor (positions interpolated)
+ *   FOCUS_ROPE_NTK     base * factor^(rot_dim / (rot_dim - 2)) in the place of base
+ *   FOCUS_ROPE_BANDS   by turns within the trained length, t = trained f_i / 2 pi: f_i where t >= high, f_i / factor where
+ *                      t <= low, in between mixed with the weight (t - low) / (high - low) of f_i
+ *   FOCUS_ROPE_YARN    by pair number: f_i up to pair floor(i(high)), f_i / factor from pair ceil(i(low)), i(t) = the pair
+ *                      (as a real number) that makes t turns, mixed linearly in between; m = 0.1 ln(factor) + 1
+ * m is 1 for the others.  A plan is plain data that focus_rope_init fills; it holds f_i / 2 pi as fractions of 2^64, so
+ * that a phase is one integer product: exact to 2^-33 turns at any position. */
+typedef enum { FOCUS_ROPE_HALVES = 0, FOCUS_ROPE_PAIRS = 1 } focus_rope_layout;
+typedef enum { FOCUS_ROPE_PLAIN = 0, FOCUS_ROPE_LINEAR = 1, FOCUS_ROPE_NTK = 2, FOCUS_ROPE_BANDS = 3,
+               FOCUS_ROPE_YARN = 4 } focus_rope_scaling;
+typedef struct {
+  int32_t rot_dim, layout;         /* multiple of 16, at most 128; focus_rope_layout */
+  float magnitude;                 /* m */
+  int32_t reserved;
+  uint64_t turn[64];               /* rot_dim / 2 entries: turns per position, in units of 2^-64 */
+} focus_rope;
+
+/* ---- paged K/V cache: several sequences in one pool ------------------------------------------------------------
+ * Token j of sequence s lies in page page_table[s * max_pages + j / page_size], at place j % page_size of it; element c of
+ * KV head g there is K[page * stride_page + place * stride_tok + g * stride_head + c] (strides in elements, multiples of
+ * 8, the same for V), so [pages, tokens, heads, d] and [pages, heads, tokens, d] are both cases of it.  kv_len[s] is the
+ * number of tokens that sequence s holds; entries of the table beyond them are not read.  In calls that take this cache
+ * the shape's L is the longest length a sequence may have (max_pages * page_size >= L); its M, kv_block and kv strides
+ * are not used.  Page numbers outside [0, n_pages), positions outside [0, L) and lengths outside [0, L] are reported
+ * through the status word: such a row is not written, such keys are not attended, such a length counts as L or 0.
+ * New rows are packed: those of sequence s are the rows row_start[s] .. row_start[s + 1] - 1 (device, n_seqs + 1 entries,
+ * not decreasing, within [0, max_rows]); row_start NULL: one new row per sequence, row s, and max_rows == n_seqs.  Rows
+ * of outputs that belong to no sequence are left as they were. */
+typedef struct {
+  void* K; void* V;                                   /* pools (device), shape.dtype */
+  int64_t stride_page, stride_tok, stride_head;
+  const int32_t* page_table;                          /* int32[n_seqs * max_pages] (device) */
+  const int32_t* kv_len;                              /* int32[n_seqs] (device) */
+  int32_t page_size, n_pages, n_seqs, max_pages;      /* any page_size >= 1 */
+} focus_paged_cache;
+
 /* ---- context ------------------------------------------------------------------------------- */
 
 /* Creates a context on `device` and allocates its workspace (workspace_bytes == 0: 256 MiB) and a
@@ -129,7 +173,7 @@ uint64_t focus_launch_count(void);
  * two query tiles per CTA (taken for >= 256 stacked rows per KV head and >= 24 key tiles per CTA), 4 = tensor-core
  * kernel with one query tile and two softmax warpgroups on alternating key tiles (>= 128 stacked rows per KV head
  * and >= 4 key tiles per CTA, where 3 does not apply), 5 = the tensor-core kernel for 8-bit caches (the two
- * _quantized calls on bf16 queries); 0 = none yet. */
+ * _quantized calls on bf16 queries); 6 = focus_paged_attn on bf16, 7 = on fp32; 0 = none yet. */
 int32_t focus_last_attn_variant(focus_ctx* ctx);
 
 /* Selects the attention implementation for bf16 inputs (head_dim 128 or 64): 0 = automatic (tensor-core
@@ -424,6 +468,63 @@ focus_status focus_commit_step(focus_ctx* ctx, const float* conf_new, const int3
                                const int32_t* rows, const int32_t* n_rows, int32_t max_rows, int32_t L,
                                int32_t blk_lo, int32_t blk_hi, int32_t n_unmask, float* conf, uint8_t* masked,
                                int32_t* x, int32_t* unmasked_idx, int32_t* n_unmasked, focus_stream stream);
+
+/* ---- batched decoding over a paged cache (no counterpart in the paper: its batch is 1) ---------------------- */
+
+/* Fills a rotation plan (host only, no device work).  low, high and trained_len are read by BANDS and YARN only, factor by
+ * all but PLAIN.  Errors: INVALID_ARG (rot_dim not a multiple of 16 in 16 .. 128, unknown layout or scaling, base <= 1,
+ * factor < 1, and for BANDS and YARN low <= 0, high <= low or trained_len <= 0). */
+focus_status focus_rope_init(focus_rope* rope, int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor,
+                             double low, double high, int32_t trained_len);
+/* The same from the caller's own frequencies: radians_per_position[rot_dim / 2] (host), finite and not negative;
+ * magnitude finite. */
+focus_status focus_rope_from_frequencies(focus_rope* rope, int32_t rot_dim, int32_t layout,
+                                         const double* radians_per_position, double magnitude);
+
+/* Turns rows by their positions (rotary positions, above); elements from rot_dim on are copied.
+ *   rope       host pointer, read before the call returns
+ *   direction  1, or -1: by the opposite angle (the transpose, times m: the gradient of X from that of Y)
+ *   X, Y       row r, head h at [r * stride_row + h * stride_head], n_heads heads of head_dim (64 or 128) elements, dtype
+ *              FOCUS_F32 or FOCUS_BF16; Y may be X (then with equal strides), and may not overlap it otherwise.  Strides in
+ *              elements, multiples of 8
+ *   positions  int32[max_rows] with n_rows int32[1] (device), or both NULL: row r is at pos_base + r.  Negative positions
+ *              are reported and their rows left as they were, as are rows beyond n_rows.
+ * Angles, sines and products are fp32; the result is rounded once.  Errors: INVALID_ARG, UNSUPPORTED (head_dim; a rot_dim
+ * above head_dim). */
+focus_status focus_rotate(focus_ctx* ctx, const focus_rope* rope, int32_t direction, const void* X, void* Y, int32_t dtype,
+                          int32_t n_heads, int32_t head_dim, int64_t x_stride_row, int64_t x_stride_head,
+                          int64_t y_stride_row, int64_t y_stride_head, int32_t pos_base, const int32_t* positions,
+                          const int32_t* n_rows, int32_t max_rows, focus_stream stream);
+
+/* focus_update_kv for a paged cache, with the rotation on the way: row r of K_new (turned) and of V_new (as it is) goes to
+ * its sequence's place in the pools, and row r of Q (turned) to Q_out.
+ *   rope         host pointer, or NULL: nothing is turned
+ *   Q            may be NULL (then Q_out too); K_new, V_new may both be NULL (queries only)
+ *                row r, head h of each at [r * new_stride_row + h * new_stride_head]: the parts of a fused projection's rows
+ *   Q_out        by the shape's q strides: row r, head h at [r * q_stride_row + h * q_stride_head], as focus_paged_attn
+ *                reads it.  May be Q where the strides are equal
+ *   row_start    which rows are whose (focus_paged_cache, above)
+ *   positions    int32[max_rows] (device): positions within the sequences; or NULL: the new rows are the last ones,
+ *                kv_len[s] counting them already
+ * What the cache holds at a position that two rows name is not defined.  A row that is reported (position out of range, no
+ * page) is skipped whole.  Errors: INVALID_ARG, UNSUPPORTED. */
+focus_status focus_append_kv_paged(focus_ctx* ctx, const focus_shape* shape, const focus_rope* rope, const void* Q,
+                                   const void* K_new, const void* V_new, int64_t new_stride_row, int64_t new_stride_head,
+                                   const int32_t* row_start, const int32_t* positions, int32_t max_rows,
+                                   const focus_paged_cache* cache, void* Q_out, focus_stream stream);
+
+/* focus_dense_attn over a paged cache: every new row attends all kv_len[s] tokens of its sequence (its own among them, once
+ * focus_append_kv_paged has written them).
+ *   Q     [max_rows rows] by the shape's q strides, row r at [r * q_stride_row]
+ *   O     [max_rows, H, d] contiguous, shape.dtype; lse float[H * max_rows] (lse[h * max_rows + r]) or NULL
+ * A row of a sequence without tokens gives O = 0 and lse = -inf.  What the pools hold outside the sequences' tokens has no
+ * effect, NaN included.  bf16: tensor-core products, numerators rounded to bf16 (2^-8 of each at
+ * most), sums fp32; fp32: fp32
+ * products.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL (needs focus_paged_attn_workspace_bytes).  One launch. */
+focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shape, const void* Q, const int32_t* row_start,
+                              int32_t max_rows, const focus_paged_cache* cache, void* O, float* lse, focus_stream stream);
+/* Upper bound of the scratch that focus_paged_attn needs on the context's device for this shape, whatever the lengths. */
+focus_status focus_paged_attn_workspace_bytes(focus_ctx* ctx, const focus_shape* shape, size_t* out_bytes);
 
 #ifdef __cplusplus
 }

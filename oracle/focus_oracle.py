@@ -27,6 +27,9 @@ Functions and the passages they follow
 Beside the paper (deployment variants of its cache and its decoding rule, stated in include/focus.h)
   quantize_rows    rows as 8-bit codes with one scale each, and the numbers the codes stand for.
   sample_token     one token of a logits row by temperature, top-k, top-p, min-p and a uniform number.
+  rope_frequencies, rotate   rotary positions: radians per position of each pair, and rows turned by them.
+  paged_rows, paged_attn     the rows of a sequence gathered from its pages, and attention of its new rows over them.
+  token_logprobs   log probability and rank of a token, entropy and the most probable tokens of a logits row.
 
 Readings where the paper leaves a choice (parity unpinned by the paper for these):
   * Eq. 6 writes one softmax over an "aggregated query representation"; here every
@@ -343,3 +346,85 @@ def sample_token(x: np.ndarray, temperature: float, top_k: int, top_p: float, mi
             break
     z = math.fsum(weight(v, 1.0) for v in cand)
     return tok, weight(tok, temperature) / total, weight(tok, 1.0) / z, n
+
+
+def rope_frequencies(rot_dim: int, base: float, scaling: str = "plain", factor: float = 1.0, low: float = 1.0,
+                     high: float = 1.0, trained_len: int = 0):
+    """(radians per position of the rot_dim / 2 pairs, magnitude)."""
+    if scaling == "ntk":
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    out = []
+    for i in range(rot_dim // 2):
+        f = base ** (-2.0 * i / rot_dim)
+        if scaling == "linear":
+            f = f / factor
+        if scaling == "bands":
+            t = trained_len * f / (2 * math.pi)
+            if t <= low:
+                f = f / factor
+            elif t < high:
+                w = (t - low) / (high - low)
+                f = w * f + (1 - w) * f / factor
+        if scaling == "yarn":
+            pair = [rot_dim * math.log(trained_len / (2 * math.pi * t)) / (2 * math.log(base)) for t in (high, low)]
+            lo, hi = max(math.floor(pair[0]), 0), min(math.ceil(pair[1]), rot_dim - 1)
+            w = 0.0 if i <= lo else 1.0 if i >= hi else (i - lo) / (hi - lo)
+            f = (1 - w) * f + w * f / factor
+        out.append(f)
+    return np.array(out), (0.1 * math.log(factor) + 1.0 if scaling == "yarn" else 1.0)
+
+
+def rotate(x: np.ndarray, positions, frequencies: np.ndarray, layout: str = "halves", magnitude: float = 1.0,
+           direction: int = 1) -> np.ndarray:
+    """Rows x [rows, heads, d] turned by their positions; the first 2 * len(frequencies) elements of a head are pairs."""
+    half = len(frequencies)
+    y = np.array(x, dtype=np.float64)
+    first, second = ((np.arange(half), np.arange(half) + half) if layout == "halves"
+                     else (2 * np.arange(half), 2 * np.arange(half) + 1))
+    for r, p in enumerate(positions):
+        c, s = np.cos(p * frequencies) * magnitude, np.sin(p * frequencies) * magnitude * direction
+        a, b = y[r][:, first].copy(), y[r][:, second].copy()
+        y[r][:, first] = a * c - b * s
+        y[r][:, second] = b * c + a * s
+    return y
+
+
+def paged_rows(pool: np.ndarray, table, n: int) -> np.ndarray:
+    """Tokens 0 .. n - 1 of a sequence [n, Hkv, d] from a pool [pages, tokens of a page, Hkv, d] and its row of the table."""
+    page = pool.shape[1]
+    return np.stack([pool[table[j // page], j % page] for j in range(n)]) if n else np.zeros((0,) + pool.shape[2:])
+
+
+def paged_attn(q: np.ndarray, keys: np.ndarray, values: np.ndarray, scale: float):
+    """New rows q [rows, H, d] over keys, values [n, Hkv, d]: (O [rows, H, d], lse [H, rows]); without keys 0 and -inf."""
+    rows, H, d = q.shape
+    O, lse = np.zeros((rows, H, d)), np.full((H, rows), -np.inf)
+    if len(keys):
+        for h in range(H):
+            g = h // (H // keys.shape[1])
+            z = scale * (q[:, h] @ keys[:, g].T)
+            m = z.max(-1, keepdims=True)
+            w = np.exp(z - m)
+            O[:, h] = (w @ values[:, g]) / w.sum(-1, keepdims=True)
+            lse[h] = (m + np.log(w.sum(-1, keepdims=True)))[:, 0]
+    return O, lse
+
+
+def token_logprobs(x: np.ndarray, temperature: float, token: int, n_top: int):
+    """(log probability of `token`, its rank, entropy, top tokens, their log probabilities), or None for a row without a
+    finite or infinite positive logit.  Order: descending logit, ties by lower index; NaN counts as -inf."""
+    x = np.where(np.isnan(x), -np.inf, np.asarray(x, dtype=np.float64))
+    m = x.max()
+    if m == -np.inf:
+        return None
+    if m == np.inf:
+        z = np.where(x == np.inf, 0.0, -np.inf)
+    else:
+        z = (x - m) / temperature
+    total = math.fsum(np.exp(z))
+    lp = z - math.log(total)
+    p = np.exp(lp)
+    entropy = -math.fsum(p[p > 0] * lp[p > 0])
+    order = sorted(range(len(x)), key=lambda v: (-x[v], v))
+    top = order[:n_top]
+    return (lp[token] if token >= 0 else None, order.index(token) if token >= 0 else None, entropy, top, lp[top])

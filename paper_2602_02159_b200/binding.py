@@ -17,6 +17,8 @@ F32, BF16 = 0, 1
 HEADS_PER_KV_GROUP, HEADS_ALL = 0, 1
 SINK_TOKENS, SINK_BLOCKS = 0, 1
 KV_INT8, KV_E4M3 = 0, 1
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = range(5)
 OPT_MERGE_MODE, OPT_NO_WIDE, OPT_NO_PDL = 0, 1, 2
 MERGE_AUTO, MERGE_COUNTERS, MERGE_KERNEL = 0, 1, 2
 
@@ -39,10 +41,22 @@ class focus_quant_cache(C.Structure):
                 ("V_scale", C.c_void_p), ("scale_stride_head", C.c_int64)]
 
 
+class focus_rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("turn", C.c_uint64 * 64)]
+
+
+class focus_paged_cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("stride_page", C.c_int64), ("stride_tok", C.c_int64),
+                ("stride_head", C.c_int64), ("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
 _lib = None
 _P, _I, _Z = C.c_void_p, C.c_int32, C.c_size_t
 _SH = C.POINTER(focus_shape)
 _QC, _F = C.POINTER(focus_quant_cache), C.c_float
+_RP, _PC, _L, _D = C.POINTER(focus_rope), C.POINTER(focus_paged_cache), C.c_int64, C.c_double
 
 _SIGS = {
     "focus_create": (_I, [C.POINTER(_P), C.c_int, _Z]),
@@ -75,6 +89,12 @@ _SIGS = {
     "focus_sparse_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _I, _P, _I, _P, _P, _P, _I, _P, _P, _P]),
     "focus_dense_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _P, _P, _P]),
     "focus_sample": (_I, [_P, _P, _I, C.c_int64, _I, _I, _I, _P, _P, _I, _F, _I, _F, _F, _P, _P, _P, _P, _P, _P]),
+    "focus_rope_init": (_I, [_RP, _I, _I, _D, _I, _D, _D, _D, _I]),
+    "focus_rope_from_frequencies": (_I, [_RP, _I, _I, C.POINTER(_D), _D]),
+    "focus_rotate": (_I, [_P, _RP, _I, _P, _P, _I, _I, _I, _L, _L, _L, _L, _I, _P, _P, _I, _P]),
+    "focus_append_kv_paged": (_I, [_P, _SH, _RP, _P, _P, _P, _L, _L, _P, _P, _I, _PC, _P, _P]),
+    "focus_paged_attn": (_I, [_P, _SH, _P, _P, _I, _PC, _P, _P, _P]),
+    "focus_paged_attn_workspace_bytes": (_I, [_P, _SH, C.POINTER(_Z)]),
     "focus_dense_attn": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P]),
 }
 
@@ -148,6 +168,31 @@ def make_quant_cache(format, K, V, K_scale, V_scale, scale_stride_head=0) -> foc
     scales [Hkv, >= L] with scale_stride_head floats per KV head (0: the shape's L).  The tensors stay the caller's to
     keep alive."""
     return focus_quant_cache(format, _ptr(K), _ptr(V), _ptr(K_scale), _ptr(V_scale), scale_stride_head)
+
+
+def make_rope(rot_dim, layout, base, scaling=ROPE_PLAIN, factor=1.0, low=1.0, high=1.0, trained_len=0) -> focus_rope:
+    """A rotation plan (focus_rope_init): plain data, made once and kept by the caller."""
+    r = focus_rope()
+    _check(load_library().focus_rope_init(C.byref(r), rot_dim, layout, base, scaling, factor, low, high, trained_len),
+           "focus_rope_init")
+    return r
+
+
+def make_rope_from_frequencies(layout, radians_per_position, magnitude=1.0) -> focus_rope:
+    """The same from rot_dim / 2 frequencies of the caller's."""
+    f = [float(v) for v in radians_per_position]
+    r = focus_rope()
+    _check(load_library().focus_rope_from_frequencies(C.byref(r), 2 * len(f), layout, (_D * len(f))(*f), magnitude),
+           "focus_rope_from_frequencies")
+    return r
+
+
+def make_paged_cache(K, V, page_table, kv_len, page_size, n_pages, n_seqs, max_pages, stride_page, stride_tok,
+                     stride_head) -> focus_paged_cache:
+    """A paged cache over the caller's tensors: pools K, V (strides in elements, alike for both), page_table int32
+    [n_seqs, max_pages], kv_len int32 [n_seqs].  The tensors stay the caller's to keep alive."""
+    return focus_paged_cache(_ptr(K), _ptr(V), stride_page, stride_tok, stride_head, _ptr(page_table), _ptr(kv_len),
+                             page_size, n_pages, n_seqs, max_pages)
 
 
 class Context:
@@ -340,3 +385,30 @@ def focus_sample(ctx, logits, dtype, row_stride, vocab, pos_base, n_pos, rows, n
     _check(ctx._lib.focus_sample(ctx.handle, _ptr(logits), dtype, row_stride, vocab, pos_base, n_pos, _ptr(rows),
                                  _ptr(n_rows), max_rows, temperature, top_k, top_p, min_p, _ptr(u), _ptr(conf),
                                  _ptr(token), _ptr(prob), _ptr(n_kept), _stream(stream)), "focus_sample")
+
+
+def focus_rotate(ctx, rope, direction, X, Y, dtype, n_heads, head_dim, x_stride_row, x_stride_head, y_stride_row,
+                 y_stride_head, pos_base, positions, n_rows, max_rows, stream=None):
+    _check(ctx._lib.focus_rotate(ctx.handle, C.byref(rope), direction, _ptr(X), _ptr(Y), dtype, n_heads, head_dim,
+                                 x_stride_row, x_stride_head, y_stride_row, y_stride_head, pos_base, _ptr(positions),
+                                 _ptr(n_rows), max_rows, _stream(stream)), "focus_rotate")
+
+
+def focus_append_kv_paged(ctx, shape, rope, Q, K_new, V_new, new_stride_row, new_stride_head, row_start, positions, max_rows,
+                          cache, Q_out, stream=None):
+    _check(ctx._lib.focus_append_kv_paged(ctx.handle, C.byref(shape), None if rope is None else C.byref(rope), _ptr(Q),
+                                          _ptr(K_new), _ptr(V_new), new_stride_row, new_stride_head, _ptr(row_start),
+                                          _ptr(positions), max_rows, C.byref(cache), _ptr(Q_out), _stream(stream)),
+           "focus_append_kv_paged")
+
+
+def focus_paged_attn_workspace_bytes(ctx, shape: focus_shape) -> int:
+    out = _Z(0)
+    _check(load_library().focus_paged_attn_workspace_bytes(ctx.handle, C.byref(shape), C.byref(out)),
+           "focus_paged_attn_workspace_bytes")
+    return out.value
+
+
+def focus_paged_attn(ctx, shape, Q, row_start, max_rows, cache, O, lse=None, stream=None):
+    _check(ctx._lib.focus_paged_attn(ctx.handle, C.byref(shape), _ptr(Q), _ptr(row_start), max_rows, C.byref(cache), _ptr(O),
+                                     _ptr(lse), _stream(stream)), "focus_paged_attn")

@@ -1,0 +1,688 @@
+// focus_paged_attn: softmax attention of each sequence's new rows over the sequence's pages.
+//
+//     o_r = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q_r . k_j - m_r)
+//
+// With one new token per sequence a key meets hpg = H / Hkv query rows (1 .. 40), 4 hpg flops for each 2 bytes of K and V:
+// HBM bounds it, and what counts is that every SM always has loads in flight, whatever the lengths.
+//
+// Work.  A segment is (sequence, KV head, tile of RT stacked rows = new rows x query heads of the group), a run of 16-key
+// tiles.  Lengths are on the device, so the split is made there: every CTA sums the segments' costs (tiles + SEG_COST, the
+// price of filling and draining the pipeline), and CTA c of G takes the stretch [c T / G, (c + 1) T / G) of the total T.
+// A stretch covers whole segments and pieces of at most two: those leave (max, sum, unnormalised O) in the workspace, and
+// the CTA that arrives last at the segment's counter joins them in CTA order (in groups of JOIN, then the groups' results,
+// where there are more than 2 JOIN), so results do not depend on timing.
+//
+// CTA: four warps, each on its own tiles (w, w + 4, ...) through a ring of its own, filled by 16-byte cp.async with the
+// page looked up per key (any page size), no barrier inside a segment.  Two CTAs per SM (fp32 with 128 columns: one) cover
+// each other's segment ends.
+//
+// bf16: products by mma.sync with keys on the M side, S^T = K Q^T and O^T = V^T P^T, so one to eight rows cost one N tile;
+// an SM needs one m16n8k16 pair per 64 bytes of cache it reads, an eighth of what it can issue at HBM's rate.  (tcgen05 has
+// M = 128 keys per instruction and its scores come back through TMEM: latency, where bytes are the bound.)  A tile's row
+// statistics are shuffles over the lanes that hold its keys; P^T becomes the B operand by movmatrix.
+// fp32: fp32 products on the CUDA cores, a lane per key (and half row) for the scores, per column for the values.
+#include <math.h>
+
+#include "focus_common.cuh"
+
+namespace {
+
+constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
+constexpr int KT = 16;                   // keys per tile
+constexpr int SEG_COST = 6;              // cost of a segment beside its tiles, in tiles
+constexpr int MIN_COST = 16;             // least cost per CTA: below, joining costs more than sharing gains
+constexpr int JOIN = 8;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LAZY = 8.f;              // the running maximum may lag by this much (base 2): numerators stay below 2^8
+
+struct PagedArgs {
+  const void* Q;
+  long long q_row, q_head;
+  const void* K;
+  const void* V;
+  long long st_page, st_tok, st_head;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* row_start;
+  int page, n_pages, n_seqs, max_pages, L, max_rows, H, Hkv, hpg;
+  float scale;                           // softmax scale * log2 e
+  void* O;
+  float* lse;
+  float* part;                           // [gridDim.x][2] partials: RT (max, sum) pairs, then RT rows of D
+  int32_t* counters;                     // 3 per CTA, zero between launches
+  int32_t* status;
+};
+
+template <typename T, int D, int NT>
+struct Cfg {
+  static constexpr int RT = 8 * NT;                                       // stacked rows per tile
+  static constexpr int ROW_BYTES = D * (int)sizeof(T);
+  static constexpr int STAGES = ROW_BYTES == 128 ? 6 : 3;
+  static constexpr int OPERAND = KT * ROW_BYTES, STAGE = 2 * OPERAND, RING = STAGES * STAGE;   // per warp
+  static constexpr int Q_PITCH = sizeof(T) == 2 ? D + 8 : D;              // elements; 16 bytes on: ldmatrix without conflicts
+  static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
+  static constexpr int PART = RT * (D + 2);                               // floats of one partial in the workspace
+  static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
+  static constexpr int OFF_Q = RING * PA_WARPS;
+  static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][8][KT]
+  static constexpr int OFF_ML = OFF_P + (sizeof(T) == 4 ? PA_WARPS * 8 * KT * 4 : 0);
+  static constexpr int OFF_MASK = OFF_ML + PA_WARPS * RT * 8;
+  static constexpr int SMEM = OFF_MASK + PA_WARPS * STAGES * 4;
+  static_assert(RT * O_PITCH * 4 <= RING, "a warp's partial lies in its ring");
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+struct Seq {
+  int len, first, rows, row_tiles;       // tokens; first new row, how many; tiles of stacked rows
+};
+
+template <int RT>
+__device__ __forceinline__ Seq seq_of(const PagedArgs& a, int s) {
+  Seq q;
+  q.len = a.kv_len[s];
+  if (q.len < 0 || q.len > a.L) {
+    set_status(a.status, FOCUS_ERR_INVALID_ARG);
+    q.len = q.len < 0 ? 0 : a.L;
+  }
+  q.first = s; q.rows = 1;
+  if (a.row_start) {
+    const int lo = a.row_start[s], hi = a.row_start[s + 1];
+    q.first = lo; q.rows = hi - lo;
+    if (lo < 0 || hi < lo || hi > a.max_rows) { set_status(a.status, FOCUS_ERR_INVALID_ARG); q.rows = 0; }
+  }
+  q.row_tiles = (int)(((long long)q.rows * a.hpg + RT - 1) / RT);
+  return q;
+}
+__device__ __forceinline__ int seg_cost(const Seq& q) { return (q.len + KT - 1) / KT + SEG_COST; }
+__device__ __forceinline__ long long seq_cost(const Seq& q, int Hkv) { return (long long)seg_cost(q) * q.row_tiles * Hkv; }
+
+// where in the pools the keys of tile t lie: lane l has key 16 t + (l & 15), -1 where there is none to attend
+__device__ __forceinline__ long long key_offset(const PagedArgs& a, int s, int len, int t, int lane) {
+  const int j = t * KT + (lane & 15);
+  if (j >= len) return -1;
+  const int at = j / a.page, page = a.table[(long long)s * a.max_pages + at];
+  if (page < 0 || page >= a.n_pages) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return -1; }
+  return (long long)page * a.st_page + (long long)(j - at * a.page) * a.st_tok;
+}
+
+// a tile's K and V rows into one stage: row k at k * ROW_BYTES, its 16-byte chunk c at place c ^ (k & 7)
+template <typename T, int D>
+__device__ __forceinline__ void load_tile(const PagedArgs& a, const T* K, const T* V, long long off, uint32_t dst, int lane) {
+  constexpr int CPR = D * (int)sizeof(T) / 16, KPI = 32 / CPR, OPERAND = KT * D * (int)sizeof(T);
+  const int c = lane % CPR;
+#pragma unroll
+  for (int i = 0; i < KT / KPI; ++i) {
+    const int k = i * KPI + lane / CPR;
+    const long long o = __shfl_sync(0xffffffffu, off, k);
+    const bool valid = o >= 0;
+    const long long e = (valid ? o : 0) + c * (16 / (int)sizeof(T));
+    const uint32_t d = dst + k * (CPR * 16) + ((c ^ (k & 7)) << 4);
+    copy16(d, K + e, valid);
+    copy16(d + OPERAND, V + e, valid);
+  }
+}
+
+// ---- the two cores: one warp's running state of RT rows ---------------------------------------------------------
+template <typename T, int D, int NT> struct Core;
+
+template <int D, int NT>
+struct Core<__nv_bfloat16, D, NT> {
+  static constexpr int KS = D / 16, RB = D * 2;
+  static constexpr bool Q_IN_REGS = NT <= 2;
+  float m[NT][2], l[NT][2], o[KS][NT][4];     // lane (g, t) = (lane / 4, lane % 4): rows 8 n + 2 t, + 1; columns 16 i + g, + 8
+  uint32_t q[Q_IN_REGS ? NT : 1][Q_IN_REGS ? KS : 1][2];
+  uint32_t q_addr;
+
+  __device__ __forceinline__ void init(const __nv_bfloat16* Qs, float*, int lane) {
+    constexpr int P = (D + 8) * 2;
+    q_addr = smem_addr(Qs);
+    if constexpr (Q_IN_REGS) {
+      const uint32_t b = q_addr + (lane & 7) * P + (lane >> 3) * 16;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < KS; k += 2) {
+          uint32_t r[4];
+          ldmatrix4(r, b + n * 8 * P + k * 32);
+          q[n][k][0] = r[0]; q[n][k][1] = r[1]; q[n][k + 1][0] = r[2]; q[n][k + 1][1] = r[3];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+    }
+  }
+
+  __device__ __forceinline__ void tile(uint32_t ks, uint32_t mask, float scale, int lane) {
+    float s[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    {
+      const int key = lane & 15;
+      const uint32_t row = ks + key * RB;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t a[4];
+        ldmatrix4(a, row + (((2 * k + (lane >> 4)) ^ (key & 7)) << 4));
+        if constexpr (Q_IN_REGS) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16816(s[n], a, q[n][k][0], q[n][k][1]);
+        } else {
+          constexpr int P = (D + 8) * 2;
+#pragma unroll
+          for (int n = 0; n < NT; n += 2) {
+            uint32_t b[4];
+            ldmatrix4(b, q_addr + (n * 8 + (lane & 7) + (lane >> 4) * 8) * P + k * 32 + ((lane >> 3) & 1) * 16);
+            mma16816(s[n], a, b[0], b[1]);
+            mma16816(s[n + 1], a, b[2], b[3]);
+          }
+        }
+      }
+    }
+    const int g = lane >> 2;
+    const bool lo = (mask >> g) & 1u, hi = (mask >> (g + 8)) & 1u;
+    bool grow = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        s[n][c] = lo ? s[n][c] * scale : -INFINITY;
+        s[n][c + 2] = hi ? s[n][c + 2] * scale : -INFINITY;
+        grow |= fmaxf(s[n][c], s[n][c + 2]) > m[n][c] + LAZY;
+      }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x = fmaxf(s[n][c], s[n][c + 2]);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+          const float to = fmaxf(m[n][c], x), f = to == -INFINITY ? 1.f : exp2_approx(m[n][c] - to);
+          m[n][c] = to;
+          l[n][c] *= f;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) { o[i][n][c] *= f; o[i][n][c + 2] *= f; }
+        }
+    }
+    uint32_t b[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float base = m[n][c] == -INFINITY ? 0.f : m[n][c];
+        s[n][c] = exp2_approx(s[n][c] - base);
+        s[n][c + 2] = exp2_approx(s[n][c + 2] - base);
+        l[n][c] += s[n][c] + s[n][c + 2];
+      }
+      b[n][0] = transpose8(pack_bf16(s[n][0], s[n][1]));
+      b[n][1] = transpose8(pack_bf16(s[n][2], s[n][3]));
+    }
+    const int key = (lane & 7) + ((lane >> 4) << 3);
+    const uint32_t row = ks + KT * RB + key * RB;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      uint32_t a[4];
+      ldmatrix4_t(a, row + (((2 * i + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
+#pragma unroll
+      for (int n = 0; n < NT; ++n) mma16816(o[i][n], a, b[n][0], b[n][1]);
+    }
+  }
+
+  // (max, sum) and unnormalised O of the first nq rows
+  __device__ __forceinline__ void store(float* os, float2* ml, int nq, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
+        const int r = 8 * n + 2 * t + c;
+        if (r >= nq) continue;
+        if (g == 0) ml[r] = make_float2(m[n][c], l[n][c]);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          os[r * (D + 4) + 16 * i + g] = o[i][n][c];
+          os[r * (D + 4) + 16 * i + 8 + g] = o[i][n][c + 2];
+        }
+      }
+  }
+};
+
+template <int D>
+struct Core<float, D, 1> {
+  static constexpr int RB = D * 4, CV = D / 32;     // columns per lane
+  float m[8], l[8], o[8][CV];                       // l: of the lane's keys alone
+  const float* q;
+  float* p;
+
+  __device__ __forceinline__ void init(const float* Qs, float* Ps, int) {
+    q = Qs; p = Ps;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < CV; ++i) o[r][i] = 0.f;
+    }
+  }
+
+  __device__ __forceinline__ void tile(uint32_t ks, uint32_t mask, float scale, int lane) {
+    const int key = lane & 15, half = lane >> 4;
+    float s[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) s[r] = 0.f;
+    const uint32_t row = ks + key * RB;
+    const float* qh = q + half * (D / 2);
+#pragma unroll 4
+    for (int c = 0; c < D / 8; ++c) {
+      float4 k;
+      asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
+                   : "r"(row + (((half * (D / 8) + c) ^ (key & 7)) << 4)) : "memory");
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float4 x = *reinterpret_cast<const float4*>(qh + r * D + c * 4);
+        s[r] = fmaf(k.x, x.x, fmaf(k.y, x.y, fmaf(k.z, x.z, fmaf(k.w, x.w, s[r]))));
+      }
+    }
+    const bool live = (mask >> key) & 1u;
+    bool grow = false;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
+      s[r] = live ? s[r] * scale : -INFINITY;
+      grow |= s[r] > m[r] + LAZY;
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        float x = s[r];
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+        const float to = fmaxf(m[r], x), f = to == -INFINITY ? 1.f : exp2f(m[r] - to);
+        m[r] = to;
+        l[r] *= f;
+#pragma unroll
+        for (int i = 0; i < CV; ++i) o[r][i] *= f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      s[r] = exp2f(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+      l[r] += s[r];                                 // in both halves alike
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[(half * 4 + r) * KT + key] = half ? s[r + 4] : s[r];
+    __syncwarp();
+    const uint32_t v0 = ks + KT * RB;
+#pragma unroll
+    for (int k4 = 0; k4 < KT / 4; ++k4) {
+      float v[4][CV];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int kk = k4 * 4 + k, c = lane * CV / 4;
+        const uint32_t at = v0 + kk * RB + ((c ^ (kk & 7)) << 4) + (lane * CV % 4) * 4;
+        if constexpr (CV == 4)
+          asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[k][0]), "=f"(v[k][1]), "=f"(v[k][CV - 2]), "=f"(v[k][CV - 1])
+                       : "r"(at) : "memory");
+        else
+          asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[k][0]), "=f"(v[k][1]) : "r"(at) : "memory");
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float4 w = *reinterpret_cast<const float4*>(p + r * KT + k4 * 4);
+#pragma unroll
+        for (int i = 0; i < CV; ++i)
+          o[r][i] = fmaf(w.x, v[0][i], fmaf(w.y, v[1][i], fmaf(w.z, v[2][i], fmaf(w.w, v[3][i], o[r][i]))));
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(float* os, float2* ml, int nq, int lane) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+      if (r >= nq) continue;
+      if (lane == 0) ml[r] = make_float2(m[r], l[r]);
+#pragma unroll
+      for (int i = 0; i < CV; ++i) os[r * (D + 4) + lane * CV + i] = o[r][i];
+    }
+  }
+};
+
+// four neighbouring columns of one row into O
+__device__ __forceinline__ void put4(__nv_bfloat16* o, const float4& v) {
+  *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+__device__ __forceinline__ void put4(float* o, const float4& v) { *reinterpret_cast<float4*>(o) = v; }
+
+template <typename T, int D>
+struct Out {                             // where the stacked rows of a segment go
+  T* O;
+  float* lse;
+  int H, hpg, first, g, q0, max_rows;
+  __device__ __forceinline__ void row(int r, int& out_row, int& head) const {
+    out_row = first + (q0 + r) / hpg;
+    head = g * hpg + (q0 + r) % hpg;
+  }
+  // columns c .. c + 3 of row r, whose numerators' sum is l; -inf maximum: nothing attended
+  __device__ __forceinline__ void put(int r, int c, float4 v, float m, float l) const {
+    int i, h;
+    row(r, i, h);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    put4(O + ((long long)i * H + h) * D + c, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+    if (lse && c == 0) lse[(long long)h * max_rows + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+  }
+};
+
+__device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& y) {
+  return make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w));
+}
+// 2^(m - M), 0 for a part without keys
+__device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
+
+// Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
+// wts: shared, nq * n weights and nq (max, sum) pairs.
+template <typename T, int D, int RT>
+__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, float* wts,
+                                     float2* ml, const Out<T, D>& out, float* dst) {
+  // the first partial of a segment lies in its CTA's other slot
+  auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
+  for (int r = threadIdx.x; r < nq; r += PA_THREADS) {
+    float M = -INFINITY, L = 0.f;
+    for (int i = 0; i < n; ++i) M = fmaxf(M, __ldcg(at(i) + 2 * r));
+    for (int i = 0; i < n; ++i) {
+      const float w = part_weight(__ldcg(at(i) + 2 * r), M);
+      wts[r * n + i] = w;
+      L = fmaf(w, __ldcg(at(i) + 2 * r + 1), L);
+    }
+    ml[r] = make_float2(M, L);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < nq * (D / 4); e += PA_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i)
+      acc = axpy4(wts[r * n + i], __ldcg(reinterpret_cast<const float4*>(at(i) + 2 * RT + r * D + c)), acc);
+    if (dst) {
+      *reinterpret_cast<float4*>(dst + 2 * RT + r * D + c) = acc;
+      if (c == 0) *reinterpret_cast<float2*>(dst + 2 * r) = ml[r];
+    } else {
+      out.put(r, c, acc, ml[r].x, ml[r].y);
+    }
+  }
+}
+
+// true in every thread of the CTA that is the last of n to arrive
+__device__ __forceinline__ bool arrive_last(int32_t* counter, int n, int* flag) {
+  __threadfence();                       // this thread's partial is visible before the arrival
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = atomicAdd(counter, 1) == n - 1;
+    if (last) *counter = 0;              // ready for the next launch
+    *flag = last;
+  }
+  __syncthreads();
+  const bool last = *flag;
+  if (last) __threadfence();
+  return last;
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_kernel(const PagedArgs a) {
+  using C = Cfg<T, D, NT>;
+  constexpr int RT = C::RT;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ long long scan[PA_WARPS + 1];
+  __shared__ long long start_base;
+  __shared__ int start_seq, flag;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  T* Qs = reinterpret_cast<T*>(smem + C::OFF_Q);
+  float2* ML = reinterpret_cast<float2*>(smem + C::OFF_ML);              // [warp][RT]
+  uint32_t* masks = reinterpret_cast<uint32_t*>(smem + C::OFF_MASK) + w * C::STAGES;
+  const uint32_t ring = smem_addr(smem) + w * C::RING;
+
+  // ---- the split: total cost, this CTA's stretch and where it starts
+  const int per = (a.n_seqs + PA_THREADS - 1) / PA_THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) mine += seq_cost(seq_of<RT>(a, s), a.Hkv);
+  long long incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += y;
+  }
+  if (lane == 31) scan[w] = incl;
+  if (tid == 0) { start_seq = a.n_seqs; start_base = 0; }
+  __syncthreads();
+  long long total = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < PA_WARPS; ++i) {
+    if (i < w) before += scan[i];
+    total += scan[i];
+  }
+  if (total == 0) return;
+  const long long G = min((long long)gridDim.x, max(1ll, total / MIN_COST)), cta = blockIdx.x;
+  if (cta >= G) return;
+  const long long p0 = cta * total / G, p1 = (cta + 1) * total / G;
+  {
+    long long at = before + incl - mine;
+    if (p0 >= at && p0 < at + mine) {
+      int s = s0;
+      for (; s < s1; ++s) {
+        const long long c = seq_cost(seq_of<RT>(a, s), a.Hkv);
+        if (p0 < at + c) break;
+        at += c;
+      }
+      start_seq = s;
+      start_base = at;
+    }
+  }
+  __syncthreads();
+
+  int s = start_seq;
+  long long base = start_base, p = p0;
+  while (p < p1 && s < a.n_seqs) {
+    const Seq q = seq_of<RT>(a, s);
+    const int cost = seg_cost(q), tiles = cost - SEG_COST;
+    const long long whole = seq_cost(q, a.Hkv);
+    if (p >= base + whole) { base += whole; ++s; continue; }
+    const int seg = (int)((p - base) / cost);
+    const long long seg_at = base + (long long)seg * cost, first_tile = seg_at + SEG_COST;
+    const int g = seg / q.row_tiles, q0 = (seg - g * q.row_tiles) * RT;
+    const int nq = (int)min((long long)RT, (long long)q.rows * a.hpg - q0);
+    const Out<T, D> out{(T*)a.O, a.lse, a.H, a.hpg, q.first, g, q0, a.max_rows};
+    const int t_lo = (int)max(0ll, p - first_tile), t_hi = (int)min((long long)tiles, p1 - first_tile);
+    if (tiles == 0 && p == seg_at) {     // no keys: its first unit's CTA writes the row
+      for (int e = tid; e < nq * (D / 4); e += PA_THREADS)
+        out.put(e / (D / 4), e % (D / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f);
+    }
+    p = min(p1, seg_at + cost);
+    if (t_hi <= t_lo) continue;
+
+    // ---- the tiles t_lo + w, + 4, ...
+    const T* K = (const T*)a.K + (long long)g * a.st_head;
+    const T* V = (const T*)a.V + (long long)g * a.st_head;
+    int t_load = t_lo + w;
+    long long off = t_load < t_hi ? key_offset(a, s, q.len, t_load, lane) : -1;
+    auto fetch = [&](int stage) {        // requests tile t_load, looks up the next one
+      if (t_load < t_hi) {
+        const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
+        if (lane == 0) masks[stage] = mask;
+        load_tile<T, D>(a, K, V, off, ring + stage * C::STAGE, lane);
+        t_load += PA_WARPS;
+        off = t_load < t_hi ? key_offset(a, s, q.len, t_load, lane) : -1;
+      }
+      commit_group();
+    };
+#pragma unroll
+    for (int i = 0; i < C::STAGES - 1; ++i) fetch(i);
+    // query rows beyond nq are zeros: their results are dropped
+    for (int e = tid; e < RT * (D * (int)sizeof(T) / 16); e += PA_THREADS) {
+      constexpr int CPR = D * (int)sizeof(T) / 16, EPC = 16 / (int)sizeof(T);
+      const int r = e / CPR, c = e % CPR;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (r < nq) {
+        int i, h;
+        out.row(r, i, h);
+        x = *reinterpret_cast<const uint4*>((const T*)a.Q + (long long)i * a.q_row + (long long)h * a.q_head + c * EPC);
+      }
+      *reinterpret_cast<uint4*>(Qs + r * C::Q_PITCH + c * EPC) = x;
+    }
+    __syncthreads();
+    Core<T, D, NT> core;
+    core.init(Qs, reinterpret_cast<float*>(smem + C::OFF_P) + w * 8 * KT, lane);
+    int stage = 0;
+    for (int t = t_lo + w; t < t_hi; t += PA_WARPS) {
+      wait_group<C::STAGES - 2>();
+      __syncwarp();                      // every lane's copies are there, and nobody reads the stage refilled next
+      fetch(stage == 0 ? C::STAGES - 1 : stage - 1);
+      core.tile(ring + stage * C::STAGE, masks[stage], a.scale, lane);
+      stage = stage + 1 == C::STAGES ? 0 : stage + 1;
+    }
+    wait_group<0>();
+    __syncwarp();
+    core.store(reinterpret_cast<float*>(smem + w * C::RING), ML + w * RT, nq, lane);
+    __syncthreads();
+
+    // ---- the four warps' parts are joined: into O, or, for a piece of a segment, into the workspace
+    const bool piece = first_tile < p0 || first_tile + tiles > p1;
+    auto cta_of = [&](long long pos) { return (int)(((pos + 1) * G - 1) / total); };
+    const int c0 = piece ? cta_of(first_tile) : 0, parts = piece ? cta_of(first_tile + tiles - 1) - c0 + 1 : 1;
+    float* slot = a.part + ((long long)cta * 2 + (cta == c0 ? 1 : 0)) * C::PART;
+    for (int e = tid; e < nq * (D / 4); e += PA_THREADS) {
+      const int r = e / (D / 4), c = e % (D / 4) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int i = 0; i < PA_WARPS; ++i) M = fmaxf(M, ML[i * RT + r].x);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < PA_WARPS; ++i) {
+        const float f = part_weight(ML[i * RT + r].x, M);
+        L = fmaf(f, ML[i * RT + r].y, L);
+        acc = axpy4(f, *reinterpret_cast<const float4*>(smem + i * C::RING + (r * C::O_PITCH + c) * 4), acc);
+      }
+      if (piece) {
+        *reinterpret_cast<float4*>(slot + 2 * RT + r * D + c) = acc;
+        if (c == 0) *reinterpret_cast<float2*>(slot + 2 * r) = make_float2(M, L);
+      } else {
+        out.put(r, c, acc, M, L);
+      }
+    }
+    if (piece) {
+      constexpr long long STRIDE = 2ll * C::PART;
+      float* all = a.part + (long long)c0 * STRIDE;                      // slot 0 of CTA c0; its own piece is in slot 1
+      float* wts = reinterpret_cast<float*>(smem);                       // the rings are free until the next segment
+      float2* mls = reinterpret_cast<float2*>(smem + 64 * 1024);
+      if (parts <= 2 * JOIN) {
+        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, RT>(all, STRIDE, C::PART, parts, nq, wts, mls, out, nullptr);
+      } else {
+        const int groups = (parts + JOIN - 1) / JOIN, mygrp = ((int)cta - c0) / JOIN, lead = mygrp * JOIN;
+        float* from = all + lead * STRIDE;
+        const long long extra = lead == 0 ? C::PART : 0;
+        if (arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(JOIN, parts - lead), &flag)) {
+          join<T, D, RT>(from, STRIDE, extra, min(JOIN, parts - lead), nq, wts, mls, out, from + extra);
+          if (arrive_last(a.counters + 3 * c0 + 2, groups, &flag))
+            join<T, D, RT>(all, JOIN * STRIDE, C::PART, groups, nq, wts, mls, out, nullptr);
+        }
+      }
+    }
+    __syncthreads();                     // rings, queries and (max, sum) pairs are read out
+  }
+}
+
+template <typename T, int D, int NT>
+focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
+  using C = Cfg<T, D, NT>;
+  if (!ctx->ls.paged_attr_set[attr]) {
+    if (cudaFuncSetAttribute(paged_attn_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
+      return FOCUS_ERR_CUDA;
+    ctx->ls.paged_attr_set[attr] = true;
+  }
+  const int grid = C::CTAS * ctx->sm_count;
+  if (3 * grid > FOCUS_N_COUNTERS) return FOCUS_ERR_UNSUPPORTED;
+  WsAlloc ws(ctx);
+  a.part = ws.get<float>((size_t)grid * 2 * C::PART);
+  if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
+  paged_attn_kernel<T, D, NT><<<grid, PA_THREADS, C::SMEM, st>>>(a);
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
+
+}  // namespace
+
+extern "C" focus_status focus_paged_attn_workspace_bytes(focus_ctx* ctx, const focus_shape* shape, size_t* out_bytes) {
+  if (!ctx || !shape_ok_basic(shape) || !out_bytes) return FOCUS_ERR_INVALID_ARG;
+  *out_bytes = (size_t)2 * ctx->sm_count * 2 * 32 * (shape->head_dim + 2) * sizeof(float) + 256;
+  return FOCUS_OK;
+}
+
+extern "C" focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shape, const void* Q, const int32_t* row_start,
+                                         int32_t max_rows, const focus_paged_cache* cache, void* O, float* lse,
+                                         focus_stream stream) {
+  FOCUS_STAGE("focus_paged_attn");
+  if (!ctx || !Q || !O || !paged_cache_ok(shape, cache, row_start, max_rows)) return FOCUS_ERR_INVALID_ARG;
+  if (!all_aligned16(Q, O) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return FOCUS_ERR_INVALID_ARG;
+  if (shape->head_dim != 64 && shape->head_dim != 128) return FOCUS_ERR_UNSUPPORTED;
+  if (max_rows == 0 || cache->n_seqs == 0) return FOCUS_OK;
+  const DeviceGuard guard(ctx);
+  if (!guard.ok) return FOCUS_ERR_CUDA;
+  PagedArgs a;
+  a.Q = Q; a.q_row = shape->q_stride_row; a.q_head = shape->q_stride_head;
+  a.K = cache->K; a.V = cache->V;
+  a.st_page = cache->stride_page; a.st_tok = cache->stride_tok; a.st_head = cache->stride_head;
+  a.table = cache->page_table; a.kv_len = cache->kv_len; a.row_start = row_start;
+  a.page = cache->page_size; a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+  a.L = shape->L; a.max_rows = max_rows; a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.hpg = a.H / a.Hkv;
+  a.scale = shape_scale(shape) * LOG2E;
+  a.O = O; a.lse = lse; a.part = nullptr; a.counters = ctx->d_counters; a.status = ctx->d_status;
+  const bool d128 = shape->head_dim == 128;
+  if (shape->dtype == FOCUS_F32) {
+    ctx->last_attn_variant = 7;
+    return d128 ? launch<float, 128, 1>(ctx, a, 0, stream) : launch<float, 64, 1>(ctx, a, 1, stream);
+  }
+  ctx->last_attn_variant = 6;
+  // stacked rows per sequence, on average where they are packed: the fewest N tiles that hold them
+  const long long rows = ((long long)max_rows * a.hpg + cache->n_seqs - 1) / cache->n_seqs;
+  if (rows <= 8) return d128 ? launch<__nv_bfloat16, 128, 1>(ctx, a, 2, stream) : launch<__nv_bfloat16, 64, 1>(ctx, a, 3, stream);
+  if (rows <= 16) return d128 ? launch<__nv_bfloat16, 128, 2>(ctx, a, 4, stream) : launch<__nv_bfloat16, 64, 2>(ctx, a, 5, stream);
+  return d128 ? launch<__nv_bfloat16, 128, 4>(ctx, a, 6, stream) : launch<__nv_bfloat16, 64, 4>(ctx, a, 7, stream);
+}

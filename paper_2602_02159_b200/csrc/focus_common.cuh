@@ -27,7 +27,7 @@ struct focus_ctx {
   // launch state that belongs to the device (function attributes, occupancy answers): kept per context, since a
   // process may hold contexts on several devices.  Zero-initialised by focus_create.
   struct LaunchState {
-    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[4], quant_attr_set[4];
+    bool attn_attr_set, select_attr_set, topn_attr_set, sample_attr_set[4], quant_attr_set[4], paged_attr_set[16];
     int sink_attr_smem;
     int cluster_cap[9], cluster_cap_w[9], cluster_cap_k[9];   // co-resident clusters per cluster size, value + 1 (0 = not asked yet)
     int select_cluster;                        // 0 not tried, 1 works, 2 the cluster launch was refused once
@@ -110,6 +110,34 @@ static inline bool quant_cache_ok(const focus_shape* s, const focus_quant_cache*
   if ((s->kv_stride_tok | s->kv_stride_head) & 15) return false;
   return c->scale_stride_head == 0 || c->scale_stride_head >= s->L;
 }
+// Host checks of a paged cache (the shape's L bounds a sequence's length) and of the packed rows of a call on it.
+static inline bool paged_cache_ok(const focus_shape* s, const focus_paged_cache* c, const int32_t* row_start, int max_rows) {
+  if (!shape_ok_basic(s) || !c || !c->K || !c->V || !c->page_table || !c->kv_len) return false;
+  if (!all_aligned16(c->K, c->V)) return false;
+  if ((reinterpret_cast<uintptr_t>(c->page_table) | reinterpret_cast<uintptr_t>(c->kv_len) |
+       reinterpret_cast<uintptr_t>(row_start)) & 3u)
+    return false;
+  if (c->page_size < 1 || c->n_pages < 1 || c->n_seqs < 0 || c->max_pages < 1) return false;
+  if ((long long)c->max_pages * c->page_size < s->L) return false;
+  if (c->stride_page < s->head_dim || c->stride_tok < s->head_dim || c->stride_head < s->head_dim) return false;
+  if ((c->stride_page | c->stride_tok | c->stride_head) & 7) return false;
+  return max_rows >= 0 && (row_start || max_rows == c->n_seqs);
+}
+// The context's device is made current for a call and the caller's put back after it.
+struct DeviceGuard {
+  int prev;
+  bool ok;
+  explicit DeviceGuard(const focus_ctx* c) : prev(-1), ok(true) {
+    int now = -1;
+    if (cudaGetDevice(&now) != cudaSuccess) { ok = false; return; }
+    if (now == c->device) return;
+    ok = cudaSetDevice(c->device) == cudaSuccess;
+    prev = now;
+  }
+  ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+  DeviceGuard(const DeviceGuard&) = delete;
+  DeviceGuard& operator=(const DeviceGuard&) = delete;
+};
 static inline int shape_nb(const focus_shape* s) { return (s->M + s->kv_block - 1) / s->kv_block; }
 
 #ifdef __CUDACC__

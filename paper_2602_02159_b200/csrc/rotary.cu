@@ -1,0 +1,332 @@
+// Rotary positions and the write side of the paged cache:
+//   focus_rope_init, focus_rope_from_frequencies   the rotation plan (host)
+//   focus_rotate            rows turned by their positions
+//   focus_append_kv_paged   K and V rows to their pages, K (and Q) turned on the way
+//
+// A pair (x1, x2) at position p turns by p f: y1 = m (x1 cos - x2 sin), y2 = m (x2 cos + x1 sin).  The plan holds f / 2 pi as
+// a fraction of 2^64, so the phase is p * turn modulo 2^64: exact where p f in fp32 would be off by whole turns (p = 10^6,
+// f = 1: half a radian).  The upper bits, taken about the nearest quarter turn, go through sincospif, whose argument is then
+// within 1/4 and right to 2^-26; the quarter turns swap and negate.
+//
+// Both kernels are bound by HBM (3 flops per element moved twice).  One kernel does both: a block takes a few rows, makes
+// their tables of cosines and sines in shared memory (one sincospif per pair and row, shared by all heads) and walks over
+// (row, head, slot), a slot being two sixteen-byte vectors: the two halves' ends of the same pairs (HALVES) or neighbours
+// (PAIRS), so that either layout needs pairs slot * EPC .. + EPC - 1 and every access is a full sector.
+#include <math.h>
+
+#include "focus_common.cuh"
+
+namespace {
+
+constexpr int RT_THREADS = 256;
+constexpr int RT_ROWS = 4;               // rows per block at most
+
+struct TurnArgs {
+  focus_rope rope;                       // rot_dim 0: nothing turns
+  const void* src[3];                    // focus_rotate: X; append: Q, K_new, V_new
+  void* dst[3];                          // focus_rotate: Y; append: Q_out and the pools
+  long long src_row, src_head, dst_row, dst_head;
+  int heads[3], n_heads;                 // heads of each source, their sum
+  int head_dim, max_rows, rows_per_block, in_place;
+  float sign;                            // direction
+  // positions
+  int pos_base;
+  const int32_t* positions;
+  const int32_t* n_rows;
+  // append
+  const int32_t* row_start;
+  const int32_t* page_table;
+  const int32_t* kv_len;
+  long long st_page, st_tok, st_head;
+  int page_size, n_pages, n_seqs, max_pages, L;
+  int32_t* status;
+};
+
+struct RowInfo {
+  long long slot;                        // append: the row's place in the pools, without the head
+  int pos;                               // -1: the row is skipped
+};
+
+// the sequence whose rows contain row r, or -1
+__device__ __forceinline__ int owner_of(const TurnArgs& a, int r) {
+  if (!a.row_start) return r;
+  int lo = 0, hi = a.n_seqs;             // the last s with row_start[s] <= r
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.row_start[mid] <= r) lo = mid; else hi = mid - 1;
+  }
+  return lo < a.n_seqs && a.row_start[lo] <= r && r < a.row_start[lo + 1] ? lo : -1;
+}
+
+template <bool APPEND>
+__device__ __forceinline__ RowInfo row_info(const TurnArgs& a, int r) {
+  RowInfo i;
+  i.slot = 0; i.pos = -1;
+  if constexpr (!APPEND) {
+    if (a.positions) {
+      if (r >= min(max(*a.n_rows, 0), a.max_rows)) return i;
+      i.pos = a.positions[r];
+    } else {
+      i.pos = a.pos_base + r;
+    }
+    if (i.pos < 0) { i.pos = -1; set_status(a.status, FOCUS_ERR_INVALID_ARG); }
+  } else {
+    const int s = owner_of(a, r);
+    if (s < 0) return i;
+    long long at_pos;
+    if (a.positions) at_pos = a.positions[r];
+    else at_pos = (long long)a.kv_len[s] - (a.row_start ? a.row_start[s + 1] - r : 1);
+    const int pos = (int)at_pos;
+    if (at_pos < 0 || at_pos >= a.L) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return i; }
+    if (a.heads[1]) {                    // K and V are written
+      const int at = pos / a.page_size, page = a.page_table[(long long)s * a.max_pages + at];
+      if (page < 0 || page >= a.n_pages) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return i; }
+      i.slot = (long long)page * a.st_page + (long long)(pos - at * a.page_size) * a.st_tok;
+    }
+    i.pos = pos;
+  }
+  return i;
+}
+
+// m cos and m sin of position * turn
+__device__ __forceinline__ float2 turn_of(uint64_t turn, int pos, float magnitude, float sign) {
+  const uint32_t phase = (uint32_t)((turn * (uint64_t)(uint32_t)pos + 0x80000000ull) >> 32);
+  const uint32_t q = (phase + 0x20000000u) >> 30;                           // nearest quarter turn
+  float s, c;
+  sincospif((float)(int32_t)(phase - (q << 30)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
+  float x = (q & 1u) ? -s : c, y = (q & 1u) ? c : s;
+  if (q & 2u) { x = -x; y = -y; }
+  return make_float2(x * magnitude, y * magnitude * sign);
+}
+
+__device__ __forceinline__ void turn_pair(float& x1, float& x2, const float2& cs) {
+  const float y = fmaf(-x2, cs.y, x1 * cs.x);
+  x2 = fmaf(x1, cs.y, x2 * cs.x);
+  x1 = y;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& raw, float (&x)[16 / sizeof(T)]) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      x[i] = __uint_as_float(w[i]);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&x)[16 / sizeof(T)]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+      w[i] = __float_as_uint(x[i]);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T, bool APPEND>
+__global__ void __launch_bounds__(RT_THREADS) turn_rows_kernel(const __grid_constant__ TurnArgs a) {
+  constexpr int EPC = 16 / sizeof(T);
+  __shared__ float2 table[RT_ROWS][64];
+  __shared__ RowInfo info[RT_ROWS];
+  const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_per_block;
+  const int rows = min(a.rows_per_block, a.max_rows - r0);
+  const int pairs = a.rope.rot_dim >> 1;
+  if (tid < rows) info[tid] = row_info<APPEND>(a, r0 + tid);
+  __syncthreads();
+  for (int i = tid; i < rows * 64; i += RT_THREADS) {
+    const int p = i & 63, pos = info[i >> 6].pos;
+    if (p < pairs && pos >= 0) table[i >> 6][p] = turn_of(a.rope.turn[p], pos, a.rope.magnitude, a.sign);
+  }
+  __syncthreads();
+  const int slots = a.head_dim / (2 * EPC), turned = pairs / EPC;          // slots is a power of two
+  const int j = tid % slots, step = RT_THREADS / slots;
+  const bool halves = a.rope.layout == FOCUS_ROPE_HALVES, turns = j < turned;
+  const int c0 = halves && turns ? j * EPC : j * 2 * EPC, c1 = halves && turns ? pairs + j * EPC : c0 + EPC;
+  int row = 0, h = tid / slots;
+  while (true) {
+    while (h >= a.n_heads) { h -= a.n_heads; ++row; }
+    if (row >= rows) break;
+    const RowInfo ri = info[row];
+    int part = 0, hp = h;
+    if constexpr (APPEND) {
+      if (hp >= a.heads[0]) { hp -= a.heads[0]; part = 1; }
+      if (part == 1 && hp >= a.heads[1]) { hp -= a.heads[1]; part = 2; }
+    }
+    const bool turn = turns && part < 2;
+    if (ri.pos >= 0 && !(a.in_place && part == 0 && !turn)) {
+      const T* src = (const T*)a.src[part] + (long long)(r0 + row) * a.src_row + (long long)hp * a.src_head;
+      T* dst = (T*)a.dst[part];
+      if (APPEND && part) dst += ri.slot + (long long)hp * a.st_head;
+      else dst += (long long)(r0 + row) * a.dst_row + (long long)hp * a.dst_head;
+      uint4 lo = *reinterpret_cast<const uint4*>(src + c0), hi = *reinterpret_cast<const uint4*>(src + c1);
+      if (turn) {
+        float u[EPC], v[EPC];
+        unpack<T>(lo, u);
+        unpack<T>(hi, v);
+        const float2* cs = &table[row][j * EPC];
+        if (halves) {
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) turn_pair(u[e], v[e], cs[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPC / 2; ++e) {
+            turn_pair(u[2 * e], u[2 * e + 1], cs[e]);
+            turn_pair(v[2 * e], v[2 * e + 1], cs[EPC / 2 + e]);
+          }
+        }
+        lo = pack<T>(u);
+        hi = pack<T>(v);
+      }
+      *reinterpret_cast<uint4*>(dst + c0) = lo;
+      *reinterpret_cast<uint4*>(dst + c1) = hi;
+    }
+    h += step;
+  }
+  publish_outputs();
+}
+
+focus_status launch_turn(focus_ctx* ctx, TurnArgs& a, int dtype, bool append, cudaStream_t st) {
+  const DeviceGuard guard(ctx);
+  if (!guard.ok) return FOCUS_ERR_CUDA;
+  a.status = ctx->d_status;
+  // several rows per block once every SM has eight blocks of them
+  a.rows_per_block = a.max_rows >= 8ll * ctx->sm_count * RT_ROWS ? RT_ROWS : 1;
+  const int grid = (a.max_rows + a.rows_per_block - 1) / a.rows_per_block;
+  if (dtype == FOCUS_BF16) {
+    if (append) turn_rows_kernel<__nv_bfloat16, true><<<grid, RT_THREADS, 0, st>>>(a);
+    else turn_rows_kernel<__nv_bfloat16, false><<<grid, RT_THREADS, 0, st>>>(a);
+  } else {
+    if (append) turn_rows_kernel<float, true><<<grid, RT_THREADS, 0, st>>>(a);
+    else turn_rows_kernel<float, false><<<grid, RT_THREADS, 0, st>>>(a);
+  }
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
+
+bool rope_ok(const focus_rope* r) {
+  return r->rot_dim >= 16 && r->rot_dim <= 128 && r->rot_dim % 16 == 0 &&
+         (r->layout == FOCUS_ROPE_HALVES || r->layout == FOCUS_ROPE_PAIRS) && isfinite(r->magnitude);
+}
+
+bool row_strides_ok(long long row, long long head, int head_dim) {
+  return row >= head_dim && head >= head_dim && ((row | head) & 7) == 0;
+}
+
+}  // namespace
+
+extern "C" focus_status focus_rope_from_frequencies(focus_rope* rope, int32_t rot_dim, int32_t layout,
+                                                    const double* radians_per_position, double magnitude) {
+  if (!rope || !radians_per_position || !isfinite(magnitude)) return FOCUS_ERR_INVALID_ARG;
+  focus_rope r = {};
+  r.rot_dim = rot_dim; r.layout = layout; r.magnitude = (float)magnitude;
+  if (!rope_ok(&r)) return FOCUS_ERR_INVALID_ARG;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = radians_per_position[i];
+    if (!(f >= 0.0) || !isfinite(f)) return FOCUS_ERR_INVALID_ARG;
+    // the fraction of a turn, in the 64-bit significand of long double
+    long double t = (long double)f / 6.283185307179586476925286766559005768L;
+    t = ldexpl(t - floorl(t), 64);
+    r.turn[i] = t >= 18446744073709551615.0L ? ~0ull : (uint64_t)roundl(t);
+  }
+  *rope = r;
+  return FOCUS_OK;
+}
+
+extern "C" focus_status focus_rope_init(focus_rope* rope, int32_t rot_dim, int32_t layout, double base, int32_t scaling,
+                                        double factor, double low, double high, int32_t trained_len) {
+  if (!rope || rot_dim < 16 || rot_dim > 128 || rot_dim % 16) return FOCUS_ERR_INVALID_ARG;
+  if (!(base > 1.0) || !isfinite(base) || scaling < FOCUS_ROPE_PLAIN || scaling > FOCUS_ROPE_YARN) return FOCUS_ERR_INVALID_ARG;
+  if (scaling != FOCUS_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return FOCUS_ERR_INVALID_ARG;
+  const bool banded = scaling == FOCUS_ROPE_BANDS || scaling == FOCUS_ROPE_YARN;
+  if (banded && (!(low > 0.0) || !(high > low) || !isfinite(high) || trained_len <= 0)) return FOCUS_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586, d = rot_dim;
+  if (scaling == FOCUS_ROPE_NTK) base *= pow(factor, d / (d - 2.0));
+  if (!isfinite(base)) return FOCUS_ERR_INVALID_ARG;
+  double magnitude = 1.0, first = 0.0, last = 0.0;
+  if (scaling == FOCUS_ROPE_YARN) {
+    // the pair that makes t turns within the trained length: base^(-2 i / d) trained / 2 pi = t
+    first = fmax(floor(d * log(trained_len / (high * two_pi)) / (2.0 * log(base))), 0.0);
+    last = fmin(ceil(d * log(trained_len / (low * two_pi)) / (2.0 * log(base))), d - 1.0);
+    magnitude = 0.1 * log(factor) + 1.0;
+  }
+  double f[64];
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    f[i] = pow(base, -2.0 * i / d);
+    double keep = scaling == FOCUS_ROPE_LINEAR ? 0.0 : 1.0;
+    if (scaling == FOCUS_ROPE_BANDS) keep = (trained_len * f[i] / two_pi - low) / (high - low);
+    if (scaling == FOCUS_ROPE_YARN) keep = 1.0 - (i - first) / fmax(last - first, 0.001);
+    keep = fmin(fmax(keep, 0.0), 1.0);
+    if (keep < 1.0) f[i] = f[i] * keep + f[i] / factor * (1.0 - keep);
+  }
+  return focus_rope_from_frequencies(rope, rot_dim, layout, f, magnitude);
+}
+
+extern "C" focus_status focus_rotate(focus_ctx* ctx, const focus_rope* rope, int32_t direction, const void* X, void* Y,
+                                     int32_t dtype, int32_t n_heads, int32_t head_dim, int64_t x_stride_row,
+                                     int64_t x_stride_head, int64_t y_stride_row, int64_t y_stride_head, int32_t pos_base,
+                                     const int32_t* positions, const int32_t* n_rows, int32_t max_rows,
+                                     focus_stream stream) {
+  FOCUS_STAGE("focus_rotate");
+  if (!ctx || !rope || !X || !Y || !rope_ok(rope)) return FOCUS_ERR_INVALID_ARG;
+  if (direction != 1 && direction != -1) return FOCUS_ERR_INVALID_ARG;
+  if (dtype != FOCUS_F32 && dtype != FOCUS_BF16) return FOCUS_ERR_INVALID_ARG;
+  if (n_heads <= 0 || max_rows < 0 || !all_aligned16(X, Y)) return FOCUS_ERR_INVALID_ARG;
+  if (!row_strides_ok(x_stride_row, x_stride_head, head_dim) || !row_strides_ok(y_stride_row, y_stride_head, head_dim))
+    return FOCUS_ERR_INVALID_ARG;
+  if (X == Y && (x_stride_row != y_stride_row || x_stride_head != y_stride_head)) return FOCUS_ERR_INVALID_ARG;
+  if ((positions == nullptr) != (n_rows == nullptr)) return FOCUS_ERR_INVALID_ARG;
+  if (!positions && (pos_base < 0 || max_rows > 0x7fffffff - pos_base)) return FOCUS_ERR_INVALID_ARG;
+  if ((head_dim != 64 && head_dim != 128) || rope->rot_dim > head_dim) return FOCUS_ERR_UNSUPPORTED;
+  if (max_rows == 0) return FOCUS_OK;
+  TurnArgs a = {};
+  a.rope = *rope;
+  a.src[0] = X; a.dst[0] = Y;
+  a.src_row = x_stride_row; a.src_head = x_stride_head; a.dst_row = y_stride_row; a.dst_head = y_stride_head;
+  a.heads[0] = a.n_heads = n_heads;
+  a.head_dim = head_dim; a.max_rows = max_rows; a.in_place = X == Y; a.sign = (float)direction;
+  a.pos_base = pos_base; a.positions = positions; a.n_rows = n_rows;
+  return launch_turn(ctx, a, dtype, false, stream);
+}
+
+extern "C" focus_status focus_append_kv_paged(focus_ctx* ctx, const focus_shape* shape, const focus_rope* rope, const void* Q,
+                                              const void* K_new, const void* V_new, int64_t new_stride_row,
+                                              int64_t new_stride_head, const int32_t* row_start, const int32_t* positions,
+                                              int32_t max_rows, const focus_paged_cache* cache, void* Q_out,
+                                              focus_stream stream) {
+  FOCUS_STAGE("focus_append_kv_paged");
+  if (!ctx || !paged_cache_ok(shape, cache, row_start, max_rows)) return FOCUS_ERR_INVALID_ARG;
+  if ((K_new == nullptr) != (V_new == nullptr) || (Q == nullptr) != (Q_out == nullptr) || (!Q && !K_new))
+    return FOCUS_ERR_INVALID_ARG;
+  if (!all_aligned16(Q, K_new, V_new, Q_out) || !row_strides_ok(new_stride_row, new_stride_head, shape->head_dim))
+    return FOCUS_ERR_INVALID_ARG;
+  if (Q && Q == Q_out && (new_stride_row != shape->q_stride_row || new_stride_head != shape->q_stride_head))
+    return FOCUS_ERR_INVALID_ARG;
+  if (rope && !rope_ok(rope)) return FOCUS_ERR_INVALID_ARG;
+  if ((shape->head_dim != 64 && shape->head_dim != 128) || (rope && rope->rot_dim > shape->head_dim))
+    return FOCUS_ERR_UNSUPPORTED;
+  if (max_rows == 0) return FOCUS_OK;
+  TurnArgs a = {};
+  if (rope) a.rope = *rope;
+  a.src[0] = Q; a.src[1] = K_new; a.src[2] = V_new;
+  a.dst[0] = Q_out; a.dst[1] = cache->K; a.dst[2] = cache->V;
+  a.src_row = new_stride_row; a.src_head = new_stride_head; a.dst_row = shape->q_stride_row; a.dst_head = shape->q_stride_head;
+  a.heads[0] = Q ? shape->n_q_heads : 0;
+  a.heads[1] = a.heads[2] = K_new ? shape->n_kv_heads : 0;
+  a.n_heads = a.heads[0] + 2 * a.heads[1];
+  a.head_dim = shape->head_dim; a.max_rows = max_rows; a.in_place = Q && Q == Q_out; a.sign = 1.f;
+  a.positions = positions; a.row_start = row_start; a.page_table = cache->page_table; a.kv_len = cache->kv_len;
+  a.st_page = cache->stride_page; a.st_tok = cache->stride_tok; a.st_head = cache->stride_head;
+  a.page_size = cache->page_size; a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+  a.L = shape->L;
+  return launch_turn(ctx, a, shape->dtype, true, stream);
+}
