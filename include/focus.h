@@ -469,6 +469,27 @@ focus_status focus_commit_step(focus_ctx* ctx, const float* conf_new, const int3
                                int32_t blk_lo, int32_t blk_hi, int32_t n_unmask, float* conf, uint8_t* masked,
                                int32_t* x, int32_t* unmasked_idx, int32_t* n_unmasked, focus_stream stream);
 
+/* Scores instead of decisions, next to focus_confidence and focus_sample: for each listed position, with x its logits row
+ * and p = softmax(x / temperature),
+ *   logprob    ln p of the given token (natural logarithm, as all here)
+ *   rank       how many tokens come before it in descending order of x (ties: lower index first)
+ *   entropy    -sum p ln p
+ *   top_token, top_logprob   the n_top first tokens of that order and their ln p
+ * NaN logits count as -inf, whose ln p is -inf; +inf logits share all probability.
+ *   given      int32[max_rows]: given[r] belongs to row r; -1: none (logprob 0, rank -1), other values outside [0, vocab)
+ *              likewise, and reported through the status word.  NULL together with logprob: tops and entropy only
+ *   logprob, entropy float[max_rows], rank int32[max_rows]; rank and entropy may be NULL
+ *   n_top      0 .. 32; top_token int32[max_rows * n_top], top_logprob float[max_rows * n_top], NULL when it is 0.
+ *              Beyond the vocabulary: -1 and -inf
+ * logits, rows and layout as for focus_confidence.  Rows beyond n_rows get logprob 0, rank -1, entropy 0, top_token -1,
+ * top_logprob 0; so does a row without a finite or +inf logit, and a row whose position is out of range, which is reported.
+ * Requires temperature > 0 (finite).  logprob and entropy are off by fp32 rounding of the weights (2^-21 of Z) and of the
+ * result.  One launch, no workspace. */
+focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits, int32_t dtype, int64_t row_stride, int32_t vocab,
+                                  int32_t pos_base, int32_t n_pos, const int32_t* rows, const int32_t* n_rows,
+                                  int32_t max_rows, float temperature, const int32_t* given, float* logprob, int32_t* rank,
+                                  float* entropy, int32_t n_top, int32_t* top_token, float* top_logprob, focus_stream stream);
+
 /* ---- batched decoding over a paged cache (no counterpart in the paper: its batch is 1) ---------------------- */
 
 /* Fills a rotation plan (host only, no device work).  low, high and trained_len are read by BANDS and YARN only, factor by

@@ -89,6 +89,7 @@ _SIGS = {
     "focus_sparse_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _I, _P, _I, _P, _P, _P, _I, _P, _P, _P]),
     "focus_dense_attn_quantized": (_I, [_P, _SH, _P, _I, _I, _P, _P, _I, _QC, _P, _P, _P]),
     "focus_sample": (_I, [_P, _P, _I, C.c_int64, _I, _I, _I, _P, _P, _I, _F, _I, _F, _F, _P, _P, _P, _P, _P, _P]),
+    "focus_token_logprobs": (_I, [_P, _P, _I, _L, _I, _I, _I, _P, _P, _I, _F, _P, _P, _P, _P, _I, _P, _P, _P]),
     "focus_rope_init": (_I, [_RP, _I, _I, _D, _I, _D, _D, _D, _I]),
     "focus_rope_from_frequencies": (_I, [_RP, _I, _I, C.POINTER(_D), _D]),
     "focus_rotate": (_I, [_P, _RP, _I, _P, _P, _I, _I, _I, _L, _L, _L, _L, _I, _P, _P, _I, _P]),
@@ -412,3 +413,11 @@ def focus_paged_attn_workspace_bytes(ctx, shape: focus_shape) -> int:
 def focus_paged_attn(ctx, shape, Q, row_start, max_rows, cache, O, lse=None, stream=None):
     _check(ctx._lib.focus_paged_attn(ctx.handle, C.byref(shape), _ptr(Q), _ptr(row_start), max_rows, C.byref(cache), _ptr(O),
                                      _ptr(lse), _stream(stream)), "focus_paged_attn")
+
+
+def focus_token_logprobs(ctx, logits, dtype, row_stride, vocab, pos_base, n_pos, rows, n_rows, max_rows, temperature, given,
+                         logprob, rank=None, entropy=None, n_top=0, top_token=None, top_logprob=None, stream=None):
+    _check(ctx._lib.focus_token_logprobs(ctx.handle, _ptr(logits), dtype, row_stride, vocab, pos_base, n_pos, _ptr(rows),
+                                         _ptr(n_rows), max_rows, temperature, _ptr(given), _ptr(logprob), _ptr(rank),
+                                         _ptr(entropy), n_top, _ptr(top_token), _ptr(top_logprob), _stream(stream)),
+           "focus_token_logprobs")

@@ -1,0 +1,480 @@
+// focus_token_logprobs: for each listed position the log probability and rank of a given token, the entropy of the row's
+// distribution and its most probable tokens, in one pass over the logits and one launch.
+//
+// With z_v = (x_v - m) / T, m = max x:  log p_t = z_t - ln Z,  Z = sum e^z;  H = ln Z - (sum e^z z) / Z.  A thread keeps a
+// running maximum with its two sums, in base 2: exponents are (x - m) k, k = log2 e / T (one fma of x k and a rounded m k
+// would save an instruction, and overflow for logits near the end of the range).  Threads' sums are fp32 over a few hundred
+// logits, joined in fp32 per warp and in fp64 beyond.
+//
+// Top tokens.  A thread remembers its maximum and the vector where it first met it.  Of 64 groups of threads the n-th
+// largest such pair is a lower bound of the n-th largest logit that few more logits reach (20 of 64: 24 on average); only the
+// threads whose maximum reaches it have any, and their warp looks their vectors through again, a lane per vector.  The list
+// is ordered by counting, per logit, those ahead of it.  A list that overflows (more than LP_LIST logits above the bound,
+// which takes logits that repeat with the threads' stride) is replaced by n searches for the next largest.
+//
+// A row belongs to one CTA where there are many, else to a cluster of up to eight, whose first CTA joins what the others
+// put into its shared memory.  What bounds it: HBM (512 rows of 126464 bf16 logits: 20 us) with the exponentials close behind
+// (16 per clock and SM: 14 us).
+#include <math.h>
+
+#include "focus_common.cuh"
+
+namespace {
+
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
+constexpr int LP_GROUPS = 64, LP_PER_GROUP = LP_THREADS / LP_GROUPS;
+constexpr int LP_MAX_CLUSTER = 8, LP_MAX_TOP = 32;
+constexpr int LP_LIST = 1024;
+constexpr int LP_UNROLL = 4;             // vectors in flight per thread
+constexpr float LP_FLOOR = -1.0e4f;      // exponents are clamped here: weight 0, and 0 times it is 0 (NaN logits end here too)
+
+struct LpParams {
+  const void* logits;
+  long long row_stride;
+  int vocab, pos_base, n_pos, max_rows, n_top;
+  const int32_t* rows;
+  const int32_t* n_rows;
+  float temperature, k;                  // k = log2 e / temperature
+  const int32_t* given;
+  float* logprob;
+  int32_t* rank;
+  float* entropy;
+  int32_t* top_token;
+  float* top_logprob;
+  int32_t* status;
+};
+
+struct Sums {                            // weights 2^((x - m) k): z their sum, s the sum of weight times exponent
+  float m, z, s;
+};
+struct Part {                            // of one warp, in the leader's shared memory
+  float m, z, s;
+  int n_inf, ahead;
+};
+
+struct LpShared {
+  Part part[LP_MAX_CLUSTER * LP_WARPS];
+  unsigned long long top[LP_MAX_CLUSTER * LP_MAX_TOP];
+  unsigned long long group[LP_GROUPS], bound, best[LP_WARPS];
+  unsigned long long list[LP_LIST];
+  int list_n;
+  double ln_z;
+  float m;
+};
+
+// Order of tokens: larger logit first, then the lower index.  Position: index of the token, or of its vector.
+__device__ __forceinline__ unsigned long long order_key(float x, uint32_t position) {
+  const uint32_t k = x != x ? float_key(-INFINITY) : float_key(x);
+  return (unsigned long long)k << 32 | (0xffffffffu - position);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// sums of two shares, relative to the larger maximum (with an infinite one they mean nothing: such rows go by the number of
+// infinite logits)
+__device__ __forceinline__ void join(Sums& a, const Sums& o, float k) {
+  if (!(o.m > -INFINITY)) return;
+  if (!(a.m > -INFINITY)) { a = o; return; }
+  const float m = fmaxf(a.m, o.m), da = fmaxf((a.m - m) * k, LP_FLOOR), db = fmaxf((o.m - m) * k, LP_FLOOR);
+  const float fa = ex2(da), fb = ex2(db);
+  a.s = fa * fmaf(a.z, da, a.s) + fb * fmaf(o.z, db, o.s);
+  a.z = fa * a.z + fb * o.z;
+  a.m = m;
+}
+
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int EPC = 8;
+  __device__ static void load(const __nv_bfloat16* row, int v, int vocab, uint4& r) {
+    if (v * EPC + EPC <= vocab) { r = __ldg(reinterpret_cast<const uint4*>(row) + v); return; }
+    uint32_t w[4] = {0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};             // -inf beyond the row's end
+#pragma unroll
+    for (int e = 0; e < EPC; ++e)
+      if (v * EPC + e < vocab) {
+        const uint32_t b = __bfloat16_as_ushort(row[v * EPC + e]);
+        w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | b << 16 : (w[e / 2] & 0xffff0000u) | b;
+      }
+    r = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ static void floats(const uint4& r, float (&x)[EPC]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  __device__ static float largest(const uint4& r) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+    const __nv_bfloat162 a = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return __bfloat162float(__hmax(__low2bfloat16(a), __high2bfloat16(a)));
+  }
+  // how many elements are above t, or (equal) not below it
+  __device__ static int ahead(const uint4& r, float t, bool equal) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+    const __nv_bfloat162 t2 = __float2bfloat162_rn(t);
+    __nv_bfloat162 n = __float2bfloat162_rn(0.f);                                     // counts to 4 are exact
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n = __hadd2(n, equal ? __hge2(h[i], t2) : __hgt2(h[i], t2));
+    return (int)(__low2float(n) + __high2float(n));
+  }
+};
+template <> struct Vec<float> {
+  static constexpr int EPC = 4;
+  __device__ static void load(const float* row, int v, int vocab, uint4& r) {
+    if (v * EPC + EPC <= vocab) { r = __ldg(reinterpret_cast<const uint4*>(row) + v); return; }
+    float x[EPC];
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) x[e] = v * EPC + e < vocab ? row[v * EPC + e] : -INFINITY;
+    r = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  __device__ static void floats(const uint4& r, float (&x)[EPC]) {
+    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+  }
+  __device__ static float largest(const uint4& r) {
+    return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+  }
+  __device__ static int ahead(const uint4& r, float t, bool equal) {
+    float x[EPC];
+    floats(r, x);
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) n += equal ? x[e] >= t : x[e] > t;
+    return n;
+  }
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t leader_addr(const void* p) {                      // the same variable in CTA 0 of the cluster
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)));
+  return r;
+}
+__device__ __forceinline__ void put_far(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void put_far(uint32_t addr, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+// grid: clusters of `cl` CTAs, one per row
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpParams p, const int cl) {
+  constexpr int EPC = Vec<T>::EPC;
+  __shared__ LpShared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int q = cl > 1 ? (int)cluster_rank() : 0, r = blockIdx.x / cl;
+  if (cl > 1) cluster_arrive();          // a CTA's shared memory may be written once it has started
+  const int n = p.rows ? min(max(*p.n_rows, 0), p.max_rows) : p.max_rows;
+  const int pos = r < n ? (p.rows ? p.rows[r] : p.pos_base + r) : -1;
+  const bool live = r < n && pos >= p.pos_base && pos - p.pos_base < p.n_pos;         // alike in the cluster
+  const int t = live && p.given ? p.given[r] : -1;
+  const bool scored = t >= 0 && t < p.vocab;
+  if (q == 0 && tid == 0 && ((r < n && !live) || (live && !scored && t != -1))) set_status(p.status, FOCUS_ERR_INVALID_ARG);
+  if (tid == 0) sh.list_n = 0;
+
+  // ---- the pass: vectors v0 + tid, + LP_THREADS, ... of this CTA's slice
+  Sums a = {-INFINITY, 0.f, 0.f};
+  int n_inf = 0, ahead = 0, first = 0;
+  const T* row = (const T*)p.logits + (long long)(live ? pos - p.pos_base : 0) * p.row_stride;
+  const int vectors = live ? (p.vocab + EPC - 1) / EPC : 0, per = (vectors + cl - 1) / cl;
+  const int v0 = min(q * per, vectors), v1 = min(v0 + per, vectors);
+  float xt = scored ? load_as_float(row + t) : 0.f;
+  if (xt != xt) xt = -INFINITY;
+  const bool low = xt == -INFINITY;      // then every token before t is ahead of it: added at the end
+  const int tv = t / EPC;
+  first = v0 + tid;
+  for (int v = v0 + tid; v < v1; v += LP_THREADS * LP_UNROLL) {
+    uint4 raw[LP_UNROLL];
+    float big[LP_UNROLL];
+#pragma unroll
+    for (int u = 0; u < LP_UNROLL; ++u) {
+      const int at = v + u * LP_THREADS;
+      if (at < v1) Vec<T>::load(row, at, p.vocab, raw[u]);
+      else raw[u] = EPC == 8 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                             : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < LP_UNROLL; ++u) {
+      big[u] = Vec<T>::largest(raw[u]);
+      top = fmaxf(top, big[u]);
+    }
+    if (top > a.m) {
+      int u0 = LP_UNROLL - 1;
+#pragma unroll
+      for (int u = LP_UNROLL - 2; u >= 0; --u) u0 = big[u] == top ? u : u0;
+      first = v + u0 * LP_THREADS;
+      const float d = fmaxf((a.m - top) * p.k, LP_FLOOR), f = ex2(d);     // 0 for the first maximum
+      a.s = f * fmaf(a.z, d, a.s);
+      a.z *= f;
+      a.m = top;
+    }
+    if (scored) {
+#pragma unroll
+      for (int u = 0; u < LP_UNROLL; ++u) {
+        const int at = v + u * LP_THREADS;
+        if (at != tv) {
+          if (!(low && at < tv)) ahead += Vec<T>::ahead(raw[u], xt, at < tv);
+        } else {
+          float x[EPC];
+          Vec<T>::floats(raw[u], x);
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) ahead += x[e] > xt ? !(low && at * EPC + e < t) : (x[e] == xt && at * EPC + e < t && !low);
+        }
+      }
+    }
+    if (top == INFINITY) {
+#pragma unroll
+      for (int u = 0; u < LP_UNROLL; ++u) {
+        float x[EPC];
+        Vec<T>::floats(raw[u], x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) n_inf += x[e] == INFINITY;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < LP_UNROLL; ++u) {
+      float x[EPC];
+      Vec<T>::floats(raw[u], x);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        const float d = fmaxf((x[e] - a.m) * p.k, LP_FLOOR), w = ex2(d);
+        a.z += w;
+        a.s = fmaf(w, d, a.s);
+      }
+    }
+  }
+
+  // ---- sums: per warp, into the leader
+  {
+    Sums w = a;
+    int ni = n_inf, ah = ahead;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      Sums o;
+      o.m = __shfl_xor_sync(0xffffffffu, w.m, d);
+      o.z = __shfl_xor_sync(0xffffffffu, w.z, d);
+      o.s = __shfl_xor_sync(0xffffffffu, w.s, d);
+      join(w, o, p.k);
+    }
+    ni = __reduce_add_sync(0xffffffffu, ni);
+    ah = __reduce_add_sync(0xffffffffu, ah);
+    if (cl > 1) cluster_wait();
+    if (lane == 0) {
+      const Part part = {w.m, w.z, w.s, ni, ah};
+      if (cl == 1) {
+        sh.part[warp] = part;
+      } else {
+        const uint32_t at = leader_addr(&sh.part[q * LP_WARPS + warp]);
+        put_far(at, __float_as_uint(w.m)); put_far(at + 4, __float_as_uint(w.z)); put_far(at + 8, __float_as_uint(w.s));
+        put_far(at + 12, (uint32_t)ni); put_far(at + 16, (uint32_t)ah);
+      }
+    }
+  }
+
+  // ---- top tokens of the slice
+  if (p.n_top > 0) {
+    const unsigned long long mine = first < v1 ? order_key(a.m, (uint32_t)first) : 0ull;
+    unsigned long long g = mine;
+#pragma unroll
+    for (int d = 1; d < LP_PER_GROUP; d <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, d));
+    if (tid % LP_PER_GROUP == 0) sh.group[tid / LP_PER_GROUP] = g;
+    if (tid == 0) sh.bound = 0ull;
+    __syncthreads();
+    if (tid < LP_GROUPS) {
+      const unsigned long long own = sh.group[tid];
+      int before = 0;
+#pragma unroll 16
+      for (int i = 0; i < LP_GROUPS; ++i) before += sh.group[i] > own;
+      if (own != 0ull && before == p.n_top - 1) sh.bound = own;                       // keys are distinct
+    }
+    __syncthreads();
+    const unsigned long long bound = sh.bound;                                        // 0: fewer groups than that, all is listed
+    const int trips = (v1 - v0 + LP_THREADS - 1) / LP_THREADS;
+    uint32_t owners = __ballot_sync(0xffffffffu, mine != 0ull && mine >= bound);
+    while (owners) {                                                                  // a lane per vector of the owner's
+      const int o = __ffs(owners) - 1;
+      owners &= owners - 1;
+      for (int i = lane; i < trips; i += 32) {
+        const int at = v0 + warp * 32 + o + i * LP_THREADS;
+        if (at >= v1) continue;
+        uint4 raw;
+        float x[EPC];
+        Vec<T>::load(row, at, p.vocab, raw);
+        Vec<T>::floats(raw, x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          if (at * EPC + e < p.vocab && order_key(x[e], (uint32_t)at) >= bound) {
+            const int slot = atomicAdd(&sh.list_n, 1);
+            if (slot < LP_LIST) sh.list[slot] = order_key(x[e], (uint32_t)(at * EPC + e));
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const int listed = sh.list_n;
+    const uint32_t to = cl > 1 ? leader_addr(&sh.top[q * LP_MAX_TOP]) : 0u;
+    auto put = [&](int i, unsigned long long key) {
+      if (cl > 1) put_far(to + i * 8, key); else sh.top[i] = key;
+    };
+    if (listed <= LP_LIST) {
+      for (int i = tid; i < listed; i += LP_THREADS) {
+        const unsigned long long own = sh.list[i];
+        int before = 0;
+        for (int j = 0; j < listed; ++j) before += sh.list[j] > own;
+        if (before < p.n_top) put(before, own);
+      }
+      for (int i = listed + tid; i < p.n_top; i += LP_THREADS) put(i, 0ull);
+    } else {
+      unsigned long long last = ~0ull;
+      for (int i = 0; i < p.n_top; ++i) {
+        unsigned long long best = 0ull;
+        for (int v = v0 + tid; v < v1; v += LP_THREADS) {
+          uint4 raw;
+          float x[EPC];
+          Vec<T>::load(row, v, p.vocab, raw);
+          Vec<T>::floats(raw, x);
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) {
+            const unsigned long long key = v * EPC + e < p.vocab ? order_key(x[e], (uint32_t)(v * EPC + e)) : 0ull;
+            if (key < last && key > best) best = key;
+          }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
+        __syncthreads();
+        if (lane == 0) sh.best[warp] = best;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < LP_WARPS; ++w) best = max(best, sh.best[w]);
+        if (tid == 0) put(i, best);
+        last = best;
+      }
+    }
+  }
+  if (cl > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (q != 0) return;
+  } else {
+    __syncthreads();
+  }
+
+  // ---- the leader joins the warps' sums and orders the CTAs' tokens
+  if (warp == 0) {
+    const int parts = cl * LP_WARPS;
+    float m = -INFINITY;
+    int ni = 0, ah = 0;
+    for (int i = lane; i < parts; i += 32) {
+      const Part& x = sh.part[i];
+      ni += x.n_inf;
+      ah += x.ahead;
+      m = fmaxf(m, x.m);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    ni = __reduce_add_sync(0xffffffffu, ni);
+    ah = __reduce_add_sync(0xffffffffu, ah);
+    double z = 0.0, s = 0.0;
+    if (ni == 0) {
+      for (int i = lane; i < parts; i += 32) {
+        const Part& x = sh.part[i];
+        if (!(x.m > -INFINITY)) continue;
+        const double d = fmax(((double)x.m - (double)m) * (double)p.k, -1000.0), f = exp2(d);
+        z += f * x.z;
+        s += f * ((double)x.s + (double)x.z * d);
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) {
+        z += __shfl_xor_sync(0xffffffffu, z, d);
+        s += __shfl_xor_sync(0xffffffffu, s, d);
+      }
+    }
+    if (lane == 0) {
+      const double ln_z = ni > 0 ? log((double)ni) : log(z), mean = ni > 0 ? 0.0 : s / z * 0.69314718055994531;
+      const bool some = m > -INFINITY;   // else the row has no distribution
+      sh.ln_z = ln_z;
+      sh.m = m;
+      if (p.entropy) p.entropy[r] = some ? (float)(ln_z - mean) : 0.f;
+      if (p.logprob) {
+        const double zt = ni > 0 ? (xt == INFINITY ? 0.0 : -(double)INFINITY) : ((double)xt - (double)m) / (double)p.temperature;
+        p.logprob[r] = some && scored ? (float)(zt - ln_z) : 0.f;
+      }
+      if (p.rank) p.rank[r] = some && scored ? ah + (low ? t : 0) : -1;
+    }
+  }
+  if (p.n_top > 0) {
+    __syncthreads();
+    const bool some = sh.m > -INFINITY;
+    const int have = some ? min(p.n_top, p.vocab) : 0, all = cl * p.n_top;
+    for (int i = tid; i < all; i += LP_THREADS) {
+      const unsigned long long own = sh.top[i / p.n_top * LP_MAX_TOP + i % p.n_top];
+      int before = 0;
+      if (cl == 1) before = i;
+      else for (int j = 0; j < all; ++j) before += sh.top[j / p.n_top * LP_MAX_TOP + j % p.n_top] > own;
+      if (own == 0ull || before >= have) continue;
+      const float x = key_to_float((uint32_t)(own >> 32));
+      double z = ((double)x - (double)sh.m) / (double)p.temperature;
+      if (sh.m == INFINITY) z = x == INFINITY ? 0.0 : -(double)INFINITY;
+      p.top_token[(long long)r * p.n_top + before] = (int32_t)(0xffffffffu - (uint32_t)own);
+      p.top_logprob[(long long)r * p.n_top + before] = (float)(z - sh.ln_z);
+    }
+    for (int i = have + tid; i < p.n_top; i += LP_THREADS) {
+      p.top_token[(long long)r * p.n_top + i] = -1;
+      p.top_logprob[(long long)r * p.n_top + i] = some ? -INFINITY : 0.f;
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits, int32_t dtype, int64_t row_stride,
+                                             int32_t vocab, int32_t pos_base, int32_t n_pos, const int32_t* rows,
+                                             const int32_t* n_rows, int32_t max_rows, float temperature,
+                                             const int32_t* given, float* logprob, int32_t* rank, float* entropy,
+                                             int32_t n_top, int32_t* top_token, float* top_logprob, focus_stream stream) {
+  FOCUS_STAGE("focus_token_logprobs");
+  if (!ctx || !logits || vocab <= 0 || row_stride < vocab || n_pos < 0 || max_rows < 0) return FOCUS_ERR_INVALID_ARG;
+  if (dtype != FOCUS_F32 && dtype != FOCUS_BF16) return FOCUS_ERR_INVALID_ARG;
+  if (!aligned16(logits) || row_stride % (dtype == FOCUS_BF16 ? 8 : 4)) return FOCUS_ERR_INVALID_ARG;
+  if ((rows == nullptr) != (n_rows == nullptr)) return FOCUS_ERR_INVALID_ARG;
+  if (pos_base < 0 || n_pos > 0x7fffffff - pos_base || (!rows && max_rows > n_pos)) return FOCUS_ERR_INVALID_ARG;
+  if (!(temperature > 0.f) || !isfinite(temperature)) return FOCUS_ERR_INVALID_ARG;
+  if (n_top < 0 || (n_top > 0) != (top_token != nullptr) || (n_top > 0) != (top_logprob != nullptr)) return FOCUS_ERR_INVALID_ARG;
+  if ((given == nullptr) != (logprob == nullptr) || (rank && !given)) return FOCUS_ERR_INVALID_ARG;
+  if (!logprob && !entropy && n_top == 0) return FOCUS_ERR_INVALID_ARG;
+  const float k = (float)(1.4426950408889634 / (double)temperature);
+  if (n_top > LP_MAX_TOP || !isfinite(k) || k < 1e-30f) return FOCUS_ERR_UNSUPPORTED;
+  if (max_rows == 0) return FOCUS_OK;
+  const DeviceGuard guard(ctx);
+  if (!guard.ok) return FOCUS_ERR_CUDA;
+  const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, given, logprob,
+                      rank, entropy, top_token, top_logprob, ctx->d_status};
+  // CTAs per row: until there are six per SM (so that a last, partly filled wave is a small part of the whole) or a
+  // thread would have less than two vectors
+  const int vectors = (vocab + (dtype == FOCUS_BF16 ? 7 : 3)) / (dtype == FOCUS_BF16 ? 8 : 4);
+  int cl = 1;
+  while (cl < LP_MAX_CLUSTER && (long long)max_rows * cl < 6ll * ctx->sm_count && vectors >= 4 * cl * LP_THREADS) cl *= 2;
+  if ((long long)max_rows * cl > 0x7fffffffll) return FOCUS_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(max_rows * cl));
+  cfg.blockDim = dim3(LP_THREADS);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)cl; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = cl > 1 ? 1 : 0;
+  if (dtype == FOCUS_BF16) cudaLaunchKernelEx(&cfg, token_logprobs_kernel<__nv_bfloat16>, p, cl);
+  else cudaLaunchKernelEx(&cfg, token_logprobs_kernel<float>, p, cl);
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
