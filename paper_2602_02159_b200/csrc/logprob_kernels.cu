@@ -4,17 +4,19 @@
 // With z_v = (x_v - m) / T, m = max x:  log p_t = z_t - ln Z,  Z = sum e^z;  H = ln Z - (sum e^z z) / Z.  A thread keeps a
 // running maximum with its two sums, in base 2: exponents are (x - m) k, k = log2 e / T (one fma of x k and a rounded m k
 // would save an instruction, and overflow for logits near the end of the range).  Threads' sums are fp32 over a few hundred
-// logits, joined in fp32 per warp and in fp64 beyond.
+// logits, joined in fp32, in a fixed order.
 //
-// Top tokens.  A thread remembers its maximum and the vector where it first met it.  Of 64 groups of threads the n-th
+// Top tokens.  A thread remembers its maximum and the run of vectors where it first met it.  Of 64 groups of threads the n-th
 // largest such pair is a lower bound of the n-th largest logit that few more logits reach (20 of 64: 24 on average); only the
-// threads whose maximum reaches it have any, and their warp looks their vectors through again, a lane per vector.  The list
-// is ordered by counting, per logit, those ahead of it.  A list that overflows (more than LP_LIST logits above the bound,
+// threads whose maximum reaches it have any, and the CTA looks their runs through again, one per thread.  The list is
+// ordered by counting, per logit, those ahead of it.  A list that overflows (more than LP_LIST logits above the bound,
 // which takes logits that repeat with the threads' stride) is replaced by n searches for the next largest.
 //
 // A row belongs to one CTA where there are many, else to a cluster of up to eight, whose first CTA joins what the others
-// put into its shared memory.  What bounds it: HBM (512 rows of 126464 bf16 logits: 20 us) with the exponentials close behind
-// (16 per clock and SM: 14 us).
+// put into its shared memory.  What bounds it: 512 rows of 126464 bf16 logits with 20 alternatives take 42 us, of which HBM
+// needs 20 and the exponentials 14 (16 per clock and SM); the pass alone is 28 (8 instructions a logit, packed where there are
+// packed forms; 34 with scalar ones), ranks are 4, the alternatives 10: a chain of barriers per row, which four CTAs per SM
+// hide in part.  One row of 50257 fp32 logits: 8.6 us, five dependent steps of a microsecond and the launch.
 #include <math.h>
 
 #include "focus_common.cuh"
@@ -26,7 +28,7 @@ constexpr int LP_GROUPS = 64, LP_PER_GROUP = LP_THREADS / LP_GROUPS;
 constexpr int LP_MAX_CLUSTER = 8, LP_MAX_TOP = 32;
 constexpr int LP_LIST = 1024;
 constexpr int LP_UNROLL = 4;             // vectors in flight per thread
-constexpr float LP_FLOOR = -1.0e4f;      // exponents are clamped here: weight 0, and 0 times it is 0 (NaN logits end here too)
+constexpr float LP_FLOOR = -1.0e4f;      // exponents end here: weight 0, and 0 times it is 0 (NaN and -inf logits too)
 
 struct LpParams {
   const void* logits;
@@ -34,7 +36,7 @@ struct LpParams {
   int vocab, pos_base, n_pos, max_rows, n_top;
   const int32_t* rows;
   const int32_t* n_rows;
-  float temperature, k;                  // k = log2 e / temperature
+  float temperature, k, reach;           // k = log2 e / temperature, reach = LP_FLOOR / k
   const int32_t* given;
   float* logprob;
   int32_t* rank;
@@ -57,12 +59,13 @@ struct LpShared {
   unsigned long long top[LP_MAX_CLUSTER * LP_MAX_TOP];
   unsigned long long group[LP_GROUPS], bound, best[LP_WARPS];
   unsigned long long list[LP_LIST];
-  int list_n;
+  int list_n, owners;
+  uint8_t owner[LP_THREADS];
   double ln_z;
   float m;
 };
 
-// Order of tokens: larger logit first, then the lower index.  Position: index of the token, or of its vector.
+// Order of tokens: larger logit first, then the lower index.  Position: index of the token, or of its run.
 __device__ __forceinline__ unsigned long long order_key(float x, uint32_t position) {
   const uint32_t k = x != x ? float_key(-INFINITY) : float_key(x);
   return (unsigned long long)k << 32 | (0xffffffffu - position);
@@ -72,6 +75,23 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+__device__ __forceinline__ unsigned long long bits2(const float2& v) { return *reinterpret_cast<const unsigned long long*>(&v); }
+__device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&r)) : "l"(bits2(a)), "l"(bits2(b)));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(const float2& a, const float2& b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&r)) : "l"(bits2(a)), "l"(bits2(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const float2& c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*reinterpret_cast<unsigned long long*>(&r)) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return r;
 }
 
 // sums of two shares, relative to the larger maximum (with an infinite one they mean nothing: such rows go by the number of
@@ -105,19 +125,28 @@ template <> struct Vec<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
   }
-  __device__ static float largest(const uint4& r) {
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
-    const __nv_bfloat162 a = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-    return __bfloat162float(__hmax(__low2bfloat16(a), __high2bfloat16(a)));
-  }
-  // how many elements are above t, or (equal) not below it
-  __device__ static int ahead(const uint4& r, float t, bool equal) {
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
-    const __nv_bfloat162 t2 = __float2bfloat162_rn(t);
-    __nv_bfloat162 n = __float2bfloat162_rn(0.f);                                     // counts to 4 are exact
+  template <int N> __device__ static float largest(const uint4 (&r)[N]) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(r);
+    __nv_bfloat162 a = h[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n = __hadd2(n, equal ? __hge2(h[i], t2) : __hgt2(h[i], t2));
+    for (int i = 1; i < 4 * N; ++i) a = __hmax2(a, h[i]);
+    return fmaxf(__low2float(a), __high2float(a));
+  }
+  // how many elements are above t, or (EQUAL) not below it
+  template <bool EQUAL, int N> __device__ static int ahead(const uint4 (&r)[N], float t) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(r);
+    const __nv_bfloat162 t2 = __float2bfloat162_rn(t);
+    __nv_bfloat162 n = __float2bfloat162_rn(0.f);                                     // counts to 4 N <= 256 are exact
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) n = __hadd2(n, EQUAL ? __hge2(h[i], t2) : __hgt2(h[i], t2));
     return (int)(__low2float(n) + __high2float(n));
+  }
+  // no element below c, NaN none either
+  __device__ static void raise(uint4& r, float c) {
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
+    const __nv_bfloat162 c2 = __bfloat162bfloat162(__float2bfloat16_rd(c));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __hmax2(h[i], c2);
   }
 };
 template <> struct Vec<float> {
@@ -132,18 +161,38 @@ template <> struct Vec<float> {
   __device__ static void floats(const uint4& r, float (&x)[EPC]) {
     x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
   }
-  __device__ static float largest(const uint4& r) {
-    return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+  template <int N> __device__ static float largest(const uint4 (&r)[N]) {
+    const float* x = reinterpret_cast<const float*>(r);
+    float a = x[0];
+#pragma unroll
+    for (int i = 1; i < 4 * N; ++i) a = fmaxf(a, x[i]);
+    return a;
   }
-  __device__ static int ahead(const uint4& r, float t, bool equal) {
-    float x[EPC];
-    floats(r, x);
+  template <bool EQUAL, int N> __device__ static int ahead(const uint4 (&r)[N], float t) {
+    const float* x = reinterpret_cast<const float*>(r);
     int n = 0;
 #pragma unroll
-    for (int e = 0; e < EPC; ++e) n += equal ? x[e] >= t : x[e] > t;
+    for (int i = 0; i < 4 * N; ++i) n += EQUAL ? x[i] >= t : x[i] > t;
     return n;
   }
+  __device__ static void raise(uint4& r, float c) {
+    float* x = reinterpret_cast<float*>(&r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fmaxf(x[i], c);
+  }
 };
+
+// run v of a row: LP_UNROLL neighbouring vectors, -inf beyond the row's end
+template <typename T>
+__device__ __forceinline__ void load_run(const T* row, int v, int vocab, uint4 (&r)[LP_UNROLL]) {
+  if ((v + 1) * (LP_UNROLL * Vec<T>::EPC) <= vocab) {
+    const uint4* at = reinterpret_cast<const uint4*>(row) + (long long)v * LP_UNROLL;
+#pragma unroll
+    for (int u = 0; u < LP_UNROLL; ++u) r[u] = __ldg(at + u);
+  } else {
+    for (int u = 0; u < LP_UNROLL; ++u) Vec<T>::load(row, v * LP_UNROLL + u, vocab, r[u]);
+  }
+}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
@@ -166,7 +215,7 @@ __device__ __forceinline__ void put_far(uint32_t addr, unsigned long long v) {
 
 // grid: clusters of `cl` CTAs, one per row
 template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpParams p, const int cl) {
+__global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpParams p, const int cl) {
   constexpr int EPC = Vec<T>::EPC;
   __shared__ LpShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -178,56 +227,54 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
   const int t = live && p.given ? p.given[r] : -1;
   const bool scored = t >= 0 && t < p.vocab;
   if (q == 0 && tid == 0 && ((r < n && !live) || (live && !scored && t != -1))) set_status(p.status, FOCUS_ERR_INVALID_ARG);
-  if (tid == 0) sh.list_n = 0;
+  if (tid == 0) sh.list_n = sh.owners = 0;
 
-  // ---- the pass: vectors v0 + tid, + LP_THREADS, ... of this CTA's slice
+  // ---- the pass: runs v0 + tid, + LP_THREADS, ... of this CTA's slice, a run being LP_UNROLL neighbouring vectors
   Sums a = {-INFINITY, 0.f, 0.f};
-  int n_inf = 0, ahead = 0, first = 0;
+  int n_inf = 0, ahead = 0;
   const T* row = (const T*)p.logits + (long long)(live ? pos - p.pos_base : 0) * p.row_stride;
-  const int vectors = live ? (p.vocab + EPC - 1) / EPC : 0, per = (vectors + cl - 1) / cl;
-  const int v0 = min(q * per, vectors), v1 = min(v0 + per, vectors);
+  constexpr int RUN = EPC * LP_UNROLL;
+  const int runs = live ? (p.vocab + RUN - 1) / RUN : 0, per = (runs + cl - 1) / cl;
+  const int v0 = min(q * per, runs), v1 = min(v0 + per, runs);
   float xt = scored ? load_as_float(row + t) : 0.f;
   if (xt != xt) xt = -INFINITY;
   const bool low = xt == -INFINITY;      // then every token before t is ahead of it: added at the end
-  const int tv = t / EPC;
-  first = v0 + tid;
-  for (int v = v0 + tid; v < v1; v += LP_THREADS * LP_UNROLL) {
+  const int tv = t / RUN;
+  int first = v0 + tid;                  // the run that holds the maximum
+  static_assert(LP_UNROLL == 4, "the selection above the clamped loop");
+  float floor = -INFINITY;               // logits below it have no weight: as far under the maximum as LP_FLOOR says
+  float2 z2 = {0.f, 0.f}, s2 = {0.f, 0.f};                             // a.z and a.s, for the even and the odd logits
+  uint4 next[LP_UNROLL];
+  if (v0 + tid < v1) load_run(row, v0 + tid, p.vocab, next);
+  for (int v = v0 + tid; v < v1; v += LP_THREADS) {
     uint4 raw[LP_UNROLL];
-    float big[LP_UNROLL];
 #pragma unroll
-    for (int u = 0; u < LP_UNROLL; ++u) {
-      const int at = v + u * LP_THREADS;
-      if (at < v1) Vec<T>::load(row, at, p.vocab, raw[u]);
-      else raw[u] = EPC == 8 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
-                             : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < LP_UNROLL; ++u) {
-      big[u] = Vec<T>::largest(raw[u]);
-      top = fmaxf(top, big[u]);
-    }
+    for (int u = 0; u < LP_UNROLL; ++u) raw[u] = next[u];
+    if (v + LP_THREADS < v1) load_run(row, v + LP_THREADS, p.vocab, next);
+    const float top = Vec<T>::largest(raw);
     if (top > a.m) {
-      int u0 = LP_UNROLL - 1;
-#pragma unroll
-      for (int u = LP_UNROLL - 2; u >= 0; --u) u0 = big[u] == top ? u : u0;
-      first = v + u0 * LP_THREADS;
+      first = v;
       const float d = fmaxf((a.m - top) * p.k, LP_FLOOR), f = ex2(d);     // 0 for the first maximum
-      a.s = f * fmaf(a.z, d, a.s);
-      a.z *= f;
+      s2 = mul2(make_float2(f, f), fma2(z2, make_float2(d, d), s2));
+      z2 = mul2(make_float2(f, f), z2);
       a.m = top;
+      floor = __fadd_rd(top, p.reach);                                    // rounded down: below the maximum however large it is
     }
     if (scored) {
+      if (v < tv) {
+        if (!low) ahead += Vec<T>::template ahead<true>(raw, xt);
+      } else if (v > tv) {
+        ahead += Vec<T>::template ahead<false>(raw, xt);
+      } else {
 #pragma unroll
-      for (int u = 0; u < LP_UNROLL; ++u) {
-        const int at = v + u * LP_THREADS;
-        if (at != tv) {
-          if (!(low && at < tv)) ahead += Vec<T>::ahead(raw[u], xt, at < tv);
-        } else {
+        for (int u = 0; u < LP_UNROLL; ++u) {
           float x[EPC];
           Vec<T>::floats(raw[u], x);
 #pragma unroll
-          for (int e = 0; e < EPC; ++e) ahead += x[e] > xt ? !(low && at * EPC + e < t) : (x[e] == xt && at * EPC + e < t && !low);
+          for (int e = 0; e < EPC; ++e) {
+            const bool before = v * RUN + u * EPC + e < t;
+            ahead += before ? x[e] >= xt && !low : x[e] > xt;
+          }
         }
       }
     }
@@ -240,18 +287,36 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
         for (int e = 0; e < EPC; ++e) n_inf += x[e] == INFINITY;
       }
     }
+    if (floor > -3.3e38f) {
 #pragma unroll
-    for (int u = 0; u < LP_UNROLL; ++u) {
-      float x[EPC];
-      Vec<T>::floats(raw[u], x);
+      for (int u = 0; u < LP_UNROLL; ++u) {
+        float x[EPC];
+        Vec<T>::raise(raw[u], floor);
+        Vec<T>::floats(raw[u], x);
 #pragma unroll
-      for (int e = 0; e < EPC; ++e) {
-        const float d = fmaxf((x[e] - a.m) * p.k, LP_FLOOR), w = ex2(d);
-        a.z += w;
-        a.s = fmaf(w, d, a.s);
+        for (int e = 0; e < EPC; e += 2) {                                // packed pairs: half the instructions
+          const float2 d = mul2(add2(make_float2(x[e], x[e + 1]), make_float2(-a.m, -a.m)), make_float2(p.k, p.k));
+          const float2 w = make_float2(ex2(d.x), ex2(d.y));
+          z2 = add2(z2, w);
+          s2 = fma2(w, d, s2);
+        }
+      }
+    } else if (a.m > -INFINITY) {        // nothing finite lies that far under the maximum: exponents are clamped one by one
+#pragma unroll 1
+      for (int u = 0; u < LP_UNROLL; ++u) {
+        float x[EPC];
+        Vec<T>::floats(u == 0 ? raw[0] : u == 1 ? raw[1] : u == 2 ? raw[2] : raw[3], x);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+          const float d = fmaxf((x[e] - a.m) * p.k, LP_FLOOR), w = ex2(d);
+          z2.x += w;
+          s2.x = fmaf(w, d, s2.x);
+        }
       }
     }
   }
+  a.z = z2.x + z2.y;
+  a.s = s2.x + s2.y;
 
   // ---- sums: per warp, into the leader
   {
@@ -289,48 +354,58 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
     if (tid % LP_PER_GROUP == 0) sh.group[tid / LP_PER_GROUP] = g;
     if (tid == 0) sh.bound = 0ull;
     __syncthreads();
-    if (tid < LP_GROUPS) {
-      const unsigned long long own = sh.group[tid];
+    {                                    // LP_PER_GROUP threads count for one group
+      const unsigned long long own = sh.group[tid / LP_PER_GROUP];
       int before = 0;
-#pragma unroll 16
-      for (int i = 0; i < LP_GROUPS; ++i) before += sh.group[i] > own;
+#pragma unroll
+      for (int i = tid % LP_PER_GROUP; i < LP_GROUPS; i += LP_PER_GROUP) before += sh.group[i] > own;
+#pragma unroll
+      for (int d = 1; d < LP_PER_GROUP; d <<= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
       if (own != 0ull && before == p.n_top - 1) sh.bound = own;                       // keys are distinct
     }
     __syncthreads();
     const unsigned long long bound = sh.bound;                                        // 0: fewer groups than that, all is listed
-    const int trips = (v1 - v0 + LP_THREADS - 1) / LP_THREADS;
-    uint32_t owners = __ballot_sync(0xffffffffu, mine != 0ull && mine >= bound);
-    while (owners) {                                                                  // a lane per vector of the owner's
-      const int o = __ffs(owners) - 1;
-      owners &= owners - 1;
-      for (int i = lane; i < trips; i += 32) {
-        const int at = v0 + warp * 32 + o + i * LP_THREADS;
-        if (at >= v1) continue;
-        uint4 raw;
+    if (mine != 0ull && mine >= bound) sh.owner[atomicAdd(&sh.owners, 1)] = (uint8_t)tid;
+    __syncthreads();
+    const float least = bound ? key_to_float((uint32_t)(bound >> 32)) : -INFINITY;
+    // the owners' runs, one per thread and trip
+    const int trips = (v1 - v0 + LP_THREADS - 1) / LP_THREADS, all = sh.owners * trips;
+    for (int i = tid; i < all; i += LP_THREADS) {
+      const int at = v0 + sh.owner[i / trips] + i % trips * LP_THREADS;
+      if (at >= v1) continue;
+      uint4 raw[LP_UNROLL];
+      load_run(row, at, p.vocab, raw);
+      if (order_key(Vec<T>::largest(raw), (uint32_t)at) < bound) continue;
+#pragma unroll
+      for (int u = 0; u < LP_UNROLL; ++u) {
         float x[EPC];
-        Vec<T>::load(row, at, p.vocab, raw);
-        Vec<T>::floats(raw, x);
+        Vec<T>::floats(raw[u], x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
-          if (at * EPC + e < p.vocab && order_key(x[e], (uint32_t)at) >= bound) {
+          if (x[e] < least) continue;    // false for NaN, which counts as -inf
+          const int v = at * RUN + u * EPC + e;
+          if (v < p.vocab && order_key(x[e], (uint32_t)at) >= bound) {
             const int slot = atomicAdd(&sh.list_n, 1);
-            if (slot < LP_LIST) sh.list[slot] = order_key(x[e], (uint32_t)(at * EPC + e));
+            if (slot < LP_LIST) sh.list[slot] = order_key(x[e], (uint32_t)v);
           }
         }
       }
     }
     __syncthreads();
     const int listed = sh.list_n;
-    const uint32_t to = cl > 1 ? leader_addr(&sh.top[q * LP_MAX_TOP]) : 0u;
+    const uint32_t to = cl > 1 ? leader_addr(&sh.top[q * p.n_top]) : 0u;
     auto put = [&](int i, unsigned long long key) {
       if (cl > 1) put_far(to + i * 8, key); else sh.top[i] = key;
     };
     if (listed <= LP_LIST) {
-      for (int i = tid; i < listed; i += LP_THREADS) {
-        const unsigned long long own = sh.list[i];
+      for (int i0 = 0; i0 < listed; i0 += LP_THREADS / 4) {                           // four threads count for one entry
+        const int i = i0 + tid / 4;
+        const unsigned long long own = i < listed ? sh.list[i] : 0ull;
         int before = 0;
-        for (int j = 0; j < listed; ++j) before += sh.list[j] > own;
-        if (before < p.n_top) put(before, own);
+        for (int j = tid % 4; j < listed; j += 4) before += sh.list[j] > own;
+        before += __shfl_xor_sync(0xffffffffu, before, 1);
+        before += __shfl_xor_sync(0xffffffffu, before, 2);
+        if (tid % 4 == 0 && i < listed && before < p.n_top) put(before, own);
       }
       for (int i = listed + tid; i < p.n_top; i += LP_THREADS) put(i, 0ull);
     } else {
@@ -338,14 +413,18 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
       for (int i = 0; i < p.n_top; ++i) {
         unsigned long long best = 0ull;
         for (int v = v0 + tid; v < v1; v += LP_THREADS) {
-          uint4 raw;
-          float x[EPC];
-          Vec<T>::load(row, v, p.vocab, raw);
-          Vec<T>::floats(raw, x);
+          uint4 raw[LP_UNROLL];
+          load_run(row, v, p.vocab, raw);
 #pragma unroll
-          for (int e = 0; e < EPC; ++e) {
-            const unsigned long long key = v * EPC + e < p.vocab ? order_key(x[e], (uint32_t)(v * EPC + e)) : 0ull;
-            if (key < last && key > best) best = key;
+          for (int u = 0; u < LP_UNROLL; ++u) {
+            float x[EPC];
+            Vec<T>::floats(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < EPC; ++e) {
+              const int at = v * RUN + u * EPC + e;
+              const unsigned long long key = at < p.vocab ? order_key(x[e], (uint32_t)at) : 0ull;
+              if (key < last && key > best) best = key;
+            }
           }
         }
 #pragma unroll
@@ -371,35 +450,28 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
   // ---- the leader joins the warps' sums and orders the CTAs' tokens
   if (warp == 0) {
     const int parts = cl * LP_WARPS;
-    float m = -INFINITY;
+    Sums a = {-INFINITY, 0.f, 0.f};
     int ni = 0, ah = 0;
     for (int i = lane; i < parts; i += 32) {
       const Part& x = sh.part[i];
+      const Sums o = {x.m, x.z, x.s};
+      join(a, o, p.k);
       ni += x.n_inf;
       ah += x.ahead;
-      m = fmaxf(m, x.m);
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int d = 16; d > 0; d >>= 1) {
+      Sums o;
+      o.m = __shfl_xor_sync(0xffffffffu, a.m, d);
+      o.z = __shfl_xor_sync(0xffffffffu, a.z, d);
+      o.s = __shfl_xor_sync(0xffffffffu, a.s, d);
+      join(a, o, p.k);
+    }
     ni = __reduce_add_sync(0xffffffffu, ni);
     ah = __reduce_add_sync(0xffffffffu, ah);
-    double z = 0.0, s = 0.0;
-    if (ni == 0) {
-      for (int i = lane; i < parts; i += 32) {
-        const Part& x = sh.part[i];
-        if (!(x.m > -INFINITY)) continue;
-        const double d = fmax(((double)x.m - (double)m) * (double)p.k, -1000.0), f = exp2(d);
-        z += f * x.z;
-        s += f * ((double)x.s + (double)x.z * d);
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        z += __shfl_xor_sync(0xffffffffu, z, d);
-        s += __shfl_xor_sync(0xffffffffu, s, d);
-      }
-    }
     if (lane == 0) {
-      const double ln_z = ni > 0 ? log((double)ni) : log(z), mean = ni > 0 ? 0.0 : s / z * 0.69314718055994531;
+      const float m = a.m;
+      const double ln_z = log(ni > 0 ? (double)ni : (double)a.z), mean = ni > 0 ? 0.0 : (double)(a.s / a.z) * 0.69314718055994531;
       const bool some = m > -INFINITY;   // else the row has no distribution
       sh.ln_z = ln_z;
       sh.m = m;
@@ -416,10 +488,10 @@ __global__ void __launch_bounds__(LP_THREADS) token_logprobs_kernel(const LpPara
     const bool some = sh.m > -INFINITY;
     const int have = some ? min(p.n_top, p.vocab) : 0, all = cl * p.n_top;
     for (int i = tid; i < all; i += LP_THREADS) {
-      const unsigned long long own = sh.top[i / p.n_top * LP_MAX_TOP + i % p.n_top];
+      const unsigned long long own = sh.top[i];
       int before = 0;
       if (cl == 1) before = i;
-      else for (int j = 0; j < all; ++j) before += sh.top[j / p.n_top * LP_MAX_TOP + j % p.n_top] > own;
+      else for (int j = 0; j < all; ++j) before += sh.top[j] > own;
       if (own == 0ull || before >= have) continue;
       const float x = key_to_float((uint32_t)(own >> 32));
       double z = ((double)x - (double)sh.m) / (double)p.temperature;
@@ -456,13 +528,13 @@ extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits,
   if (max_rows == 0) return FOCUS_OK;
   const DeviceGuard guard(ctx);
   if (!guard.ok) return FOCUS_ERR_CUDA;
-  const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, given, logprob,
+  const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, LP_FLOOR / k, given, logprob,
                       rank, entropy, top_token, top_logprob, ctx->d_status};
-  // CTAs per row: until there are six per SM (so that a last, partly filled wave is a small part of the whole) or a
-  // thread would have less than two vectors
-  const int vectors = (vocab + (dtype == FOCUS_BF16 ? 7 : 3)) / (dtype == FOCUS_BF16 ? 8 : 4);
+  // CTAs per row: until there are three per SM (512 rows of 126464 in one CTA each 42 us, in two 44: fewer ends to rows) or a
+  // thread would have no run of its own
+  const int runs = vocab / (dtype == FOCUS_BF16 ? 8 * LP_UNROLL : 4 * LP_UNROLL);
   int cl = 1;
-  while (cl < LP_MAX_CLUSTER && (long long)max_rows * cl < 6ll * ctx->sm_count && vectors >= 4 * cl * LP_THREADS) cl *= 2;
+  while (cl < LP_MAX_CLUSTER && (long long)max_rows * cl < 3ll * ctx->sm_count && runs >= cl * LP_THREADS) cl *= 2;
   if ((long long)max_rows * cl > 0x7fffffffll) return FOCUS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(max_rows * cl));
