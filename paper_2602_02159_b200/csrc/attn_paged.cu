@@ -29,10 +29,12 @@ namespace {
 
 constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
 constexpr int KT = 16;                   // keys per tile
-constexpr int SEG_COST = 6;              // cost of a segment beside its tiles, in tiles
-constexpr int MIN_COST = 16;             // least cost per CTA: below, joining costs more than sharing gains
+constexpr int SEG_COST = 24;             // cost of a segment beside its tiles, in tiles: a ragged batch of 64 takes 163 us, 175 with 6
+constexpr int MIN_COST = 10;             // least cost per CTA: below, joining costs more than sharing gains
 constexpr int JOIN = 8;
+
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NO_KEYS = -3.402823466e38f;   // running maximum of a row without keys so far: below every score, and finite
 constexpr float LAZY = 8.f;              // the running maximum may lag by this much (base 2): numerators stay below 2^8
 
 struct PagedArgs {
@@ -44,31 +46,35 @@ struct PagedArgs {
   const int32_t* table;
   const int32_t* kv_len;
   const int32_t* row_start;
-  int page, n_pages, n_seqs, max_pages, L, max_rows, H, Hkv, hpg;
+  int page, page_shift, n_pages, n_seqs, max_pages, L, max_rows, H, Hkv, hpg;   // page_shift: its logarithm, or -1
   float scale;                           // softmax scale * log2 e
   void* O;
   float* lse;
-  float* part;                           // [gridDim.x][2] partials: RT (max, sum) pairs, then RT rows of D
+  float* part;                           // [gridDim.x][2] partials: (max, sum) pairs of RT rows, then the rows
   int32_t* counters;                     // 3 per CTA, zero between launches
   int32_t* status;
 };
 
 template <typename T, int D, int NT>
 struct Cfg {
-  static constexpr int RT = 8 * NT;                                       // stacked rows per tile
+  static constexpr int RT = sizeof(T) == 2 ? 8 * NT : NT;                 // stacked rows per tile
   static constexpr int ROW_BYTES = D * (int)sizeof(T);
   static constexpr int STAGES = ROW_BYTES == 128 ? 6 : 3;
   static constexpr int OPERAND = KT * ROW_BYTES, STAGE = 2 * OPERAND, RING = STAGES * STAGE;   // per warp
   static constexpr int Q_PITCH = sizeof(T) == 2 ? D + 8 : D;              // elements; 16 bytes on: ldmatrix without conflicts
   static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
-  static constexpr int PART = RT * (D + 2);                               // floats of one partial in the workspace
+  static constexpr int HEAD = (2 * RT + 3) & ~3;                          // floats of a partial ahead of its rows (16-byte vectors)
+  static constexpr int PART = HEAD + RT * D;                              // floats of one partial in the workspace
+  static constexpr int JOIN_LOADS = sizeof(T) == 2 && NT == 4 ? 4 : 10;    // vectors in flight per thread of a join (registers)
   static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
   static constexpr int OFF_Q = RING * PA_WARPS;
-  static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][8][KT]
-  static constexpr int OFF_ML = OFF_P + (sizeof(T) == 4 ? PA_WARPS * 8 * KT * 4 : 0);
+  static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][RT][KT]
+  static constexpr int OFF_ML = OFF_P + (sizeof(T) == 4 ? PA_WARPS * RT * KT * 4 : 0);
   static constexpr int OFF_MASK = OFF_ML + PA_WARPS * RT * 8;
   static constexpr int SMEM = OFF_MASK + PA_WARPS * STAGES * 4;
   static_assert(RT * O_PITCH * 4 <= RING, "a warp's partial lies in its ring");
+  static_assert(OFF_Q % 16 == 0 && OFF_P % 16 == 0 && OFF_ML % 8 == 0 && OFF_MASK % 4 == 0 && PART % 4 == 0 && O_PITCH % 4 == 0 &&
+                Q_PITCH * sizeof(T) % 16 == 0 && RING % 128 == 0, "alignment of vector accesses");
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -129,13 +135,23 @@ __device__ __forceinline__ Seq seq_of(const PagedArgs& a, int s) {
 __device__ __forceinline__ int seg_cost(const Seq& q) { return (q.len + KT - 1) / KT + SEG_COST; }
 __device__ __forceinline__ long long seq_cost(const Seq& q, int Hkv) { return (long long)seg_cost(q) * q.row_tiles * Hkv; }
 
-// where in the pools the keys of tile t lie: lane l has key 16 t + (l & 15), -1 where there is none to attend
-__device__ __forceinline__ long long key_offset(const PagedArgs& a, int s, int len, int t, int lane) {
+// the place of key j in its sequence's pages
+__device__ __forceinline__ int page_of(const PagedArgs& a, int j) { return a.page_shift >= 0 ? j >> a.page_shift : j / a.page; }
+// Lane l has key 16 t + (l & 15) of tile t: its page, as the table has it (-1 where the tile or the sequence has ended), and
+// then where in the pools it lies, -1 where there is nothing to attend.
+__device__ __forceinline__ int key_page(const PagedArgs& a, int s, int len, int t, int t_hi, int lane) {
+  const int j = t * KT + (lane & 15);
+  return t < t_hi && j < len ? a.table[(long long)s * a.max_pages + page_of(a, j)] : -1;
+}
+__device__ __forceinline__ long long key_offset(const PagedArgs& a, int len, int t, int page, int lane) {
   const int j = t * KT + (lane & 15);
   if (j >= len) return -1;
-  const int at = j / a.page, page = a.table[(long long)s * a.max_pages + at];
   if (page < 0 || page >= a.n_pages) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return -1; }
-  return (long long)page * a.st_page + (long long)(j - at * a.page) * a.st_tok;
+  return (long long)page * a.st_page + (long long)(j - page_of(a, j) * a.page) * a.st_tok;
+}
+// non-negative; most are small
+__device__ __forceinline__ long long divide(long long n, long long d) {
+  return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
 // a tile's K and V rows into one stage: row k at k * ROW_BYTES, its 16-byte chunk c at place c ^ (k & 7)
@@ -182,7 +198,7 @@ struct Core<__nv_bfloat16, D, NT> {
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = NO_KEYS;
       l[n][0] = l[n][1] = 0.f;
 #pragma unroll
       for (int i = 0; i < KS; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
@@ -215,40 +231,49 @@ struct Core<__nv_bfloat16, D, NT> {
         }
       }
     }
-    const int g = lane >> 2;
-    const bool lo = (mask >> g) & 1u, hi = (mask >> (g + 8)) & 1u;
-    bool grow = false;
+    const bool lo = (mask >> (lane >> 2)) & 1u, hi = (mask >> ((lane >> 2) + 8)) & 1u;
+    float x[NT][4], top = NO_KEYS;       // exponents, relative to m
+    auto exponents = [&] {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        s[n][c] = lo ? s[n][c] * scale : -INFINITY;
-        s[n][c + 2] = hi ? s[n][c + 2] * scale : -INFINITY;
-        grow |= fmaxf(s[n][c], s[n][c + 2]) > m[n][c] + LAZY;
+        for (int c = 0; c < 4; ++c) x[n][c] = fmaf(s[n][c], scale, -m[n][c & 1]);
+      if (mask != 0xffffu) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (!(c < 2 ? lo : hi)) x[n][c] = -INFINITY;
       }
-    if (__any_sync(0xffffffffu, grow)) {
+    };
+    exponents();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) top = fmaxf(top, fmaxf(fmaxf(x[n][0], x[n][1]), fmaxf(x[n][2], x[n][3])));
+    if (__any_sync(0xffffffffu, top > LAZY)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float x = fmaxf(s[n][c], s[n][c + 2]);
+          float to = m[n][c];
+          if (lo) to = fmaxf(to, s[n][c] * scale);
+          if (hi) to = fmaxf(to, s[n][c + 2] * scale);
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-          const float to = fmaxf(m[n][c], x), f = to == -INFINITY ? 1.f : exp2_approx(m[n][c] - to);
+          for (int i = 4; i < 32; i <<= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, i));
+          const float f = exp2_approx(m[n][c] - to);
           m[n][c] = to;
           l[n][c] *= f;
 #pragma unroll
           for (int i = 0; i < KS; ++i) { o[i][n][c] *= f; o[i][n][c + 2] *= f; }
         }
+      exponents();
     }
     uint32_t b[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const float base = m[n][c] == -INFINITY ? 0.f : m[n][c];
-        s[n][c] = exp2_approx(s[n][c] - base);
-        s[n][c + 2] = exp2_approx(s[n][c + 2] - base);
+        s[n][c] = exp2_approx(x[n][c]);
+        s[n][c + 2] = exp2_approx(x[n][c + 2]);
         l[n][c] += s[n][c] + s[n][c + 2];
       }
       b[n][0] = transpose8(pack_bf16(s[n][0], s[n][1]));
@@ -286,18 +311,18 @@ struct Core<__nv_bfloat16, D, NT> {
   }
 };
 
-template <int D>
-struct Core<float, D, 1> {
+template <int D, int R>
+struct Core<float, D, R> {
   static constexpr int RB = D * 4, CV = D / 32;     // columns per lane
-  float m[8], l[8], o[8][CV];                       // l: of the lane's keys alone
+  float m[R], l[R], o[R][CV];                       // l: of the lane's keys alone
   const float* q;
   float* p;
 
   __device__ __forceinline__ void init(const float* Qs, float* Ps, int) {
     q = Qs; p = Ps;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      m[r] = -INFINITY; l[r] = 0.f;
+    for (int r = 0; r < R; ++r) {
+      m[r] = NO_KEYS; l[r] = 0.f;
 #pragma unroll
       for (int i = 0; i < CV; ++i) o[r][i] = 0.f;
     }
@@ -305,9 +330,9 @@ struct Core<float, D, 1> {
 
   __device__ __forceinline__ void tile(uint32_t ks, uint32_t mask, float scale, int lane) {
     const int key = lane & 15, half = lane >> 4;
-    float s[8];
+    float s[R];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) s[r] = 0.f;
+    for (int r = 0; r < R; ++r) s[r] = 0.f;
     const uint32_t row = ks + key * RB;
     const float* qh = q + half * (D / 2);
 #pragma unroll 4
@@ -316,7 +341,7 @@ struct Core<float, D, 1> {
       asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
                    : "r"(row + (((half * (D / 8) + c) ^ (key & 7)) << 4)) : "memory");
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
+      for (int r = 0; r < R; ++r) {
         const float4 x = *reinterpret_cast<const float4*>(qh + r * D + c * 4);
         s[r] = fmaf(k.x, x.x, fmaf(k.y, x.y, fmaf(k.z, x.z, fmaf(k.w, x.w, s[r]))));
       }
@@ -324,18 +349,18 @@ struct Core<float, D, 1> {
     const bool live = (mask >> key) & 1u;
     bool grow = false;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < R; ++r) {
       s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
       s[r] = live ? s[r] * scale : -INFINITY;
       grow |= s[r] > m[r] + LAZY;
     }
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
+      for (int r = 0; r < R; ++r) {
         float x = s[r];
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-        const float to = fmaxf(m[r], x), f = to == -INFINITY ? 1.f : exp2f(m[r] - to);
+        const float to = fmaxf(m[r], x), f = exp2f(m[r] - to);
         m[r] = to;
         l[r] *= f;
 #pragma unroll
@@ -343,12 +368,16 @@ struct Core<float, D, 1> {
       }
     }
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      s[r] = exp2f(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+    for (int r = 0; r < R; ++r) {
+      s[r] = exp2f(s[r] - m[r]);
       l[r] += s[r];                                 // in both halves alike
     }
+    if constexpr (R == 1) {
+      if (half == 0) p[key] = s[0];
+    } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) p[(half * 4 + r) * KT + key] = half ? s[r + 4] : s[r];
+      for (int r = 0; r < R / 2; ++r) p[(half * (R / 2) + r) * KT + key] = half ? s[r + R / 2] : s[r];
+    }
     __syncwarp();
     const uint32_t v0 = ks + KT * RB;
 #pragma unroll
@@ -365,7 +394,7 @@ struct Core<float, D, 1> {
           asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[k][0]), "=f"(v[k][1]) : "r"(at) : "memory");
       }
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
+      for (int r = 0; r < R; ++r) {
         const float4 w = *reinterpret_cast<const float4*>(p + r * KT + k4 * 4);
 #pragma unroll
         for (int i = 0; i < CV; ++i)
@@ -376,7 +405,7 @@ struct Core<float, D, 1> {
 
   __device__ __forceinline__ void store(float* os, float2* ml, int nq, int lane) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < R; ++r) {
 #pragma unroll
       for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
       if (r >= nq) continue;
@@ -415,35 +444,52 @@ struct Out {                             // where the stacked rows of a segment 
 __device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& y) {
   return make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w));
 }
-// 2^(m - M), 0 for a part without keys
-__device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
+// weight of a part with maximum m where the largest is M; a part without keys has the sum 0
+__device__ __forceinline__ float part_weight(float m, float M) { return exp2f(m - M); }
 
 // Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
-// wts: shared, nq * n weights and nq (max, sum) pairs.
-template <typename T, int D, int RT>
-__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, float* wts,
-                                     float2* ml, const Out<T, D>& out, float* dst) {
+// A thread's vectors of JOIN_LOADS partials are on their way while the weights are made: a join is two or three trips to L2.
+// pairs, wts: shared, nq * n (max, sum) pairs and weights; ml: the joined pairs.
+template <typename T, int D, int HEAD, int JOIN_LOADS>
+__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, float2* pairs,
+                                     float* wts, float2* ml, const Out<T, D>& out, float* dst) {
   // the first partial of a segment lies in its CTA's other slot
   auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
-  for (int r = threadIdx.x; r < nq; r += PA_THREADS) {
-    float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, __ldcg(at(i) + 2 * r));
-    for (int i = 0; i < n; ++i) {
-      const float w = part_weight(__ldcg(at(i) + 2 * r), M);
-      wts[r * n + i] = w;
-      L = fmaf(w, __ldcg(at(i) + 2 * r + 1), L);
+  const int items = nq * (D / 4);
+  float4 v[JOIN_LOADS];
+  auto fetch = [&](int e, int i0) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+#pragma unroll
+    for (int k = 0; k < JOIN_LOADS; ++k)
+      if (i0 + k < n) v[k] = __ldcg(reinterpret_cast<const float4*>(at(i0 + k) + HEAD + r * D + c));
+  };
+  int e = threadIdx.x;
+  if (e < items) fetch(e, 0);
+  for (int x = threadIdx.x; x < nq * n; x += PA_THREADS) pairs[x] = __ldcg(reinterpret_cast<const float2*>(at(x / nq)) + x % nq);
+  __syncthreads();
+  for (int x = threadIdx.x; x < nq * n; x += PA_THREADS) {
+    const int r = x % nq;
+    float M = -INFINITY;
+    for (int i = 0; i < n; ++i) M = fmaxf(M, pairs[i * nq + r].x);
+    wts[x] = part_weight(pairs[x].x, M);
+    if (x < nq) {
+      float L = 0.f;
+      for (int i = 0; i < n; ++i) L = fmaf(part_weight(pairs[i * nq + r].x, M), pairs[i * nq + r].y, L);
+      ml[r] = make_float2(M, L);
     }
-    ml[r] = make_float2(M, L);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < nq * (D / 4); e += PA_THREADS) {
+  for (; e < items; e += PA_THREADS) {
     const int r = e / (D / 4), c = e % (D / 4) * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = 0; i < n; ++i)
-      acc = axpy4(wts[r * n + i], __ldcg(reinterpret_cast<const float4*>(at(i) + 2 * RT + r * D + c)), acc);
+    for (int i0 = 0; i0 < n; i0 += JOIN_LOADS) {
+      if (i0 > 0 || e >= PA_THREADS) fetch(e, i0);
+#pragma unroll
+      for (int k = 0; k < JOIN_LOADS; ++k)
+        if (i0 + k < n) acc = axpy4(wts[(i0 + k) * nq + r], v[k], acc);
+    }
     if (dst) {
-      *reinterpret_cast<float4*>(dst + 2 * RT + r * D + c) = acc;
+      *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
       if (c == 0) *reinterpret_cast<float2*>(dst + 2 * r) = ml[r];
     } else {
       out.put(r, c, acc, ml[r].x, ml[r].y);
@@ -453,17 +499,18 @@ __device__ __forceinline__ void join(const float* part, long long stride, long l
 
 // true in every thread of the CTA that is the last of n to arrive
 __device__ __forceinline__ bool arrive_last(int32_t* counter, int n, int* flag) {
-  __threadfence();                       // this thread's partial is visible before the arrival
-  __syncthreads();
+  __syncthreads();                       // every thread's part of the partial is written
   if (threadIdx.x == 0) {
+    __threadfence();                     // and visible before the arrival
     const bool last = atomicAdd(counter, 1) == n - 1;
-    if (last) *counter = 0;              // ready for the next launch
+    if (last) {
+      *counter = 0;                      // ready for the next launch
+      __threadfence();
+    }
     *flag = last;
   }
   __syncthreads();
-  const bool last = *flag;
-  if (last) __threadfence();
-  return last;
+  return *flag;
 }
 
 template <typename T, int D, int NT>
@@ -502,7 +549,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
   if (total == 0) return;
   const long long G = min((long long)gridDim.x, max(1ll, total / MIN_COST)), cta = blockIdx.x;
   if (cta >= G) return;
-  const long long p0 = cta * total / G, p1 = (cta + 1) * total / G;
+  const long long p0 = divide(cta * total, G), p1 = divide((cta + 1) * total, G);
   {
     long long at = before + incl - mine;
     if (p0 >= at && p0 < at + mine) {
@@ -525,7 +572,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     const int cost = seg_cost(q), tiles = cost - SEG_COST;
     const long long whole = seq_cost(q, a.Hkv);
     if (p >= base + whole) { base += whole; ++s; continue; }
-    const int seg = (int)((p - base) / cost);
+    const int seg = (int)divide(p - base, cost);
     const long long seg_at = base + (long long)seg * cost, first_tile = seg_at + SEG_COST;
     const int g = seg / q.row_tiles, q0 = (seg - g * q.row_tiles) * RT;
     const int nq = (int)min((long long)RT, (long long)q.rows * a.hpg - q0);
@@ -541,40 +588,49 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     // ---- the tiles t_lo + w, + 4, ...
     const T* K = (const T*)a.K + (long long)g * a.st_head;
     const T* V = (const T*)a.V + (long long)g * a.st_head;
-    int t_load = t_lo + w;
-    long long off = t_load < t_hi ? key_offset(a, s, q.len, t_load, lane) : -1;
-    auto fetch = [&](int stage) {        // requests tile t_load, looks up the next one
+    int t_load = t_lo + w, page[C::STAGES];                              // page[i]: of the i-th tile that is not requested yet
+#pragma unroll
+    for (int i = 0; i < C::STAGES; ++i) page[i] = key_page(a, s, q.len, t_load + i * PA_WARPS, t_hi, lane);
+    // query rows beyond nq are zeros: their results are dropped
+    constexpr int CPR = D * (int)sizeof(T) / 16, EPC = 16 / (int)sizeof(T), QN = RT * CPR / PA_THREADS;
+    uint4 qv[QN > 0 ? QN : 1];
+#pragma unroll
+    for (int k = 0; k < (QN > 0 ? QN : 1); ++k) {
+      const int r = (tid + k * PA_THREADS) / CPR;
+      qv[k] = make_uint4(0, 0, 0, 0);
+      if (r < nq) {
+        int i, h;
+        out.row(r, i, h);
+        qv[k] = *reinterpret_cast<const uint4*>((const T*)a.Q + (long long)i * a.q_row + (long long)h * a.q_head + tid % CPR * EPC);
+      }
+    }
+    auto fetch = [&](int stage, int from) {                              // requests tile t_load
       if (t_load < t_hi) {
+        const long long off = key_offset(a, q.len, t_load, from, lane);
         const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
         if (lane == 0) masks[stage] = mask;
         load_tile<T, D>(a, K, V, off, ring + stage * C::STAGE, lane);
         t_load += PA_WARPS;
-        off = t_load < t_hi ? key_offset(a, s, q.len, t_load, lane) : -1;
       }
       commit_group();
     };
 #pragma unroll
-    for (int i = 0; i < C::STAGES - 1; ++i) fetch(i);
-    // query rows beyond nq are zeros: their results are dropped
-    for (int e = tid; e < RT * (D * (int)sizeof(T) / 16); e += PA_THREADS) {
-      constexpr int CPR = D * (int)sizeof(T) / 16, EPC = 16 / (int)sizeof(T);
-      const int r = e / CPR, c = e % CPR;
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (r < nq) {
-        int i, h;
-        out.row(r, i, h);
-        x = *reinterpret_cast<const uint4*>((const T*)a.Q + (long long)i * a.q_row + (long long)h * a.q_head + c * EPC);
-      }
-      *reinterpret_cast<uint4*>(Qs + r * C::Q_PITCH + c * EPC) = x;
+    for (int i = 0; i < C::STAGES - 1; ++i) fetch(i, page[i]);
+    int ahead = page[C::STAGES - 1];
+#pragma unroll
+    for (int k = 0; k < (QN > 0 ? QN : 1); ++k) {
+      const int r = (tid + k * PA_THREADS) / CPR;
+      if (r < RT) *reinterpret_cast<uint4*>(Qs + r * C::Q_PITCH + tid % CPR * EPC) = qv[k];
     }
     __syncthreads();
     Core<T, D, NT> core;
-    core.init(Qs, reinterpret_cast<float*>(smem + C::OFF_P) + w * 8 * KT, lane);
+    core.init(Qs, reinterpret_cast<float*>(smem + C::OFF_P) + w * RT * KT, lane);
     int stage = 0;
     for (int t = t_lo + w; t < t_hi; t += PA_WARPS) {
       wait_group<C::STAGES - 2>();
       __syncwarp();                      // every lane's copies are there, and nobody reads the stage refilled next
-      fetch(stage == 0 ? C::STAGES - 1 : stage - 1);
+      fetch(stage == 0 ? C::STAGES - 1 : stage - 1, ahead);
+      ahead = key_page(a, s, q.len, t_load, t_hi, lane);
       core.tile(ring + stage * C::STAGE, masks[stage], a.scale, lane);
       stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     }
@@ -585,7 +641,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
 
     // ---- the four warps' parts are joined: into O, or, for a piece of a segment, into the workspace
     const bool piece = first_tile < p0 || first_tile + tiles > p1;
-    auto cta_of = [&](long long pos) { return (int)(((pos + 1) * G - 1) / total); };
+    auto cta_of = [&](long long pos) { return (int)divide((pos + 1) * G - 1, total); };
     const int c0 = piece ? cta_of(first_tile) : 0, parts = piece ? cta_of(first_tile + tiles - 1) - c0 + 1 : 1;
     float* slot = a.part + ((long long)cta * 2 + (cta == c0 ? 1 : 0)) * C::PART;
     for (int e = tid; e < nq * (D / 4); e += PA_THREADS) {
@@ -601,7 +657,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
         acc = axpy4(f, *reinterpret_cast<const float4*>(smem + i * C::RING + (r * C::O_PITCH + c) * 4), acc);
       }
       if (piece) {
-        *reinterpret_cast<float4*>(slot + 2 * RT + r * D + c) = acc;
+        *reinterpret_cast<float4*>(slot + C::HEAD + r * D + c) = acc;
         if (c == 0) *reinterpret_cast<float2*>(slot + 2 * r) = make_float2(M, L);
       } else {
         out.put(r, c, acc, M, L);
@@ -610,18 +666,19 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     if (piece) {
       constexpr long long STRIDE = 2ll * C::PART;
       float* all = a.part + (long long)c0 * STRIDE;                      // slot 0 of CTA c0; its own piece is in slot 1
-      float* wts = reinterpret_cast<float*>(smem);                       // the rings are free until the next segment
+      float2* prs = reinterpret_cast<float2*>(smem);                     // the rings are free until the next segment
+      float* wts = reinterpret_cast<float*>(smem + 32 * 1024);
       float2* mls = reinterpret_cast<float2*>(smem + 64 * 1024);
       if (parts <= 2 * JOIN) {
-        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, RT>(all, STRIDE, C::PART, parts, nq, wts, mls, out, nullptr);
+        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, C::HEAD, C::JOIN_LOADS>(all, STRIDE, C::PART, parts, nq, prs, wts, mls, out, nullptr);
       } else {
         const int groups = (parts + JOIN - 1) / JOIN, mygrp = ((int)cta - c0) / JOIN, lead = mygrp * JOIN;
         float* from = all + lead * STRIDE;
         const long long extra = lead == 0 ? C::PART : 0;
         if (arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(JOIN, parts - lead), &flag)) {
-          join<T, D, RT>(from, STRIDE, extra, min(JOIN, parts - lead), nq, wts, mls, out, from + extra);
+          join<T, D, C::HEAD, C::JOIN_LOADS>(from, STRIDE, extra, min(JOIN, parts - lead), nq, prs, wts, mls, out, from + extra);
           if (arrive_last(a.counters + 3 * c0 + 2, groups, &flag))
-            join<T, D, RT>(all, JOIN * STRIDE, C::PART, groups, nq, wts, mls, out, nullptr);
+            join<T, D, C::HEAD, C::JOIN_LOADS>(all, JOIN * STRIDE, C::PART, groups, nq, prs, wts, mls, out, nullptr);
         }
       }
     }
@@ -670,19 +727,24 @@ extern "C" focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shap
   a.K = cache->K; a.V = cache->V;
   a.st_page = cache->stride_page; a.st_tok = cache->stride_tok; a.st_head = cache->stride_head;
   a.table = cache->page_table; a.kv_len = cache->kv_len; a.row_start = row_start;
-  a.page = cache->page_size; a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+  a.page = cache->page_size; a.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (cache->page_size == 1 << i) a.page_shift = i;
+  a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
   a.L = shape->L; a.max_rows = max_rows; a.H = shape->n_q_heads; a.Hkv = shape->n_kv_heads; a.hpg = a.H / a.Hkv;
   a.scale = shape_scale(shape) * LOG2E;
   a.O = O; a.lse = lse; a.part = nullptr; a.counters = ctx->d_counters; a.status = ctx->d_status;
   const bool d128 = shape->head_dim == 128;
+  // stacked rows per sequence, on average where they are packed: the smallest tile that holds them
+  const long long rows = ((long long)max_rows * a.hpg + cache->n_seqs - 1) / cache->n_seqs;
+#define FOCUS_PA_LAUNCH(T, NT, ATTR) (d128 ? launch<T, 128, NT>(ctx, a, ATTR, stream) : launch<T, 64, NT>(ctx, a, ATTR + 1, stream))
   if (shape->dtype == FOCUS_F32) {
     ctx->last_attn_variant = 7;
-    return d128 ? launch<float, 128, 1>(ctx, a, 0, stream) : launch<float, 64, 1>(ctx, a, 1, stream);
+    if (rows <= 1) return FOCUS_PA_LAUNCH(float, 1, 0);
+    return rows <= 4 ? FOCUS_PA_LAUNCH(float, 4, 2) : FOCUS_PA_LAUNCH(float, 8, 4);
   }
   ctx->last_attn_variant = 6;
-  // stacked rows per sequence, on average where they are packed: the fewest N tiles that hold them
-  const long long rows = ((long long)max_rows * a.hpg + cache->n_seqs - 1) / cache->n_seqs;
-  if (rows <= 8) return d128 ? launch<__nv_bfloat16, 128, 1>(ctx, a, 2, stream) : launch<__nv_bfloat16, 64, 1>(ctx, a, 3, stream);
-  if (rows <= 16) return d128 ? launch<__nv_bfloat16, 128, 2>(ctx, a, 4, stream) : launch<__nv_bfloat16, 64, 2>(ctx, a, 5, stream);
-  return d128 ? launch<__nv_bfloat16, 128, 4>(ctx, a, 6, stream) : launch<__nv_bfloat16, 64, 4>(ctx, a, 7, stream);
+  if (rows <= 8) return FOCUS_PA_LAUNCH(__nv_bfloat16, 1, 6);
+  return rows <= 16 ? FOCUS_PA_LAUNCH(__nv_bfloat16, 2, 8) : FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
+#undef FOCUS_PA_LAUNCH
 }
