@@ -65,13 +65,13 @@ struct Cfg {
   static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
   static constexpr int HEAD = (2 * RT + 3) & ~3;                          // floats of a partial ahead of its rows (16-byte vectors)
   static constexpr int PART = HEAD + RT * D;                              // floats of one partial in the workspace
-  static constexpr int JOIN_LOADS = sizeof(T) == 2 && NT == 4 ? 4 : 10;    // vectors in flight per thread of a join (registers)
   static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
   static constexpr int OFF_Q = RING * PA_WARPS;
   static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][RT][KT]
   static constexpr int OFF_ML = OFF_P + (sizeof(T) == 4 ? PA_WARPS * RT * KT * 4 : 0);
   static constexpr int OFF_MASK = OFF_ML + PA_WARPS * RT * 8;
   static constexpr int SMEM = OFF_MASK + PA_WARPS * STAGES * 4;
+  static_assert(RING * PA_WARPS >= 96 * 1024, "a join uses that much of the rings");
   static_assert(RT * O_PITCH * 4 <= RING, "a warp's partial lies in its ring");
   static_assert(OFF_Q % 16 == 0 && OFF_P % 16 == 0 && OFF_ML % 8 == 0 && OFF_MASK % 4 == 0 && PART % 4 == 0 && O_PITCH % 4 == 0 &&
                 Q_PITCH * sizeof(T) % 16 == 0 && RING % 128 == 0, "alignment of vector accesses");
@@ -448,28 +448,33 @@ __device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& 
 __device__ __forceinline__ float part_weight(float m, float M) { return exp2f(m - M); }
 
 // Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
-// A thread's vectors of JOIN_LOADS partials are on their way while the weights are made: a join is two or three trips to L2.
-// pairs, wts: shared, nq * n (max, sum) pairs and weights; ml: the joined pairs.
-template <typename T, int D, int HEAD, int JOIN_LOADS>
-__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, float2* pairs,
-                                     float* wts, float2* ml, const Out<T, D>& out, float* dst) {
+// The rows come into the drained rings, as many at a time as fit, all of their bytes in flight at once: with loads into
+// registers one CTA moved 16 KB a microsecond, and the join of 16 partials of 32 rows took as long.
+constexpr int JOIN_DATA = 80 * 1024, JOIN_PAIRS = JOIN_DATA, JOIN_WTS = JOIN_DATA + 10 * 1024, JOIN_ML = JOIN_DATA + 15 * 1024;
+template <typename T, int D, int HEAD>
+__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, uint8_t* smem,
+                                     const Out<T, D>& out, float* dst) {
+  constexpr int ROW = D / 4;                                             // vectors of a row
+  float2* pairs = reinterpret_cast<float2*>(smem + JOIN_PAIRS);          // nq * n (max, sum) pairs
+  float* wts = reinterpret_cast<float*>(smem + JOIN_WTS);
+  float2* ml = reinterpret_cast<float2*>(smem + JOIN_ML);                // joined
   // the first partial of a segment lies in its CTA's other slot
   auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
-  const int items = nq * (D / 4);
-  float4 v[JOIN_LOADS];
-  auto fetch = [&](int e, int i0) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
-#pragma unroll
-    for (int k = 0; k < JOIN_LOADS; ++k)
-      if (i0 + k < n) v[k] = __ldcg(reinterpret_cast<const float4*>(at(i0 + k) + HEAD + r * D + c));
+  const int tid = threadIdx.x, some = min(nq, JOIN_DATA / (n * ROW * 16));
+  auto fetch = [&](int r0) {
+    const int cnt = min(some, nq - r0) * ROW;
+    for (int i = 0; i < n; ++i) {
+      const float* src = at(i) + HEAD + r0 * D;
+      for (int e = tid; e < cnt; e += PA_THREADS) copy16(smem_addr(smem) + (i * some * ROW + e) * 16, src + e * 4, true);
+    }
+    commit_group();
   };
-  int e = threadIdx.x;
-  if (e < items) fetch(e, 0);
-  for (int x = threadIdx.x; x < nq * n; x += PA_THREADS) pairs[x] = __ldcg(reinterpret_cast<const float2*>(at(x / nq)) + x % nq);
+  fetch(0);
+  for (int x = tid; x < nq * n; x += PA_THREADS) pairs[x] = __ldcg(reinterpret_cast<const float2*>(at(x / nq)) + x % nq);
   __syncthreads();
-  for (int x = threadIdx.x; x < nq * n; x += PA_THREADS) {
+  for (int x = tid; x < nq * n; x += PA_THREADS) {
     const int r = x % nq;
-    float M = -INFINITY;
+    float M = NO_KEYS;
     for (int i = 0; i < n; ++i) M = fmaxf(M, pairs[i * nq + r].x);
     wts[x] = part_weight(pairs[x].x, M);
     if (x < nq) {
@@ -478,22 +483,23 @@ __device__ __forceinline__ void join(const float* part, long long stride, long l
       ml[r] = make_float2(M, L);
     }
   }
-  __syncthreads();
-  for (; e < items; e += PA_THREADS) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < n; i0 += JOIN_LOADS) {
-      if (i0 > 0 || e >= PA_THREADS) fetch(e, i0);
-#pragma unroll
-      for (int k = 0; k < JOIN_LOADS; ++k)
-        if (i0 + k < n) acc = axpy4(wts[(i0 + k) * nq + r], v[k], acc);
+  for (int r0 = 0; r0 < nq; r0 += some) {
+    if (r0 > 0) fetch(r0);
+    wait_group<0>();
+    __syncthreads();
+    const int cnt = min(some, nq - r0) * ROW;
+    for (int e = tid; e < cnt; e += PA_THREADS) {
+      const int r = r0 + e / ROW, c = e % ROW * 4;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < n; ++i) acc = axpy4(wts[i * nq + r], *reinterpret_cast<const float4*>(smem + (i * some * ROW + e) * 16), acc);
+      if (dst) {
+        *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
+        if (c == 0) *reinterpret_cast<float2*>(dst + 2 * r) = ml[r];
+      } else {
+        out.put(r, c, acc, ml[r].x, ml[r].y);
+      }
     }
-    if (dst) {
-      *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
-      if (c == 0) *reinterpret_cast<float2*>(dst + 2 * r) = ml[r];
-    } else {
-      out.put(r, c, acc, ml[r].x, ml[r].y);
-    }
+    __syncthreads();
   }
 }
 
@@ -665,20 +671,17 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     }
     if (piece) {
       constexpr long long STRIDE = 2ll * C::PART;
-      float* all = a.part + (long long)c0 * STRIDE;                      // slot 0 of CTA c0; its own piece is in slot 1
-      float2* prs = reinterpret_cast<float2*>(smem);                     // the rings are free until the next segment
-      float* wts = reinterpret_cast<float*>(smem + 32 * 1024);
-      float2* mls = reinterpret_cast<float2*>(smem + 64 * 1024);
+      float* all = a.part + (long long)c0 * STRIDE;                      // slot 0 of CTA c0; its own piece is in slot 1.  The rings are free
       if (parts <= 2 * JOIN) {
-        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, C::HEAD, C::JOIN_LOADS>(all, STRIDE, C::PART, parts, nq, prs, wts, mls, out, nullptr);
+        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, C::HEAD>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
       } else {
         const int groups = (parts + JOIN - 1) / JOIN, mygrp = ((int)cta - c0) / JOIN, lead = mygrp * JOIN;
         float* from = all + lead * STRIDE;
         const long long extra = lead == 0 ? C::PART : 0;
         if (arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(JOIN, parts - lead), &flag)) {
-          join<T, D, C::HEAD, C::JOIN_LOADS>(from, STRIDE, extra, min(JOIN, parts - lead), nq, prs, wts, mls, out, from + extra);
+          join<T, D, C::HEAD>(from, STRIDE, extra, min(JOIN, parts - lead), nq, smem, out, from + extra);
           if (arrive_last(a.counters + 3 * c0 + 2, groups, &flag))
-            join<T, D, C::HEAD, C::JOIN_LOADS>(all, JOIN * STRIDE, C::PART, groups, nq, prs, wts, mls, out, nullptr);
+            join<T, D, C::HEAD>(all, JOIN * STRIDE, C::PART, groups, nq, smem, out, nullptr);
         }
       }
     }
