@@ -31,7 +31,9 @@ constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
 constexpr int KT = 16;                   // keys per tile
 constexpr int SEG_COST = 24;             // cost of a segment beside its tiles, in tiles: a ragged batch of 64 takes 163 us, 175 with 6
 constexpr int MIN_COST = 10;             // least cost per CTA: below, joining costs more than sharing gains
-constexpr int JOIN = 8;
+constexpr int JOIN = 8, JOIN_SMEM = 96 * 1024;
+constexpr int MAX_GRID = 296;            // a join of its groups' partials has room for that many / JOIN
+static_assert(3 * MAX_GRID <= FOCUS_N_COUNTERS, "three counters per CTA");
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_KEYS = -3.402823466e38f;   // running maximum of a row without keys so far: below every score, and finite
@@ -65,13 +67,14 @@ struct Cfg {
   static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
   static constexpr int HEAD = (2 * RT + 3) & ~3;                          // floats of a partial ahead of its rows (16-byte vectors)
   static constexpr int PART = HEAD + RT * D;                              // floats of one partial in the workspace
+  static constexpr int JOIN_ONCE = 2 * JOIN, JOIN_FEW = JOIN;             // partials joined in one go, and in a group of up to 4 JOIN
   static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
   static constexpr int OFF_Q = RING * PA_WARPS;
   static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][RT][KT]
   static constexpr int OFF_ML = OFF_P + (sizeof(T) == 4 ? PA_WARPS * RT * KT * 4 : 0);
   static constexpr int OFF_MASK = OFF_ML + PA_WARPS * RT * 8;
-  static constexpr int SMEM = OFF_MASK + PA_WARPS * STAGES * 4;
-  static_assert(RING * PA_WARPS >= 96 * 1024, "a join uses that much of the rings");
+  static constexpr int OFF_SCR = (OFF_MASK + PA_WARPS * STAGES * 4 + 15) & ~15, SMEM = OFF_SCR + RT * 24;
+  static_assert(RING * PA_WARPS >= JOIN_SMEM, "a join uses that much of the rings");
   static_assert(RT * O_PITCH * 4 <= RING, "a warp's partial lies in its ring");
   static_assert(OFF_Q % 16 == 0 && OFF_P % 16 == 0 && OFF_ML % 8 == 0 && OFF_MASK % 4 == 0 && PART % 4 == 0 && O_PITCH % 4 == 0 &&
                 Q_PITCH * sizeof(T) % 16 == 0 && RING % 128 == 0, "alignment of vector accesses");
@@ -154,10 +157,10 @@ __device__ __forceinline__ long long divide(long long n, long long d) {
   return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
-// a tile's K and V rows into one stage: row k at k * ROW_BYTES, its 16-byte chunk c at place c ^ (k & 7)
+// a tile's K rows to dst and its V rows to dst + v_off: row k at k * ROW_BYTES, its 16-byte chunk c at place c ^ (k & 7)
 template <typename T, int D>
-__device__ __forceinline__ void load_tile(const PagedArgs& a, const T* K, const T* V, long long off, uint32_t dst, int lane) {
-  constexpr int CPR = D * (int)sizeof(T) / 16, KPI = 32 / CPR, OPERAND = KT * D * (int)sizeof(T);
+__device__ __forceinline__ void load_tile(const PagedArgs& a, const T* K, const T* V, long long off, uint32_t dst, int v_off, int lane) {
+  constexpr int CPR = D * (int)sizeof(T) / 16, KPI = 32 / CPR;
   const int c = lane % CPR;
 #pragma unroll
   for (int i = 0; i < KT / KPI; ++i) {
@@ -167,7 +170,7 @@ __device__ __forceinline__ void load_tile(const PagedArgs& a, const T* K, const 
     const long long e = (valid ? o : 0) + c * (16 / (int)sizeof(T));
     const uint32_t d = dst + k * (CPR * 16) + ((c ^ (k & 7)) << 4);
     copy16(d, K + e, valid);
-    copy16(d + OPERAND, V + e, valid);
+    copy16(d + v_off, V + e, valid);
   }
 }
 
@@ -205,31 +208,44 @@ struct Core<__nv_bfloat16, D, NT> {
     }
   }
 
-  __device__ __forceinline__ void tile(uint32_t ks, uint32_t mask, float scale, int lane) {
+  __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, uint32_t mask, float scale, int lane) {
     float s[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    // all fragments of an operand are requested before the first product that uses them
+    uint32_t f[KS][4];
     {
       const int key = lane & 15;
       const uint32_t row = ks + key * RB;
 #pragma unroll
+      for (int k = 0; k < KS; ++k) ldmatrix4(f[k], row + (((2 * k + (lane >> 4)) ^ (key & 7)) << 4));
+    }
+    if constexpr (Q_IN_REGS) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma16816(s[n], f[k], q[n][k][0], q[n][k][1]);
+    } else {
+      constexpr int P = (D + 8) * 2;
+      const uint32_t at = q_addr + ((lane & 7) + (lane >> 4) * 8) * P + ((lane >> 3) & 1) * 16;
+      uint32_t b[2][NT / 2][4];
+#pragma unroll
+      for (int n = 0; n < NT; n += 2) ldmatrix4(b[0][n / 2], at + n * 8 * P);
+#pragma unroll
       for (int k = 0; k < KS; ++k) {
-        uint32_t a[4];
-        ldmatrix4(a, row + (((2 * k + (lane >> 4)) ^ (key & 7)) << 4));
-        if constexpr (Q_IN_REGS) {
+        if (k + 1 < KS) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma16816(s[n], a, q[n][k][0], q[n][k][1]);
-        } else {
-          constexpr int P = (D + 8) * 2;
-#pragma unroll
-          for (int n = 0; n < NT; n += 2) {
-            uint32_t b[4];
-            ldmatrix4(b, q_addr + (n * 8 + (lane & 7) + (lane >> 4) * 8) * P + k * 32 + ((lane >> 3) & 1) * 16);
-            mma16816(s[n], a, b[0], b[1]);
-            mma16816(s[n + 1], a, b[2], b[3]);
-          }
+          for (int n = 0; n < NT; n += 2) ldmatrix4(b[(k + 1) & 1][n / 2], at + n * 8 * P + (k + 1) * 32);
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma16816(s[n], f[k], b[k & 1][n / 2][n % 2 * 2], b[k & 1][n / 2][n % 2 * 2 + 1]);
       }
+    }
+    {
+      const int key = (lane & 7) + ((lane >> 4) << 3);
+      const uint32_t row = vs + key * RB;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) ldmatrix4_t(f[i], row + (((2 * i + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
     }
     const bool lo = (mask >> (lane >> 2)) & 1u, hi = (mask >> ((lane >> 2) + 8)) & 1u;
     float x[NT][4], top = NO_KEYS;       // exponents, relative to m
@@ -279,15 +295,10 @@ struct Core<__nv_bfloat16, D, NT> {
       b[n][0] = transpose8(pack_bf16(s[n][0], s[n][1]));
       b[n][1] = transpose8(pack_bf16(s[n][2], s[n][3]));
     }
-    const int key = (lane & 7) + ((lane >> 4) << 3);
-    const uint32_t row = ks + KT * RB + key * RB;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      uint32_t a[4];
-      ldmatrix4_t(a, row + (((2 * i + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
+    for (int i = 0; i < KS; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) mma16816(o[i][n], a, b[n][0], b[n][1]);
-    }
+      for (int n = 0; n < NT; ++n) mma16816(o[i][n], f[i], b[n][0], b[n][1]);
   }
 
   // (max, sum) and unnormalised O of the first nq rows
@@ -328,7 +339,7 @@ struct Core<float, D, R> {
     }
   }
 
-  __device__ __forceinline__ void tile(uint32_t ks, uint32_t mask, float scale, int lane) {
+  __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, uint32_t mask, float scale, int lane) {
     const int key = lane & 15, half = lane >> 4;
     float s[R];
 #pragma unroll
@@ -379,14 +390,13 @@ struct Core<float, D, R> {
       for (int r = 0; r < R / 2; ++r) p[(half * (R / 2) + r) * KT + key] = half ? s[r + R / 2] : s[r];
     }
     __syncwarp();
-    const uint32_t v0 = ks + KT * RB;
 #pragma unroll
     for (int k4 = 0; k4 < KT / 4; ++k4) {
       float v[4][CV];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int kk = k4 * 4 + k, c = lane * CV / 4;
-        const uint32_t at = v0 + kk * RB + ((c ^ (kk & 7)) << 4) + (lane * CV % 4) * 4;
+        const uint32_t at = vs + kk * RB + ((c ^ (kk & 7)) << 4) + (lane * CV % 4) * 4;
         if constexpr (CV == 4)
           asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[k][0]), "=f"(v[k][1]), "=f"(v[k][CV - 2]), "=f"(v[k][CV - 1])
                        : "r"(at) : "memory");
@@ -431,15 +441,27 @@ struct Out {                             // where the stacked rows of a segment 
     out_row = first + (q0 + r) / hpg;
     head = g * hpg + (q0 + r) % hpg;
   }
-  // columns c .. c + 3 of row r, whose numerators' sum is l; -inf maximum: nothing attended
-  __device__ __forceinline__ void put(int r, int c, float4 v, float m, float l) const {
+  // where row r lies in O; its lse is written
+  __device__ __forceinline__ long long place(int r, float m, float l) const {
     int i, h;
     row(r, i, h);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    put4(O + ((long long)i * H + h) * D + c, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-    if (lse && c == 0) lse[(long long)h * max_rows + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (lse) lse[(long long)h * max_rows + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    return ((long long)i * H + h) * D;
   }
 };
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }   // 0: nothing attended, the row is 0
+
+// rows without keys
+template <typename T, int D>
+__device__ __forceinline__ void put_zeros(const Out<T, D>& out, int nq) {
+  for (int e = threadIdx.x; e < nq * (D / 4); e += PA_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    int i, h;
+    out.row(r, i, h);
+    put4(out.O + ((long long)i * out.H + h) * D + c, make_float4(0.f, 0.f, 0.f, 0.f));
+    if (c == 0) out.place(r, 0.f, 0.f);
+  }
+}
 
 __device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& y) {
   return make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w));
@@ -447,25 +469,61 @@ __device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& 
 // weight of a part with maximum m where the largest is M; a part without keys has the sum 0
 __device__ __forceinline__ float part_weight(float m, float M) { return exp2f(m - M); }
 
+// The warps' parts of nq rows into O, or, for a piece of a segment, into its slot.  Part k of row r: (max, sum) at
+// ML[k * kml + r], numerators at os + k * kos + r * (D + 4).  scr: RT weights per part, then RT places.
+template <typename T, int D, int RT, int HEAD>
+__device__ __forceinline__ void merge(const float2* ML, int kml, const float* os, int kos, int parts, int nq, bool piece, float* slot,
+                                      uint8_t* scr, const Out<T, D>& out) {
+  float* wt = reinterpret_cast<float*>(scr);
+  long long* place = reinterpret_cast<long long*>(scr + 4 * RT * sizeof(float));
+  for (int r = threadIdx.x; r < nq; r += PA_THREADS) {
+    float M = NO_KEYS, L = 0.f, f[4];
+    for (int k = 0; k < parts; ++k) M = fmaxf(M, ML[k * kml + r].x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < parts) {
+        const float2 ml = ML[k * kml + r];
+        f[k] = part_weight(ml.x, M);
+        L = fmaf(f[k], ml.y, L);
+      }
+    const float inv = piece ? 1.f : inverse(L);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < parts) wt[k * RT + r] = f[k] * inv;
+    if (piece) *reinterpret_cast<float2*>(slot + 2 * r) = make_float2(M, L);
+    else place[r] = out.place(r, M, L);
+  }
+  __syncthreads();
+#pragma unroll 2
+  for (int e = threadIdx.x; e < nq * (D / 4); e += PA_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < parts; ++k)
+      acc = axpy4(wt[k * RT + r], *reinterpret_cast<const float4*>(os + k * kos + r * (D + 4) + c), acc);
+    if (piece) *reinterpret_cast<float4*>(slot + HEAD + r * D + c) = acc;
+    else put4(out.O + place[r] + c, acc);
+  }
+}
+
 // Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
 // The rows come into the drained rings, as many at a time as fit, all of their bytes in flight at once: with loads into
 // registers one CTA moved 16 KB a microsecond, and the join of 16 partials of 32 rows took as long.
-constexpr int JOIN_DATA = 80 * 1024, JOIN_PAIRS = JOIN_DATA, JOIN_WTS = JOIN_DATA + 10 * 1024, JOIN_ML = JOIN_DATA + 15 * 1024;
 template <typename T, int D, int HEAD>
 __device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, uint8_t* smem,
                                      const Out<T, D>& out, float* dst) {
   constexpr int ROW = D / 4;                                             // vectors of a row
-  float2* pairs = reinterpret_cast<float2*>(smem + JOIN_PAIRS);          // nq * n (max, sum) pairs
-  float* wts = reinterpret_cast<float*>(smem + JOIN_WTS);
-  float2* ml = reinterpret_cast<float2*>(smem + JOIN_ML);                // joined
+  float2* pairs = reinterpret_cast<float2*>(smem);                       // nq * n (max, sum) pairs, the rows' places in O, the weights
+  long long* place = reinterpret_cast<long long*>(pairs + nq * n);
+  float* wts = reinterpret_cast<float*>(place + nq);
+  uint8_t* data = smem + ((nq * n * 12 + nq * 8 + 127) & ~127);          // at most 58 KB on: 128 rows of 37 partials
   // the first partial of a segment lies in its CTA's other slot
   auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
-  const int tid = threadIdx.x, some = min(nq, JOIN_DATA / (n * ROW * 16));
+  const int tid = threadIdx.x, some = min(nq, (JOIN_SMEM - (int)(data - smem)) / (n * ROW * 16));
   auto fetch = [&](int r0) {
     const int cnt = min(some, nq - r0) * ROW;
     for (int i = 0; i < n; ++i) {
       const float* src = at(i) + HEAD + r0 * D;
-      for (int e = tid; e < cnt; e += PA_THREADS) copy16(smem_addr(smem) + (i * some * ROW + e) * 16, src + e * 4, true);
+      for (int e = tid; e < cnt; e += PA_THREADS) copy16(smem_addr(data) + (i * some * ROW + e) * 16, src + e * 4, true);
     }
     commit_group();
   };
@@ -474,13 +532,13 @@ __device__ __forceinline__ void join(const float* part, long long stride, long l
   __syncthreads();
   for (int x = tid; x < nq * n; x += PA_THREADS) {
     const int r = x % nq;
-    float M = NO_KEYS;
+    float M = NO_KEYS, L = 0.f;
     for (int i = 0; i < n; ++i) M = fmaxf(M, pairs[i * nq + r].x);
-    wts[x] = part_weight(pairs[x].x, M);
+    for (int i = 0; i < n; ++i) L = fmaf(part_weight(pairs[i * nq + r].x, M), pairs[i * nq + r].y, L);
+    wts[x] = part_weight(pairs[x].x, M) * (dst ? 1.f : inverse(L));
     if (x < nq) {
-      float L = 0.f;
-      for (int i = 0; i < n; ++i) L = fmaf(part_weight(pairs[i * nq + r].x, M), pairs[i * nq + r].y, L);
-      ml[r] = make_float2(M, L);
+      if (dst) *reinterpret_cast<float2*>(dst + 2 * r) = make_float2(M, L);
+      else place[r] = out.place(r, M, L);
     }
   }
   for (int r0 = 0; r0 < nq; r0 += some) {
@@ -491,20 +549,17 @@ __device__ __forceinline__ void join(const float* part, long long stride, long l
     for (int e = tid; e < cnt; e += PA_THREADS) {
       const int r = r0 + e / ROW, c = e % ROW * 4;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < n; ++i) acc = axpy4(wts[i * nq + r], *reinterpret_cast<const float4*>(smem + (i * some * ROW + e) * 16), acc);
-      if (dst) {
-        *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
-        if (c == 0) *reinterpret_cast<float2*>(dst + 2 * r) = ml[r];
-      } else {
-        out.put(r, c, acc, ml[r].x, ml[r].y);
-      }
+      for (int i = 0; i < n; ++i) acc = axpy4(wts[i * nq + r], *reinterpret_cast<const float4*>(data + (i * some * ROW + e) * 16), acc);
+      if (dst) *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
+      else put4(out.O + place[r] + c, acc);
     }
     __syncthreads();
   }
 }
 
 // true in every thread of the CTA that is the last of n to arrive
-__device__ __forceinline__ bool arrive_last(int32_t* counter, int n, int* flag) {
+__device__ __forceinline__ bool arrive_last(int32_t* counter, int n) {
+  __shared__ int flag;
   __syncthreads();                       // every thread's part of the partial is written
   if (threadIdx.x == 0) {
     __threadfence();                     // and visible before the arrival
@@ -513,30 +568,45 @@ __device__ __forceinline__ bool arrive_last(int32_t* counter, int n, int* flag) 
       *counter = 0;                      // ready for the next launch
       __threadfence();
     }
-    *flag = last;
+    flag = last;
   }
   __syncthreads();
-  return *flag;
+  return flag;
 }
 
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_kernel(const PagedArgs a) {
-  using C = Cfg<T, D, NT>;
-  constexpr int RT = C::RT;
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long scan[PA_WARPS + 1];
-  __shared__ long long start_base;
-  __shared__ int start_seq, flag;
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  T* Qs = reinterpret_cast<T*>(smem + C::OFF_Q);
-  float2* ML = reinterpret_cast<float2*>(smem + C::OFF_ML);              // [warp][RT]
-  uint32_t* masks = reinterpret_cast<uint32_t*>(smem + C::OFF_MASK) + w * C::STAGES;
-  const uint32_t ring = smem_addr(smem) + w * C::RING;
+// a piece of a segment that the CTAs c0 .. c0 + parts - 1 share is in the workspace: the last to arrive joins them
+template <typename T, int D, typename C>
+__device__ __forceinline__ void finish_piece(const PagedArgs& a, int cta, int c0, int parts, int nq, uint8_t* smem, const Out<T, D>& out) {
+  constexpr long long STRIDE = 2ll * C::PART;
+  float* all = a.part + (long long)c0 * STRIDE;                          // slot 0 of CTA c0; its own piece is in slot 1
+  if (parts <= C::JOIN_ONCE) {
+    if (arrive_last(a.counters + 3 * c0, parts)) join<T, D, C::HEAD>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
+    return;
+  }
+  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN, groups = (parts + J - 1) / J, lead = (cta - c0) / J * J;
+  float* from = all + lead * STRIDE;
+  const long long extra = lead == 0 ? C::PART : 0;
+  if (!arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(J, parts - lead))) return;
+  join<T, D, C::HEAD>(from, STRIDE, extra, min(J, parts - lead), nq, smem, out, from + extra);
+  if (arrive_last(a.counters + 3 * c0 + 2, groups))
+    join<T, D, C::HEAD>(all, J * STRIDE, C::PART, groups, nq, smem, out, nullptr);
+}
 
-  // ---- the split: total cost, this CTA's stretch and where it starts
+// A CTA's share of the work: the total cost of the sequences, the CTAs that take part, this one's stretch [p0, p1) and the
+// sequence in which it starts, whose cost begins at `base`.
+struct Stretch {
+  long long total, G, p0, p1, base;
+  int s;
+};
+// false where this CTA has nothing to do; called by all threads
+template <typename Cost>
+__device__ __forceinline__ bool stretch_of(const PagedArgs& a, Cost cost_of, Stretch& st) {
+  __shared__ long long scan[PA_WARPS], start_base;
+  __shared__ int start_seq;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int per = (a.n_seqs + PA_THREADS - 1) / PA_THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
   long long mine = 0;
-  for (int s = s0; s < s1; ++s) mine += seq_cost(seq_of<RT>(a, s), a.Hkv);
+  for (int s = s0; s < s1; ++s) mine += cost_of(s);
   long long incl = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -552,27 +622,48 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     if (i < w) before += scan[i];
     total += scan[i];
   }
-  if (total == 0) return;
-  const long long G = min((long long)gridDim.x, max(1ll, total / MIN_COST)), cta = blockIdx.x;
-  if (cta >= G) return;
-  const long long p0 = divide(cta * total, G), p1 = divide((cta + 1) * total, G);
-  {
-    long long at = before + incl - mine;
-    if (p0 >= at && p0 < at + mine) {
-      int s = s0;
-      for (; s < s1; ++s) {
-        const long long c = seq_cost(seq_of<RT>(a, s), a.Hkv);
-        if (p0 < at + c) break;
-        at += c;
-      }
-      start_seq = s;
-      start_base = at;
+  if (total == 0) return false;
+  st.total = total;
+  st.G = min((long long)gridDim.x, max(1ll, total / MIN_COST));
+  const long long cta = blockIdx.x;
+  if (cta >= st.G) return false;
+  st.p0 = divide(cta * total, st.G);
+  st.p1 = divide((cta + 1) * total, st.G);
+  long long at = before + incl - mine;
+  if (st.p0 >= at && st.p0 < at + mine) {
+    int s = s0;
+    for (; s < s1; ++s) {
+      const long long c = cost_of(s);
+      if (st.p0 < at + c) break;
+      at += c;
     }
+    start_seq = s;
+    start_base = at;
   }
   __syncthreads();
+  st.s = start_seq;
+  st.base = start_base;
+  return true;
+}
 
-  int s = start_seq;
-  long long base = start_base, p = p0;
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_kernel(const PagedArgs a) {
+  using C = Cfg<T, D, NT>;
+  constexpr int RT = C::RT;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  T* Qs = reinterpret_cast<T*>(smem + C::OFF_Q);
+  float2* ML = reinterpret_cast<float2*>(smem + C::OFF_ML);              // [warp][RT]
+  uint32_t* masks = reinterpret_cast<uint32_t*>(smem + C::OFF_MASK) + w * C::STAGES;
+  const uint32_t ring = smem_addr(smem) + w * C::RING;
+
+  Stretch st;
+  if (!stretch_of(a, [&](int s) { return seq_cost(seq_of<RT>(a, s), a.Hkv); }, st)) return;
+  const long long total = st.total, G = st.G, p0 = st.p0, p1 = st.p1;
+  const int cta = blockIdx.x;
+
+  int s = st.s;
+  long long base = st.base, p = p0;
   while (p < p1 && s < a.n_seqs) {
     const Seq q = seq_of<RT>(a, s);
     const int cost = seg_cost(q), tiles = cost - SEG_COST;
@@ -584,10 +675,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     const int nq = (int)min((long long)RT, (long long)q.rows * a.hpg - q0);
     const Out<T, D> out{(T*)a.O, a.lse, a.H, a.hpg, q.first, g, q0, a.max_rows};
     const int t_lo = (int)max(0ll, p - first_tile), t_hi = (int)min((long long)tiles, p1 - first_tile);
-    if (tiles == 0 && p == seg_at) {     // no keys: its first unit's CTA writes the row
-      for (int e = tid; e < nq * (D / 4); e += PA_THREADS)
-        out.put(e / (D / 4), e % (D / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f);
-    }
+    if (tiles == 0 && p == seg_at) put_zeros(out, nq);                   // no keys: its first unit's CTA writes the rows
     p = min(p1, seg_at + cost);
     if (t_hi <= t_lo) continue;
 
@@ -615,7 +703,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
         const long long off = key_offset(a, q.len, t_load, from, lane);
         const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
         if (lane == 0) masks[stage] = mask;
-        load_tile<T, D>(a, K, V, off, ring + stage * C::STAGE, lane);
+        load_tile<T, D>(a, K, V, off, ring + stage * C::STAGE, C::OPERAND, lane);
         t_load += PA_WARPS;
       }
       commit_group();
@@ -637,7 +725,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
       __syncwarp();                      // every lane's copies are there, and nobody reads the stage refilled next
       fetch(stage == 0 ? C::STAGES - 1 : stage - 1, ahead);
       ahead = key_page(a, s, q.len, t_load, t_hi, lane);
-      core.tile(ring + stage * C::STAGE, masks[stage], a.scale, lane);
+      core.tile(ring + stage * C::STAGE, ring + stage * C::STAGE + C::OPERAND, masks[stage], a.scale, lane);
       stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     }
     wait_group<0>();
@@ -650,61 +738,31 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     auto cta_of = [&](long long pos) { return (int)divide((pos + 1) * G - 1, total); };
     const int c0 = piece ? cta_of(first_tile) : 0, parts = piece ? cta_of(first_tile + tiles - 1) - c0 + 1 : 1;
     float* slot = a.part + ((long long)cta * 2 + (cta == c0 ? 1 : 0)) * C::PART;
-    for (int e = tid; e < nq * (D / 4); e += PA_THREADS) {
-      const int r = e / (D / 4), c = e % (D / 4) * 4;
-      float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int i = 0; i < PA_WARPS; ++i) M = fmaxf(M, ML[i * RT + r].x);
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < PA_WARPS; ++i) {
-        const float f = part_weight(ML[i * RT + r].x, M);
-        L = fmaf(f, ML[i * RT + r].y, L);
-        acc = axpy4(f, *reinterpret_cast<const float4*>(smem + i * C::RING + (r * C::O_PITCH + c) * 4), acc);
-      }
-      if (piece) {
-        *reinterpret_cast<float4*>(slot + C::HEAD + r * D + c) = acc;
-        if (c == 0) *reinterpret_cast<float2*>(slot + 2 * r) = make_float2(M, L);
-      } else {
-        out.put(r, c, acc, M, L);
-      }
-    }
-    if (piece) {
-      constexpr long long STRIDE = 2ll * C::PART;
-      float* all = a.part + (long long)c0 * STRIDE;                      // slot 0 of CTA c0; its own piece is in slot 1.  The rings are free
-      if (parts <= 2 * JOIN) {
-        if (arrive_last(a.counters + 3 * c0, parts, &flag)) join<T, D, C::HEAD>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
-      } else {
-        const int groups = (parts + JOIN - 1) / JOIN, mygrp = ((int)cta - c0) / JOIN, lead = mygrp * JOIN;
-        float* from = all + lead * STRIDE;
-        const long long extra = lead == 0 ? C::PART : 0;
-        if (arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(JOIN, parts - lead), &flag)) {
-          join<T, D, C::HEAD>(from, STRIDE, extra, min(JOIN, parts - lead), nq, smem, out, from + extra);
-          if (arrive_last(a.counters + 3 * c0 + 2, groups, &flag))
-            join<T, D, C::HEAD>(all, JOIN * STRIDE, C::PART, groups, nq, smem, out, nullptr);
-        }
-      }
-    }
+    merge<T, D, RT, C::HEAD>(ML, RT, reinterpret_cast<const float*>(smem), C::RING / 4, PA_WARPS, nq, piece, slot,
+                             smem + C::OFF_SCR, out);
+    if (piece) finish_piece<T, D, C>(a, cta, c0, parts, nq, smem, out);
     __syncthreads();                     // rings, queries and (max, sum) pairs are read out
   }
 }
 
-template <typename T, int D, int NT>
-focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
-  using C = Cfg<T, D, NT>;
+template <typename C, typename Kernel>
+focus_status launch_kernel(focus_ctx* ctx, PagedArgs& a, Kernel kernel, int ctas, int attr, cudaStream_t st) {
   if (!ctx->ls.paged_attr_set[attr]) {
-    if (cudaFuncSetAttribute(paged_attn_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
-      return FOCUS_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return FOCUS_ERR_CUDA;
     ctx->ls.paged_attr_set[attr] = true;
   }
-  const int grid = C::CTAS * ctx->sm_count;
-  if (3 * grid > FOCUS_N_COUNTERS) return FOCUS_ERR_UNSUPPORTED;
+  const int grid = ctas * ctx->sm_count;
+  if (grid > MAX_GRID) return FOCUS_ERR_UNSUPPORTED;
   WsAlloc ws(ctx);
   a.part = ws.get<float>((size_t)grid * 2 * C::PART);
   if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
-  paged_attn_kernel<T, D, NT><<<grid, PA_THREADS, C::SMEM, st>>>(a);
+  kernel<<<grid, PA_THREADS, C::SMEM, st>>>(a);
   FOCUS_CHECK_LAUNCH();
   return FOCUS_OK;
+}
+template <typename T, int D, int NT>
+focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
+  return launch_kernel<Cfg<T, D, NT>>(ctx, a, paged_attn_kernel<T, D, NT>, Cfg<T, D, NT>::CTAS, attr, st);
 }
 
 }  // namespace
@@ -748,6 +806,7 @@ extern "C" focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shap
   }
   ctx->last_attn_variant = 6;
   if (rows <= 8) return FOCUS_PA_LAUNCH(__nv_bfloat16, 1, 6);
-  return rows <= 16 ? FOCUS_PA_LAUNCH(__nv_bfloat16, 2, 8) : FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
+  if (rows <= 16) return FOCUS_PA_LAUNCH(__nv_bfloat16, 2, 8);
+  return FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
 #undef FOCUS_PA_LAUNCH
 }

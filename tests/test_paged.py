@@ -422,6 +422,9 @@ def check_attention(c, n, Q, O, ls, H, scale):
     ("bf16", 28, 4, 128, 64, [500, 40, 0, 7], [35, 1, 3, 0], False),         # windows, rows without keys, keys without rows
     ("bf16", 5, 5, 64, 16, [333, 20], [64, 2], True),
     ("bf16", 3, 1, 128, 8, [90, 0, 12], [0, 0, 1], False),
+    ("bf16", 28, 4, 128, 16, [900, 2000, 64, 63, 0, 1], [19, 37, 9, 5, 20, 18], False),      # 133, 259, 63, 35, 140, 126 stacked rows
+    ("bf16", 6, 2, 64, 48, [3000, 129, 700], [128, 11, 85], True),            # 384, 33, 255
+    ("bf16", 4, 4, 128, 5, [1, 64, 65, 250], [300, 96, 32, 1], False),
     ("f32", 8, 8, 64, 32, [1024, 1, 37, 0, 500], None, False),
     ("f32", 12, 4, 128, 3, [200, 17, 0], [4, 9, 1], True),
     ("f32", 40, 1, 128, 16, [77, 2500], None, False),
@@ -439,6 +442,8 @@ def test_long_sequences_are_split_and_joined(ctx, dtype):
     for lengths, H, Hkv, gain in (([20011], 2, 1, 1.0), ([9000, 5, 7001], 8, 2, 6.0), ([700] * 90, 4, 2, 1.0)):
         attend_case(ctx, dtype, H, Hkv, 128, 64, lengths, None, gain=gain)
         attend_case(ctx, dtype, H, Hkv, 64, 16, lengths, None, gain=gain, lse=False)
+    attend_case(ctx, dtype, 8, 1, 128, 32, [9000, 300], [14, 3])
+    attend_case(ctx, dtype, 4, 1, 64, 64, [15000], [10], gain=6.0)
     assert ctx.poll_status() == 0
 
 
