@@ -173,7 +173,8 @@ uint64_t focus_launch_count(void);
  * two query tiles per CTA (taken for >= 256 stacked rows per KV head and >= 24 key tiles per CTA), 4 = tensor-core
  * kernel with one query tile and two softmax warpgroups on alternating key tiles (>= 128 stacked rows per KV head
  * and >= 4 key tiles per CTA, where 3 does not apply), 5 = the tensor-core kernel for 8-bit caches (the two
- * _quantized calls on bf16 queries); 6 = focus_paged_attn on bf16, 7 = on fp32; 0 = none yet. */
+ * _quantized calls on bf16 queries); 6 = focus_paged_attn on bf16 with up to 32 stacked rows per sequence
+ * and KV head, 7 = on fp32, 8 = on bf16 with more; 0 = none yet. */
 int32_t focus_last_attn_variant(focus_ctx* ctx);
 
 /* Selects the attention implementation for bf16 inputs (head_dim 128 or 64): 0 = automatic (tensor-core

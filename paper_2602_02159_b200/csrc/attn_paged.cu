@@ -21,41 +21,17 @@
 // M = 128 keys per instruction and its scores come back through TMEM: latency, where bytes are the bound.)  A tile's row
 // statistics are shuffles over the lanes that hold its keys; P^T becomes the B operand by movmatrix.
 // fp32: fp32 products on the CUDA cores, a lane per key (and half row) for the scores, per column for the values.
-#include <math.h>
+#include "attn_paged.cuh"
 
-#include "focus_common.cuh"
+using namespace paged;
 
 namespace {
 
-constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
 constexpr int KT = 16;                   // keys per tile
 constexpr int SEG_COST = 24;             // cost of a segment beside its tiles, in tiles: a ragged batch of 64 takes 163 us, 175 with 6
 constexpr int MIN_COST = 10;             // least cost per CTA: below, joining costs more than sharing gains
-constexpr int JOIN = 8, JOIN_SMEM = 96 * 1024;
-constexpr int MAX_GRID = 296;            // a join of its groups' partials has room for that many / JOIN
-static_assert(3 * MAX_GRID <= FOCUS_N_COUNTERS, "three counters per CTA");
-
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float NO_KEYS = -3.402823466e38f;   // running maximum of a row without keys so far: below every score, and finite
 constexpr float LAZY = 8.f;              // the running maximum may lag by this much (base 2): numerators stay below 2^8
 
-struct PagedArgs {
-  const void* Q;
-  long long q_row, q_head;
-  const void* K;
-  const void* V;
-  long long st_page, st_tok, st_head;
-  const int32_t* table;
-  const int32_t* kv_len;
-  const int32_t* row_start;
-  int page, page_shift, n_pages, n_seqs, max_pages, L, max_rows, H, Hkv, hpg;   // page_shift: its logarithm, or -1
-  float scale;                           // softmax scale * log2 e
-  void* O;
-  float* lse;
-  float* part;                           // [gridDim.x][2] partials: (max, sum) pairs of RT rows, then the rows
-  int32_t* counters;                     // 3 per CTA, zero between launches
-  int32_t* status;
-};
 
 template <typename T, int D, int NT>
 struct Cfg {
@@ -67,7 +43,7 @@ struct Cfg {
   static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
   static constexpr int HEAD = (2 * RT + 3) & ~3;                          // floats of a partial ahead of its rows (16-byte vectors)
   static constexpr int PART = HEAD + RT * D;                              // floats of one partial in the workspace
-  static constexpr int JOIN_ONCE = 2 * JOIN, JOIN_FEW = JOIN;             // partials joined in one go, and in a group of up to 4 JOIN
+  static constexpr int JOIN_ONCE = 2 * JOIN, JOIN_FEW = JOIN, JOIN_SMEM = 96 * 1024;   // see finish_piece
   static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
   static constexpr int OFF_Q = RING * PA_WARPS;
   static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][RT][KT]
@@ -80,12 +56,6 @@ struct Cfg {
                 Q_PITCH * sizeof(T) % 16 == 0 && RING % 128 == 0, "alignment of vector accesses");
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool valid) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void commit_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -109,53 +79,9 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&b);
-}
-
-struct Seq {
-  int len, first, rows, row_tiles;       // tokens; first new row, how many; tiles of stacked rows
-};
-
-template <int RT>
-__device__ __forceinline__ Seq seq_of(const PagedArgs& a, int s) {
-  Seq q;
-  q.len = a.kv_len[s];
-  if (q.len < 0 || q.len > a.L) {
-    set_status(a.status, FOCUS_ERR_INVALID_ARG);
-    q.len = q.len < 0 ? 0 : a.L;
-  }
-  q.first = s; q.rows = 1;
-  if (a.row_start) {
-    const int lo = a.row_start[s], hi = a.row_start[s + 1];
-    q.first = lo; q.rows = hi - lo;
-    if (lo < 0 || hi < lo || hi > a.max_rows) { set_status(a.status, FOCUS_ERR_INVALID_ARG); q.rows = 0; }
-  }
-  q.row_tiles = (int)(((long long)q.rows * a.hpg + RT - 1) / RT);
-  return q;
-}
 __device__ __forceinline__ int seg_cost(const Seq& q) { return (q.len + KT - 1) / KT + SEG_COST; }
 __device__ __forceinline__ long long seq_cost(const Seq& q, int Hkv) { return (long long)seg_cost(q) * q.row_tiles * Hkv; }
 
-// the place of key j in its sequence's pages
-__device__ __forceinline__ int page_of(const PagedArgs& a, int j) { return a.page_shift >= 0 ? j >> a.page_shift : j / a.page; }
-// Lane l has key 16 t + (l & 15) of tile t: its page, as the table has it (-1 where the tile or the sequence has ended), and
-// then where in the pools it lies, -1 where there is nothing to attend.
-__device__ __forceinline__ int key_page(const PagedArgs& a, int s, int len, int t, int t_hi, int lane) {
-  const int j = t * KT + (lane & 15);
-  return t < t_hi && j < len ? a.table[(long long)s * a.max_pages + page_of(a, j)] : -1;
-}
-__device__ __forceinline__ long long key_offset(const PagedArgs& a, int len, int t, int page, int lane) {
-  const int j = t * KT + (lane & 15);
-  if (j >= len) return -1;
-  if (page < 0 || page >= a.n_pages) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return -1; }
-  return (long long)page * a.st_page + (long long)(j - page_of(a, j) * a.page) * a.st_tok;
-}
-// non-negative; most are small
-__device__ __forceinline__ long long divide(long long n, long long d) {
-  return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
-}
 
 // a tile's K rows to dst and its V rows to dst + v_off: row k at k * ROW_BYTES, its 16-byte chunk c at place c ^ (k & 7)
 template <typename T, int D>
@@ -426,49 +352,6 @@ struct Core<float, D, R> {
   }
 };
 
-// four neighbouring columns of one row into O
-__device__ __forceinline__ void put4(__nv_bfloat16* o, const float4& v) {
-  *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-}
-__device__ __forceinline__ void put4(float* o, const float4& v) { *reinterpret_cast<float4*>(o) = v; }
-
-template <typename T, int D>
-struct Out {                             // where the stacked rows of a segment go
-  T* O;
-  float* lse;
-  int H, hpg, first, g, q0, max_rows;
-  __device__ __forceinline__ void row(int r, int& out_row, int& head) const {
-    out_row = first + (q0 + r) / hpg;
-    head = g * hpg + (q0 + r) % hpg;
-  }
-  // where row r lies in O; its lse is written
-  __device__ __forceinline__ long long place(int r, float m, float l) const {
-    int i, h;
-    row(r, i, h);
-    if (lse) lse[(long long)h * max_rows + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
-    return ((long long)i * H + h) * D;
-  }
-};
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }   // 0: nothing attended, the row is 0
-
-// rows without keys
-template <typename T, int D>
-__device__ __forceinline__ void put_zeros(const Out<T, D>& out, int nq) {
-  for (int e = threadIdx.x; e < nq * (D / 4); e += PA_THREADS) {
-    const int r = e / (D / 4), c = e % (D / 4) * 4;
-    int i, h;
-    out.row(r, i, h);
-    put4(out.O + ((long long)i * out.H + h) * D + c, make_float4(0.f, 0.f, 0.f, 0.f));
-    if (c == 0) out.place(r, 0.f, 0.f);
-  }
-}
-
-__device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& y) {
-  return make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w));
-}
-// weight of a part with maximum m where the largest is M; a part without keys has the sum 0
-__device__ __forceinline__ float part_weight(float m, float M) { return exp2f(m - M); }
-
 // The warps' parts of nq rows into O, or, for a piece of a segment, into its slot.  Part k of row r: (max, sum) at
 // ML[k * kml + r], numerators at os + k * kos + r * (D + 4).  scr: RT weights per part, then RT places.
 template <typename T, int D, int RT, int HEAD>
@@ -505,147 +388,6 @@ __device__ __forceinline__ void merge(const float2* ML, int kml, const float* os
   }
 }
 
-// Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
-// The rows come into the drained rings, as many at a time as fit, all of their bytes in flight at once: with loads into
-// registers one CTA moved 16 KB a microsecond, and the join of 16 partials of 32 rows took as long.
-template <typename T, int D, int HEAD>
-__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, uint8_t* smem,
-                                     const Out<T, D>& out, float* dst) {
-  constexpr int ROW = D / 4;                                             // vectors of a row
-  float2* pairs = reinterpret_cast<float2*>(smem);                       // nq * n (max, sum) pairs, the rows' places in O, the weights
-  long long* place = reinterpret_cast<long long*>(pairs + nq * n);
-  float* wts = reinterpret_cast<float*>(place + nq);
-  uint8_t* data = smem + ((nq * n * 12 + nq * 8 + 127) & ~127);          // at most 58 KB on: 128 rows of 37 partials
-  // the first partial of a segment lies in its CTA's other slot
-  auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
-  const int tid = threadIdx.x, some = min(nq, (JOIN_SMEM - (int)(data - smem)) / (n * ROW * 16));
-  auto fetch = [&](int r0) {
-    const int cnt = min(some, nq - r0) * ROW;
-    for (int i = 0; i < n; ++i) {
-      const float* src = at(i) + HEAD + r0 * D;
-      for (int e = tid; e < cnt; e += PA_THREADS) copy16(smem_addr(data) + (i * some * ROW + e) * 16, src + e * 4, true);
-    }
-    commit_group();
-  };
-  fetch(0);
-  for (int x = tid; x < nq * n; x += PA_THREADS) pairs[x] = __ldcg(reinterpret_cast<const float2*>(at(x / nq)) + x % nq);
-  __syncthreads();
-  for (int x = tid; x < nq * n; x += PA_THREADS) {
-    const int r = x % nq;
-    float M = NO_KEYS, L = 0.f;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, pairs[i * nq + r].x);
-    for (int i = 0; i < n; ++i) L = fmaf(part_weight(pairs[i * nq + r].x, M), pairs[i * nq + r].y, L);
-    wts[x] = part_weight(pairs[x].x, M) * (dst ? 1.f : inverse(L));
-    if (x < nq) {
-      if (dst) *reinterpret_cast<float2*>(dst + 2 * r) = make_float2(M, L);
-      else place[r] = out.place(r, M, L);
-    }
-  }
-  for (int r0 = 0; r0 < nq; r0 += some) {
-    if (r0 > 0) fetch(r0);
-    wait_group<0>();
-    __syncthreads();
-    const int cnt = min(some, nq - r0) * ROW;
-    for (int e = tid; e < cnt; e += PA_THREADS) {
-      const int r = r0 + e / ROW, c = e % ROW * 4;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < n; ++i) acc = axpy4(wts[i * nq + r], *reinterpret_cast<const float4*>(data + (i * some * ROW + e) * 16), acc);
-      if (dst) *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
-      else put4(out.O + place[r] + c, acc);
-    }
-    __syncthreads();
-  }
-}
-
-// true in every thread of the CTA that is the last of n to arrive
-__device__ __forceinline__ bool arrive_last(int32_t* counter, int n) {
-  __shared__ int flag;
-  __syncthreads();                       // every thread's part of the partial is written
-  if (threadIdx.x == 0) {
-    __threadfence();                     // and visible before the arrival
-    const bool last = atomicAdd(counter, 1) == n - 1;
-    if (last) {
-      *counter = 0;                      // ready for the next launch
-      __threadfence();
-    }
-    flag = last;
-  }
-  __syncthreads();
-  return flag;
-}
-
-// a piece of a segment that the CTAs c0 .. c0 + parts - 1 share is in the workspace: the last to arrive joins them
-template <typename T, int D, typename C>
-__device__ __forceinline__ void finish_piece(const PagedArgs& a, int cta, int c0, int parts, int nq, uint8_t* smem, const Out<T, D>& out) {
-  constexpr long long STRIDE = 2ll * C::PART;
-  float* all = a.part + (long long)c0 * STRIDE;                          // slot 0 of CTA c0; its own piece is in slot 1
-  if (parts <= C::JOIN_ONCE) {
-    if (arrive_last(a.counters + 3 * c0, parts)) join<T, D, C::HEAD>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
-    return;
-  }
-  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN, groups = (parts + J - 1) / J, lead = (cta - c0) / J * J;
-  float* from = all + lead * STRIDE;
-  const long long extra = lead == 0 ? C::PART : 0;
-  if (!arrive_last(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(J, parts - lead))) return;
-  join<T, D, C::HEAD>(from, STRIDE, extra, min(J, parts - lead), nq, smem, out, from + extra);
-  if (arrive_last(a.counters + 3 * c0 + 2, groups))
-    join<T, D, C::HEAD>(all, J * STRIDE, C::PART, groups, nq, smem, out, nullptr);
-}
-
-// A CTA's share of the work: the total cost of the sequences, the CTAs that take part, this one's stretch [p0, p1) and the
-// sequence in which it starts, whose cost begins at `base`.
-struct Stretch {
-  long long total, G, p0, p1, base;
-  int s;
-};
-// false where this CTA has nothing to do; called by all threads
-template <typename Cost>
-__device__ __forceinline__ bool stretch_of(const PagedArgs& a, Cost cost_of, Stretch& st) {
-  __shared__ long long scan[PA_WARPS], start_base;
-  __shared__ int start_seq;
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  const int per = (a.n_seqs + PA_THREADS - 1) / PA_THREADS, s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
-  long long mine = 0;
-  for (int s = s0; s < s1; ++s) mine += cost_of(s);
-  long long incl = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += y;
-  }
-  if (lane == 31) scan[w] = incl;
-  if (tid == 0) { start_seq = a.n_seqs; start_base = 0; }
-  __syncthreads();
-  long long total = 0, before = 0;
-#pragma unroll
-  for (int i = 0; i < PA_WARPS; ++i) {
-    if (i < w) before += scan[i];
-    total += scan[i];
-  }
-  if (total == 0) return false;
-  st.total = total;
-  st.G = min((long long)gridDim.x, max(1ll, total / MIN_COST));
-  const long long cta = blockIdx.x;
-  if (cta >= st.G) return false;
-  st.p0 = divide(cta * total, st.G);
-  st.p1 = divide((cta + 1) * total, st.G);
-  long long at = before + incl - mine;
-  if (st.p0 >= at && st.p0 < at + mine) {
-    int s = s0;
-    for (; s < s1; ++s) {
-      const long long c = cost_of(s);
-      if (st.p0 < at + c) break;
-      at += c;
-    }
-    start_seq = s;
-    start_base = at;
-  }
-  __syncthreads();
-  st.s = start_seq;
-  st.base = start_base;
-  return true;
-}
-
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_kernel(const PagedArgs a) {
   using C = Cfg<T, D, NT>;
@@ -658,7 +400,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
   const uint32_t ring = smem_addr(smem) + w * C::RING;
 
   Stretch st;
-  if (!stretch_of(a, [&](int s) { return seq_cost(seq_of<RT>(a, s), a.Hkv); }, st)) return;
+  if (!stretch_of<PA_WARPS>(a, MIN_COST, [&](int s) { return seq_cost(seq_of<RT>(a, s), a.Hkv); }, st)) return;
   const long long total = st.total, G = st.G, p0 = st.p0, p1 = st.p1;
   const int cta = blockIdx.x;
 
@@ -675,16 +417,17 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     const int nq = (int)min((long long)RT, (long long)q.rows * a.hpg - q0);
     const Out<T, D> out{(T*)a.O, a.lse, a.H, a.hpg, q.first, g, q0, a.max_rows};
     const int t_lo = (int)max(0ll, p - first_tile), t_hi = (int)min((long long)tiles, p1 - first_tile);
-    if (tiles == 0 && p == seg_at) put_zeros(out, nq);                   // no keys: its first unit's CTA writes the rows
+    if (tiles == 0 && p == seg_at) put_zeros(out, nq, tid);                   // no keys: its first unit's CTA writes the rows
     p = min(p1, seg_at + cost);
     if (t_hi <= t_lo) continue;
 
     // ---- the tiles t_lo + w, + 4, ...
     const T* K = (const T*)a.K + (long long)g * a.st_head;
     const T* V = (const T*)a.V + (long long)g * a.st_head;
+    const int end = min(q.len, t_hi * KT);
     int t_load = t_lo + w, page[C::STAGES];                              // page[i]: of the i-th tile that is not requested yet
 #pragma unroll
-    for (int i = 0; i < C::STAGES; ++i) page[i] = key_page(a, s, q.len, t_load + i * PA_WARPS, t_hi, lane);
+    for (int i = 0; i < C::STAGES; ++i) page[i] = key_page(a, s, (t_load + i * PA_WARPS) * KT + (lane & 15), end);
     // query rows beyond nq are zeros: their results are dropped
     constexpr int CPR = D * (int)sizeof(T) / 16, EPC = 16 / (int)sizeof(T), QN = RT * CPR / PA_THREADS;
     uint4 qv[QN > 0 ? QN : 1];
@@ -700,7 +443,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     }
     auto fetch = [&](int stage, int from) {                              // requests tile t_load
       if (t_load < t_hi) {
-        const long long off = key_offset(a, q.len, t_load, from, lane);
+        const long long off = key_offset(a, t_load * KT + (lane & 15), end, from);
         const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
         if (lane == 0) masks[stage] = mask;
         load_tile<T, D>(a, K, V, off, ring + stage * C::STAGE, C::OPERAND, lane);
@@ -724,7 +467,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
       wait_group<C::STAGES - 2>();
       __syncwarp();                      // every lane's copies are there, and nobody reads the stage refilled next
       fetch(stage == 0 ? C::STAGES - 1 : stage - 1, ahead);
-      ahead = key_page(a, s, q.len, t_load, t_hi, lane);
+      ahead = key_page(a, s, t_load * KT + (lane & 15), end);
       core.tile(ring + stage * C::STAGE, ring + stage * C::STAGE + C::OPERAND, masks[stage], a.scale, lane);
       stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     }
@@ -740,7 +483,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
     float* slot = a.part + ((long long)cta * 2 + (cta == c0 ? 1 : 0)) * C::PART;
     merge<T, D, RT, C::HEAD>(ML, RT, reinterpret_cast<const float*>(smem), C::RING / 4, PA_WARPS, nq, piece, slot,
                              smem + C::OFF_SCR, out);
-    if (piece) finish_piece<T, D, C>(a, cta, c0, parts, nq, smem, out);
+    if (piece) finish_piece<T, D, C, PA_THREADS>(a, cta, c0, parts, nq, smem, out);
     __syncthreads();                     // rings, queries and (max, sum) pairs are read out
   }
 }
@@ -769,7 +512,9 @@ focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
 
 extern "C" focus_status focus_paged_attn_workspace_bytes(focus_ctx* ctx, const focus_shape* shape, size_t* out_bytes) {
   if (!ctx || !shape_ok_basic(shape) || !out_bytes) return FOCUS_ERR_INVALID_ARG;
-  *out_bytes = (size_t)2 * ctx->sm_count * 2 * 32 * (shape->head_dim + 2) * sizeof(float) + 256;
+  const size_t rows32 = (size_t)2 * ctx->sm_count * 2 * 32 * (shape->head_dim + 2) * sizeof(float) + 256;
+  const size_t rows128 = paged_attn_tc_workspace(ctx, shape->head_dim);
+  *out_bytes = rows32 > rows128 ? rows32 : rows128;
   return FOCUS_OK;
 }
 
@@ -807,6 +552,8 @@ extern "C" focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shap
   ctx->last_attn_variant = 6;
   if (rows <= 8) return FOCUS_PA_LAUNCH(__nv_bfloat16, 1, 6);
   if (rows <= 16) return FOCUS_PA_LAUNCH(__nv_bfloat16, 2, 8);
-  return FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
+  if (rows <= 32 || !paged_attn_tc_supported(ctx)) return FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
+  ctx->last_attn_variant = 8;
+  return launch_paged_attn_tc(ctx, a, shape->head_dim, stream);
 #undef FOCUS_PA_LAUNCH
 }

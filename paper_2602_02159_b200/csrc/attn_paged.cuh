@@ -1,0 +1,280 @@
+// What the kernels of focus_paged_attn share: their arguments, the split of a ragged batch over the CTAs, where keys and output
+// rows lie, and how pieces of a segment are joined.
+#pragma once
+
+#include <math.h>
+
+#include "focus_common.cuh"
+
+namespace paged {
+
+constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
+constexpr int JOIN = 8;
+constexpr int MAX_GRID = 296;            // a join of its groups' partials has room for that many / JOIN
+static_assert(3 * MAX_GRID <= FOCUS_N_COUNTERS, "three counters per CTA");
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NO_KEYS = -3.402823466e38f;   // running maximum of a row without keys so far: below every score, and finite
+
+struct PagedArgs {
+  const void* Q;
+  long long q_row, q_head;
+  const void* K;
+  const void* V;
+  long long st_page, st_tok, st_head;
+  const int32_t* table;
+  const int32_t* kv_len;
+  const int32_t* row_start;
+  int page, page_shift, n_pages, n_seqs, max_pages, L, max_rows, H, Hkv, hpg;   // page_shift: its logarithm, or -1
+  float scale;                           // softmax scale * log2 e
+  void* O;
+  float* lse;
+  float* part;                           // [gridDim.x][2] partials: (max, sum) pairs of RT rows, then the rows
+  int32_t* counters;                     // 3 per CTA, zero between launches
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+struct Seq {
+  int len, first, rows, row_tiles;       // tokens; first new row, how many; tiles of stacked rows
+};
+
+template <int RT>
+__device__ __forceinline__ Seq seq_of(const PagedArgs& a, int s) {
+  Seq q;
+  q.len = a.kv_len[s];
+  if (q.len < 0 || q.len > a.L) {
+    set_status(a.status, FOCUS_ERR_INVALID_ARG);
+    q.len = q.len < 0 ? 0 : a.L;
+  }
+  q.first = s; q.rows = 1;
+  if (a.row_start) {
+    const int lo = a.row_start[s], hi = a.row_start[s + 1];
+    q.first = lo; q.rows = hi - lo;
+    if (lo < 0 || hi < lo || hi > a.max_rows) { set_status(a.status, FOCUS_ERR_INVALID_ARG); q.rows = 0; }
+  }
+  q.row_tiles = (int)(((long long)q.rows * a.hpg + RT - 1) / RT);
+  return q;
+}
+// the place of key j in its sequence's pages
+__device__ __forceinline__ int page_of(const PagedArgs& a, int j) { return a.page_shift >= 0 ? j >> a.page_shift : j / a.page; }
+// The page of key j, as the table has it (-1 from `end` on), and then where in the pools the key lies, -1 where there is
+// nothing to attend.
+__device__ __forceinline__ int key_page(const PagedArgs& a, int s, int j, int end) {
+  return j < end ? a.table[(long long)s * a.max_pages + page_of(a, j)] : -1;
+}
+__device__ __forceinline__ long long key_offset(const PagedArgs& a, int j, int end, int page) {
+  if (j >= end) return -1;
+  if (page < 0 || page >= a.n_pages) { set_status(a.status, FOCUS_ERR_INVALID_ARG); return -1; }
+  return (long long)page * a.st_page + (long long)(j - page_of(a, j) * a.page) * a.st_tok;
+}
+// non-negative; most are small
+__device__ __forceinline__ long long divide(long long n, long long d) {
+  return ((n | d) >> 32) == 0 ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
+}
+
+// four neighbouring columns of one row into O
+__device__ __forceinline__ void put4(__nv_bfloat16* o, const float4& v) {
+  *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+__device__ __forceinline__ void put4(float* o, const float4& v) { *reinterpret_cast<float4*>(o) = v; }
+
+template <typename T, int D>
+struct Out {                             // where the stacked rows of a segment go
+  T* O;
+  float* lse;
+  int H, hpg, first, g, q0, max_rows;
+  __device__ __forceinline__ void row(int r, int& out_row, int& head) const {
+    out_row = first + (q0 + r) / hpg;
+    head = g * hpg + (q0 + r) % hpg;
+  }
+  // where row r lies in O; its lse is written
+  __device__ __forceinline__ long long place(int r, float m, float l) const {
+    int i, h;
+    row(r, i, h);
+    if (lse) lse[(long long)h * max_rows + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    return ((long long)i * H + h) * D;
+  }
+};
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }   // 0: nothing attended, the row is 0
+
+// rows without keys
+template <typename T, int D>
+__device__ __forceinline__ void put_zeros(const Out<T, D>& out, int nq, int tid) {
+  for (int e = tid; e < nq * (D / 4); e += PA_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    int i, h;
+    out.row(r, i, h);
+    put4(out.O + ((long long)i * out.H + h) * D + c, make_float4(0.f, 0.f, 0.f, 0.f));
+    if (c == 0) out.place(r, 0.f, 0.f);
+  }
+}
+
+__device__ __forceinline__ float4 axpy4(float w, const float4& x, const float4& y) {
+  return make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w));
+}
+// weight of a part with maximum m where the largest is M; a part without keys has the sum 0
+__device__ __forceinline__ float part_weight(float m, float M) { return exp2f(m - M); }
+
+// the threads 0 .. NTH - 1 of the CTA
+template <int NTH>
+__device__ __forceinline__ void sync_threads() { asm volatile("bar.sync 1, %0;" ::"n"(NTH) : "memory"); }
+
+// Joins n partials (partial i at part + i * stride floats) of nq rows, into O or into `dst`, which may be the first of them.
+// The rows come into the drained rings, as many at a time as fit, all of their bytes in flight at once: with loads into
+// registers one CTA moved 16 KB a microsecond, and the join of 16 partials of 32 rows took as long.
+template <typename T, int D, int HEAD, int NTH, int SMEM>
+__device__ __forceinline__ void join(const float* part, long long stride, long long first_extra, int n, int nq, uint8_t* smem,
+                                     const Out<T, D>& out, float* dst) {
+  constexpr int ROW = D / 4;                                             // vectors of a row
+  float2* pairs = reinterpret_cast<float2*>(smem);                       // nq * n (max, sum) pairs, the rows' places in O, the weights
+  long long* place = reinterpret_cast<long long*>(pairs + nq * n);
+  float* wts = reinterpret_cast<float*>(place + nq);
+  uint8_t* data = smem + ((nq * n * 12 + nq * 8 + 127) & ~127);          // at most 58 KB on: 128 rows of 37 partials
+  // the first partial of a segment lies in its CTA's other slot
+  auto at = [&](int i) { return part + i * stride + (i == 0 ? first_extra : 0); };
+  const int tid = threadIdx.x, some = min(nq, (SMEM - (int)(data - smem)) / (n * ROW * 16));
+  auto fetch = [&](int r0) {
+    const int cnt = min(some, nq - r0) * ROW;
+    for (int i = 0; i < n; ++i) {
+      const float* src = at(i) + HEAD + r0 * D;
+      for (int e = tid; e < cnt; e += NTH) copy16(smem_addr(data) + (i * some * ROW + e) * 16, src + e * 4, true);
+    }
+    commit_group();
+  };
+  fetch(0);
+  for (int x = tid; x < nq * n; x += NTH) pairs[x] = __ldcg(reinterpret_cast<const float2*>(at(x / nq)) + x % nq);
+  sync_threads<NTH>();
+  for (int x = tid; x < nq * n; x += NTH) {
+    const int r = x % nq;
+    float M = NO_KEYS, L = 0.f;
+    for (int i = 0; i < n; ++i) M = fmaxf(M, pairs[i * nq + r].x);
+    for (int i = 0; i < n; ++i) L = fmaf(part_weight(pairs[i * nq + r].x, M), pairs[i * nq + r].y, L);
+    wts[x] = part_weight(pairs[x].x, M) * (dst ? 1.f : inverse(L));
+    if (x < nq) {
+      if (dst) *reinterpret_cast<float2*>(dst + 2 * r) = make_float2(M, L);
+      else place[r] = out.place(r, M, L);
+    }
+  }
+  for (int r0 = 0; r0 < nq; r0 += some) {
+    if (r0 > 0) fetch(r0);
+    wait_group<0>();
+    sync_threads<NTH>();
+    const int cnt = min(some, nq - r0) * ROW;
+    for (int e = tid; e < cnt; e += NTH) {
+      const int r = r0 + e / ROW, c = e % ROW * 4;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < n; ++i) acc = axpy4(wts[i * nq + r], *reinterpret_cast<const float4*>(data + (i * some * ROW + e) * 16), acc);
+      if (dst) *reinterpret_cast<float4*>(dst + HEAD + r * D + c) = acc;
+      else put4(out.O + place[r] + c, acc);
+    }
+    sync_threads<NTH>();
+  }
+}
+
+// true in every thread of the CTA that is the last of n to arrive
+template <int NTH>
+__device__ __forceinline__ bool arrive_last(int32_t* counter, int n) {
+  __shared__ int flag;
+  sync_threads<NTH>();                       // every thread's part of the partial is written
+  if (threadIdx.x == 0) {
+    __threadfence();                     // and visible before the arrival
+    const bool last = atomicAdd(counter, 1) == n - 1;
+    if (last) {
+      *counter = 0;                      // ready for the next launch
+      __threadfence();
+    }
+    flag = last;
+  }
+  sync_threads<NTH>();
+  return flag;
+}
+
+// a piece of a segment that the CTAs c0 .. c0 + parts - 1 share is in the workspace: the last to arrive joins them
+template <typename T, int D, typename C, int NTH>
+__device__ __forceinline__ void finish_piece(const PagedArgs& a, int cta, int c0, int parts, int nq, uint8_t* smem, const Out<T, D>& out) {
+  constexpr long long STRIDE = 2ll * C::PART;
+  float* all = a.part + (long long)c0 * STRIDE;                          // slot 0 of CTA c0; its own piece is in slot 1
+  if (parts <= C::JOIN_ONCE) {
+    if (arrive_last<NTH>(a.counters + 3 * c0, parts)) join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
+    return;
+  }
+  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN, groups = (parts + J - 1) / J, lead = (cta - c0) / J * J;
+  float* from = all + lead * STRIDE;
+  const long long extra = lead == 0 ? C::PART : 0;
+  if (!arrive_last<NTH>(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(J, parts - lead))) return;
+  join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(from, STRIDE, extra, min(J, parts - lead), nq, smem, out, from + extra);
+  if (arrive_last<NTH>(a.counters + 3 * c0 + 2, groups))
+    join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(all, J * STRIDE, C::PART, groups, nq, smem, out, nullptr);
+}
+
+// A CTA's share of the work: the total cost of the sequences, the CTAs that take part, this one's stretch [p0, p1) and the
+// sequence in which it starts, whose cost begins at `base`.
+struct Stretch {
+  long long total, G, p0, p1, base;
+  int s;
+};
+// false where this CTA has nothing to do; called by all threads
+template <int WARPS, typename Cost>
+__device__ __forceinline__ bool stretch_of(const PagedArgs& a, int min_cost, Cost cost_of, Stretch& st) {
+  __shared__ long long scan[WARPS], start_base;
+  __shared__ int start_seq;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int per = (a.n_seqs + 32 * WARPS - 1) / (32 * WARPS), s0 = min(tid * per, a.n_seqs), s1 = min(s0 + per, a.n_seqs);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) mine += cost_of(s);
+  long long incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += y;
+  }
+  if (lane == 31) scan[w] = incl;
+  if (tid == 0) { start_seq = a.n_seqs; start_base = 0; }
+  __syncthreads();
+  long long total = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) {
+    if (i < w) before += scan[i];
+    total += scan[i];
+  }
+  if (total == 0) return false;
+  st.total = total;
+  st.G = min((long long)gridDim.x, max(1ll, total / min_cost));
+  const long long cta = blockIdx.x;
+  if (cta >= st.G) return false;
+  st.p0 = divide(cta * total, st.G);
+  st.p1 = divide((cta + 1) * total, st.G);
+  long long at = before + incl - mine;
+  if (st.p0 >= at && st.p0 < at + mine) {
+    int s = s0;
+    for (; s < s1; ++s) {
+      const long long c = cost_of(s);
+      if (st.p0 < at + c) break;
+      at += c;
+    }
+    start_seq = s;
+    start_base = at;
+  }
+  __syncthreads();
+  st.s = start_seq;
+  st.base = start_base;
+  return true;
+}
+
+}  // namespace paged
+
+// many stacked rows per sequence, bf16 (attn_paged_tc.cu)
+focus_status launch_paged_attn_tc(focus_ctx* ctx, paged::PagedArgs& a, int head_dim, cudaStream_t st);
+bool paged_attn_tc_supported(const focus_ctx* ctx);
+size_t paged_attn_tc_workspace(const focus_ctx* ctx, int head_dim);

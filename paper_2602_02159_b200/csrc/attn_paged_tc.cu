@@ -1,0 +1,467 @@
+// focus_paged_attn for many stacked rows per sequence and KV head (windows of a denoising step, chunks of a prompt), bf16:
+// the arithmetic counts there, so the products run on tcgen05 tensor cores with TMEM accumulators.
+//
+// One CTA per SM walks over its stretch of the work (see attn_paged.cu; here a segment has 128 stacked rows and its tiles 128
+// keys).  Roles of its eight warps (nine would leave the softmax 168 registers a thread, and a row of scores is 128):
+//   0, 1     producers: K and V rows of their 64 keys of a tile by 16-byte cp.async, page by page, into the 128-byte swizzled
+//            layout that the matrix descriptors ask for (any page size: a tensor map would need pages of whole tiles), four
+//            slots of one operand each, three in flight
+//   2        one thread issues S = Q K^T (into one of two buffers) and O += P V; both operands' slots are handed back by commits
+//   4 .. 7   softmax, one row per thread: S from TMEM, running maximum (O is rescaled only where it grows by 2^8), numerators
+//            as bf16 over S, row sums in fp32; then the segment's O from TMEM to memory
+// Barriers run on through all segments of a CTA: load q uses slot q % 4, key tile t (counted over the CTA's life) buffer t % 2.
+// Queries of the next segment are staged as soon as the last scores of this one are there, before its O is written out.
+// Pieces of segments are joined when the CTA's stretch is done and the slots are free.
+//
+// What bounds it: the softmax of a tile, one row per thread, about 1.2 us per 128 keys (64 KB of K and V, HBM's rate per SM).
+// On the mma.sync kernel of attn_paged.cu, which reads K and V once per 32 rows, the same windows are held by its MMAs: an
+// m16n8k16 per 8 cycles and SM sub-partition at best, half of that reached.
+#include "attn_paged.cuh"
+#include "tc_common.cuh"
+
+using namespace paged;
+using namespace tc;
+
+namespace {
+
+constexpr int TM = 128, TN = 128;        // rows and keys of a tile
+constexpr int SLOTS = 4, LAG = 2;        // operand slots; loads that a producer has in flight behind the latest
+constexpr int TC_THREADS = 256, PRODUCERS = 64;
+constexpr int TILE_SEG_COST = 3;         // price of a segment beside its tiles, in tiles
+constexpr int TILE_MIN_COST = 3;         // least cost per CTA
+constexpr float RESCALE = 8.f;
+
+template <int D>
+struct TcCfg {
+  static constexpr int HALVES = D / 64, HALF = TN * 128, SLOT = HALVES * HALF;    // a half: 128 rows of 64 columns
+  static constexpr int OFF_RING = SLOT, OFF_BAR = OFF_RING + SLOTS * SLOT;        // queries lie like an operand
+  static constexpr int N_BAR = 2 * SLOTS + 2 * 4 + 4 + 1;
+  static constexpr int OFF_MASK = OFF_BAR + ((N_BAR * 8 + 15) & ~15), OFF_TMEM = OFF_MASK + 4 * 16;
+  static constexpr int SMEM = OFF_TMEM + 16 + 1024;                               // and alignment to 1024 bytes
+  static constexpr int HEAD = 2 * TM, PART = HEAD + TM * D;
+  static constexpr int JOIN_ONCE = 6, JOIN_FEW = 4, JOIN_SMEM = OFF_BAR;
+};
+
+__device__ __forceinline__ long long tile_cost(const Seq& q) { return (q.len + TN - 1) / TN + TILE_SEG_COST; }
+
+struct Segment {                         // a run of key tiles [t_lo, t_hi) for nq stacked rows of KV head g
+  int s, len, first, g, q0, nq, t_lo, t_hi, tiles;
+  long long first_tile;                  // cost at which its tiles begin
+};
+struct Walk {                            // a stretch, walked through segment by segment (by every thread for itself, alike)
+  Stretch st;
+  int s;
+  long long base, p;
+};
+// the next segment with tiles; segments of sequences without tokens are handed to `empty`
+template <typename Empty>
+__device__ __forceinline__ bool next_segment(const PagedArgs& a, Walk& w, Segment& g, Empty empty) {
+  while (w.p < w.st.p1 && w.s < a.n_seqs) {
+    const Seq q = seq_of<TM>(a, w.s);
+    const long long cost = tile_cost(q), whole = cost * q.row_tiles * a.Hkv;
+    if (w.p >= w.base + whole) { w.base += whole; ++w.s; continue; }
+    const long long seg = divide(w.p - w.base, cost), seg_at = w.base + seg * cost;
+    g.s = w.s; g.len = q.len; g.first = q.first;
+    g.tiles = (int)(cost - TILE_SEG_COST);
+    g.g = (int)divide(seg, q.row_tiles);
+    g.q0 = (int)(seg - (long long)g.g * q.row_tiles) * TM;
+    g.nq = (int)min((long long)TM, (long long)q.rows * a.hpg - g.q0);
+    g.first_tile = seg_at + TILE_SEG_COST;
+    g.t_lo = (int)max(0ll, w.p - g.first_tile);
+    g.t_hi = (int)min((long long)g.tiles, w.st.p1 - g.first_tile);
+    const bool none = g.tiles == 0 && w.p == seg_at;
+    w.p = min(w.st.p1, seg_at + cost);
+    if (none) empty(g);
+    if (g.t_hi > g.t_lo) return true;
+  }
+  return false;
+}
+
+// load q of a segment of nt tiles, in the order the products consume them: K0, K1, V0, K2, V1, ..., V(nt - 1)
+__device__ __forceinline__ int load_tile_of(int q, int nt, bool& value) {
+  if (q == 0) { value = false; return 0; }
+  if (q == 2 * nt - 1) { value = true; return nt - 1; }
+  value = (q & 1) == 0;
+  return value ? (q >> 1) - 1 : (q + 1) >> 1;
+}
+
+template <int D>
+__global__ void __launch_bounds__(TC_THREADS, 1) paged_attn_tc_kernel(const PagedArgs a) {
+  using T = __nv_bfloat16;
+  using C = TcCfg<D>;
+  constexpr int CPR = D / 8;             // 16-byte chunks of a row
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - smem_u32(smem_raw));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+  const uint32_t bar = sbase + C::OFF_BAR;
+  auto bar_full = [&](uint32_t s) { return bar + 8u * s; };              // an operand is there (all producers)
+  auto bar_empty = [&](uint32_t s) { return bar + 8u * (SLOTS + s); };   // its slot is free
+  auto bar_sfull = [&](uint32_t b) { return bar + 8u * (2 * SLOTS + b); };
+  auto bar_pready = [&](uint32_t b) { return bar + 8u * (2 * SLOTS + 2 + b); };    // keys 0 .. 63 of P are stored
+  auto bar_pready2 = [&](uint32_t b) { return bar + 8u * (2 * SLOTS + 4 + b); };   // and the others
+  auto bar_pvdone = [&](uint32_t b) { return bar + 8u * (2 * SLOTS + 6 + b); };
+  auto bar_mask = [&](uint32_t m) { return bar + 8u * (2 * SLOTS + 8 + m); };      // which keys of a tile count (2 producer warps)
+  const uint32_t bar_q = bar + 8u * (2 * SLOTS + 12);
+  uint32_t* masks = reinterpret_cast<uint32_t*>(smem + C::OFF_MASK);     // [tile % 4][32 keys]
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  Walk w;
+  if (!stretch_of<TC_THREADS / 32>(a, TILE_MIN_COST, [&](int s) {
+        const Seq q = seq_of<TM>(a, s);
+        return tile_cost(q) * q.row_tiles * a.Hkv;
+      }, w.st)) return;
+  w.s = w.st.s; w.base = w.st.base; w.p = w.st.p0;
+  if (warp == 2) {
+    if (lane == 0) {
+      for (int i = 0; i < SLOTS; ++i) { mbar_init(bar_full(i), PRODUCERS); mbar_init(bar_empty(i), 1); }
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(bar_sfull(b), 1); mbar_init(bar_pready(b), 128); mbar_init(bar_pready2(b), 128); mbar_init(bar_pvdone(b), 1);
+      }
+      for (int i = 0; i < 4; ++i) mbar_init(bar_mask(i), PRODUCERS / 32);
+      mbar_init(bar_q, 128);
+      *abort_flag = 0;
+      fence_barrier_init();
+      fence_proxy_async();
+    }
+    __syncwarp();
+    tmem_alloc(smem_u32(tmem_holder), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder, tmem_O = tmem + 256;
+  const float scale = fabsf(a.scale);    // a negative scale is the queries' sign
+
+  // pieces of this CTA, its first and its last segment at most, as the first producer meets them
+  __shared__ Segment piece[2];
+  __shared__ int pieces;
+  if (tid == 0) pieces = 0;
+  auto note = [&](const Segment& g) {
+    if (tid == 0 && (g.t_lo > 0 || g.t_hi < g.tiles)) piece[min(pieces++, 1)] = g;
+  };
+  auto cta_of = [&](long long pos) { return (int)divide((pos + 1) * w.st.G - 1, w.st.total); };
+  Segment g;
+
+  if (warp < 2) {
+    // ================================ producers ====================================================
+    uint32_t slot = 0, round = 0;        // of the next load
+    uint32_t pend = 0, pend_slot = 0;    // loads whose arrival is due, the oldest one's slot
+    uint32_t tile = 0;                   // key tiles begun
+    bool ok = true;
+    while (ok && next_segment(a, w, g, [](const Segment&) {})) {
+      note(g);
+      const T* pool[2] = {(const T*)a.K + (long long)g.g * a.st_head, (const T*)a.V + (long long)g.g * a.st_head};
+      const int nt = g.t_hi - g.t_lo, key0 = g.t_lo * TN + warp * 64 + lane;
+      long long even[2] = {-1, -1}, odd[2] = {-1, -1};                   // of this lane's two keys in the tiles of either parity
+      int page[2] = {key_page(a, g.s, key0, g.len), key_page(a, g.s, key0 + 32, g.len)};
+      for (int q = 0; q < 2 * nt; ++q) {
+        bool value;
+        const int i = load_tile_of(q, nt, value);
+        long long mine[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (!value) {
+            const int j = key0 + i * TN + x * 32;
+            mine[x] = key_offset(a, j, g.len, page[x]);
+            if (i & 1) odd[x] = mine[x]; else even[x] = mine[x];
+            page[x] = key_page(a, g.s, j + TN, g.len);
+          } else {
+            mine[x] = i & 1 ? odd[x] : even[x];
+          }
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_empty(slot), (round & 1u) ^ 1u, abort_flag, a.status))) { ok = false; break; }
+        if (!value) {
+          const uint32_t lo = __ballot_sync(0xffffffffu, mine[0] >= 0), hi = __ballot_sync(0xffffffffu, mine[1] >= 0);
+          if (lane == 0) {
+            masks[(tile & 3) * 4 + warp * 2] = lo;
+            masks[(tile & 3) * 4 + warp * 2 + 1] = hi;
+            mbar_arrive(bar_mask(tile & 3));
+          }
+          ++tile;
+        }
+        const uint32_t dst = sbase + C::OFF_RING + slot * C::SLOT;
+        const T* src = value ? pool[1] : pool[0];
+        const int c = lane % CPR;
+#pragma unroll
+        for (int x = 0; x < 2 * CPR; ++x) {                              // 32 / CPR rows at a time
+          const int k = x % CPR * (32 / CPR) + lane / CPR, row = warp * 64 + x / CPR * 32 + k;
+          const long long o = __shfl_sync(0xffffffffu, mine[x / CPR], k);
+          const bool valid = o >= 0;
+          copy16(dst + (c >> 3) * C::HALF + row * 128 + (((c & 7) ^ (row & 7)) << 4), src + (valid ? o : 0) + c * 8, valid);
+        }
+        commit_group();
+        if (++slot == SLOTS) { slot = 0; ++round; }
+        if (++pend > LAG) {
+          wait_group<LAG>();
+          fence_proxy_async();           // the tensor core reads what this thread's copies wrote
+          mbar_arrive(bar_full(pend_slot));
+          pend_slot = pend_slot + 1 == SLOTS ? 0 : pend_slot + 1;
+          --pend;
+        }
+      }
+    }
+    wait_group<0>();
+    fence_proxy_async();
+    for (; pend > 0; --pend) {
+      mbar_arrive(bar_full(pend_slot));
+      pend_slot = pend_slot + 1 == SLOTS ? 0 : pend_slot + 1;
+    }
+    while (next_segment(a, w, g, [](const Segment&) {})) note(g);        // after a wait that ran out: announced all the same
+  } else if (warp == 2) {
+    // ================================ products =====================================================
+    if (lane == 0) {
+      constexpr uint32_t IDESC_QK = make_idesc(TM, TN, 0), IDESC_PV = make_idesc(TM, D, 1);
+      const uint64_t qdesc = make_sdesc(sbase, 16, 1024);
+      uint32_t slot = 0, round = 0, tile = 0, seg = 0;
+      bool ok = true;
+      auto do_pv = [&](uint32_t t, bool fresh) -> bool {
+        const uint32_t b = t & 1, ph = (t >> 1) & 1;
+        if (!mbar_wait(bar_pready(b), ph, abort_flag, a.status)) return false;
+        if (!mbar_wait(bar_full(slot), round & 1u, abort_flag, a.status)) return false;
+        tc_fence_after();
+        const uint64_t vdesc = make_sdesc(sbase + C::OFF_RING + slot * C::SLOT, C::HALF, 1024);
+        const uint32_t pt = tmem + b * 128;
+#pragma unroll
+        for (int ks = 0; ks < TN / 32; ++ks)
+          mma_ts(tmem_O, pt + ks * 8, vdesc + (uint64_t)(ks * (2048 >> 4)), IDESC_PV, (!fresh || ks > 0) ? 1u : 0u);
+        if (!mbar_wait(bar_pready2(b), ph, abort_flag, a.status)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = TN / 32; ks < TN / 16; ++ks)
+          mma_ts(tmem_O, pt + ks * 8, vdesc + (uint64_t)(ks * (2048 >> 4)), IDESC_PV, 1u);
+        tc_commit(bar_empty(slot));
+        tc_commit(bar_pvdone(b));
+        if (++slot == SLOTS) { slot = 0; ++round; }
+        return true;
+      };
+      while (ok && next_segment(a, w, g, [](const Segment&) {})) {
+        const int nt = g.t_hi - g.t_lo;
+        if (!mbar_wait(bar_q, seg & 1u, abort_flag, a.status)) break;
+        ++seg;
+        for (int i = 0; i < nt && ok; ++i, ++tile) {
+          if (!mbar_wait(bar_full(slot), round & 1u, abort_flag, a.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t kdesc = make_sdesc(sbase + C::OFF_RING + slot * C::SLOT, 16, 1024);
+#pragma unroll
+          for (int half = 0; half < C::HALVES; ++half)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+              const uint64_t o = (uint64_t)((half * C::HALF + ks * 32) >> 4);
+              mma_ss(tmem + (tile & 1) * 128, qdesc + o, kdesc + o, IDESC_QK, (half | ks) ? 1u : 0u);
+            }
+          tc_commit(bar_empty(slot));
+          tc_commit(bar_sfull(tile & 1));
+          if (++slot == SLOTS) { slot = 0; ++round; }
+          if (i > 0) ok = do_pv(tile - 1, i == 1);
+        }
+        if (ok) ok = do_pv(tile - 1, nt == 1);
+      }
+    }
+  } else if (warp >= 4) {
+    // ================================ softmax, output ==============================================
+    const int row = tid - 128;           // of the tile; this warp reads TMEM lanes 32 (warp % 4) .. + 31
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    auto out_of = [&](const Segment& x) { return Out<T, D>{(T*)a.O, a.lse, a.H, a.hpg, x.first, x.g, x.q0, a.max_rows}; };
+    auto stage_q = [&](const Segment& x) {                               // rows beyond nq as zeros
+      uint4 v[CPR];
+#pragma unroll
+      for (int c = 0; c < CPR; ++c) v[c] = make_uint4(0, 0, 0, 0);
+      if (row < x.nq) {
+        int i, h;
+        out_of(x).row(row, i, h);
+        const uint4* src = reinterpret_cast<const uint4*>((const T*)a.Q + (long long)i * a.q_row + (long long)h * a.q_head);
+#pragma unroll
+        for (int c = 0; c < CPR; ++c) {
+          v[c] = src[c];
+          v[c].x ^= flip; v[c].y ^= flip; v[c].z ^= flip; v[c].w ^= flip;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < CPR; ++c)
+        *reinterpret_cast<uint4*>(smem + (c >> 3) * C::HALF + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v[c];
+      fence_proxy_async();
+      mbar_arrive(bar_q);
+    };
+    auto empty = [&](const Segment& x) { put_zeros(out_of(x), x.nq, row); };
+    uint32_t tile = 0;
+    bool ok = true, have = next_segment(a, w, g, empty);
+    if (have) stage_q(g);
+    while (have) {
+      float m_ref = NO_KEYS, l = 0.f;
+      const int nt = g.t_hi - g.t_lo;
+      for (int i = 0; i < nt && ok; ++i, ++tile) {
+        const uint32_t b = tile & 1;
+        // votes keep the warp together: TMEM loads and stores are warp-collective
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_mask(tile & 3), (tile >> 2) & 1u, abort_flag, a.status) &&
+                                         mbar_wait(bar_sfull(b), (tile >> 1) & 1u, abort_flag, a.status))) { ok = false; break; }
+        tc_fence_after();
+        uint32_t s[128];
+        const uint32_t ts = tmem + lane_off + b * 128;
+        TC_LD32(ts, (s + 0));
+        TC_LD32(ts + 32, (s + 32));
+        TC_LD32(ts + 64, (s + 64));
+        TC_LD32(ts + 96, (s + 96));
+        tc_wait_ld();
+        const uint4 mask = *reinterpret_cast<const uint4*>(masks + (tile & 3) * 4);
+        if ((mask.x & mask.y & mask.z & mask.w) != 0xffffffffu) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c) {
+            const uint32_t word = c < 32 ? mask.x : c < 64 ? mask.y : c < 96 ? mask.z : mask.w;
+            if (!((word >> (c & 31)) & 1u)) s[c] = 0xff800000u;
+          }
+        }
+        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 128; c += 8) {
+          t4[0] = fmax3(t4[0], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+          t4[1] = fmax3(t4[1], __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+          t4[2] = fmax3(t4[2], __uint_as_float(s[c + 4]), __uint_as_float(s[c + 5]));
+          t4[3] = fmax3(t4[3], __uint_as_float(s[c + 6]), __uint_as_float(s[c + 7]));
+        }
+        const float tmax = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * scale;
+        float alpha = 1.f;
+        bool grow = false;
+        if (tmax > m_ref + RESCALE) {    // also true for the first finite maximum
+          alpha = ex2(m_ref - tmax);     // 0 then
+          grow = true;
+          m_ref = tmax;
+        }
+        if (i > 0 && __any_sync(0xffffffffu, grow)) {
+          // P V of the tile before must have left the tensor core before O is touched
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_pvdone((tile - 1) & 1), ((tile - 1) >> 1) & 1u, abort_flag, a.status))) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int cb = 0; cb < D / 32; ++cb) {
+            uint32_t o[32];
+            TC_LD32(tmem_O + lane_off + cb * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
+            TC_ST32(tmem_O + lane_off + cb * 32, o);
+          }
+        }
+        const float neg = -m_ref;        // no key so far: every exponent is -inf
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const int c = ch * 32 + 2 * k;
+            float x0, x1;
+            ffma2(x0, x1, __uint_as_float(s[c]), __uint_as_float(s[c + 1]), scale, scale, neg, neg);
+            const float p0 = ex2(x0), p1 = ex2(x1);
+            p[k] = tc::pack_bf16(p0, p1);
+            fadd2(acc[(k & 1) * 2], acc[(k & 1) * 2 + 1], acc[(k & 1) * 2], acc[(k & 1) * 2 + 1], p0, p1);
+          }
+          TC_ST16(ts + ch * 16, p);
+          if (ch == 1) {
+            tc_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar_pready(b));
+          }
+        }
+        tc_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_pready2(b));
+        l = l * alpha + ((acc[0] + acc[1]) + (acc[2] + acc[3]));
+      }
+      // all scores of the segment are read: the next one's queries may replace its own
+      Segment next;
+      const Segment cur = g;
+      const bool more = ok && next_segment(a, w, next, empty);
+      if (more) stage_q(next);
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_pvdone((tile - 1) & 1), ((tile - 1) >> 1) & 1u, abort_flag, a.status));
+      if (!ok) break;
+      tc_fence_after();
+      const bool valid = row < cur.nq;
+      if (cur.t_lo > 0 || cur.t_hi < cur.tiles) {
+        float* slot = a.part + ((long long)cta * 2 + (cta == cta_of(cur.first_tile) ? 1 : 0)) * C::PART;
+        if (valid) *reinterpret_cast<float2*>(slot + 2 * row) = make_float2(m_ref, l);
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) {
+          uint32_t o[32];
+          TC_LD32(tmem_O + lane_off + cb * 32, o);
+          tc_wait_ld();
+          if (valid) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4)
+              *reinterpret_cast<uint4*>(slot + C::HEAD + row * D + cb * 32 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+          }
+        }
+      } else {
+        const float inv = inverse(l);
+        T* to = (T*)a.O;
+        if (valid) to += out_of(cur).place(row, m_ref, l);
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) {
+          uint32_t o[32];
+          TC_LD32(tmem_O + lane_off + cb * 32, o);
+          tc_wait_ld();
+          if (valid) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 8) {
+              uint4 v;
+              v.x = tc::pack_bf16(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv);
+              v.y = tc::pack_bf16(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+              v.z = tc::pack_bf16(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv);
+              v.w = tc::pack_bf16(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv);
+              *reinterpret_cast<uint4*>(to + cb * 32 + c) = v;
+            }
+          }
+        }
+      }
+      tc_fence_before();                 // O is read out before the next segment's numerators are handed over
+      have = more;
+      if (more) g = next;
+    }
+  }
+
+  // ---- teardown: every role comes here, also after a wait that ran out; then the pieces
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    __syncwarp();
+    tmem_dealloc(tmem, 512);
+  }
+  const int n = pieces;
+  for (int i = 0; i < n && i < 2; ++i) {
+    const Segment x = piece[i];
+    const int c0 = cta_of(x.first_tile), parts = cta_of(x.first_tile + x.tiles - 1) - c0 + 1;
+    finish_piece<T, D, C, TC_THREADS>(a, cta, c0, parts, x.nq, smem, Out<T, D>{(T*)a.O, a.lse, a.H, a.hpg, x.first, x.g, x.q0, a.max_rows});
+    __syncthreads();
+  }
+}
+
+template <int D>
+focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
+  using C = TcCfg<D>;
+  if (!ctx->ls.paged_attr_set[attr]) {
+    if (cudaFuncSetAttribute(paged_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
+      return FOCUS_ERR_CUDA;
+    ctx->ls.paged_attr_set[attr] = true;
+  }
+  if (ctx->sm_count > MAX_GRID) return FOCUS_ERR_UNSUPPORTED;
+  WsAlloc ws(ctx);
+  a.part = ws.get<float>((size_t)ctx->sm_count * 2 * C::PART);
+  if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
+  paged_attn_tc_kernel<D><<<ctx->sm_count, TC_THREADS, C::SMEM, st>>>(a);
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
+
+}  // namespace
+
+bool paged_attn_tc_supported(const focus_ctx* ctx) { return ctx->encode_tiled != nullptr; }   // found on sm_100 alone
+
+size_t paged_attn_tc_workspace(const focus_ctx* ctx, int head_dim) {
+  return (size_t)ctx->sm_count * 2 * TM * (head_dim + 2) * sizeof(float) + 256;
+}
+
+focus_status launch_paged_attn_tc(focus_ctx* ctx, PagedArgs& a, int head_dim, cudaStream_t st) {
+  return head_dim == 128 ? launch<128>(ctx, a, 12, st) : launch<64>(ctx, a, 13, st);
+}
