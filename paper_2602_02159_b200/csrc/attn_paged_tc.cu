@@ -3,9 +3,9 @@
 //
 // One CTA per SM walks over its stretch of the work (see attn_paged.cu; here a segment has 128 stacked rows and its tiles 128
 // keys).  Roles of its eight warps (nine would leave the softmax 168 registers a thread, and a row of scores is 128):
-//   0, 1     producers: K and V rows of their 64 keys of a tile by 16-byte cp.async, page by page, into the 128-byte swizzled
-//            layout that the matrix descriptors ask for (any page size: a tensor map would need pages of whole tiles), four
-//            slots of one operand each, three in flight
+//   0, 1     producers, 64 keys of a tile each: pages whose size divides a tile (or is a multiple of it) by TMA, a box per page
+//            and 64 columns; the last tile of a sequence, whose page goes on with somebody's old rows, and other page sizes
+//            by 16-byte cp.async into the same 128-byte swizzled layout.  Four slots of one operand each
 //   2        one thread issues S = Q K^T (into one of two buffers) and O += P V; both operands' slots are handed back by commits
 //   4 .. 7   softmax, one row per thread: S from TMEM, running maximum (O is rescaled only where it grows by 2^8), numerators
 //            as bf16 over S, row sums in fp32; then the segment's O from TMEM to memory
@@ -85,8 +85,18 @@ __device__ __forceinline__ int load_tile_of(int q, int nt, bool& value) {
   return value ? (q >> 1) - 1 : (q + 1) >> 1;
 }
 
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// box: rows of a page that one TMA box brings (a divisor of 128, at least 8), or 0: cp.async throughout
 template <int D>
-__global__ void __launch_bounds__(TC_THREADS, 1) paged_attn_tc_kernel(const PagedArgs a) {
+__global__ void __launch_bounds__(TC_THREADS, 1)
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PagedArgs a,
+                     const int box) {
   using T = __nv_bfloat16;
   using C = TcCfg<D>;
   constexpr int CPR = D / 8;             // 16-byte chunks of a row
@@ -148,33 +158,43 @@ __global__ void __launch_bounds__(TC_THREADS, 1) paged_attn_tc_kernel(const Page
   if (warp < 2) {
     // ================================ producers ====================================================
     uint32_t slot = 0, round = 0;        // of the next load
-    uint32_t pend = 0, pend_slot = 0;    // loads whose arrival is due, the oldest one's slot
+    uint32_t pend = 0, pend_slot = 0;    // cp.async loads whose arrival is due, the oldest one's slot
     uint32_t tile = 0;                   // key tiles begun
     bool ok = true;
+    auto arrive_oldest = [&] {
+      fence_proxy_async();               // the tensor core reads what this thread's copies wrote
+      mbar_arrive(bar_full(pend_slot));
+      pend_slot = pend_slot + 1 == SLOTS ? 0 : pend_slot + 1;
+      --pend;
+    };
+    // this lane's box of a tile: `half` of the columns, rows from box_row on (of this warp's 64); -1: none
+    const int box_half = lane % C::HALVES, box_at = lane / C::HALVES * box;
+    const int box_row = box == 128 ? (warp == 0 && box_at == 0 ? 0 : -1) : (box_at < 64 ? box_at : -1);
     while (ok && next_segment(a, w, g, [](const Segment&) {})) {
       note(g);
-      const T* pool[2] = {(const T*)a.K + (long long)g.g * a.st_head, (const T*)a.V + (long long)g.g * a.st_head};
       const int nt = g.t_hi - g.t_lo, key0 = g.t_lo * TN + warp * 64 + lane;
-      long long even[2] = {-1, -1}, odd[2] = {-1, -1};                   // of this lane's two keys in the tiles of either parity
-      int page[2] = {key_page(a, g.s, key0, g.len), key_page(a, g.s, key0 + 32, g.len)};
+      // of this lane's two keys in the tiles of either parity: their pages, and the places in the pools
+      int page[2] = {key_page(a, g.s, key0, g.len), key_page(a, g.s, key0 + 32, g.len)}, page_even[2] = {-1, -1}, page_odd[2] = {-1, -1};
       for (int q = 0; q < 2 * nt; ++q) {
         bool value;
         const int i = load_tile_of(q, nt, value);
-        long long mine[2];
+        int now[2];
+        long long at[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+          const int j = key0 + i * TN + x * 32;
           if (!value) {
-            const int j = key0 + i * TN + x * 32;
-            mine[x] = key_offset(a, j, g.len, page[x]);
-            if (i & 1) odd[x] = mine[x]; else even[x] = mine[x];
+            now[x] = page[x];
+            if (i & 1) page_odd[x] = now[x]; else page_even[x] = now[x];
             page[x] = key_page(a, g.s, j + TN, g.len);
           } else {
-            mine[x] = i & 1 ? odd[x] : even[x];
+            now[x] = i & 1 ? page_odd[x] : page_even[x];
           }
+          at[x] = key_offset(a, j, g.len, now[x]);
         }
         if (!__all_sync(0xffffffffu, mbar_wait(bar_empty(slot), (round & 1u) ^ 1u, abort_flag, a.status))) { ok = false; break; }
         if (!value) {
-          const uint32_t lo = __ballot_sync(0xffffffffu, mine[0] >= 0), hi = __ballot_sync(0xffffffffu, mine[1] >= 0);
+          const uint32_t lo = __ballot_sync(0xffffffffu, at[0] >= 0), hi = __ballot_sync(0xffffffffu, at[1] >= 0);
           if (lane == 0) {
             masks[(tile & 3) * 4 + warp * 2] = lo;
             masks[(tile & 3) * 4 + warp * 2 + 1] = hi;
@@ -183,31 +203,50 @@ __global__ void __launch_bounds__(TC_THREADS, 1) paged_attn_tc_kernel(const Page
           ++tile;
         }
         const uint32_t dst = sbase + C::OFF_RING + slot * C::SLOT;
-        const T* src = value ? pool[1] : pool[0];
-        const int c = lane % CPR;
+        if (box > 0 && (g.t_lo + i + 1) * TN <= g.len) {
+          const int r = max(box_row, 0);
+          const int p0 = __shfl_sync(0xffffffffu, now[0], r & 31), p1 = __shfl_sync(0xffffffffu, now[1], r & 31);
+          if (box_row >= 0) {
+            // a page that does not exist lies outside the map: it arrives as zeros, and its keys are masked
+            const int j = (g.t_lo + i) * TN + warp * 64 + box_row, pg = r < 32 ? p0 : p1;
+            mbar_expect_tx(bar_full(slot), box * 128);
+            tma_load_4d(dst + box_half * C::HALF + (warp * 64 + box_row) * 128, value ? &map_v : &map_k, bar_full(slot), box_half * 64,
+                        j - page_of(a, j) * a.page, g.g, (uint32_t)pg < (uint32_t)a.n_pages ? pg : a.n_pages);
+          } else {
+            mbar_arrive(bar_full(slot));
+          }
+          if (pend > 0) {
+            wait_group<0>();
+            while (pend > 0) arrive_oldest();
+          }
+        } else {
+          const T* src = (value ? (const T*)a.V : (const T*)a.K) + (long long)g.g * a.st_head;
+          const int c = lane % CPR;
 #pragma unroll
-        for (int x = 0; x < 2 * CPR; ++x) {                              // 32 / CPR rows at a time
-          const int k = x % CPR * (32 / CPR) + lane / CPR, row = warp * 64 + x / CPR * 32 + k;
-          const long long o = __shfl_sync(0xffffffffu, mine[x / CPR], k);
-          const bool valid = o >= 0;
-          copy16(dst + (c >> 3) * C::HALF + row * 128 + (((c & 7) ^ (row & 7)) << 4), src + (valid ? o : 0) + c * 8, valid);
+          for (int x = 0; x < 2 * CPR; ++x) {                            // 32 / CPR rows at a time
+            const int k = x % CPR * (32 / CPR) + lane / CPR, row = warp * 64 + x / CPR * 32 + k;
+            const long long o = __shfl_sync(0xffffffffu, at[x / CPR], k);
+            const bool valid = o >= 0;
+            copy16(dst + (c >> 3) * C::HALF + row * 128 + (((c & 7) ^ (row & 7)) << 4), src + (valid ? o : 0) + c * 8, valid);
+          }
+          commit_group();
+          if (pend++ == 0) pend_slot = slot;
+          if (pend > LAG) {
+            wait_group<LAG>();
+            arrive_oldest();
+          }
         }
-        commit_group();
         if (++slot == SLOTS) { slot = 0; ++round; }
-        if (++pend > LAG) {
-          wait_group<LAG>();
-          fence_proxy_async();           // the tensor core reads what this thread's copies wrote
-          mbar_arrive(bar_full(pend_slot));
-          pend_slot = pend_slot + 1 == SLOTS ? 0 : pend_slot + 1;
-          --pend;
-        }
       }
     }
     wait_group<0>();
-    fence_proxy_async();
-    for (; pend > 0; --pend) {
-      mbar_arrive(bar_full(pend_slot));
-      pend_slot = pend_slot + 1 == SLOTS ? 0 : pend_slot + 1;
+    while (pend > 0) arrive_oldest();
+    if (!ok) {                           // copies under way land before the CTA's shared memory is given up
+      for (uint32_t n = min(round * SLOTS + slot, (uint32_t)SLOTS); n > 0; --n) {
+        const uint32_t q = round * SLOTS + slot - n;
+        const uint64_t t0 = global_ns();
+        while (!mbar_try_wait(bar_full(q % SLOTS), (q / SLOTS) & 1u) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+      }
     }
     while (next_segment(a, w, g, [](const Segment&) {})) note(g);        // after a wait that ran out: announced all the same
   } else if (warp == 2) {
@@ -437,6 +476,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) paged_attn_tc_kernel(const Page
   }
 }
 
+// [d, tokens of a page, heads, pages] with boxes of 64 columns and `rows` tokens
+bool encode_pool(const focus_ctx* ctx, CUtensorMap* map, const void* pool, const PagedArgs& a, int d, int rows) {
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)a.page, (cuuint64_t)a.Hkv, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)a.st_tok * 2, (cuuint64_t)a.st_head * 2, (cuuint64_t)a.st_page * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return ((EncodeTiledFn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, one,
+                                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
   using C = TcCfg<D>;
@@ -449,7 +498,11 @@ focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
   WsAlloc ws(ctx);
   a.part = ws.get<float>((size_t)ctx->sm_count * 2 * C::PART);
   if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
-  paged_attn_tc_kernel<D><<<ctx->sm_count, TC_THREADS, C::SMEM, st>>>(a);
+  // a box per page where pages divide a tile (and are whole swizzle groups of eight rows) or tiles divide a page
+  int box = a.page % TN == 0 ? TN : a.page >= 8 && TN % a.page == 0 ? a.page : 0;
+  CUtensorMap map_k = {}, map_v = {};
+  if (box > 0 && !(encode_pool(ctx, &map_k, a.K, a, D, box) && encode_pool(ctx, &map_v, a.V, a, D, box))) box = 0;
+  paged_attn_tc_kernel<D><<<ctx->sm_count, TC_THREADS, C::SMEM, st>>>(map_k, map_v, a, box);
   FOCUS_CHECK_LAUNCH();
   return FOCUS_OK;
 }

@@ -425,6 +425,10 @@ def check_attention(c, n, Q, O, ls, H, scale):
     ("bf16", 28, 4, 128, 16, [900, 2000, 64, 63, 0, 1], [19, 37, 9, 5, 20, 18], False),      # 133, 259, 63, 35, 140, 126 stacked rows
     ("bf16", 6, 2, 64, 48, [3000, 129, 700], [128, 11, 85], True),            # 384, 33, 255
     ("bf16", 4, 4, 128, 5, [1, 64, 65, 250], [300, 96, 32, 1], False),
+    ("bf16", 4, 1, 128, 8, [128, 127, 129, 1000], [9, 12, 33, 10], True),
+    ("bf16", 14, 2, 64, 128, [1, 256, 383, 5], [5, 7, 64, 0], False),
+    ("bf16", 40, 1, 128, 256, [700, 0, 2305], [1, 1, 1], True),
+    ("bf16", 5, 1, 64, 32, [31, 32, 33, 4096], [40, 7, 8, 26], False),
     ("f32", 8, 8, 64, 32, [1024, 1, 37, 0, 500], None, False),
     ("f32", 12, 4, 128, 3, [200, 17, 0], [4, 9, 1], True),
     ("f32", 40, 1, 128, 16, [77, 2500], None, False),
@@ -490,6 +494,33 @@ def test_bad_pages_lengths_and_rows_are_reported_not_followed(ctx, dtype):
     for start in ([0, 3, 3], [0, -1, 2], [1, 0, 2], [-1, 1, 2]):
         O, ls, st = call(start=i32(start))
         assert st == fb.ERR_INVALID_ARG
+
+
+@gpu
+@pytest.mark.parametrize("page", [16, 24])
+def test_windows_skip_pages_that_do_not_exist(ctx, page):
+    rng = np.random.default_rng(page)
+    c = Cache(rng, "bf16", 2, 128, page, [600, 290], 600)
+    n = [12, 9]
+    Q = torch.from_numpy(rng.standard_normal((21, 8, 128))).cuda().bfloat16()
+    start = i32([0, 12, 21])
+
+    def call():
+        O, ls = torch.zeros((21, 8, 128), device="cuda").bfloat16(), torch.zeros((8, 21), device="cuda")
+        fb.focus_paged_attn(ctx, c.shape(8), Q, start, 21, c.c(), O, ls)
+        return O, ls, ctx.poll_status()
+
+    good, _, st = call()
+    assert st == 0 and ctx.last_attn_variant() == 8
+    c.d_table[0, 3], c.d_table[0, 8:20], c.d_table[0, 24] = -1, c.n_pages, 2 ** 31 - 1
+    O, ls, st = call()
+    assert st == fb.ERR_INVALID_ARG and torch.equal(O[12:], good[12:])
+    keep = np.array([j for j in range(600) if not (j // page in (3, 24) or 8 <= j // page < 20)])
+    c.tokens[0], c.lengths = [t[keep] for t in c.tokens[0]], [len(keep), 290]
+    check_attention(c, n, Q, O, ls, 8, 128 ** -0.5)
+    c.d_table[0, :] = -1
+    O, ls, st = call()
+    assert st == fb.ERR_INVALID_ARG and (O[:12] == 0).all() and torch.isinf(ls[:, :12]).all() and torch.equal(O[12:], good[12:])
 
 
 @gpu
