@@ -399,6 +399,7 @@ __global__ void __launch_bounds__(PA_THREADS, Cfg<T, D, NT>::CTAS) paged_attn_ke
   uint32_t* masks = reinterpret_cast<uint32_t*>(smem + C::OFF_MASK) + w * C::STAGES;
   const uint32_t ring = smem_addr(smem) + w * C::RING;
 
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   Stretch st;
   if (!stretch_of<PA_WARPS>(a, MIN_COST, [&](int s) { return seq_cost(seq_of<RT>(a, s), a.Hkv); }, st)) return;
   const long long total = st.total, G = st.G, p0 = st.p0, p1 = st.p1;
@@ -499,9 +500,7 @@ focus_status launch_kernel(focus_ctx* ctx, PagedArgs& a, Kernel kernel, int ctas
   WsAlloc ws(ctx);
   a.part = ws.get<float>((size_t)grid * 2 * C::PART);
   if (!ws.ok) return FOCUS_ERR_WORKSPACE_TOO_SMALL;
-  kernel<<<grid, PA_THREADS, C::SMEM, st>>>(a);
-  FOCUS_CHECK_LAUNCH();
-  return FOCUS_OK;
+  return launch_chained(ctx, kernel, grid, PA_THREADS, C::SMEM, st, a);
 }
 template <typename T, int D, int NT>
 focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {

@@ -272,6 +272,25 @@ __device__ __forceinline__ bool stretch_of(const PagedArgs& a, int min_cost, Cos
   return true;
 }
 
+// Launches a kernel as a programmatic dependent of its predecessor in the stream: its CTAs take their places while that one's
+// last ones are at work, and wait for its end before they touch global memory.
+template <typename... P, typename... A>
+focus_status launch_chained(const focus_ctx* ctx, void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = ctx->no_pdl ? 0 : 1;
+  cudaLaunchKernelEx(&cfg, kernel, args...);
+  FOCUS_CHECK_LAUNCH();
+  return FOCUS_OK;
+}
+
 }  // namespace paged
 
 // many stacked rows per sequence, bf16 (attn_paged_tc.cu)

@@ -27,8 +27,8 @@ namespace {
 constexpr int TM = 128, TN = 128;        // rows and keys of a tile
 constexpr int SLOTS = 4, LAG = 2;        // operand slots; loads that a producer has in flight behind the latest
 constexpr int TC_THREADS = 256, PRODUCERS = 64;
-constexpr int TILE_SEG_COST = 3;         // price of a segment beside its tiles, in tiles
-constexpr int TILE_MIN_COST = 3;         // least cost per CTA
+constexpr int TILE_SEG_COST = 5;         // price of a segment beside its tiles, in tiles (six ragged windows 52 us, 66 with 3)
+constexpr int TILE_MIN_COST = 4;         // least cost per CTA
 constexpr float RESCALE = 8.f;
 
 template <int D>
@@ -39,7 +39,7 @@ struct TcCfg {
   static constexpr int OFF_MASK = OFF_BAR + ((N_BAR * 8 + 15) & ~15), OFF_TMEM = OFF_MASK + 4 * 16;
   static constexpr int SMEM = OFF_TMEM + 16 + 1024;                               // and alignment to 1024 bytes
   static constexpr int HEAD = 2 * TM, PART = HEAD + TM * D;
-  static constexpr int JOIN_ONCE = 6, JOIN_FEW = 4, JOIN_SMEM = OFF_BAR;
+  static constexpr int JOIN_ONCE = 12, JOIN_FEW = 4, JOIN_SMEM = OFF_BAR;
 };
 
 __device__ __forceinline__ long long tile_cost(const Seq& q) { return (q.len + TN - 1) / TN + TILE_SEG_COST; }
@@ -117,6 +117,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + C::OFF_TMEM);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   Walk w;
   if (!stretch_of<TC_THREADS / 32>(a, TILE_MIN_COST, [&](int s) {
         const Seq q = seq_of<TM>(a, s);
@@ -502,9 +503,7 @@ focus_status launch(focus_ctx* ctx, PagedArgs& a, int attr, cudaStream_t st) {
   int box = a.page % TN == 0 ? TN : a.page >= 8 && TN % a.page == 0 ? a.page : 0;
   CUtensorMap map_k = {}, map_v = {};
   if (box > 0 && !(encode_pool(ctx, &map_k, a.K, a, D, box) && encode_pool(ctx, &map_v, a.V, a, D, box))) box = 0;
-  paged_attn_tc_kernel<D><<<ctx->sm_count, TC_THREADS, C::SMEM, st>>>(map_k, map_v, a, box);
-  FOCUS_CHECK_LAUNCH();
-  return FOCUS_OK;
+  return launch_chained(ctx, paged_attn_tc_kernel<D>, ctx->sm_count, TC_THREADS, C::SMEM, st, map_k, map_v, a, box);
 }
 
 }  // namespace
