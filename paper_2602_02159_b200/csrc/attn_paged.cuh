@@ -204,18 +204,31 @@ __device__ __forceinline__ bool arrive_last(int32_t* counter, int n) {
 template <typename T, int D, typename C, int NTH>
 __device__ __forceinline__ void finish_piece(const PagedArgs& a, int cta, int c0, int parts, int nq, uint8_t* smem, const Out<T, D>& out) {
   constexpr long long STRIDE = 2ll * C::PART;
-  float* all = a.part + (long long)c0 * STRIDE;                          // slot 0 of CTA c0; its own piece is in slot 1
-  if (parts <= C::JOIN_ONCE) {
-    if (arrive_last<NTH>(a.counters + 3 * c0, parts)) join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(all, STRIDE, C::PART, parts, nq, smem, out, nullptr);
-    return;
+  float* part = a.part + (long long)c0 * STRIDE;                         // slot 0 of CTA c0; its own piece is in slot 1
+  long long stride = STRIDE, extra = C::PART;
+  int n = parts, groups = 0;
+  int32_t* counter = a.counters + 3 * c0;
+  float* dst = nullptr;
+  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN;
+  if (parts > C::JOIN_ONCE) {            // this CTA's group first
+    groups = (parts + J - 1) / J;
+    const int lead = (cta - c0) / J * J;
+    part += lead * STRIDE;
+    if (lead > 0) { extra = 0; counter += 3 * lead + 1; }
+    n = min(J, parts - lead);
+    dst = part + extra;
   }
-  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN, groups = (parts + J - 1) / J, lead = (cta - c0) / J * J;
-  float* from = all + lead * STRIDE;
-  const long long extra = lead == 0 ? C::PART : 0;
-  if (!arrive_last<NTH>(a.counters + 3 * (c0 + lead) + (lead == 0 ? 0 : 1), min(J, parts - lead))) return;
-  join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(from, STRIDE, extra, min(J, parts - lead), nq, smem, out, from + extra);
-  if (arrive_last<NTH>(a.counters + 3 * c0 + 2, groups))
-    join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(all, J * STRIDE, C::PART, groups, nq, smem, out, nullptr);
+  while (true) {                         // one copy of the code: the second round finds it in the instruction cache
+    if (!arrive_last<NTH>(counter, n)) return;
+    join<T, D, C::HEAD, NTH, C::JOIN_SMEM>(part, stride, extra, n, nq, smem, out, dst);
+    if (!dst) return;
+    part = a.part + (long long)c0 * STRIDE;
+    stride = J * STRIDE;
+    extra = C::PART;
+    n = groups;
+    counter = a.counters + 3 * c0 + 2;
+    dst = nullptr;
+  }
 }
 
 // A CTA's share of the work: the total cost of the sequences, the CTAs that take part, this one's stretch [p0, p1) and the
