@@ -43,7 +43,7 @@ struct Cfg {
   static constexpr int O_PITCH = D + 4;                                   // floats, of a warp's partial in its ring
   static constexpr int HEAD = (2 * RT + 3) & ~3;                          // floats of a partial ahead of its rows (16-byte vectors)
   static constexpr int PART = HEAD + RT * D;                              // floats of one partial in the workspace
-  static constexpr int JOIN_ONCE = 2 * JOIN, JOIN_FEW = JOIN, JOIN_SMEM = 96 * 1024;   // see finish_piece
+  static constexpr int JOIN_ONCE = 16, JOIN_SMEM = 96 * 1024;   // pieces that are joined in one go, shared memory of a join
   static constexpr int CTAS = RING * PA_WARPS > 100 * 1024 ? 1 : 2;       // per SM
   static constexpr int OFF_Q = RING * PA_WARPS;
   static constexpr int OFF_P = OFF_Q + RT * Q_PITCH * (int)sizeof(T);     // fp32: numerators [warp][RT][KT]

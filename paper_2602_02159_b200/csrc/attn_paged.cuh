@@ -9,8 +9,7 @@
 namespace paged {
 
 constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
-constexpr int JOIN = 8;
-constexpr int MAX_GRID = 296;            // a join of its groups' partials has room for that many / JOIN
+constexpr int MAX_GRID = 296;            // so a segment has that many pieces at most, and a join 18 of them
 static_assert(3 * MAX_GRID <= FOCUS_N_COUNTERS, "three counters per CTA");
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -209,7 +208,8 @@ __device__ __forceinline__ void finish_piece(const PagedArgs& a, int cta, int c0
   int n = parts, groups = 0;
   int32_t* counter = a.counters + 3 * c0;
   float* dst = nullptr;
-  const int J = parts <= 4 * JOIN ? C::JOIN_FEW : JOIN;
+  int J = 2;                             // partials of a group: as many as there are groups
+  while (J * J < parts) ++J;
   if (parts > C::JOIN_ONCE) {            // this CTA's group first
     groups = (parts + J - 1) / J;
     const int lead = (cta - c0) / J * J;

@@ -39,7 +39,7 @@ struct TcCfg {
   static constexpr int OFF_MASK = OFF_BAR + ((N_BAR * 8 + 15) & ~15), OFF_TMEM = OFF_MASK + 4 * 16;
   static constexpr int SMEM = OFF_TMEM + 16 + 1024;                               // and alignment to 1024 bytes
   static constexpr int HEAD = 2 * TM, PART = HEAD + TM * D;
-  static constexpr int JOIN_ONCE = 12, JOIN_FEW = 4, JOIN_SMEM = OFF_BAR;
+  static constexpr int JOIN_ONCE = 12, JOIN_SMEM = OFF_BAR;
 };
 
 __device__ __forceinline__ long long tile_cost(const Seq& q) { return (q.len + TN - 1) / TN + TILE_SEG_COST; }
