@@ -6,11 +6,11 @@
 // would save an instruction, and overflow for logits near the end of the range).  Threads' sums are fp32 over a few hundred
 // logits, joined in fp32, in a fixed order.
 //
-// Top tokens.  A thread remembers its maximum and the run of vectors where it first met it.  Of 64 groups of threads the n-th
-// largest such pair is a lower bound of the n-th largest logit that few more logits reach (20 of 64: 24 on average); only the
-// threads whose maximum reaches it have any, and the CTA looks their runs through again, one per thread.  The list is
-// ordered by counting, per logit, those ahead of it.  A list that overflows (more than LP_LIST logits above the bound,
-// which takes logits that repeat with the threads' stride) is replaced by n searches for the next largest.
+// Top tokens.  A thread remembers its maximum and the run of vectors where it first met it.  Of 64 groups of threads (tid modulo
+// 64) the n-th largest such pair is a lower bound of the n-th largest logit that few more logits reach (20 of 64: 24 on
+// average); only the threads whose maximum reaches it have any, and the CTA looks their runs through again, one per thread.
+// The list is ordered by counting, per logit, those ahead of it.  A list that overflows (more than LP_LIST logits above the
+// bound, which takes logits that repeat with the threads' stride) is replaced by n searches for the next largest.
 //
 // A row belongs to one CTA where there are many, else to a cluster of up to eight, whose first CTA joins what the others
 // put into its shared memory.  What bounds it: 512 rows of 126464 bf16 logits with 20 alternatives take 42 us, of which HBM
@@ -27,7 +27,7 @@ constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 constexpr int LP_GROUPS = 64, LP_PER_GROUP = LP_THREADS / LP_GROUPS;
 constexpr int LP_MAX_CLUSTER = 8, LP_MAX_TOP = 32;
 constexpr int LP_LIST = 1024;
-constexpr int LP_UNROLL = 4;             // vectors in flight per thread
+constexpr int LP_UNROLL = 4;             // vectors of a run in a long row
 constexpr float LP_FLOOR = -1.0e4f;      // exponents end here: weight 0, and 0 times it is 0 (NaN and -inf logits too)
 
 struct LpParams {
@@ -182,15 +182,16 @@ template <> struct Vec<float> {
   }
 };
 
-// run v of a row: LP_UNROLL neighbouring vectors, -inf beyond the row's end
-template <typename T>
-__device__ __forceinline__ void load_run(const T* row, int v, int vocab, uint4 (&r)[LP_UNROLL]) {
-  if ((v + 1) * (LP_UNROLL * Vec<T>::EPC) <= vocab) {
-    const uint4* at = reinterpret_cast<const uint4*>(row) + (long long)v * LP_UNROLL;
+// run v of a row: U neighbouring vectors, -inf beyond the row's end
+template <typename T, int U>
+__device__ __forceinline__ void load_run(const T* row, int v, int vocab, uint4 (&r)[U]) {
+  if ((v + 1) * (U * Vec<T>::EPC) <= vocab) {
+    const uint4* at = reinterpret_cast<const uint4*>(row) + (long long)v * U;
 #pragma unroll
-    for (int u = 0; u < LP_UNROLL; ++u) r[u] = __ldg(at + u);
+    for (int u = 0; u < U; ++u) r[u] = __ldg(at + u);
   } else {
-    for (int u = 0; u < LP_UNROLL; ++u) Vec<T>::load(row, v * LP_UNROLL + u, vocab, r[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) Vec<T>::load(row, v * U + u, vocab, r[u]);
   }
 }
 
@@ -214,12 +215,13 @@ __device__ __forceinline__ void put_far(uint32_t addr, unsigned long long v) {
 }
 
 // grid: clusters of `cl` CTAs, one per row
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpParams p, const int cl) {
   constexpr int EPC = Vec<T>::EPC;
   __shared__ LpShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int q = cl > 1 ? (int)cluster_rank() : 0, r = blockIdx.x / cl;
+  if (tid == 0) sh.list_n = sh.owners = 0;
   if (cl > 1) cluster_arrive();          // a CTA's shared memory may be written once it has started
   const int n = p.rows ? min(max(*p.n_rows, 0), p.max_rows) : p.max_rows;
   const int pos = r < n ? (p.rows ? p.rows[r] : p.pos_base + r) : -1;
@@ -227,13 +229,12 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
   const int t = live && p.given ? p.given[r] : -1;
   const bool scored = t >= 0 && t < p.vocab;
   if (q == 0 && tid == 0 && ((r < n && !live) || (live && !scored && t != -1))) set_status(p.status, FOCUS_ERR_INVALID_ARG);
-  if (tid == 0) sh.list_n = sh.owners = 0;
 
-  // ---- the pass: runs v0 + tid, + LP_THREADS, ... of this CTA's slice, a run being LP_UNROLL neighbouring vectors
+  // ---- the pass: runs v0 + tid, + LP_THREADS, ... of this CTA's slice, a run being U neighbouring vectors
   Sums a = {-INFINITY, 0.f, 0.f};
   int n_inf = 0, ahead = 0;
   const T* row = (const T*)p.logits + (long long)(live ? pos - p.pos_base : 0) * p.row_stride;
-  constexpr int RUN = EPC * LP_UNROLL;
+  constexpr int RUN = EPC * U;
   const int runs = live ? (p.vocab + RUN - 1) / RUN : 0, per = (runs + cl - 1) / cl;
   const int v0 = min(q * per, runs), v1 = min(v0 + per, runs);
   float xt = scored ? load_as_float(row + t) : 0.f;
@@ -241,15 +242,15 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
   const bool low = xt == -INFINITY;      // then every token before t is ahead of it: added at the end
   const int tv = t / RUN;
   int first = v0 + tid;                  // the run that holds the maximum
-  static_assert(LP_UNROLL == 4, "the selection above the clamped loop");
+  static_assert(U <= 4, "the selection ahead of the clamped exponents");
   float floor = -INFINITY;               // logits below it have no weight: as far under the maximum as LP_FLOOR says
   float2 z2 = {0.f, 0.f}, s2 = {0.f, 0.f};                             // a.z and a.s, for the even and the odd logits
-  uint4 next[LP_UNROLL];
+  uint4 next[U];
   if (v0 + tid < v1) load_run(row, v0 + tid, p.vocab, next);
   for (int v = v0 + tid; v < v1; v += LP_THREADS) {
-    uint4 raw[LP_UNROLL];
+    uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < LP_UNROLL; ++u) raw[u] = next[u];
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
     if (v + LP_THREADS < v1) load_run(row, v + LP_THREADS, p.vocab, next);
     const float top = Vec<T>::largest(raw);
     if (top > a.m) {
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
         ahead += Vec<T>::template ahead<false>(raw, xt);
       } else {
 #pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u) {
+        for (int u = 0; u < U; ++u) {
           float x[EPC];
           Vec<T>::floats(raw[u], x);
 #pragma unroll
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
     }
     if (top == INFINITY) {
 #pragma unroll
-      for (int u = 0; u < LP_UNROLL; ++u) {
+      for (int u = 0; u < U; ++u) {
         float x[EPC];
         Vec<T>::floats(raw[u], x);
 #pragma unroll
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
     }
     if (floor > -3.3e38f) {
 #pragma unroll
-      for (int u = 0; u < LP_UNROLL; ++u) {
+      for (int u = 0; u < U; ++u) {
         float x[EPC];
         Vec<T>::raise(raw[u], floor);
         Vec<T>::floats(raw[u], x);
@@ -303,9 +304,9 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
       }
     } else if (a.m > -INFINITY) {        // nothing finite lies that far under the maximum: exponents are clamped one by one
 #pragma unroll 1
-      for (int u = 0; u < LP_UNROLL; ++u) {
+      for (int u = 0; u < U; ++u) {
         float x[EPC];
-        Vec<T>::floats(u == 0 ? raw[0] : u == 1 ? raw[1] : u == 2 ? raw[2] : raw[3], x);
+        Vec<T>::floats(u == 0 ? raw[0] : u == 1 ? raw[1 % U] : u == 2 ? raw[2 % U] : raw[3 % U], x);
 #pragma unroll
         for (int e = 0; e < EPC; ++e) {
           const float d = fmaxf((x[e] - a.m) * p.k, LP_FLOOR), w = ex2(d);
@@ -348,11 +349,10 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
   // ---- top tokens of the slice
   if (p.n_top > 0) {
     const unsigned long long mine = first < v1 ? order_key(a.m, (uint32_t)first) : 0ull;
-    unsigned long long g = mine;
-#pragma unroll
-    for (int d = 1; d < LP_PER_GROUP; d <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, d));
-    if (tid % LP_PER_GROUP == 0) sh.group[tid / LP_PER_GROUP] = g;
+    if (tid < LP_GROUPS) sh.group[tid] = 0ull;
     if (tid == 0) sh.bound = 0ull;
+    __syncthreads();
+    if (mine != 0ull) atomicMax(&sh.group[tid % LP_GROUPS], mine);                    // a maximum does not depend on the order
     __syncthreads();
     {                                    // LP_PER_GROUP threads count for one group
       const unsigned long long own = sh.group[tid / LP_PER_GROUP];
@@ -373,11 +373,11 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
     for (int i = tid; i < all; i += LP_THREADS) {
       const int at = v0 + sh.owner[i / trips] + i % trips * LP_THREADS;
       if (at >= v1) continue;
-      uint4 raw[LP_UNROLL];
+      uint4 raw[U];
       load_run(row, at, p.vocab, raw);
       if (order_key(Vec<T>::largest(raw), (uint32_t)at) < bound) continue;
 #pragma unroll
-      for (int u = 0; u < LP_UNROLL; ++u) {
+      for (int u = 0; u < U; ++u) {
         float x[EPC];
         Vec<T>::floats(raw[u], x);
 #pragma unroll
@@ -402,6 +402,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
         const int i = i0 + tid / 4;
         const unsigned long long own = i < listed ? sh.list[i] : 0ull;
         int before = 0;
+#pragma unroll 4
         for (int j = tid % 4; j < listed; j += 4) before += sh.list[j] > own;
         before += __shfl_xor_sync(0xffffffffu, before, 1);
         before += __shfl_xor_sync(0xffffffffu, before, 2);
@@ -413,10 +414,10 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
       for (int i = 0; i < p.n_top; ++i) {
         unsigned long long best = 0ull;
         for (int v = v0 + tid; v < v1; v += LP_THREADS) {
-          uint4 raw[LP_UNROLL];
+          uint4 raw[U];
           load_run(row, v, p.vocab, raw);
 #pragma unroll
-          for (int u = 0; u < LP_UNROLL; ++u) {
+          for (int u = 0; u < U; ++u) {
             float x[EPC];
             Vec<T>::floats(raw[u], x);
 #pragma unroll
@@ -489,9 +490,11 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
     const int have = some ? min(p.n_top, p.vocab) : 0, all = cl * p.n_top;
     for (int i = tid; i < all; i += LP_THREADS) {
       const unsigned long long own = sh.top[i];
-      int before = 0;
-      if (cl == 1) before = i;
-      else for (int j = 0; j < all; ++j) before += sh.top[j] > own;
+      int before = cl == 1 ? i : 0;
+      if (cl > 1) {
+#pragma unroll 8
+        for (int j = 0; j < all; ++j) before += sh.top[j] > own;
+      }
       if (own == 0ull || before >= have) continue;
       const float x = key_to_float((uint32_t)(own >> 32));
       double z = ((double)x - (double)sh.m) / (double)p.temperature;
@@ -531,10 +534,13 @@ extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits,
   const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, LP_FLOOR / k, given, logprob,
                       rank, entropy, top_token, top_logprob, ctx->d_status};
   // CTAs per row: until there are three per SM (512 rows of 126464 in one CTA each 42 us, in two 44: fewer ends to rows) or a
-  // thread would have no run of its own
+  // thread would have no run of its own, which its group needs for the tops
   const int runs = vocab / (dtype == FOCUS_BF16 ? 8 * LP_UNROLL : 4 * LP_UNROLL);
+  // short rows: runs of one vector, so that there are more groups of threads than tops to bound, or so few logits (32 groups of
+  // four vectors: 1024) that all are listed
+  const bool wide = runs >= LP_THREADS;
   int cl = 1;
-  while (cl < LP_MAX_CLUSTER && (long long)max_rows * cl < 3ll * ctx->sm_count && runs >= cl * LP_THREADS) cl *= 2;
+  while (cl < LP_MAX_CLUSTER && (long long)max_rows * cl < 3ll * ctx->sm_count && runs >= 2 * cl * LP_THREADS) cl *= 2;
   if ((long long)max_rows * cl > 0x7fffffffll) return FOCUS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(max_rows * cl));
@@ -545,8 +551,10 @@ extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits,
   attr.val.clusterDim.x = (unsigned)cl; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = cl > 1 ? 1 : 0;
-  if (dtype == FOCUS_BF16) cudaLaunchKernelEx(&cfg, token_logprobs_kernel<__nv_bfloat16>, p, cl);
-  else cudaLaunchKernelEx(&cfg, token_logprobs_kernel<float>, p, cl);
+  if (dtype == FOCUS_BF16)
+    cudaLaunchKernelEx(&cfg, wide ? token_logprobs_kernel<__nv_bfloat16, LP_UNROLL> : token_logprobs_kernel<__nv_bfloat16, 1>, p, cl);
+  else
+    cudaLaunchKernelEx(&cfg, wide ? token_logprobs_kernel<float, LP_UNROLL> : token_logprobs_kernel<float, 1>, p, cl);
   FOCUS_CHECK_LAUNCH();
   return FOCUS_OK;
 }

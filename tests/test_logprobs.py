@@ -104,7 +104,8 @@ def logits(rng, n, vocab, dtype, spread=3.0):
 @gpu
 @pytest.mark.parametrize("dtype,vocab,n,T,n_top", [
     ("bf16", 1, 2, 1.0, 3), ("f32", 7, 3, 0.7, 5), ("bf16", 33, 4, 1.0, 32), ("f32", 257, 5, 1.3, 1), ("bf16", 1000, 40, 0.8, 20),
-    ("f32", 1025, 7, 1.0, 32), ("bf16", 2049, 3, 1.0, 0), ("bf16", 32001, 9, 0.5, 20), ("f32", 50257, 2, 1.0, 5),
+    ("f32", 1025, 7, 1.0, 32), ("bf16", 2049, 3, 1.0, 0), ("bf16", 255, 3, 1.0, 32), ("bf16", 521, 3, 1.0, 32), ("bf16", 3000, 5, 1.0, 32),
+    ("f32", 4095, 3, 1.0, 32), ("bf16", 8191, 2, 1.0, 32), ("bf16", 8192, 2, 1.0, 32), ("f32", 4097, 2, 1.0, 20), ("bf16", 32001, 9, 0.5, 20), ("f32", 50257, 2, 1.0, 5),
     ("bf16", 126464, 3, 1.0, 32), ("f32", 151643, 1, 2.0, 20), ("bf16", 8200, 900, 1.0, 8)])
 def test_scores_of_tokens(ctx, dtype, vocab, n, T, n_top):
     rng = np.random.default_rng(vocab + n)
