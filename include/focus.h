@@ -25,8 +25,8 @@
  *     these kernels may have written (outputs, lists, workspace).  A kernel of another library placed after a call
  *     sees complete results.  Ahead of that wait these kernels read only inputs that none of them writes:
  *     focus_sparse_layer reads Q, the focus and sink index lists, the pooled keys and the sinks' K/V rows there,
- *     its attention kernel the row list and Q; focus_dense_attn, focus_sparse_attn and their _quantized forms read
- *     nothing ahead of it.
+ *     its attention kernel the row list and Q; focus_dense_attn, focus_sparse_attn, their _quantized forms and
+ *     focus_paged_attn read nothing ahead of it.
  *     Such an input is complete if its producer finished before the call's predecessor in the stream started, or if
  *     the producer is a kernel of this library (those make their outputs visible before they exit).  An input
  *     written by a foreign kernel that runs immediately before a focus_sparse_layer call, with nothing in between
@@ -484,7 +484,7 @@ focus_status focus_commit_step(focus_ctx* ctx, const float* conf_new, const int3
  *              Beyond the vocabulary: -1 and -inf
  * logits, rows and layout as for focus_confidence.  Rows beyond n_rows get logprob 0, rank -1, entropy 0, top_token -1,
  * top_logprob 0; so does a row without a finite or +inf logit, and a row whose position is out of range, which is reported.
- * Requires temperature > 0 (finite).  logprob and entropy are off by fp32 rounding of the weights (2^-21 of Z) and of the
+ * Requires temperature > 0 (10^-7 to 10^30), vocab at most 2^30.  logprob and entropy are off by fp32 rounding of the weights (2^-21 of Z) and of the
  * result.  One launch, no workspace. */
 focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits, int32_t dtype, int64_t row_stride, int32_t vocab,
                                   int32_t pos_base, int32_t n_pos, const int32_t* rows, const int32_t* n_rows,
@@ -512,7 +512,7 @@ focus_status focus_rope_from_frequencies(focus_rope* rope, int32_t rot_dim, int3
  *   positions  int32[max_rows] with n_rows int32[1] (device), or both NULL: row r is at pos_base + r.  Negative positions
  *              are reported and their rows left as they were, as are rows beyond n_rows.
  * Angles, sines and products are fp32; the result is rounded once.  Errors: INVALID_ARG, UNSUPPORTED (head_dim; a rot_dim
- * above head_dim). */
+ * above head_dim; more than 2^30 rows). */
 focus_status focus_rotate(focus_ctx* ctx, const focus_rope* rope, int32_t direction, const void* X, void* Y, int32_t dtype,
                           int32_t n_heads, int32_t head_dim, int64_t x_stride_row, int64_t x_stride_head,
                           int64_t y_stride_row, int64_t y_stride_head, int32_t pos_base, const int32_t* positions,
@@ -542,7 +542,9 @@ focus_status focus_append_kv_paged(focus_ctx* ctx, const focus_shape* shape, con
  * A row of a sequence without tokens gives O = 0 and lse = -inf.  What the pools hold outside the sequences' tokens has no
  * effect, NaN included.  bf16: tensor-core products, numerators rounded to bf16 (2^-8 of each at
  * most), sums fp32; fp32: fp32
- * products.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL (needs focus_paged_attn_workspace_bytes).  One launch. */
+ * products.  Sequences may have different numbers of rows; which kernel runs goes by their average (one to 32 stacked rows, that
+ * is rows times n_q_heads / n_kv_heads, or more), the result does not.  Errors: INVALID_ARG, UNSUPPORTED (head_dim, L above
+ * 2^30, max_rows * n_q_heads above 2^30), WORKSPACE_TOO_SMALL (needs focus_paged_attn_workspace_bytes).  One launch. */
 focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shape, const void* Q, const int32_t* row_start,
                               int32_t max_rows, const focus_paged_cache* cache, void* O, float* lse, focus_stream stream);
 /* Upper bound of the scratch that focus_paged_attn needs on the context's device for this shape, whatever the lengths. */

@@ -526,8 +526,8 @@ extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits,
   if (n_top < 0 || (n_top > 0) != (top_token != nullptr) || (n_top > 0) != (top_logprob != nullptr)) return FOCUS_ERR_INVALID_ARG;
   if ((given == nullptr) != (logprob == nullptr) || (rank && !given)) return FOCUS_ERR_INVALID_ARG;
   if (!logprob && !entropy && n_top == 0) return FOCUS_ERR_INVALID_ARG;
-  const float k = (float)(1.4426950408889634 / (double)temperature);
-  if (n_top > LP_MAX_TOP || !isfinite(k) || k < 1e-30f) return FOCUS_ERR_UNSUPPORTED;
+  const float k = (float)(1.4426950408889634 / (double)temperature);     // from 1e-7 on, k times the spacing of any logits is finite
+  if (n_top > LP_MAX_TOP || temperature < 1e-7f || temperature > 1e30f || vocab > 1 << 30) return FOCUS_ERR_UNSUPPORTED;
   if (max_rows == 0) return FOCUS_OK;
   const DeviceGuard guard(ctx);
   if (!guard.ok) return FOCUS_ERR_CUDA;

@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(RT_THREADS, 6) turn_rows_kernel(const __grid_c
 }
 
 focus_status launch_turn(focus_ctx* ctx, TurnArgs& a, int dtype, bool append, cudaStream_t st) {
+  if (a.max_rows > 1 << 30) return FOCUS_ERR_UNSUPPORTED;                // row numbers with a block's rows on top fit 32 bits
   const DeviceGuard guard(ctx);
   if (!guard.ok) return FOCUS_ERR_CUDA;
   a.status = ctx->d_status;

@@ -45,7 +45,8 @@ def test_refusals_need_no_device():
                 dict(tlp=None), dict(given=None, lp=None, rank=None, ent=None, n_top=0, tok=None, tlp=None),
                 dict(dt=fb.F32, stride=1002)):
         assert call(**bad) == fb.ERR_INVALID_ARG, bad
-    assert call(n_top=33) == fb.ERR_UNSUPPORTED and call(T=1e-39) == fb.ERR_UNSUPPORTED and call(max_rows=0) == fb.OK
+    assert call(n_top=33) == fb.ERR_UNSUPPORTED and call(T=9e-8) == fb.ERR_UNSUPPORTED and call(T=1e35) == fb.ERR_UNSUPPORTED and call(max_rows=0) == fb.OK
+    assert call(vocab=2 ** 30 + 8, stride=2 ** 30 + 8) == fb.ERR_UNSUPPORTED
 
 
 def run(ctx, x, dtype, vocab, T, given, n_top, rows=None, max_rows=None, pos_base=0, use=("logprob", "rank", "entropy")):
@@ -190,7 +191,8 @@ def test_a_list_that_overflows_is_searched(ctx):
 @gpu
 def test_large_logits_and_temperatures(ctx):
     rng = np.random.default_rng(3)
-    for dtype, spread, T in (("f32", 1e4, 1.0), ("bf16", 2e3, 100.0), ("f32", 3.0, 0.01), ("f32", 3.0, 1e4), ("f32", 1e30, 1e29)):
+    for dtype, spread, T in (("f32", 1e4, 1.0), ("bf16", 2e3, 100.0), ("f32", 3.0, 0.01), ("f32", 3.0, 1e4), ("f32", 1e30, 1e29), ("f32", 1e36, 2e-7),
+                             ("bf16", 1e3, 1e-3)):
         x = logits(rng, 6, 5001, dtype, spread)
         given = rng.integers(0, 5001, 6)
         check(run(ctx, x, dtype, 5001, T, given, 10), x, 5001, T, given, 10)

@@ -154,6 +154,10 @@ def test_refusals_need_no_device(lib):
     assert append(rope=wide) == fb.ERR_UNSUPPORTED
     for bad in (dict(Q=None), dict(O=None), dict(Q=P + 8), dict(O=P + 8), dict(lse=P + 2)):
         assert attend(**bad) == fb.ERR_INVALID_ARG, bad
+    assert rotate(rows=2 ** 30 + 1) == fb.ERR_UNSUPPORTED and append(rows=2 ** 30 + 1) == fb.ERR_UNSUPPORTED
+    assert attend(rows=2 ** 28 + 1) == fb.ERR_UNSUPPORTED                                    # 4 heads
+    far = fb.make_shape(2 ** 30 + 1, 0, 4, 2, 64, 64, fb.BF16)
+    assert attend(shape=far, c=cache(wide=2 ** 27)) == fb.ERR_UNSUPPORTED
     out = ctypes.c_size_t(0)
     assert lib.focus_paged_attn_workspace_bytes(None, B(sh), ctypes.byref(out)) == fb.ERR_INVALID_ARG
     assert lib.focus_paged_attn_workspace_bytes(h, B(sh), None) == fb.ERR_INVALID_ARG
