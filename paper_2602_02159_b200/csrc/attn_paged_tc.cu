@@ -27,7 +27,7 @@ namespace {
 constexpr int TM = 128, TN = 128;        // rows and keys of a tile
 constexpr int SLOTS = 4, LAG = 2;        // operand slots; loads that a producer has in flight behind the latest
 constexpr int TC_THREADS = 256, PRODUCERS = 64;
-constexpr int TILE_SEG_COST = 5;         // price of a segment beside its tiles, in tiles (six ragged windows 52 us, 66 with 3)
+constexpr int TILE_SEG_COST = 6;         // price of a segment beside its tiles, in tiles (six ragged windows 53 us, 66 with 3)
 constexpr int TILE_MIN_COST = 4;         // least cost per CTA
 constexpr float RESCALE = 8.f;
 
@@ -39,7 +39,7 @@ struct TcCfg {
   static constexpr int OFF_MASK = OFF_BAR + ((N_BAR * 8 + 15) & ~15), OFF_TMEM = OFF_MASK + 4 * 16;
   static constexpr int SMEM = OFF_TMEM + 16 + 1024;                               // and alignment to 1024 bytes
   static constexpr int HEAD = 2 * TM, PART = HEAD + TM * D;
-  static constexpr int JOIN_ONCE = 12, JOIN_SMEM = OFF_BAR;
+  static constexpr int JOIN_ONCE = 6, JOIN_SMEM = OFF_BAR;
 };
 
 __device__ __forceinline__ long long tile_cost(const Seq& q) { return (q.len + TN - 1) / TN + TILE_SEG_COST; }
@@ -174,28 +174,27 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     while (ok && next_segment(a, w, g, [](const Segment&) {})) {
       note(g);
       const int nt = g.t_hi - g.t_lo, key0 = g.t_lo * TN + warp * 64 + lane;
-      // of this lane's two keys in the tiles of either parity: their pages, and the places in the pools
+      // the pages of this lane's two keys in the tile to come and in the tiles of either parity
       int page[2] = {key_page(a, g.s, key0, g.len), key_page(a, g.s, key0 + 32, g.len)}, page_even[2] = {-1, -1}, page_odd[2] = {-1, -1};
       for (int q = 0; q < 2 * nt; ++q) {
         bool value;
         const int i = load_tile_of(q, nt, value);
         int now[2];
-        long long at[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int j = key0 + i * TN + x * 32;
           if (!value) {
             now[x] = page[x];
             if (i & 1) page_odd[x] = now[x]; else page_even[x] = now[x];
-            page[x] = key_page(a, g.s, j + TN, g.len);
+            page[x] = key_page(a, g.s, key0 + (i + 1) * TN + x * 32, g.len);
           } else {
             now[x] = i & 1 ? page_odd[x] : page_even[x];
           }
-          at[x] = key_offset(a, j, g.len, now[x]);
         }
         if (!__all_sync(0xffffffffu, mbar_wait(bar_empty(slot), (round & 1u) ^ 1u, abort_flag, a.status))) { ok = false; break; }
         if (!value) {
-          const uint32_t lo = __ballot_sync(0xffffffffu, at[0] >= 0), hi = __ballot_sync(0xffffffffu, at[1] >= 0);
+          const bool in0 = (uint32_t)now[0] < (uint32_t)a.n_pages, in1 = (uint32_t)now[1] < (uint32_t)a.n_pages;
+          const uint32_t lo = __ballot_sync(0xffffffffu, in0), hi = __ballot_sync(0xffffffffu, in1);
+          if ((!in0 && key0 + i * TN < g.len) || (!in1 && key0 + i * TN + 32 < g.len)) set_status(a.status, FOCUS_ERR_INVALID_ARG);
           if (lane == 0) {
             masks[(tile & 3) * 4 + warp * 2] = lo;
             masks[(tile & 3) * 4 + warp * 2 + 1] = hi;
@@ -222,6 +221,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
           }
         } else {
           const T* src = (value ? (const T*)a.V : (const T*)a.K) + (long long)g.g * a.st_head;
+          const long long at[2] = {key_offset(a, key0 + i * TN, g.len, now[0]), key_offset(a, key0 + i * TN + 32, g.len, now[1])};
           const int c = lane % CPR;
 #pragma unroll
           for (int x = 0; x < 2 * CPR; ++x) {                            // 32 / CPR rows at a time
