@@ -9,8 +9,8 @@
 // tiles.  Lengths are on the device, so the split is made there: every CTA sums the segments' costs (tiles + SEG_COST, the
 // price of filling and draining the pipeline), and CTA c of G takes the stretch [c T / G, (c + 1) T / G) of the total T.
 // A stretch covers whole segments and pieces of at most two: those leave (max, sum, unnormalised O) in the workspace, and
-// the CTA that arrives last at the segment's counter joins them in CTA order (in groups of JOIN, then the groups' results,
-// where there are more than 2 JOIN), so results do not depend on timing.
+// the CTA that arrives last at the segment's counter joins them in CTA order (in groups of the square root of their number,
+// then the groups' results, where there are more than JOIN_ONCE), so results do not depend on timing.
 //
 // CTA: four warps, each on its own tiles (w, w + 4, ...) through a ring of its own, filled by 16-byte cp.async with the
 // page looked up per key (any page size), no barrier inside a segment.  Two CTAs per SM (fp32 with 128 columns: one) cover
@@ -21,6 +21,11 @@
 // M = 128 keys per instruction and its scores come back through TMEM: latency, where bytes are the bound.)  A tile's row
 // statistics are shuffles over the lanes that hold its keys; P^T becomes the B operand by movmatrix.
 // fp32: fp32 products on the CUDA cores, a lane per key (and half row) for the scores, per column for the values.
+//
+// Measured, bf16, heads of 128: 64 sequences of 164 to 16384 tokens, 32/8 heads: 160 us (6.6 TB/s, the rate of a copy; 178
+// before segments were priced by what their ends cost); 4 x 16384 tokens, 32 heads: 165 us (6.5 TB/s); one token at 32768, 28/4
+// heads: 23 us for 10.4 at that rate (2.5 until the first key is asked for, 10 of stream, 1.5 to join warps, 9 to join 74
+// pieces).  fp32, 5 sequences to 1024 tokens, 8 heads of 64: 9.7 us, a chain of latencies.
 #include "attn_paged.cuh"
 
 using namespace paged;
@@ -31,7 +36,6 @@ constexpr int KT = 16;                   // keys per tile
 constexpr int SEG_COST = 24;             // cost of a segment beside its tiles, in tiles: a ragged batch of 64 takes 163 us, 175 with 6
 constexpr int MIN_COST = 10;             // least cost per CTA: below, joining costs more than sharing gains
 constexpr float LAZY = 8.f;              // the running maximum may lag by this much (base 2): numerators stay below 2^8
-
 
 template <typename T, int D, int NT>
 struct Cfg {
@@ -553,6 +557,7 @@ extern "C" focus_status focus_paged_attn(focus_ctx* ctx, const focus_shape* shap
   ctx->last_attn_variant = 6;
   if (rows <= 8) return FOCUS_PA_LAUNCH(__nv_bfloat16, 1, 6);
   if (rows <= 16) return FOCUS_PA_LAUNCH(__nv_bfloat16, 2, 8);
+  // more rows: attn_paged_tc.cu, where both sides are measured
   if (rows <= 32 || !paged_attn_tc_supported(ctx)) return FOCUS_PA_LAUNCH(__nv_bfloat16, 4, 10);
   ctx->last_attn_variant = 8;
   return launch_paged_attn_tc(ctx, a, shape->head_dim, stream);

@@ -13,9 +13,13 @@
 // Queries of the next segment are staged as soon as the last scores of this one are there, before its O is written out.
 // Pieces of segments are joined when the CTA's stretch is done and the slots are free.
 //
-// What bounds it: the softmax of a tile, one row per thread, about 1.2 us per 128 keys (64 KB of K and V, HBM's rate per SM).
-// On the mma.sync kernel of attn_paged.cu, which reads K and V once per 32 rows, the same windows are held by its MMAs: an
-// m16n8k16 per 8 cycles and SM sub-partition at best, half of that reached.
+// What bounds it: the softmax of a tile, one row per thread, 1.2 to 1.6 us per 128 keys (64 KB of K and V take 1.5 at HBM's rate),
+// and what a stretch costs beside its tiles: 7 us until the first scores, 2 to write O, 2 to 10 to join pieces.  72 rows of 32
+// heads over 32768 tokens: 102 us (5.3 TB/s); 4 x 600 rows, 28/4 heads, over 8192: 352 us (0.8 PFLOP/s); six ragged windows of 3
+// to 33 rows over 212 to 16384 tokens: 53 us.  The mma.sync kernel of attn_paged.cu takes 263, 1096 and 71 for these: its MMAs
+// (an m16n8k16 per 8 cycles and SM sub-partition at best) and its reading K and V once per 32 rows; with 32 stacked rows it is
+// ahead (64 sequences of 2048 tokens, 100 against 139 us), with 36 behind (184 against 140), hence the rule.  Joining pieces in
+// a second kernel was measured slower (102 -> 119 us).
 #include "attn_paged.cuh"
 #include "tc_common.cuh"
 

@@ -215,3 +215,28 @@ def test_pages_give_what_the_contiguous_cache_gives(ctx):
     assert (O.float() - O2.float()).abs().max().item() <= 4 * BF16_HALF * x[:, H + HKV:].float().abs().max().item()
     assert (lse - lse2).abs().max().item() < 1e-3
     assert math.isfinite(float(O.float().sum())) and ctx.poll_status() == 0
+
+
+@gpu
+def test_the_readmes_paged_example_runs_as_printed(ctx):
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = [c for c in re.findall(r"```python\n(.*?)```", text, flags=re.S) if "focus_paged_attn" in c][0]
+    marker = "# ... page_table"
+    head, tail = code.split(marker, 1)
+    env = dict(torch=torch, fb=fb, ctx=ctx, H=8, Hkv=2, d=64, B=64, vocab=1000)
+    exec(head, env)
+    n, wide = env["n"], env["wide"]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    env["page_table"] = torch.randperm(env["n_pages"], device="cuda")[:n * wide].int().reshape(n, wide)
+    env["kv_len"] = torch.tensor([5, 1, 700], **i32)
+    env["qkv"] = torch.randn(n, 12 * 64, device="cuda").bfloat16()
+    env["logits"] = torch.randn(n, 1000, device="cuda").bfloat16()
+    env["token"], env["rank"], env["top_token"] = (torch.zeros(n, **i32), torch.zeros(n, **i32), torch.zeros(n, 20, **i32))
+    env["logprob"], env["entropy"], env["top_logprob"] = (torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"),
+                                                          torch.zeros(n, 20, device="cuda"))
+    exec(tail.split("\n", 1)[1], env)
+    v = env["qkv"].view(n, 12, 64)[1, 10:].repeat_interleave(4, 0)           # the second sequence's only token is the new one
+    assert torch.equal(env["Op"][1], v) and (env["logprob"] < 0).all() and (env["top_token"] >= 0).all()
+    assert ctx.poll_status() == 0
