@@ -138,7 +138,8 @@ typedef struct {
  * through the status word: such a row is not written, such keys are not attended, such a length counts as L or 0.
  * New rows are packed: those of sequence s are the rows row_start[s] .. row_start[s + 1] - 1 (device, n_seqs + 1 entries,
  * not decreasing, within [0, max_rows]); row_start NULL: one new row per sequence, row s, and max_rows == n_seqs.  Rows
- * of outputs that belong to no sequence are left as they were. */
+ * of outputs that belong to no sequence are left as they were.  Table, lengths and row_start must not change while a call
+ * that reads them runs. */
 typedef struct {
   void* K; void* V;                                   /* pools (device), shape.dtype */
   int64_t stride_page, stride_tok, stride_head;
@@ -178,7 +179,8 @@ uint64_t focus_launch_count(void);
 int32_t focus_last_attn_variant(focus_ctx* ctx);
 
 /* Selects the attention implementation for bf16 inputs (head_dim 128 or 64): 0 = automatic (tensor-core
- * kernel where supported), 1 = force the generic SIMT kernels.  Returns the previous value. */
+ * kernel where supported), 1 = force the generic SIMT kernels (focus_paged_attn has none for bf16).  Returns the previous
+ * value. */
 int32_t focus_set_force_simt(focus_ctx* ctx, int32_t force);
 
 /* Launch options of the attention kernels (no counterpart in the paper): every one of them selects between

@@ -240,3 +240,34 @@ def test_the_readmes_paged_example_runs_as_printed(ctx):
     v = env["qkv"].view(n, 12, 64)[1, 10:].repeat_interleave(4, 0)           # the second sequence's only token is the new one
     assert torch.equal(env["Op"][1], v) and (env["logprob"] < 0).all() and (env["top_token"] >= 0).all()
     assert ctx.poll_status() == 0
+
+
+@gpu
+def test_first_calls_of_a_context_may_be_captured(ctx):
+    """A context whose calls have not run yet: append, both forms of attention and scores captured, then replayed."""
+    m, fresh = Model(2, 6), fb.Context(0)
+    m.kv_len.copy_(torch.tensor([100, 90], dtype=torch.int32))
+    x = m.qkv[torch.arange(190, device="cuda")].reshape(190, -1, D)
+    Q, O, lse = buffers(190)
+    Q1, O1, lse1 = buffers(2)
+    row_start = torch.tensor([0, 100, 190], dtype=torch.int32, device="cuda")
+    lp, tok = torch.zeros(2, device="cuda"), torch.tensor([3, 4], dtype=torch.int32, device="cuda")
+    logits = torch.randn(2, 1008, device="cuda").bfloat16()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        m.layer(fresh, x, Q, O, lse, row_start)
+        assert fresh.last_attn_variant() == 8
+        m.layer(fresh, x[99::90], Q1, O1, lse1)
+        assert fresh.last_attn_variant() == 6
+        fb.focus_token_logprobs(fresh, logits, fb.BF16, 1008, VOCAB, 0, 2, None, None, 2, 1.0, tok, lp)
+    for _ in range(3):
+        O.zero_(), O1.zero_(), lp.zero_()
+        g.replay()
+    seqs, pos = np.repeat([0, 1], (100, 90)), np.concatenate([np.arange(100), np.arange(90)])
+    tokens = [list(range(100)), list(range(100, 190))]
+    check_rows(m, tokens, pos, O, seqs)
+    check_rows(m, tokens, [99, 89], O1, [0, 1])
+    assert (lp < 0).all() and fresh.poll_status() == 0
+    fresh.close()
