@@ -542,8 +542,8 @@ focus_status focus_append_kv_paged(focus_ctx* ctx, const focus_shape* shape, con
  *   Q     [max_rows rows] by the shape's q strides, row r at [r * q_stride_row]
  *   O     [max_rows, H, d] contiguous, shape.dtype; lse float[H * max_rows] (lse[h * max_rows + r]) or NULL
  * A row of a sequence without tokens gives O = 0 and lse = -inf.  What the pools hold outside the sequences' tokens has no
- * effect, NaN included.  bf16: tensor-core products, numerators rounded to bf16 (2^-8 of each at
- * most), sums fp32; fp32: fp32
+ * effect, NaN included.  bf16: tensor-core products, numerators as two bf16 terms (2^-16 of each at most is lost) for up to 16
+ * stacked rows, as one (2^-8) for more, sums fp32; fp32: fp32
  * products.  Sequences may have different numbers of rows; which kernel runs goes by their average (one to 32 stacked rows, that
  * is rows times n_q_heads / n_kv_heads, or more), the result does not.  Errors: INVALID_ARG, UNSUPPORTED (head_dim, L above
  * 2^30, max_rows * n_q_heads above 2^30), WORKSPACE_TOO_SMALL (needs focus_paged_attn_workspace_bytes).  One launch. */

@@ -4,7 +4,8 @@
 Tolerances, in units of what is computed.  A stored element is off by half a step of its type (HALF, relative).  A turn is
 off by 2^-21 of |x1| + |x2|: the phase 2^-33 turns and 2^-26 by its conversion, cosine and sine 2 units in the last place,
 product and sum 2^-24 each.  A logit, a sum of d fp32 products, is off by d 2^-24 of the sum of their magnitudes; a
-numerator by that (and 2^-20 for the exponential and the scale), and in bf16 by HALF more; an output by the numerators'
+numerator by that (and 2^-20 for the exponential and the scale), and in bf16 by HALF more, or 2^-16 where it is
+held in two terms (up to 16 stacked rows on average); an output by the numerators'
 error times sum w |v| (which also bounds the sums' errors, n 2^-24, in fp32) and HALF of itself."""
 import ctypes
 import math
@@ -409,7 +410,9 @@ def check_attention(c, n, Q, O, ls, H, scale):
         size = np.repeat(np.abs(keys), H // c.Hkv, axis=1)                   # [t, H, d]
         logit = np.einsum("rhd,thd->rht", np.abs(q[rows]), size).max(-1) * abs(scale)
         delta = logit * d * 2.0 ** -24 + 2.0 ** -20                          # [rows, H]
-        num = delta * 2 + (HALF["bf16"] if c.dtype == "bf16" else t * 2.0 ** -24)
+        stacked = -(-Q.shape[0] * (H // c.Hkv) // len(c.lengths))
+        held = t * 2.0 ** -24 + (0 if c.dtype == "f32" else 2.0 ** -16 if stacked <= 16 else HALF["bf16"])
+        num = delta * 2 + held
         assert (np.abs(got[rows] - want) <= num[..., None] * spread + HALF[c.dtype] * np.abs(want) + 1e-30).all(), s
         if ls is not None:
             assert (np.abs(f64(ls)[:, rows] - wl) <= delta.T * 2 + np.abs(wl) * 2.0 ** -22 + t * 2.0 ** -24).all(), s
