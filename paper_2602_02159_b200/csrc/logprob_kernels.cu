@@ -36,7 +36,7 @@ struct LpParams {
   int vocab, pos_base, n_pos, max_rows, n_top;
   const int32_t* rows;
   const int32_t* n_rows;
-  float temperature, k, reach;           // k = log2 e / temperature, reach = LP_FLOOR / k
+  float temperature, k, k_err, reach;    // k = log2 e / temperature, off by k_err of itself; reach = LP_FLOOR / k
   const int32_t* given;
   float* logprob;
   int32_t* rank;
@@ -94,16 +94,24 @@ __device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const f
   return r;
 }
 
-// sums of two shares, relative to the larger maximum (with an infinite one they mean nothing: such rows go by the number of
-// infinite logits)
-__device__ __forceinline__ void join(Sums& a, const Sums& o, float k) {
-  if (!(o.m > -INFINITY)) return;
-  if (!(a.m > -INFINITY)) { a = o; return; }
-  const float m = fmaxf(a.m, o.m), da = fmaxf((a.m - m) * k, LP_FLOOR), db = fmaxf((o.m - m) * k, LP_FLOOR);
-  const float fa = ex2(da), fb = ex2(db);
-  a.s = fa * fmaf(a.z, da, a.s) + fb * fmaf(o.z, db, o.s);
-  a.z = fa * a.z + fb * o.z;
+// A warp's shares relative to their largest maximum and added: every share is scaled once, since each approximate power would
+// leave its error, of one sign, in the sum.  (With an infinite maximum the sums mean nothing: such rows go by the number of
+// infinite logits.)
+__device__ __forceinline__ void join_warp(Sums& a, float k) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (a.m > -INFINITY) {
+    const float d = fmaxf((a.m - m) * k, LP_FLOOR), f = ex2(d);
+    a.s = f * fmaf(a.z, d, a.s);
+    a.z *= f;
+  }
   a.m = m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a.z += __shfl_xor_sync(0xffffffffu, a.z, d);
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
+  }
 }
 
 template <typename T> struct Vec;
@@ -323,14 +331,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
   {
     Sums w = a;
     int ni = n_inf, ah = ahead;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      Sums o;
-      o.m = __shfl_xor_sync(0xffffffffu, w.m, d);
-      o.z = __shfl_xor_sync(0xffffffffu, w.z, d);
-      o.s = __shfl_xor_sync(0xffffffffu, w.s, d);
-      join(w, o, p.k);
-    }
+    join_warp(w, p.k);
     ni = __reduce_add_sync(0xffffffffu, ni);
     ah = __reduce_add_sync(0xffffffffu, ah);
     if (cl > 1) cluster_wait();
@@ -453,26 +454,26 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const LpP
     const int parts = cl * LP_WARPS;
     Sums a = {-INFINITY, 0.f, 0.f};
     int ni = 0, ah = 0;
-    for (int i = lane; i < parts; i += 32) {
+    for (int i = lane; i < parts; i += 32) {                                          // two parts of a lane at most
       const Part& x = sh.part[i];
-      const Sums o = {x.m, x.z, x.s};
-      join(a, o, p.k);
+      const float m = fmaxf(a.m, x.m);
+      if (m > -INFINITY) {
+        const float da = fmaxf((a.m - m) * p.k, LP_FLOOR), dx = fmaxf((x.m - m) * p.k, LP_FLOOR), fa = ex2(da), fx = ex2(dx);
+        a.s = fa * fmaf(a.z, da, a.s) + fx * fmaf(x.z, dx, x.s);
+        a.z = fa * a.z + fx * x.z;
+        a.m = m;
+      }
       ni += x.n_inf;
       ah += x.ahead;
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      Sums o;
-      o.m = __shfl_xor_sync(0xffffffffu, a.m, d);
-      o.z = __shfl_xor_sync(0xffffffffu, a.z, d);
-      o.s = __shfl_xor_sync(0xffffffffu, a.s, d);
-      join(a, o, p.k);
-    }
+    join_warp(a, p.k);
     ni = __reduce_add_sync(0xffffffffu, ni);
     ah = __reduce_add_sync(0xffffffffu, ah);
     if (lane == 0) {
       const float m = a.m;
-      const double ln_z = log(ni > 0 ? (double)ni : (double)a.z), mean = ni > 0 ? 0.0 : (double)(a.s / a.z) * 0.69314718055994531;
+      // exponents were formed with the fp32 number next to k: to first order that moves ln Z by its error times their mean
+      const double mean = ni > 0 ? 0.0 : (double)(a.s / a.z) * 0.69314718055994531;
+      const double ln_z = log(ni > 0 ? (double)ni : (double)a.z) + (double)p.k_err * mean;
       const bool some = m > -INFINITY;   // else the row has no distribution
       sh.ln_z = ln_z;
       sh.m = m;
@@ -528,10 +529,11 @@ extern "C" focus_status focus_token_logprobs(focus_ctx* ctx, const void* logits,
   if (!logprob && !entropy && n_top == 0) return FOCUS_ERR_INVALID_ARG;
   const float k = (float)(1.4426950408889634 / (double)temperature);     // from 1e-7 on, k times the spacing of any logits is finite
   if (n_top > LP_MAX_TOP || temperature < 1e-7f || temperature > 1e30f || vocab > 1 << 30) return FOCUS_ERR_UNSUPPORTED;
+  const float k_err = (float)((1.4426950408889634 / (double)temperature - (double)k) / (double)k);
   if (max_rows == 0) return FOCUS_OK;
   const DeviceGuard guard(ctx);
   if (!guard.ok) return FOCUS_ERR_CUDA;
-  const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, LP_FLOOR / k, given, logprob,
+  const LpParams p = {logits, row_stride, vocab, pos_base, n_pos, max_rows, n_top, rows, n_rows, temperature, k, k_err, LP_FLOOR / k, given, logprob,
                       rank, entropy, top_token, top_logprob, ctx->d_status};
   // CTAs per row: until there are three per SM (512 rows of 126464 in one CTA each 42 us, in two 44: fewer ends to rows) or a
   // thread would have no run of its own, which its group needs for the tops
